@@ -10,6 +10,10 @@
  *   wq_reorder_quantize  window-level KV cache computation, prefill   (Sec. 3.3.1, Sec. 3.3.3, Alg. 2 first half)
  *   wq_decode_attention  ... and decoding over the mixed cache        (Alg. 2 second half, Sec. 3.3.2)
  *
+ * and, around them, what a serving program does with the same rows and caches: wq_rope and wq_rope_append_kv (rotary
+ * positions of the rows that are cached), wq_prefill_attention (attention of a prompt's rows before they are packed)
+ * and wq_decode_attention_shared (requests that ask about the same packed video).
+ *
  * Conventions
  *   - Every pointer named "dev" or documented as device memory is a HIP device pointer on the current
  *     device; every scalar and the structs themselves live on the host.  The library reads no device
@@ -74,6 +78,8 @@ typedef enum { WQ_F32 = 0, WQ_BF16 = 1, WQ_F16 = 2 } wq_dtype;
 typedef enum { WQ_OK = 0, WQ_ERR_ARG = -1, WQ_ERR_UNSUPPORTED = -2, WQ_ERR_HIP = -3, WQ_ERR_WORKSPACE = -4 } wq_status;
 typedef enum { WQ_SCORE_AUTO = 0, WQ_SCORE_PAIRWISE_MFMA = 1, WQ_SCORE_POOLED = 2 } wq_score_algo;
 typedef enum { WQ_MODE_QUOTA = 0, WQ_MODE_THRESHOLD = 1 } wq_assign_mode;
+typedef enum { WQ_ROPE_HALF = 0, WQ_ROPE_PAIRS = 1 } wq_rope_layout;
+typedef enum { WQ_ROPE_PLAIN = 0, WQ_ROPE_EVEN = 1, WQ_ROPE_BASE = 2, WQ_ROPE_PARTS = 3 } wq_rope_scaling;
 typedef enum { WQ_DECODE_AUTO = 0, WQ_DECODE_GENERIC = 1, WQ_DECODE_MFMA = 2 } wq_decode_algo;
 /* or-ed into algo: every wavefront of the matrix-core kernel gets a fixed share of the token axis, so that the
  * summation order, and with it every bit of the result, is the same on every run.  Without it the wavefronts of a
@@ -304,6 +310,83 @@ int wq_decode_attention_static(void* hip_stream, const void* q, int q_dtype, int
                                float sm_scale, int num_splits, int64_t max_seq_tokens, int algo, float* out, float* lse);
 /* message of the last wq_decode_attention_static error on the current device (host string, valid until the next call) */
 const char* wq_static_last_error(void);
+
+/* ---- rotary positions ----------------------------------------------------------------------------------------------
+ * The channel pairs (x_a, x_b) of the first rot_dim channels of every head are turned by t = position * inv_freq[i],
+ * i = 0 .. rot_dim/2 - 1:
+ *     y_a = (x_a cos t - x_b sin t) mscale,   y_b = (x_b cos t + x_a sin t) mscale
+ * with (a, b) = (i, i + rot_dim/2) (WQ_ROPE_HALF) or (2i, 2i + 1) (WQ_ROPE_PAIRS); the other channels are copied.  The
+ * angle is formed in fp64 (positions and frequencies are taken as they are, however far), the products in fp32.
+ * q [rows, Hq, hd], k [rows, Hkv, hd], element type `dtype`: a row's heads lie one after the other, rows are *_stride
+ * elements apart (a projection that holds queries, keys and values of a row behind each other need not be split).
+ * q_out, k_out likewise; they may be q and k themselves (with the same strides), and must not overlap the inputs in
+ * another way.  k may be NULL with Hkv = 0.  positions [rows] int32, inv_freq [rot_dim/2] fp32: device.
+ * hd 64 or 128; rot_dim a multiple of 16 up to hd; pointers 16-byte aligned and rows a multiple of 16 bytes apart
+ * (WQ_ERR_UNSUPPORTED / WQ_ERR_ARG beyond).                                                                          */
+int wq_rope(wq_ctx* ctx, const void* q, int64_t q_stride, const void* k, int64_t k_stride, int dtype, int64_t rows, int Hq, int Hkv, int hd,
+            int rot_dim, int layout, const int32_t* positions, const float* inv_freq, float mscale, void* q_out, int64_t q_out_stride,
+            void* k_out, int64_t k_out_stride);
+
+/* A decode step's rotary positions and append in one launch: like wq_rope on q and k (one row per sequence, rows = B,
+ * Hkv and hd those of the cache) followed by wq_append_kv of the turned keys and of v.  q_out gets the turned queries, the
+ * turned key and v become row off16[b] + len16[b] of sequence b's 16-bit segment, len16[b] is raised.  The key is rounded
+ * once, into dtype16 (which pairs with dtype as in wq_append_kv).  A sequence whose segment is full is left unchanged, its
+ * query is turned all the same, and WQ_DEV_SEG16_OVERFLOW is raised.  The cache's k16 and v16 must be 16-byte aligned.   */
+int wq_rope_append_kv(wq_ctx* ctx, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int dtype,
+                      int B, int Hq, int rot_dim, int layout, const int32_t* positions, const float* inv_freq, float mscale, void* q_out,
+                      int64_t q_out_stride, const wq_packed_kv* kv);
+
+/* Host-only, pure: inv_freq [rot_dim/2] and *mscale (host) for a model trained with `base`, stretched `factor` times (>= 1):
+ *   WQ_ROPE_PLAIN  f_i = base^(-2i/rot_dim)                               (factor is not read)
+ *   WQ_ROPE_EVEN   f_i / factor
+ *   WQ_ROPE_BASE   f_i of the base  base * factor^(rot_dim/(rot_dim-2))
+ *   WQ_ROPE_PARTS  (1 - g) f_i/factor + g f_i,  g = clamp((r - 1)/(32 - 1), 0, 1),  r = trained_context f_i / 2 pi the turns that a
+ *                  pair makes over the context the model was trained with;  mscale = 0.1 ln(factor) + 1   (1 otherwise)
+ * Evaluated in double.  A model that was trained with another rule brings its own table.  WQ_ERR_ARG on NULL, a rot_dim that is not
+ * a positive multiple of 16, base <= 1, factor < 1, an unknown rule, trained_context <= 0 with WQ_ROPE_PARTS.            */
+int wq_rope_frequencies(int rot_dim, double base, int scaling, double factor, int64_t trained_context, float* inv_freq, float* mscale);
+
+/* ---- attention of a prompt's rows ------------------------------------------------------------------------------------
+ * What a layer computes over a batch of prompts before wq_reorder_quantize packs the same keys and values.  Sequence b has
+ * the key and value rows kv_off[b] .. kv_off[b+1]-1 (as in wq_reorder_quantize; rows of different sequences never meet) and
+ * the query rows q_off[b] .. q_off[b+1]-1, which are its last ones: with L = number of keys, n = number of queries, query
+ * row i has position L - n + i.  All rows at once, a chunk behind rows that are there already, or single tokens (n = 1).
+ *     out[i,h,:] = sum_j softmax_j(sm_scale * q[i,h].k_j) v_j   over the keys  j <= position  or  j < prefix_len[b]
+ * prefix_len [B] (NULL: none): the sequence's first rows that every row sees (visual tokens that see each other); clipped to
+ * 0 .. L.  Head h reads KV head h/(Hq/Hkv).  A row that sees no key (n > L) becomes zeros, its lse -infinity.
+ * q [total_q, Hq, hd], k, v [total_kv, Hkv, hd], element type `dtype` for all, rows *_stride elements apart; out [total_q, Hq, hd]
+ * of the same type, contiguous; rows of out and lse that belong to no sequence are left as they were.  lse [total_q, Hq]
+ * fp32 or NULL.  q_off, kv_off [B+1] ascending, device; total_q, total_kv: host bounds (rows beyond them are not read).
+ * max_kv_rows: host bound on one sequence's keys, used for the number of splits only.  num_splits: workgroups that
+ * share a tile of query rows' keys, 1 .. 64, or 0 = automatic (more than one where there are few query rows).
+ * Values of the sequences' rows must be finite.  fp32: fp32 arithmetic throughout.  16-bit types: exact products, fp32 sums,
+ * weights rounded to the type in front of their product with the values.  Pointers 16-byte aligned, rows a multiple of 16
+ * bytes apart; out must not overlap the inputs.  Workspace: wq_prefill_workspace_bytes (WQ_ERR_WORKSPACE below it).       */
+int wq_prefill_attention(wq_ctx* ctx, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int dtype,
+                         int B, int Hq, int Hkv, int hd, const int32_t* q_off, const int32_t* kv_off, const int32_t* prefix_len, int64_t total_q,
+                         int64_t total_kv, int64_t max_kv_rows, float sm_scale, int num_splits, void* out, float* lse);
+/* Host-only, pure: workspace of a call with these arguments. */
+size_t wq_prefill_workspace_bytes(int64_t total_q, int B, int Hq, int Hkv, int hd, int64_t max_kv_rows, int num_splits);
+
+/* ---- decode attention of requests that share packed caches -----------------------------------------------------------
+ * Several requests ask about one video: its packed cache is kept once and read once for all of them.  Sequence p of
+ * `prefix` (prefix->B >= 1 sequences, all four segments) is shared by the requests req_off[p] .. req_off[p+1]-1 (req_off
+ * [prefix->B + 1] ascending, device); request b also has sequence b of `own` (own->B == B: its question and generated
+ * tokens, kept with wq_append_kv or wq_rope_append_kv; packed segments are allowed) unless own is NULL.  One softmax over both:
+ *     out[b,h,:] = sum_t softmax_t(sm_scale * q[b,h].k^_t) v^_t    over the prefix of b's group and b's own cache
+ * A request in no group has its own cache only; with no token at all its row becomes zeros and its lse -infinity.
+ * q [B, Hq, hd], out [B, Hq, hd], both of type q_dtype, which pairs with the caches' dtype16 as in wq_reorder_quantize (bf16 with
+ * bf16; fp16 and fp32 with fp16); lse [B, Hq] fp32 or NULL.  Both caches: the same Hkv, hd and dtype16.
+ * 16-bit queries: packed keys and values are expanded to fp16 and met by fp16 weights (errors of 2^-11 relative to a value, the
+ * result has the query's type); a bf16 query is exact down to 2^-24 of its head's largest entry.  fp32 queries: fp32 arithmetic.
+ * num_splits: workgroups that share the tokens of a prefix per 128 query rows, 1 .. 64, or 0 = automatic; max_prefix_tokens,
+ * max_own_tokens: host bounds on the tokens of one sequence (used for splits only).  q, out and the prefix's buffers
+ * 16-byte aligned.  Workspace: wq_shared_workspace_bytes (max_own_tokens 0 where own is NULL).                            */
+int wq_decode_attention_shared(wq_ctx* ctx, const void* q, int q_dtype, int B, int Hq, const wq_packed_kv* prefix, const int32_t* req_off,
+                               const wq_packed_kv* own, float sm_scale, int num_splits, int64_t max_prefix_tokens, int64_t max_own_tokens, void* out,
+                               float* lse);
+/* Host-only, pure: workspace of a call with these arguments (P: sequences of the shared cache). */
+size_t wq_shared_workspace_bytes(int B, int P, int Hq, int Hkv, int hd, int64_t max_prefix_tokens, int64_t max_own_tokens, int num_splits);
 
 #ifdef __cplusplus
 }

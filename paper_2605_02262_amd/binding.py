@@ -20,6 +20,8 @@ DECODE_PARTIALS_ONLY = 0x100
 DECODE_FIXED_SHARES = 0x200
 DECODE_BY_LENGTH = 0x400
 DECODE_SEPARATE_MERGE = 0x800
+ROPE_HALF, ROPE_PAIRS = 0, 1
+ROPE_PLAIN, ROPE_EVEN, ROPE_BASE, ROPE_PARTS = 0, 1, 2, 3
 CLASS_BITS = (2, 4, 8)
 DEV_CLASS_OVERFLOW, DEV_SEG16_OVERFLOW, DEV_APPEND_TIMEOUT, DEV_TOO_MANY_WINDOWS, DEV_BAD_ASSIGNMENT = 1, 2, 4, 16, 32
 
@@ -76,6 +78,15 @@ def lib() -> C.CDLL:
         L.wq_decode_attention_static.argtypes = [vp, vp, i32, i32, i32, C.POINTER(_PackedKV), f32, i32, i64, i32, vp, vp]
         L.wq_static_last_error.argtypes = []
         L.wq_static_last_error.restype = C.c_char_p
+        L.wq_rope.argtypes = [vp, vp, i64, vp, i64, i32, i64, i32, i32, i32, i32, i32, vp, vp, f32, vp, i64, vp, i64]
+        L.wq_rope_append_kv.argtypes = [vp, vp, i64, vp, i64, vp, i64, i32, i32, i32, i32, i32, vp, vp, f32, vp, i64, C.POINTER(_PackedKV)]
+        L.wq_rope_frequencies.argtypes = [i32, C.c_double, i32, C.c_double, i64, C.POINTER(C.c_float), C.POINTER(C.c_float)]
+        L.wq_prefill_attention.argtypes = [vp, vp, i64, vp, i64, vp, i64, i32, i32, i32, i32, i32, vp, vp, vp, i64, i64, i64, f32, i32, vp, vp]
+        L.wq_prefill_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i64, i32]
+        L.wq_prefill_workspace_bytes.restype = C.c_size_t
+        L.wq_decode_attention_shared.argtypes = [vp, vp, i32, i32, i32, C.POINTER(_PackedKV), vp, C.POINTER(_PackedKV), f32, i32, i64, i64, vp, vp]
+        L.wq_shared_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i64, i64, i32]
+        L.wq_shared_workspace_bytes.restype = C.c_size_t
         L.wq_probe_stream.argtypes = [vp, vp, vp, i64, i32]
         L.wq_probe_mfma.argtypes = [vp, i32, i32, i32, C.POINTER(C.c_double)]
         L.wq_decode_timing.argtypes = [vp, i32]
@@ -308,6 +319,126 @@ def wq_decode_attention_static(q, kv: PackedKV, sm_scale: float, num_splits: int
                                           max_seq_tokens, algo, _ptr(out), _ptr(lse))
     if rc != 0:
         raise WQError(rc, lib().wq_static_last_error().decode())
+    return out
+
+
+# ------------------------------------------------------------------------------------------------------------
+# rotary positions, prompt attention, decode over shared caches
+# ------------------------------------------------------------------------------------------------------------
+def _rows(name: str, t: torch.Tensor, like: Optional[torch.Tensor] = None) -> int:
+    """Row stride of [rows, heads, hd] whose rows are contiguous inside."""
+    if t.dim() != 3 or (t.numel() and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]))):
+        raise ValueError(f"{name}: [rows, heads, head_dim] with contiguous rows expected, got shape {tuple(t.shape)}, strides {t.stride()}")
+    if like is not None and (t.dtype != like.dtype or t.shape[2] != like.shape[2]):
+        raise ValueError(f"{name}: type or head_dim differ from the queries'")
+    return max(t.stride(0), t.shape[1] * t.shape[2]) if t.shape[0] <= 1 else t.stride(0)
+
+
+def _contiguous(name: str, t: torch.Tensor, dtype: torch.dtype, numel: int):
+    if t.dtype != dtype or not t.is_contiguous() or t.numel() != numel:
+        raise ValueError(f"{name}: {numel} contiguous elements of {dtype} expected, got {tuple(t.shape)} of {t.dtype}")
+
+
+def wq_rope_frequencies(rot_dim: int, base: float, scaling: int = ROPE_PLAIN, factor: float = 1.0, trained_context: int = 0):
+    """(inv_freq as an fp32 list, mscale) (host-only call)."""
+    f, m = (C.c_float * max(rot_dim // 2, 1))(), C.c_float(0.0)
+    rc = lib().wq_rope_frequencies(rot_dim, float(base), scaling, float(factor), trained_context, f, C.byref(m))
+    if rc != 0:
+        raise WQError(rc, "wq_rope_frequencies: bad argument")
+    return [float(x) for x in f], float(m.value)
+
+
+def wq_rope(ctx: Context, q, k, positions, inv_freq, layout: int = ROPE_HALF, mscale: float = 1.0, q_out: Optional[torch.Tensor] = None,
+            k_out: Optional[torch.Tensor] = None):
+    """Turns q [rows, Hq, hd] and k [rows, Hkv, hd] (or None); 2 * inv_freq.numel() channels of every head."""
+    rows, Hq, hd = q.shape
+    qs = _rows("q", q)
+    _contiguous("positions", positions, torch.int32, rows)
+    _contiguous("inv_freq", inv_freq, torch.float32, inv_freq.numel())
+    if q_out is None:
+        q_out = torch.empty(rows, Hq, hd, dtype=q.dtype, device=q.device)
+    qo = _rows("q_out", q_out, q)
+    ks = ko = Hkv = 0
+    if k is not None:
+        ks, Hkv = _rows("k", k, q), k.shape[1]
+        if k_out is None:
+            k_out = torch.empty(rows, Hkv, hd, dtype=k.dtype, device=k.device)
+        ko = _rows("k_out", k_out, q)
+        if k.shape[0] != rows or k_out.shape != k.shape:
+            raise ValueError("k, k_out: as many rows as q expected")
+    if q_out.shape != q.shape:
+        raise ValueError("q_out: the shape of q expected")
+    ctx.check(lib().wq_rope(ctx.handle, _ptr(q), qs, _ptr(k), ks, _dtype_id(q), rows, Hq, Hkv, hd, 2 * inv_freq.numel(), layout, _ptr(positions),
+                            _ptr(inv_freq), mscale, _ptr(q_out), qo, _ptr(k_out) if k is not None else None, ko))
+    return q_out, k_out
+
+
+def wq_rope_append_kv(ctx: Context, q, k, v, positions, inv_freq, kv: PackedKV, layout: int = ROPE_HALF, mscale: float = 1.0,
+                      q_out: Optional[torch.Tensor] = None):
+    """Turns q [B, Hq, hd] (returned) and k [B, Hkv, hd]; k and v become the cache's next rows."""
+    B, Hq, hd = q.shape
+    qs, ks, vs = _rows("q", q), _rows("k", k, q), _rows("v", v, q)
+    if k.shape != (B, kv.Hkv, kv.hd) or v.shape != k.shape:
+        raise ValueError("k, v: [B, Hkv, hd] of the cache expected")
+    _contiguous("positions", positions, torch.int32, B)
+    _contiguous("inv_freq", inv_freq, torch.float32, inv_freq.numel())
+    if q_out is None:
+        q_out = torch.empty(B, Hq, hd, dtype=q.dtype, device=q.device)
+    if q_out.shape != q.shape:
+        raise ValueError("q_out: the shape of q expected")
+    ctx.check(lib().wq_rope_append_kv(ctx.handle, _ptr(q), qs, _ptr(k), ks, _ptr(v), vs, _dtype_id(q), B, Hq, 2 * inv_freq.numel(), layout,
+                                      _ptr(positions), _ptr(inv_freq), mscale, _ptr(q_out), _rows("q_out", q_out, q), C.byref(kv.desc)))
+    return q_out
+
+
+def prefill_workspace_bytes(total_q: int, B: int, Hq: int, Hkv: int, hd: int, max_kv_rows: int, num_splits: int = 0) -> int:
+    return int(lib().wq_prefill_workspace_bytes(total_q, B, Hq, Hkv, hd, max_kv_rows, num_splits))
+
+
+def wq_prefill_attention(ctx: Context, q, k, v, q_off, kv_off, sm_scale: float, prefix_len: Optional[torch.Tensor] = None, max_kv_rows: int = 0,
+                         num_splits: int = 0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None):
+    """q [total_q, Hq, hd] over k, v [total_kv, Hkv, hd]; q_off, kv_off [B+1], prefix_len [B] int32."""
+    total_q, Hq, hd = q.shape
+    total_kv, Hkv, _ = k.shape
+    B = q_off.numel() - 1
+    qs, ks, vs = _rows("q", q), _rows("k", k, q), _rows("v", v, q)
+    if v.shape != k.shape:
+        raise ValueError("v: the shape of k expected")
+    _contiguous("q_off", q_off, torch.int32, B + 1)
+    _contiguous("kv_off", kv_off, torch.int32, B + 1)
+    if prefix_len is not None:
+        _contiguous("prefix_len", prefix_len, torch.int32, B)
+    if out is None:
+        out = torch.empty(total_q, Hq, hd, dtype=q.dtype, device=q.device)
+    _contiguous("out", out, q.dtype, q.numel())
+    if lse is not None:
+        _contiguous("lse", lse, torch.float32, total_q * Hq)
+    ctx.check(lib().wq_prefill_attention(ctx.handle, _ptr(q), qs, _ptr(k), ks, _ptr(v), vs, _dtype_id(q), B, Hq, Hkv, hd, _ptr(q_off), _ptr(kv_off),
+                                         _ptr(prefix_len), total_q, total_kv, max_kv_rows, sm_scale, num_splits, _ptr(out), _ptr(lse)))
+    return out
+
+
+def shared_workspace_bytes(B: int, P: int, Hq: int, Hkv: int, hd: int, max_prefix_tokens: int, max_own_tokens: int = 0, num_splits: int = 0) -> int:
+    return int(lib().wq_shared_workspace_bytes(B, P, Hq, Hkv, hd, max_prefix_tokens, max_own_tokens, num_splits))
+
+
+def wq_decode_attention_shared(ctx: Context, q, prefix: PackedKV, req_off, own: Optional[PackedKV], sm_scale: float, num_splits: int = 0,
+                               max_prefix_tokens: int = 0, max_own_tokens: int = 0, out: Optional[torch.Tensor] = None,
+                               lse: Optional[torch.Tensor] = None):
+    """q [B, Hq, hd]; requests req_off[p] .. req_off[p+1]-1 share sequence p of prefix, request b has sequence b of own (or None)."""
+    B, Hq, hd = q.shape
+    if hd != prefix.hd:
+        raise ValueError("q: the head_dim of the cache expected")
+    _contiguous("q", q, q.dtype, q.numel())
+    _contiguous("req_off", req_off, torch.int32, prefix.B + 1)
+    if out is None:
+        out = torch.empty(B, Hq, hd, dtype=q.dtype, device=q.device)
+    _contiguous("out", out, q.dtype, q.numel())
+    if lse is not None:
+        _contiguous("lse", lse, torch.float32, B * Hq)
+    ctx.check(lib().wq_decode_attention_shared(ctx.handle, _ptr(q), _dtype_id(q), B, Hq, C.byref(prefix.desc), _ptr(req_off),
+                                               None if own is None else C.byref(own.desc), sm_scale, num_splits, max_prefix_tokens, max_own_tokens,
+                                               _ptr(out), _ptr(lse)))
     return out
 
 

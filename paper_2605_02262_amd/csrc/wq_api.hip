@@ -1,6 +1,7 @@
 // C-ABI entry points of libwq: context handling, host-side argument validation, dispatch.
 // Every check that needs only host data happens here, before anything is enqueued.
 #include <math.h>
+#include <initializer_list>
 #include <mutex>
 #include <new>
 #include <string.h>
@@ -379,6 +380,183 @@ int wq_decode_attention(wq_ctx* ctx, const void* q, int q_dtype, int B, int Hq, 
     const int rc = check_decode(ctx, q, q_dtype, B, Hq, kv, sm_scale, &num_splits, max_seq_tokens, algo, out, &longest);
     if (rc != WQ_OK || B == 0) return rc;
     return wq_launch_decode(ctx, q, q_dtype, B, Hq, kv, sm_scale, num_splits, algo, out, lse, nullptr, nullptr, longest);
+}
+
+// ---- rotary positions, prompt attention, decode over shared caches -----------------------------------------------------
+
+static bool on_16_bytes(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+// rows of H heads of hd elements, `stride` elements apart
+static int check_rows(wq_ctx* ctx, const char* name, const void* p, int64_t stride, int64_t rows, int H, int hd, int dtype)
+{
+    if (rows == 0) return WQ_OK;
+    if (!p) return wq_fail(ctx, WQ_ERR_ARG, "%s is NULL", name);
+    if (stride < (int64_t)H * hd) return wq_fail(ctx, WQ_ERR_ARG, "%s: rows of %d x %d elements are %lld elements apart", name, H, hd, (long long)stride);
+    if (!on_16_bytes(p) || stride % (dtype == WQ_F32 ? 4 : 8) != 0)
+        return wq_fail(ctx, WQ_ERR_ARG, "%s must be 16-byte aligned, its rows a multiple of 16 bytes apart", name);
+    return WQ_OK;
+}
+
+static int check_rope(wq_ctx* ctx, const WqRope& r)
+{
+    if (r.rows < 0) return wq_fail(ctx, WQ_ERR_ARG, "negative size");
+    if (r.rows > INT32_MAX) return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "too many rows");
+    if (!dtype_ok(r.dtype)) return wq_fail(ctx, WQ_ERR_ARG, "unknown dtype %d", r.dtype);
+    if (r.hd != 64 && r.hd != 128) return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "unsupported head dimension %d", r.hd);
+    if (r.Hq <= 0 || r.Hkv < 0) return wq_fail(ctx, WQ_ERR_ARG, "bad head counts %d, %d", r.Hq, r.Hkv);
+    if (r.Hq > 65536 || r.Hkv > 65536) return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "more than 65536 heads");
+    if (r.rot_dim <= 0 || r.rot_dim > r.hd || r.rot_dim % 16 != 0)
+        return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "rot_dim=%d must be a multiple of 16 up to the head dimension %d", r.rot_dim, r.hd);
+    if (r.layout != WQ_ROPE_HALF && r.layout != WQ_ROPE_PAIRS) return wq_fail(ctx, WQ_ERR_ARG, "unknown layout %d", r.layout);
+    if (!isfinite(r.mscale)) return wq_fail(ctx, WQ_ERR_ARG, "mscale must be finite");
+    if (r.rows > 0 && (!r.positions || !r.inv_freq)) return wq_fail(ctx, WQ_ERR_ARG, "NULL positions or frequencies");
+    int rc = check_rows(ctx, "q", r.q, r.q_stride, r.rows, r.Hq, r.hd, r.dtype);
+    if (rc == WQ_OK) rc = check_rows(ctx, "q_out", r.q_out, r.q_out_stride, r.rows, r.Hq, r.hd, r.dtype);
+    if (rc == WQ_OK && r.Hkv > 0) rc = check_rows(ctx, "k", r.k, r.k_stride, r.rows, r.Hkv, r.hd, r.dtype);
+    return rc;
+}
+
+int wq_rope(wq_ctx* ctx, const void* q, int64_t q_stride, const void* k, int64_t k_stride, int dtype, int64_t rows, int Hq, int Hkv, int hd,
+            int rot_dim, int layout, const int32_t* positions, const float* inv_freq, float mscale, void* q_out, int64_t q_out_stride,
+            void* k_out, int64_t k_out_stride)
+{
+    if (!ctx) return WQ_ERR_ARG;
+    const WqRope r = {q, k, q_out, k_out, q_stride, k_stride, q_out_stride, k_out_stride, dtype, Hq, Hkv, hd, rot_dim, layout, rows, positions, inv_freq, mscale};
+    int rc = check_rope(ctx, r);
+    if (rc == WQ_OK && Hkv > 0) rc = check_rows(ctx, "k_out", k_out, k_out_stride, rows, Hkv, hd, dtype);
+    if (rc == WQ_OK && q == q_out && q_stride != q_out_stride) rc = wq_fail(ctx, WQ_ERR_ARG, "q in place with another stride");
+    if (rc == WQ_OK && Hkv > 0 && k == k_out && k_stride != k_out_stride) rc = wq_fail(ctx, WQ_ERR_ARG, "k in place with another stride");
+    if (rc != WQ_OK || rows == 0) return rc;
+    return wq_launch_rope(ctx, r);
+}
+
+int wq_rope_append_kv(wq_ctx* ctx, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int dtype,
+                      int B, int Hq, int rot_dim, int layout, const int32_t* positions, const float* inv_freq, float mscale, void* q_out,
+                      int64_t q_out_stride, const wq_packed_kv* kv)
+{
+    if (!ctx) return WQ_ERR_ARG;
+    if (B < 0) return wq_fail(ctx, WQ_ERR_ARG, "negative size");
+    int rc = check_packed(ctx, kv, B, false);
+    if (rc != WQ_OK) return rc;
+    const WqRope r = {q, k, q_out, nullptr, q_stride, k_stride, q_out_stride, 0, dtype, Hq, kv->Hkv, kv->hd, rot_dim, layout, B, positions, inv_freq, mscale};
+    rc = check_rope(ctx, r);
+    if (rc == WQ_OK) rc = check_rows(ctx, "v", v, v_stride, B, kv->Hkv, kv->hd, dtype);
+    if (rc != WQ_OK) return rc;
+    if ((dtype == WQ_BF16) != (kv->dtype16 == WQ_BF16))
+        return wq_fail(ctx, WQ_ERR_ARG, "dtype16 must be bf16 for bf16 input and fp16 for fp16/fp32 input");
+    if (q == q_out && q_stride != q_out_stride) return wq_fail(ctx, WQ_ERR_ARG, "q in place with another stride");
+    if (!on_16_bytes(kv->k16) || !on_16_bytes(kv->v16)) return wq_fail(ctx, WQ_ERR_ARG, "k16 and v16 must be 16-byte aligned");
+    if (B == 0) return WQ_OK;
+    if (!ctx->ws || ctx->ws_bytes < WQ_WS_HEADER) return wq_fail(ctx, WQ_ERR_WORKSPACE, "no workspace");
+    return wq_launch_rope_append(ctx, r, v, v_stride, kv);
+}
+
+int wq_rope_frequencies(int rot_dim, double base, int scaling, double factor, int64_t trained_context, float* inv_freq, float* mscale)
+{
+    if (!inv_freq || !mscale || rot_dim <= 0 || rot_dim % 16 != 0 || !isfinite(base) || !(base > 1.0)) return WQ_ERR_ARG;
+    if (scaling < WQ_ROPE_PLAIN || scaling > WQ_ROPE_PARTS) return WQ_ERR_ARG;
+    if (scaling != WQ_ROPE_PLAIN && !(isfinite(factor) && factor >= 1.0)) return WQ_ERR_ARG;
+    if (scaling == WQ_ROPE_PARTS && trained_context <= 0) return WQ_ERR_ARG;
+    if (scaling == WQ_ROPE_BASE) base *= pow(factor, (double)rot_dim / (rot_dim - 2));
+    for (int i = 0; i < rot_dim / 2; i++) {
+        double f = pow(base, -2.0 * i / rot_dim);
+        if (scaling == WQ_ROPE_EVEN) f /= factor;
+        if (scaling == WQ_ROPE_PARTS) {
+            const double turns = (double)trained_context * f / 6.28318530717958647692;
+            const double g = fmin(fmax((turns - 1.0) / (32.0 - 1.0), 0.0), 1.0);
+            f = (1.0 - g) * f / factor + g * f;
+        }
+        inv_freq[i] = (float)f;
+    }
+    *mscale = scaling == WQ_ROPE_PARTS ? (float)(0.1 * log(factor) + 1.0) : 1.0f;
+    return WQ_OK;
+}
+
+size_t wq_prefill_workspace_bytes(int64_t total_q, int B, int Hq, int Hkv, int hd, int64_t max_kv_rows, int num_splits)
+{
+    if (total_q <= 0 || B <= 0 || Hq <= 0 || Hkv <= 0 || hd <= 0 || Hq % Hkv != 0) return WQ_WS_HEADER;
+    return WQ_WS_HEADER + wq_prefill_ws_bytes(total_q, Hq, hd, num_splits > 0 ? num_splits : wq_prefill_splits(total_q, B, Hq, Hkv, max_kv_rows));
+}
+
+int wq_prefill_attention(wq_ctx* ctx, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int dtype,
+                         int B, int Hq, int Hkv, int hd, const int32_t* q_off, const int32_t* kv_off, const int32_t* prefix_len, int64_t total_q,
+                         int64_t total_kv, int64_t max_kv_rows, float sm_scale, int num_splits, void* out, float* lse)
+{
+    if (!ctx) return WQ_ERR_ARG;
+    if (B < 0 || total_q < 0 || total_kv < 0) return wq_fail(ctx, WQ_ERR_ARG, "negative size");
+    if (!dtype_ok(dtype)) return wq_fail(ctx, WQ_ERR_ARG, "unknown dtype %d", dtype);
+    if (hd != 64 && hd != 128) return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "unsupported head dimension %d", hd);
+    if (Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || Hq / Hkv > WQ_MAX_REP)
+        return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "Hq=%d must be a multiple of Hkv=%d, at most %d query heads per KV head", Hq, Hkv, WQ_MAX_REP);
+    const int rep = Hq / Hkv;
+    if (total_q > INT32_MAX / rep || total_kv > INT32_MAX || B > INT32_MAX / 2 || (total_q / 64 * rep + B + 1) > INT32_MAX / Hkv)
+        return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "too many rows");
+    if (num_splits < 0 || num_splits > WQ_MAX_ATTEND_SPLITS) return wq_fail(ctx, WQ_ERR_ARG, "num_splits out of range");
+    if (!(sm_scale > 0.0f) || sm_scale > 3.0e38f) return wq_fail(ctx, WQ_ERR_ARG, "sm_scale must be positive and finite");
+    if (B == 0 || total_q == 0) return WQ_OK;
+    if (!q_off || !kv_off || !out) return wq_fail(ctx, WQ_ERR_ARG, "NULL table or output");
+    if (!on_16_bytes(out)) return wq_fail(ctx, WQ_ERR_ARG, "out must be 16-byte aligned");
+    int rc = check_rows(ctx, "q", q, q_stride, total_q, Hq, hd, dtype);
+    if (rc == WQ_OK) rc = check_rows(ctx, "k", k, k_stride, total_kv, Hkv, hd, dtype);
+    if (rc == WQ_OK) rc = check_rows(ctx, "v", v, v_stride, total_kv, Hkv, hd, dtype);
+    if (rc != WQ_OK) return rc;
+    const int splits = num_splits > 0 ? num_splits : wq_prefill_splits(total_q, B, Hq, Hkv, max_kv_rows);
+    if (ctx->ws_bytes < WQ_WS_HEADER + wq_prefill_ws_bytes(total_q, Hq, hd, splits) || !ctx->ws)
+        return wq_fail(ctx, WQ_ERR_WORKSPACE, "workspace too small for %d splits of %lld rows", splits, (long long)total_q);
+    return wq_launch_prefill(ctx, {q, k, v, q_stride, k_stride, v_stride, dtype, B, Hq, Hkv, hd, splits, q_off, kv_off, prefix_len, total_q, total_kv, sm_scale,
+                                   out, lse});
+}
+
+size_t wq_shared_workspace_bytes(int B, int P, int Hq, int Hkv, int hd, int64_t max_prefix_tokens, int64_t max_own_tokens, int num_splits)
+{
+    if (B <= 0 || P <= 0 || Hq <= 0 || Hkv <= 0 || hd <= 0 || Hq % Hkv != 0) return WQ_WS_HEADER;
+    const int splits = num_splits > 0 ? num_splits : wq_shared_splits(B, P, Hq, Hkv, max_prefix_tokens);
+    return WQ_WS_HEADER + wq_decode_ws_bytes(B, Hq, hd, wq_auto_splits(B, Hkv, max_own_tokens)) + wq_shared_ws_bytes(B, Hq, hd, splits);
+}
+
+int wq_decode_attention_shared(wq_ctx* ctx, const void* q, int q_dtype, int B, int Hq, const wq_packed_kv* prefix, const int32_t* req_off,
+                               const wq_packed_kv* own, float sm_scale, int num_splits, int64_t max_prefix_tokens, int64_t max_own_tokens, void* out,
+                               float* lse)
+{
+    if (!ctx) return WQ_ERR_ARG;
+    if (B < 0 || Hq <= 0) return wq_fail(ctx, WQ_ERR_ARG, "bad B or Hq");
+    if (B > 65535) return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "more than 65535 requests in one call");
+    if (!dtype_ok(q_dtype)) return wq_fail(ctx, WQ_ERR_ARG, "unknown q dtype %d", q_dtype);
+    if (prefix && prefix->B <= 0) return wq_fail(ctx, WQ_ERR_ARG, "no shared sequence");
+    int rc = check_packed(ctx, prefix, prefix ? prefix->B : 0, true);
+    if (rc != WQ_OK) return rc;
+    if (prefix->B > 65535) return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "more than 65535 shared sequences in one call");
+    if (Hq % prefix->Hkv != 0 || Hq / prefix->Hkv > WQ_MAX_REP)
+        return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "Hq=%d must be a multiple of Hkv=%d, at most %d query heads per KV head", Hq, prefix->Hkv, WQ_MAX_REP);
+    if ((q_dtype == WQ_BF16) != (prefix->dtype16 == WQ_BF16))
+        return wq_fail(ctx, WQ_ERR_ARG, "dtype16 must be bf16 for bf16 queries and fp16 for fp16/fp32 queries");
+    for (const void* p : {q, static_cast<const void*>(out), static_cast<const void*>(prefix->k16), static_cast<const void*>(prefix->v16)})
+        if (!on_16_bytes(p)) return wq_fail(ctx, WQ_ERR_ARG, "q, out, k16 and v16 must be 16-byte aligned");
+    for (int c = 0; c < 3; c++)
+        if (!on_16_bytes(prefix->codes[c]) || !on_16_bytes(prefix->meta[c])) return wq_fail(ctx, WQ_ERR_ARG, "class %d is not 16-byte aligned", c);
+    if (num_splits < 0 || num_splits > WQ_MAX_ATTEND_SPLITS) return wq_fail(ctx, WQ_ERR_ARG, "num_splits out of range");
+    if (!(sm_scale > 0.0f) || sm_scale > 3.0e38f) return wq_fail(ctx, WQ_ERR_ARG, "sm_scale must be positive and finite");
+    if (own) {
+        rc = check_packed(ctx, own, B, true);
+        if (rc != WQ_OK) return rc;
+        if (own->Hkv != prefix->Hkv || own->hd != prefix->hd || own->dtype16 != prefix->dtype16)
+            return wq_fail(ctx, WQ_ERR_ARG, "the shared and the requests' own cache differ in Hkv, hd or dtype16");
+    }
+    if (B == 0) return WQ_OK;
+    if (!q || !out || !req_off) return wq_fail(ctx, WQ_ERR_ARG, "NULL q, out or req_off");
+    const int splits = num_splits > 0 ? num_splits : wq_shared_splits(B, prefix->B, Hq, prefix->Hkv, max_prefix_tokens);
+    const size_t own_bytes = own ? wq_decode_ws_bytes(B, Hq, own->hd, wq_auto_splits(B, own->Hkv, max_own_tokens)) : 0;
+    if (!ctx->ws || ctx->ws_bytes < WQ_WS_HEADER + own_bytes + wq_shared_ws_bytes(B, Hq, prefix->hd, splits))
+        return wq_fail(ctx, WQ_ERR_WORKSPACE, "workspace too small for %d splits of %d requests", splits, B);
+    // an fp32 query's own cache in fp32 arithmetic, like its shared one
+    const int algo = q_dtype == WQ_F32 ? WQ_DECODE_GENERIC : WQ_DECODE_AUTO;
+    int own_splits = 0;
+    if (own) {
+        int64_t longest = 0;
+        rc = check_decode(ctx, q, q_dtype, B, Hq, own, sm_scale, &own_splits, max_own_tokens, algo, static_cast<const float*>(out), &longest);
+        if (rc != WQ_OK) return rc;
+    }
+    return wq_launch_shared(ctx, {q, q_dtype, B, Hq, splits, prefix, own, req_off, sm_scale, own_splits, algo, own_bytes, out, lse});
 }
 
 // ---- the entry point that allocates nothing ---------------------------------------------------------------------

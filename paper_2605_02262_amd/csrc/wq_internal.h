@@ -168,3 +168,47 @@ bool wq_decode_can_append(const void* q, int q_dtype, int B, int Hq, const wq_pa
                           const void* v_new, int new_dtype);
 size_t wq_decode_ws_bytes(int B, int Hq, int hd, int splits);
 size_t wq_scores_ws_bytes(int B, int64_t total_vis, int64_t total_txt, int D);
+
+// ---- the operators around the cache: a call's checked arguments ------------------------------------------------------
+struct WqRope {
+    const void *q, *k;
+    void *q_out, *k_out;
+    int64_t q_stride, k_stride, q_out_stride, k_out_stride;       // elements from row to row
+    int dtype, Hq, Hkv, hd, rot_dim, layout;
+    int64_t rows;
+    const int32_t* positions;
+    const float* inv_freq;
+    float mscale;
+};
+int wq_launch_rope(wq_ctx* ctx, const WqRope& r);
+int wq_launch_rope_append(wq_ctx* ctx, const WqRope& r, const void* v, int64_t v_stride, const wq_packed_kv* kv);
+
+constexpr int WQ_MAX_ATTEND_SPLITS = 64;
+struct WqPrefill {
+    const void *q, *k, *v;
+    int64_t q_stride, k_stride, v_stride;                         // elements from row to row
+    int dtype, B, Hq, Hkv, hd, splits;
+    const int32_t *q_off, *kv_off, *prefix_len;
+    int64_t total_q, total_kv;
+    float sm_scale;
+    void* out;
+    float* lse;
+};
+int wq_prefill_splits(int64_t total_q, int B, int Hq, int Hkv, int64_t max_kv_rows);
+size_t wq_prefill_ws_bytes(int64_t total_q, int Hq, int hd, int splits);
+int wq_launch_prefill(wq_ctx* ctx, const WqPrefill& f);
+
+struct WqShared {
+    const void* q;
+    int q_dtype, B, Hq, splits;
+    const wq_packed_kv *prefix, *own;                             // own: NULL, or a cache of B sequences
+    const int32_t* req_off;
+    float sm_scale;
+    int own_splits, own_algo;
+    size_t own_ws_bytes;                                          // what the decode launch over `own` takes of the workspace
+    void* out;
+    float* lse;
+};
+int wq_shared_splits(int B, int P, int Hq, int Hkv, int64_t max_prefix_tokens);
+size_t wq_shared_ws_bytes(int B, int Hq, int hd, int splits);     // without own_ws_bytes
+int wq_launch_shared(wq_ctx* ctx, const WqShared& f);
