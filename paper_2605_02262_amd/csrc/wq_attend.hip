@@ -108,9 +108,9 @@ __device__ __forceinline__ float sum_of_column(float x)
     return x + __shfl_xor(x, 32, 64);
 }
 
-template <typename CT, int HD>
-__device__ __forceinline__ void attend_tile(Rows<HD>& r, const Query<CT, HD>& q, const u4* __restrict__ k_tile, const u4* __restrict__ v_tile,
-                                            int key0, bool masked)
+// keys(t, st), values(vs, ct): this lane's part of the A operands
+template <typename CT, int HD, typename Keys, typename Values>
+__device__ __forceinline__ void attend_tile(Rows<HD>& r, const Query<CT, HD>& q, const Keys& keys, const Values& values, int key0, bool masked)
 {
     const int lane = threadIdx.x & 63;
     f4 s[KEYS / 16][COLS];
@@ -120,7 +120,7 @@ __device__ __forceinline__ void attend_tile(Rows<HD>& r, const Query<CT, HD>& q,
         for (int n = 0; n < COLS; n++) s[t][n] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int st = 0; st < STEPS<CT, HD>; st++) {
-            const u4 a = k_tile[(t * STEPS<CT, HD> + st) * 64 + lane];
+            const u4 a = keys(t, st);
 #pragma unroll
             for (int n = 0; n < COLS; n++) s[t][n] = product<CT>(a, q[n][st], s[t][n]);
         }
@@ -183,10 +183,20 @@ __device__ __forceinline__ void attend_tile(Rows<HD>& r, const Query<CT, HD>& q,
     for (int vs = 0; vs < VSTEPS<CT>; vs++)
 #pragma unroll
         for (int ct = 0; ct < HD / 16; ct++) {
-            const u4 a = v_tile[(vs * (HD / 16) + ct) * 64 + lane];
+            const u4 a = values(vs, ct);
 #pragma unroll
             for (int n = 0; n < COLS; n++) r.o[ct][n] = product<CT>(a, p[vs][n], r.o[ct][n]);
         }
+}
+
+// ... from a tile staged in the operands' order
+template <typename CT, int HD>
+__device__ __forceinline__ void attend_staged(Rows<HD>& r, const Query<CT, HD>& q, const u4* __restrict__ k_tile, const u4* __restrict__ v_tile, int key0,
+                                              bool masked)
+{
+    const int lane = threadIdx.x & 63;
+    attend_tile<CT, HD>(r, q, [&](int t, int st) { return k_tile[(t * STEPS<CT, HD> + st) * 64 + lane]; },
+                        [&](int vs, int ct) { return v_tile[(vs * (HD / 16) + ct) * 64 + lane]; }, key0, masked);
 }
 
 // ---- staging: plain rows -----------------------------------------------------------------------------------------------
@@ -275,6 +285,64 @@ __device__ void stage_rows(const char* k, const char* v, int64_t k_stride, int64
         }
     }
 }
+
+// ---- staging: plain rows of a 16-bit type, from memory to LDS without registers between ----------------------------------
+// A load of 16 bytes per lane lands in LDS at 16 bytes per lane in the lanes' order, so a tile lies there row by row.  What is free
+// is which 16 bytes of its row a lane takes: piece c of row r goes to place c ^ f(r), so that the products' reads, which go down
+// the rows, meet all banks.  Values are read with the transposing load: 16 lanes give the addresses of 4 rows x 16 channels and
+// get 4 rows of one channel each.
+template <int HD>
+struct Direct {
+    static constexpr int PIECES = HD / 8, PER_LOAD = 64 * WAVES / PIECES, LOADS = KEYS / PER_LOAD;      // rows of one load of the workgroup
+    uint32_t k_off, v_off, k_step, v_step;     // this lane's offset in a tile, and from load to load
+    int row;
+    uint32_t k_piece, v_piece, k_stride, v_stride;
+    int k_lds, v_lds;                          // byte offsets in a tile of this lane's operands: key tile 0, step 0; first value tile
+    __device__ __forceinline__ Direct(int64_t ks, int64_t vs)
+    {
+        const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, j = lane >> 4;
+        row = tid / PIECES;
+        const int slot = tid % PIECES;
+        k_piece = 16 * (slot ^ swizzle(row)), v_piece = 16 * (slot ^ (swizzle(row) * 2 & (PIECES - 1)));
+        k_stride = (uint32_t)ks, v_stride = (uint32_t)vs;
+        k_off = row * k_stride + k_piece, v_off = row * v_stride + v_piece;
+        k_step = PER_LOAD * k_stride, v_step = PER_LOAD * v_stride;
+        k_lds = m * (2 * HD) + 16 * (j ^ swizzle(m));
+        const int r = 4 * j + (m >> 2);
+        v_lds = r * (2 * HD) + 8 * (m & 3) + 16 * (swizzle(r) * 2 & (PIECES - 1));
+    }
+    // 16-byte places of 16 neighbouring rows meet different banks (256 bytes)
+    static __device__ __forceinline__ int swizzle(int r) { return HD == 128 ? r & 15 : (r >> 1) & 7; }
+
+    // rows from k, v on, n of them (the last one is read again for the rest: its weights are zero)
+    __device__ __forceinline__ void load(const char* k, const char* v, int n, char* k_tile, char* v_tile) const
+    {
+        const int wave = threadIdx.x >> 6;
+#pragma unroll
+        for (int i = 0; i < LOADS; i++) {
+            uint32_t ko = k_off + i * k_step, vo = v_off + i * v_step;
+            if (n < KEYS) {
+                const uint32_t at = row + i * PER_LOAD < n ? row + i * PER_LOAD : n - 1;
+                ko = at * k_stride + k_piece, vo = at * v_stride + v_piece;
+            }
+            const int to = (i * 64 * WAVES + wave * 64) * 16;
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(k + ko), (__attribute__((address_space(3))) void*)(k_tile + to), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(v + vo), (__attribute__((address_space(3))) void*)(v_tile + to), 16, 0, 0);
+        }
+    }
+    __device__ __forceinline__ u4 keys(const char* k_tile, int t, int st) const
+    {
+        return *reinterpret_cast<const u4*>(k_tile + ((k_lds + t * 16 * (2 * HD)) ^ (64 * st)));
+    }
+    __device__ __forceinline__ u4 values(const char* v_tile, int vs, int ct) const
+    {
+        typedef short s4 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) s4* lds4;
+        const char* p = v_tile + ((v_lds + vs * 32 * (2 * HD)) ^ (32 * ct));
+        struct { s4 a, b; } x = {__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p)), __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + 16 * (2 * HD)))};
+        return __builtin_bit_cast(u4, x);
+    }
+};
 
 // ---- staging: a class of the packed cache ------------------------------------------------------------------------------
 template <int BITS>
@@ -489,7 +557,8 @@ struct PrefillArgs {
 template <typename CT, int HD>
 __global__ __launch_bounds__(64 * WAVES, 2) void k_prefill(PrefillArgs a)
 {
-    __shared__ __align__(16) u4 s_k[K_PIECES<CT, HD>], s_v[V_PIECES<CT, HD>];
+    constexpr bool DIRECT = ESIZE<CT> == 2;                       // two tiles in LDS: one is met while the next one arrives
+    __shared__ __align__(16) u4 s_k[1 + DIRECT][K_PIECES<CT, HD>], s_v[1 + DIRECT][V_PIECES<CT, HD>];
     const int Hkv = a.Hq / a.rep, kvh = blockIdx.x % Hkv, split = blockIdx.y;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     Place p;
@@ -529,12 +598,32 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_prefill(PrefillArgs a)
     const int least = any ? limit_of(wrow0) : 0, most = any ? limit_of(wlast) : 0;
     const char* k = a.k + kv0 * a.k_stride + kvh * (HD * ESIZE<CT>);
     const char* v = a.v + kv0 * a.v_stride + kvh * (HD * ESIZE<CT>);
-    for (int t = lo; t < hi; t++) {
-        const int key0 = t * KEYS;
+    if constexpr (DIRECT) {
+        const Direct<HD> rows(a.k_stride, a.v_stride);
+        auto load = [&](int t) {
+            const int64_t key0 = (int64_t)t * KEYS;
+            rows.load(k + key0 * a.k_stride, v + key0 * a.v_stride, len - (int)key0, reinterpret_cast<char*>(s_k[t & 1]), reinterpret_cast<char*>(s_v[t & 1]));
+        };
+        if (lo < hi) load(lo);
         __syncthreads();
-        stage_rows<CT, CT, HD, false>(k + key0 * a.k_stride, v + key0 * a.v_stride, a.k_stride, a.v_stride, len - key0, s_k, s_v);
-        __syncthreads();
-        if (key0 < most) attend_tile<CT, HD>(r, q, s_k, s_v, key0, key0 + KEYS > least);
+        for (int t = lo; t < hi; t++) {
+            if (t + 1 < hi) load(t + 1);
+            __builtin_amdgcn_sched_barrier(0);                     // (the loads go out here)
+            const int key0 = t * KEYS;
+            const char *k_tile = reinterpret_cast<const char*>(s_k[t & 1]), *v_tile = reinterpret_cast<const char*>(s_v[t & 1]);
+            if (key0 < most)
+                attend_tile<CT, HD>(r, q, [&](int kt, int st) { return rows.keys(k_tile, kt, st); },
+                                    [&](int vs, int ct) { return rows.values(v_tile, vs, ct); }, key0, key0 + KEYS > least);
+            __syncthreads();                                       // the next tile is there, this one is free
+        }
+    } else {
+        for (int t = lo; t < hi; t++) {
+            const int key0 = t * KEYS;
+            __syncthreads();
+            stage_rows<CT, CT, HD, false>(k + key0 * a.k_stride, v + key0 * a.v_stride, a.k_stride, a.v_stride, len - key0, s_k[0], s_v[0]);
+            __syncthreads();
+            if (key0 < most) attend_staged<CT, HD>(r, q, s_k[0], s_v[0], key0, key0 + KEYS > least);
+        }
     }
     store_rows<CT, HD>(r, p, a.rep, a.Hq, kvh, wave, split, a.splits, a.splits > 1, a.out);
 }
@@ -602,7 +691,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_shared(SharedArgs a)
             __syncthreads();
 #pragma unroll
             for (int n = 0; n < COLS; n++) r.limit[n] = len[c];
-            if (any) attend_tile<CT, HD>(r, q, s_k, s_v, key0, key0 + KEYS > len[c]);
+            if (any) attend_staged<CT, HD>(r, q, s_k, s_v, key0, key0 + KEYS > len[c]);
         }
         done += tiles[c];
     };
@@ -629,7 +718,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_shared(SharedArgs a)
             __syncthreads();
 #pragma unroll
             for (int n = 0; n < COLS; n++) r.limit[n] = len[3];
-            if (any) attend_tile<CR, HD>(r, q, s_k, s_v, key0, key0 + KEYS > len[3]);
+            if (any) attend_staged<CR, HD>(r, q, s_k, s_v, key0, key0 + KEYS > len[3]);
         }
     }
     store_rows<QT, HD>(r, p, a.rep, a.Hq, kvh, wave, split, a.splits, true, a.out);
