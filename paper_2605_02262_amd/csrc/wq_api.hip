@@ -386,6 +386,13 @@ int wq_decode_attention(wq_ctx* ctx, const void* q, int q_dtype, int B, int Hq, 
 
 static bool on_16_bytes(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
+static bool aligned_cache(const wq_packed_kv* kv)
+{
+    bool ok = on_16_bytes(kv->k16) && on_16_bytes(kv->v16);
+    for (int c = 0; c < 3; c++) ok = ok && on_16_bytes(kv->codes[c]) && on_16_bytes(kv->meta[c]);
+    return ok;
+}
+
 // rows of H heads of hd elements, `stride` elements apart
 static int check_rows(wq_ctx* ctx, const char* name, const void* p, int64_t stride, int64_t rows, int H, int hd, int dtype)
 {
@@ -500,6 +507,8 @@ int wq_prefill_attention(wq_ctx* ctx, const void* q, int64_t q_stride, const voi
     if (rc == WQ_OK) rc = check_rows(ctx, "k", k, k_stride, total_kv, Hkv, hd, dtype);
     if (rc == WQ_OK) rc = check_rows(ctx, "v", v, v_stride, total_kv, Hkv, hd, dtype);
     if (rc != WQ_OK) return rc;
+    if (total_kv > 0 && (k_stride > 1 << 22 || v_stride > 1 << 22))       // (offsets inside a tile have 32 bits)
+        return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "rows of k or v are more than 2^22 elements apart");
     const int splits = num_splits > 0 ? num_splits : wq_prefill_splits(total_q, B, Hq, Hkv, max_kv_rows);
     if (ctx->ws_bytes < WQ_WS_HEADER + wq_prefill_ws_bytes(total_q, Hq, hd, splits) || !ctx->ws)
         return wq_fail(ctx, WQ_ERR_WORKSPACE, "workspace too small for %d splits of %lld rows", splits, (long long)total_q);
@@ -510,8 +519,13 @@ int wq_prefill_attention(wq_ctx* ctx, const void* q, int64_t q_stride, const voi
 size_t wq_shared_workspace_bytes(int B, int P, int Hq, int Hkv, int hd, int64_t max_prefix_tokens, int64_t max_own_tokens, int num_splits)
 {
     if (B <= 0 || P <= 0 || Hq <= 0 || Hkv <= 0 || hd <= 0 || Hq % Hkv != 0) return WQ_WS_HEADER;
-    const int splits = num_splits > 0 ? num_splits : wq_shared_splits(B, P, Hq, Hkv, max_prefix_tokens);
-    return WQ_WS_HEADER + wq_decode_ws_bytes(B, Hq, hd, wq_auto_splits(B, Hkv, max_own_tokens)) + wq_shared_ws_bytes(B, Hq, hd, splits);
+    size_t most = 0;                                              // over the queries' types, with and without own caches
+    for (int dtype : {WQ_F32, WQ_BF16})
+        for (bool own : {false, true}) {
+            const size_t n = wq_shared_plan(B, P, Hq, Hkv, hd, dtype, max_prefix_tokens, max_own_tokens, own, num_splits).bytes;
+            if (n > most) most = n;
+        }
+    return WQ_WS_HEADER + most;
 }
 
 int wq_decode_attention_shared(wq_ctx* ctx, const void* q, int q_dtype, int B, int Hq, const wq_packed_kv* prefix, const int32_t* req_off,
@@ -530,33 +544,33 @@ int wq_decode_attention_shared(wq_ctx* ctx, const void* q, int q_dtype, int B, i
         return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "Hq=%d must be a multiple of Hkv=%d, at most %d query heads per KV head", Hq, prefix->Hkv, WQ_MAX_REP);
     if ((q_dtype == WQ_BF16) != (prefix->dtype16 == WQ_BF16))
         return wq_fail(ctx, WQ_ERR_ARG, "dtype16 must be bf16 for bf16 queries and fp16 for fp16/fp32 queries");
-    for (const void* p : {q, static_cast<const void*>(out), static_cast<const void*>(prefix->k16), static_cast<const void*>(prefix->v16)})
-        if (!on_16_bytes(p)) return wq_fail(ctx, WQ_ERR_ARG, "q, out, k16 and v16 must be 16-byte aligned");
-    for (int c = 0; c < 3; c++)
-        if (!on_16_bytes(prefix->codes[c]) || !on_16_bytes(prefix->meta[c])) return wq_fail(ctx, WQ_ERR_ARG, "class %d is not 16-byte aligned", c);
+    if (!on_16_bytes(q) || !on_16_bytes(out)) return wq_fail(ctx, WQ_ERR_ARG, "q and out must be 16-byte aligned");
+    if (!aligned_cache(prefix)) return wq_fail(ctx, WQ_ERR_ARG, "the shared cache's buffers must be 16-byte aligned");
     if (num_splits < 0 || num_splits > WQ_MAX_ATTEND_SPLITS) return wq_fail(ctx, WQ_ERR_ARG, "num_splits out of range");
     if (!(sm_scale > 0.0f) || sm_scale > 3.0e38f) return wq_fail(ctx, WQ_ERR_ARG, "sm_scale must be positive and finite");
     if (own) {
         rc = check_packed(ctx, own, B, true);
         if (rc != WQ_OK) return rc;
+        if (!aligned_cache(own)) return wq_fail(ctx, WQ_ERR_ARG, "the requests' own cache's buffers must be 16-byte aligned");
         if (own->Hkv != prefix->Hkv || own->hd != prefix->hd || own->dtype16 != prefix->dtype16)
             return wq_fail(ctx, WQ_ERR_ARG, "the shared and the requests' own cache differ in Hkv, hd or dtype16");
     }
     if (B == 0) return WQ_OK;
     if (!q || !out || !req_off) return wq_fail(ctx, WQ_ERR_ARG, "NULL q, out or req_off");
-    const int splits = num_splits > 0 ? num_splits : wq_shared_splits(B, prefix->B, Hq, prefix->Hkv, max_prefix_tokens);
-    const size_t own_bytes = own ? wq_decode_ws_bytes(B, Hq, own->hd, wq_auto_splits(B, own->Hkv, max_own_tokens)) : 0;
-    if (!ctx->ws || ctx->ws_bytes < WQ_WS_HEADER + own_bytes + wq_shared_ws_bytes(B, Hq, prefix->hd, splits))
-        return wq_fail(ctx, WQ_ERR_WORKSPACE, "workspace too small for %d splits of %d requests", splits, B);
+    const WqSharedPlan plan = wq_shared_plan(B, prefix->B, Hq, prefix->Hkv, prefix->hd, q_dtype, max_prefix_tokens, max_own_tokens, own != nullptr, num_splits);
+    if (((int64_t)B * (Hq / prefix->Hkv) / 64 + prefix->B) * prefix->Hkv * plan.splits + (int64_t)B * prefix->Hkv * plan.own_splits > INT32_MAX)
+        return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "too many workgroups");
+    if (!ctx->ws || ctx->ws_bytes < WQ_WS_HEADER + plan.bytes)
+        return wq_fail(ctx, WQ_ERR_WORKSPACE, "workspace too small for %d splits of %d requests", plan.splits, B);
     // an fp32 query's own cache in fp32 arithmetic, like its shared one
     const int algo = q_dtype == WQ_F32 ? WQ_DECODE_GENERIC : WQ_DECODE_AUTO;
-    int own_splits = 0;
-    if (own) {
+    int decode_splits = 0;
+    if (own && !plan.own_inside) {
         int64_t longest = 0;
-        rc = check_decode(ctx, q, q_dtype, B, Hq, own, sm_scale, &own_splits, max_own_tokens, algo, static_cast<const float*>(out), &longest);
+        rc = check_decode(ctx, q, q_dtype, B, Hq, own, sm_scale, &decode_splits, max_own_tokens, algo, static_cast<const float*>(out), &longest);
         if (rc != WQ_OK) return rc;
     }
-    return wq_launch_shared(ctx, {q, q_dtype, B, Hq, splits, prefix, own, req_off, sm_scale, own_splits, algo, own_bytes, out, lse});
+    return wq_launch_shared(ctx, {q, q_dtype, B, Hq, prefix, own, req_off, sm_scale, plan, decode_splits, algo, out, lse});
 }
 
 // ---- the entry point that allocates nothing ---------------------------------------------------------------------

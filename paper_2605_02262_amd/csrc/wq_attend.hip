@@ -31,9 +31,9 @@ struct Bf16 {};
 struct F16 {};
 struct F32 {};
 
-constexpr int WAVES = 4, COLS = 2;                 // wavefronts per workgroup, 16-row columns per wavefront
-constexpr int ROWS = WAVES * COLS * 16;            // query rows of a workgroup
-constexpr int KEYS = 64;                           // keys of a tile
+constexpr int COLS = 2;                            // 16-row columns of a wavefront
+constexpr int KEYS = 64;                           // keys of a staged tile
+constexpr int HALF = 32;                           // keys of a step
 constexpr float LOG2E = 1.44269504088896340736f;
 // The reference of a row's exponents moves only when a logit exceeds it by 2^SLACK; weights are kept 2^SHIFT too large, so that
 // in fp16 one is lost only below 2^-34 of the largest (SHIFT + SLACK < 16).
@@ -41,11 +41,11 @@ constexpr float SLACK = 5.f, SHIFT = 10.f;
 
 template <typename CT> constexpr int ESIZE = std::is_same_v<CT, F32> ? 4 : 2;
 template <typename CT, int HD> constexpr int STEPS = HD * ESIZE<CT> / 64;          // products of a key tile: 32 (16) channels each
-template <typename CT> constexpr int VSTEPS = KEYS * ESIZE<CT> / 64;               // products over a tile's keys: 32 (16) keys each
-template <typename CT, int HD> constexpr int K_PIECES = KEYS / 16 * STEPS<CT, HD> * 64;     // 16-byte pieces of a staged key tile
-template <typename CT, int HD> constexpr int V_PIECES = VSTEPS<CT> * (HD / 16) * 64;
-
-template <typename CT, int HD> using Query = u4[COLS][STEPS<CT, HD>];             // B operands of a wavefront's rows
+template <typename CT> constexpr int VSTEPS = HALF * ESIZE<CT> / 64;               // products over a step's keys: 32 (16) keys each
+template <typename CT, int HD> constexpr int TILE_BYTES = KEYS * HD * ESIZE<CT>;   // a staged tile of keys, or of values
+template <typename CT, int HD> using Query = u4[COLS][STEPS<CT, HD>];              // B operands of a wavefront's rows
+typedef __attribute__((address_space(3))) char* Lds;
+typedef __attribute__((address_space(3))) u4* Lds4;
 
 template <typename CT>
 __device__ __forceinline__ f4 product(u4 a, u4 b, f4 c)
@@ -72,8 +72,6 @@ __device__ __forceinline__ uint32_t pack2(float x, float y, F16)
     typedef _Float16 h2 __attribute__((ext_vector_type(2)));
     return __builtin_bit_cast(uint32_t, h2{(_Float16)x, (_Float16)y});
 }
-// a value of a packed group: rounding of the group's scale can carry its largest value past fp16's range
-__device__ __forceinline__ float in_range(float x) { return fminf(fmaxf(x, -65504.f), 65504.f); }
 
 // ---- a wavefront's part of the arithmetic ------------------------------------------------------------------------------
 template <int HD>
@@ -97,6 +95,9 @@ __device__ __forceinline__ void clear(Rows<HD>& r)
     }
 }
 
+// (a scalar: what follows from it is one branch for the wavefront, not a mask)
+__device__ __forceinline__ int this_wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+
 __device__ __forceinline__ float max_of_column(float x)
 {
     x = fmaxf(x, __shfl_xor(x, 16, 64));
@@ -108,14 +109,31 @@ __device__ __forceinline__ float sum_of_column(float x)
     return x + __shfl_xor(x, 32, 64);
 }
 
-// keys(t, st), values(vs, ct): this lane's part of the A operands
-template <typename CT, int HD, typename Keys, typename Values>
-__device__ __forceinline__ void attend_tile(Rows<HD>& r, const Query<CT, HD>& q, const Keys& keys, const Values& values, int key0, bool masked)
+// The order in which a step's weights go into the value product's operand: register e holds the weights of the keys first(e) and
+// second(e) of the lane's eight (its four of the first 16 keys, then of the second).  Free, as long as the values' operand has the
+// same: a packed class is expanded fastest with the pairs that its masks leave in the two halves of a register.
+struct Natural {
+    static constexpr int first(int e) { return 2 * e; }
+    static constexpr int second(int e) { return 2 * e + 1; }
+};
+struct Far {                   // 2- and 4-bit codes
+    static constexpr int first(int e) { return e; }
+    static constexpr int second(int e) { return e + 4; }
+};
+struct Near {                  // 8-bit codes
+    static constexpr int first(int e) { return 4 * (e >> 1) + (e & 1); }
+    static constexpr int second(int e) { return first(e) + 2; }
+};
+
+// One step: 32 keys.  keys(t, st), values(vs, ct): this lane's part of the A operands
+template <typename CT, int HD, typename Order, typename Keys, typename Values>
+__device__ __forceinline__ void attend(Rows<HD>& r, const Query<CT, HD>& q, const Keys& keys, const Values& values, int key0, bool masked)
 {
     const int lane = threadIdx.x & 63;
-    f4 s[KEYS / 16][COLS];
+    constexpr int T = HALF / 16;
+    f4 s[T][COLS];
 #pragma unroll
-    for (int t = 0; t < KEYS / 16; t++) {
+    for (int t = 0; t < T; t++) {
 #pragma unroll
         for (int n = 0; n < COLS; n++) s[t][n] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -130,7 +148,7 @@ __device__ __forceinline__ void attend_tile(Rows<HD>& r, const Query<CT, HD>& q,
 #pragma unroll
         for (int n = 0; n < COLS; n++)
 #pragma unroll
-            for (int t = 0; t < KEYS / 16; t++)
+            for (int t = 0; t < T; t++)
 #pragma unroll
                 for (int i = 0; i < 4; i++)
                     if (k0 + 16 * t + i >= r.limit[n]) s[t][n][i] = -INFINITY;
@@ -141,7 +159,7 @@ __device__ __forceinline__ void attend_tile(Rows<HD>& r, const Query<CT, HD>& q,
     for (int n = 0; n < COLS; n++) {
         float m = s[0][n][0];
 #pragma unroll
-        for (int t = 0; t < KEYS / 16; t++)
+        for (int t = 0; t < T; t++)
 #pragma unroll
             for (int i = 0; i < 4; i++) m = fmaxf(m, s[t][n][i]);
         most[n] = m * r.scale[n];
@@ -158,25 +176,22 @@ __device__ __forceinline__ void attend_tile(Rows<HD>& r, const Query<CT, HD>& q,
             for (int ct = 0; ct < HD / 16; ct++) r.o[ct][n] *= by;
         }
     }
-    constexpr int PER = ESIZE<CT> == 2 ? 8 : 4;       // keys of a lane per product
     u4 p[VSTEPS<CT>][COLS];
 #pragma unroll
     for (int n = 0; n < COLS; n++) {
         const float shift = r.ref[n] == -INFINITY ? 0.f : SHIFT - r.ref[n];
+        float w[8];
 #pragma unroll
-        for (int vs = 0; vs < VSTEPS<CT>; vs++) {
-            float w[PER];
+        for (int e = 0; e < 8; e++) {
+            w[e] = __builtin_amdgcn_exp2f(fmaf(s[e >> 2][n][e & 3], r.scale[n], shift));
+            r.sum[n] += w[e];
+        }
+        if constexpr (ESIZE<CT> == 2) {
 #pragma unroll
-            for (int e = 0; e < PER; e++) {
-                const int t = vs * PER / 4 + e / 4;
-                w[e] = __builtin_amdgcn_exp2f(fmaf(s[t][n][e & 3], r.scale[n], shift));
-                r.sum[n] += w[e];
-            }
+            for (int e = 0; e < 4; e++) p[0][n][e] = pack2(w[Order::first(e)], w[Order::second(e)], CT());
+        } else {
 #pragma unroll
-            for (int e = 0; e < 4; e++) {
-                if constexpr (ESIZE<CT> == 2) p[vs][n][e] = pack2(w[2 * e], w[2 * e + 1], CT());
-                else p[vs][n][e] = __float_as_uint(w[e]);
-            }
+            for (int e = 0; e < 8; e++) p[e >> 2][n][e & 3] = __float_as_uint(w[e]);
         }
     }
 #pragma unroll
@@ -189,25 +204,28 @@ __device__ __forceinline__ void attend_tile(Rows<HD>& r, const Query<CT, HD>& q,
         }
 }
 
-// ... from a tile staged in the operands' order
-template <typename CT, int HD>
-__device__ __forceinline__ void attend_staged(Rows<HD>& r, const Query<CT, HD>& q, const u4* __restrict__ k_tile, const u4* __restrict__ v_tile, int key0,
-                                              bool masked)
+// The two steps of a tile staged in the operands' order, [step][lane][16 bytes]
+template <typename CT, int HD, typename Order>
+__device__ __forceinline__ void attend_staged(Rows<HD>& r, const Query<CT, HD>& q, Lds4 k_tile, Lds4 v_tile, int key0, int least, int most)
 {
     const int lane = threadIdx.x & 63;
-    attend_tile<CT, HD>(r, q, [&](int t, int st) { return k_tile[(t * STEPS<CT, HD> + st) * 64 + lane]; },
-                        [&](int vs, int ct) { return v_tile[(vs * (HD / 16) + ct) * 64 + lane]; }, key0, masked);
+#pragma unroll
+    for (int h = 0; h < KEYS / HALF; h++) {
+        auto keys = [&](int t, int st) { return k_tile[((2 * h + t) * STEPS<CT, HD> + st) * 64 + lane]; };
+        auto values = [&](int vs, int ct) { return v_tile[((h * VSTEPS<CT> + vs) * (HD / 16) + ct) * 64 + lane]; };
+        if (key0 + HALF * h < most) attend<CT, HD, Order>(r, q, keys, values, key0 + HALF * h, key0 + HALF * (h + 1) > least);
+    }
 }
 
-// ---- staging: plain rows -----------------------------------------------------------------------------------------------
-// 16 bytes of elements of type CT from a row that holds elements of type ST
-template <typename CT, typename ST>
+// ---- plain rows, fp32 arithmetic: through registers --------------------------------------------------------------------
+// 16 bytes of fp32 from a row that holds elements of type ST
+template <typename ST>
 __device__ __forceinline__ u4 row_piece(const char* p)
 {
-    if constexpr (std::is_same_v<CT, ST>) {
+    if constexpr (std::is_same_v<ST, F32>) {
         return *reinterpret_cast<const u4*>(p);
-    } else {                                           // fp16 rows, fp32 arithmetic
-        static_assert(std::is_same_v<CT, F32> && std::is_same_v<ST, F16>, "");
+    } else {
+        static_assert(std::is_same_v<ST, F16>, "");
         const uint2 u = *reinterpret_cast<const uint2*>(p);
         u4 r;
         r[0] = __float_as_uint(wq_f16_bits_to_float(u.x & 0xFFFF)), r[1] = __float_as_uint(wq_f16_bits_to_float(u.x >> 16));
@@ -216,84 +234,46 @@ __device__ __forceinline__ u4 row_piece(const char* p)
     }
 }
 
-// Where the c-th 16-byte piece of a head's channels lies in the products: in the packed cache's order (a lane group holds a
-// quarter of the channels) or the rows' (a step holds neighbouring channels).
-template <int NSTEPS, bool QUARTERS>
-__device__ __forceinline__ void place_of(int c, int& step, int& group)
+// n rows from k, v (stride: bytes from row to row), KEYS at most; the tile's other rows become zeros.  The c-th 4 channels of a row are part of
+// product c / 4, lane group c % 4; four keys of four channels are transposed by naming registers.
+template <typename ST, int HD, int W>
+__device__ void stage_rows(const char* k, const char* v, int64_t k_stride, int64_t v_stride, int n, Lds4 k_tile, Lds4 v_tile)
 {
-    if constexpr (QUARTERS) {
-        group = c / NSTEPS;
-        step = c % NSTEPS;
-    } else {
-        step = c / 4;
-        group = c % 4;
-    }
-}
-
-// n <= KEYS rows from k, v (stride: bytes from row to row); the tile's other rows become zeros
-template <typename CT, typename ST, int HD, bool QUARTERS>
-__device__ void stage_rows(const char* k, const char* v, int64_t k_stride, int64_t v_stride, int n, u4* __restrict__ k_tile, u4* __restrict__ v_tile)
-{
-    constexpr int PIECES = HD * ESIZE<CT> / 16;        // of a row
-    constexpr int PB = 16 / ESIZE<CT> * ESIZE<ST>;     // bytes of a piece in memory
+    constexpr int PIECES = HD / 4, PB = 4 * ESIZE<ST>;
     const int tid = threadIdx.x;
 #pragma unroll 4
-    for (int u = tid; u < KEYS * PIECES; u += 64 * WAVES) {
+    for (int u = tid; u < KEYS * PIECES; u += 64 * W) {
         const int row = u / PIECES, c = u % PIECES;
-        int step, group;
-        place_of<STEPS<CT, HD>, QUARTERS>(c, step, group);
         u4 x = {0, 0, 0, 0};
-        if (row < n) x = row_piece<CT, ST>(k + row * k_stride + c * PB);
-        k_tile[((row >> 4) * STEPS<CT, HD> + step) * 64 + 16 * group + (row & 15)] = x;
+        if (row < n) x = row_piece<ST>(k + row * k_stride + c * PB);
+        k_tile[((row >> 4) * STEPS<F32, HD> + (c >> 2)) * 64 + 16 * (c & 3) + (row & 15)] = x;
     }
-    if constexpr (ESIZE<CT> == 2) {
-        // 8 keys x 8 channels are transposed in registers
-        for (int u = tid; u < KEYS / 8 * PIECES; u += 64 * WAVES) {
-            const int c = u % PIECES, jj = u / PIECES % 4, blk = u / PIECES / 4;
-            u4 x[8];
+    for (int u = tid; u < KEYS / 4 * PIECES; u += 64 * W) {
+        const int c = u % PIECES, jj = u / PIECES % 4, t16 = u / PIECES / 4;
+        u4 x[4];
 #pragma unroll
-            for (int t = 0; t < 8; t++) {
-                const int row = 32 * blk + 16 * (t >> 2) + 4 * jj + (t & 3);
-                x[t] = u4{0, 0, 0, 0};
-                if (row < n) x[t] = row_piece<CT, ST>(v + row * v_stride + c * PB);
-            }
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                u4 y;
-#pragma unroll
-                for (int w = 0; w < 4; w++)
-                    y[w] = __builtin_amdgcn_perm(x[2 * w + 1][i >> 1], x[2 * w][i >> 1], (i & 1) ? 0x07060302 : 0x05040100);
-                const int ch = 8 * c + i;
-                v_tile[(blk * (HD / 16) + (ch >> 4)) * 64 + 16 * jj + (ch & 15)] = y;
-            }
+        for (int t = 0; t < 4; t++) {
+            const int row = 16 * t16 + 4 * jj + t;
+            x[t] = u4{0, 0, 0, 0};
+            if (row < n) x[t] = row_piece<ST>(v + row * v_stride + c * PB);
         }
-    } else {
-        for (int u = tid; u < KEYS / 4 * PIECES; u += 64 * WAVES) {
-            const int c = u % PIECES, jj = u / PIECES % 4, t16 = u / PIECES / 4;
-            u4 x[4];
 #pragma unroll
-            for (int t = 0; t < 4; t++) {
-                const int row = 16 * t16 + 4 * jj + t;
-                x[t] = u4{0, 0, 0, 0};
-                if (row < n) x[t] = row_piece<CT, ST>(v + row * v_stride + c * PB);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const int ch = 4 * c + i;
-                v_tile[(t16 * (HD / 16) + (ch >> 4)) * 64 + 16 * jj + (ch & 15)] = u4{x[0][i], x[1][i], x[2][i], x[3][i]};
-            }
+        for (int i = 0; i < 4; i++) {
+            const int ch = 4 * c + i;
+            v_tile[(t16 * (HD / 16) + (ch >> 4)) * 64 + 16 * jj + (ch & 15)] = u4{x[0][i], x[1][i], x[2][i], x[3][i]};
         }
     }
 }
 
-// ---- staging: plain rows of a 16-bit type, from memory to LDS without registers between ----------------------------------
+// ---- plain rows of a 16-bit type: from memory to LDS without registers between ------------------------------------------
 // A load of 16 bytes per lane lands in LDS at 16 bytes per lane in the lanes' order, so a tile lies there row by row.  What is free
 // is which 16 bytes of its row a lane takes: piece c of row r goes to place c ^ f(r), so that the products' reads, which go down
 // the rows, meet all banks.  Values are read with the transposing load: 16 lanes give the addresses of 4 rows x 16 channels and
 // get 4 rows of one channel each.
-template <int HD>
+template <int HD, int W, int KT>               // KT: keys of a tile
 struct Direct {
-    static constexpr int PIECES = HD / 8, PER_LOAD = 64 * WAVES / PIECES, LOADS = KEYS / PER_LOAD;      // rows of one load of the workgroup
+    static constexpr int PIECES = HD / 8, PER_LOAD = 64 * W / PIECES, LOADS = KT / PER_LOAD;      // rows of one load of the workgroup
+    static_assert(KT % PER_LOAD == 0, "");
     uint32_t k_off, v_off, k_step, v_step;     // this lane's offset in a tile, and from load to load
     int row;
     uint32_t k_piece, v_piece, k_stride, v_stride;
@@ -315,42 +295,72 @@ struct Direct {
     static __device__ __forceinline__ int swizzle(int r) { return HD == 128 ? r & 15 : (r >> 1) & 7; }
 
     // rows from k, v on, n of them (the last one is read again for the rest: its weights are zero)
-    __device__ __forceinline__ void load(const char* k, const char* v, int n, char* k_tile, char* v_tile) const
+    __device__ __forceinline__ void load(const char* k, const char* v, int n, Lds k_tile, Lds v_tile) const
     {
-        const int wave = threadIdx.x >> 6;
+        const int wave = this_wave();
 #pragma unroll
         for (int i = 0; i < LOADS; i++) {
             uint32_t ko = k_off + i * k_step, vo = v_off + i * v_step;
-            if (n < KEYS) {
+            if (n < KT) {
                 const uint32_t at = row + i * PER_LOAD < n ? row + i * PER_LOAD : n - 1;
                 ko = at * k_stride + k_piece, vo = at * v_stride + v_piece;
             }
-            const int to = (i * 64 * WAVES + wave * 64) * 16;
+            const int to = (i * 64 * W + wave * 64) * 16;
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(k + ko), (__attribute__((address_space(3))) void*)(k_tile + to), 16, 0, 0);
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(v + vo), (__attribute__((address_space(3))) void*)(v_tile + to), 16, 0, 0);
         }
     }
-    __device__ __forceinline__ u4 keys(const char* k_tile, int t, int st) const
+    __device__ __forceinline__ u4 keys(Lds k_tile, int t, int st) const
     {
-        return *reinterpret_cast<const u4*>(k_tile + ((k_lds + t * 16 * (2 * HD)) ^ (64 * st)));
+        return *(const Lds4)(k_tile + ((k_lds + t * 16 * (2 * HD)) ^ (64 * st)));
     }
-    __device__ __forceinline__ u4 values(const char* v_tile, int vs, int ct) const
+    __device__ __forceinline__ u4 values(Lds v_tile, int vs, int ct) const
     {
         typedef short s4 __attribute__((ext_vector_type(4)));
         typedef __attribute__((address_space(3))) s4* lds4;
-        const char* p = v_tile + ((v_lds + vs * 32 * (2 * HD)) ^ (32 * ct));
+        const Lds p = v_tile + ((v_lds + vs * 32 * (2 * HD)) ^ (32 * ct));
         struct { s4 a, b; } x = {__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p)), __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + 16 * (2 * HD)))};
         return __builtin_bit_cast(u4, x);
     }
 };
 
-// ---- staging: a class of the packed cache ------------------------------------------------------------------------------
-template <int BITS>
-__device__ __forceinline__ float code_of(const uint32_t* w, int i)
+// Tiles lo .. hi-1 of the n rows from k, v on.  Two tiles in LDS, one is met while the next one arrives.  A wavefront's rows all see the keys
+// below `least`, none sees one from `most` on.
+template <typename CT, int HD, int W, int KT>
+__device__ __forceinline__ void walk_rows(Rows<HD>& r, const Query<CT, HD>& q, const char* k, const char* v, int64_t k_stride, int64_t v_stride, int n, int lo,
+                                          int hi, int least, int most, Lds k_lds, Lds v_lds)
 {
-    constexpr int PER = 32 / BITS;
-    return (float)((w[i / PER] >> (i % PER * BITS)) & ((1u << BITS) - 1));
+    constexpr int BYTES = KT * HD * 2;
+    const Direct<HD, W, KT> rows(k_stride, v_stride);
+    auto load = [&](int t) {
+        const int64_t key0 = (int64_t)t * KT;
+        rows.load(k + key0 * k_stride, v + key0 * v_stride, n - (int)key0, k_lds + (t & 1) * BYTES, v_lds + (t & 1) * BYTES);
+    };
+    __syncthreads();                                           // (whatever was in LDS before has been read)
+    if (lo < hi) load(lo);
+    __syncthreads();
+    for (int t = lo; t < hi; t++) {
+        if (t + 1 < hi) load(t + 1);
+        __builtin_amdgcn_sched_barrier(0);                     // (the loads go out here)
+        const Lds k_tile = k_lds + (t & 1) * BYTES, v_tile = v_lds + (t & 1) * BYTES;
+#pragma unroll
+        for (int h = 0; h < KT / HALF; h++) {
+            const int key0 = t * KT + h * HALF;
+            auto keys = [&](int kt, int st) { return rows.keys(k_tile, 2 * h + kt, st); };
+            auto values = [&](int, int ct) { return rows.values(v_tile, h, ct); };
+            if (key0 < most) attend<CT, HD, Natural>(r, q, keys, values, key0, key0 + HALF > least);
+        }
+        __syncthreads();                                       // the next tile is there, this one is free
+    }
 }
+
+// ---- a class of the packed cache -----------------------------------------------------------------------------------------
+// Token slots from slots_left on (a multiple of 32) are not the sequence's: they become zeros, because a weight of zero times
+// whatever lies there need not be zero.
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100); }
+__device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302); }
+
 template <int BYTES>
 __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* w)
 {
@@ -369,96 +379,193 @@ __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* w)
     }
 }
 
-// The 64 token slots from tok0 (a multiple of 32) of class BITS.  Slots from slots_left on (a multiple of 32) are not the sequence's: they become zeros,
-// because a weight of zero times whatever lies there need not be zero.
-template <typename CT, int HD, int BITS>
-__device__ void stage_packed(const wq_packed_kv& kv, int kvh, int64_t tok0, int64_t slots_left, u4* __restrict__ k_tile, u4* __restrict__ v_tile)
-{
-    constexpr int C = BITS == 2 ? 0 : (BITS == 4 ? 1 : 2);
-    constexpr int CT16 = HD / 16;
-    const int tid = threadIdx.x, lane = tid & 63, group = kv.group, G = HD / group;
-    const int64_t cap = kv.cap[C];
-    const uint8_t* kc = static_cast<const uint8_t*>(kv.codes[C]) + (int64_t)kvh * cap * HD * BITS / 8;
-    const uint8_t* vc = static_cast<const uint8_t*>(kv.codes[C]) + ((int64_t)kv.Hkv + kvh) * cap * HD * BITS / 8;
-    const uint32_t* km = static_cast<const uint32_t*>(kv.meta[C]) + (int64_t)kvh * cap * G;
-    const uint32_t* vm = static_cast<const uint32_t*>(kv.meta[C]) + ((int64_t)kv.Hkv + kvh) * cap * G;
-    {   // keys: thread = (16-token tile, lane of the product): a quarter of a token's channels
-        constexpr int N = HD / 4, BYTES = N * BITS / 8;
-        const int t16 = tid >> 6, m = lane & 15, j = lane >> 4;
-        uint32_t w[(BYTES + 3) / 4] = {};
-        uint32_t meta = 0;                             // (a quarter lies in one group: a group has at least 32 channels)
-        if (16 * t16 < slots_left) {
-            const int64_t tile = (tok0 >> 4) + t16;
-            load_words<BYTES>(kc + (tile * 64 + lane) * BYTES, w);
-            meta = km[(tile * G + j * N / group) * 16 + m];
-        }
-        const float s = wq_f16_bits_to_float(meta & 0xFFFF), mn = wq_f16_bits_to_float(meta >> 16);
+// The tile in flight between memory and LDS, in registers.  A key unit is a quarter of a token's channels (lane of the product), 256 of
+// them; a value unit is 8 tokens of every 16th channel of half of the head, 256 of them.  Four wavefronts take one of each per
+// lane, of eight wavefronts half take the keys and half the values.
+template <int HD, int BITS, int W>
+struct Packed {
+    static constexpr int C = BITS == 2 ? 0 : (BITS == 4 ? 1 : 2);
+    static constexpr int CT16 = HD / 16, N = HD / 4, K_BYTES = N * BITS / 8, V_CT = CT16 / 2, V_BYTES = V_CT * BITS;
+    static constexpr int VG = HD / 64;             // groups that a value unit's channels can belong to
+    uint32_t kw[(K_BYTES + 3) / 4], km, vw[(V_BYTES + 3) / 4];
+    uint4 vm[VG][2];
+
+    static __device__ __forceinline__ bool does_keys() { return W == 4 || this_wave() < 4; }
+    static __device__ __forceinline__ bool does_values() { return W == 4 || this_wave() >= 4; }
+
+    __device__ __forceinline__ void load(const wq_packed_kv& kv, int kvh, int64_t tok0, int64_t slots_left)
+    {
+        const int unit = threadIdx.x & 255, lane = unit & 63, group = kv.group, G = HD / group;
+        const int64_t cap = kv.cap[C];
+        if (does_keys()) {
+            const uint8_t* kc = static_cast<const uint8_t*>(kv.codes[C]) + (int64_t)kvh * cap * HD * BITS / 8;
+            const uint32_t* m = static_cast<const uint32_t*>(kv.meta[C]) + (int64_t)kvh * cap * G;
+            const int t16 = unit >> 6;
+            km = 0;
 #pragma unroll
-        for (int st = 0; st < STEPS<CT, HD>; st++) {
-            constexpr int E = 16 / ESIZE<CT>;
-            float x[E];
-#pragma unroll
-            for (int e = 0; e < E; e++) x[e] = in_range(fmaf(s, code_of<BITS>(w, E * st + e), mn));
-            u4 y;
-#pragma unroll
-            for (int e = 0; e < 4; e++) {
-                if constexpr (ESIZE<CT> == 2) y[e] = pack2(x[2 * e], x[2 * e + 1], CT());
-                else y[e] = __float_as_uint(x[e]);
+            for (int i = 0; i < (K_BYTES + 3) / 4; i++) kw[i] = 0;
+            if (16 * t16 < slots_left) {
+                const int64_t tile = (tok0 >> 4) + t16;
+                load_words<K_BYTES>(kc + (tile * 64 + lane) * K_BYTES, kw);
+                km = m[(tile * G + (lane >> 4) * N / group) * 16 + (lane & 15)];       // (a quarter lies in one group: a group has at least 32 channels)
             }
-            k_tile[(t16 * STEPS<CT, HD> + st) * 64 + lane] = y;
         }
-    }
-    {   // values: thread = (32-token block, half of the channels, lane of the product): 8 tokens of every 16th channel
-        constexpr int N = CT16 / 2, BYTES = N * BITS;
-        const int blk = tid >> 7, half = (tid >> 6) & 1, jj = lane >> 4;
-        uint32_t w[(BYTES + 3) / 4] = {};
-        uint32_t meta[8] = {};
-        int have = -1;
-        const bool real = 32 * blk < slots_left;
-        const int64_t block = (tok0 >> 5) + blk;
-        if (real) load_words<BYTES>(vc + (block * 64 + lane) * (CT16 * BITS) + half * BYTES, w);
+        if (does_values()) {
+            const uint8_t* vc = static_cast<const uint8_t*>(kv.codes[C]) + ((int64_t)kv.Hkv + kvh) * cap * HD * BITS / 8;
+            const uint32_t* m = static_cast<const uint32_t*>(kv.meta[C]) + ((int64_t)kv.Hkv + kvh) * cap * G;
+            const int blk = unit >> 7, half = (unit >> 6) & 1, jj = lane >> 4;
 #pragma unroll
-        for (int i = 0; i < N; i++) {
-            const int ct = half * N + i, g = ct * 16 / group;
-            if (real && g != have) {
-                const uint4 a = *reinterpret_cast<const uint4*>(vm + ((2 * block) * G + g) * 16 + 4 * jj);
-                const uint4 b = *reinterpret_cast<const uint4*>(vm + ((2 * block + 1) * G + g) * 16 + 4 * jj);
-                meta[0] = a.x, meta[1] = a.y, meta[2] = a.z, meta[3] = a.w;
-                meta[4] = b.x, meta[5] = b.y, meta[6] = b.z, meta[7] = b.w;
-                have = g;
-            }
-            float x[8];
+            for (int i = 0; i < (V_BYTES + 3) / 4; i++) vw[i] = 0;
 #pragma unroll
-            for (int t = 0; t < 8; t++)
-                x[t] = in_range(fmaf(wq_f16_bits_to_float(meta[t] & 0xFFFF), code_of<BITS>(w, 8 * i + t), wq_f16_bits_to_float(meta[t] >> 16)));
-            if constexpr (ESIZE<CT> == 2) {
-                v_tile[(blk * CT16 + ct) * 64 + lane] = u4{pack2(x[0], x[1], CT()), pack2(x[2], x[3], CT()), pack2(x[4], x[5], CT()), pack2(x[6], x[7], CT())};
-            } else {
+            for (int g = 0; g < VG; g++) vm[g][0] = vm[g][1] = make_uint4(0, 0, 0, 0);
+            if (32 * blk < slots_left) {
+                const int64_t block = (tok0 >> 5) + blk;
+                load_words<V_BYTES>(vc + (block * 64 + lane) * (CT16 * BITS) + half * V_BYTES, vw);
 #pragma unroll
-                for (int h = 0; h < 2; h++)
-                    v_tile[((2 * blk + h) * CT16 + ct) * 64 + lane] =
-                        u4{__float_as_uint(x[4 * h]), __float_as_uint(x[4 * h + 1]), __float_as_uint(x[4 * h + 2]), __float_as_uint(x[4 * h + 3])};
+                for (int g = 0; g < VG; g++) {
+                    const int64_t of = (half * (HD / 2) + 32 * g) / group;
+                    vm[g][0] = *reinterpret_cast<const uint4*>(m + ((2 * block) * G + of) * 16 + 4 * jj);
+                    vm[g][1] = *reinterpret_cast<const uint4*>(m + ((2 * block + 1) * G + of) * 16 + 4 * jj);
+                }
             }
         }
     }
-}
+
+    // Field f of both halves of w as fp16: placed in the significand of a power of two, which is then taken away (exact)
+    template <int AT>
+    static __device__ __forceinline__ uint32_t placed(uint32_t w)
+    {
+        constexpr uint32_t MASK = ((1u << BITS) - 1) << AT, ONE = (25u - AT) << 10;      // 2^(10 - AT)
+        return (w & (MASK | MASK << 16)) | (ONE | ONE << 16);
+    }
+    template <int AT>
+    static __device__ __forceinline__ uint32_t value(uint32_t x, h2 s, h2 m)
+    {
+        constexpr _Float16 BIAS = (_Float16)(float)(1 << (10 - AT));
+        const h2 code = __builtin_bit_cast(h2, x) - h2{BIAS, BIAS};
+        return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(code, s, m));       // (one rounding)
+    }
+
+    // fp16 operands.  Key unit: the pairs of channels that a masked word holds, see query_pair below; value unit: the pairs of Far or Near.
+    __device__ __forceinline__ void stage(Lds4 k_tile, Lds4 v_tile) const
+    {
+        const int unit = threadIdx.x & 255, lane = unit & 63;
+        if (does_keys()) {
+            const h2 sm = __builtin_bit_cast(h2, km), s = {sm[0], sm[0]}, m = {sm[1], sm[1]};
+            Lds4 to = k_tile + (unit >> 6) * STEPS<F16, HD> * 64 + lane;
+#pragma unroll
+            for (int st = 0; st < STEPS<F16, HD>; st++) {
+                u4 y;
+                if constexpr (BITS == 8) {
+#pragma unroll
+                    for (int i = 0; i < 2; i++) {
+                        y[2 * i] = value<0>(placed<0>(kw[2 * st + i]), s, m);
+                        y[2 * i + 1] = value<0>(placed<0>(kw[2 * st + i] >> 8), s, m);
+                    }
+                } else if constexpr (BITS == 4) {
+                    const uint32_t w = kw[st], z = w >> 8;
+                    y[0] = value<0>(placed<0>(w), s, m), y[1] = value<4>(placed<4>(w), s, m);
+                    y[2] = value<0>(placed<0>(z), s, m), y[3] = value<4>(placed<4>(z), s, m);
+                } else {
+                    const uint32_t w = kw[st >> 1] >> (st & 1) * 8;
+                    y[0] = value<0>(placed<0>(w), s, m), y[1] = value<2>(placed<2>(w), s, m);
+                    y[2] = value<4>(placed<4>(w), s, m), y[3] = value<6>(placed<6>(w), s, m);
+                }
+                to[st * 64] = y;
+            }
+        }
+        if (does_values()) {
+            const int blk = unit >> 7, half = (unit >> 6) & 1;
+            Lds4 to = v_tile + (blk * CT16 + half * V_CT) * 64 + lane;
+#pragma unroll
+            for (int g = 0; g < VG; g++) {
+                h2 s[4], m[4];
+                const uint32_t t[8] = {vm[g][0].x, vm[g][0].y, vm[g][0].z, vm[g][0].w, vm[g][1].x, vm[g][1].y, vm[g][1].z, vm[g][1].w};
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    using O = std::conditional_t<BITS == 8, Near, Far>;
+                    s[e] = __builtin_bit_cast(h2, low_halves(t[O::first(e)], t[O::second(e)]));
+                    m[e] = __builtin_bit_cast(h2, high_halves(t[O::first(e)], t[O::second(e)]));
+                }
+#pragma unroll
+                for (int i = 2 * g; i < 2 * g + 2; i++) {          // 16-channel tiles of the group's 32 channels
+                    u4 y;
+                    if constexpr (BITS == 8) {
+#pragma unroll
+                        for (int k = 0; k < 2; k++) {
+                            y[2 * k] = value<0>(placed<0>(vw[2 * i + k]), s[2 * k], m[2 * k]);
+                            y[2 * k + 1] = value<0>(placed<0>(vw[2 * i + k] >> 8), s[2 * k + 1], m[2 * k + 1]);
+                        }
+                    } else if constexpr (BITS == 4) {
+                        const uint32_t w = vw[i], z = w >> 8;
+                        y[0] = value<0>(placed<0>(w), s[0], m[0]), y[1] = value<4>(placed<4>(w), s[1], m[1]);
+                        y[2] = value<0>(placed<0>(z), s[2], m[2]), y[3] = value<4>(placed<4>(z), s[3], m[3]);
+                    } else {                                       // a word holds two tiles, one per half
+                        const uint32_t w = vw[i >> 1], z = w >> 8;
+                        auto both = [&](uint32_t a, uint32_t b) { return i & 1 ? high_halves(a, b) : low_halves(a, b); };
+                        y[0] = value<0>(both(placed<0>(w), placed<0>(z)), s[0], m[0]), y[1] = value<2>(both(placed<2>(w), placed<2>(z)), s[1], m[1]);
+                        y[2] = value<4>(both(placed<4>(w), placed<4>(z)), s[2], m[2]), y[3] = value<6>(both(placed<6>(w), placed<6>(z)), s[3], m[3]);
+                    }
+                    to[i * 64] = y;
+                }
+            }
+        }
+    }
+
+    // fp32 operands, codes one by one
+    static __device__ __forceinline__ float code(const uint32_t* w, int i)
+    {
+        constexpr int PER = 32 / BITS;
+        return (float)((w[i / PER] >> (i % PER * BITS)) & ((1u << BITS) - 1));
+    }
+    __device__ __forceinline__ void stage_f32(Lds4 k_tile, Lds4 v_tile) const
+    {
+        const int unit = threadIdx.x & 255, lane = unit & 63;
+        if (does_keys()) {
+            const float s = wq_f16_bits_to_float(km & 0xFFFF), m = wq_f16_bits_to_float(km >> 16);
+#pragma unroll
+            for (int st = 0; st < STEPS<F32, HD>; st++) {
+                u4 y;
+#pragma unroll
+                for (int e = 0; e < 4; e++) y[e] = __float_as_uint(fmaf(s, code(kw, 4 * st + e), m));
+                k_tile[((unit >> 6) * STEPS<F32, HD> + st) * 64 + lane] = y;
+            }
+        }
+        if (does_values()) {
+            const int blk = unit >> 7, half = (unit >> 6) & 1;
+#pragma unroll
+            for (int i = 0; i < V_CT; i++)
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    const uint4 t = vm[i >> 1][h];
+                    const uint32_t meta[4] = {t.x, t.y, t.z, t.w};
+                    u4 y;
+#pragma unroll
+                    for (int e = 0; e < 4; e++)
+                        y[e] = __float_as_uint(fmaf(wq_f16_bits_to_float(meta[e] & 0xFFFF), code(vw, 8 * i + 4 * h + e), wq_f16_bits_to_float(meta[e] >> 16)));
+                    v_tile[((2 * blk + h) * CT16 + half * V_CT + i) * 64 + lane] = y;
+                }
+        }
+    }
+};
 
 // ---- what both kernels share -------------------------------------------------------------------------------------------
 struct Out {
     void* out;                 // [rows of q][Hq][hd]
     float* lse;                // [rows of q][Hq] or NULL
-    float* part;               // numerators of the splits [row of q * Hq + head][split][hd]
-    float* part_ml;            // their references (log2) and sums [..][split][2]
+    float* part;               // numerators of the parts [row of q * Hq + head][part][hd]
+    float* part_ml;            // their references (log2) and sums [..][part][2]
 };
 
 // The sequence that workgroup `tile` works for and its first row there.  Sequence b's rows are off[b] * rep .. off[b+1] * rep - 1
-// (a row per query head); its tiles are numbered from off[b] * rep / ROWS + b: at least as many numbers as it has tiles.
+// (a row per query head); its tiles of ROWS rows are numbered from off[b] * rep / ROWS + b: at least as many numbers as it has tiles.
 // False: nothing to do.
 struct Place {
     int seq, row0, rows;       // the tile's first row in its sequence, rows of the sequence
     int64_t first;             // first q row of the sequence
 };
 __device__ __forceinline__ int64_t clipped(int32_t x, int64_t most) { return x < 0 ? 0 : (x > most ? most : x); }
+template <int ROWS>
 __device__ __forceinline__ bool find_place(const int32_t* off, int nseq, int rep, int64_t total, int64_t tile, Place& p)
 {
     int lo = 0, hi = nseq;
@@ -473,15 +580,40 @@ __device__ __forceinline__ bool find_place(const int32_t* off, int nseq, int rep
     return true;
 }
 
-template <typename CT, typename ST, int HD, bool QUARTERS>
+// 16-byte pieces of a row's channels: those of lane group j in the rows' order (32 neighbouring channels per product)
+template <typename CT, int HD>
 __device__ __forceinline__ void load_query(Query<CT, HD>& q, int n, const char* row)
 {
     const int group = (threadIdx.x & 63) >> 4;
 #pragma unroll
-    for (int st = 0; st < STEPS<CT, HD>; st++) {
-        const int c = QUARTERS ? group * STEPS<CT, HD> + st : 4 * st + group;
-        q[n][st] = row ? row_piece<CT, ST>(row + c * (16 / ESIZE<CT> * ESIZE<ST>)) : u4{0, 0, 0, 0};
+    for (int st = 0; st < STEPS<CT, HD>; st++) q[n][st] = row ? *reinterpret_cast<const u4*>(row + (4 * st + group) * 16) : u4{0, 0, 0, 0};
+}
+// ... or a quarter of the channels, as in the packed cache
+template <typename CT, int HD>
+__device__ __forceinline__ void load_query_quarter(Query<CT, HD>& q, int n, const char* row)
+{
+    const int group = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int st = 0; st < STEPS<CT, HD>; st++) q[n][st] = row ? *reinterpret_cast<const u4*>(row + (group * STEPS<CT, HD> + st) * 16) : u4{0, 0, 0, 0};
+}
+// A quarter's pairs of channels in the order in which Packed::stage leaves a class's keys
+template <int BITS, int HD>
+__device__ __forceinline__ void order_query(Query<F16, HD>& q, int n)
+{
+    u4 y[STEPS<F16, HD>];
+#pragma unroll
+    for (int st = 0; st < STEPS<F16, HD>; st++) {
+        u4 a = q[n][st], b = a;
+        int i0 = 0, i1 = 1, j0 = 2, j1 = 3;                    // 8 bits: registers 0 with 1, 2 with 3
+        if constexpr (BITS == 4) i1 = 2, j0 = 1;               // 0 with 2, 1 with 3
+        if constexpr (BITS == 2) {                             // of two neighbouring pieces
+            a = q[n][st & ~1], b = q[n][st | 1];
+            i0 = i1 = 2 * (st & 1), j0 = j1 = i0 + 1;
+        }
+        y[st] = u4{low_halves(a[i0], b[i1]), high_halves(a[i0], b[i1]), low_halves(a[j0], b[j1]), high_halves(a[j0], b[j1])};
     }
+#pragma unroll
+    for (int st = 0; st < STEPS<F16, HD>; st++) q[n][st] = y[st];
 }
 
 // ... a bf16 query as fp16, divided by the power of two above the row's largest entry: exact down to 2^-24 of that power
@@ -507,9 +639,9 @@ __device__ __forceinline__ float query_as_f16(Query<F16, HD>& q, int n)
     return 1.0f / down;
 }
 
-// As a partial for the merge (parts), or as the result.
+// As one of several parts for the merge, or as the result (parts == 0).
 template <typename CT, int HD>
-__device__ __forceinline__ void store_rows(const Rows<HD>& r, const Place& p, int rep, int Hq, int kvh, int wave, int split, int splits, bool parts, const Out& out)
+__device__ __forceinline__ void store_rows(const Rows<HD>& r, const Place& p, int rep, int Hq, int kvh, int wave, int part, int parts, const Out& out)
 {
     const int lane = threadIdx.x & 63, group = lane >> 4;
 #pragma unroll
@@ -519,13 +651,13 @@ __device__ __forceinline__ void store_rows(const Rows<HD>& r, const Place& p, in
         if (row >= p.rows) continue;
         const int64_t at = (p.first + row / rep) * Hq + kvh * rep + row % rep;
         const float ref = r.ref[n] - SHIFT;
-        if (parts) {
-            float* to = out.part + (at * splits + split) * HD;
+        if (parts > 0) {
+            float* to = out.part + (at * parts + part) * HD;
 #pragma unroll
             for (int ct = 0; ct < HD / 16; ct++) *reinterpret_cast<f4*>(to + 16 * ct + 4 * group) = r.o[ct][n];
             if (group == 0) {
-                out.part_ml[(at * splits + split) * 2] = ref;
-                out.part_ml[(at * splits + split) * 2 + 1] = sum;
+                out.part_ml[(at * parts + part) * 2] = ref;
+                out.part_ml[(at * parts + part) * 2 + 1] = sum;
             }
             continue;
         }
@@ -554,15 +686,19 @@ struct PrefillArgs {
     Out out;
 };
 
+constexpr int PREFILL_WAVES = 4, PREFILL_KEYS = 32;
+
+// 16-bit types: three wavefronts per SIMD (168 registers), tiles of 32 keys so that three workgroups fit the LDS
 template <typename CT, int HD>
-__global__ __launch_bounds__(64 * WAVES, 2) void k_prefill(PrefillArgs a)
+__global__ __launch_bounds__(64 * PREFILL_WAVES, ESIZE<CT> == 2 ? 3 : 2) void k_prefill(PrefillArgs a)
 {
-    constexpr bool DIRECT = ESIZE<CT> == 2;                       // two tiles in LDS: one is met while the next one arrives
-    __shared__ __align__(16) u4 s_k[1 + DIRECT][K_PIECES<CT, HD>], s_v[1 + DIRECT][V_PIECES<CT, HD>];
+    constexpr int W = PREFILL_WAVES, ROWS = W * COLS * 16, KT = ESIZE<CT> == 2 ? PREFILL_KEYS : KEYS;
+    constexpr int BYTES = ESIZE<CT> == 2 ? 2 * KT * HD * 2 : TILE_BYTES<CT, HD>;
+    __shared__ __align__(16) char s_k[BYTES], s_v[BYTES];
     const int Hkv = a.Hq / a.rep, kvh = blockIdx.x % Hkv, split = blockIdx.y;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int wave = this_wave(), lane = threadIdx.x & 63;
     Place p;
-    if (!find_place(a.q_off, a.B, a.rep, a.total_q, (gridDim.x - 1 - blockIdx.x) / Hkv, p)) return;      // (the last rows see the most keys: they begin first)
+    if (!find_place<ROWS>(a.q_off, a.B, a.rep, a.total_q, (gridDim.x - 1 - blockIdx.x) / Hkv, p)) return;      // (the last rows see the most keys: they begin first)
     const int64_t kv0 = clipped(a.kv_off[p.seq], a.total_kv), kv1 = clipped(a.kv_off[p.seq + 1], a.total_kv);
     const int len = kv1 > kv0 ? (int)(kv1 - kv0) : 0;
     const int first = len - p.rows / a.rep;                       // position of the sequence's first query row
@@ -574,7 +710,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_prefill(PrefillArgs a)
         return seen > prefix ? seen : prefix;
     };
     const int last_row = (p.row0 + ROWS < p.rows ? p.row0 + ROWS : p.rows) - 1;
-    const int tiles = (limit_of(last_row) + KEYS - 1) / KEYS;
+    const int tiles = (limit_of(last_row) + KT - 1) / KT;
     const int lo = (int)((int64_t)split * tiles / a.splits), hi = (int)((int64_t)(split + 1) * tiles / a.splits);
 
     Rows<HD> r;
@@ -591,191 +727,235 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_prefill(PrefillArgs a)
             at = a.q + (p.first + row / a.rep) * a.q_stride + (kvh * a.rep + row % a.rep) * (HD * ESIZE<CT>);
             r.limit[n] = limit_of(row);
         }
-        load_query<CT, CT, HD, false>(q, n, at);
+        load_query<CT, HD>(q, n, at);
     }
     const bool any = wrow0 < p.rows;
     const int wlast = wrow0 + COLS * 16 <= p.rows ? wrow0 + COLS * 16 - 1 : p.rows - 1;
     const int least = any ? limit_of(wrow0) : 0, most = any ? limit_of(wlast) : 0;
     const char* k = a.k + kv0 * a.k_stride + kvh * (HD * ESIZE<CT>);
     const char* v = a.v + kv0 * a.v_stride + kvh * (HD * ESIZE<CT>);
-    if constexpr (DIRECT) {
-        const Direct<HD> rows(a.k_stride, a.v_stride);
-        auto load = [&](int t) {
-            const int64_t key0 = (int64_t)t * KEYS;
-            rows.load(k + key0 * a.k_stride, v + key0 * a.v_stride, len - (int)key0, reinterpret_cast<char*>(s_k[t & 1]), reinterpret_cast<char*>(s_v[t & 1]));
-        };
-        if (lo < hi) load(lo);
-        __syncthreads();
-        for (int t = lo; t < hi; t++) {
-            if (t + 1 < hi) load(t + 1);
-            __builtin_amdgcn_sched_barrier(0);                     // (the loads go out here)
-            const int key0 = t * KEYS;
-            const char *k_tile = reinterpret_cast<const char*>(s_k[t & 1]), *v_tile = reinterpret_cast<const char*>(s_v[t & 1]);
-            if (key0 < most)
-                attend_tile<CT, HD>(r, q, [&](int kt, int st) { return rows.keys(k_tile, kt, st); },
-                                    [&](int vs, int ct) { return rows.values(v_tile, vs, ct); }, key0, key0 + KEYS > least);
-            __syncthreads();                                       // the next tile is there, this one is free
-        }
+    if constexpr (ESIZE<CT> == 2) {
+        walk_rows<CT, HD, W, KT>(r, q, k, v, a.k_stride, a.v_stride, len, lo, hi, least, most, (Lds)s_k, (Lds)s_v);
     } else {
         for (int t = lo; t < hi; t++) {
-            const int key0 = t * KEYS;
+            const int key0 = t * KT;
             __syncthreads();
-            stage_rows<CT, CT, HD, false>(k + key0 * a.k_stride, v + key0 * a.v_stride, a.k_stride, a.v_stride, len - key0, s_k[0], s_v[0]);
+            stage_rows<CT, HD, W>(k + key0 * a.k_stride, v + key0 * a.v_stride, a.k_stride, a.v_stride, len - key0, (Lds4)s_k, (Lds4)s_v);
             __syncthreads();
-            if (key0 < most) attend_staged<CT, HD>(r, q, s_k[0], s_v[0], key0, key0 + KEYS > least);
+            attend_staged<CT, HD, Natural>(r, q, (Lds4)s_k, (Lds4)s_v, key0, least, most);
         }
     }
-    store_rows<CT, HD>(r, p, a.rep, a.Hq, kvh, wave, split, a.splits, a.splits > 1, a.out);
+    store_rows<CT, HD>(r, p, a.rep, a.Hq, kvh, wave, split, a.splits > 1 ? a.splits : 0, a.out);
 }
 
-// ---- wq_decode_attention_shared: the shared part --------------------------------------------------------------------------
+// ---- wq_decode_attention_shared ------------------------------------------------------------------------------------------
 struct SharedArgs {
     const char* q;                             // [B][Hq][hd]
     const int32_t* req_off;
-    int B, P, Hq, rep, splits;
+    int B, P, Hq, rep;
+    int units, splits;                         // (tile of rows, KV head) pairs of the shared caches, and the parts that each is cut into
+    int own_splits;                            // parts of a request's own cache: B * Hkv * own_splits workgroups more (0: none)
     float scale;
-    wq_packed_kv kv;
+    wq_packed_kv kv, own;
     Out out;
 };
 
-// QT: the query's type; packed tokens are walked in fp16 (fp32 for fp32 queries), 16-bit rows in the cache's own type
-template <typename QT, int HD>
-__global__ __launch_bounds__(64 * WAVES, 2) void k_shared(SharedArgs a)
+// W wavefronts of 32 rows each.  QT: the query's type; packed tokens are walked in fp16 (fp32 for fp32 queries), 16-bit rows in the
+// cache's own type.  A request's own cache is a unit of rep rows.
+template <typename QT, int HD, int W>
+__global__ __launch_bounds__(64 * W, 2) void k_shared(SharedArgs a)
 {
     using CT = std::conditional_t<std::is_same_v<QT, F32>, F32, F16>;
-    using ST = std::conditional_t<std::is_same_v<QT, Bf16>, Bf16, F16>;        // of the 16-bit rows
-    __shared__ __align__(16) u4 s_k[K_PIECES<CT, HD>], s_v[V_PIECES<CT, HD>];
-    const int Hkv = a.kv.Hkv, kvh = blockIdx.x % Hkv, split = blockIdx.y;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    constexpr bool PIPED = ESIZE<QT> == 2;
+    constexpr int ROWS = W * COLS * 16, BYTES = TILE_BYTES<CT, HD> * (1 + PIPED);
+    __shared__ __align__(16) char s_k[BYTES], s_v[BYTES];
+    const int Hkv = a.kv.Hkv, wave = this_wave(), lane = threadIdx.x & 63;
+    const bool own = (int)blockIdx.x >= a.units * a.splits;
+    const int at = own ? (int)blockIdx.x - a.units * a.splits : (int)blockIdx.x;
+    const int units = own ? a.B * Hkv : a.units, unit = at % units, split = at / units, splits = own ? a.own_splits : a.splits;
+    const int kvh = unit % Hkv;
     Place p;
-    if (!find_place(a.req_off, a.P, a.rep, a.B, blockIdx.x / Hkv, p)) return;
+    if (own) {
+        p.seq = unit / Hkv, p.first = p.seq, p.row0 = 0, p.rows = a.rep;
+    } else if (!find_place<ROWS>(a.req_off, a.P, a.rep, a.B, unit / Hkv, p)) {
+        return;
+    }
+    const wq_packed_kv& kv = own ? a.own : a.kv;
     int tiles[4], all = 0, len[4];
 #pragma unroll
     for (int c = 0; c < 4; c++) {
-        const int64_t room = c < 3 ? a.kv.cap[c] - a.kv.cls_off[c][p.seq] : a.kv.cap16 - a.kv.off16[p.seq];
-        len[c] = c < 3 ? a.kv.cls_len[c][p.seq] : a.kv.len16[p.seq];
+        const int64_t room = c < 3 ? kv.cap[c] - kv.cls_off[c][p.seq] : kv.cap16 - kv.off16[p.seq];
+        len[c] = c < 3 ? kv.cls_len[c][p.seq] : kv.len16[p.seq];
         if (len[c] > room) len[c] = (int)room;
         tiles[c] = len[c] > 0 ? (len[c] + KEYS - 1) / KEYS : 0;
         all += tiles[c];
     }
-    const int lo = (int)((int64_t)split * all / a.splits), hi = (int)((int64_t)(split + 1) * all / a.splits);
+    const int lo = (int)((int64_t)split * all / splits), hi = (int)((int64_t)(split + 1) * all / splits);
 
+    if constexpr (PIPED) __builtin_amdgcn_s_setreg(1 | 23 << 6, 1);        // MODE.FP16_OVFL: an expanded value past fp16's range becomes its largest one
     Rows<HD> r;
     Query<CT, HD> q;
     clear(r);
     const int wrow0 = p.row0 + wave * COLS * 16;
-    const char* at[COLS];
+    const char* row_at[COLS];
 #pragma unroll
     for (int n = 0; n < COLS; n++) {
         const int row = wrow0 + 16 * n + (lane & 15);
-        at[n] = row < p.rows ? a.q + ((p.first + row / a.rep) * a.Hq + kvh * a.rep + row % a.rep) * (HD * ESIZE<QT>) : nullptr;
-        r.scale[n] = a.scale;
-        if constexpr (std::is_same_v<QT, Bf16>) {
-            load_query<Bf16, Bf16, HD, true>(q, n, at[n]);
-            r.scale[n] = a.scale * query_as_f16<HD>(q, n);
-        } else {
-            load_query<CT, QT, HD, true>(q, n, at[n]);
-        }
+        row_at[n] = row < p.rows ? a.q + ((p.first + row / a.rep) * a.Hq + kvh * a.rep + row % a.rep) * (HD * ESIZE<QT>) : nullptr;
     }
-    const bool any = wrow0 < p.rows;
-    int done = 0;                              // tiles of the classes before
+    const int none = wrow0 < p.rows ? 0 : INT32_MIN;           // (a wavefront without rows only stages)
+    int done = 0;                                              // tiles of the classes before
     auto walk = [&](auto bits) __attribute__((always_inline)) {
         constexpr int BITS = decltype(bits)::value, c = BITS == 2 ? 0 : (BITS == 4 ? 1 : 2);
-        const int64_t tok0 = a.kv.cls_off[c][p.seq];
-        const int64_t slots = (len[c] + 31) / 32 * 32;
+        using Order = std::conditional_t<BITS == 8, Near, Far>;
         const int t0 = lo > done ? lo - done : 0, t1 = hi - done < tiles[c] ? hi - done : tiles[c];
-        for (int t = t0; t < t1; t++) {
-            const int key0 = t * KEYS;
-            __syncthreads();
-            stage_packed<CT, HD, BITS>(a.kv, kvh, tok0 + key0, slots - key0, s_k, s_v);
-            __syncthreads();
-#pragma unroll
-            for (int n = 0; n < COLS; n++) r.limit[n] = len[c];
-            if (any) attend_staged<CT, HD>(r, q, s_k, s_v, key0, key0 + KEYS > len[c]);
-        }
         done += tiles[c];
+        if (t0 >= t1) return;
+        const int64_t tok0 = kv.cls_off[c][p.seq], slots = (len[c] + 31) / 32 * 32;
+#pragma unroll
+        for (int n = 0; n < COLS; n++) {
+            r.limit[n] = len[c];
+            r.scale[n] = a.scale;
+            load_query_quarter<CT, HD>(q, n, row_at[n]);
+            if constexpr (std::is_same_v<QT, Bf16>) r.scale[n] = a.scale * query_as_f16<HD>(q, n);
+            if constexpr (PIPED) order_query<BITS, HD>(q, n);
+        }
+        Packed<HD, BITS, W> tile;
+        __syncthreads();                                       // (whatever was in LDS before has been read)
+        tile.load(kv, kvh, tok0 + t0 * KEYS, slots - t0 * KEYS);
+        if constexpr (PIPED) {
+            constexpr int N = TILE_BYTES<CT, HD>;
+            auto k_of = [&](int t) { return (Lds4)((Lds)s_k + (t & 1) * N); };
+            auto v_of = [&](int t) { return (Lds4)((Lds)s_v + (t & 1) * N); };
+            tile.stage(k_of(t0), v_of(t0));
+            if (t0 + 1 < t1) tile.load(kv, kvh, tok0 + (t0 + 1) * KEYS, slots - (t0 + 1) * KEYS);
+            __syncthreads();
+            for (int t = t0; t < t1; t++) {
+                if (t + 1 < t1) tile.stage(k_of(t + 1), v_of(t + 1));
+                if (t + 2 < t1) tile.load(kv, kvh, tok0 + (t + 2) * KEYS, slots - (t + 2) * KEYS);
+                __builtin_amdgcn_sched_barrier(0);             // (the loads go out here)
+                attend_staged<CT, HD, Order>(r, q, k_of(t), v_of(t), t * KEYS, len[c] + none, len[c] + none);
+                __syncthreads();
+            }
+        } else {
+            for (int t = t0; t < t1; t++) {
+                tile.stage_f32((Lds4)s_k, (Lds4)s_v);
+                __syncthreads();
+                if (t + 1 < t1) tile.load(kv, kvh, tok0 + (t + 1) * KEYS, slots - (t + 1) * KEYS);
+                __builtin_amdgcn_sched_barrier(0);
+                attend_staged<CT, HD, Natural>(r, q, (Lds4)s_k, (Lds4)s_v, t * KEYS, len[c] + none, len[c] + none);
+                __syncthreads();
+            }
+        }
     };
     walk(std::integral_constant<int, 2>());
     walk(std::integral_constant<int, 4>());
     walk(std::integral_constant<int, 8>());
     if (hi > done) {
-        using CR = std::conditional_t<std::is_same_v<QT, Bf16>, Bf16, CT>;
-        if constexpr (std::is_same_v<QT, Bf16>) {
+        const int t0 = lo > done ? lo - done : 0, t1 = hi - done;
 #pragma unroll
-            for (int n = 0; n < COLS; n++) {
-                load_query<Bf16, Bf16, HD, true>(q, n, at[n]);
-                r.scale[n] = a.scale;
+        for (int n = 0; n < COLS; n++) {
+            r.limit[n] = len[3];
+            r.scale[n] = a.scale;
+            load_query<CT, HD>(q, n, row_at[n]);
+        }
+        const int64_t row0 = kv.off16[p.seq], stride = (int64_t)Hkv * HD * 2;
+        const char* k = static_cast<const char*>(kv.k16) + row0 * stride + kvh * (HD * 2);
+        const char* v = static_cast<const char*>(kv.v16) + row0 * stride + kvh * (HD * 2);
+        if constexpr (PIPED) {
+            walk_rows<QT, HD, W, KEYS>(r, q, k, v, stride, stride, len[3], t0, t1, len[3] + none, len[3] + none, (Lds)s_k, (Lds)s_v);
+        } else {
+            for (int t = t0; t < t1; t++) {
+                const int key0 = t * KEYS;
+                __syncthreads();
+                stage_rows<F16, HD, W>(k + key0 * stride, v + key0 * stride, stride, stride, len[3] - key0, (Lds4)s_k, (Lds4)s_v);
+                __syncthreads();
+                attend_staged<CT, HD, Natural>(r, q, (Lds4)s_k, (Lds4)s_v, key0, len[3] + none, len[3] + none);
             }
         }
-        const int64_t row0 = a.kv.off16[p.seq], stride = (int64_t)a.kv.Hkv * HD * 2;
-        const char* k = static_cast<const char*>(a.kv.k16) + row0 * stride + kvh * (HD * 2);
-        const char* v = static_cast<const char*>(a.kv.v16) + row0 * stride + kvh * (HD * 2);
-        const int t0 = lo > done ? lo - done : 0;
-        for (int t = t0; t < hi - done; t++) {
-            const int key0 = t * KEYS;
-            __syncthreads();
-            stage_rows<CR, ST, HD, true>(k + key0 * stride, v + key0 * stride, stride, stride, len[3] - key0, s_k, s_v);
-            __syncthreads();
-#pragma unroll
-            for (int n = 0; n < COLS; n++) r.limit[n] = len[3];
-            if (any) attend_staged<CR, HD>(r, q, s_k, s_v, key0, key0 + KEYS > len[3]);
-        }
     }
-    store_rows<QT, HD>(r, p, a.rep, a.Hq, kvh, wave, split, a.splits, true, a.out);
+    store_rows<QT, HD>(r, p, a.rep, a.Hq, kvh, wave, own ? a.splits + split : split, a.splits + a.own_splits, a.out);
 }
 
-// ---- the splits' merge -------------------------------------------------------------------------------------------------
+// ---- the parts' merge ----------------------------------------------------------------------------------------------------
 struct CombineArgs {
     int64_t rows;              // (q row, head) pairs
-    int Hq, splits, dtype;
-    const int32_t* off;        // rows of q outside off[0] .. off[nseq] - 1 have no partials,
-    int nseq;
-    bool leave;                // ... and are left as they were
-    const float* own_out;      // NULL, or one more partial, normalised [rows][hd], with its log-sum-exp
+    int Hq, parts, dtype;
+    const int32_t* off;        // the first `grouped` parts of q rows outside off[0] .. off[nseq] - 1 were not written,
+    int nseq, grouped;
+    bool leave;                // ... and such rows are left as they were
+    const float* own_out;      // NULL, or one more part, normalised [rows][hd], with its log-sum-exp
     const float* own_lse;
     Out out;
 };
 
-// A wavefront per row; a lane takes one or two channels.
+__device__ __forceinline__ float wave_max(float x)
+{
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, 64));
+    return x;
+}
+__device__ __forceinline__ float wave_sum(float x)
+{
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+    return x;
+}
+
+// A wavefront per row.  A lane finds the weights of two parts; then HD / 4 lanes take a part's numerators, 16 bytes each, the wavefront's
+// groups of lanes every second (fourth) part, four in flight: part by part the loads' round trips were the whole call.
 template <int HD>
 __global__ __launch_bounds__(256) void k_attend_combine(CombineArgs a)
 {
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    constexpr int LANES = HD / 4, GROUPS = 64 / LANES, FLIGHT = 4;
+    const int64_t row = (int64_t)blockIdx.x * 4 + this_wave();
     if (row >= a.rows) return;
-    const int lane = threadIdx.x & 63;
-    int n = a.splits;
+    const int lane = threadIdx.x & 63, group = lane / LANES, c = lane % LANES;
     const int64_t b = row / a.Hq;
-    if (b < a.off[0] || b >= a.off[a.nseq]) {
-        if (a.leave) return;
-        n = 0;
+    const bool grouped = b >= a.off[0] && b < a.off[a.nseq];
+    if (!grouped && a.leave) return;
+    const int from = grouped ? 0 : a.grouped;
+    float m[2], l[2], w[2];
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+        const int s = 64 * i + lane;
+        const bool have = s >= from && s < a.parts;
+        m[i] = have ? a.out.part_ml[(row * a.parts + s) * 2] : -INFINITY;
+        l[i] = have ? a.out.part_ml[(row * a.parts + s) * 2 + 1] : 0.f;
     }
-    const float* ml = a.out.part_ml + row * a.splits * 2;
-    float M = -INFINITY;
-    for (int s = 0; s < n; s++) M = fmaxf(M, ml[2 * s]);
     const float own = a.own_lse ? a.own_lse[row] * LOG2E : -INFINITY;
-    M = fmaxf(M, own);
-    float L = 0.f, x[HD / 64] = {};
-    if (M > -INFINITY) {
-        for (int s = 0; s < n; s++) {
-            const float m = ml[2 * s], w = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
-            L = fmaf(ml[2 * s + 1], w, L);
+    const float M = fmaxf(wave_max(fmaxf(m[0], m[1])), own);
+    const float base = M == -INFINITY ? 0.f : M;
 #pragma unroll
-            for (int i = 0; i < HD / 64; i++) x[i] = fmaf(a.out.part[(row * a.splits + s) * HD + 64 * i + lane], w, x[i]);
-        }
-        if (own > -INFINITY) {
-            const float w = __builtin_amdgcn_exp2f(own - M);
-            L += w;
+    for (int i = 0; i < 2; i++) w[i] = __builtin_amdgcn_exp2f(m[i] - base);
+    const float w_own = __builtin_amdgcn_exp2f(own - base);
+    const float L = wave_sum(l[0] * w[0] + l[1] * w[1]) + w_own;
+    f4 x = {0.f, 0.f, 0.f, 0.f};
+    const f4* part = reinterpret_cast<const f4*>(a.out.part) + row * a.parts * LANES + c;
+    for (int s0 = from; s0 < a.parts; s0 += GROUPS * FLIGHT) {
+        f4 y[FLIGHT];
+        float by[FLIGHT];
 #pragma unroll
-            for (int i = 0; i < HD / 64; i++) x[i] = fmaf(a.own_out[row * HD + 64 * i + lane], w, x[i]);
+        for (int i = 0; i < FLIGHT; i++) {
+            const int s = s0 + i * GROUPS + group;
+            y[i] = s < a.parts ? part[(int64_t)s * LANES] : f4{0.f, 0.f, 0.f, 0.f};
+            const float low = __shfl(w[0], s & 63, 64), high = __shfl(w[1], s & 63, 64);
+            by[i] = s < 64 ? low : high;
         }
+#pragma unroll
+        for (int i = 0; i < FLIGHT; i++) x += y[i] * (s0 + i * GROUPS + group < a.parts ? by[i] : 0.f);
     }
-    const float inv = L > 0.f ? 1.f / L : 0.f;
 #pragma unroll
-    for (int i = 0; i < HD / 64; i++) {
-        const int64_t at = row * HD + 64 * i + lane;
-        const float y = x[i] * inv;
-        if (a.dtype == WQ_F32) static_cast<float*>(a.out.out)[at] = y;
-        else static_cast<uint16_t*>(a.out.out)[at] = a.dtype == WQ_BF16 ? (uint16_t)pack2(y, 0.f, Bf16()) : (uint16_t)pack2(y, 0.f, F16());
+    for (int o = LANES; o < 64; o *= 2)
+#pragma unroll
+        for (int i = 0; i < 4; i++) x[i] += __shfl_xor(x[i], o, 64);
+    if (a.own_out && own > -INFINITY) x += reinterpret_cast<const f4*>(a.own_out)[row * LANES + c] * w_own;
+    x *= L > 0.f ? 1.f / L : 0.f;
+    if (group == 0) {
+        const int64_t at = row * LANES + c;
+        if (a.dtype == WQ_F32) static_cast<f4*>(a.out.out)[at] = x;
+        else if (a.dtype == WQ_BF16) static_cast<uint2*>(a.out.out)[at] = make_uint2(pack2(x[0], x[1], Bf16()), pack2(x[2], x[3], Bf16()));
+        else static_cast<uint2*>(a.out.out)[at] = make_uint2(pack2(x[0], x[1], F16()), pack2(x[2], x[3], F16()));
     }
     if (a.out.lse && lane == 0) a.out.lse[row] = L > 0.f ? (M + log2f(L)) * 0.69314718055994530942f : -INFINITY;
 }
@@ -785,38 +965,50 @@ void combine(wq_ctx* ctx, const CombineArgs& c, int hd)
     hipLaunchKernelGGL(hd == 128 ? k_attend_combine<128> : k_attend_combine<64>, dim3((unsigned)((c.rows + 3) / 4)), dim3(256), 0, ctx->stream, c);
 }
 
-int64_t tiles_of(int64_t total, int rep, int nseq) { return total * rep / ROWS + nseq; }
+int64_t tiles_of(int64_t total, int rep, int nseq, int rows) { return total * rep / rows + nseq; }
 
-int auto_splits_of(int64_t workgroups, int64_t max_keys)
+// Parts for about `want` workgroups, of at least `keys` keys each
+int auto_splits_of(int64_t workgroups, int64_t max_keys, int want, int keys)
 {
-    int64_t s = workgroups > 0 ? (512 + workgroups - 1) / workgroups : 1;
-    const int64_t most = (max_keys + 4 * KEYS - 1) / (4 * KEYS);
+    int64_t s = workgroups > 0 ? (want + workgroups - 1) / workgroups : 1;
+    const int64_t most = (max_keys + keys - 1) / keys;
     if (s > most) s = most;
     if (s > WQ_MAX_ATTEND_SPLITS) s = WQ_MAX_ATTEND_SPLITS;
     return s < 1 ? 1 : (int)s;
 }
 
-size_t partials_bytes(int64_t rows, int hd, int splits) { return wq_align256((size_t)rows * splits * (hd + 2) * sizeof(float)); }
+size_t partials_bytes(int64_t rows, int hd, int parts) { return wq_align256((size_t)rows * parts * (hd + 2) * sizeof(float)); }
+
+// Wavefronts of a workgroup over shared caches: what is staged serves up to 256 rows, if there are that many
+int shared_waves(int B, int rep, int q_dtype) { return q_dtype != WQ_F32 && (int64_t)B * rep > 128 ? 8 : 4; }
+
+// Longer own caches have a decode launch of their own
+constexpr int64_t OWN_INSIDE = 2048;
 
 }  // namespace
 
 int wq_prefill_splits(int64_t total_q, int B, int Hq, int Hkv, int64_t max_kv_rows)
 {
-    return auto_splits_of(tiles_of(total_q, Hq / Hkv, 0) * Hkv + (int64_t)Hkv * (total_q < B ? total_q : B), max_kv_rows);
+    constexpr int ROWS = PREFILL_WAVES * COLS * 16;
+    return auto_splits_of(tiles_of(total_q, Hq / Hkv, 0, ROWS) * Hkv + (int64_t)Hkv * (total_q < B ? total_q : B), max_kv_rows, 512, 256);
 }
 size_t wq_prefill_ws_bytes(int64_t total_q, int Hq, int hd, int splits)
 {
     return splits > 1 ? partials_bytes(total_q * Hq, hd, splits) : 0;
 }
 
-int wq_shared_splits(int B, int P, int Hq, int Hkv, int64_t max_prefix_tokens)
+WqSharedPlan wq_shared_plan(int B, int P, int Hq, int Hkv, int hd, int q_dtype, int64_t max_prefix_tokens, int64_t max_own_tokens, bool own, int num_splits)
 {
-    return auto_splits_of(tiles_of(B, Hq / Hkv, P) * Hkv, max_prefix_tokens);
-}
-size_t wq_shared_ws_bytes(int B, int Hq, int hd, int splits)
-{
-    const size_t rows = (size_t)B * Hq;
-    return partials_bytes(rows, hd, splits) + wq_align256(rows * hd * sizeof(float)) + wq_align256(rows * sizeof(float));
+    WqSharedPlan s;
+    const int rep = Hq / Hkv, waves = shared_waves(B, rep, q_dtype);
+    s.splits = num_splits > 0 ? num_splits : auto_splits_of(tiles_of(B, rep, P, waves * COLS * 16) * Hkv, max_prefix_tokens, 2048 / waves, 256);
+    s.own_inside = own && max_own_tokens <= OWN_INSIDE;
+    s.own_splits = s.own_inside ? auto_splits_of((int64_t)B * Hkv, max_own_tokens, 256, 256) : 0;
+    const int64_t rows = (int64_t)B * Hq;
+    s.decode_bytes = own && !s.own_inside ? wq_decode_ws_bytes(B, Hq, hd, wq_auto_splits(B, Hkv, max_own_tokens)) : 0;
+    s.bytes = s.decode_bytes + partials_bytes(rows, hd, s.splits + s.own_splits);
+    if (own && !s.own_inside) s.bytes += wq_align256(rows * hd * sizeof(float)) + wq_align256(rows * sizeof(float));
+    return s;
 }
 
 int wq_launch_prefill(wq_ctx* ctx, const WqPrefill& f)
@@ -832,46 +1024,55 @@ int wq_launch_prefill(wq_ctx* ctx, const WqPrefill& f)
     a.out.out = f.out, a.out.lse = f.lse;
     a.out.part = reinterpret_cast<float*>(ctx->ws + WQ_WS_HEADER);
     a.out.part_ml = a.out.part + f.total_q * f.Hq * f.splits * f.hd;
-    const dim3 grid((unsigned)(f.Hkv * tiles_of(f.total_q, a.rep, f.B)), (unsigned)f.splits);
+    const dim3 grid((unsigned)(f.Hkv * tiles_of(f.total_q, a.rep, f.B, PREFILL_WAVES * COLS * 16)), (unsigned)f.splits);
     void (*kernel)(PrefillArgs) = f.dtype == WQ_F32 ? (f.hd == 128 ? k_prefill<F32, 128> : k_prefill<F32, 64>)
                                 : f.dtype == WQ_BF16 ? (f.hd == 128 ? k_prefill<Bf16, 128> : k_prefill<Bf16, 64>)
                                                      : (f.hd == 128 ? k_prefill<F16, 128> : k_prefill<F16, 64>);
-    hipLaunchKernelGGL(kernel, grid, dim3(64 * WAVES), 0, ctx->stream, a);
-    if (f.splits > 1) combine(ctx, CombineArgs{f.total_q * f.Hq, f.Hq, f.splits, f.dtype, f.q_off, f.B, true, nullptr, nullptr, a.out}, f.hd);
+    hipLaunchKernelGGL(kernel, grid, dim3(64 * PREFILL_WAVES), 0, ctx->stream, a);
+    if (f.splits > 1) combine(ctx, CombineArgs{f.total_q * f.Hq, f.Hq, f.splits, f.dtype, f.q_off, f.B, f.splits, true, nullptr, nullptr, a.out}, f.hd);
     WQ_HIP_CHECK(ctx, hipGetLastError());
     return WQ_OK;
 }
 
-// Three launches: every request over its own cache (wq_decode_attention's kernels), the shared caches, the merge.
+// The shared caches and, up to OWN_INSIDE tokens, the requests' own ones in one launch; else those in one of wq_decode_attention's
+// kernels.  Then the merge.
 int wq_launch_shared(wq_ctx* ctx, const WqShared& f)
 {
     const wq_packed_kv* kv = f.prefix;
     const int64_t rows = (int64_t)f.B * f.Hq;
+    const int waves = shared_waves(f.B, f.Hq / kv->Hkv, f.q_dtype);
     SharedArgs a;
     a.q = static_cast<const char*>(f.q);
     a.req_off = f.req_off;
-    a.B = f.B, a.P = kv->B, a.Hq = f.Hq, a.rep = f.Hq / kv->Hkv, a.splits = f.splits;
+    a.B = f.B, a.P = kv->B, a.Hq = f.Hq, a.rep = f.Hq / kv->Hkv;
+    a.units = (int)(kv->Hkv * tiles_of(f.B, a.rep, a.P, waves * COLS * 16));
+    a.splits = f.plan.splits, a.own_splits = f.plan.own_splits;
     a.scale = f.sm_scale * LOG2E;
     a.kv = *kv;
+    a.own = f.plan.own_inside ? *f.own : *kv;
     a.out.out = f.out, a.out.lse = f.lse;
-    char* at = ctx->ws + WQ_WS_HEADER + f.own_ws_bytes;
+    const int parts = a.splits + a.own_splits;
+    char* at = ctx->ws + WQ_WS_HEADER + f.plan.decode_bytes;
     a.out.part = reinterpret_cast<float*>(at);
-    a.out.part_ml = a.out.part + rows * f.splits * kv->hd;
-    at += partials_bytes(rows, kv->hd, f.splits);
+    a.out.part_ml = a.out.part + rows * parts * kv->hd;
+    at += partials_bytes(rows, kv->hd, parts);
     float* own_out = nullptr;
     float* own_lse = nullptr;
-    if (f.own) {
+    if (f.own && !f.plan.own_inside) {
         own_out = reinterpret_cast<float*>(at);
         own_lse = reinterpret_cast<float*>(at + wq_align256(rows * kv->hd * sizeof(float)));
-        const int rc = wq_launch_decode(ctx, f.q, f.q_dtype, f.B, f.Hq, f.own, f.sm_scale, f.own_splits, f.own_algo, own_out, own_lse);
+        const int rc = wq_launch_decode(ctx, f.q, f.q_dtype, f.B, f.Hq, f.own, f.sm_scale, f.decode_splits, f.decode_algo, own_out, own_lse);
         if (rc != WQ_OK) return rc;
     }
-    const dim3 grid((unsigned)(kv->Hkv * tiles_of(f.B, a.rep, a.P)), (unsigned)f.splits);
-    void (*kernel)(SharedArgs) = f.q_dtype == WQ_F32 ? (kv->hd == 128 ? k_shared<F32, 128> : k_shared<F32, 64>)
-                               : f.q_dtype == WQ_BF16 ? (kv->hd == 128 ? k_shared<Bf16, 128> : k_shared<Bf16, 64>)
-                                                      : (kv->hd == 128 ? k_shared<F16, 128> : k_shared<F16, 64>);
-    hipLaunchKernelGGL(kernel, grid, dim3(64 * WAVES), 0, ctx->stream, a);
-    combine(ctx, CombineArgs{rows, f.Hq, f.splits, f.q_dtype, f.req_off, a.P, false, own_out, own_lse, a.out}, kv->hd);
+    const dim3 grid((unsigned)(a.units * a.splits + f.B * kv->Hkv * a.own_splits));
+    void (*kernel)(SharedArgs);
+    if (f.q_dtype == WQ_F32) kernel = kv->hd == 128 ? k_shared<F32, 128, 4> : k_shared<F32, 64, 4>;
+    else if (f.q_dtype == WQ_BF16 && waves == 4) kernel = kv->hd == 128 ? k_shared<Bf16, 128, 4> : k_shared<Bf16, 64, 4>;
+    else if (f.q_dtype == WQ_BF16) kernel = kv->hd == 128 ? k_shared<Bf16, 128, 8> : k_shared<Bf16, 64, 8>;
+    else if (waves == 4) kernel = kv->hd == 128 ? k_shared<F16, 128, 4> : k_shared<F16, 64, 4>;
+    else kernel = kv->hd == 128 ? k_shared<F16, 128, 8> : k_shared<F16, 64, 8>;
+    hipLaunchKernelGGL(kernel, grid, dim3(64 * waves), 0, ctx->stream, a);
+    combine(ctx, CombineArgs{rows, f.Hq, parts, f.q_dtype, f.req_off, a.P, a.splits, false, own_out, own_lse, a.out}, kv->hd);
     WQ_HIP_CHECK(ctx, hipGetLastError());
     return WQ_OK;
 }

@@ -198,17 +198,22 @@ int wq_prefill_splits(int64_t total_q, int B, int Hq, int Hkv, int64_t max_kv_ro
 size_t wq_prefill_ws_bytes(int64_t total_q, int Hq, int hd, int splits);
 int wq_launch_prefill(wq_ctx* ctx, const WqPrefill& f);
 
+struct WqSharedPlan {
+    int splits;                                                   // of the shared caches
+    bool own_inside;                                              // the requests' own caches are part of the same launch
+    int own_splits;                                               // ... cut into so many parts
+    size_t decode_bytes, bytes;                                   // workspace: of the decode launch over them otherwise; in all
+};
+WqSharedPlan wq_shared_plan(int B, int P, int Hq, int Hkv, int hd, int q_dtype, int64_t max_prefix_tokens, int64_t max_own_tokens, bool own, int num_splits);
 struct WqShared {
     const void* q;
-    int q_dtype, B, Hq, splits;
+    int q_dtype, B, Hq;
     const wq_packed_kv *prefix, *own;                             // own: NULL, or a cache of B sequences
     const int32_t* req_off;
     float sm_scale;
-    int own_splits, own_algo;
-    size_t own_ws_bytes;                                          // what the decode launch over `own` takes of the workspace
+    WqSharedPlan plan;
+    int decode_splits, decode_algo;
     void* out;
     float* lse;
 };
-int wq_shared_splits(int B, int P, int Hq, int Hkv, int64_t max_prefix_tokens);
-size_t wq_shared_ws_bytes(int B, int Hq, int hd, int splits);     // without own_ws_bytes
 int wq_launch_shared(wq_ctx* ctx, const WqShared& f);

@@ -97,6 +97,35 @@ def test_long_prefix():
     _check([(700, 0, 1100, 1250)], [3], None, SMALL, 64, torch.float16)
 
 
+@pytest.mark.parametrize("own_len", [(0, 0, 0, 3000), (1000, 700, 500, 40)])
+def test_long_own_caches(own_len):
+    """Beyond the length up to which they are part of the shared launch, and just below."""
+    for dtype in DTYPES:
+        _check([(64, 0, 40, 30)], [2], [own_len, (0, 0, 0, 9)], SMALL, 32, dtype)
+    _check([(64, 0, 40, 30)], [1], [tuple(x * 2048 // 3000 for x in own_len)], LARGE, 64, torch.bfloat16)
+
+
+@pytest.mark.parametrize("bits", [2, 4, 8])
+def test_values_at_the_end_of_fp16(bits):
+    """A group from -65504 to 65504: the rounded scale carries its largest code past fp16's range, where the result is fp16's largest value."""
+    hd, Hkv, n, c = 64, 1, 32, {2: 0, 4: 1, 8: 2}[bits]
+    top = 2 ** bits - 1
+    s = np.float16((65504.0 + 65504.0) / top)
+    assert -65504.0 + float(s) * top >= 65520.0 or bits == 8
+    for dtype in (torch.float16, torch.bfloat16):
+        kv = W.PackedKV(1, Hkv, hd, 32, dtype, [n if i == c else 0 for i in range(3)], [0, 0], fill=0)
+        kv.codes[c].fill_(255)                                              # every code the largest one
+        kv.meta[c].fill_(int(np.uint32(np.float16(s).view(np.uint16)) | np.uint32(np.float16(-65504).view(np.uint16)) << 16) - (1 << 32))
+        kv.meta[c][0].zero_()                                               # keys of zero
+        kv.cls_off[c].copy_(R.i32([0, n]))
+        kv.cls_len[c].copy_(R.i32([n]))
+        ctx = W.Context(W.shared_workspace_bytes(1, 1, 1, 1, hd, n))
+        q = torch.ones(1, 1, hd, dtype=dtype, device="cuda")
+        out = W.wq_decode_attention_shared(ctx, q, kv, R.i32([0, 1]), None, 0.125).float()
+        want = min(-65504.0 + float(s) * top, 65504.0)
+        assert bool(((out - want).abs() <= 2 * R.HALF_STEP[dtype] * want).all()), (dtype, out.min(), out.max(), want)
+
+
 def test_bf16_queries_beyond_fp16():
     """A bf16 query's magnitude has no bound of fp16's: the result is that of the scaled query and the inverse softmax scale."""
     rng = np.random.default_rng(0)
