@@ -1,7 +1,6 @@
 // C-ABI entry points of libwq: context handling, host-side argument validation, dispatch.
 // Every check that needs only host data happens here, before anything is enqueued.
 #include <math.h>
-#include <initializer_list>
 #include <mutex>
 #include <new>
 #include <string.h>
@@ -482,7 +481,9 @@ int wq_rope_frequencies(int rot_dim, double base, int scaling, double factor, in
 size_t wq_prefill_workspace_bytes(int64_t total_q, int B, int Hq, int Hkv, int hd, int64_t max_kv_rows, int num_splits)
 {
     if (total_q <= 0 || B <= 0 || Hq <= 0 || Hkv <= 0 || hd <= 0 || Hq % Hkv != 0) return WQ_WS_HEADER;
-    return WQ_WS_HEADER + wq_prefill_ws_bytes(total_q, Hq, hd, num_splits > 0 ? num_splits : wq_prefill_splits(total_q, B, Hq, Hkv, max_kv_rows));
+    if (num_splits > 0) return WQ_WS_HEADER + wq_prefill_ws_bytes(total_q, Hq, hd, num_splits);
+    const int a = wq_prefill_splits(total_q, B, Hq, Hkv, WQ_F32, max_kv_rows), b = wq_prefill_splits(total_q, B, Hq, Hkv, WQ_BF16, max_kv_rows);
+    return WQ_WS_HEADER + wq_prefill_ws_bytes(total_q, Hq, hd, a > b ? a : b);
 }
 
 int wq_prefill_attention(wq_ctx* ctx, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int dtype,
@@ -509,7 +510,7 @@ int wq_prefill_attention(wq_ctx* ctx, const void* q, int64_t q_stride, const voi
     if (rc != WQ_OK) return rc;
     if (total_kv > 0 && (k_stride > 1 << 22 || v_stride > 1 << 22))       // (offsets inside a tile have 32 bits)
         return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "rows of k or v are more than 2^22 elements apart");
-    const int splits = num_splits > 0 ? num_splits : wq_prefill_splits(total_q, B, Hq, Hkv, max_kv_rows);
+    const int splits = num_splits > 0 ? num_splits : wq_prefill_splits(total_q, B, Hq, Hkv, dtype, max_kv_rows);
     if (ctx->ws_bytes < WQ_WS_HEADER + wq_prefill_ws_bytes(total_q, Hq, hd, splits) || !ctx->ws)
         return wq_fail(ctx, WQ_ERR_WORKSPACE, "workspace too small for %d splits of %lld rows", splits, (long long)total_q);
     return wq_launch_prefill(ctx, {q, k, v, q_stride, k_stride, v_stride, dtype, B, Hq, Hkv, hd, splits, q_off, kv_off, prefix_len, total_q, total_kv, sm_scale,
@@ -519,13 +520,10 @@ int wq_prefill_attention(wq_ctx* ctx, const void* q, int64_t q_stride, const voi
 size_t wq_shared_workspace_bytes(int B, int P, int Hq, int Hkv, int hd, int64_t max_prefix_tokens, int64_t max_own_tokens, int num_splits)
 {
     if (B <= 0 || P <= 0 || Hq <= 0 || Hkv <= 0 || hd <= 0 || Hq % Hkv != 0) return WQ_WS_HEADER;
-    size_t most = 0;                                              // over the queries' types, with and without own caches
-    for (int dtype : {WQ_F32, WQ_BF16})
-        for (bool own : {false, true}) {
-            const size_t n = wq_shared_plan(B, P, Hq, Hkv, hd, dtype, max_prefix_tokens, max_own_tokens, own, num_splits).bytes;
-            if (n > most) most = n;
-        }
-    return WQ_WS_HEADER + most;
+    // (own caches only add to it)
+    const size_t a = wq_shared_plan(B, P, Hq, Hkv, hd, WQ_F32, max_prefix_tokens, max_own_tokens, true, num_splits).bytes;
+    const size_t b = wq_shared_plan(B, P, Hq, Hkv, hd, WQ_BF16, max_prefix_tokens, max_own_tokens, true, num_splits).bytes;
+    return WQ_WS_HEADER + (a > b ? a : b);
 }
 
 int wq_decode_attention_shared(wq_ctx* ctx, const void* q, int q_dtype, int B, int Hq, const wq_packed_kv* prefix, const int32_t* req_off,

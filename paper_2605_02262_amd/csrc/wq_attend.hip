@@ -32,8 +32,9 @@ struct F16 {};
 struct F32 {};
 
 constexpr int COLS = 2;                            // 16-row columns of a wavefront
-constexpr int KEYS = 64;                           // keys of a staged tile
-constexpr int HALF = 32;                           // keys of a step
+// fp32: four wavefronts of 32 rows, 32 keys at a time.  16-bit types: two groups of four wavefronts, 64 keys at a time.
+template <typename CT> constexpr int WAVES = std::is_same_v<CT, F32> ? 4 : 8;
+template <typename CT> constexpr int KEYS = std::is_same_v<CT, F32> ? 32 : 64;
 constexpr float LOG2E = 1.44269504088896340736f;
 // The reference of a row's exponents moves only when a logit exceeds it by 2^SLACK; weights are kept 2^SHIFT too large, so that
 // in fp16 one is lost only below 2^-34 of the largest (SHIFT + SLACK < 16).
@@ -41,8 +42,8 @@ constexpr float SLACK = 5.f, SHIFT = 10.f;
 
 template <typename CT> constexpr int ESIZE = std::is_same_v<CT, F32> ? 4 : 2;
 template <typename CT, int HD> constexpr int STEPS = HD * ESIZE<CT> / 64;          // products of a key tile: 32 (16) channels each
-template <typename CT> constexpr int VSTEPS = HALF * ESIZE<CT> / 64;               // products over a step's keys: 32 (16) keys each
-template <typename CT, int HD> constexpr int TILE_BYTES = KEYS * HD * ESIZE<CT>;   // a staged tile of keys, or of values
+template <typename CT> constexpr int VSTEPS = KEYS<CT> * ESIZE<CT> / 64;           // products over a tile's keys: 32 (16) keys each
+template <typename CT, int HD> constexpr int TILE_BYTES = KEYS<CT> * HD * ESIZE<CT>;   // a staged tile of keys, or of values
 template <typename CT, int HD> using Query = u4[COLS][STEPS<CT, HD>];              // B operands of a wavefront's rows
 typedef __attribute__((address_space(3))) char* Lds;
 typedef __attribute__((address_space(3))) u4* Lds4;
@@ -109,7 +110,7 @@ __device__ __forceinline__ float sum_of_column(float x)
     return x + __shfl_xor(x, 32, 64);
 }
 
-// The order in which a step's weights go into the value product's operand: register e holds the weights of the keys first(e) and
+// The order in which a tile's weights go into the value product's operand: register e holds the weights of the keys first(e) and
 // second(e) of the lane's eight (its four of the first 16 keys, then of the second).  Free, as long as the values' operand has the
 // same: a packed class is expanded fastest with the pairs that its masks leave in the two halves of a register.
 struct Natural {
@@ -125,26 +126,65 @@ struct Near {                  // 8-bit codes
     static constexpr int second(int e) { return first(e) + 2; }
 };
 
-// One step: 32 keys.  keys(t, st), values(vs, ct): this lane's part of the A operands
-template <typename CT, int HD, typename Order, typename Keys, typename Values>
-__device__ __forceinline__ void attend(Rows<HD>& r, const Query<CT, HD>& q, const Keys& keys, const Values& values, int key0, bool masked)
+template <typename CT> using Products = f4[KEYS<CT> / 16][COLS];          // of a tile's keys and a wavefront's rows
+template <typename CT> using Weights = u4[VSTEPS<CT>][COLS];              // B operands of the value products
+
+// keys(t, st): this lane's part of the A operand.  Operands are read from LDS one 16-key tile ahead (and no more: left to itself the compiler
+// reads all of them first, and spills).
+template <typename CT, int HD, typename Keys>
+__device__ __forceinline__ void multiply_keys(Products<CT>& s, const Query<CT, HD>& q, const Keys& keys)
 {
-    const int lane = threadIdx.x & 63;
-    constexpr int T = HALF / 16;
-    f4 s[T][COLS];
+    constexpr int T = KEYS<CT> / 16, ST = STEPS<CT, HD>;
+    u4 a[2][ST];
+#pragma unroll
+    for (int st = 0; st < ST; st++) a[0][st] = keys(0, st);
 #pragma unroll
     for (int t = 0; t < T; t++) {
+        if (t + 1 < T) {
+#pragma unroll
+            for (int st = 0; st < ST; st++) a[(t + 1) & 1][st] = keys(t + 1, st);
+        }
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int n = 0; n < COLS; n++) s[t][n] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int st = 0; st < STEPS<CT, HD>; st++) {
-            const u4 a = keys(t, st);
+        for (int st = 0; st < ST; st++)
 #pragma unroll
-            for (int n = 0; n < COLS; n++) s[t][n] = product<CT>(a, q[n][st], s[t][n]);
-        }
+            for (int n = 0; n < COLS; n++) s[t][n] = product<CT>(a[t & 1][st], q[n][st], s[t][n]);
+        __builtin_amdgcn_sched_barrier(0);
     }
+}
+
+// values(vs, ct): this lane's part of the A operand
+template <typename CT, int HD, typename Values>
+__device__ __forceinline__ void multiply_values(Rows<HD>& r, const Weights<CT>& p, const Values& values)
+{
+    constexpr int AT_ONCE = 4, N = VSTEPS<CT> * (HD / 16);
+    u4 a[2][AT_ONCE];
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; i++) a[0][i] = values(i / (HD / 16), i % (HD / 16));
+#pragma unroll
+    for (int j = 0; j < N; j += AT_ONCE) {
+        if (j + AT_ONCE < N) {
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; i++) a[(j / AT_ONCE + 1) & 1][i] = values((j + AT_ONCE + i) / (HD / 16), (j + AT_ONCE + i) % (HD / 16));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; i++)
+#pragma unroll
+            for (int n = 0; n < COLS; n++) r.o[(j + i) % (HD / 16)][n] = product<CT>(a[j / AT_ONCE & 1][i], p[(j + i) / (HD / 16)][n], r.o[(j + i) % (HD / 16)][n]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// The weights of the keys from key0 on
+template <typename CT, int HD, typename Order>
+__device__ __forceinline__ void form_weights(Rows<HD>& r, Products<CT>& s, Weights<CT>& p, int key0, bool masked)
+{
+    constexpr int T = KEYS<CT> / 16;
     if (masked) {
-        const int k0 = key0 + 4 * (lane >> 4);
+        const int k0 = key0 + 4 * ((threadIdx.x & 63) >> 4);
 #pragma unroll
         for (int n = 0; n < COLS; n++)
 #pragma unroll
@@ -176,45 +216,100 @@ __device__ __forceinline__ void attend(Rows<HD>& r, const Query<CT, HD>& q, cons
             for (int ct = 0; ct < HD / 16; ct++) r.o[ct][n] *= by;
         }
     }
-    u4 p[VSTEPS<CT>][COLS];
 #pragma unroll
     for (int n = 0; n < COLS; n++) {
         const float shift = r.ref[n] == -INFINITY ? 0.f : SHIFT - r.ref[n];
-        float w[8];
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
-            w[e] = __builtin_amdgcn_exp2f(fmaf(s[e >> 2][n][e & 3], r.scale[n], shift));
-            r.sum[n] += w[e];
-        }
-        if constexpr (ESIZE<CT> == 2) {
+        for (int g = 0; g < T / 2; g++) {                      // 8 keys of this lane
+            float w[8];
 #pragma unroll
-            for (int e = 0; e < 4; e++) p[0][n][e] = pack2(w[Order::first(e)], w[Order::second(e)], CT());
-        } else {
+            for (int e = 0; e < 8; e++) {
+                w[e] = __builtin_amdgcn_exp2f(fmaf(s[2 * g + (e >> 2)][n][e & 3], r.scale[n], shift));
+                r.sum[n] += w[e];
+            }
+            if constexpr (ESIZE<CT> == 2) {
 #pragma unroll
-            for (int e = 0; e < 8; e++) p[e >> 2][n][e & 3] = __float_as_uint(w[e]);
+                for (int e = 0; e < 4; e++) p[g][n][e] = pack2(w[Order::first(e)], w[Order::second(e)], CT());
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; e++) p[2 * g + (e >> 2)][n][e & 3] = __float_as_uint(w[e]);
+            }
         }
     }
+}
+
+// fp32: a tile staged in the operands' order, [step][lane][16 bytes]
+template <int HD>
+__device__ __forceinline__ void attend_f32(Rows<HD>& r, const Query<F32, HD>& q, Lds4 k_tile, Lds4 v_tile, int key0, int least, int most)
+{
+    const int lane = threadIdx.x & 63;
+    if (key0 >= most) return;
+    Products<F32> s;
+    Weights<F32> p;
+    multiply_keys<F32, HD>(s, q, [&](int t, int st) { return k_tile[(t * STEPS<F32, HD> + st) * 64 + lane]; });
+    form_weights<F32, HD, Natural>(r, s, p, key0, key0 + KEYS<F32> > least);
+    multiply_values<F32, HD>(r, p, [&](int vs, int ct) { return v_tile[(vs * (HD / 16) + ct) * 64 + lane]; });
+}
+
+// ---- 16-bit types: two groups of wavefronts in turn ----------------------------------------------------------------------------
+// A wavefront alternates between products (keys of its tile, values of the one before: 64 matrix instructions) and weights (the vector unit).
+// The two wavefronts of a SIMD belong to different groups, and the groups are half a turn apart: in every phase one of them has the
+// matrix cores and the other one the vector unit.  (Left to themselves they hardly overlap: a wavefront issues at most one instruction in
+// 6 cycles, the older one of a SIMD goes first, and two that mix matrix and vector instructions take twice the time of one.)
+//   phase 2i      group 0: products of tile i      group 1: weights of tile i - 1, brings the values of tile i
+//   phase 2i + 1  group 0: weights of tile i       group 1: products of tile i       (the keys of tile i + 1 are brought by group 0)
+// A tile's keys and values are read in two neighbouring phases, so two tiles of each in LDS are enough.
+// With up to 128 rows only group 0 has any, and group 1 brings it keys and values (SPLIT).
+__device__ __forceinline__ int group_of_wave() { return this_wave() >> 2; }
+
+// Tiles t0 .. t1-1.  bring_keys(t), bring_values(t): of the group that does so, into LDS; settle(): a phase's end.  The products of the first tile meet
+// weights of zero with what lies in front of its values: zeros.  (No condition inside the loop but who brings what: the compiler
+// copies the accumulators around every one, and spills them.)
+template <typename CT, int HD, bool SPLIT, typename Order, typename Keys, typename Values, typename BringKeys, typename BringValues, typename Settle>
+__device__ __forceinline__ void take_turns(Rows<HD>& r, const Query<CT, HD>& q, int t0, int t1, int least, const Keys& keys, const Values& values,
+                                           const BringKeys& bring_keys, const BringValues& bring_values, const Settle& settle)
+{
+    const int group = group_of_wave();
+    if (SPLIT && group == 1) {
+#pragma unroll 1
+        for (int t = t0; t < t1; t++) {
+            bring_values(t);
+            settle();
+            if (t + 1 < t1) bring_keys(t + 1);
+            settle();
+        }
+        settle();
+        return;
+    }
+    Products<CT> s;
+    Weights<CT> p;
 #pragma unroll
     for (int vs = 0; vs < VSTEPS<CT>; vs++)
 #pragma unroll
-        for (int ct = 0; ct < HD / 16; ct++) {
-            const u4 a = values(vs, ct);
-#pragma unroll
-            for (int n = 0; n < COLS; n++) r.o[ct][n] = product<CT>(a, p[vs][n], r.o[ct][n]);
-        }
-}
-
-// The two steps of a tile staged in the operands' order, [step][lane][16 bytes]
-template <typename CT, int HD, typename Order>
-__device__ __forceinline__ void attend_staged(Rows<HD>& r, const Query<CT, HD>& q, Lds4 k_tile, Lds4 v_tile, int key0, int least, int most)
-{
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int h = 0; h < KEYS / HALF; h++) {
-        auto keys = [&](int t, int st) { return k_tile[((2 * h + t) * STEPS<CT, HD> + st) * 64 + lane]; };
-        auto values = [&](int vs, int ct) { return v_tile[((h * VSTEPS<CT> + vs) * (HD / 16) + ct) * 64 + lane]; };
-        if (key0 + HALF * h < most) attend<CT, HD, Order>(r, q, keys, values, key0 + HALF * h, key0 + HALF * (h + 1) > least);
+        for (int n = 0; n < COLS; n++) p[vs][n] = u4{0, 0, 0, 0};
+    if (!SPLIT && group == 1) {
+        bring_values(t0);
+        settle();
     }
+#pragma unroll 1
+    for (int t = t0; t < t1; t++) {
+        multiply_keys<CT, HD>(s, q, [&](int kt, int st) { return keys(t, kt, st); });
+        multiply_values<CT, HD>(r, p, [&](int vs, int ct) { return values(t - 1, vs, ct); });
+        settle();
+        form_weights<CT, HD, Order>(r, s, p, t * KEYS<CT>, (t + 1) * KEYS<CT> > least);
+        if (!SPLIT && t + 1 < t1) {
+            if (group == 0) bring_keys(t + 1);
+            else bring_values(t + 1);
+        }
+        settle();
+    }
+    if (SPLIT || group == 0) settle();
+    multiply_values<CT, HD>(r, p, [&](int vs, int ct) { return values(t1 - 1, vs, ct); });
+}
+template <typename CT, int HD>
+__device__ __forceinline__ void clear_tile(Lds tile)
+{
+    for (int i = threadIdx.x & 255; i < TILE_BYTES<CT, HD> / 16; i += 256) ((Lds4)tile)[i] = u4{0, 0, 0, 0};
 }
 
 // ---- plain rows, fp32 arithmetic: through registers --------------------------------------------------------------------
@@ -234,21 +329,21 @@ __device__ __forceinline__ u4 row_piece(const char* p)
     }
 }
 
-// n rows from k, v (stride: bytes from row to row), KEYS at most; the tile's other rows become zeros.  The c-th 4 channels of a row are part of
+// n rows from k, v (stride: bytes from row to row), a tile's at most; the tile's other rows become zeros.  The c-th 4 channels of a row are part of
 // product c / 4, lane group c % 4; four keys of four channels are transposed by naming registers.
-template <typename ST, int HD, int W>
+template <typename ST, int HD>
 __device__ void stage_rows(const char* k, const char* v, int64_t k_stride, int64_t v_stride, int n, Lds4 k_tile, Lds4 v_tile)
 {
     constexpr int PIECES = HD / 4, PB = 4 * ESIZE<ST>;
     const int tid = threadIdx.x;
 #pragma unroll 4
-    for (int u = tid; u < KEYS * PIECES; u += 64 * W) {
+    for (int u = tid; u < KEYS<F32> * PIECES; u += 64 * WAVES<F32>) {
         const int row = u / PIECES, c = u % PIECES;
         u4 x = {0, 0, 0, 0};
         if (row < n) x = row_piece<ST>(k + row * k_stride + c * PB);
         k_tile[((row >> 4) * STEPS<F32, HD> + (c >> 2)) * 64 + 16 * (c & 3) + (row & 15)] = x;
     }
-    for (int u = tid; u < KEYS / 4 * PIECES; u += 64 * W) {
+    for (int u = tid; u < KEYS<F32> / 4 * PIECES; u += 64 * WAVES<F32>) {
         const int c = u % PIECES, jj = u / PIECES % 4, t16 = u / PIECES / 4;
         u4 x[4];
 #pragma unroll
@@ -270,17 +365,16 @@ __device__ void stage_rows(const char* k, const char* v, int64_t k_stride, int64
 // is which 16 bytes of its row a lane takes: piece c of row r goes to place c ^ f(r), so that the products' reads, which go down
 // the rows, meet all banks.  Values are read with the transposing load: 16 lanes give the addresses of 4 rows x 16 channels and
 // get 4 rows of one channel each.
-template <int HD, int W, int KT>               // KT: keys of a tile
+template <int HD>
 struct Direct {
-    static constexpr int PIECES = HD / 8, PER_LOAD = 64 * W / PIECES, LOADS = KT / PER_LOAD;      // rows of one load of the workgroup
-    static_assert(KT % PER_LOAD == 0, "");
+    static constexpr int PIECES = HD / 8, PER_LOAD = 256 / PIECES, LOADS = KEYS<Bf16> / PER_LOAD;      // rows of one load of a group
     uint32_t k_off, v_off, k_step, v_step;     // this lane's offset in a tile, and from load to load
     int row;
     uint32_t k_piece, v_piece, k_stride, v_stride;
     int k_lds, v_lds;                          // byte offsets in a tile of this lane's operands: key tile 0, step 0; first value tile
     __device__ __forceinline__ Direct(int64_t ks, int64_t vs)
     {
-        const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, j = lane >> 4;
+        const int tid = threadIdx.x & 255, lane = tid & 63, m = lane & 15, j = lane >> 4;
         row = tid / PIECES;
         const int slot = tid % PIECES;
         k_piece = 16 * (slot ^ swizzle(row)), v_piece = 16 * (slot ^ (swizzle(row) * 2 & (PIECES - 1)));
@@ -294,22 +388,20 @@ struct Direct {
     // 16-byte places of 16 neighbouring rows meet different banks (256 bytes)
     static __device__ __forceinline__ int swizzle(int r) { return HD == 128 ? r & 15 : (r >> 1) & 7; }
 
-    // rows from k, v on, n of them (the last one is read again for the rest: its weights are zero)
-    __device__ __forceinline__ void load(const char* k, const char* v, int n, Lds k_tile, Lds v_tile) const
+    // rows from p on, n of them (the last one is read again for the rest: its weights are zero)
+    __device__ __forceinline__ void load(const char* p, int n, uint32_t off, uint32_t piece, uint32_t step, uint32_t stride, Lds tile) const
     {
-        const int wave = this_wave();
+        const int wave = this_wave() & 3;
 #pragma unroll
         for (int i = 0; i < LOADS; i++) {
-            uint32_t ko = k_off + i * k_step, vo = v_off + i * v_step;
-            if (n < KT) {
-                const uint32_t at = row + i * PER_LOAD < n ? row + i * PER_LOAD : n - 1;
-                ko = at * k_stride + k_piece, vo = at * v_stride + v_piece;
-            }
-            const int to = (i * 64 * W + wave * 64) * 16;
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(k + ko), (__attribute__((address_space(3))) void*)(k_tile + to), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(v + vo), (__attribute__((address_space(3))) void*)(v_tile + to), 16, 0, 0);
+            uint32_t o = off + i * step;
+            if (n < KEYS<Bf16>) o = (uint32_t)(row + i * PER_LOAD < n ? row + i * PER_LOAD : n - 1) * stride + piece;
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(p + o),
+                                             (__attribute__((address_space(3))) void*)(tile + (i * 256 + wave * 64) * 16), 16, 0, 0);
         }
     }
+    __device__ __forceinline__ void load_keys(const char* p, int n, Lds tile) const { load(p, n, k_off, k_piece, k_step, k_stride, tile); }
+    __device__ __forceinline__ void load_values(const char* p, int n, Lds tile) const { load(p, n, v_off, v_piece, v_step, v_stride, tile); }
     __device__ __forceinline__ u4 keys(Lds k_tile, int t, int st) const
     {
         return *(const Lds4)(k_tile + ((k_lds + t * 16 * (2 * HD)) ^ (64 * st)));
@@ -324,43 +416,38 @@ struct Direct {
     }
 };
 
-// Tiles lo .. hi-1 of the n rows from k, v on.  Two tiles in LDS, one is met while the next one arrives.  A wavefront's rows all see the keys
-// below `least`, none sees one from `most` on.
-template <typename CT, int HD, int W, int KT>
+// Tiles lo .. hi-1 of the n rows from k, v on, brought by group 1: a tile's values and the next one's keys while group 0 multiplies.
+template <typename CT, int HD, bool SPLIT>
 __device__ __forceinline__ void walk_rows(Rows<HD>& r, const Query<CT, HD>& q, const char* k, const char* v, int64_t k_stride, int64_t v_stride, int n, int lo,
-                                          int hi, int least, int most, Lds k_lds, Lds v_lds)
+                                          int hi, int least, Lds k_lds, Lds v_lds)
 {
-    constexpr int BYTES = KT * HD * 2;
-    const Direct<HD, W, KT> rows(k_stride, v_stride);
-    auto load = [&](int t) {
-        const int64_t key0 = (int64_t)t * KT;
-        rows.load(k + key0 * k_stride, v + key0 * v_stride, n - (int)key0, k_lds + (t & 1) * BYTES, v_lds + (t & 1) * BYTES);
+    constexpr int BYTES = TILE_BYTES<CT, HD>, TK = KEYS<CT>;
+    const Direct<HD> rows(k_stride, v_stride);
+    auto load_keys = [&](int t) { rows.load_keys(k + (int64_t)t * TK * k_stride, n - t * TK, k_lds + (t & 1) * BYTES); };
+    auto bring_values = [&](int t) {
+        rows.load_values(v + (int64_t)t * TK * v_stride, n - t * TK, v_lds + (t & 1) * BYTES);
+        if (t + 1 < hi) load_keys(t + 1);
     };
     __syncthreads();                                           // (whatever was in LDS before has been read)
-    if (lo < hi) load(lo);
+    if (group_of_wave() == 1) load_keys(lo);
+    else clear_tile<CT, HD>(v_lds + (~lo & 1) * BYTES);
     __syncthreads();
-    for (int t = lo; t < hi; t++) {
-        if (t + 1 < hi) load(t + 1);
-        __builtin_amdgcn_sched_barrier(0);                     // (the loads go out here)
-        const Lds k_tile = k_lds + (t & 1) * BYTES, v_tile = v_lds + (t & 1) * BYTES;
-#pragma unroll
-        for (int h = 0; h < KT / HALF; h++) {
-            const int key0 = t * KT + h * HALF;
-            auto keys = [&](int kt, int st) { return rows.keys(k_tile, 2 * h + kt, st); };
-            auto values = [&](int, int ct) { return rows.values(v_tile, h, ct); };
-            if (key0 < most) attend<CT, HD, Natural>(r, q, keys, values, key0, key0 + HALF > least);
-        }
-        __syncthreads();                                       // the next tile is there, this one is free
-    }
+    take_turns<CT, HD, SPLIT, Natural>(
+        r, q, lo, hi, least, [&](int t, int kt, int st) { return rows.keys(k_lds + (t & 1) * BYTES, kt, st); },
+        [&](int t, int vs, int ct) { return rows.values(v_lds + (t & 1) * BYTES, vs, ct); }, [](int) {}, bring_values, [] { __syncthreads(); });
 }
 
 // ---- a class of the packed cache -----------------------------------------------------------------------------------------
-// Token slots from slots_left on (a multiple of 32) are not the sequence's: they become zeros, because a weight of zero times
-// whatever lies there need not be zero.
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100); }
 __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302); }
 
+template <int BITS>
+__device__ __forceinline__ float code_of(const uint32_t* w, int i)
+{
+    constexpr int PER = 32 / BITS;
+    return (float)((w[i / PER] >> (i % PER * BITS)) & ((1u << BITS) - 1));
+}
 template <int BYTES>
 __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* w)
 {
@@ -379,175 +466,217 @@ __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* w)
     }
 }
 
-// The tile in flight between memory and LDS, in registers.  A key unit is a quarter of a token's channels (lane of the product), 256 of
-// them; a value unit is 8 tokens of every 16th channel of half of the head, 256 of them.  Four wavefronts take one of each per
-// lane, of eight wavefronts half take the keys and half the values.
-template <int HD, int BITS, int W>
-struct Packed {
-    static constexpr int C = BITS == 2 ? 0 : (BITS == 4 ? 1 : 2);
-    static constexpr int CT16 = HD / 16, N = HD / 4, K_BYTES = N * BITS / 8, V_CT = CT16 / 2, V_BYTES = V_CT * BITS;
-    static constexpr int VG = HD / 64;             // groups that a value unit's channels can belong to
-    uint32_t kw[(K_BYTES + 3) / 4], km, vw[(V_BYTES + 3) / 4];
-    uint4 vm[VG][2];
+// A tile in flight between memory and LDS, in registers, brought by 64 * 4 (TOKENS = 64) or 64 * 2 (32) threads each of keys and of values.  A key
+// unit is a quarter of a token's channels (lane of the product), a value unit 8 tokens of every 16th channel of half of the head.
+// Addresses are a scalar base that moves with the tile and a lane's offset that does not.  A sequence's segment is padded to 32
+// tokens: where a tile's second 32 are not the sequence's, its first 32 are taken again (their weights are zero, but zero times
+// whatever lies there need not be zero).
+// Field f of both halves of w as fp16: placed in the significand of a power of two, which is then taken away (exact)
+template <int BITS, int AT>
+__device__ __forceinline__ uint32_t placed(uint32_t w)
+{
+    constexpr uint32_t MASK = ((1u << BITS) - 1) << AT, ONE = (25u - AT) << 10;      // 2^(10 - AT)
+    uint32_t one = ONE | ONE << 16;
+    asm("" : "+v"(one));                                   // (in a vector register, so that both steps are one instruction)
+    return (w & (MASK | MASK << 16)) | one;
+}
+template <int BITS, int AT>
+__device__ __forceinline__ uint32_t expanded(uint32_t x, h2 s, h2 m)
+{
+    constexpr _Float16 BIAS = (_Float16)(float)(1 << (10 - AT));
+    const h2 code = __builtin_bit_cast(h2, x) - h2{BIAS, BIAS};
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(code, s, m));       // (one rounding)
+}
 
-    static __device__ __forceinline__ bool does_keys() { return W == 4 || this_wave() < 4; }
-    static __device__ __forceinline__ bool does_values() { return W == 4 || this_wave() >= 4; }
 
-    __device__ __forceinline__ void load(const wq_packed_kv& kv, int kvh, int64_t tok0, int64_t slots_left)
+template <int HD, int BITS, int TOKENS>
+struct PackedKeys {
+    static constexpr int C = BITS == 2 ? 0 : (BITS == 4 ? 1 : 2), N = HD / 4, BYTES = N * BITS / 8;
+    const uint8_t* codes;                          // at the first tile
+    const uint32_t* metas;
+    uint32_t code_off, meta_off, G;
+    int unit, slots;                               // token slots of the segment
+    uint32_t w[(BYTES + 3) / 4], meta;
+
+    __device__ __forceinline__ PackedKeys(const wq_packed_kv& kv, int kvh, int64_t tok0, int segment_slots)
     {
-        const int unit = threadIdx.x & 255, lane = unit & 63, group = kv.group, G = HD / group;
-        const int64_t cap = kv.cap[C];
-        if (does_keys()) {
-            const uint8_t* kc = static_cast<const uint8_t*>(kv.codes[C]) + (int64_t)kvh * cap * HD * BITS / 8;
-            const uint32_t* m = static_cast<const uint32_t*>(kv.meta[C]) + (int64_t)kvh * cap * G;
-            const int t16 = unit >> 6;
-            km = 0;
-#pragma unroll
-            for (int i = 0; i < (K_BYTES + 3) / 4; i++) kw[i] = 0;
-            if (16 * t16 < slots_left) {
-                const int64_t tile = (tok0 >> 4) + t16;
-                load_words<K_BYTES>(kc + (tile * 64 + lane) * K_BYTES, kw);
-                km = m[(tile * G + (lane >> 4) * N / group) * 16 + (lane & 15)];       // (a quarter lies in one group: a group has at least 32 channels)
-            }
-        }
-        if (does_values()) {
-            const uint8_t* vc = static_cast<const uint8_t*>(kv.codes[C]) + ((int64_t)kv.Hkv + kvh) * cap * HD * BITS / 8;
-            const uint32_t* m = static_cast<const uint32_t*>(kv.meta[C]) + ((int64_t)kv.Hkv + kvh) * cap * G;
-            const int blk = unit >> 7, half = (unit >> 6) & 1, jj = lane >> 4;
-#pragma unroll
-            for (int i = 0; i < (V_BYTES + 3) / 4; i++) vw[i] = 0;
-#pragma unroll
-            for (int g = 0; g < VG; g++) vm[g][0] = vm[g][1] = make_uint4(0, 0, 0, 0);
-            if (32 * blk < slots_left) {
-                const int64_t block = (tok0 >> 5) + blk;
-                load_words<V_BYTES>(vc + (block * 64 + lane) * (CT16 * BITS) + half * V_BYTES, vw);
-#pragma unroll
-                for (int g = 0; g < VG; g++) {
-                    const int64_t of = (half * (HD / 2) + 32 * g) / group;
-                    vm[g][0] = *reinterpret_cast<const uint4*>(m + ((2 * block) * G + of) * 16 + 4 * jj);
-                    vm[g][1] = *reinterpret_cast<const uint4*>(m + ((2 * block + 1) * G + of) * 16 + 4 * jj);
-                }
-            }
-        }
+        slots = segment_slots, unit = threadIdx.x & (4 * TOKENS - 1), G = HD / kv.group;
+        const int lane = unit & 63;
+        const int64_t slot = kvh * kv.cap[C] + tok0;
+        codes = static_cast<const uint8_t*>(kv.codes[C]) + slot * HD * BITS / 8;
+        metas = static_cast<const uint32_t*>(kv.meta[C]) + slot * G;
+        code_off = unit * BYTES;
+        meta_off = ((unit >> 6) * G + (lane >> 4) * N / kv.group) * 16 + (lane & 15);      // (a quarter lies in one group: a group has at least 32 channels)
     }
-
-    // Field f of both halves of w as fp16: placed in the significand of a power of two, which is then taken away (exact)
-    template <int AT>
-    static __device__ __forceinline__ uint32_t placed(uint32_t w)
+    __device__ __forceinline__ void load(int t)
     {
-        constexpr uint32_t MASK = ((1u << BITS) - 1) << AT, ONE = (25u - AT) << 10;      // 2^(10 - AT)
-        return (w & (MASK | MASK << 16)) | (ONE | ONE << 16);
+        const bool again = TOKENS == 64 && t * 64 + 16 * (unit >> 6) >= slots;
+        load_words<BYTES>(codes + (int64_t)t * (TOKENS * HD * BITS / 8) + (code_off - (again ? 128 * BYTES : 0)), w);
+        meta = (metas + (int64_t)t * (TOKENS * G))[meta_off - (again ? 32 * G : 0)];
     }
-    template <int AT>
-    static __device__ __forceinline__ uint32_t value(uint32_t x, h2 s, h2 m)
+    // pairs of channels as a masked word holds them: see order_query
+    __device__ __forceinline__ void stage(Lds4 k_tile) const
     {
-        constexpr _Float16 BIAS = (_Float16)(float)(1 << (10 - AT));
-        const h2 code = __builtin_bit_cast(h2, x) - h2{BIAS, BIAS};
-        return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(code, s, m));       // (one rounding)
-    }
-
-    // fp16 operands.  Key unit: the pairs of channels that a masked word holds, see query_pair below; value unit: the pairs of Far or Near.
-    __device__ __forceinline__ void stage(Lds4 k_tile, Lds4 v_tile) const
-    {
-        const int unit = threadIdx.x & 255, lane = unit & 63;
-        if (does_keys()) {
-            const h2 sm = __builtin_bit_cast(h2, km), s = {sm[0], sm[0]}, m = {sm[1], sm[1]};
-            Lds4 to = k_tile + (unit >> 6) * STEPS<F16, HD> * 64 + lane;
+        const int lane = unit & 63;
+        const h2 sm = __builtin_bit_cast(h2, meta), s = {sm[0], sm[0]}, m = {sm[1], sm[1]};
+        Lds4 to = k_tile + (unit >> 6) * STEPS<F16, HD> * 64 + lane;
 #pragma unroll
-            for (int st = 0; st < STEPS<F16, HD>; st++) {
-                u4 y;
-                if constexpr (BITS == 8) {
+        for (int st = 0; st < STEPS<F16, HD>; st++) {
+            u4 y;
+            if constexpr (BITS == 8) {
 #pragma unroll
-                    for (int i = 0; i < 2; i++) {
-                        y[2 * i] = value<0>(placed<0>(kw[2 * st + i]), s, m);
-                        y[2 * i + 1] = value<0>(placed<0>(kw[2 * st + i] >> 8), s, m);
-                    }
-                } else if constexpr (BITS == 4) {
-                    const uint32_t w = kw[st], z = w >> 8;
-                    y[0] = value<0>(placed<0>(w), s, m), y[1] = value<4>(placed<4>(w), s, m);
-                    y[2] = value<0>(placed<0>(z), s, m), y[3] = value<4>(placed<4>(z), s, m);
-                } else {
-                    const uint32_t w = kw[st >> 1] >> (st & 1) * 8;
-                    y[0] = value<0>(placed<0>(w), s, m), y[1] = value<2>(placed<2>(w), s, m);
-                    y[2] = value<4>(placed<4>(w), s, m), y[3] = value<6>(placed<6>(w), s, m);
+                for (int i = 0; i < 2; i++) {
+                    y[2 * i] = expanded<BITS, 0>(placed<BITS, 0>(w[2 * st + i]), s, m);
+                    y[2 * i + 1] = expanded<BITS, 0>(placed<BITS, 0>(w[2 * st + i] >> 8), s, m);
                 }
-                to[st * 64] = y;
+            } else if constexpr (BITS == 4) {
+                const uint32_t x = w[st], z = x >> 8;
+                y[0] = expanded<BITS, 0>(placed<BITS, 0>(x), s, m), y[1] = expanded<BITS, 4>(placed<BITS, 4>(x), s, m);
+                y[2] = expanded<BITS, 0>(placed<BITS, 0>(z), s, m), y[3] = expanded<BITS, 4>(placed<BITS, 4>(z), s, m);
+            } else {
+                const uint32_t x = w[st >> 1] >> (st & 1) * 8;
+                y[0] = expanded<BITS, 0>(placed<BITS, 0>(x), s, m), y[1] = expanded<BITS, 2>(placed<BITS, 2>(x), s, m);
+                y[2] = expanded<BITS, 4>(placed<BITS, 4>(x), s, m), y[3] = expanded<BITS, 6>(placed<BITS, 6>(x), s, m);
             }
-        }
-        if (does_values()) {
-            const int blk = unit >> 7, half = (unit >> 6) & 1;
-            Lds4 to = v_tile + (blk * CT16 + half * V_CT) * 64 + lane;
-#pragma unroll
-            for (int g = 0; g < VG; g++) {
-                h2 s[4], m[4];
-                const uint32_t t[8] = {vm[g][0].x, vm[g][0].y, vm[g][0].z, vm[g][0].w, vm[g][1].x, vm[g][1].y, vm[g][1].z, vm[g][1].w};
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    using O = std::conditional_t<BITS == 8, Near, Far>;
-                    s[e] = __builtin_bit_cast(h2, low_halves(t[O::first(e)], t[O::second(e)]));
-                    m[e] = __builtin_bit_cast(h2, high_halves(t[O::first(e)], t[O::second(e)]));
-                }
-#pragma unroll
-                for (int i = 2 * g; i < 2 * g + 2; i++) {          // 16-channel tiles of the group's 32 channels
-                    u4 y;
-                    if constexpr (BITS == 8) {
-#pragma unroll
-                        for (int k = 0; k < 2; k++) {
-                            y[2 * k] = value<0>(placed<0>(vw[2 * i + k]), s[2 * k], m[2 * k]);
-                            y[2 * k + 1] = value<0>(placed<0>(vw[2 * i + k] >> 8), s[2 * k + 1], m[2 * k + 1]);
-                        }
-                    } else if constexpr (BITS == 4) {
-                        const uint32_t w = vw[i], z = w >> 8;
-                        y[0] = value<0>(placed<0>(w), s[0], m[0]), y[1] = value<4>(placed<4>(w), s[1], m[1]);
-                        y[2] = value<0>(placed<0>(z), s[2], m[2]), y[3] = value<4>(placed<4>(z), s[3], m[3]);
-                    } else {                                       // a word holds two tiles, one per half
-                        const uint32_t w = vw[i >> 1], z = w >> 8;
-                        auto both = [&](uint32_t a, uint32_t b) { return i & 1 ? high_halves(a, b) : low_halves(a, b); };
-                        y[0] = value<0>(both(placed<0>(w), placed<0>(z)), s[0], m[0]), y[1] = value<2>(both(placed<2>(w), placed<2>(z)), s[1], m[1]);
-                        y[2] = value<4>(both(placed<4>(w), placed<4>(z)), s[2], m[2]), y[3] = value<6>(both(placed<6>(w), placed<6>(z)), s[3], m[3]);
-                    }
-                    to[i * 64] = y;
-                }
-            }
+            to[st * 64] = y;
         }
     }
-
-    // fp32 operands, codes one by one
-    static __device__ __forceinline__ float code(const uint32_t* w, int i)
+    // fp32, codes one by one
+    __device__ __forceinline__ void stage_f32(Lds4 k_tile) const
     {
-        constexpr int PER = 32 / BITS;
-        return (float)((w[i / PER] >> (i % PER * BITS)) & ((1u << BITS) - 1));
-    }
-    __device__ __forceinline__ void stage_f32(Lds4 k_tile, Lds4 v_tile) const
-    {
-        const int unit = threadIdx.x & 255, lane = unit & 63;
-        if (does_keys()) {
-            const float s = wq_f16_bits_to_float(km & 0xFFFF), m = wq_f16_bits_to_float(km >> 16);
+        const float s = wq_f16_bits_to_float(meta & 0xFFFF), m = wq_f16_bits_to_float(meta >> 16);
 #pragma unroll
-            for (int st = 0; st < STEPS<F32, HD>; st++) {
-                u4 y;
+        for (int st = 0; st < STEPS<F32, HD>; st++) {
+            u4 y;
 #pragma unroll
-                for (int e = 0; e < 4; e++) y[e] = __float_as_uint(fmaf(s, code(kw, 4 * st + e), m));
-                k_tile[((unit >> 6) * STEPS<F32, HD> + st) * 64 + lane] = y;
-            }
-        }
-        if (does_values()) {
-            const int blk = unit >> 7, half = (unit >> 6) & 1;
-#pragma unroll
-            for (int i = 0; i < V_CT; i++)
-#pragma unroll
-                for (int h = 0; h < 2; h++) {
-                    const uint4 t = vm[i >> 1][h];
-                    const uint32_t meta[4] = {t.x, t.y, t.z, t.w};
-                    u4 y;
-#pragma unroll
-                    for (int e = 0; e < 4; e++)
-                        y[e] = __float_as_uint(fmaf(wq_f16_bits_to_float(meta[e] & 0xFFFF), code(vw, 8 * i + 4 * h + e), wq_f16_bits_to_float(meta[e] >> 16)));
-                    v_tile[((2 * blk + h) * CT16 + half * V_CT + i) * 64 + lane] = y;
-                }
+            for (int e = 0; e < 4; e++) y[e] = __float_as_uint(fmaf(s, code_of<BITS>(w, 4 * st + e), m));
+            k_tile[((unit >> 6) * STEPS<F32, HD> + st) * 64 + (unit & 63)] = y;
         }
     }
 };
+
+template <int HD, int BITS, int TOKENS>
+struct PackedValues {
+    static constexpr int C = BITS == 2 ? 0 : (BITS == 4 ? 1 : 2), CT16 = HD / 16, V_CT = CT16 / 2, BYTES = V_CT * BITS;
+    static constexpr int VG = HD / 64;             // groups that a unit's channels can belong to
+    const uint8_t* codes;
+    const uint32_t* metas;
+    uint32_t code_off, meta_off[VG], G;
+    int unit, slots;
+    uint32_t w[(BYTES + 3) / 4];
+    uint4 meta[VG][2];
+
+    __device__ __forceinline__ PackedValues(const wq_packed_kv& kv, int kvh, int64_t tok0, int segment_slots)
+    {
+        slots = segment_slots, unit = threadIdx.x & (4 * TOKENS - 1), G = HD / kv.group;
+        const int lane = unit & 63, half = (unit >> 6) & 1, blk = unit >> 7;
+        const int64_t slot = (kv.Hkv + kvh) * kv.cap[C] + tok0;
+        codes = static_cast<const uint8_t*>(kv.codes[C]) + slot * HD * BITS / 8;
+        metas = static_cast<const uint32_t*>(kv.meta[C]) + slot * G;
+        code_off = (blk * 64 + lane) * (CT16 * BITS) + half * BYTES;
+#pragma unroll
+        for (int g = 0; g < VG; g++) meta_off[g] = (2 * blk * G + (half * (HD / 2) + 32 * g) / kv.group) * 16 + 4 * (lane >> 4);
+    }
+    __device__ __forceinline__ void load(int t)
+    {
+        const bool again = TOKENS == 64 && t * 64 + 32 * (unit >> 7) >= slots;
+        load_words<BYTES>(codes + (int64_t)t * (TOKENS * HD * BITS / 8) + (code_off - (again ? 64 * CT16 * BITS : 0)), w);
+        const uint32_t* m = metas + (int64_t)t * (TOKENS * G);
+#pragma unroll
+        for (int g = 0; g < VG; g++) {
+            const uint32_t at = meta_off[g] - (again ? 32 * G : 0);
+            meta[g][0] = *reinterpret_cast<const uint4*>(m + at);
+            meta[g][1] = *reinterpret_cast<const uint4*>(m + at + 16 * G);
+        }
+    }
+    // pairs of tokens: those of Far or Near
+    __device__ __forceinline__ void stage(Lds4 v_tile) const
+    {
+        const int lane = unit & 63, blk = unit >> 7, half = (unit >> 6) & 1;
+        Lds4 to = v_tile + (blk * CT16 + half * V_CT) * 64 + lane;
+#pragma unroll
+        for (int g = 0; g < VG; g++) {
+            h2 s[4], m[4];
+            const uint32_t t[8] = {meta[g][0].x, meta[g][0].y, meta[g][0].z, meta[g][0].w, meta[g][1].x, meta[g][1].y, meta[g][1].z, meta[g][1].w};
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                using O = std::conditional_t<BITS == 8, Near, Far>;
+                s[e] = __builtin_bit_cast(h2, low_halves(t[O::first(e)], t[O::second(e)]));
+                m[e] = __builtin_bit_cast(h2, high_halves(t[O::first(e)], t[O::second(e)]));
+            }
+#pragma unroll
+            for (int i = 2 * g; i < 2 * g + 2; i++) {          // 16-channel tiles of the group's 32 channels
+                u4 y;
+                if constexpr (BITS == 8) {
+#pragma unroll
+                    for (int k = 0; k < 2; k++) {
+                        y[2 * k] = expanded<BITS, 0>(placed<BITS, 0>(w[2 * i + k]), s[2 * k], m[2 * k]);
+                        y[2 * k + 1] = expanded<BITS, 0>(placed<BITS, 0>(w[2 * i + k] >> 8), s[2 * k + 1], m[2 * k + 1]);
+                    }
+                } else if constexpr (BITS == 4) {
+                    const uint32_t x = w[i], z = x >> 8;
+                    y[0] = expanded<BITS, 0>(placed<BITS, 0>(x), s[0], m[0]), y[1] = expanded<BITS, 4>(placed<BITS, 4>(x), s[1], m[1]);
+                    y[2] = expanded<BITS, 0>(placed<BITS, 0>(z), s[2], m[2]), y[3] = expanded<BITS, 4>(placed<BITS, 4>(z), s[3], m[3]);
+                } else {                                       // a word holds two tiles, one per half
+                    const uint32_t x = w[i >> 1], z = x >> 8;
+                    auto both = [&](uint32_t a, uint32_t b) { return i & 1 ? high_halves(a, b) : low_halves(a, b); };
+                    y[0] = expanded<BITS, 0>(both(placed<BITS, 0>(x), placed<BITS, 0>(z)), s[0], m[0]), y[1] = expanded<BITS, 2>(both(placed<BITS, 2>(x), placed<BITS, 2>(z)), s[1], m[1]);
+                    y[2] = expanded<BITS, 4>(both(placed<BITS, 4>(x), placed<BITS, 4>(z)), s[2], m[2]), y[3] = expanded<BITS, 6>(both(placed<BITS, 6>(x), placed<BITS, 6>(z)), s[3], m[3]);
+                }
+                to[i * 64] = y;
+            }
+        }
+    }
+    __device__ __forceinline__ void stage_f32(Lds4 v_tile) const
+    {
+        const int half = (unit >> 6) & 1, blk = unit >> 7;
+#pragma unroll
+        for (int i = 0; i < V_CT; i++)
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const uint4 t = meta[i >> 1][h];
+                const uint32_t sm[4] = {t.x, t.y, t.z, t.w};
+                u4 y;
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    y[e] = __float_as_uint(fmaf(wq_f16_bits_to_float(sm[e] & 0xFFFF), code_of<BITS>(w, 8 * i + 4 * h + e), wq_f16_bits_to_float(sm[e] >> 16)));
+                v_tile[((2 * blk + h) * CT16 + half * V_CT + i) * 64 + (unit & 63)] = y;
+            }
+    }
+};
+
+// Tiles t0 .. t1-1 of a class's segment
+template <int HD, int BITS, bool SPLIT>
+__device__ __forceinline__ void walk_packed(Rows<HD>& r, const Query<F16, HD>& q, const wq_packed_kv& kv, int kvh, int64_t tok0, int len, int t0, int t1,
+                                            Lds k_lds, Lds v_lds)
+{
+    using Order = std::conditional_t<BITS == 8, Near, Far>;
+    constexpr int BYTES = TILE_BYTES<F16, HD>;
+    const int slots = (len + 31) / 32 * 32, lane = threadIdx.x & 63, keys_by = SPLIT ? 1 : 0;
+    PackedKeys<HD, BITS, 64> keys(kv, kvh, tok0, slots);
+    PackedValues<HD, BITS, 64> values(kv, kvh, tok0, slots);
+    auto k_of = [&](int t) { return (Lds4)(k_lds + (t & 1) * BYTES); };
+    auto v_of = [&](int t) { return (Lds4)(v_lds + (t & 1) * BYTES); };
+    auto bring_keys = [&](int t) {
+        keys.stage(k_of(t));
+        if (t + 1 < t1) keys.load(t + 1);
+    };
+    auto bring_values = [&](int t) {
+        values.stage(v_of(t));
+        if (t + 1 < t1) values.load(t + 1);
+    };
+    __syncthreads();                                           // (whatever was in LDS before has been read)
+    if (group_of_wave() == 1) values.load(t0);
+    else clear_tile<F16, HD>(v_lds + (~t0 & 1) * BYTES);
+    if (group_of_wave() == keys_by) {
+        keys.load(t0);
+        bring_keys(t0);
+    }
+    __syncthreads();
+    take_turns<F16, HD, SPLIT, Order>(
+        r, q, t0, t1, len, [&](int t, int kt, int st) { return k_of(t)[(kt * STEPS<F16, HD> + st) * 64 + lane]; },
+        [&](int t, int vs, int ct) { return v_of(t)[(vs * (HD / 16) + ct) * 64 + lane]; }, bring_keys, bring_values, [] { __syncthreads(); });
+}
 
 // ---- what both kernels share -------------------------------------------------------------------------------------------
 struct Out {
@@ -686,19 +815,17 @@ struct PrefillArgs {
     Out out;
 };
 
-constexpr int PREFILL_WAVES = 4, PREFILL_KEYS = 32;
+template <typename CT, bool SPLIT> constexpr int ROWS = std::is_same_v<CT, F32> || SPLIT ? 128 : 256;       // of a workgroup
 
-// 16-bit types: three wavefronts per SIMD (168 registers), tiles of 32 keys so that three workgroups fit the LDS
-template <typename CT, int HD>
-__global__ __launch_bounds__(64 * PREFILL_WAVES, ESIZE<CT> == 2 ? 3 : 2) void k_prefill(PrefillArgs a)
+template <typename CT, int HD, bool SPLIT>
+__global__ __launch_bounds__(64 * WAVES<CT>, 2) void k_prefill(PrefillArgs a)
 {
-    constexpr int W = PREFILL_WAVES, ROWS = W * COLS * 16, KT = ESIZE<CT> == 2 ? PREFILL_KEYS : KEYS;
-    constexpr int BYTES = ESIZE<CT> == 2 ? 2 * KT * HD * 2 : TILE_BYTES<CT, HD>;
+    constexpr int BYTES = TILE_BYTES<CT, HD> * (ESIZE<CT> == 2 ? 2 : 1), R = ROWS<CT, SPLIT>;
     __shared__ __align__(16) char s_k[BYTES], s_v[BYTES];
     const int Hkv = a.Hq / a.rep, kvh = blockIdx.x % Hkv, split = blockIdx.y;
     const int wave = this_wave(), lane = threadIdx.x & 63;
     Place p;
-    if (!find_place<ROWS>(a.q_off, a.B, a.rep, a.total_q, (gridDim.x - 1 - blockIdx.x) / Hkv, p)) return;      // (the last rows see the most keys: they begin first)
+    if (!find_place<R>(a.q_off, a.B, a.rep, a.total_q, (gridDim.x - 1 - blockIdx.x) / Hkv, p)) return;      // (the last rows see the most keys: they begin first)
     const int64_t kv0 = clipped(a.kv_off[p.seq], a.total_kv), kv1 = clipped(a.kv_off[p.seq + 1], a.total_kv);
     const int len = kv1 > kv0 ? (int)(kv1 - kv0) : 0;
     const int first = len - p.rows / a.rep;                       // position of the sequence's first query row
@@ -709,8 +836,8 @@ __global__ __launch_bounds__(64 * PREFILL_WAVES, ESIZE<CT> == 2 ? 3 : 2) void k_
         const int seen = first + row / a.rep + 1;
         return seen > prefix ? seen : prefix;
     };
-    const int last_row = (p.row0 + ROWS < p.rows ? p.row0 + ROWS : p.rows) - 1;
-    const int tiles = (limit_of(last_row) + KT - 1) / KT;
+    const int last_row = (p.row0 + R < p.rows ? p.row0 + R : p.rows) - 1;
+    const int tiles = (limit_of(last_row) + KEYS<CT> - 1) / KEYS<CT>;
     const int lo = (int)((int64_t)split * tiles / a.splits), hi = (int)((int64_t)(split + 1) * tiles / a.splits);
 
     Rows<HD> r;
@@ -729,23 +856,23 @@ __global__ __launch_bounds__(64 * PREFILL_WAVES, ESIZE<CT> == 2 ? 3 : 2) void k_
         }
         load_query<CT, HD>(q, n, at);
     }
-    const bool any = wrow0 < p.rows;
+    const bool any = wrow0 < p.rows && wave * COLS * 16 < R;
     const int wlast = wrow0 + COLS * 16 <= p.rows ? wrow0 + COLS * 16 - 1 : p.rows - 1;
     const int least = any ? limit_of(wrow0) : 0, most = any ? limit_of(wlast) : 0;
     const char* k = a.k + kv0 * a.k_stride + kvh * (HD * ESIZE<CT>);
     const char* v = a.v + kv0 * a.v_stride + kvh * (HD * ESIZE<CT>);
     if constexpr (ESIZE<CT> == 2) {
-        walk_rows<CT, HD, W, KT>(r, q, k, v, a.k_stride, a.v_stride, len, lo, hi, least, most, (Lds)s_k, (Lds)s_v);
+        if (lo < hi) walk_rows<CT, HD, SPLIT>(r, q, k, v, a.k_stride, a.v_stride, len, lo, hi, least, (Lds)s_k, (Lds)s_v);
     } else {
         for (int t = lo; t < hi; t++) {
-            const int key0 = t * KT;
+            const int key0 = t * KEYS<CT>;
             __syncthreads();
-            stage_rows<CT, HD, W>(k + key0 * a.k_stride, v + key0 * a.v_stride, a.k_stride, a.v_stride, len - key0, (Lds4)s_k, (Lds4)s_v);
+            stage_rows<CT, HD>(k + key0 * a.k_stride, v + key0 * a.v_stride, a.k_stride, a.v_stride, len - key0, (Lds4)s_k, (Lds4)s_v);
             __syncthreads();
-            attend_staged<CT, HD, Natural>(r, q, (Lds4)s_k, (Lds4)s_v, key0, least, most);
+            attend_f32<HD>(r, q, (Lds4)s_k, (Lds4)s_v, key0, least, most);
         }
     }
-    store_rows<CT, HD>(r, p, a.rep, a.Hq, kvh, wave, split, a.splits > 1 ? a.splits : 0, a.out);
+    if (any) store_rows<CT, HD>(r, p, a.rep, a.Hq, kvh, wave, split, a.splits > 1 ? a.splits : 0, a.out);
 }
 
 // ---- wq_decode_attention_shared ------------------------------------------------------------------------------------------
@@ -760,14 +887,14 @@ struct SharedArgs {
     Out out;
 };
 
-// W wavefronts of 32 rows each.  QT: the query's type; packed tokens are walked in fp16 (fp32 for fp32 queries), 16-bit rows in the
+// QT: the query's type; packed tokens are walked in fp16 (fp32 for fp32 queries), 16-bit rows in the
 // cache's own type.  A request's own cache is a unit of rep rows.
-template <typename QT, int HD, int W>
-__global__ __launch_bounds__(64 * W, 2) void k_shared(SharedArgs a)
+template <typename QT, int HD, bool SPLIT>
+__global__ __launch_bounds__(64 * WAVES<QT>, 2) void k_shared(SharedArgs a)
 {
     using CT = std::conditional_t<std::is_same_v<QT, F32>, F32, F16>;
     constexpr bool PIPED = ESIZE<QT> == 2;
-    constexpr int ROWS = W * COLS * 16, BYTES = TILE_BYTES<CT, HD> * (1 + PIPED);
+    constexpr int BYTES = TILE_BYTES<CT, HD> * (1 + PIPED), R = ROWS<QT, SPLIT>, TK = KEYS<QT>;
     __shared__ __align__(16) char s_k[BYTES], s_v[BYTES];
     const int Hkv = a.kv.Hkv, wave = this_wave(), lane = threadIdx.x & 63;
     const bool own = (int)blockIdx.x >= a.units * a.splits;
@@ -777,7 +904,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_shared(SharedArgs a)
     Place p;
     if (own) {
         p.seq = unit / Hkv, p.first = p.seq, p.row0 = 0, p.rows = a.rep;
-    } else if (!find_place<ROWS>(a.req_off, a.P, a.rep, a.B, unit / Hkv, p)) {
+    } else if (!find_place<R>(a.req_off, a.P, a.rep, a.B, unit / Hkv, p)) {
         return;
     }
     const wq_packed_kv& kv = own ? a.own : a.kv;
@@ -787,7 +914,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_shared(SharedArgs a)
         const int64_t room = c < 3 ? kv.cap[c] - kv.cls_off[c][p.seq] : kv.cap16 - kv.off16[p.seq];
         len[c] = c < 3 ? kv.cls_len[c][p.seq] : kv.len16[p.seq];
         if (len[c] > room) len[c] = (int)room;
-        tiles[c] = len[c] > 0 ? (len[c] + KEYS - 1) / KEYS : 0;
+        tiles[c] = len[c] > 0 ? (len[c] + TK - 1) / TK : 0;
         all += tiles[c];
     }
     const int lo = (int)((int64_t)split * all / splits), hi = (int)((int64_t)(split + 1) * all / splits);
@@ -803,15 +930,13 @@ __global__ __launch_bounds__(64 * W, 2) void k_shared(SharedArgs a)
         const int row = wrow0 + 16 * n + (lane & 15);
         row_at[n] = row < p.rows ? a.q + ((p.first + row / a.rep) * a.Hq + kvh * a.rep + row % a.rep) * (HD * ESIZE<QT>) : nullptr;
     }
-    const int none = wrow0 < p.rows ? 0 : INT32_MIN;           // (a wavefront without rows only stages)
+    const bool any = wrow0 < p.rows && wave * COLS * 16 < R;   // (a wavefront without rows only brings tiles)
     int done = 0;                                              // tiles of the classes before
-    auto walk = [&](auto bits) __attribute__((always_inline)) {
+    auto walk_class = [&](auto bits) __attribute__((always_inline)) {
         constexpr int BITS = decltype(bits)::value, c = BITS == 2 ? 0 : (BITS == 4 ? 1 : 2);
-        using Order = std::conditional_t<BITS == 8, Near, Far>;
         const int t0 = lo > done ? lo - done : 0, t1 = hi - done < tiles[c] ? hi - done : tiles[c];
         done += tiles[c];
         if (t0 >= t1) return;
-        const int64_t tok0 = kv.cls_off[c][p.seq], slots = (len[c] + 31) / 32 * 32;
 #pragma unroll
         for (int n = 0; n < COLS; n++) {
             r.limit[n] = len[c];
@@ -820,37 +945,32 @@ __global__ __launch_bounds__(64 * W, 2) void k_shared(SharedArgs a)
             if constexpr (std::is_same_v<QT, Bf16>) r.scale[n] = a.scale * query_as_f16<HD>(q, n);
             if constexpr (PIPED) order_query<BITS, HD>(q, n);
         }
-        Packed<HD, BITS, W> tile;
-        __syncthreads();                                       // (whatever was in LDS before has been read)
-        tile.load(kv, kvh, tok0 + t0 * KEYS, slots - t0 * KEYS);
         if constexpr (PIPED) {
-            constexpr int N = TILE_BYTES<CT, HD>;
-            auto k_of = [&](int t) { return (Lds4)((Lds)s_k + (t & 1) * N); };
-            auto v_of = [&](int t) { return (Lds4)((Lds)s_v + (t & 1) * N); };
-            tile.stage(k_of(t0), v_of(t0));
-            if (t0 + 1 < t1) tile.load(kv, kvh, tok0 + (t0 + 1) * KEYS, slots - (t0 + 1) * KEYS);
-            __syncthreads();
-            for (int t = t0; t < t1; t++) {
-                if (t + 1 < t1) tile.stage(k_of(t + 1), v_of(t + 1));
-                if (t + 2 < t1) tile.load(kv, kvh, tok0 + (t + 2) * KEYS, slots - (t + 2) * KEYS);
-                __builtin_amdgcn_sched_barrier(0);             // (the loads go out here)
-                attend_staged<CT, HD, Order>(r, q, k_of(t), v_of(t), t * KEYS, len[c] + none, len[c] + none);
-                __syncthreads();
-            }
+            walk_packed<HD, BITS, SPLIT>(r, q, kv, kvh, kv.cls_off[c][p.seq], len[c], t0, t1, (Lds)s_k, (Lds)s_v);
         } else {
+            PackedKeys<HD, BITS, 32> keys(kv, kvh, kv.cls_off[c][p.seq], 0);
+            PackedValues<HD, BITS, 32> values(kv, kvh, kv.cls_off[c][p.seq], 0);
+            const bool brings_keys = this_wave() < 2;
+            auto load = [&](int t) {
+                if (brings_keys) keys.load(t);
+                else values.load(t);
+            };
+            __syncthreads();                                   // (whatever was in LDS before has been read)
+            load(t0);
             for (int t = t0; t < t1; t++) {
-                tile.stage_f32((Lds4)s_k, (Lds4)s_v);
+                if (brings_keys) keys.stage_f32((Lds4)s_k);
+                else values.stage_f32((Lds4)s_v);
                 __syncthreads();
-                if (t + 1 < t1) tile.load(kv, kvh, tok0 + (t + 1) * KEYS, slots - (t + 1) * KEYS);
+                if (t + 1 < t1) load(t + 1);
                 __builtin_amdgcn_sched_barrier(0);
-                attend_staged<CT, HD, Natural>(r, q, (Lds4)s_k, (Lds4)s_v, t * KEYS, len[c] + none, len[c] + none);
+                attend_f32<HD>(r, q, (Lds4)s_k, (Lds4)s_v, t * TK, len[c], any ? len[c] : 0);
                 __syncthreads();
             }
         }
     };
-    walk(std::integral_constant<int, 2>());
-    walk(std::integral_constant<int, 4>());
-    walk(std::integral_constant<int, 8>());
+    walk_class(std::integral_constant<int, 2>());
+    walk_class(std::integral_constant<int, 4>());
+    walk_class(std::integral_constant<int, 8>());
     if (hi > done) {
         const int t0 = lo > done ? lo - done : 0, t1 = hi - done;
 #pragma unroll
@@ -863,18 +983,18 @@ __global__ __launch_bounds__(64 * W, 2) void k_shared(SharedArgs a)
         const char* k = static_cast<const char*>(kv.k16) + row0 * stride + kvh * (HD * 2);
         const char* v = static_cast<const char*>(kv.v16) + row0 * stride + kvh * (HD * 2);
         if constexpr (PIPED) {
-            walk_rows<QT, HD, W, KEYS>(r, q, k, v, stride, stride, len[3], t0, t1, len[3] + none, len[3] + none, (Lds)s_k, (Lds)s_v);
+            walk_rows<QT, HD, SPLIT>(r, q, k, v, stride, stride, len[3], t0, t1, len[3], (Lds)s_k, (Lds)s_v);
         } else {
             for (int t = t0; t < t1; t++) {
-                const int key0 = t * KEYS;
+                const int key0 = t * TK;
                 __syncthreads();
-                stage_rows<F16, HD, W>(k + key0 * stride, v + key0 * stride, stride, stride, len[3] - key0, (Lds4)s_k, (Lds4)s_v);
+                stage_rows<F16, HD>(k + key0 * stride, v + key0 * stride, stride, stride, len[3] - key0, (Lds4)s_k, (Lds4)s_v);
                 __syncthreads();
-                attend_staged<CT, HD, Natural>(r, q, (Lds4)s_k, (Lds4)s_v, key0, len[3] + none, len[3] + none);
+                attend_f32<HD>(r, q, (Lds4)s_k, (Lds4)s_v, key0, len[3], any ? len[3] : 0);
             }
         }
     }
-    store_rows<QT, HD>(r, p, a.rep, a.Hq, kvh, wave, own ? a.splits + split : split, a.splits + a.own_splits, a.out);
+    if (any) store_rows<QT, HD>(r, p, a.rep, a.Hq, kvh, wave, own ? a.splits + split : split, a.splits + a.own_splits, a.out);
 }
 
 // ---- the parts' merge ----------------------------------------------------------------------------------------------------
@@ -979,18 +1099,33 @@ int auto_splits_of(int64_t workgroups, int64_t max_keys, int want, int keys)
 
 size_t partials_bytes(int64_t rows, int hd, int parts) { return wq_align256((size_t)rows * parts * (hd + 2) * sizeof(float)); }
 
-// Wavefronts of a workgroup over shared caches: what is staged serves up to 256 rows, if there are that many
-int shared_waves(int B, int rep, int q_dtype) { return q_dtype != WQ_F32 && (int64_t)B * rep > 128 ? 8 : 4; }
+// Query rows of a workgroup
+int rows_of(int64_t q_rows, int rep, int dtype) { return dtype != WQ_F32 && q_rows * rep > 128 ? 256 : 128; }
+
+template <typename CT>
+auto prefill_kernel(int hd, bool split) -> void (*)(PrefillArgs)
+{
+    if constexpr (!std::is_same_v<CT, F32>)
+        if (split) return hd == 128 ? k_prefill<CT, 128, true> : k_prefill<CT, 64, true>;
+    return hd == 128 ? k_prefill<CT, 128, false> : k_prefill<CT, 64, false>;
+}
+template <typename QT>
+auto shared_kernel(int hd, bool split) -> void (*)(SharedArgs)
+{
+    if constexpr (!std::is_same_v<QT, F32>)
+        if (split) return hd == 128 ? k_shared<QT, 128, true> : k_shared<QT, 64, true>;
+    return hd == 128 ? k_shared<QT, 128, false> : k_shared<QT, 64, false>;
+}
 
 // Longer own caches have a decode launch of their own
 constexpr int64_t OWN_INSIDE = 2048;
 
 }  // namespace
 
-int wq_prefill_splits(int64_t total_q, int B, int Hq, int Hkv, int64_t max_kv_rows)
+int wq_prefill_splits(int64_t total_q, int B, int Hq, int Hkv, int dtype, int64_t max_kv_rows)
 {
-    constexpr int ROWS = PREFILL_WAVES * COLS * 16;
-    return auto_splits_of(tiles_of(total_q, Hq / Hkv, 0, ROWS) * Hkv + (int64_t)Hkv * (total_q < B ? total_q : B), max_kv_rows, 512, 256);
+    const int rep = Hq / Hkv, rows = rows_of((total_q + B - 1) / B, rep, dtype);
+    return auto_splits_of(tiles_of(total_q, rep, 0, rows) * Hkv + (int64_t)Hkv * (total_q < B ? total_q : B), max_kv_rows, 256, 64);
 }
 size_t wq_prefill_ws_bytes(int64_t total_q, int Hq, int hd, int splits)
 {
@@ -1000,8 +1135,7 @@ size_t wq_prefill_ws_bytes(int64_t total_q, int Hq, int hd, int splits)
 WqSharedPlan wq_shared_plan(int B, int P, int Hq, int Hkv, int hd, int q_dtype, int64_t max_prefix_tokens, int64_t max_own_tokens, bool own, int num_splits)
 {
     WqSharedPlan s;
-    const int rep = Hq / Hkv, waves = shared_waves(B, rep, q_dtype);
-    s.splits = num_splits > 0 ? num_splits : auto_splits_of(tiles_of(B, rep, P, waves * COLS * 16) * Hkv, max_prefix_tokens, 2048 / waves, 256);
+    s.splits = num_splits > 0 ? num_splits : auto_splits_of(tiles_of(B, Hq / Hkv, P, rows_of(B, Hq / Hkv, q_dtype)) * Hkv, max_prefix_tokens, 256, 64);
     s.own_inside = own && max_own_tokens <= OWN_INSIDE;
     s.own_splits = s.own_inside ? auto_splits_of((int64_t)B * Hkv, max_own_tokens, 256, 256) : 0;
     const int64_t rows = (int64_t)B * Hq;
@@ -1024,11 +1158,11 @@ int wq_launch_prefill(wq_ctx* ctx, const WqPrefill& f)
     a.out.out = f.out, a.out.lse = f.lse;
     a.out.part = reinterpret_cast<float*>(ctx->ws + WQ_WS_HEADER);
     a.out.part_ml = a.out.part + f.total_q * f.Hq * f.splits * f.hd;
-    const dim3 grid((unsigned)(f.Hkv * tiles_of(f.total_q, a.rep, f.B, PREFILL_WAVES * COLS * 16)), (unsigned)f.splits);
-    void (*kernel)(PrefillArgs) = f.dtype == WQ_F32 ? (f.hd == 128 ? k_prefill<F32, 128> : k_prefill<F32, 64>)
-                                : f.dtype == WQ_BF16 ? (f.hd == 128 ? k_prefill<Bf16, 128> : k_prefill<Bf16, 64>)
-                                                     : (f.hd == 128 ? k_prefill<F16, 128> : k_prefill<F16, 64>);
-    hipLaunchKernelGGL(kernel, grid, dim3(64 * PREFILL_WAVES), 0, ctx->stream, a);
+    const int rows = rows_of((f.total_q + f.B - 1) / f.B, a.rep, f.dtype);
+    const dim3 grid((unsigned)(f.Hkv * tiles_of(f.total_q, a.rep, f.B, rows)), (unsigned)f.splits);
+    void (*const kernel)(PrefillArgs) = f.dtype == WQ_F32 ? prefill_kernel<F32>(f.hd, false) : f.dtype == WQ_BF16 ? prefill_kernel<Bf16>(f.hd, rows == 128)
+                                                                                                          : prefill_kernel<F16>(f.hd, rows == 128);
+    hipLaunchKernelGGL(kernel, grid, dim3(f.dtype == WQ_F32 ? 256 : 512), 0, ctx->stream, a);
     if (f.splits > 1) combine(ctx, CombineArgs{f.total_q * f.Hq, f.Hq, f.splits, f.dtype, f.q_off, f.B, f.splits, true, nullptr, nullptr, a.out}, f.hd);
     WQ_HIP_CHECK(ctx, hipGetLastError());
     return WQ_OK;
@@ -1040,12 +1174,12 @@ int wq_launch_shared(wq_ctx* ctx, const WqShared& f)
 {
     const wq_packed_kv* kv = f.prefix;
     const int64_t rows = (int64_t)f.B * f.Hq;
-    const int waves = shared_waves(f.B, f.Hq / kv->Hkv, f.q_dtype);
+    const int tile_rows = rows_of(f.B, f.Hq / kv->Hkv, f.q_dtype);
     SharedArgs a;
     a.q = static_cast<const char*>(f.q);
     a.req_off = f.req_off;
     a.B = f.B, a.P = kv->B, a.Hq = f.Hq, a.rep = f.Hq / kv->Hkv;
-    a.units = (int)(kv->Hkv * tiles_of(f.B, a.rep, a.P, waves * COLS * 16));
+    a.units = (int)(kv->Hkv * tiles_of(f.B, a.rep, a.P, tile_rows));
     a.splits = f.plan.splits, a.own_splits = f.plan.own_splits;
     a.scale = f.sm_scale * LOG2E;
     a.kv = *kv;
@@ -1065,13 +1199,9 @@ int wq_launch_shared(wq_ctx* ctx, const WqShared& f)
         if (rc != WQ_OK) return rc;
     }
     const dim3 grid((unsigned)(a.units * a.splits + f.B * kv->Hkv * a.own_splits));
-    void (*kernel)(SharedArgs);
-    if (f.q_dtype == WQ_F32) kernel = kv->hd == 128 ? k_shared<F32, 128, 4> : k_shared<F32, 64, 4>;
-    else if (f.q_dtype == WQ_BF16 && waves == 4) kernel = kv->hd == 128 ? k_shared<Bf16, 128, 4> : k_shared<Bf16, 64, 4>;
-    else if (f.q_dtype == WQ_BF16) kernel = kv->hd == 128 ? k_shared<Bf16, 128, 8> : k_shared<Bf16, 64, 8>;
-    else if (waves == 4) kernel = kv->hd == 128 ? k_shared<F16, 128, 4> : k_shared<F16, 64, 4>;
-    else kernel = kv->hd == 128 ? k_shared<F16, 128, 8> : k_shared<F16, 64, 8>;
-    hipLaunchKernelGGL(kernel, grid, dim3(64 * waves), 0, ctx->stream, a);
+    void (*const kernel)(SharedArgs) = f.q_dtype == WQ_F32 ? shared_kernel<F32>(kv->hd, false) : f.q_dtype == WQ_BF16 ? shared_kernel<Bf16>(kv->hd, tile_rows == 128)
+                                                                                                              : shared_kernel<F16>(kv->hd, tile_rows == 128);
+    hipLaunchKernelGGL(kernel, grid, dim3(f.q_dtype == WQ_F32 ? 256 : 512), 0, ctx->stream, a);
     combine(ctx, CombineArgs{rows, f.Hq, parts, f.q_dtype, f.req_off, a.P, a.splits, false, own_out, own_lse, a.out}, kv->hd);
     WQ_HIP_CHECK(ctx, hipGetLastError());
     return WQ_OK;

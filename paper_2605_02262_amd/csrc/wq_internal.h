@@ -194,7 +194,7 @@ struct WqPrefill {
     void* out;
     float* lse;
 };
-int wq_prefill_splits(int64_t total_q, int B, int Hq, int Hkv, int64_t max_kv_rows);
+int wq_prefill_splits(int64_t total_q, int B, int Hq, int Hkv, int dtype, int64_t max_kv_rows);
 size_t wq_prefill_ws_bytes(int64_t total_q, int Hq, int hd, int splits);
 int wq_launch_prefill(wq_ctx* ctx, const WqPrefill& f);
 
