@@ -520,9 +520,9 @@ int wq_prefill_attention(wq_ctx* ctx, const void* q, int64_t q_stride, const voi
 size_t wq_shared_workspace_bytes(int B, int P, int Hq, int Hkv, int hd, int64_t max_prefix_tokens, int64_t max_own_tokens, int num_splits)
 {
     if (B <= 0 || P <= 0 || Hq <= 0 || Hkv <= 0 || hd <= 0 || Hq % Hkv != 0) return WQ_WS_HEADER;
-    // (own caches only add to it)
-    const size_t a = wq_shared_plan(B, P, Hq, Hkv, hd, WQ_F32, max_prefix_tokens, max_own_tokens, true, num_splits).bytes;
-    const size_t b = wq_shared_plan(B, P, Hq, Hkv, hd, WQ_BF16, max_prefix_tokens, max_own_tokens, true, num_splits).bytes;
+    // (own caches that need a decode launch take the most)
+    const size_t a = wq_shared_plan(B, P, Hq, Hkv, hd, WQ_F32, max_prefix_tokens, max_own_tokens, true, true, num_splits).bytes;
+    const size_t b = wq_shared_plan(B, P, Hq, Hkv, hd, WQ_BF16, max_prefix_tokens, max_own_tokens, true, true, num_splits).bytes;
     return WQ_WS_HEADER + (a > b ? a : b);
 }
 
@@ -555,15 +555,16 @@ int wq_decode_attention_shared(wq_ctx* ctx, const void* q, int q_dtype, int B, i
     }
     if (B == 0) return WQ_OK;
     if (!q || !out || !req_off) return wq_fail(ctx, WQ_ERR_ARG, "NULL q, out or req_off");
-    const WqSharedPlan plan = wq_shared_plan(B, prefix->B, Hq, prefix->Hkv, prefix->hd, q_dtype, max_prefix_tokens, max_own_tokens, own != nullptr, num_splits);
-    if (((int64_t)B * (Hq / prefix->Hkv) / 64 + prefix->B) * prefix->Hkv * plan.splits + (int64_t)B * prefix->Hkv * plan.own_splits > INT32_MAX)
+    const WqSharedPlan plan = wq_shared_plan(B, prefix->B, Hq, prefix->Hkv, prefix->hd, q_dtype, max_prefix_tokens, max_own_tokens, own != nullptr,
+                                             own && own->cap[0] + own->cap[1] + own->cap[2] > 0, num_splits);
+    if (((int64_t)B * (Hq / prefix->Hkv) / 64 + prefix->B) * prefix->Hkv * plan.splits > INT32_MAX || (int64_t)B * prefix->Hkv > INT32_MAX)
         return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "too many workgroups");
     if (!ctx->ws || ctx->ws_bytes < WQ_WS_HEADER + plan.bytes)
         return wq_fail(ctx, WQ_ERR_WORKSPACE, "workspace too small for %d splits of %d requests", plan.splits, B);
     // an fp32 query's own cache in fp32 arithmetic, like its shared one
     const int algo = q_dtype == WQ_F32 ? WQ_DECODE_GENERIC : WQ_DECODE_AUTO;
     int decode_splits = 0;
-    if (own && !plan.own_inside) {
+    if (plan.own_decode) {
         int64_t longest = 0;
         rc = check_decode(ctx, q, q_dtype, B, Hq, own, sm_scale, &decode_splits, max_own_tokens, algo, static_cast<const float*>(out), &longest);
         if (rc != WQ_OK) return rc;

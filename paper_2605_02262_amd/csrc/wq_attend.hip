@@ -293,8 +293,10 @@ __device__ __forceinline__ void take_turns(Rows<HD>& r, const Query<CT, HD>& q, 
     }
 #pragma unroll 1
     for (int t = t0; t < t1; t++) {
+        __builtin_amdgcn_s_setprio(3);
         multiply_keys<CT, HD>(s, q, [&](int kt, int st) { return keys(t, kt, st); });
         multiply_values<CT, HD>(r, p, [&](int vs, int ct) { return values(t - 1, vs, ct); });
+        __builtin_amdgcn_s_setprio(0);
         settle();
         form_weights<CT, HD, Order>(r, s, p, t * KEYS<CT>, (t + 1) * KEYS<CT> > least);
         if (!SPLIT && t + 1 < t1) {
@@ -881,14 +883,13 @@ struct SharedArgs {
     const int32_t* req_off;
     int B, P, Hq, rep;
     int units, splits;                         // (tile of rows, KV head) pairs of the shared caches, and the parts that each is cut into
-    int own_splits;                            // parts of a request's own cache: B * Hkv * own_splits workgroups more (0: none)
     float scale;
-    wq_packed_kv kv, own;
+    wq_packed_kv kv;
     Out out;
 };
 
 // QT: the query's type; packed tokens are walked in fp16 (fp32 for fp32 queries), 16-bit rows in the
-// cache's own type.  A request's own cache is a unit of rep rows.
+// cache's own type.
 template <typename QT, int HD, bool SPLIT>
 __global__ __launch_bounds__(64 * WAVES<QT>, 2) void k_shared(SharedArgs a)
 {
@@ -897,17 +898,10 @@ __global__ __launch_bounds__(64 * WAVES<QT>, 2) void k_shared(SharedArgs a)
     constexpr int BYTES = TILE_BYTES<CT, HD> * (1 + PIPED), R = ROWS<QT, SPLIT>, TK = KEYS<QT>;
     __shared__ __align__(16) char s_k[BYTES], s_v[BYTES];
     const int Hkv = a.kv.Hkv, wave = this_wave(), lane = threadIdx.x & 63;
-    const bool own = (int)blockIdx.x >= a.units * a.splits;
-    const int at = own ? (int)blockIdx.x - a.units * a.splits : (int)blockIdx.x;
-    const int units = own ? a.B * Hkv : a.units, unit = at % units, split = at / units, splits = own ? a.own_splits : a.splits;
-    const int kvh = unit % Hkv;
+    const wq_packed_kv& kv = a.kv;
+    const int unit = (int)blockIdx.x % a.units, split = (int)blockIdx.x / a.units, kvh = unit % Hkv;
     Place p;
-    if (own) {
-        p.seq = unit / Hkv, p.first = p.seq, p.row0 = 0, p.rows = a.rep;
-    } else if (!find_place<R>(a.req_off, a.P, a.rep, a.B, unit / Hkv, p)) {
-        return;
-    }
-    const wq_packed_kv& kv = own ? a.own : a.kv;
+    if (!find_place<R>(a.req_off, a.P, a.rep, a.B, unit / Hkv, p)) return;
     int tiles[4], all = 0, len[4];
 #pragma unroll
     for (int c = 0; c < 4; c++) {
@@ -917,7 +911,7 @@ __global__ __launch_bounds__(64 * WAVES<QT>, 2) void k_shared(SharedArgs a)
         tiles[c] = len[c] > 0 ? (len[c] + TK - 1) / TK : 0;
         all += tiles[c];
     }
-    const int lo = (int)((int64_t)split * all / splits), hi = (int)((int64_t)(split + 1) * all / splits);
+    const int lo = (int)((int64_t)split * all / a.splits), hi = (int)((int64_t)(split + 1) * all / a.splits);
 
     if constexpr (PIPED) __builtin_amdgcn_s_setreg(1 | 23 << 6, 1);        // MODE.FP16_OVFL: an expanded value past fp16's range becomes its largest one
     Rows<HD> r;
@@ -994,21 +988,10 @@ __global__ __launch_bounds__(64 * WAVES<QT>, 2) void k_shared(SharedArgs a)
             }
         }
     }
-    if (any) store_rows<QT, HD>(r, p, a.rep, a.Hq, kvh, wave, own ? a.splits + split : split, a.splits + a.own_splits, a.out);
+    if (any) store_rows<QT, HD>(r, p, a.rep, a.Hq, kvh, wave, split, a.splits, a.out);
 }
 
 // ---- the parts' merge ----------------------------------------------------------------------------------------------------
-struct CombineArgs {
-    int64_t rows;              // (q row, head) pairs
-    int Hq, parts, dtype;
-    const int32_t* off;        // the first `grouped` parts of q rows outside off[0] .. off[nseq] - 1 were not written,
-    int nseq, grouped;
-    bool leave;                // ... and such rows are left as they were
-    const float* own_out;      // NULL, or one more part, normalised [rows][hd], with its log-sum-exp
-    const float* own_lse;
-    Out out;
-};
-
 __device__ __forceinline__ float wave_max(float x)
 {
 #pragma unroll
@@ -1022,67 +1005,245 @@ __device__ __forceinline__ float wave_sum(float x)
     return x;
 }
 
-// A wavefront per row.  A lane finds the weights of two parts; then HD / 4 lanes take a part's numerators, 16 bytes each, the wavefront's
-// groups of lanes every second (fourth) part, four in flight: part by part the loads' round trips were the whole call.
+// Sum over the parts of a row, weights w (lane s: part s): HD / 4 lanes take a part's numerators, 16 bytes each, the wavefront's groups of lanes
+// every second (fourth) part, FLIGHT in flight (one after the other the loads' round trips were the whole call).  This lane's
+// channels are 4 (lane % (HD / 4)) ..; the groups' sums are still apart.
 template <int HD>
-__global__ __launch_bounds__(256) void k_attend_combine(CombineArgs a)
+__device__ __forceinline__ f4 sum_of_parts(const float* part, int parts, float w)
 {
-    constexpr int LANES = HD / 4, GROUPS = 64 / LANES, FLIGHT = 4;
-    const int64_t row = (int64_t)blockIdx.x * 4 + this_wave();
-    if (row >= a.rows) return;
-    const int lane = threadIdx.x & 63, group = lane / LANES, c = lane % LANES;
-    const int64_t b = row / a.Hq;
-    const bool grouped = b >= a.off[0] && b < a.off[a.nseq];
-    if (!grouped && a.leave) return;
-    const int from = grouped ? 0 : a.grouped;
-    float m[2], l[2], w[2];
-#pragma unroll
-    for (int i = 0; i < 2; i++) {
-        const int s = 64 * i + lane;
-        const bool have = s >= from && s < a.parts;
-        m[i] = have ? a.out.part_ml[(row * a.parts + s) * 2] : -INFINITY;
-        l[i] = have ? a.out.part_ml[(row * a.parts + s) * 2 + 1] : 0.f;
-    }
-    const float own = a.own_lse ? a.own_lse[row] * LOG2E : -INFINITY;
-    const float M = fmaxf(wave_max(fmaxf(m[0], m[1])), own);
-    const float base = M == -INFINITY ? 0.f : M;
-#pragma unroll
-    for (int i = 0; i < 2; i++) w[i] = __builtin_amdgcn_exp2f(m[i] - base);
-    const float w_own = __builtin_amdgcn_exp2f(own - base);
-    const float L = wave_sum(l[0] * w[0] + l[1] * w[1]) + w_own;
+    constexpr int LANES = HD / 4, GROUPS = 64 / LANES, FLIGHT = 16;
+    const int lane = threadIdx.x & 63, group = lane / LANES;
+    const f4* at = reinterpret_cast<const f4*>(part) + lane % LANES;
     f4 x = {0.f, 0.f, 0.f, 0.f};
-    const f4* part = reinterpret_cast<const f4*>(a.out.part) + row * a.parts * LANES + c;
-    for (int s0 = from; s0 < a.parts; s0 += GROUPS * FLIGHT) {
+    for (int s0 = 0; s0 < parts; s0 += GROUPS * FLIGHT) {
         f4 y[FLIGHT];
-        float by[FLIGHT];
 #pragma unroll
         for (int i = 0; i < FLIGHT; i++) {
             const int s = s0 + i * GROUPS + group;
-            y[i] = s < a.parts ? part[(int64_t)s * LANES] : f4{0.f, 0.f, 0.f, 0.f};
-            const float low = __shfl(w[0], s & 63, 64), high = __shfl(w[1], s & 63, 64);
-            by[i] = s < 64 ? low : high;
+            y[i] = s < parts ? at[(int64_t)s * LANES] : f4{0.f, 0.f, 0.f, 0.f};
         }
 #pragma unroll
-        for (int i = 0; i < FLIGHT; i++) x += y[i] * (s0 + i * GROUPS + group < a.parts ? by[i] : 0.f);
+        for (int i = 0; i < FLIGHT; i++) {
+            const int s = s0 + i * GROUPS + group;
+            const float by = __shfl(w, s & 63, 64);
+            x += y[i] * (s < parts ? by : 0.f);
+        }
     }
+    return x;
+}
+template <int HD>
+__device__ __forceinline__ f4 sum_of_groups(f4 x)
+{
 #pragma unroll
-    for (int o = LANES; o < 64; o *= 2)
+    for (int o = HD / 4; o < 64; o *= 2)
 #pragma unroll
         for (int i = 0; i < 4; i++) x[i] += __shfl_xor(x[i], o, 64);
-    if (a.own_out && own > -INFINITY) x += reinterpret_cast<const f4*>(a.own_out)[row * LANES + c] * w_own;
+    return x;
+}
+// Row `row` of the result from its numerators and the sum of weights L, relative to 2^M
+template <int HD>
+__device__ __forceinline__ void store_merged(const Out& out, int dtype, int64_t row, f4 x, float M, float L)
+{
+    const int lane = threadIdx.x & 63;
     x *= L > 0.f ? 1.f / L : 0.f;
-    if (group == 0) {
-        const int64_t at = row * LANES + c;
-        if (a.dtype == WQ_F32) static_cast<f4*>(a.out.out)[at] = x;
-        else if (a.dtype == WQ_BF16) static_cast<uint2*>(a.out.out)[at] = make_uint2(pack2(x[0], x[1], Bf16()), pack2(x[2], x[3], Bf16()));
-        else static_cast<uint2*>(a.out.out)[at] = make_uint2(pack2(x[0], x[1], F16()), pack2(x[2], x[3], F16()));
+    if (lane < HD / 4) {
+        const int64_t at = row * (HD / 4) + lane;
+        if (dtype == WQ_F32) static_cast<f4*>(out.out)[at] = x;
+        else if (dtype == WQ_BF16) static_cast<uint2*>(out.out)[at] = make_uint2(pack2(x[0], x[1], Bf16()), pack2(x[2], x[3], Bf16()));
+        else static_cast<uint2*>(out.out)[at] = make_uint2(pack2(x[0], x[1], F16()), pack2(x[2], x[3], F16()));
     }
-    if (a.out.lse && lane == 0) a.out.lse[row] = L > 0.f ? (M + log2f(L)) * 0.69314718055994530942f : -INFINITY;
+    if (out.lse && lane == 0) out.lse[row] = L > 0.f ? (M + log2f(L)) * 0.69314718055994530942f : -INFINITY;
 }
 
-void combine(wq_ctx* ctx, const CombineArgs& c, int hd)
+struct MergeArgs {
+    int64_t rows;              // (q row, head) pairs
+    int Hq, parts, dtype;
+    const int32_t* q_off;
+    int nseq;
+    Out out;
+};
+
+// wq_prefill_attention: a wavefront per row.  Rows that belong to no sequence are left as they were.
+template <int HD>
+__global__ __launch_bounds__(256) void k_merge(MergeArgs a)
 {
-    hipLaunchKernelGGL(hd == 128 ? k_attend_combine<128> : k_attend_combine<64>, dim3((unsigned)((c.rows + 3) / 4)), dim3(256), 0, ctx->stream, c);
+    const int64_t row = (int64_t)blockIdx.x * 4 + this_wave();
+    if (row >= a.rows) return;
+    const int lane = threadIdx.x & 63;
+    const int64_t b = row / a.Hq;
+    if (b < a.q_off[0] || b >= a.q_off[a.nseq]) return;
+    const float m = lane < a.parts ? a.out.part_ml[(row * a.parts + lane) * 2] : -INFINITY;
+    const float l = lane < a.parts ? a.out.part_ml[(row * a.parts + lane) * 2 + 1] : 0.f;
+    const float M = wave_max(m), w = __builtin_amdgcn_exp2f(m - (M == -INFINITY ? 0.f : M));
+    const f4 x = sum_of_groups<HD>(sum_of_parts<HD>(a.out.part + row * a.parts * HD, a.parts, w));
+    store_merged<HD>(a.out, a.dtype, row, x, M, wave_sum(l * w));
+}
+
+// ---- wq_decode_attention_shared: the requests' own 16-bit rows, and the merge ------------------------------------------------
+struct FinishArgs {
+    const char* q;
+    const int32_t* req_off;
+    int P, Hq, rep, parts, dtype;
+    float scale;
+    const char *k, *v;         // own 16-bit rows [row][Hkv][hd], or NULL
+    const int32_t *off16, *len16;
+    int64_t cap16;
+    const float* own_out;      // or: one more part, normalised [B * Hq][hd], with its log-sum-exp
+    const float* own_lse;
+    Out out;
+};
+
+// A wavefront's numerators, reference and sum over its share of a request's own rows: 32 keys of every 256.  Keys come straight into the
+// operands' registers (nothing else reads them), values row by row into this wavefront's own piece of LDS (`tile`), as in Direct.
+template <typename QT, int HD>
+__device__ __forceinline__ void own_rows(const FinishArgs& a, const char* q_row, const char* k, const char* v, int64_t stride, int len, Lds tile, f4 (&o)[HD / 16],
+                                         float& ref, float& sum)
+{
+    constexpr int ST = STEPS<QT, HD>, CT16 = HD / 16, PIECES = HD / 8, PER_LOAD = 64 / PIECES, LOADS = 32 / PER_LOAD;
+    using D = Direct<HD>;
+    const int lane = threadIdx.x & 63, m = lane & 15, j = lane >> 4;
+    Query<QT, HD> q;                                           // (fp32: read again at each use, from L1; 128 registers would not be left)
+    if constexpr (!std::is_same_v<QT, F32>) load_query<QT, HD>(q, 0, q_row);
+    ref = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int ct = 0; ct < CT16; ct++) o[ct] = f4{0.f, 0.f, 0.f, 0.f};
+    for (int key0 = 32 * this_wave(); key0 < len; key0 += 256) {
+        const int left = len - key0;                           // (the last row is read again for the rest: its weights are zero)
+#pragma unroll
+        for (int i = 0; i < LOADS; i++) {
+            const int r = i * PER_LOAD + lane / PIECES, piece = (lane % PIECES) ^ (D::swizzle(r) * 2 & (PIECES - 1));
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(v + (key0 + (r < left ? r : left - 1)) * stride + 16 * piece),
+                                             (__attribute__((address_space(3))) void*)(tile + i * 1024), 16, 0, 0);
+        }
+        f4 s[2];
+#pragma unroll
+        for (int t = 0; t < 2; t++) {
+            const int r = 16 * t + m;
+            const char* row = k + (key0 + (r < left ? r : left - 1)) * stride;
+            s[t] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int st = 0; st < ST; st++) {
+                if constexpr (std::is_same_v<QT, F32>) {
+                    const u4 y = q_row ? *reinterpret_cast<const u4*>(q_row + (4 * st + j) * 16) : u4{0, 0, 0, 0};
+                    s[t] = product<F32>(row_piece<F16>(row + (4 * st + j) * 8), y, s[t]);
+                } else {
+                    s[t] = product<QT>(*reinterpret_cast<const u4*>(row + (4 * st + j) * 16), q[0][st], s[t]);
+                }
+            }
+        }
+        float most = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < 2; t++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                s[t][i] = 16 * t + 4 * j + i < left ? s[t][i] * a.scale : -INFINITY;
+                most = fmaxf(most, s[t][i]);
+            }
+        const float next = fmaxf(ref, max_of_column(most));    // (finite: a wavefront's first key is there)
+        const float by = __builtin_amdgcn_exp2f(ref - next);
+        ref = next, sum *= by;
+        float w[8];
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            w[e] = __builtin_amdgcn_exp2f(s[e >> 2][e & 3] - ref + SHIFT);
+            sum += w[e];
+        }
+        __builtin_amdgcn_s_waitcnt(0x0F70);                    // vmcnt(0): the values are in LDS
+        asm volatile("" ::: "memory");
+        if constexpr (std::is_same_v<QT, F32>) {
+#pragma unroll
+            for (int ct = 0; ct < CT16; ct++) {
+                o[ct] *= by;
+#pragma unroll
+                for (int t = 0; t < 2; t++) {
+                    u4 x, p;
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const int r = 16 * t + 4 * j + i, ch = 16 * ct + m;
+                        const uint16_t h = *(const __attribute__((address_space(3))) uint16_t*)(tile + r * (2 * HD) + 16 * ((ch >> 3) ^ (D::swizzle(r) * 2 & (PIECES - 1))) + 2 * (ch & 7));
+                        x[i] = __float_as_uint(wq_f16_bits_to_float(h)), p[i] = __float_as_uint(w[4 * t + i]);
+                    }
+                    o[ct] = product<F32>(x, p, o[ct]);
+                }
+            }
+        } else {
+            u4 p;
+#pragma unroll
+            for (int e = 0; e < 4; e++) p[e] = pack2(w[2 * e], w[2 * e + 1], QT());
+            const D rows(stride, stride);
+#pragma unroll
+            for (int ct = 0; ct < CT16; ct++) o[ct] = product<QT>(rows.values(tile, 0, ct), p, o[ct] * by);
+        }
+        __builtin_amdgcn_s_waitcnt(0xC07F);                    // lgkmcnt(0): they are out of it again
+        asm volatile("" ::: "memory");
+    }
+    sum = sum_of_column(sum);
+    ref -= SHIFT;
+}
+
+// A workgroup per (request, KV head): eight wavefronts walk the request's own rows, while wavefront 8 + r merges query head r's parts;
+// then each of those takes in what the eight have found.
+template <typename QT, int HD>
+__global__ __launch_bounds__(1024) void k_shared_finish(FinishArgs a)
+{
+    constexpr int W = 8, LANES = HD / 4, GROUPS = 64 / LANES;
+    __shared__ __align__(16) char s_v[W][32 * HD * 2];         // values; then the wavefronts' numerators, [head][hd] fp32
+    __shared__ float s_m[W][WQ_MAX_REP], s_l[W][WQ_MAX_REP];
+    static_assert(WQ_MAX_REP * HD * 4 <= 32 * HD * 2 && WQ_MAX_REP == W, "");
+    const int Hkv = a.Hq / a.rep, b = blockIdx.x / Hkv, kvh = blockIdx.x % Hkv, wave = this_wave(), lane = threadIdx.x & 63;
+    const int64_t row0 = (int64_t)b * a.Hq + kvh * a.rep;
+    int len = 0;
+    if (a.k) {
+        const int64_t room = a.cap16 - a.off16[b];
+        len = a.len16[b];
+        if (len > room) len = (int)room;
+    }
+    const int r = wave - W;
+    const int64_t row = row0 + r;
+    f4 x = {0.f, 0.f, 0.f, 0.f};
+    float m2 = -INFINITY, l2 = 0.f;                            // lanes 0 .. 7: the wavefronts' sums; lane 8: an own part from outside; lane 9: the parts
+    if (wave < W) {
+        if (len > 0) {
+            const int64_t stride = (int64_t)Hkv * HD * 2, first = a.off16[b] * stride + kvh * (HD * 2);
+            f4 o[HD / 16];
+            float ref, sum;
+            const int n = lane & 15;
+            own_rows<QT, HD>(a, n < a.rep ? a.q + (row0 + n) * (HD * ESIZE<QT>) : nullptr, a.k + first, a.v + first, stride, len, (Lds)s_v[wave], o, ref, sum);
+            if (n < a.rep) {
+#pragma unroll
+                for (int ct = 0; ct < HD / 16; ct++) *reinterpret_cast<f4*>(s_v[wave] + (n * HD + 16 * ct + 4 * (lane >> 4)) * 4) = o[ct];
+                if (lane < 16) s_m[wave][n] = ref, s_l[wave][n] = sum;
+            }
+        }
+    } else {
+        const int parts = b >= a.req_off[0] && b < a.req_off[a.P] ? a.parts : 0;
+        float m = -INFINITY, l = 0.f;                          // lane s: part s
+        if (lane < parts) {
+            m = a.out.part_ml[(row * a.parts + lane) * 2];
+            l = a.out.part_ml[(row * a.parts + lane) * 2 + 1];
+        }
+        const float most = wave_max(m), w = __builtin_amdgcn_exp2f(m - (most == -INFINITY ? 0.f : most));
+        x = sum_of_parts<HD>(a.out.part + row * a.parts * HD, parts, w);
+        l = wave_sum(l * w);
+        if (a.own_lse && lane == W) m2 = a.own_lse[row] * LOG2E, l2 = m2 == -INFINITY ? 0.f : 1.f;
+        if (lane == W + 1) m2 = most, l2 = l;
+    }
+    __syncthreads();
+    if (wave < W) return;
+    if (len > 0 && lane < W) m2 = s_m[lane][r], l2 = s_l[lane][r];
+    const float M = wave_max(m2), w2 = __builtin_amdgcn_exp2f(m2 - (M == -INFINITY ? 0.f : M));
+    x *= __shfl(w2, W + 1, 64);
+    if (len > 0) {
+#pragma unroll
+        for (int k = 0; k < W; k += GROUPS) {
+            const int from = k + lane / LANES;
+            const float by = __shfl(w2, from, 64);
+            if (32 * from < len) x += *reinterpret_cast<const f4*>(s_v[from] + (r * HD + 4 * (lane % LANES)) * 4) * by;
+        }
+    }
+    x = sum_of_groups<HD>(x);
+    if (a.own_out) x += reinterpret_cast<const f4*>(a.own_out)[row * LANES + lane % LANES] * __shfl(w2, W, 64);
+    store_merged<HD>(a.out, a.dtype, row, x, M, wave_sum(l2 * w2));
 }
 
 int64_t tiles_of(int64_t total, int rep, int nseq, int rows) { return total * rep / rows + nseq; }
@@ -1117,7 +1278,10 @@ auto shared_kernel(int hd, bool split) -> void (*)(SharedArgs)
     return hd == 128 ? k_shared<QT, 128, false> : k_shared<QT, 64, false>;
 }
 
-// Longer own caches have a decode launch of their own
+template <typename QT>
+auto finish_kernel(int hd) -> void (*)(FinishArgs) { return hd == 128 ? k_shared_finish<QT, 128> : k_shared_finish<QT, 64>; }
+
+// Longer own caches, and those with room for packed tokens, have a decode launch of their own
 constexpr int64_t OWN_INSIDE = 2048;
 
 }  // namespace
@@ -1132,16 +1296,18 @@ size_t wq_prefill_ws_bytes(int64_t total_q, int Hq, int hd, int splits)
     return splits > 1 ? partials_bytes(total_q * Hq, hd, splits) : 0;
 }
 
-WqSharedPlan wq_shared_plan(int B, int P, int Hq, int Hkv, int hd, int q_dtype, int64_t max_prefix_tokens, int64_t max_own_tokens, bool own, int num_splits)
+WqSharedPlan wq_shared_plan(int B, int P, int Hq, int Hkv, int hd, int q_dtype, int64_t max_prefix_tokens, int64_t max_own_tokens, bool own, bool own_packed,
+                            int num_splits)
 {
     WqSharedPlan s;
-    s.splits = num_splits > 0 ? num_splits : auto_splits_of(tiles_of(B, Hq / Hkv, P, rows_of(B, Hq / Hkv, q_dtype)) * Hkv, max_prefix_tokens, 256, 64);
-    s.own_inside = own && max_own_tokens <= OWN_INSIDE;
-    s.own_splits = s.own_inside ? auto_splits_of((int64_t)B * Hkv, max_own_tokens, 256, 256) : 0;
+    s.splits = num_splits > 0 ? num_splits
+                              : auto_splits_of(tiles_of(B, Hq / Hkv, P, rows_of(B, Hq / Hkv, q_dtype)) * Hkv, max_prefix_tokens, 256,
+                                              q_dtype == WQ_F32 ? 32 : 64);
+    s.own_decode = own && (own_packed || max_own_tokens > OWN_INSIDE);
     const int64_t rows = (int64_t)B * Hq;
-    s.decode_bytes = own && !s.own_inside ? wq_decode_ws_bytes(B, Hq, hd, wq_auto_splits(B, Hkv, max_own_tokens)) : 0;
-    s.bytes = s.decode_bytes + partials_bytes(rows, hd, s.splits + s.own_splits);
-    if (own && !s.own_inside) s.bytes += wq_align256(rows * hd * sizeof(float)) + wq_align256(rows * sizeof(float));
+    s.decode_bytes = s.own_decode ? wq_decode_ws_bytes(B, Hq, hd, wq_auto_splits(B, Hkv, max_own_tokens)) : 0;
+    s.bytes = s.decode_bytes + partials_bytes(rows, hd, s.splits);
+    if (s.own_decode) s.bytes += wq_align256(rows * hd * sizeof(float)) + wq_align256(rows * sizeof(float));
     return s;
 }
 
@@ -1163,13 +1329,16 @@ int wq_launch_prefill(wq_ctx* ctx, const WqPrefill& f)
     void (*const kernel)(PrefillArgs) = f.dtype == WQ_F32 ? prefill_kernel<F32>(f.hd, false) : f.dtype == WQ_BF16 ? prefill_kernel<Bf16>(f.hd, rows == 128)
                                                                                                           : prefill_kernel<F16>(f.hd, rows == 128);
     hipLaunchKernelGGL(kernel, grid, dim3(f.dtype == WQ_F32 ? 256 : 512), 0, ctx->stream, a);
-    if (f.splits > 1) combine(ctx, CombineArgs{f.total_q * f.Hq, f.Hq, f.splits, f.dtype, f.q_off, f.B, f.splits, true, nullptr, nullptr, a.out}, f.hd);
+    if (f.splits > 1) {
+        const MergeArgs m = {f.total_q * f.Hq, f.Hq, f.splits, f.dtype, f.q_off, f.B, a.out};
+        hipLaunchKernelGGL(f.hd == 128 ? k_merge<128> : k_merge<64>, dim3((unsigned)((m.rows + 3) / 4)), dim3(256), 0, ctx->stream, m);
+    }
     WQ_HIP_CHECK(ctx, hipGetLastError());
     return WQ_OK;
 }
 
-// The shared caches and, up to OWN_INSIDE tokens, the requests' own ones in one launch; else those in one of wq_decode_attention's
-// kernels.  Then the merge.
+// The shared caches; then the requests' own rows and the merge.  Own caches that this is not for go first, through
+// wq_decode_attention's kernels.
 int wq_launch_shared(wq_ctx* ctx, const WqShared& f)
 {
     const wq_packed_kv* kv = f.prefix;
@@ -1180,29 +1349,39 @@ int wq_launch_shared(wq_ctx* ctx, const WqShared& f)
     a.req_off = f.req_off;
     a.B = f.B, a.P = kv->B, a.Hq = f.Hq, a.rep = f.Hq / kv->Hkv;
     a.units = (int)(kv->Hkv * tiles_of(f.B, a.rep, a.P, tile_rows));
-    a.splits = f.plan.splits, a.own_splits = f.plan.own_splits;
+    a.splits = f.plan.splits;
     a.scale = f.sm_scale * LOG2E;
     a.kv = *kv;
-    a.own = f.plan.own_inside ? *f.own : *kv;
     a.out.out = f.out, a.out.lse = f.lse;
-    const int parts = a.splits + a.own_splits;
+    const int parts = a.splits;
     char* at = ctx->ws + WQ_WS_HEADER + f.plan.decode_bytes;
     a.out.part = reinterpret_cast<float*>(at);
     a.out.part_ml = a.out.part + rows * parts * kv->hd;
     at += partials_bytes(rows, kv->hd, parts);
     float* own_out = nullptr;
     float* own_lse = nullptr;
-    if (f.own && !f.plan.own_inside) {
+    if (f.plan.own_decode) {
         own_out = reinterpret_cast<float*>(at);
         own_lse = reinterpret_cast<float*>(at + wq_align256(rows * kv->hd * sizeof(float)));
         const int rc = wq_launch_decode(ctx, f.q, f.q_dtype, f.B, f.Hq, f.own, f.sm_scale, f.decode_splits, f.decode_algo, own_out, own_lse);
         if (rc != WQ_OK) return rc;
     }
-    const dim3 grid((unsigned)(a.units * a.splits + f.B * kv->Hkv * a.own_splits));
+    const dim3 grid((unsigned)(a.units * a.splits));
     void (*const kernel)(SharedArgs) = f.q_dtype == WQ_F32 ? shared_kernel<F32>(kv->hd, false) : f.q_dtype == WQ_BF16 ? shared_kernel<Bf16>(kv->hd, tile_rows == 128)
                                                                                                               : shared_kernel<F16>(kv->hd, tile_rows == 128);
     hipLaunchKernelGGL(kernel, grid, dim3(f.q_dtype == WQ_F32 ? 256 : 512), 0, ctx->stream, a);
-    combine(ctx, CombineArgs{rows, f.Hq, parts, f.q_dtype, f.req_off, a.P, a.splits, false, own_out, own_lse, a.out}, kv->hd);
+    FinishArgs m;
+    m.q = a.q, m.req_off = f.req_off;
+    m.P = a.P, m.Hq = f.Hq, m.rep = a.rep, m.parts = parts, m.dtype = f.q_dtype;
+    m.scale = a.scale;
+    const bool inside = f.own && !f.plan.own_decode;
+    m.k = inside ? static_cast<const char*>(f.own->k16) : nullptr, m.v = inside ? static_cast<const char*>(f.own->v16) : nullptr;
+    m.off16 = inside ? f.own->off16 : nullptr, m.len16 = inside ? f.own->len16 : nullptr;
+    m.cap16 = inside ? f.own->cap16 : 0;
+    m.own_out = own_out, m.own_lse = own_lse;
+    m.out = a.out;
+    hipLaunchKernelGGL(f.q_dtype == WQ_F32 ? finish_kernel<F32>(kv->hd) : f.q_dtype == WQ_BF16 ? finish_kernel<Bf16>(kv->hd) : finish_kernel<F16>(kv->hd),
+                       dim3((unsigned)(f.B * kv->Hkv)), dim3(64 * (8 + a.rep)), 0, ctx->stream, m);
     WQ_HIP_CHECK(ctx, hipGetLastError());
     return WQ_OK;
 }

@@ -200,11 +200,11 @@ int wq_launch_prefill(wq_ctx* ctx, const WqPrefill& f);
 
 struct WqSharedPlan {
     int splits;                                                   // of the shared caches
-    bool own_inside;                                              // the requests' own caches are part of the same launch
-    int own_splits;                                               // ... cut into so many parts
-    size_t decode_bytes, bytes;                                   // workspace: of the decode launch over them otherwise; in all
+    bool own_decode;                                              // the requests' own caches have a decode launch of their own
+    size_t decode_bytes, bytes;                                   // workspace: of that launch; in all
 };
-WqSharedPlan wq_shared_plan(int B, int P, int Hq, int Hkv, int hd, int q_dtype, int64_t max_prefix_tokens, int64_t max_own_tokens, bool own, int num_splits);
+WqSharedPlan wq_shared_plan(int B, int P, int Hq, int Hkv, int hd, int q_dtype, int64_t max_prefix_tokens, int64_t max_own_tokens, bool own, bool own_packed,
+                            int num_splits);
 struct WqShared {
     const void* q;
     int q_dtype, B, Hq;
