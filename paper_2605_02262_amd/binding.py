@@ -327,11 +327,18 @@ def wq_decode_attention_static(q, kv: PackedKV, sm_scale: float, num_splits: int
 # ------------------------------------------------------------------------------------------------------------
 def _rows(name: str, t: torch.Tensor, like: Optional[torch.Tensor] = None) -> int:
     """Row stride of [rows, heads, hd] whose rows are contiguous inside."""
-    if t.dim() != 3 or (t.numel() and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]))):
-        raise ValueError(f"{name}: [rows, heads, head_dim] with contiguous rows expected, got shape {tuple(t.shape)}, strides {t.stride()}")
-    if like is not None and (t.dtype != like.dtype or t.shape[2] != like.shape[2]):
+    shape = tuple(t.shape)                          # (read once: each attribute of a tensor costs about 0.1 us)
+    if len(shape) != 3:
+        raise ValueError(f"{name}: [rows, heads, head_dim] expected, got shape {shape}")
+    rows, heads, hd = shape
+    if like is not None and (t.dtype != like.dtype or hd != like.shape[2]):
         raise ValueError(f"{name}: type or head_dim differ from the queries'")
-    return max(t.stride(0), t.shape[1] * t.shape[2]) if t.shape[0] <= 1 else t.stride(0)
+    if t.is_contiguous():
+        return heads * hd
+    row, head, channel = t.stride()
+    if channel != 1 or (heads > 1 and head != hd):
+        raise ValueError(f"{name}: [rows, heads, head_dim] with contiguous rows expected, got shape {shape}, strides {t.stride()}")
+    return max(row, heads * hd) if rows <= 1 else row
 
 
 def _contiguous(name: str, t: torch.Tensor, dtype: torch.dtype, numel: int):
@@ -351,8 +358,8 @@ def wq_rope_frequencies(rot_dim: int, base: float, scaling: int = ROPE_PLAIN, fa
 def wq_rope(ctx: Context, q, k, positions, inv_freq, layout: int = ROPE_HALF, mscale: float = 1.0, q_out: Optional[torch.Tensor] = None,
             k_out: Optional[torch.Tensor] = None):
     """Turns q [rows, Hq, hd] and k [rows, Hkv, hd] (or None); 2 * inv_freq.numel() channels of every head."""
-    rows, Hq, hd = q.shape
     qs = _rows("q", q)
+    rows, Hq, hd = q.shape
     _contiguous("positions", positions, torch.int32, rows)
     _contiguous("inv_freq", inv_freq, torch.float32, inv_freq.numel())
     if q_out is None:
@@ -398,10 +405,10 @@ def prefill_workspace_bytes(total_q: int, B: int, Hq: int, Hkv: int, hd: int, ma
 def wq_prefill_attention(ctx: Context, q, k, v, q_off, kv_off, sm_scale: float, prefix_len: Optional[torch.Tensor] = None, max_kv_rows: int = 0,
                          num_splits: int = 0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None):
     """q [total_q, Hq, hd] over k, v [total_kv, Hkv, hd]; q_off, kv_off [B+1], prefix_len [B] int32."""
+    qs, ks, vs = _rows("q", q), _rows("k", k, q), _rows("v", v, q)
     total_q, Hq, hd = q.shape
     total_kv, Hkv, _ = k.shape
     B = q_off.numel() - 1
-    qs, ks, vs = _rows("q", q), _rows("k", k, q), _rows("v", v, q)
     if v.shape != k.shape:
         raise ValueError("v: the shape of k expected")
     _contiguous("q_off", q_off, torch.int32, B + 1)
