@@ -497,7 +497,7 @@ int wq_prefill_attention(wq_ctx* ctx, const void* q, int64_t q_stride, const voi
     if (Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || Hq / Hkv > WQ_MAX_REP)
         return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "Hq=%d must be a multiple of Hkv=%d, at most %d query heads per KV head", Hq, Hkv, WQ_MAX_REP);
     const int rep = Hq / Hkv;
-    if (total_q > INT32_MAX / rep || total_kv > INT32_MAX || B > INT32_MAX / 2 || (total_q / 64 * rep + B + 1) > INT32_MAX / Hkv)
+    if (total_q > INT32_MAX / rep || total_kv > INT32_MAX || B > INT32_MAX / 2 || (total_q * rep / 16 + B + 1) > INT32_MAX / Hkv)
         return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "too many rows");
     if (num_splits < 0 || num_splits > WQ_MAX_ATTEND_SPLITS) return wq_fail(ctx, WQ_ERR_ARG, "num_splits out of range");
     if (!(sm_scale > 0.0f) || sm_scale > 3.0e38f) return wq_fail(ctx, WQ_ERR_ARG, "sm_scale must be positive and finite");

@@ -1079,25 +1079,15 @@ __global__ __launch_bounds__(256) void k_merge(MergeArgs a)
     store_merged<HD>(a.out, a.dtype, row, x, M, wave_sum(l * w));
 }
 
-// ---- wq_decode_attention_shared: the requests' own 16-bit rows, and the merge ------------------------------------------------
-struct FinishArgs {
-    const char* q;
-    const int32_t* req_off;
-    int P, Hq, rep, parts, dtype;
-    float scale;
-    const char *k, *v;         // own 16-bit rows [row][Hkv][hd], or NULL
-    const int32_t *off16, *len16;
-    int64_t cap16;
-    const float* own_out;      // or: one more part, normalised [B * Hq][hd], with its log-sum-exp
-    const float* own_lse;
-    Out out;
-};
+// ---- few query rows: a wavefront's share of the keys ---------------------------------------------------------------------------
+// Where all of a sequence's query rows fit the 16 columns of one product, keys are what is shared out: wavefront w of FEW takes 32 of them,
+// FEW chunks on the next.  Its keys come straight into the operands' registers (nothing else reads them), its values row by row into its own
+// piece of LDS (`tile`), as in Direct; nothing waits for another wavefront until join() brings their numerators together.
+constexpr int FEW = 8;
 
-// A wavefront's numerators, reference and sum over its share of a request's own rows: 32 keys of every 256.  Keys come straight into the
-// operands' registers (nothing else reads them), values row by row into this wavefront's own piece of LDS (`tile`), as in Direct.
 template <typename QT, int HD>
-__device__ __forceinline__ void own_rows(const FinishArgs& a, const char* q_row, const char* k, const char* v, int64_t stride, int len, Lds tile, f4 (&o)[HD / 16],
-                                         float& ref, float& sum)
+__device__ __forceinline__ void walk_few(const char* q_row, float scale, int limit, const char* k, const char* v, int64_t k_stride, int64_t v_stride, int n, int lo,
+                                         int hi, Lds tile, f4 (&o)[HD / 16], float& ref, float& sum)
 {
     constexpr int ST = STEPS<QT, HD>, CT16 = HD / 16, PIECES = HD / 8, PER_LOAD = 64 / PIECES, LOADS = 32 / PER_LOAD;
     using D = Direct<HD>;
@@ -1107,19 +1097,20 @@ __device__ __forceinline__ void own_rows(const FinishArgs& a, const char* q_row,
     ref = -INFINITY, sum = 0.f;
 #pragma unroll
     for (int ct = 0; ct < CT16; ct++) o[ct] = f4{0.f, 0.f, 0.f, 0.f};
-    for (int key0 = 32 * this_wave(); key0 < len; key0 += 256) {
-        const int left = len - key0;                           // (the last row is read again for the rest: its weights are zero)
+    const D rows(v_stride, v_stride);
+    for (int t32 = lo + this_wave(); t32 < hi; t32 += FEW) {
+        const int key0 = 32 * t32, left = n - key0;                         // (the last row is read again for the rest: its weights are zero)
 #pragma unroll
         for (int i = 0; i < LOADS; i++) {
             const int r = i * PER_LOAD + lane / PIECES, piece = (lane % PIECES) ^ (D::swizzle(r) * 2 & (PIECES - 1));
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(v + (key0 + (r < left ? r : left - 1)) * stride + 16 * piece),
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(v + (key0 + (r < left ? r : left - 1)) * v_stride + 16 * piece),
                                              (__attribute__((address_space(3))) void*)(tile + i * 1024), 16, 0, 0);
         }
         f4 s[2];
 #pragma unroll
         for (int t = 0; t < 2; t++) {
             const int r = 16 * t + m;
-            const char* row = k + (key0 + (r < left ? r : left - 1)) * stride;
+            const char* row = k + (key0 + (r < left ? r : left - 1)) * k_stride;
             s[t] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int st = 0; st < ST; st++) {
@@ -1136,16 +1127,16 @@ __device__ __forceinline__ void own_rows(const FinishArgs& a, const char* q_row,
         for (int t = 0; t < 2; t++)
 #pragma unroll
             for (int i = 0; i < 4; i++) {
-                s[t][i] = 16 * t + 4 * j + i < left ? s[t][i] * a.scale : -INFINITY;
+                s[t][i] = key0 + 16 * t + 4 * j + i < limit ? s[t][i] * scale : -INFINITY;
                 most = fmaxf(most, s[t][i]);
             }
-        const float next = fmaxf(ref, max_of_column(most));    // (finite: a wavefront's first key is there)
-        const float by = __builtin_amdgcn_exp2f(ref - next);
+        const float next = fmaxf(ref, max_of_column(most)), base = next == -INFINITY ? 0.f : next;
+        const float by = __builtin_amdgcn_exp2f(ref - base);
         ref = next, sum *= by;
         float w[8];
 #pragma unroll
         for (int e = 0; e < 8; e++) {
-            w[e] = __builtin_amdgcn_exp2f(s[e >> 2][e & 3] - ref + SHIFT);
+            w[e] = __builtin_amdgcn_exp2f(s[e >> 2][e & 3] - base + SHIFT);
             sum += w[e];
         }
         __builtin_amdgcn_s_waitcnt(0x0F70);                    // vmcnt(0): the values are in LDS
@@ -1170,7 +1161,6 @@ __device__ __forceinline__ void own_rows(const FinishArgs& a, const char* q_row,
             u4 p;
 #pragma unroll
             for (int e = 0; e < 4; e++) p[e] = pack2(w[2 * e], w[2 * e + 1], QT());
-            const D rows(stride, stride);
 #pragma unroll
             for (int ct = 0; ct < CT16; ct++) o[ct] = product<QT>(rows.values(tile, 0, ct), p, o[ct] * by);
         }
@@ -1181,15 +1171,103 @@ __device__ __forceinline__ void own_rows(const FinishArgs& a, const char* q_row,
     ref -= SHIFT;
 }
 
+// Wavefronts' numerators [row][hd] in their pieces of LDS, references and sums beside them
+template <int HD>
+struct Few {
+    __align__(16) char v[FEW][32 * HD * 2];
+    float m[FEW][16], l[FEW][16];
+};
+template <int HD>
+__device__ __forceinline__ void leave_few(Few<HD>& s, const f4 (&o)[HD / 16], float ref, float sum)
+{
+    const int lane = threadIdx.x & 63, n = lane & 15, wave = this_wave();
+#pragma unroll
+    for (int ct = 0; ct < HD / 16; ct++) *reinterpret_cast<f4*>(s.v[wave] + (n * HD + 16 * ct + 4 * (lane >> 4)) * 4) = o[ct];
+    if (lane < 16) s.m[wave][n] = ref, s.l[wave][n] = sum;
+}
+// Row r's numerators, those of wavefront f by weight w (lane f); lanes' channels and groups as in sum_of_parts
+template <int HD>
+__device__ __forceinline__ f4 join_few(const Few<HD>& s, int r, float w)
+{
+    constexpr int LANES = HD / 4, GROUPS = 64 / LANES;
+    const int lane = threadIdx.x & 63;
+    f4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < FEW; k += GROUPS) {
+        const int from = k + lane / LANES;
+        const float by = __shfl(w, from, 64);
+        x += *reinterpret_cast<const f4*>(s.v[from] + (r * HD + 4 * (lane % LANES)) * 4) * by;
+    }
+    return x;
+}
+
+// wq_prefill_attention over few query rows: a workgroup per 16 of them and part of the keys
+template <typename CT, int HD>
+__global__ __launch_bounds__(64 * FEW, 4) void k_prefill_few(PrefillArgs a, int dtype)
+{
+    __shared__ Few<HD> s;
+    const int Hkv = a.Hq / a.rep, kvh = blockIdx.x % Hkv, split = blockIdx.y, wave = this_wave(), lane = threadIdx.x & 63;
+    Place p;
+    if (!find_place<16>(a.q_off, a.B, a.rep, a.total_q, blockIdx.x / Hkv, p)) return;
+    const int64_t kv0 = clipped(a.kv_off[p.seq], a.total_kv), kv1 = clipped(a.kv_off[p.seq + 1], a.total_kv);
+    const int len = kv1 > kv0 ? (int)(kv1 - kv0) : 0, first = len - p.rows / a.rep;
+    int prefix = a.prefix_len ? a.prefix_len[p.seq] : 0;
+    prefix = prefix < 0 ? 0 : (prefix > len ? len : prefix);
+    auto limit_of = [&](int row) {
+        const int seen = first + row / a.rep + 1;
+        return seen > prefix ? seen : prefix;
+    };
+    const int rows = p.rows - p.row0 < 16 ? p.rows - p.row0 : 16;
+    const int most = limit_of(p.row0 + rows - 1), chunks = most > 0 ? (most + 31) / 32 : 0;
+    const int lo = (int)((int64_t)split * chunks / a.splits), hi = (int)((int64_t)(split + 1) * chunks / a.splits);
+    {
+        const int row = p.row0 + (lane & 15);
+        const bool there = row < p.rows;
+        f4 o[HD / 16];
+        float ref, sum;
+        walk_few<CT, HD>(there ? a.q + (p.first + row / a.rep) * a.q_stride + (kvh * a.rep + row % a.rep) * (HD * ESIZE<CT>) : nullptr, a.scale,
+                         there ? limit_of(row) : 0, a.k + kv0 * a.k_stride + kvh * (HD * ESIZE<CT>), a.v + kv0 * a.v_stride + kvh * (HD * ESIZE<CT>), a.k_stride,
+                         a.v_stride, len, lo, hi, (Lds)s.v[wave], o, ref, sum);
+        leave_few<HD>(s, o, ref, sum);
+    }
+    __syncthreads();
+    for (int r = wave; r < rows; r += FEW) {
+        const float m = lane < FEW ? s.m[lane][r] : -INFINITY, l = lane < FEW ? s.l[lane][r] : 0.f;
+        const float M = wave_max(m), w = __builtin_amdgcn_exp2f(m - (M == -INFINITY ? 0.f : M));
+        const f4 x = sum_of_groups<HD>(join_few<HD>(s, r, w));
+        const float L = wave_sum(l * w);
+        const int row = p.row0 + r;
+        const int64_t at = (p.first + row / a.rep) * a.Hq + kvh * a.rep + row % a.rep;
+        if (a.splits == 1) {
+            store_merged<HD>(a.out, dtype, at, x, M, L);
+        } else {
+            if (lane < HD / 4) reinterpret_cast<f4*>(a.out.part)[(at * a.splits + split) * (HD / 4) + lane] = x;
+            if (lane == 0) a.out.part_ml[(at * a.splits + split) * 2] = M, a.out.part_ml[(at * a.splits + split) * 2 + 1] = L;
+        }
+    }
+}
+
+// ---- wq_decode_attention_shared: the requests' own 16-bit rows, and the merge ------------------------------------------------
+struct FinishArgs {
+    const char* q;
+    const int32_t* req_off;
+    int P, Hq, rep, parts, dtype;
+    float scale;
+    const char *k, *v;         // own 16-bit rows [row][Hkv][hd], or NULL
+    const int32_t *off16, *len16;
+    int64_t cap16;
+    const float* own_out;      // or: one more part, normalised [B * Hq][hd], with its log-sum-exp
+    const float* own_lse;
+    Out out;
+};
+
 // A workgroup per (request, KV head): eight wavefronts walk the request's own rows, while wavefront 8 + r merges query head r's parts;
 // then each of those takes in what the eight have found.
 template <typename QT, int HD>
 __global__ __launch_bounds__(1024) void k_shared_finish(FinishArgs a)
 {
-    constexpr int W = 8, LANES = HD / 4, GROUPS = 64 / LANES;
-    __shared__ __align__(16) char s_v[W][32 * HD * 2];         // values; then the wavefronts' numerators, [head][hd] fp32
-    __shared__ float s_m[W][WQ_MAX_REP], s_l[W][WQ_MAX_REP];
-    static_assert(WQ_MAX_REP * HD * 4 <= 32 * HD * 2 && WQ_MAX_REP == W, "");
+    constexpr int W = FEW, LANES = HD / 4;
+    __shared__ Few<HD> s;
     const int Hkv = a.Hq / a.rep, b = blockIdx.x / Hkv, kvh = blockIdx.x % Hkv, wave = this_wave(), lane = threadIdx.x & 63;
     const int64_t row0 = (int64_t)b * a.Hq + kvh * a.rep;
     int len = 0;
@@ -1208,12 +1286,9 @@ __global__ __launch_bounds__(1024) void k_shared_finish(FinishArgs a)
             f4 o[HD / 16];
             float ref, sum;
             const int n = lane & 15;
-            own_rows<QT, HD>(a, n < a.rep ? a.q + (row0 + n) * (HD * ESIZE<QT>) : nullptr, a.k + first, a.v + first, stride, len, (Lds)s_v[wave], o, ref, sum);
-            if (n < a.rep) {
-#pragma unroll
-                for (int ct = 0; ct < HD / 16; ct++) *reinterpret_cast<f4*>(s_v[wave] + (n * HD + 16 * ct + 4 * (lane >> 4)) * 4) = o[ct];
-                if (lane < 16) s_m[wave][n] = ref, s_l[wave][n] = sum;
-            }
+            walk_few<QT, HD>(n < a.rep ? a.q + (row0 + n) * (HD * ESIZE<QT>) : nullptr, a.scale, len, a.k + first, a.v + first, stride, stride, len, 0,
+                             (len + 31) / 32, (Lds)s.v[wave], o, ref, sum);
+            leave_few<HD>(s, o, ref, sum);
         }
     } else {
         const int parts = b >= a.req_off[0] && b < a.req_off[a.P] ? a.parts : 0;
@@ -1230,17 +1305,10 @@ __global__ __launch_bounds__(1024) void k_shared_finish(FinishArgs a)
     }
     __syncthreads();
     if (wave < W) return;
-    if (len > 0 && lane < W) m2 = s_m[lane][r], l2 = s_l[lane][r];
+    if (len > 0 && lane < W) m2 = s.m[lane][r], l2 = s.l[lane][r];
     const float M = wave_max(m2), w2 = __builtin_amdgcn_exp2f(m2 - (M == -INFINITY ? 0.f : M));
     x *= __shfl(w2, W + 1, 64);
-    if (len > 0) {
-#pragma unroll
-        for (int k = 0; k < W; k += GROUPS) {
-            const int from = k + lane / LANES;
-            const float by = __shfl(w2, from, 64);
-            if (32 * from < len) x += *reinterpret_cast<const f4*>(s_v[from] + (r * HD + 4 * (lane % LANES)) * 4) * by;
-        }
-    }
+    if (len > 0) x += join_few<HD>(s, r, w2);
     x = sum_of_groups<HD>(x);
     if (a.own_out) x += reinterpret_cast<const f4*>(a.own_out)[row * LANES + lane % LANES] * __shfl(w2, W, 64);
     store_merged<HD>(a.out, a.dtype, row, x, M, wave_sum(l2 * w2));
@@ -1260,8 +1328,11 @@ int auto_splits_of(int64_t workgroups, int64_t max_keys, int want, int keys)
 
 size_t partials_bytes(int64_t rows, int hd, int parts) { return wq_align256((size_t)rows * parts * (hd + 2) * sizeof(float)); }
 
-// Query rows of a workgroup
+// Query rows of a workgroup of the prompt's and the shared kernels: 256, or 128 where that is all there are (two groups of wavefronts, half the
+// keys each)
 int rows_of(int64_t q_rows, int rep, int dtype) { return dtype != WQ_F32 && q_rows * rep > 128 ? 256 : 128; }
+// Prompt attention over so few that k_prefill_few takes them (on the average: any number is right)
+bool few_rows(int64_t total_q, int B, int rep, int dtype) { return dtype != WQ_F32 && total_q * rep <= (int64_t)B * 16; }
 
 template <typename CT>
 auto prefill_kernel(int hd, bool split) -> void (*)(PrefillArgs)
@@ -1289,7 +1360,9 @@ constexpr int64_t OWN_INSIDE = 2048;
 int wq_prefill_splits(int64_t total_q, int B, int Hq, int Hkv, int dtype, int64_t max_kv_rows)
 {
     const int rep = Hq / Hkv, rows = rows_of((total_q + B - 1) / B, rep, dtype);
-    return auto_splits_of(tiles_of(total_q, rep, 0, rows) * Hkv + (int64_t)Hkv * (total_q < B ? total_q : B), max_kv_rows, 256, 64);
+    const int64_t used = total_q < B ? total_q : B;           // sequences that have rows
+    if (few_rows(total_q, B, rep, dtype)) return auto_splits_of((tiles_of(total_q, rep, 0, 16) + used) * Hkv, max_kv_rows, 512, 32 * FEW);
+    return auto_splits_of((tiles_of(total_q, rep, 0, rows) + used) * Hkv, max_kv_rows, 256, dtype == WQ_F32 ? 32 : 64);
 }
 size_t wq_prefill_ws_bytes(int64_t total_q, int Hq, int hd, int splits)
 {
@@ -1324,11 +1397,18 @@ int wq_launch_prefill(wq_ctx* ctx, const WqPrefill& f)
     a.out.out = f.out, a.out.lse = f.lse;
     a.out.part = reinterpret_cast<float*>(ctx->ws + WQ_WS_HEADER);
     a.out.part_ml = a.out.part + f.total_q * f.Hq * f.splits * f.hd;
-    const int rows = rows_of((f.total_q + f.B - 1) / f.B, a.rep, f.dtype);
+    const bool few = few_rows(f.total_q, f.B, a.rep, f.dtype);
+    const int rows = few ? 16 : rows_of((f.total_q + f.B - 1) / f.B, a.rep, f.dtype);
     const dim3 grid((unsigned)(f.Hkv * tiles_of(f.total_q, a.rep, f.B, rows)), (unsigned)f.splits);
-    void (*const kernel)(PrefillArgs) = f.dtype == WQ_F32 ? prefill_kernel<F32>(f.hd, false) : f.dtype == WQ_BF16 ? prefill_kernel<Bf16>(f.hd, rows == 128)
-                                                                                                          : prefill_kernel<F16>(f.hd, rows == 128);
-    hipLaunchKernelGGL(kernel, grid, dim3(f.dtype == WQ_F32 ? 256 : 512), 0, ctx->stream, a);
+    if (few) {
+        void (*const kernel)(PrefillArgs, int) = f.dtype == WQ_BF16 ? (f.hd == 128 ? k_prefill_few<Bf16, 128> : k_prefill_few<Bf16, 64>)
+                                                                    : (f.hd == 128 ? k_prefill_few<F16, 128> : k_prefill_few<F16, 64>);
+        hipLaunchKernelGGL(kernel, grid, dim3(64 * FEW), 0, ctx->stream, a, f.dtype);
+    } else {
+        void (*const kernel)(PrefillArgs) = f.dtype == WQ_F32 ? prefill_kernel<F32>(f.hd, false) : f.dtype == WQ_BF16 ? prefill_kernel<Bf16>(f.hd, rows == 128)
+                                                                                                              : prefill_kernel<F16>(f.hd, rows == 128);
+        hipLaunchKernelGGL(kernel, grid, dim3(f.dtype == WQ_F32 ? 256 : 512), 0, ctx->stream, a);
+    }
     if (f.splits > 1) {
         const MergeArgs m = {f.total_q * f.Hq, f.Hq, f.splits, f.dtype, f.q_off, f.B, a.out};
         hipLaunchKernelGGL(f.hd == 128 ? k_merge<128> : k_merge<64>, dim3((unsigned)((m.rows + 3) / 4)), dim3(256), 0, ctx->stream, m);

@@ -39,6 +39,8 @@ def _check(new, rows, prefix, Hq, Hkv, hd, dtype, splits, seed=1, spread=1.0):
     assert bool((out[q_off[-1]:] == 7.0).all()) and bool((lse[q_off[-1]:] == 7.0).all()), "rows behind the last sequence"
     u = R.HALF_STEP[dtype]
     for b, n in enumerate(new):
+        if n == 0:
+            continue
         L = rows[b]
         p = 0 if prefix is None else min(max(prefix[b], 0), L)
         limit = [max(L - n + i + 1, p) for i in range(n)]
@@ -75,6 +77,15 @@ def test_ragged_batches(dtype, heads):
 def test_chunks_and_single_tokens(dtype, splits):
     _check([1, 1, 1, 1], [1, 130, 777, 64], None, *SMALL, dtype, splits)
     _check([5, 61, 1], [700, 1000, 333], [0, 990, 100], *LARGE, dtype, splits)
+
+
+@pytest.mark.parametrize("dtype", DTYPES[:2])
+@pytest.mark.parametrize("heads", [SMALL, LARGE, (16, 2, 128), (3, 3, 64)])
+@pytest.mark.parametrize("splits", [0, 1, 5, 64])
+def test_few_rows_each(dtype, heads, splits):
+    """At most 16 products' columns a sequence on the average; some have more, none, or fewer keys than queries."""
+    _check([1, 1, 0, 8, 1, 1], [31, 33, 40, 600, 2100, 1], None, *heads, dtype, splits, seed=3)
+    _check([1, 4, 1, 1, 0, 2], [256, 2, 0, 257, 0, 512], [0, 2, 0, 256, 0, 511], *heads, dtype, splits, seed=4)
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
