@@ -260,6 +260,14 @@ __device__ __forceinline__ void attend_f32(Rows<HD>& r, const Query<F32, HD>& q,
 //   phase 2i + 1  group 0: weights of tile i       group 1: products of tile i       (the keys of tile i + 1 are brought by group 0)
 // A tile's keys and values are read in two neighbouring phases, so two tiles of each in LDS are enough.
 // With up to 128 rows only group 0 has any, and group 1 brings it keys and values (SPLIT).
+// A barrier for what is in LDS: loads into registers stay in flight across it (__syncthreads() waits for them)
+__device__ __forceinline__ void meet()
+{
+    __builtin_amdgcn_s_waitcnt(0xC07F);                        // lgkmcnt(0)
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
 __device__ __forceinline__ int group_of_wave() { return this_wave() >> 2; }
 
 // Tiles t0 .. t1-1.  bring_keys(t), bring_values(t): of the group that does so, into LDS; settle(): a phase's end.  The products of the first tile meet
@@ -677,7 +685,7 @@ __device__ __forceinline__ void walk_packed(Rows<HD>& r, const Query<F16, HD>& q
     __syncthreads();
     take_turns<F16, HD, SPLIT, Order>(
         r, q, t0, t1, len, [&](int t, int kt, int st) { return k_of(t)[(kt * STEPS<F16, HD> + st) * 64 + lane]; },
-        [&](int t, int vs, int ct) { return v_of(t)[(vs * (HD / 16) + ct) * 64 + lane]; }, bring_keys, bring_values, [] { __syncthreads(); });
+        [&](int t, int vs, int ct) { return v_of(t)[(vs * (HD / 16) + ct) * 64 + lane]; }, bring_keys, bring_values, meet);
 }
 
 // ---- what both kernels share -------------------------------------------------------------------------------------------
