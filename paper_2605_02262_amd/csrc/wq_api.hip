@@ -481,9 +481,9 @@ int wq_rope_frequencies(int rot_dim, double base, int scaling, double factor, in
 size_t wq_prefill_workspace_bytes(int64_t total_q, int B, int Hq, int Hkv, int hd, int64_t max_kv_rows, int num_splits)
 {
     if (total_q <= 0 || B <= 0 || Hq <= 0 || Hkv <= 0 || hd <= 0 || Hq % Hkv != 0) return WQ_WS_HEADER;
-    if (num_splits > 0) return WQ_WS_HEADER + wq_prefill_ws_bytes(total_q, Hq, hd, num_splits);
-    const int a = wq_prefill_splits(total_q, B, Hq, Hkv, WQ_F32, max_kv_rows), b = wq_prefill_splits(total_q, B, Hq, Hkv, WQ_BF16, max_kv_rows);
-    return WQ_WS_HEADER + wq_prefill_ws_bytes(total_q, Hq, hd, a > b ? a : b);
+    const size_t a = wq_prefill_plan(total_q, B, Hq, Hkv, hd, WQ_F32, max_kv_rows, true, num_splits).bytes;
+    const size_t b = wq_prefill_plan(total_q, B, Hq, Hkv, hd, WQ_BF16, max_kv_rows, true, num_splits).bytes;
+    return WQ_WS_HEADER + (a > b ? a : b);
 }
 
 int wq_prefill_attention(wq_ctx* ctx, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int dtype,
@@ -510,10 +510,10 @@ int wq_prefill_attention(wq_ctx* ctx, const void* q, int64_t q_stride, const voi
     if (rc != WQ_OK) return rc;
     if (total_kv > 0 && (k_stride > 1 << 22 || v_stride > 1 << 22))       // (offsets inside a tile have 32 bits)
         return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "rows of k or v are more than 2^22 elements apart");
-    const int splits = num_splits > 0 ? num_splits : wq_prefill_splits(total_q, B, Hq, Hkv, dtype, max_kv_rows);
-    if (ctx->ws_bytes < WQ_WS_HEADER + wq_prefill_ws_bytes(total_q, Hq, hd, splits) || !ctx->ws)
-        return wq_fail(ctx, WQ_ERR_WORKSPACE, "workspace too small for %d splits of %lld rows", splits, (long long)total_q);
-    return wq_launch_prefill(ctx, {q, k, v, q_stride, k_stride, v_stride, dtype, B, Hq, Hkv, hd, splits, q_off, kv_off, prefix_len, total_q, total_kv, sm_scale,
+    const WqPrefillPlan plan = wq_prefill_plan(total_q, B, Hq, Hkv, hd, dtype, max_kv_rows, prefix_len != nullptr, num_splits);
+    if (ctx->ws_bytes < WQ_WS_HEADER + plan.bytes || !ctx->ws)
+        return wq_fail(ctx, WQ_ERR_WORKSPACE, "workspace too small for %d splits of %lld rows", plan.tail > 0 ? plan.tail_splits : plan.splits, (long long)total_q);
+    return wq_launch_prefill(ctx, {q, k, v, q_stride, k_stride, v_stride, dtype, B, Hq, Hkv, hd, plan, q_off, kv_off, prefix_len, total_q, total_kv, sm_scale,
                                    out, lse});
 }
 

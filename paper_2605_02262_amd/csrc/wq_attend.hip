@@ -305,12 +305,10 @@ __device__ __forceinline__ void take_turns(Rows<HD>& r, const Query<CT, HD>& q, 
         multiply_keys<CT, HD>(s, q, [&](int kt, int st) { return keys(t, kt, st); });
         multiply_values<CT, HD>(r, p, [&](int vs, int ct) { return values(t - 1, vs, ct); });
         __builtin_amdgcn_s_setprio(0);
+        if (!SPLIT && group == 0 && t + 1 < t1) bring_keys(t + 1);
         settle();
         form_weights<CT, HD, Order>(r, s, p, t * KEYS<CT>, (t + 1) * KEYS<CT> > least);
-        if (!SPLIT && t + 1 < t1) {
-            if (group == 0) bring_keys(t + 1);
-            else bring_values(t + 1);
-        }
+        if (!SPLIT && group == 1 && t + 1 < t1) bring_values(t + 1);
         settle();
     }
     if (SPLIT || group == 0) settle();
@@ -778,9 +776,11 @@ __device__ __forceinline__ float query_as_f16(Query<F16, HD>& q, int n)
     return 1.0f / down;
 }
 
-// As one of several parts for the merge, or as the result (parts == 0).
+// As one of several parts for the merge, or as the result (parts == 0).  Parts are numbered by the result's rows, or (tile_rows >= 0) by the
+// tile's from there on.
 template <typename CT, int HD>
-__device__ __forceinline__ void store_rows(const Rows<HD>& r, const Place& p, int rep, int Hq, int kvh, int wave, int part, int parts, const Out& out)
+__device__ __forceinline__ void store_rows(const Rows<HD>& r, const Place& p, int rep, int Hq, int kvh, int wave, int part, int parts, const Out& out,
+                                           int64_t tile_rows = -1)
 {
     const int lane = threadIdx.x & 63, group = lane >> 4;
 #pragma unroll
@@ -791,12 +791,13 @@ __device__ __forceinline__ void store_rows(const Rows<HD>& r, const Place& p, in
         const int64_t at = (p.first + row / rep) * Hq + kvh * rep + row % rep;
         const float ref = r.ref[n] - SHIFT;
         if (parts > 0) {
-            float* to = out.part + (at * parts + part) * HD;
+            const int64_t slot = (tile_rows < 0 ? at : tile_rows + row - p.row0) * parts + part;
+            float* to = out.part + slot * HD;
 #pragma unroll
             for (int ct = 0; ct < HD / 16; ct++) *reinterpret_cast<f4*>(to + 16 * ct + 4 * group) = r.o[ct][n];
             if (group == 0) {
-                out.part_ml[(at * parts + part) * 2] = ref;
-                out.part_ml[(at * parts + part) * 2 + 1] = sum;
+                out.part_ml[slot * 2] = ref;
+                out.part_ml[slot * 2 + 1] = sum;
             }
             continue;
         }
@@ -821,6 +822,7 @@ struct PrefillArgs {
     const int32_t *q_off, *kv_off, *prefix_len;
     int64_t total_q, total_kv;
     int B, Hq, rep, splits;
+    int units, tail, tail_splits;              // KV heads * tiles; the last so many of them in the order of the launch are cut into so many parts
     float scale;                               // log2(e) * sm_scale
     Out out;
 };
@@ -832,10 +834,12 @@ __global__ __launch_bounds__(64 * WAVES<CT>, 2) void k_prefill(PrefillArgs a)
 {
     constexpr int BYTES = TILE_BYTES<CT, HD> * (ESIZE<CT> == 2 ? 2 : 1), R = ROWS<CT, SPLIT>;
     __shared__ __align__(16) char s_k[BYTES], s_v[BYTES];
-    const int Hkv = a.Hq / a.rep, kvh = blockIdx.x % Hkv, split = blockIdx.y;
-    const int wave = this_wave(), lane = threadIdx.x & 63;
+    const int Hkv = a.Hq / a.rep, wave = this_wave(), lane = threadIdx.x & 63, in_tail = (int)blockIdx.x - (a.units - a.tail);
+    int unit = blockIdx.x, split = blockIdx.y, parts = a.splits;
+    if (in_tail >= 0 && a.tail > 0) unit = a.units - a.tail + in_tail / a.tail_splits, split = in_tail % a.tail_splits, parts = a.tail_splits;
+    const int kvh = unit % Hkv;
     Place p;
-    if (!find_place<R>(a.q_off, a.B, a.rep, a.total_q, (gridDim.x - 1 - blockIdx.x) / Hkv, p)) return;      // (the last rows see the most keys: they begin first)
+    if (!find_place<R>(a.q_off, a.B, a.rep, a.total_q, (a.units - 1 - unit) / Hkv, p)) return;      // (the last rows see the most keys: they begin first)
     const int64_t kv0 = clipped(a.kv_off[p.seq], a.total_kv), kv1 = clipped(a.kv_off[p.seq + 1], a.total_kv);
     const int len = kv1 > kv0 ? (int)(kv1 - kv0) : 0;
     const int first = len - p.rows / a.rep;                       // position of the sequence's first query row
@@ -848,7 +852,7 @@ __global__ __launch_bounds__(64 * WAVES<CT>, 2) void k_prefill(PrefillArgs a)
     };
     const int last_row = (p.row0 + R < p.rows ? p.row0 + R : p.rows) - 1;
     const int tiles = (limit_of(last_row) + KEYS<CT> - 1) / KEYS<CT>;
-    const int lo = (int)((int64_t)split * tiles / a.splits), hi = (int)((int64_t)(split + 1) * tiles / a.splits);
+    const int lo = (int)((int64_t)split * tiles / parts), hi = (int)((int64_t)(split + 1) * tiles / parts);
 
     Rows<HD> r;
     Query<CT, HD> q;
@@ -882,7 +886,7 @@ __global__ __launch_bounds__(64 * WAVES<CT>, 2) void k_prefill(PrefillArgs a)
             attend_f32<HD>(r, q, (Lds4)s_k, (Lds4)s_v, key0, least, most);
         }
     }
-    if (any) store_rows<CT, HD>(r, p, a.rep, a.Hq, kvh, wave, split, a.splits > 1 ? a.splits : 0, a.out);
+    if (any) store_rows<CT, HD>(r, p, a.rep, a.Hq, kvh, wave, split, parts > 1 ? parts : 0, a.out, a.tail > 0 ? (int64_t)(a.units - 1 - unit) * R : -1);
 }
 
 // ---- wq_decode_attention_shared ------------------------------------------------------------------------------------------
@@ -1085,6 +1089,22 @@ __global__ __launch_bounds__(256) void k_merge(MergeArgs a)
     const float M = wave_max(m), w = __builtin_amdgcn_exp2f(m - (M == -INFINITY ? 0.f : M));
     const f4 x = sum_of_groups<HD>(sum_of_parts<HD>(a.out.part + row * a.parts * HD, a.parts, w));
     store_merged<HD>(a.out, a.dtype, row, x, M, wave_sum(l * w));
+}
+
+// The tail's tiles: a wavefront per row, 64 workgroups per tile
+template <int HD>
+__global__ __launch_bounds__(256) void k_merge_tail(PrefillArgs a, int dtype)
+{
+    const int Hkv = a.Hq / a.rep, u = blockIdx.x >> 6, in_tile = (blockIdx.x & 63) * 4 + this_wave(), lane = threadIdx.x & 63, parts = a.tail_splits;
+    Place p;
+    if (!find_place<256>(a.q_off, a.B, a.rep, a.total_q, u / Hkv, p) || p.row0 + in_tile >= p.rows) return;
+    const int row = p.row0 + in_tile, kvh = (a.units - 1 - u) % Hkv;
+    const int64_t slot = ((int64_t)u * 256 + in_tile) * parts;
+    const float m = lane < parts ? a.out.part_ml[(slot + lane) * 2] : -INFINITY;
+    const float l = lane < parts ? a.out.part_ml[(slot + lane) * 2 + 1] : 0.f;
+    const float M = wave_max(m), w = __builtin_amdgcn_exp2f(m - (M == -INFINITY ? 0.f : M));
+    const f4 x = sum_of_groups<HD>(sum_of_parts<HD>(a.out.part + slot * HD, parts, w));
+    store_merged<HD>(a.out, dtype, (p.first + row / a.rep) * a.Hq + kvh * a.rep + row % a.rep, x, M, wave_sum(l * w));
 }
 
 // ---- few query rows: a wavefront's share of the keys ---------------------------------------------------------------------------
@@ -1362,19 +1382,33 @@ auto finish_kernel(int hd) -> void (*)(FinishArgs) { return hd == 128 ? k_shared
 
 // Longer own caches, and those with room for packed tokens, have a decode launch of their own
 constexpr int64_t OWN_INSIDE = 2048;
+// Below this many keys a tail's merge costs more than its parts save
+constexpr int64_t TAIL_KEYS = 2048;
 
 }  // namespace
 
-int wq_prefill_splits(int64_t total_q, int B, int Hq, int Hkv, int dtype, int64_t max_kv_rows)
+WqPrefillPlan wq_prefill_plan(int64_t total_q, int B, int Hq, int Hkv, int hd, int dtype, int64_t max_kv_rows, bool prefix, int num_splits)
 {
-    const int rep = Hq / Hkv, rows = rows_of((total_q + B - 1) / B, rep, dtype);
+    const int rep = Hq / Hkv;
     const int64_t used = total_q < B ? total_q : B;           // sequences that have rows
-    if (few_rows(total_q, B, rep, dtype)) return auto_splits_of((tiles_of(total_q, rep, 0, 16) + used) * Hkv, max_kv_rows, 512, 32 * FEW);
-    return auto_splits_of((tiles_of(total_q, rep, 0, rows) + used) * Hkv, max_kv_rows, 256, dtype == WQ_F32 ? 32 : 64);
-}
-size_t wq_prefill_ws_bytes(int64_t total_q, int Hq, int hd, int splits)
-{
-    return splits > 1 ? partials_bytes(total_q * Hq, hd, splits) : 0;
+    WqPrefillPlan s = {0, num_splits, 0, 0, 0};
+    s.few = few_rows(total_q, B, rep, dtype);
+    const int rows = s.few ? 16 : rows_of((total_q + B - 1) / B, rep, dtype);
+    s.rows = rows;
+    if (num_splits <= 0) {
+        s.splits = s.few ? auto_splits_of((tiles_of(total_q, rep, 0, rows) + used) * Hkv, max_kv_rows, 512, 32 * FEW)
+                         : auto_splits_of((tiles_of(total_q, rep, 0, rows) + used) * Hkv, max_kv_rows, 256, dtype == WQ_F32 ? 32 : 64);
+        // Tiles of equal length (a prefix) for more than the card's 256 compute units: the last round's, where they are no more than half of
+        // them, are cut along the keys to fill it.
+        const int64_t units = tiles_of(total_q, rep, B, rows) * Hkv, rest = units % 256;
+        if (rows == 256 && s.splits == 1 && prefix && units > 256 && rest > 0 && rest <= 128 && max_kv_rows >= TAIL_KEYS) {
+            s.tail = (int)rest;
+            s.tail_splits = (int)(256 / rest < max_kv_rows / 512 ? 256 / rest : max_kv_rows / 512);
+            if (s.tail_splits > WQ_MAX_ATTEND_SPLITS) s.tail_splits = WQ_MAX_ATTEND_SPLITS;
+        }
+    }
+    s.bytes = s.tail > 0 ? partials_bytes((int64_t)s.tail * 256, hd, s.tail_splits) : s.splits > 1 ? partials_bytes(total_q * Hq, hd, s.splits) : 0;
+    return s;
 }
 
 WqSharedPlan wq_shared_plan(int B, int P, int Hq, int Hkv, int hd, int q_dtype, int64_t max_prefix_tokens, int64_t max_own_tokens, bool own, bool own_packed,
@@ -1400,25 +1434,26 @@ int wq_launch_prefill(wq_ctx* ctx, const WqPrefill& f)
     a.q_stride = f.q_stride * size, a.k_stride = f.k_stride * size, a.v_stride = f.v_stride * size;
     a.q_off = f.q_off, a.kv_off = f.kv_off, a.prefix_len = f.prefix_len;
     a.total_q = f.total_q, a.total_kv = f.total_kv;
-    a.B = f.B, a.Hq = f.Hq, a.rep = f.Hq / f.Hkv, a.splits = f.splits;
+    a.B = f.B, a.Hq = f.Hq, a.rep = f.Hq / f.Hkv, a.splits = f.plan.splits;
     a.scale = f.sm_scale * LOG2E;
     a.out.out = f.out, a.out.lse = f.lse;
     a.out.part = reinterpret_cast<float*>(ctx->ws + WQ_WS_HEADER);
-    a.out.part_ml = a.out.part + f.total_q * f.Hq * f.splits * f.hd;
-    const bool few = few_rows(f.total_q, f.B, a.rep, f.dtype);
-    const int rows = few ? 16 : rows_of((f.total_q + f.B - 1) / f.B, a.rep, f.dtype);
-    const dim3 grid((unsigned)(f.Hkv * tiles_of(f.total_q, a.rep, f.B, rows)), (unsigned)f.splits);
-    if (few) {
+    a.units = (int)(f.Hkv * tiles_of(f.total_q, a.rep, f.B, f.plan.rows)), a.tail = f.plan.tail, a.tail_splits = f.plan.tail_splits;
+    a.out.part_ml = a.out.part + (a.tail > 0 ? (int64_t)a.tail * 256 * a.tail_splits : f.total_q * f.Hq * a.splits) * f.hd;
+    const dim3 grid((unsigned)(a.units - a.tail + a.tail * a.tail_splits), (unsigned)a.splits);
+    if (f.plan.few) {
         void (*const kernel)(PrefillArgs, int) = f.dtype == WQ_BF16 ? (f.hd == 128 ? k_prefill_few<Bf16, 128> : k_prefill_few<Bf16, 64>)
                                                                     : (f.hd == 128 ? k_prefill_few<F16, 128> : k_prefill_few<F16, 64>);
         hipLaunchKernelGGL(kernel, grid, dim3(64 * FEW), 0, ctx->stream, a, f.dtype);
     } else {
-        void (*const kernel)(PrefillArgs) = f.dtype == WQ_F32 ? prefill_kernel<F32>(f.hd, false) : f.dtype == WQ_BF16 ? prefill_kernel<Bf16>(f.hd, rows == 128)
-                                                                                                              : prefill_kernel<F16>(f.hd, rows == 128);
+        void (*const kernel)(PrefillArgs) = f.dtype == WQ_F32 ? prefill_kernel<F32>(f.hd, false) : f.dtype == WQ_BF16 ? prefill_kernel<Bf16>(f.hd, f.plan.rows == 128)
+                                                                                                              : prefill_kernel<F16>(f.hd, f.plan.rows == 128);
         hipLaunchKernelGGL(kernel, grid, dim3(f.dtype == WQ_F32 ? 256 : 512), 0, ctx->stream, a);
     }
-    if (f.splits > 1) {
-        const MergeArgs m = {f.total_q * f.Hq, f.Hq, f.splits, f.dtype, f.q_off, f.B, a.out};
+    if (a.tail > 0) {
+        hipLaunchKernelGGL(f.hd == 128 ? k_merge_tail<128> : k_merge_tail<64>, dim3((unsigned)a.tail * 64), dim3(256), 0, ctx->stream, a, f.dtype);
+    } else if (a.splits > 1) {
+        const MergeArgs m = {f.total_q * f.Hq, f.Hq, a.splits, f.dtype, f.q_off, f.B, a.out};
         hipLaunchKernelGGL(f.hd == 128 ? k_merge<128> : k_merge<64>, dim3((unsigned)((m.rows + 3) / 4)), dim3(256), 0, ctx->stream, m);
     }
     WQ_HIP_CHECK(ctx, hipGetLastError());

@@ -184,18 +184,24 @@ int wq_launch_rope(wq_ctx* ctx, const WqRope& r);
 int wq_launch_rope_append(wq_ctx* ctx, const WqRope& r, const void* v, int64_t v_stride, const wq_packed_kv* kv);
 
 constexpr int WQ_MAX_ATTEND_SPLITS = 64;
+struct WqPrefillPlan {
+    int rows, splits;                                             // query rows of a workgroup; parts of every row's keys
+    int tail, tail_splits;                                        // with one part: so many workgroups, the last ones, are cut into so many
+    size_t bytes;                                                 // workspace
+    bool few;
+};
 struct WqPrefill {
     const void *q, *k, *v;
     int64_t q_stride, k_stride, v_stride;                         // elements from row to row
-    int dtype, B, Hq, Hkv, hd, splits;
+    int dtype, B, Hq, Hkv, hd;
+    WqPrefillPlan plan;
     const int32_t *q_off, *kv_off, *prefix_len;
     int64_t total_q, total_kv;
     float sm_scale;
     void* out;
     float* lse;
 };
-int wq_prefill_splits(int64_t total_q, int B, int Hq, int Hkv, int dtype, int64_t max_kv_rows);
-size_t wq_prefill_ws_bytes(int64_t total_q, int Hq, int hd, int splits);
+WqPrefillPlan wq_prefill_plan(int64_t total_q, int B, int Hq, int Hkv, int hd, int dtype, int64_t max_kv_rows, bool prefix, int num_splits);
 int wq_launch_prefill(wq_ctx* ctx, const WqPrefill& f);
 
 struct WqSharedPlan {

@@ -25,7 +25,8 @@ def _case(new, rows, Hq, Hkv, hd, dtype, seed, spread=1.0):
     return q, kv[:, :n].unflatten(-1, (Hkv, hd)), kv[:, n:].unflatten(-1, (Hkv, hd))
 
 
-def _check(new, rows, prefix, Hq, Hkv, hd, dtype, splits, seed=1, spread=1.0):
+def _check(new, rows, prefix, Hq, Hkv, hd, dtype, splits, seed=1, spread=1.0, every=1):
+    """Compares every `every`-th row of a sequence, and its last."""
     q, k, v = _case(new, rows, Hq, Hkv, hd, dtype, seed, spread)
     q_off, kv_off = R.offsets(new), R.offsets(rows)
     scale = 1.0 / math.sqrt(hd)
@@ -43,8 +44,9 @@ def _check(new, rows, prefix, Hq, Hkv, hd, dtype, splits, seed=1, spread=1.0):
             continue
         L = rows[b]
         p = 0 if prefix is None else min(max(prefix[b], 0), L)
-        limit = [max(L - n + i + 1, p) for i in range(n)]
-        qs, ks = slice(q_off[b], q_off[b + 1]), slice(kv_off[b], kv_off[b + 1])
+        picked = list(range(0, n, every)) + ([n - 1] if (n - 1) % every else [])
+        limit = [max(L - n + i + 1, p) for i in picked]
+        qs, ks = [q_off[b] + i for i in picked], slice(kv_off[b], kv_off[b + 1])
         want, want_lse, spread_v, terms = R.attend(q[qs].double().cpu(), k[ks].double().cpu(), v[ks].double().cpu(), limit, scale)
         got, got_lse = out[qs].double().cpu(), lse[qs].double().cpu()
         seen = torch.isfinite(want_lse)
@@ -105,6 +107,15 @@ def test_magnitudes(dtype, spread):
 def test_long_rows():
     _check([700], [2500], [1000], 4, 2, 128, torch.bfloat16, 0)
     _check([2300], [2300], [2000], 2, 1, 64, torch.float16, 1)
+
+
+@pytest.mark.parametrize("dtype", DTYPES[:2])
+def test_a_last_round_of_tiles(dtype):
+    """More tiles than compute units: the last ones are cut along the keys.  One sequence and two, with tiles that see little or nothing."""
+    _check([4400], [4400], [4400], 16, 16, 64, dtype, 0, every=37)
+    _check([1300], [2500], [2000], 56, 8, 128, dtype, 0, every=11)
+    _check([1300], [1000], [0], 56, 8, 128, dtype, 0, every=11)
+    _check([300, 4200], [300, 4200], [10, 3000], 16, 16, 64, dtype, 0, every=37)
 
 
 def test_steep_and_rising_logits():
