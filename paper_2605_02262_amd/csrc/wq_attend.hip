@@ -3,14 +3,26 @@
 // (keys and values are a packed cache that the requests of a group all attend to).
 //
 // A row is a (token, query head) pair or a (request, query head) pair: the rep query heads of a KV head are neighbouring
-// rows of one product, so a tile of keys and values is staged once for all of them.  A workgroup of four wavefronts owns
-// 128 rows (32 per wavefront) and walks the keys 64 at a time:
+// rows of one product, so a tile of keys and values is brought once for all of them.  A workgroup walks the keys a tile at a time:
 //   S^T = K Q^T    A operand: 16 keys, B operand: 16 rows   -> a lane holds 4 x 4 keys of one row
 //   online softmax in the lane's own registers (running reference and sum, fp32)
 //   O^T += V^T P^T A operand: 16 channels, B operand: 16 rows: P^T needs no exchange between lanes, because the keys'
 //                  order inside a product is free: V's operand takes them in the order in which S^T left them
-// Tiles are staged in LDS in the operands' own order, [step][lane][16 bytes], so that every LDS read of the products is one
-// conflict-free 16-byte load per lane.
+// 16-bit types: 256 rows (32 per wavefront), 64 keys; two groups of four wavefronts in turn (take_turns), one workgroup per compute unit
+// (its accumulators, queries and scores take 220 to 240 registers a lane).  fp32: 128 rows, 32 keys, four wavefronts.
+//   k_prefill        keys and values plain rows, from memory into LDS without registers between (Direct)
+//   k_prefill_few    the same for so few query rows that the keys are shared out instead
+//   k_shared         packed classes, expanded to fp16 on their way into LDS (PackedKeys, PackedValues), then 16-bit rows
+//   k_shared_finish  a request's own 16-bit rows, and the merge of the parts; k_merge, k_merge_tail: the merges of k_prefill's
+// Packed tiles lie in LDS in the operands' own order, [step][lane][16 bytes]: every LDS read of the products is one conflict-free 16-byte
+// load per lane.  Plain rows lie as they came, their 16-byte pieces exchanged by row.
+//
+// What bounds it (28 query heads, 4 KV heads of 128, bf16, one MI355X): the vector unit.  A tile of 64 keys takes a wavefront 64 matrix
+// instructions, 1150 cycles, and 1200 to 1450 cycles of exponents, sums and conversions; the two groups' phases together are 3740
+// cycles.  12800 query rows over as many keys: 1.95 ms = 1.18 PFLOP/s, where a library product of 8192^3 reaches 1.37.  A packed tile also has to be
+// expanded, 16384 codes: 4900 cycles; 50 700 packed tokens under 64 requests (448 rows per KV head): 72 us = 0.65 PFLOP/s.
+// A lone wavefront issues one vector instruction in 6 cycles, two on a SIMD one in 2.7: more of them do not fit the registers.
+// Short walks cost what they cannot overlap: 2 us from the launch to the first load, 2 until its first product, 2 for the result.
 //
 // fp32 queries take the fp32 matrix instruction throughout.  16-bit queries take the 16-bit ones: the weights are rounded to
 // the value's type (the sum of weights is not), packed keys and values to fp16 (2^-11 of a value whose own step is its
@@ -256,9 +268,11 @@ __device__ __forceinline__ void attend_f32(Rows<HD>& r, const Query<F32, HD>& q,
 // The two wavefronts of a SIMD belong to different groups, and the groups are half a turn apart: in every phase one of them has the
 // matrix cores and the other one the vector unit.  (Left to themselves they hardly overlap: a wavefront issues at most one instruction in
 // 6 cycles, the older one of a SIMD goes first, and two that mix matrix and vector instructions take twice the time of one.)
-//   phase 2i      group 0: products of tile i      group 1: weights of tile i - 1, brings the values of tile i
-//   phase 2i + 1  group 0: weights of tile i       group 1: products of tile i       (the keys of tile i + 1 are brought by group 0)
-// A tile's keys and values are read in two neighbouring phases, so two tiles of each in LDS are enough.
+//   phase 2i      group 0: products of tile i, brings the keys of tile i + 1      group 1: weights of tile i - 1, brings the values of tile i
+//   phase 2i + 1  group 0: weights of tile i                                      group 1: products of tile i
+// A tile's keys and values are read in two neighbouring phases, so two tiles of each in LDS are enough.  Expanding packed keys fills the vector
+// slots behind the products (with the weights in the next phase: 88 us instead of 86 for the 50 700 tokens above).  Plain rows need no
+// wavefront's time: group 1 sends for values and the next keys.  The group that multiplies has priority (64 frames 2110 -> 2080 us).
 // With up to 128 rows only group 0 has any, and group 1 brings it keys and values (SPLIT).
 // A barrier for what is in LDS: loads into registers stay in flight across it (__syncthreads() waits for them)
 __device__ __forceinline__ void meet()
@@ -474,11 +488,6 @@ __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* w)
     }
 }
 
-// A tile in flight between memory and LDS, in registers, brought by 64 * 4 (TOKENS = 64) or 64 * 2 (32) threads each of keys and of values.  A key
-// unit is a quarter of a token's channels (lane of the product), a value unit 8 tokens of every 16th channel of half of the head.
-// Addresses are a scalar base that moves with the tile and a lane's offset that does not.  A sequence's segment is padded to 32
-// tokens: where a tile's second 32 are not the sequence's, its first 32 are taken again (their weights are zero, but zero times
-// whatever lies there need not be zero).
 // Field f of both halves of w as fp16: placed in the significand of a power of two, which is then taken away (exact)
 template <int BITS, int AT>
 __device__ __forceinline__ uint32_t placed(uint32_t w)
@@ -496,7 +505,11 @@ __device__ __forceinline__ uint32_t expanded(uint32_t x, h2 s, h2 m)
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(code, s, m));       // (one rounding)
 }
 
-
+// A tile in flight between memory and LDS, in registers, brought by 64 * 4 (TOKENS = 64) or 64 * 2 (32) threads each of keys and of values.  A key
+// unit is a quarter of a token's channels (lane of the product), a value unit 8 tokens of every 16th channel of half of the head.
+// Addresses are a scalar base that moves with the tile and a lane's offset that does not.  A sequence's segment is padded to 32
+// tokens: where a tile's second 32 are not the sequence's, its first 32 are taken again (their weights are zero, but zero times
+// whatever lies there need not be zero).
 template <int HD, int BITS, int TOKENS>
 struct PackedKeys {
     static constexpr int C = BITS == 2 ? 0 : (BITS == 4 ? 1 : 2), N = HD / 4, BYTES = N * BITS / 8;
@@ -1229,7 +1242,8 @@ __device__ __forceinline__ f4 join_few(const Few<HD>& s, int r, float w)
     return x;
 }
 
-// wq_prefill_attention over few query rows: a workgroup per 16 of them and part of the keys
+// wq_prefill_attention over few query rows: a workgroup per 16 of them and part of the keys.  Bound by latencies: 8 single tokens (14 query heads, 2 KV
+// heads of 64) over 6400 rows, 26 MB: 13.0 us with the merge (k_prefill: 15.4).
 template <typename CT, int HD>
 __global__ __launch_bounds__(64 * FEW, 4) void k_prefill_few(PrefillArgs a, int dtype)
 {
@@ -1289,6 +1303,8 @@ struct FinishArgs {
     Out out;
 };
 
+// Memory-bound where there are many requests: 64 of them with 200 rows each and 32 parts, 80 MB: 12.6 us.  (As further workgroups of k_shared
+// they cost the same; the merge alone first and the walk in front of it, one after the other, 3 us more for a few short ones.)
 // A workgroup per (request, KV head): eight wavefronts walk the request's own rows, while wavefront 8 + r merges query head r's parts;
 // then each of those takes in what the eight have found.
 template <typename QT, int HD>
@@ -1359,8 +1375,10 @@ size_t partials_bytes(int64_t rows, int hd, int parts) { return wq_align256((siz
 // Query rows of a workgroup of the prompt's and the shared kernels: 256, or 128 where that is all there are (two groups of wavefronts, half the
 // keys each)
 int rows_of(int64_t q_rows, int rep, int dtype) { return dtype != WQ_F32 && q_rows * rep > 128 ? 256 : 128; }
-// Prompt attention over so few that k_prefill_few takes them (on the average: any number is right)
-bool few_rows(int64_t total_q, int B, int rep, int dtype) { return dtype != WQ_F32 && total_q * rep <= (int64_t)B * 16; }
+// Prompt attention over so few that k_prefill_few takes them (on the average: any number is right): two tiles of 16, though each reads the
+// keys.  us per call, k_prefill -> k_prefill_few: 4 rows of 7 heads a group, 64 sequences of 6400 keys, heads of 64: 142 -> 79 (5 rows would be three
+// tiles: 143), of 128: 412 -> 315; one sequence of 500 keys: 8.8 -> 7.6 and 9.7 -> 11.9.
+bool few_rows(int64_t total_q, int B, int rep, int dtype) { return dtype != WQ_F32 && total_q * rep <= (int64_t)B * 32; }
 
 template <typename CT>
 auto prefill_kernel(int hd, bool split) -> void (*)(PrefillArgs)
@@ -1380,8 +1398,11 @@ auto shared_kernel(int hd, bool split) -> void (*)(SharedArgs)
 template <typename QT>
 auto finish_kernel(int hd) -> void (*)(FinishArgs) { return hd == 128 ? k_shared_finish<QT, 128> : k_shared_finish<QT, 64>; }
 
-// Longer own caches, and those with room for packed tokens, have a decode launch of their own
-constexpr int64_t OWN_INSIDE = 2048;
+// Own caches with room for packed tokens have a decode launch of their own, and longer ones where there are too few requests to fill the
+// card: k_shared_finish walks a request's rows with one workgroup per KV head, 256 keys in about 1.1 us.  us per call over 39 000 shared tokens, own
+// rows there -> apart, 4 KV heads: 1 request, 512 rows 41 -> 44, 1024: 46 -> 44, 2048: 54 -> 44; 16 requests, 1024: 51 -> 52, 2048: 60 -> 57;
+// 64 requests, 512: 78 -> 88, 4000: 168 -> 183.
+constexpr int64_t OWN_INSIDE = 1024;
 // Below this many keys a tail's merge costs more than its parts save
 constexpr int64_t TAIL_KEYS = 2048;
 
@@ -1396,10 +1417,12 @@ WqPrefillPlan wq_prefill_plan(int64_t total_q, int B, int Hq, int Hkv, int hd, i
     const int rows = s.few ? 16 : rows_of((total_q + B - 1) / B, rep, dtype);
     s.rows = rows;
     if (num_splits <= 0) {
-        s.splits = s.few ? auto_splits_of((tiles_of(total_q, rep, 0, rows) + used) * Hkv, max_kv_rows, 512, 32 * FEW)
+        // (few rows: no parts of up to 512 keys, two rounds of every wavefront: a merge costs 3 us, a round one)
+        s.splits = s.few ? max_kv_rows <= 512 ? 1 : auto_splits_of((tiles_of(total_q, rep, 0, rows) + used) * Hkv, max_kv_rows, 512, 32 * FEW)
                          : auto_splits_of((tiles_of(total_q, rep, 0, rows) + used) * Hkv, max_kv_rows, 256, dtype == WQ_F32 ? 32 : 64);
         // Tiles of equal length (a prefix) for more than the card's 256 compute units: the last round's, where they are no more than half of
-        // them, are cut along the keys to fill it.
+        // them, are cut along the keys to fill it (1404 tiles, 124 of them cut in two: 1950 us, 2050 uncut).  Where there is no prefix tiles are
+        // launched longest first, and the last ones are short.
         const int64_t units = tiles_of(total_q, rep, B, rows) * Hkv, rest = units % 256;
         if (rows == 256 && s.splits == 1 && prefix && units > 256 && rest > 0 && rest <= 128 && max_kv_rows >= TAIL_KEYS) {
             s.tail = (int)rest;
@@ -1418,7 +1441,7 @@ WqSharedPlan wq_shared_plan(int B, int P, int Hq, int Hkv, int hd, int q_dtype, 
     s.splits = num_splits > 0 ? num_splits
                               : auto_splits_of(tiles_of(B, Hq / Hkv, P, rows_of(B, Hq / Hkv, q_dtype)) * Hkv, max_prefix_tokens, 256,
                                               q_dtype == WQ_F32 ? 32 : 64);
-    s.own_decode = own && (own_packed || max_own_tokens > OWN_INSIDE);
+    s.own_decode = own && (own_packed || (max_own_tokens > OWN_INSIDE && (int64_t)B * Hkv < 256));
     const int64_t rows = (int64_t)B * Hq;
     s.decode_bytes = s.own_decode ? wq_decode_ws_bytes(B, Hq, hd, wq_auto_splits(B, Hkv, max_own_tokens)) : 0;
     s.bytes = s.decode_bytes + partials_bytes(rows, hd, s.splits);
