@@ -325,20 +325,25 @@ def wq_decode_attention_static(q, kv: PackedKV, sm_scale: float, num_splits: int
 # ------------------------------------------------------------------------------------------------------------
 # rotary positions, prompt attention, decode over shared caches
 # ------------------------------------------------------------------------------------------------------------
-def _rows(name: str, t: torch.Tensor, like: Optional[torch.Tensor] = None) -> int:
-    """Row stride of [rows, heads, hd] whose rows are contiguous inside."""
-    shape = tuple(t.shape)                          # (read once: each attribute of a tensor costs about 0.1 us)
-    if len(shape) != 3:
-        raise ValueError(f"{name}: [rows, heads, head_dim] expected, got shape {shape}")
-    rows, heads, hd = shape
-    if like is not None and (t.dtype != like.dtype or hd != like.shape[2]):
-        raise ValueError(f"{name}: type or head_dim differ from the queries'")
+# (A call's checks cost about as much as its launch: a tensor's attributes are read once, 0.1 us each, and outputs made here are not checked.)
+def _rows(name: str, t: torch.Tensor, like: Optional[torch.Tensor] = None, shape=None):
+    """(rows, heads, hd, elements from row to row) of [rows, heads, hd] whose rows are contiguous inside; like: of its type, shape: of that."""
+    have = tuple(t.shape)
+    if len(have) != 3 or (shape is not None and have != shape):
+        raise ValueError(f"{name}: {shape or '[rows, heads, head_dim]'} expected, got shape {have}")
+    if like is not None and t.dtype != like.dtype:
+        raise ValueError(f"{name}: type differs from the queries'")
+    rows, heads, hd = have
     if t.is_contiguous():
-        return heads * hd
+        return rows, heads, hd, heads * hd
     row, head, channel = t.stride()
     if channel != 1 or (heads > 1 and head != hd):
-        raise ValueError(f"{name}: [rows, heads, head_dim] with contiguous rows expected, got shape {shape}, strides {t.stride()}")
-    return max(row, heads * hd) if rows <= 1 else row
+        raise ValueError(f"{name}: [rows, heads, head_dim] with contiguous rows expected, got shape {have}, strides {t.stride()}")
+    return rows, heads, hd, max(row, heads * hd) if rows <= 1 else row
+
+
+def _like(t: torch.Tensor) -> torch.Tensor:
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
 def _contiguous(name: str, t: torch.Tensor, dtype: torch.dtype, numel: int):
@@ -358,24 +363,24 @@ def wq_rope_frequencies(rot_dim: int, base: float, scaling: int = ROPE_PLAIN, fa
 def wq_rope(ctx: Context, q, k, positions, inv_freq, layout: int = ROPE_HALF, mscale: float = 1.0, q_out: Optional[torch.Tensor] = None,
             k_out: Optional[torch.Tensor] = None):
     """Turns q [rows, Hq, hd] and k [rows, Hkv, hd] (or None); 2 * inv_freq.numel() channels of every head."""
-    qs = _rows("q", q)
-    rows, Hq, hd = q.shape
+    rows, Hq, hd, qs = _rows("q", q)
     _contiguous("positions", positions, torch.int32, rows)
-    _contiguous("inv_freq", inv_freq, torch.float32, inv_freq.numel())
+    half = inv_freq.numel()
+    _contiguous("inv_freq", inv_freq, torch.float32, half)
     if q_out is None:
-        q_out = torch.empty(rows, Hq, hd, dtype=q.dtype, device=q.device)
-    qo = _rows("q_out", q_out, q)
+        q_out, qo = _like(q), Hq * hd
+    else:
+        qo = _rows("q_out", q_out, q, (rows, Hq, hd))[3]
     ks = ko = Hkv = 0
     if k is not None:
-        ks, Hkv = _rows("k", k, q), k.shape[1]
+        k_rows, Hkv, k_hd, ks = _rows("k", k, q)
+        if k_rows != rows or k_hd != hd:
+            raise ValueError("k: the rows and head_dim of q expected")
         if k_out is None:
-            k_out = torch.empty(rows, Hkv, hd, dtype=k.dtype, device=k.device)
-        ko = _rows("k_out", k_out, q)
-        if k.shape[0] != rows or k_out.shape != k.shape:
-            raise ValueError("k, k_out: as many rows as q expected")
-    if q_out.shape != q.shape:
-        raise ValueError("q_out: the shape of q expected")
-    ctx.check(lib().wq_rope(ctx.handle, _ptr(q), qs, _ptr(k), ks, _dtype_id(q), rows, Hq, Hkv, hd, 2 * inv_freq.numel(), layout, _ptr(positions),
+            k_out, ko = _like(k), Hkv * hd
+        else:
+            ko = _rows("k_out", k_out, q, (rows, Hkv, hd))[3]
+    ctx.check(lib().wq_rope(ctx.handle, _ptr(q), qs, _ptr(k), ks, _dtype_id(q), rows, Hq, Hkv, hd, 2 * half, layout, _ptr(positions),
                             _ptr(inv_freq), mscale, _ptr(q_out), qo, _ptr(k_out) if k is not None else None, ko))
     return q_out, k_out
 
@@ -383,18 +388,20 @@ def wq_rope(ctx: Context, q, k, positions, inv_freq, layout: int = ROPE_HALF, ms
 def wq_rope_append_kv(ctx: Context, q, k, v, positions, inv_freq, kv: PackedKV, layout: int = ROPE_HALF, mscale: float = 1.0,
                       q_out: Optional[torch.Tensor] = None):
     """Turns q [B, Hq, hd] (returned) and k [B, Hkv, hd]; k and v become the cache's next rows."""
-    B, Hq, hd = q.shape
-    qs, ks, vs = _rows("q", q), _rows("k", k, q), _rows("v", v, q)
-    if k.shape != (B, kv.Hkv, kv.hd) or v.shape != k.shape:
-        raise ValueError("k, v: [B, Hkv, hd] of the cache expected")
+    B, Hq, hd, qs = _rows("q", q)
+    shape = (B, kv.Hkv, kv.hd)
+    if hd != kv.hd:
+        raise ValueError("q: the head_dim of the cache expected")
+    ks, vs = _rows("k", k, q, shape)[3], _rows("v", v, q, shape)[3]
     _contiguous("positions", positions, torch.int32, B)
-    _contiguous("inv_freq", inv_freq, torch.float32, inv_freq.numel())
+    half = inv_freq.numel()
+    _contiguous("inv_freq", inv_freq, torch.float32, half)
     if q_out is None:
-        q_out = torch.empty(B, Hq, hd, dtype=q.dtype, device=q.device)
-    if q_out.shape != q.shape:
-        raise ValueError("q_out: the shape of q expected")
-    ctx.check(lib().wq_rope_append_kv(ctx.handle, _ptr(q), qs, _ptr(k), ks, _ptr(v), vs, _dtype_id(q), B, Hq, 2 * inv_freq.numel(), layout,
-                                      _ptr(positions), _ptr(inv_freq), mscale, _ptr(q_out), _rows("q_out", q_out, q), C.byref(kv.desc)))
+        q_out, qo = _like(q), Hq * hd
+    else:
+        qo = _rows("q_out", q_out, q, (B, Hq, hd))[3]
+    ctx.check(lib().wq_rope_append_kv(ctx.handle, _ptr(q), qs, _ptr(k), ks, _ptr(v), vs, _dtype_id(q), B, Hq, 2 * half, layout, _ptr(positions),
+                                      _ptr(inv_freq), mscale, _ptr(q_out), qo, C.byref(kv.desc)))
     return q_out
 
 
@@ -405,19 +412,20 @@ def prefill_workspace_bytes(total_q: int, B: int, Hq: int, Hkv: int, hd: int, ma
 def wq_prefill_attention(ctx: Context, q, k, v, q_off, kv_off, sm_scale: float, prefix_len: Optional[torch.Tensor] = None, max_kv_rows: int = 0,
                          num_splits: int = 0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None):
     """q [total_q, Hq, hd] over k, v [total_kv, Hkv, hd]; q_off, kv_off [B+1], prefix_len [B] int32."""
-    qs, ks, vs = _rows("q", q), _rows("k", k, q), _rows("v", v, q)
-    total_q, Hq, hd = q.shape
-    total_kv, Hkv, _ = k.shape
+    total_q, Hq, hd, qs = _rows("q", q)
+    total_kv, Hkv, k_hd, ks = _rows("k", k, q)
+    if k_hd != hd:
+        raise ValueError("k: the head_dim of q expected")
+    vs = _rows("v", v, q, (total_kv, Hkv, hd))[3]
     B = q_off.numel() - 1
-    if v.shape != k.shape:
-        raise ValueError("v: the shape of k expected")
     _contiguous("q_off", q_off, torch.int32, B + 1)
     _contiguous("kv_off", kv_off, torch.int32, B + 1)
     if prefix_len is not None:
         _contiguous("prefix_len", prefix_len, torch.int32, B)
     if out is None:
-        out = torch.empty(total_q, Hq, hd, dtype=q.dtype, device=q.device)
-    _contiguous("out", out, q.dtype, q.numel())
+        out = _like(q)
+    else:
+        _contiguous("out", out, q.dtype, q.numel())
     if lse is not None:
         _contiguous("lse", lse, torch.float32, total_q * Hq)
     ctx.check(lib().wq_prefill_attention(ctx.handle, _ptr(q), qs, _ptr(k), ks, _ptr(v), vs, _dtype_id(q), B, Hq, Hkv, hd, _ptr(q_off), _ptr(kv_off),
@@ -439,8 +447,9 @@ def wq_decode_attention_shared(ctx: Context, q, prefix: PackedKV, req_off, own: 
     _contiguous("q", q, q.dtype, q.numel())
     _contiguous("req_off", req_off, torch.int32, prefix.B + 1)
     if out is None:
-        out = torch.empty(B, Hq, hd, dtype=q.dtype, device=q.device)
-    _contiguous("out", out, q.dtype, q.numel())
+        out = _like(q)
+    else:
+        _contiguous("out", out, q.dtype, q.numel())
     if lse is not None:
         _contiguous("lse", lse, torch.float32, B * Hq)
     ctx.check(lib().wq_decode_attention_shared(ctx.handle, _ptr(q), _dtype_id(q), B, Hq, C.byref(prefix.desc), _ptr(req_off),

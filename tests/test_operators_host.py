@@ -159,8 +159,11 @@ def test_frequencies(W):
 def test_binding_refuses_rows_that_it_cannot_describe(W):
     """Inner strides, types and shapes that a pointer and a row stride would silently misread."""
     t = torch.zeros(4, 14, 64)
-    assert W._rows("t", t) == 14 * 64 and W._rows("t", torch.zeros(4, 2000)[:, :14 * 64].unflatten(1, (14, 64))) == 2000
-    assert W._rows("t", t[:1]) == 14 * 64
+    wide = torch.zeros(4, 2000)[:, :14 * 64].unflatten(1, (14, 64))
+    assert W._rows("t", t) == (4, 14, 64, 14 * 64) and W._rows("t", wide) == (4, 14, 64, 2000)
+    assert W._rows("t", t[:1]) == (1, 14, 64, 14 * 64)
+    with pytest.raises(ValueError):
+        W._rows("t", t, t, (4, 14, 128))
     for bad in (t.transpose(0, 1), t[..., ::2], t[:, ::2], t.flatten(1)):
         with pytest.raises(ValueError):
             W._rows("t", bad)
