@@ -381,7 +381,7 @@ size_t wq_prefill_workspace_bytes(int64_t total_q, int B, int Hq, int Hkv, int h
  * bf16; fp16 and fp32 with fp16); lse [B, Hq] fp32 or NULL.  Both caches: the same Hkv, hd and dtype16.
  * 16-bit queries: packed keys and values are expanded to fp16 and met by fp16 weights (errors of 2^-11 relative to a value, the
  * result has the query's type); a bf16 query is exact down to 2^-24 of its head's largest entry.  fp32 queries: fp32 arithmetic.
- * num_splits: workgroups that share the tokens of a prefix per tile of 256 query rows (128: fp32, or where there are no more; a
+ * num_splits: workgroups that share the tokens of a prefix per tile of 256 query rows (fp32: 128; a
  * request has Hq/Hkv of them), 1 .. 64, or 0 = automatic; max_prefix_tokens, max_own_tokens: host bounds on the tokens of one sequence
  * (used for splits and the choice of kernels; any value gives the same result to rounding).  q, out and the caches' buffers 16-byte aligned.  Workspace: wq_shared_workspace_bytes (max_own_tokens 0 where own is NULL).                            */
 int wq_decode_attention_shared(wq_ctx* ctx, const void* q, int q_dtype, int B, int Hq, const wq_packed_kv* prefix, const int32_t* req_off,

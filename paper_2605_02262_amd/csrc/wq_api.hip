@@ -382,6 +382,7 @@ int wq_decode_attention(wq_ctx* ctx, const void* q, int q_dtype, int B, int Hq, 
 }
 
 // ---- rotary positions, prompt attention, decode over shared caches -----------------------------------------------------
+constexpr int64_t MOST_GROUPS_512 = WQ_MOST_GROUPS_256 / 2, MOST_GROUPS_1024 = WQ_MOST_GROUPS_256 / 4;
 
 static bool on_16_bytes(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
@@ -448,6 +449,7 @@ int wq_rope_append_kv(wq_ctx* ctx, const void* q, int64_t q_stride, const void* 
     rc = check_rope(ctx, r);
     if (rc == WQ_OK) rc = check_rows(ctx, "v", v, v_stride, B, kv->Hkv, kv->hd, dtype);
     if (rc != WQ_OK) return rc;
+    if (B > WQ_MOST_GROUPS_256) return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "too many sequences");
     if ((dtype == WQ_BF16) != (kv->dtype16 == WQ_BF16))
         return wq_fail(ctx, WQ_ERR_ARG, "dtype16 must be bf16 for bf16 input and fp16 for fp16/fp32 input");
     if (q == q_out && q_stride != q_out_stride) return wq_fail(ctx, WQ_ERR_ARG, "q in place with another stride");
@@ -497,7 +499,7 @@ int wq_prefill_attention(wq_ctx* ctx, const void* q, int64_t q_stride, const voi
     if (Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || Hq / Hkv > WQ_MAX_REP)
         return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "Hq=%d must be a multiple of Hkv=%d, at most %d query heads per KV head", Hq, Hkv, WQ_MAX_REP);
     const int rep = Hq / Hkv;
-    if (total_q > INT32_MAX / rep || total_kv > INT32_MAX || B > INT32_MAX / 2 || (total_q * rep / 16 + B + 1) > INT32_MAX / Hkv)
+    if (total_q > INT32_MAX / rep || total_kv > INT32_MAX - 256 || B > INT32_MAX / 2)       // (positions and tiles' ends have 32 bits)
         return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "too many rows");
     if (num_splits < 0 || num_splits > WQ_MAX_ATTEND_SPLITS) return wq_fail(ctx, WQ_ERR_ARG, "num_splits out of range");
     if (!(sm_scale > 0.0f) || sm_scale > 3.0e38f) return wq_fail(ctx, WQ_ERR_ARG, "sm_scale must be positive and finite");
@@ -511,6 +513,7 @@ int wq_prefill_attention(wq_ctx* ctx, const void* q, int64_t q_stride, const voi
     if (total_kv > 0 && (k_stride > 1 << 22 || v_stride > 1 << 22))       // (offsets inside a tile have 32 bits)
         return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "rows of k or v are more than 2^22 elements apart");
     const WqPrefillPlan plan = wq_prefill_plan(total_q, B, Hq, Hkv, hd, dtype, max_kv_rows, prefix_len != nullptr, num_splits);
+    if (plan.groups > MOST_GROUPS_512 || (plan.splits > 1 && total_q * Hq > 4 * WQ_MOST_GROUPS_256)) return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "too many rows");
     if (ctx->ws_bytes < WQ_WS_HEADER + plan.bytes || !ctx->ws)
         return wq_fail(ctx, WQ_ERR_WORKSPACE, "workspace too small for %d splits of %lld rows", plan.tail > 0 ? plan.tail_splits : plan.splits, (long long)total_q);
     return wq_launch_prefill(ctx, {q, k, v, q_stride, k_stride, v_stride, dtype, B, Hq, Hkv, hd, plan, q_off, kv_off, prefix_len, total_q, total_kv, sm_scale,
@@ -557,7 +560,7 @@ int wq_decode_attention_shared(wq_ctx* ctx, const void* q, int q_dtype, int B, i
     if (!q || !out || !req_off) return wq_fail(ctx, WQ_ERR_ARG, "NULL q, out or req_off");
     const WqSharedPlan plan = wq_shared_plan(B, prefix->B, Hq, prefix->Hkv, prefix->hd, q_dtype, max_prefix_tokens, max_own_tokens, own != nullptr,
                                              own && own->cap[0] + own->cap[1] + own->cap[2] > 0, num_splits);
-    if (((int64_t)B * (Hq / prefix->Hkv) / 64 + prefix->B) * prefix->Hkv * plan.splits > INT32_MAX || (int64_t)B * prefix->Hkv > INT32_MAX)
+    if (plan.groups > MOST_GROUPS_512 || (int64_t)B * prefix->Hkv > MOST_GROUPS_1024)
         return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "too many workgroups");
     if (!ctx->ws || ctx->ws_bytes < WQ_WS_HEADER + plan.bytes)
         return wq_fail(ctx, WQ_ERR_WORKSPACE, "workspace too small for %d splits of %d requests", plan.splits, B);

@@ -273,7 +273,7 @@ __device__ __forceinline__ void attend_f32(Rows<HD>& r, const Query<F32, HD>& q,
 // A tile's keys and values are read in two neighbouring phases, so two tiles of each in LDS are enough.  Expanding packed keys fills the vector
 // slots behind the products (with the weights in the next phase: 88 us instead of 86 for the 50 700 tokens above).  Plain rows need no
 // wavefront's time: group 1 sends for values and the next keys.  The group that multiplies has priority (64 frames 2110 -> 2080 us).
-// With up to 128 rows only group 0 has any, and group 1 brings it keys and values (SPLIT).
+// SPLIT: up to 128 rows, all group 0's; group 1 brings it keys and values.
 // A barrier for what is in LDS: loads into registers stay in flight across it (__syncthreads() waits for them)
 __device__ __forceinline__ void meet()
 {
@@ -297,7 +297,6 @@ __device__ __forceinline__ void take_turns(Rows<HD>& r, const Query<CT, HD>& q, 
         for (int t = t0; t < t1; t++) {
             bring_values(t);
             settle();
-            if (t + 1 < t1) bring_keys(t + 1);
             settle();
         }
         settle();
@@ -667,13 +666,13 @@ struct PackedValues {
 };
 
 // Tiles t0 .. t1-1 of a class's segment
-template <int HD, int BITS, bool SPLIT>
+template <int HD, int BITS>
 __device__ __forceinline__ void walk_packed(Rows<HD>& r, const Query<F16, HD>& q, const wq_packed_kv& kv, int kvh, int64_t tok0, int len, int t0, int t1,
                                             Lds k_lds, Lds v_lds)
 {
     using Order = std::conditional_t<BITS == 8, Near, Far>;
     constexpr int BYTES = TILE_BYTES<F16, HD>;
-    const int slots = (len + 31) / 32 * 32, lane = threadIdx.x & 63, keys_by = SPLIT ? 1 : 0;
+    const int slots = (len + 31) / 32 * 32, lane = threadIdx.x & 63;
     PackedKeys<HD, BITS, 64> keys(kv, kvh, tok0, slots);
     PackedValues<HD, BITS, 64> values(kv, kvh, tok0, slots);
     auto k_of = [&](int t) { return (Lds4)(k_lds + (t & 1) * BYTES); };
@@ -687,14 +686,15 @@ __device__ __forceinline__ void walk_packed(Rows<HD>& r, const Query<F16, HD>& q
         if (t + 1 < t1) values.load(t + 1);
     };
     __syncthreads();                                           // (whatever was in LDS before has been read)
-    if (group_of_wave() == 1) values.load(t0);
-    else clear_tile<F16, HD>(v_lds + (~t0 & 1) * BYTES);
-    if (group_of_wave() == keys_by) {
+    if (group_of_wave() == 1) {
+        values.load(t0);
+    } else {
+        clear_tile<F16, HD>(v_lds + (~t0 & 1) * BYTES);
         keys.load(t0);
         bring_keys(t0);
     }
     __syncthreads();
-    take_turns<F16, HD, SPLIT, Order>(
+    take_turns<F16, HD, false, Order>(
         r, q, t0, t1, len, [&](int t, int kt, int st) { return k_of(t)[(kt * STEPS<F16, HD> + st) * 64 + lane]; },
         [&](int t, int vs, int ct) { return v_of(t)[(vs * (HD / 16) + ct) * 64 + lane]; }, bring_keys, bring_values, meet);
 }
@@ -840,7 +840,7 @@ struct PrefillArgs {
     Out out;
 };
 
-template <typename CT, bool SPLIT> constexpr int ROWS = std::is_same_v<CT, F32> || SPLIT ? 128 : 256;       // of a workgroup
+template <typename CT, bool SPLIT = false> constexpr int ROWS = std::is_same_v<CT, F32> || SPLIT ? 128 : 256;       // of a workgroup
 
 template <typename CT, int HD, bool SPLIT>
 __global__ __launch_bounds__(64 * WAVES<CT>, 2) void k_prefill(PrefillArgs a)
@@ -915,12 +915,12 @@ struct SharedArgs {
 
 // QT: the query's type; packed tokens are walked in fp16 (fp32 for fp32 queries), 16-bit rows in the
 // cache's own type.
-template <typename QT, int HD, bool SPLIT>
+template <typename QT, int HD>
 __global__ __launch_bounds__(64 * WAVES<QT>, 2) void k_shared(SharedArgs a)
 {
     using CT = std::conditional_t<std::is_same_v<QT, F32>, F32, F16>;
     constexpr bool PIPED = ESIZE<QT> == 2;
-    constexpr int BYTES = TILE_BYTES<CT, HD> * (1 + PIPED), R = ROWS<QT, SPLIT>, TK = KEYS<QT>;
+    constexpr int BYTES = TILE_BYTES<CT, HD> * (1 + PIPED), R = ROWS<QT>, TK = KEYS<QT>;
     __shared__ __align__(16) char s_k[BYTES], s_v[BYTES];
     const int Hkv = a.kv.Hkv, wave = this_wave(), lane = threadIdx.x & 63;
     const wq_packed_kv& kv = a.kv;
@@ -965,7 +965,7 @@ __global__ __launch_bounds__(64 * WAVES<QT>, 2) void k_shared(SharedArgs a)
             if constexpr (PIPED) order_query<BITS, HD>(q, n);
         }
         if constexpr (PIPED) {
-            walk_packed<HD, BITS, SPLIT>(r, q, kv, kvh, kv.cls_off[c][p.seq], len[c], t0, t1, (Lds)s_k, (Lds)s_v);
+            walk_packed<HD, BITS>(r, q, kv, kvh, kv.cls_off[c][p.seq], len[c], t0, t1, (Lds)s_k, (Lds)s_v);
         } else {
             PackedKeys<HD, BITS, 32> keys(kv, kvh, kv.cls_off[c][p.seq], 0);
             PackedValues<HD, BITS, 32> values(kv, kvh, kv.cls_off[c][p.seq], 0);
@@ -1002,7 +1002,7 @@ __global__ __launch_bounds__(64 * WAVES<QT>, 2) void k_shared(SharedArgs a)
         const char* k = static_cast<const char*>(kv.k16) + row0 * stride + kvh * (HD * 2);
         const char* v = static_cast<const char*>(kv.v16) + row0 * stride + kvh * (HD * 2);
         if constexpr (PIPED) {
-            walk_rows<QT, HD, SPLIT>(r, q, k, v, stride, stride, len[3], t0, t1, len[3], (Lds)s_k, (Lds)s_v);
+            walk_rows<QT, HD, false>(r, q, k, v, stride, stride, len[3], t0, t1, len[3], (Lds)s_k, (Lds)s_v);
         } else {
             for (int t = t0; t < t1; t++) {
                 const int key0 = t * TK;
@@ -1372,8 +1372,9 @@ int auto_splits_of(int64_t workgroups, int64_t max_keys, int want, int keys)
 
 size_t partials_bytes(int64_t rows, int hd, int parts) { return wq_align256((size_t)rows * parts * (hd + 2) * sizeof(float)); }
 
-// Query rows of a workgroup of the prompt's and the shared kernels: 256, or 128 where that is all there are (two groups of wavefronts, half the
-// keys each)
+// Query rows of a workgroup of the prompt's kernels: 256, or 128 where there are no more (SPLIT).  us per call, 256 -> 128: 9 rows of 7 heads, 64
+// sequences of 6400 keys, heads of 64: 206 -> 145; one of 12544, heads of 128: 22.6 -> 19.4.  The shared kernels always take 256: both groups
+// expand tiles then, rows or not (112 rows a KV head, 19719 tokens, 128 -> 256: 34.4 -> 32.5).
 int rows_of(int64_t q_rows, int rep, int dtype) { return dtype != WQ_F32 && q_rows * rep > 128 ? 256 : 128; }
 // Prompt attention over so few that k_prefill_few takes them (on the average: any number is right): two tiles of 16, though each reads the
 // keys.  us per call, k_prefill -> k_prefill_few: 4 rows of 7 heads a group, 64 sequences of 6400 keys, heads of 64: 142 -> 79 (5 rows would be three
@@ -1388,12 +1389,7 @@ auto prefill_kernel(int hd, bool split) -> void (*)(PrefillArgs)
     return hd == 128 ? k_prefill<CT, 128, false> : k_prefill<CT, 64, false>;
 }
 template <typename QT>
-auto shared_kernel(int hd, bool split) -> void (*)(SharedArgs)
-{
-    if constexpr (!std::is_same_v<QT, F32>)
-        if (split) return hd == 128 ? k_shared<QT, 128, true> : k_shared<QT, 64, true>;
-    return hd == 128 ? k_shared<QT, 128, false> : k_shared<QT, 64, false>;
-}
+auto shared_kernel(int hd) -> void (*)(SharedArgs) { return hd == 128 ? k_shared<QT, 128> : k_shared<QT, 64>; }
 
 template <typename QT>
 auto finish_kernel(int hd) -> void (*)(FinishArgs) { return hd == 128 ? k_shared_finish<QT, 128> : k_shared_finish<QT, 64>; }
@@ -1412,10 +1408,13 @@ WqPrefillPlan wq_prefill_plan(int64_t total_q, int B, int Hq, int Hkv, int hd, i
 {
     const int rep = Hq / Hkv;
     const int64_t used = total_q < B ? total_q : B;           // sequences that have rows
-    WqPrefillPlan s = {0, num_splits, 0, 0, 0};
+    WqPrefillPlan s = {};
+    s.splits = num_splits;
     s.few = few_rows(total_q, B, rep, dtype);
     const int rows = s.few ? 16 : rows_of((total_q + B - 1) / B, rep, dtype);
     s.rows = rows;
+    const int64_t units = tiles_of(total_q, rep, B, rows) * Hkv;
+    s.groups = units;
     if (num_splits <= 0) {
         // (few rows: no parts of up to 512 keys, two rounds of every wavefront: a merge costs 3 us, a round one)
         s.splits = s.few ? max_kv_rows <= 512 ? 1 : auto_splits_of((tiles_of(total_q, rep, 0, rows) + used) * Hkv, max_kv_rows, 512, 32 * FEW)
@@ -1423,7 +1422,7 @@ WqPrefillPlan wq_prefill_plan(int64_t total_q, int B, int Hq, int Hkv, int hd, i
         // Tiles of equal length (a prefix) for more than the card's 256 compute units: the last round's, where they are no more than half of
         // them, are cut along the keys to fill it (1404 tiles, 124 of them cut in two: 1950 us, 2050 uncut).  Where there is no prefix tiles are
         // launched longest first, and the last ones are short.
-        const int64_t units = tiles_of(total_q, rep, B, rows) * Hkv, rest = units % 256;
+        const int64_t rest = units % 256;
         if (rows == 256 && s.splits == 1 && prefix && units > 256 && rest > 0 && rest <= 128 && max_kv_rows >= TAIL_KEYS) {
             s.tail = (int)rest;
             s.tail_splits = (int)(256 / rest < max_kv_rows / 512 ? 256 / rest : max_kv_rows / 512);
@@ -1437,10 +1436,11 @@ WqPrefillPlan wq_prefill_plan(int64_t total_q, int B, int Hq, int Hkv, int hd, i
 WqSharedPlan wq_shared_plan(int B, int P, int Hq, int Hkv, int hd, int q_dtype, int64_t max_prefix_tokens, int64_t max_own_tokens, bool own, bool own_packed,
                             int num_splits)
 {
+    const int rep = Hq / Hkv;
     WqSharedPlan s;
-    s.splits = num_splits > 0 ? num_splits
-                              : auto_splits_of(tiles_of(B, Hq / Hkv, P, rows_of(B, Hq / Hkv, q_dtype)) * Hkv, max_prefix_tokens, 256,
-                                              q_dtype == WQ_F32 ? 32 : 64);
+    s.rows = q_dtype == WQ_F32 ? 128 : 256;
+    s.splits = num_splits > 0 ? num_splits : auto_splits_of(tiles_of(B, rep, P, s.rows) * Hkv, max_prefix_tokens, 256, q_dtype == WQ_F32 ? 32 : 64);
+    s.groups = tiles_of(B, rep, P, s.rows) * Hkv * s.splits;
     s.own_decode = own && (own_packed || (max_own_tokens > OWN_INSIDE && (int64_t)B * Hkv < 256));
     const int64_t rows = (int64_t)B * Hq;
     s.decode_bytes = s.own_decode ? wq_decode_ws_bytes(B, Hq, hd, wq_auto_splits(B, Hkv, max_own_tokens)) : 0;
@@ -1461,7 +1461,7 @@ int wq_launch_prefill(wq_ctx* ctx, const WqPrefill& f)
     a.scale = f.sm_scale * LOG2E;
     a.out.out = f.out, a.out.lse = f.lse;
     a.out.part = reinterpret_cast<float*>(ctx->ws + WQ_WS_HEADER);
-    a.units = (int)(f.Hkv * tiles_of(f.total_q, a.rep, f.B, f.plan.rows)), a.tail = f.plan.tail, a.tail_splits = f.plan.tail_splits;
+    a.units = (int)f.plan.groups, a.tail = f.plan.tail, a.tail_splits = f.plan.tail_splits;
     a.out.part_ml = a.out.part + (a.tail > 0 ? (int64_t)a.tail * 256 * a.tail_splits : f.total_q * f.Hq * a.splits) * f.hd;
     const dim3 grid((unsigned)(a.units - a.tail + a.tail * a.tail_splits), (unsigned)a.splits);
     if (f.plan.few) {
@@ -1489,12 +1489,11 @@ int wq_launch_shared(wq_ctx* ctx, const WqShared& f)
 {
     const wq_packed_kv* kv = f.prefix;
     const int64_t rows = (int64_t)f.B * f.Hq;
-    const int tile_rows = rows_of(f.B, f.Hq / kv->Hkv, f.q_dtype);
     SharedArgs a;
     a.q = static_cast<const char*>(f.q);
     a.req_off = f.req_off;
     a.B = f.B, a.P = kv->B, a.Hq = f.Hq, a.rep = f.Hq / kv->Hkv;
-    a.units = (int)(kv->Hkv * tiles_of(f.B, a.rep, a.P, tile_rows));
+    a.units = (int)(f.plan.groups / f.plan.splits);
     a.splits = f.plan.splits;
     a.scale = f.sm_scale * LOG2E;
     a.kv = *kv;
@@ -1512,10 +1511,9 @@ int wq_launch_shared(wq_ctx* ctx, const WqShared& f)
         const int rc = wq_launch_decode(ctx, f.q, f.q_dtype, f.B, f.Hq, f.own, f.sm_scale, f.decode_splits, f.decode_algo, own_out, own_lse);
         if (rc != WQ_OK) return rc;
     }
-    const dim3 grid((unsigned)(a.units * a.splits));
-    void (*const kernel)(SharedArgs) = f.q_dtype == WQ_F32 ? shared_kernel<F32>(kv->hd, false) : f.q_dtype == WQ_BF16 ? shared_kernel<Bf16>(kv->hd, tile_rows == 128)
-                                                                                                              : shared_kernel<F16>(kv->hd, tile_rows == 128);
-    hipLaunchKernelGGL(kernel, grid, dim3(f.q_dtype == WQ_F32 ? 256 : 512), 0, ctx->stream, a);
+    const dim3 grid((unsigned)f.plan.groups);
+    hipLaunchKernelGGL(f.q_dtype == WQ_F32 ? shared_kernel<F32>(kv->hd) : f.q_dtype == WQ_BF16 ? shared_kernel<Bf16>(kv->hd) : shared_kernel<F16>(kv->hd), grid,
+                       dim3(f.q_dtype == WQ_F32 ? 256 : 512), 0, ctx->stream, a);
     FinishArgs m;
     m.q = a.q, m.req_off = f.req_off;
     m.P = a.P, m.Hq = f.Hq, m.rep = a.rep, m.parts = parts, m.dtype = f.q_dtype;

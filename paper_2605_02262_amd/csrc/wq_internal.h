@@ -169,6 +169,9 @@ bool wq_decode_can_append(const void* q, int q_dtype, int B, int Hq, const wq_pa
 size_t wq_decode_ws_bytes(int B, int Hq, int hd, int splits);
 size_t wq_scores_ws_bytes(int B, int64_t total_vis, int64_t total_txt, int D);
 
+// A launch has fewer than 2^32 threads: workgroups of 256
+constexpr int64_t WQ_MOST_GROUPS_256 = (int64_t(1) << 24) - 1;
+
 // ---- the operators around the cache: a call's checked arguments ------------------------------------------------------
 struct WqRope {
     const void *q, *k;
@@ -188,6 +191,7 @@ struct WqPrefillPlan {
     int rows, splits;                                             // query rows of a workgroup; parts of every row's keys
     int tail, tail_splits;                                        // with one part: so many workgroups, the last ones, are cut into so many
     size_t bytes;                                                 // workspace
+    int64_t groups;                                               // workgroups of one part
     bool few;
 };
 struct WqPrefill {
@@ -206,7 +210,9 @@ int wq_launch_prefill(wq_ctx* ctx, const WqPrefill& f);
 
 struct WqSharedPlan {
     int splits;                                                   // of the shared caches
+    int rows;                                                     // query rows of a workgroup
     bool own_decode;                                              // the requests' own caches have a decode launch of their own
+    int64_t groups;                                               // workgroups over the shared caches
     size_t decode_bytes, bytes;                                   // workspace: of that launch; in all
 };
 WqSharedPlan wq_shared_plan(int B, int P, int Hq, int Hkv, int hd, int q_dtype, int64_t max_prefix_tokens, int64_t max_own_tokens, bool own, bool own_packed,

@@ -225,8 +225,18 @@ __global__ __launch_bounds__(256) void k_rope_append(RopeArgs a, const T* __rest
 template <typename T, int HD>
 void rope(wq_ctx* ctx, const RopeArgs& a, bool pairs)
 {
-    const dim3 grid((unsigned)((a.rows + 3) / 4));
-    hipLaunchKernelGGL((pairs ? k_rope<T, HD, true> : k_rope<T, HD, false>), grid, dim3(256), 0, ctx->stream, a);
+    const int64_t most = 4 * WQ_MOST_GROUPS_256;               // rows of a launch
+    for (int64_t done = 0; done < a.rows; done += most) {
+        RopeArgs part = a;
+        for (int i = 0; i < 2; i++) {
+            if (!a.heads[i]) continue;
+            part.x[i] = static_cast<const T*>(a.x[i]) + done * a.x_stride[i];
+            part.y[i] = static_cast<T*>(a.y[i]) + done * a.y_stride[i];
+        }
+        part.positions += done;
+        part.rows = a.rows - done < most ? a.rows - done : most;
+        hipLaunchKernelGGL((pairs ? k_rope<T, HD, true> : k_rope<T, HD, false>), dim3((unsigned)((part.rows + 3) / 4)), dim3(256), 0, ctx->stream, part);
+    }
 }
 template <typename T, int HD>
 void append(wq_ctx* ctx, const RopeArgs& a, bool pairs, const void* v, int64_t v_stride, const wq_packed_kv* kv)

@@ -50,6 +50,20 @@ def test_rows(dtype, layout, rows, Hq, Hkv, hd, rot):
     assert torch.equal(q2, qo) and torch.equal(k2, ko) and torch.equal(v2, before)
 
 
+def test_more_rows_than_a_launch_takes():
+    """2^26 - 4 rows fill a launch of 2^24 - 1 workgroups; in place, one head, 8.6 GB."""
+    rows = (1 << 26) + 3
+    q = torch.zeros(rows, 1, 64, dtype=torch.float16, device="cuda")
+    q[-12:] = torch.randn(12, 1, 64, generator=torch.Generator().manual_seed(2)).half().cuda()
+    last = q[-12:].clone()
+    positions = torch.arange(rows, dtype=torch.int32, device="cuda")
+    inv_freq = torch.tensor(W.wq_rope_frequencies(64, 10000.0)[0]).cuda()
+    ctx = W.Context(0)
+    want = W.wq_rope(ctx, last, None, positions[-12:], inv_freq)[0]
+    W.wq_rope(ctx, q, None, positions, inv_freq, q_out=q)
+    assert torch.equal(q[-12:], want) and not bool(q[:1000].any()) and not bool(q[-1012:-12].any())
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("layout,rot", [(W.ROPE_HALF, 64), (W.ROPE_PAIRS, 64), (W.ROPE_HALF, 16)])
 def test_append_is_rope_then_append(dtype, layout, rot):

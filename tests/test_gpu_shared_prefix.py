@@ -105,6 +105,13 @@ def test_long_own_caches(own_len):
     _check([(64, 0, 40, 30)], [1], [tuple(x * 2048 // 3000 for x in own_len)], LARGE, 64, torch.bfloat16)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_long_own_rows_of_many_requests(dtype):
+    """Enough requests to fill the card: their own rows are walked beside the merge whatever their number."""
+    own = [(0, 0, 0, 1100 if b % 31 == 0 else b % 7) for b in range(65)]
+    _check([(64, 0, 40, 30), (0, 32, 0, 3)], [60, 5], own, (8, 4, 64), 32, dtype)
+
+
 @pytest.mark.parametrize("bits", [2, 4, 8])
 def test_values_at_the_end_of_fp16(bits):
     """A group from -65504 to 65504: the rounded scale carries its largest code past fp16's range, where the result is fp16's largest value."""

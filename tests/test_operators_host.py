@@ -87,7 +87,8 @@ def _prefill(W, ctx, **more):
     (dict(B=-1), -1), (dict(tq=-1), -1), (dict(tk=-1), -1), (dict(dtype=3), -1), (dict(hd=256), -2), (dict(Hq=15), -2), (dict(Hq=18, qs=18 * 64), -2), (dict(Hkv=0), -2),
     (dict(tq=1 << 31), -2), (dict(tk=1 << 31), -2), (dict(splits=-1), -1), (dict(splits=65), -1), (dict(sm=0.0), -1), (dict(sm=math.nan), -1), (dict(sm=math.inf), -1),
     (dict(q=None), -1), (dict(k=None), -1), (dict(v=None), -1), (dict(qo=None), -1), (dict(ko=None), -1), (dict(out=None), -1), (dict(out=P + 8), -1), (dict(q=P + 8), -1),
-    (dict(qs=100), -1), (dict(ks=132), -1), (dict(vs=64), -1), (dict(splits=64), -4), (dict(tq=1000000, splits=2), -4)])
+    (dict(qs=100), -1), (dict(ks=132), -1), (dict(vs=64), -1), (dict(splits=64), -4), (dict(tq=1000000, splits=2), -4),
+    (dict(B=5000000), -2), (dict(tq=1 << 27, Hq=1, Hkv=1, splits=2), -2)])
 def test_prefill_refuses(W, ctx, bad, code):
     assert _prefill(W, ctx, **bad) == code
     assert W.lib().wq_last_error(ctx)
