@@ -118,6 +118,22 @@ def test_a_last_round_of_tiles(dtype):
     _check([300, 4200], [300, 4200], [10, 3000], 16, 16, 64, dtype, 0, every=37)
 
 
+@pytest.mark.parametrize("new", [[300], [3], [40]])
+def test_rows_far_apart(new):
+    """Keys and values 2^22 elements from row to row: 5.9 GB, offsets of more than 32 bits."""
+    Hq, Hkv, hd, rows = 8, 2, 128, 700
+    g = torch.Generator().manual_seed(8)
+    wide = torch.empty(rows, 1 << 22, dtype=torch.float16, device="cuda")
+    n = Hkv * hd
+    wide[:, :n] = torch.randn(rows, n, generator=g).half().cuda()
+    wide[:, -n:] = torch.randn(rows, n, generator=g).half().cuda()
+    k, v = wide[:, :n].unflatten(-1, (Hkv, hd)), wide[:, -n:].unflatten(-1, (Hkv, hd))
+    q = torch.randn(sum(new), Hq, hd, generator=g).half().cuda()
+    ctx = W.Context(W.prefill_workspace_bytes(sum(new), 1, Hq, Hkv, hd, rows))
+    a = [W.wq_prefill_attention(ctx, q, x, y, R.i32(R.offsets(new)), R.i32([0, rows]), 0.09, None, rows) for x, y in ((k, v), (k.contiguous(), v.contiguous()))]
+    assert torch.equal(a[0], a[1]) and bool(a[0].isfinite().all())
+
+
 def test_steep_and_rising_logits():
     """Every key's logit above the one before (the reference moves again and again), and one key that takes all weight."""
     hd, L = 64, 400

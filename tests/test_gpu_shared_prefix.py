@@ -112,6 +112,33 @@ def test_long_own_rows_of_many_requests(dtype):
     _check([(64, 0, 40, 30), (0, 32, 0, 3)], [60, 5], own, (8, 4, 64), 32, dtype)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_a_segment_far_into_its_buffers(dtype):
+    """8-bit codes and 16-bit rows of which the last ones are used: 5.2 GB of codes, 4.3 GB of rows."""
+    heads, hd, t16 = (8, 2, 64), 64, torch.bfloat16 if dtype == torch.bfloat16 else torch.float16
+    near, _ = R.make_cache(np.random.default_rng(5), [(0, 0, 190, 77)], 2, hd, 32, t16)
+    far16, far = 1 << 24, 20480000
+    wide = W.PackedKV(1, 2, hd, 32, t16, [0, 0, far + near.cap[2]], [far16, far16 + 77])
+    wide.codes[2][:, :, far * hd:] = near.codes[2]
+    wide.meta[2][:, :, far * 2:] = near.meta[2]
+    wide.cls_off[2].copy_(near.cls_off[2] + far)
+    wide.cls_len[2].copy_(near.cls_len[2])
+    wide.k16[far16:], wide.v16[far16:] = near.k16, near.v16
+    wide.len16.copy_(near.len16)
+    q = torch.randn(3, 8, hd, generator=torch.Generator().manual_seed(1)).to(dtype).cuda()
+    own, _ = R.make_cache(np.random.default_rng(6), [(0, 0, 0, 40)], 2, hd, 32, t16)
+    ctx = W.Context(W.shared_workspace_bytes(3, 1, *heads, 300, 100))
+    req = R.i32([0, 3])
+    a = [W.wq_decode_attention_shared(ctx, q, x, req, None, 0.1, 2, 300) for x in (near, wide)]
+    assert torch.equal(a[0], a[1]) and bool(a[0].isfinite().all())
+    # ... and as a request's own rows
+    for x in (near, wide):
+        x.cls_len[2].zero_()
+        x.desc.cap[:] = [0, 0, 0]                # no room for packed tokens
+    b = [W.wq_decode_attention_shared(ctx, q[:1], own, R.i32([0, 1]), x, 0.1, 2, 300, 77) for x in (near, wide)]
+    assert torch.equal(b[0], b[1]) and bool(b[0].isfinite().all())
+
+
 @pytest.mark.parametrize("bits", [2, 4, 8])
 def test_values_at_the_end_of_fp16(bits):
     """A group from -65504 to 65504: the rounded scale carries its largest code past fp16's range, where the result is fp16's largest value."""
