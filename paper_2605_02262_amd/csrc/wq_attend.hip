@@ -1033,10 +1033,10 @@ __device__ __forceinline__ float wave_sum(float x)
 // Sum over the parts of a row, weights w (lane s: part s): HD / 4 lanes take a part's numerators, 16 bytes each, the wavefront's groups of lanes
 // every second (fourth) part, FLIGHT in flight (one after the other the loads' round trips were the whole call).  This lane's
 // channels are 4 (lane % (HD / 4)) ..; the groups' sums are still apart.
-template <int HD>
+template <int HD, int FLIGHT = 16>
 __device__ __forceinline__ f4 sum_of_parts(const float* part, int parts, float w)
 {
-    constexpr int LANES = HD / 4, GROUPS = 64 / LANES, FLIGHT = 16;
+    constexpr int LANES = HD / 4, GROUPS = 64 / LANES;
     const int lane = threadIdx.x & 63, group = lane / LANES;
     const f4* at = reinterpret_cast<const f4*>(part) + lane % LANES;
     f4 x = {0.f, 0.f, 0.f, 0.f};
@@ -1104,7 +1104,7 @@ __global__ __launch_bounds__(256) void k_merge(MergeArgs a)
     store_merged<HD>(a.out, a.dtype, row, x, M, wave_sum(l * w));
 }
 
-// The tail's tiles: a wavefront per row, 64 workgroups per tile
+// The tail's tiles: a wavefront per row, 64 workgroups per tile.  Many rows, few parts: four loads in flight, and twice the wavefronts
 template <int HD>
 __global__ __launch_bounds__(256) void k_merge_tail(PrefillArgs a, int dtype)
 {
@@ -1116,7 +1116,7 @@ __global__ __launch_bounds__(256) void k_merge_tail(PrefillArgs a, int dtype)
     const float m = lane < parts ? a.out.part_ml[(slot + lane) * 2] : -INFINITY;
     const float l = lane < parts ? a.out.part_ml[(slot + lane) * 2 + 1] : 0.f;
     const float M = wave_max(m), w = __builtin_amdgcn_exp2f(m - (M == -INFINITY ? 0.f : M));
-    const f4 x = sum_of_groups<HD>(sum_of_parts<HD>(a.out.part + slot * HD, parts, w));
+    const f4 x = sum_of_groups<HD>(sum_of_parts<HD, 4>(a.out.part + slot * HD, parts, w));
     store_merged<HD>(a.out, dtype, (p.first + row / a.rep) * a.Hq + kvh * a.rep + row % a.rep, x, M, wave_sum(l * w));
 }
 
