@@ -1399,7 +1399,7 @@ auto finish_kernel(int hd) -> void (*)(FinishArgs) { return hd == 128 ? k_shared
 // rows there -> apart, 4 KV heads: 1 request, 512 rows 41 -> 44, 1024: 46 -> 44, 2048: 54 -> 44; 16 requests, 1024: 51 -> 52, 2048: 60 -> 57;
 // 64 requests, 512: 78 -> 88, 4000: 168 -> 183.
 constexpr int64_t OWN_INSIDE = 1024;
-// Below this many keys a tail's merge costs more than its parts save
+// Below this many keys a tail's merge (15 to 20 us with its launch) costs about what its parts save (half of 32 tiles of 1.8 us, or more)
 constexpr int64_t TAIL_KEYS = 2048;
 
 }  // namespace

@@ -115,6 +115,7 @@ def test_a_last_round_of_tiles(dtype):
     _check([4400], [4400], [4400], 16, 16, 64, dtype, 0, every=37)
     _check([1300], [2500], [2000], 56, 8, 128, dtype, 0, every=11)
     _check([1300], [1000], [0], 56, 8, 128, dtype, 0, every=11)
+    _check([2800], [2800], [2800], 24, 3, 64, dtype, 0, every=53)       # (a last round that ends inside a tile's KV heads)
     _check([300, 4200], [300, 4200], [10, 3000], 16, 16, 64, dtype, 0, every=37)
 
 
