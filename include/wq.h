@@ -367,7 +367,9 @@ int wq_rope_frequencies(int rot_dim, double base, int scaling, double factor, in
 int wq_prefill_attention(wq_ctx* ctx, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int dtype,
                          int B, int Hq, int Hkv, int hd, const int32_t* q_off, const int32_t* kv_off, const int32_t* prefix_len, int64_t total_q,
                          int64_t total_kv, int64_t max_kv_rows, float sm_scale, int num_splits, void* out, float* lse);
-/* Host-only, pure: workspace of a call with these arguments. */
+/* Host-only, pure: workspace of a call with these arguments.  It does not grow with the call everywhere: a smaller one can have more parts.  With
+ * num_splits = 0 a call takes as many as the workspace has room for (one needs none behind the header), so a context for the largest call
+ * takes every smaller one too; the maximum over the calls it is for lets each have its own number. */
 size_t wq_prefill_workspace_bytes(int64_t total_q, int B, int Hq, int Hkv, int hd, int64_t max_kv_rows, int num_splits);
 
 /* ---- decode attention of requests that share packed caches -----------------------------------------------------------
@@ -387,7 +389,8 @@ size_t wq_prefill_workspace_bytes(int64_t total_q, int B, int Hq, int Hkv, int h
 int wq_decode_attention_shared(wq_ctx* ctx, const void* q, int q_dtype, int B, int Hq, const wq_packed_kv* prefix, const int32_t* req_off,
                                const wq_packed_kv* own, float sm_scale, int num_splits, int64_t max_prefix_tokens, int64_t max_own_tokens, void* out,
                                float* lse);
-/* Host-only, pure: workspace of a call with these arguments (P: sequences of the shared cache). */
+/* Host-only, pure: workspace of a call with these arguments (P: sequences of the shared cache).  As above: fewer requests can have more parts; with
+ * num_splits = 0 a call takes as many as there is room for, at least one (whose room grows with B). */
 size_t wq_shared_workspace_bytes(int B, int P, int Hq, int Hkv, int hd, int64_t max_prefix_tokens, int64_t max_own_tokens, int num_splits);
 
 #ifdef __cplusplus

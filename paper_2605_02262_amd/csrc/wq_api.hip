@@ -384,6 +384,9 @@ int wq_decode_attention(wq_ctx* ctx, const void* q, int q_dtype, int B, int Hq, 
 // ---- rotary positions, prompt attention, decode over shared caches -----------------------------------------------------
 constexpr int64_t MOST_GROUPS_512 = WQ_MOST_GROUPS_256 / 2, MOST_GROUPS_1024 = WQ_MOST_GROUPS_256 / 4;
 
+// what a context's workspace has behind its header
+static size_t room_of(const wq_ctx* ctx) { return ctx->ws && ctx->ws_bytes > WQ_WS_HEADER ? ctx->ws_bytes - WQ_WS_HEADER : 0; }
+
 static bool on_16_bytes(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
 static bool aligned_cache(const wq_packed_kv* kv)
@@ -512,7 +515,7 @@ int wq_prefill_attention(wq_ctx* ctx, const void* q, int64_t q_stride, const voi
     if (rc != WQ_OK) return rc;
     if (total_kv > 0 && (k_stride > 1 << 22 || v_stride > 1 << 22))       // (offsets inside a tile have 32 bits)
         return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "rows of k or v are more than 2^22 elements apart");
-    const WqPrefillPlan plan = wq_prefill_plan(total_q, B, Hq, Hkv, hd, dtype, max_kv_rows, prefix_len != nullptr, num_splits);
+    const WqPrefillPlan plan = wq_prefill_plan(total_q, B, Hq, Hkv, hd, dtype, max_kv_rows, prefix_len != nullptr, num_splits, room_of(ctx));
     if (plan.groups > MOST_GROUPS_512 || (plan.splits > 1 && total_q * Hq > 4 * WQ_MOST_GROUPS_256)) return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "too many rows");
     if (ctx->ws_bytes < WQ_WS_HEADER + plan.bytes || !ctx->ws)
         return wq_fail(ctx, WQ_ERR_WORKSPACE, "workspace too small for %d splits of %lld rows", plan.tail > 0 ? plan.tail_splits : plan.splits, (long long)total_q);
@@ -559,14 +562,14 @@ int wq_decode_attention_shared(wq_ctx* ctx, const void* q, int q_dtype, int B, i
     if (B == 0) return WQ_OK;
     if (!q || !out || !req_off) return wq_fail(ctx, WQ_ERR_ARG, "NULL q, out or req_off");
     const WqSharedPlan plan = wq_shared_plan(B, prefix->B, Hq, prefix->Hkv, prefix->hd, q_dtype, max_prefix_tokens, max_own_tokens, own != nullptr,
-                                             own && own->cap[0] + own->cap[1] + own->cap[2] > 0, num_splits);
+                                             own && own->cap[0] + own->cap[1] + own->cap[2] > 0, num_splits, room_of(ctx));
     if (plan.groups > MOST_GROUPS_512 || (int64_t)B * prefix->Hkv > MOST_GROUPS_1024)
         return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "too many workgroups");
     if (!ctx->ws || ctx->ws_bytes < WQ_WS_HEADER + plan.bytes)
         return wq_fail(ctx, WQ_ERR_WORKSPACE, "workspace too small for %d splits of %d requests", plan.splits, B);
     // an fp32 query's own cache in fp32 arithmetic, like its shared one
     const int algo = q_dtype == WQ_F32 ? WQ_DECODE_GENERIC : WQ_DECODE_AUTO;
-    int decode_splits = 0;
+    int decode_splits = plan.decode_splits;
     if (plan.own_decode) {
         int64_t longest = 0;
         rc = check_decode(ctx, q, q_dtype, B, Hq, own, sm_scale, &decode_splits, max_own_tokens, algo, static_cast<const float*>(out), &longest);

@@ -1404,7 +1404,7 @@ constexpr int64_t TAIL_KEYS = 2048;
 
 }  // namespace
 
-WqPrefillPlan wq_prefill_plan(int64_t total_q, int B, int Hq, int Hkv, int hd, int dtype, int64_t max_kv_rows, bool prefix, int num_splits)
+WqPrefillPlan wq_prefill_plan(int64_t total_q, int B, int Hq, int Hkv, int hd, int dtype, int64_t max_kv_rows, bool prefix, int num_splits, size_t room)
 {
     const int rep = Hq / Hkv;
     const int64_t used = total_q < B ? total_q : B;           // sequences that have rows
@@ -1429,23 +1429,42 @@ WqPrefillPlan wq_prefill_plan(int64_t total_q, int B, int Hq, int Hkv, int hd, i
             if (s.tail_splits > WQ_MAX_ATTEND_SPLITS) s.tail_splits = WQ_MAX_ATTEND_SPLITS;
         }
     }
-    s.bytes = s.tail > 0 ? partials_bytes((int64_t)s.tail * 256, hd, s.tail_splits) : s.splits > 1 ? partials_bytes(total_q * Hq, hd, s.splits) : 0;
+    auto bytes = [&]() -> size_t {
+        return s.tail > 0 ? partials_bytes((int64_t)s.tail * 256, hd, s.tail_splits) : s.splits > 1 ? partials_bytes(total_q * Hq, hd, s.splits) : 0;
+    };
+    // A smaller call can want more parts, and more room for them, than the one that the workspace was sized for: it makes do with fewer
+    if (num_splits <= 0) {
+        while (s.tail > 0 && bytes() > room)
+            if (--s.tail_splits < 2) s.tail = s.tail_splits = 0;
+        while (s.splits > 1 && bytes() > room) s.splits--;
+    }
+    s.bytes = bytes();
     return s;
 }
 
 WqSharedPlan wq_shared_plan(int B, int P, int Hq, int Hkv, int hd, int q_dtype, int64_t max_prefix_tokens, int64_t max_own_tokens, bool own, bool own_packed,
-                            int num_splits)
+                            int num_splits, size_t room)
 {
     const int rep = Hq / Hkv;
     WqSharedPlan s;
     s.rows = q_dtype == WQ_F32 ? 128 : 256;
     s.splits = num_splits > 0 ? num_splits : auto_splits_of(tiles_of(B, rep, P, s.rows) * Hkv, max_prefix_tokens, 256, q_dtype == WQ_F32 ? 32 : 64);
-    s.groups = tiles_of(B, rep, P, s.rows) * Hkv * s.splits;
     s.own_decode = own && (own_packed || (max_own_tokens > OWN_INSIDE && (int64_t)B * Hkv < 256));
     const int64_t rows = (int64_t)B * Hq;
-    s.decode_bytes = s.own_decode ? wq_decode_ws_bytes(B, Hq, hd, wq_auto_splits(B, Hkv, max_own_tokens)) : 0;
-    s.bytes = s.decode_bytes + partials_bytes(rows, hd, s.splits);
-    if (s.own_decode) s.bytes += wq_align256(rows * hd * sizeof(float)) + wq_align256(rows * sizeof(float));
+    const int decode_splits = wq_auto_splits(B, Hkv, max_own_tokens);
+    int fewer = decode_splits;
+    auto size = [&] {
+        s.decode_bytes = s.own_decode ? wq_decode_ws_bytes(B, Hq, hd, fewer) : 0;
+        s.bytes = s.decode_bytes + partials_bytes(rows, hd, s.splits);
+        if (s.own_decode) s.bytes += wq_align256(rows * hd * sizeof(float)) + wq_align256(rows * sizeof(float));
+        return s.bytes;
+    };
+    // (as for prompts; what one part and one split take grows with the requests)
+    while (num_splits <= 0 && s.splits > 1 && size() > room) s.splits--;
+    while (s.own_decode && fewer > 1 && size() > room) fewer--;
+    size();
+    s.decode_splits = fewer < decode_splits ? fewer : 0;
+    s.groups = tiles_of(B, rep, P, s.rows) * Hkv * s.splits;
     return s;
 }
 

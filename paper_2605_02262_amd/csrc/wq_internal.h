@@ -205,18 +205,21 @@ struct WqPrefill {
     void* out;
     float* lse;
 };
-WqPrefillPlan wq_prefill_plan(int64_t total_q, int B, int Hq, int Hkv, int hd, int dtype, int64_t max_kv_rows, bool prefix, int num_splits);
+// room: bytes of workspace that an automatic number of parts makes do with (no number of its own: fewer parts, or none)
+WqPrefillPlan wq_prefill_plan(int64_t total_q, int B, int Hq, int Hkv, int hd, int dtype, int64_t max_kv_rows, bool prefix, int num_splits,
+                              size_t room = SIZE_MAX);
 int wq_launch_prefill(wq_ctx* ctx, const WqPrefill& f);
 
 struct WqSharedPlan {
     int splits;                                                   // of the shared caches
     int rows;                                                     // query rows of a workgroup
     bool own_decode;                                              // the requests' own caches have a decode launch of their own
+    int decode_splits;                                            // ... with so many splits; 0 = automatic
     int64_t groups;                                               // workgroups over the shared caches
     size_t decode_bytes, bytes;                                   // workspace: of that launch; in all
 };
 WqSharedPlan wq_shared_plan(int B, int P, int Hq, int Hkv, int hd, int q_dtype, int64_t max_prefix_tokens, int64_t max_own_tokens, bool own, bool own_packed,
-                            int num_splits);
+                            int num_splits, size_t room = SIZE_MAX);
 struct WqShared {
     const void* q;
     int q_dtype, B, Hq;
@@ -224,7 +227,7 @@ struct WqShared {
     const int32_t* req_off;
     float sm_scale;
     WqSharedPlan plan;
-    int decode_splits, decode_algo;
+    int decode_splits, decode_algo;                               // of that launch, as it was checked
     void* out;
     float* lse;
 };
