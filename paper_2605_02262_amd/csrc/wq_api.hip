@@ -396,6 +396,13 @@ static bool aligned_cache(const wq_packed_kv* kv)
     return ok;
 }
 
+// The kernels take exponents of two: their scale, times log2(e), has to be finite too
+static int check_scale(wq_ctx* ctx, float sm_scale)
+{
+    if (sm_scale > 0.0f && isfinite(sm_scale * WQ_LOG2E)) return WQ_OK;
+    return wq_fail(ctx, WQ_ERR_ARG, "sm_scale must be positive, and finite times log2(e)");
+}
+
 // rows of H heads of hd elements, `stride` elements apart
 static int check_rows(wq_ctx* ctx, const char* name, const void* p, int64_t stride, int64_t rows, int H, int hd, int dtype)
 {
@@ -505,11 +512,12 @@ int wq_prefill_attention(wq_ctx* ctx, const void* q, int64_t q_stride, const voi
     if (total_q > INT32_MAX / rep || total_kv > INT32_MAX - 256 || B > INT32_MAX / 2)       // (positions and tiles' ends have 32 bits)
         return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "too many rows");
     if (num_splits < 0 || num_splits > WQ_MAX_ATTEND_SPLITS) return wq_fail(ctx, WQ_ERR_ARG, "num_splits out of range");
-    if (!(sm_scale > 0.0f) || sm_scale > 3.0e38f) return wq_fail(ctx, WQ_ERR_ARG, "sm_scale must be positive and finite");
+    int rc = check_scale(ctx, sm_scale);
+    if (rc != WQ_OK) return rc;
     if (B == 0 || total_q == 0) return WQ_OK;
     if (!q_off || !kv_off || !out) return wq_fail(ctx, WQ_ERR_ARG, "NULL table or output");
     if (!on_16_bytes(out)) return wq_fail(ctx, WQ_ERR_ARG, "out must be 16-byte aligned");
-    int rc = check_rows(ctx, "q", q, q_stride, total_q, Hq, hd, dtype);
+    rc = check_rows(ctx, "q", q, q_stride, total_q, Hq, hd, dtype);
     if (rc == WQ_OK) rc = check_rows(ctx, "k", k, k_stride, total_kv, Hkv, hd, dtype);
     if (rc == WQ_OK) rc = check_rows(ctx, "v", v, v_stride, total_kv, Hkv, hd, dtype);
     if (rc != WQ_OK) return rc;
@@ -551,7 +559,8 @@ int wq_decode_attention_shared(wq_ctx* ctx, const void* q, int q_dtype, int B, i
     if (!on_16_bytes(q) || !on_16_bytes(out)) return wq_fail(ctx, WQ_ERR_ARG, "q and out must be 16-byte aligned");
     if (!aligned_cache(prefix)) return wq_fail(ctx, WQ_ERR_ARG, "the shared cache's buffers must be 16-byte aligned");
     if (num_splits < 0 || num_splits > WQ_MAX_ATTEND_SPLITS) return wq_fail(ctx, WQ_ERR_ARG, "num_splits out of range");
-    if (!(sm_scale > 0.0f) || sm_scale > 3.0e38f) return wq_fail(ctx, WQ_ERR_ARG, "sm_scale must be positive and finite");
+    rc = check_scale(ctx, sm_scale);
+    if (rc != WQ_OK) return rc;
     if (own) {
         rc = check_packed(ctx, own, B, true);
         if (rc != WQ_OK) return rc;

@@ -27,6 +27,7 @@
 // fp32 queries take the fp32 matrix instruction throughout.  16-bit queries take the 16-bit ones: the weights are rounded to
 // the value's type (the sum of weights is not), packed keys and values to fp16 (2^-11 of a value whose own step is its
 // scale; below the output's own rounding).
+#include <float.h>
 #include <math.h>
 #include <type_traits>
 
@@ -47,7 +48,6 @@ constexpr int COLS = 2;                            // 16-row columns of a wavefr
 // fp32: four wavefronts of 32 rows, 32 keys at a time.  16-bit types: two groups of four wavefronts, 64 keys at a time.
 template <typename CT> constexpr int WAVES = std::is_same_v<CT, F32> ? 4 : 8;
 template <typename CT> constexpr int KEYS = std::is_same_v<CT, F32> ? 32 : 64;
-constexpr float LOG2E = 1.44269504088896340736f;
 // The reference of a row's exponents moves only when a logit exceeds it by 2^SLACK; weights are kept 2^SHIFT too large, so that
 // in fp16 one is lost only below 2^-34 of the largest (SHIFT + SLACK < 16).
 constexpr float SLACK = 5.f, SHIFT = 10.f;
@@ -961,7 +961,9 @@ __global__ __launch_bounds__(64 * WAVES<QT>, 2) void k_shared(SharedArgs a)
             r.limit[n] = len[c];
             r.scale[n] = a.scale;
             load_query_quarter<CT, HD>(q, n, row_at[n]);
-            if constexpr (std::is_same_v<QT, Bf16>) r.scale[n] = a.scale * query_as_f16<HD>(q, n);
+            // (kept from 0 and infinity: a masked logit, -infinity, times 0 and a logit of 0 times infinity would be NaN.  A scale that small leaves every
+            // logit below 2^-100; with one that large logits that differ at all differ by 2^70 or more)
+            if constexpr (std::is_same_v<QT, Bf16>) r.scale[n] = fminf(fmaxf(a.scale * query_as_f16<HD>(q, n), FLT_MIN), FLT_MAX);
             if constexpr (PIPED) order_query<BITS, HD>(q, n);
         }
         if constexpr (PIPED) {
@@ -1344,7 +1346,7 @@ __global__ __launch_bounds__(1024) void k_shared_finish(FinishArgs a)
         const float most = wave_max(m), w = __builtin_amdgcn_exp2f(m - (most == -INFINITY ? 0.f : most));
         x = sum_of_parts<HD>(a.out.part + row * a.parts * HD, parts, w);
         l = wave_sum(l * w);
-        if (a.own_lse && lane == W) m2 = a.own_lse[row] * LOG2E, l2 = m2 == -INFINITY ? 0.f : 1.f;
+        if (a.own_lse && lane == W) m2 = a.own_lse[row] * WQ_LOG2E, l2 = m2 == -INFINITY ? 0.f : 1.f;
         if (lane == W + 1) m2 = most, l2 = l;
     }
     __syncthreads();
@@ -1477,7 +1479,7 @@ int wq_launch_prefill(wq_ctx* ctx, const WqPrefill& f)
     a.q_off = f.q_off, a.kv_off = f.kv_off, a.prefix_len = f.prefix_len;
     a.total_q = f.total_q, a.total_kv = f.total_kv;
     a.B = f.B, a.Hq = f.Hq, a.rep = f.Hq / f.Hkv, a.splits = f.plan.splits;
-    a.scale = f.sm_scale * LOG2E;
+    a.scale = f.sm_scale * WQ_LOG2E;
     a.out.out = f.out, a.out.lse = f.lse;
     a.out.part = reinterpret_cast<float*>(ctx->ws + WQ_WS_HEADER);
     a.units = (int)f.plan.groups, a.tail = f.plan.tail, a.tail_splits = f.plan.tail_splits;
@@ -1514,7 +1516,7 @@ int wq_launch_shared(wq_ctx* ctx, const WqShared& f)
     a.B = f.B, a.P = kv->B, a.Hq = f.Hq, a.rep = f.Hq / kv->Hkv;
     a.units = (int)(f.plan.groups / f.plan.splits);
     a.splits = f.plan.splits;
-    a.scale = f.sm_scale * LOG2E;
+    a.scale = f.sm_scale * WQ_LOG2E;
     a.kv = *kv;
     a.out.out = f.out, a.out.lse = f.lse;
     const int parts = a.splits;

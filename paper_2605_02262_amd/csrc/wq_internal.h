@@ -169,6 +169,8 @@ bool wq_decode_can_append(const void* q, int q_dtype, int B, int Hq, const wq_pa
 size_t wq_decode_ws_bytes(int B, int Hq, int hd, int splits);
 size_t wq_scores_ws_bytes(int B, int64_t total_vis, int64_t total_txt, int D);
 
+constexpr float WQ_LOG2E = 1.44269504088896340736f;
+
 // A launch has fewer than 2^32 threads: workgroups of 256
 constexpr int64_t WQ_MOST_GROUPS_256 = (int64_t(1) << 24) - 1;
 

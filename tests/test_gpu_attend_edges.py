@@ -42,3 +42,43 @@ def test_shared_caches_on_a_workspace_for_a_larger_call(monkeypatch, B, largest,
         with monkeypatch.context() as m:
             m.setattr(W, "shared_workspace_bytes", lambda *a: bytes_)
             S._check([(700, 900, 400, 100)], [B], None if own is None else [own] * B, SMALL, 32, dtype)
+
+
+# ---- queries of zero, scales at the ends of fp32 --------------------------------------------------------------------------------------------------
+def _mean_of(kv_logical, heads):
+    return kv_logical[1].mean(0).repeat_interleave(heads[0] // heads[1], 0)
+
+
+@pytest.mark.parametrize("sm", [0.125, 0.125 * 2.0 ** -60, 2.0 ** -149, 2.0 ** 127])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_queries_of_zero(dtype, sm):
+    """Every key has the same logit, 0, whatever the scale: the mean of the values.  Lengths that end inside a tile."""
+    t16 = torch.bfloat16 if dtype == torch.bfloat16 else torch.float16
+    prefix, logical = R.make_cache(np.random.default_rng(0), [(50, 40, 30, 21)], 2, 64, 32, t16)
+    q = torch.zeros(2, 14, 64, dtype=dtype, device="cuda")
+    out = W.wq_decode_attention_shared(W.Context(W.shared_workspace_bytes(2, 1, *SMALL, 141)), q, prefix, R.i32([0, 2]), None, sm)
+    want = _mean_of(logical[0], SMALL)
+    # weights of one are exact; values rounded to fp16, their sum to the type, 141 additions
+    size = logical[0][1].abs().mean(0).repeat_interleave(7, 0)
+    bound = (0.0 if dtype == torch.float32 else 2.0 ** -11) * size + 160 * 2.0 ** -24 * size + R.HALF_STEP[dtype] * want.abs() + 2.0 ** -25
+    assert bool(((out.double().cpu() - want).abs() <= bound).all())
+    k, v = prefix.k16[:21], prefix.v16[:21]
+    if dtype != torch.float32:
+        for n in (1, 19):
+            o = W.wq_prefill_attention(W.Context(0), torch.zeros(n, 14, 64, dtype=dtype, device="cuda"), k, v, R.i32([0, n]), R.i32([0, 21]), sm)
+            want = torch.stack([v[:21 - n + i + 1].double().mean(0) for i in range(n)]).repeat_interleave(7, 1).cpu()
+            assert bool(((o.double().cpu() - want).abs() <= R.HALF_STEP[dtype] * want.abs() + 24 * 2.0 ** -24 * 6 + 2.0 ** -25).all())
+
+
+def test_large_bf16_queries_over_keys_of_zero():
+    """The scale that goes with a bf16 query's power of two is beyond fp32, the logits are 0."""
+    kv = W.PackedKV(1, 2, 64, 32, torch.bfloat16, [32, 64, 32], [0, 0], fill=0)
+    for c, n in enumerate((20, 64, 7)):
+        kv.cls_off[c].copy_(R.i32([0, kv.cap[c]]))
+        kv.cls_len[c].fill_(n)
+        kv.meta[c][1].fill_(int(np.float16(c + 1.0).view(np.uint16)) << 16)       # values of 1, 2, 3
+    q = torch.full((1, 14, 64), 2.0 ** 100, dtype=torch.bfloat16, device="cuda")
+    q[0, 3] = 2.0 ** 127
+    out = W.wq_decode_attention_shared(W.Context(W.shared_workspace_bytes(1, 1, *SMALL, 91)), q, kv, R.i32([0, 1]), None, 2.0 ** 30)
+    want = (20 + 2 * 64 + 3 * 7) / 91
+    assert bool(((out.double() - want).abs() <= (2.0 ** -8 + 100 * 2.0 ** -24) * want).all())
