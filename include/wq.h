@@ -353,7 +353,8 @@ int wq_rope_frequencies(int rot_dim, double base, int scaling, double factor, in
  * row i has position L - n + i.  All rows at once, a chunk behind rows that are there already, or single tokens (n = 1).
  *     out[i,h,:] = sum_j softmax_j(sm_scale * q[i,h].k_j) v_j   over the keys  j <= position  or  j < prefix_len[b]
  * prefix_len [B] (NULL: none): the sequence's first rows that every row sees (visual tokens that see each other); clipped to
- * 0 .. L.  sm_scale: positive, its product with log2(e) finite (below 2.35e38).  Head h reads KV head h/(Hq/Hkv).  A row that sees no key (n > L) becomes zeros, its lse -infinity.
+ * 0 .. L.  sm_scale: positive, its product with log2(e) finite (below 2.35e38).  Head h reads KV head h/(Hq/Hkv).  A row that sees
+ * no key (n > L) becomes zeros, its lse -infinity; one with NaN in its query becomes NaN, its lse too.
  * q [total_q, Hq, hd], k, v [total_kv, Hkv, hd], element type `dtype` for all, rows *_stride elements apart; out [total_q, Hq, hd]
  * of the same type, contiguous; rows of out and lse that belong to no sequence are left as they were.  lse [total_q, Hq]
  * fp32 or NULL.  q_off, kv_off [B+1] ascending, device; total_q, total_kv: host bounds (rows beyond them are not read).
@@ -379,7 +380,8 @@ size_t wq_prefill_workspace_bytes(int64_t total_q, int B, int Hq, int Hkv, int h
  * tokens, kept with wq_append_kv or wq_rope_append_kv; packed segments are allowed) unless own is NULL.  One softmax over both:
  *     out[b,h,:] = sum_t softmax_t(sm_scale * q[b,h].k^_t) v^_t    over the prefix of b's group and b's own cache
  * (sm_scale as for prompts).
- * A request in no group has its own cache only; with no token at all its row becomes zeros and its lse -infinity.
+ * A request in no group has its own cache only; with no token at all its row becomes zeros and its lse -infinity;
+ * with NaN in its query both become NaN.
  * q [B, Hq, hd], out [B, Hq, hd], both of type q_dtype, which pairs with the caches' dtype16 as in wq_reorder_quantize (bf16 with
  * bf16; fp16 and fp32 with fp16); lse [B, Hq] fp32 or NULL.  Both caches: the same Hkv, hd and dtype16.
  * 16-bit queries: packed keys and values are expanded to fp16 and met by fp16 weights (errors of 2^-11 relative to a value, the

@@ -766,6 +766,22 @@ __device__ __forceinline__ void order_query(Query<F16, HD>& q, int n)
     for (int st = 0; st < STEPS<F16, HD>; st++) q[n][st] = y[st];
 }
 
+template <typename QT> constexpr uint32_t EXPONENT16 = std::is_same_v<QT, Bf16> ? 0x7F80 : 0x7C00;
+// Has a row's query an entry that is not finite (all exponent bits set: one more at the lowest of them carries into the sign's place)?
+template <typename QT, int HD>
+__device__ __forceinline__ bool not_finite(const Query<F16, HD>& q, int n)
+{
+    constexpr uint32_t EXPONENT = EXPONENT16<QT> * 0x10001u, ONE = std::is_same_v<QT, Bf16> ? 0x00800080u : 0x04000400u;
+    uint32_t carry = 0;
+#pragma unroll
+    for (int st = 0; st < STEPS<F16, HD>; st++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) carry |= (q[n][st][e] & EXPONENT) + ONE;
+    carry |= __shfl_xor(carry, 16, 64);
+    carry |= __shfl_xor(carry, 32, 64);
+    return (carry & 0x80008000u) != 0;
+}
+
 // ... a bf16 query as fp16, divided by the power of two above the row's largest entry: exact down to 2^-24 of that power
 template <int HD>
 __device__ __forceinline__ float query_as_f16(Query<F16, HD>& q, int n)
@@ -788,6 +804,11 @@ __device__ __forceinline__ float query_as_f16(Query<F16, HD>& q, int n)
             q[n][st][e] = pack2(__uint_as_float(q[n][st][e] << 16) * down, __uint_as_float(q[n][st][e] & 0xFFFF0000u) * down, F16());
     return 1.0f / down;
 }
+
+// A row's sum of weights is 0 where it sees no key: zeros, and a log-sum-exp of -infinity.  It is NaN where a logit is: so are the results then
+// (a log-sum-exp of -infinity beside them would drop the row where results are merged by it).
+__device__ __forceinline__ float one_over(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }
+__device__ __forceinline__ float log_sum_exp(float ref, float sum) { return sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.69314718055994530942f; }
 
 // As one of several parts for the merge, or as the result (parts == 0).  Parts are numbered by the result's rows, or (tile_rows >= 0) by the
 // tile's from there on.
@@ -814,7 +835,7 @@ __device__ __forceinline__ void store_rows(const Rows<HD>& r, const Place& p, in
             }
             continue;
         }
-        const float inv = sum > 0.f ? 1.f / sum : 0.f;
+        const float inv = one_over(sum);
         char* to = static_cast<char*>(out.out) + at * HD * ESIZE<CT>;
 #pragma unroll
         for (int ct = 0; ct < HD / 16; ct++) {
@@ -824,7 +845,7 @@ __device__ __forceinline__ void store_rows(const Rows<HD>& r, const Place& p, in
             else
                 *reinterpret_cast<f4*>(to + (16 * ct + 4 * group) * 4) = x;
         }
-        if (out.lse && group == 0) out.lse[at] = sum > 0.f ? (ref + log2f(sum)) * 0.69314718055994530942f : -INFINITY;
+        if (out.lse && group == 0) out.lse[at] = log_sum_exp(ref, sum);
     }
 }
 
@@ -938,7 +959,10 @@ __global__ __launch_bounds__(64 * WAVES<QT>, 2) void k_shared(SharedArgs a)
     }
     const int lo = (int)((int64_t)split * all / a.splits), hi = (int)((int64_t)(split + 1) * all / a.splits);
 
-    if constexpr (PIPED) __builtin_amdgcn_s_setreg(1 | 23 << 6, 1);        // MODE.FP16_OVFL: an expanded value past fp16's range becomes its largest one
+    // MODE.FP16_OVFL: an expanded value past fp16's range becomes its largest one.  Matrix products read NaN and infinity as numbers then, too: a
+    // query that is not finite makes its row's scale NaN (below), and rows are walked without
+    constexpr int FP16_OVFL = 1 | 23 << 6;
+    if constexpr (PIPED) __builtin_amdgcn_s_setreg(FP16_OVFL, 1);
     Rows<HD> r;
     Query<CT, HD> q;
     clear(r);
@@ -961,9 +985,12 @@ __global__ __launch_bounds__(64 * WAVES<QT>, 2) void k_shared(SharedArgs a)
             r.limit[n] = len[c];
             r.scale[n] = a.scale;
             load_query_quarter<CT, HD>(q, n, row_at[n]);
+            bool bad = false;
+            if constexpr (PIPED) bad = not_finite<QT, HD>(q, n);
             // (kept from 0 and infinity: a masked logit, -infinity, times 0 and a logit of 0 times infinity would be NaN.  A scale that small leaves every
             // logit below 2^-100; with one that large logits that differ at all differ by 2^70 or more)
             if constexpr (std::is_same_v<QT, Bf16>) r.scale[n] = fminf(fmaxf(a.scale * query_as_f16<HD>(q, n), FLT_MIN), FLT_MAX);
+            if (bad) r.scale[n] = NAN;
             if constexpr (PIPED) order_query<BITS, HD>(q, n);
         }
         if constexpr (PIPED) {
@@ -992,6 +1019,7 @@ __global__ __launch_bounds__(64 * WAVES<QT>, 2) void k_shared(SharedArgs a)
     walk_class(std::integral_constant<int, 2>());
     walk_class(std::integral_constant<int, 4>());
     walk_class(std::integral_constant<int, 8>());
+    if constexpr (PIPED) __builtin_amdgcn_s_setreg(FP16_OVFL, 0);
     if (hi > done) {
         const int t0 = lo > done ? lo - done : 0, t1 = hi - done;
 #pragma unroll
@@ -1072,14 +1100,14 @@ template <int HD>
 __device__ __forceinline__ void store_merged(const Out& out, int dtype, int64_t row, f4 x, float M, float L)
 {
     const int lane = threadIdx.x & 63;
-    x *= L > 0.f ? 1.f / L : 0.f;
+    x *= one_over(L);
     if (lane < HD / 4) {
         const int64_t at = row * (HD / 4) + lane;
         if (dtype == WQ_F32) static_cast<f4*>(out.out)[at] = x;
         else if (dtype == WQ_BF16) static_cast<uint2*>(out.out)[at] = make_uint2(pack2(x[0], x[1], Bf16()), pack2(x[2], x[3], Bf16()));
         else static_cast<uint2*>(out.out)[at] = make_uint2(pack2(x[0], x[1], F16()), pack2(x[2], x[3], F16()));
     }
-    if (out.lse && lane == 0) out.lse[row] = L > 0.f ? (M + log2f(L)) * 0.69314718055994530942f : -INFINITY;
+    if (out.lse && lane == 0) out.lse[row] = log_sum_exp(M, L);
 }
 
 struct MergeArgs {
@@ -1346,7 +1374,18 @@ __global__ __launch_bounds__(1024) void k_shared_finish(FinishArgs a)
         const float most = wave_max(m), w = __builtin_amdgcn_exp2f(m - (most == -INFINITY ? 0.f : most));
         x = sum_of_parts<HD>(a.out.part + row * a.parts * HD, parts, w);
         l = wave_sum(l * w);
-        if (a.own_lse && lane == W) m2 = a.own_lse[row] * WQ_LOG2E, l2 = m2 == -INFINITY ? 0.f : 1.f;
+        if (a.own_lse) {
+            // (the decode kernels make zeros and -infinity of a query that is not finite: as if the cache were empty)
+            bool bad = false;
+#pragma unroll
+            for (int c = lane; c < HD; c += 64) {
+                const char* at = a.q + (row * HD + c) * ESIZE<QT>;
+                if constexpr (std::is_same_v<QT, F32>) bad = bad || !isfinite(*reinterpret_cast<const float*>(at));
+                else bad = bad || (*reinterpret_cast<const uint16_t*>(at) & EXPONENT16<QT>) == EXPONENT16<QT>;
+            }
+            bad = __any(bad);
+            if (lane == W) m2 = a.own_lse[row] * WQ_LOG2E, l2 = bad ? NAN : m2 == -INFINITY ? 0.f : 1.f;
+        }
         if (lane == W + 1) m2 = most, l2 = l;
     }
     __syncthreads();

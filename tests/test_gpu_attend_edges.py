@@ -82,3 +82,63 @@ def test_large_bf16_queries_over_keys_of_zero():
     out = W.wq_decode_attention_shared(W.Context(W.shared_workspace_bytes(1, 1, *SMALL, 91)), q, kv, R.i32([0, 1]), None, 2.0 ** 30)
     want = (20 + 2 * 64 + 3 * 7) / 91
     assert bool(((out.double() - want).abs() <= (2.0 ** -8 + 100 * 2.0 ** -24) * want).all())
+
+
+# ---- NaN -----------------------------------------------------------------------------------------------------------------
+def _nan_where(out, lse, hit):
+    assert torch.equal(out.isnan().all(-1), hit) and torch.equal(out.isnan().any(-1), hit), "result"
+    assert torch.equal(lse.isnan(), hit) and bool(lse[~hit].isfinite().all()), "log-sum-exp"
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("new,splits", [([90], 1), ([90], 3), ([400], 1), ([2, 1], 1), ([2, 1], 3)])
+def test_a_query_that_is_not_a_number(dtype, new, splits):
+    """Its own row becomes NaN, and so does that row's log-sum-exp: -infinity would read as "saw nothing" where results are merged by it."""
+    rows = [x + 300 for x in new]
+    q, k, v = P._case(new, rows, *SMALL, dtype, 5)
+    hit = torch.zeros(q.shape[:2], dtype=torch.bool, device="cuda")
+    n = sum(new)
+    q, hit = q[:n].clone(), hit[:n]
+    for row, head in ((0, 3), (n - 1, 13)):
+        q[row, head, 7] = math.nan
+        hit[row, head] = True
+    lse = torch.zeros(n, 14, device="cuda")
+    ctx = W.Context(W.prefill_workspace_bytes(n, len(new), *SMALL, max(rows), splits))
+    out = W.wq_prefill_attention(ctx, q, k, v, R.i32(R.offsets(new)), R.i32(R.offsets(rows)), 0.125, max_kv_rows=max(rows), num_splits=splits, lse=lse)
+    _nan_where(out, lse, hit)
+
+
+@pytest.mark.parametrize("entry", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("lens,own", [((50, 40, 30, 20), None), ((50, 0, 0, 0), (0, 0, 0, 40)), ((0, 0, 0, 0), (0, 0, 0, 40)), ((50, 0, 0, 20), (33, 0, 0, 4))])
+def test_a_request_that_is_not_a_number(dtype, lens, own, entry):
+    t16 = torch.bfloat16 if dtype == torch.bfloat16 else torch.float16
+    rng = np.random.default_rng(1)
+    prefix = R.make_cache(rng, [lens], 2, 64, 32, t16)[0]
+    mine = None if own is None else R.make_cache(rng, [own] * 3, 2, 64, 32, t16)[0]
+    q = torch.from_numpy(rng.normal(0, 1, (3, 14, 64))).to(dtype).cuda()
+    hit = torch.zeros(3, 14, dtype=torch.bool, device="cuda")
+    q[1, 5, 9], hit[1, 5] = entry, True
+    lse = torch.zeros(3, 14, device="cuda")
+    ctx = W.Context(W.shared_workspace_bytes(3, 1, *SMALL, 200, 100, 2))
+    _nan_where(W.wq_decode_attention_shared(ctx, q, prefix, R.i32([0, 3]), mine, 0.125, 2, 200, 100, lse=lse), lse, hit)
+    if own is not None and not any(own[:3]):
+        mine.desc.cap[:] = [0, 0, 0]                     # no room for packed tokens: no launch of their own
+        _nan_where(W.wq_decode_attention_shared(ctx, q, prefix, R.i32([0, 3]), mine, 0.125, 2, 200, 100, lse=lse), lse, hit)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("lens", [(0, 0, 0, 100), (50, 40, 30, 20)])
+@pytest.mark.parametrize("plane", ["k16", "v16"])
+def test_a_cached_row_that_is_not_a_number(dtype, lens, plane):
+    """A key's NaN is every row's of its KV head, a value's that of its channel."""
+    t16 = torch.bfloat16 if dtype == torch.bfloat16 else torch.float16
+    rng = np.random.default_rng(1)
+    prefix = R.make_cache(rng, [lens], 2, 64, 32, t16)[0]
+    getattr(prefix, plane)[lens[3] - 3, 1, 17] = math.nan
+    q = torch.from_numpy(rng.normal(0, 1, (3, 14, 64))).to(dtype).cuda()
+    hit = torch.zeros(3, 14, 64, dtype=torch.bool, device="cuda")
+    hit[:, 7:, slice(None) if plane == "k16" else 17] = True
+    for splits in (1, 3):
+        out = W.wq_decode_attention_shared(W.Context(W.shared_workspace_bytes(3, 1, *SMALL, 200, 0, splits)), q, prefix, R.i32([0, 3]), None, 0.125, splits, 200)
+        assert torch.equal(out.isnan(), hit)
