@@ -361,7 +361,8 @@ int wq_rope_frequencies(int rot_dim, double base, int scaling, double factor, in
  * max_kv_rows: host bound on one sequence's keys, used for the number of splits only.  num_splits: workgroups that
  * share a tile of query rows' keys, 1 .. 64, or 0 = automatic (more than one where there are few query rows; with a prefix also for
  * the tiles that would have the last round of compute units to themselves).
- * Values of the sequences' rows must be finite.  fp32: fp32 arithmetic throughout.  16-bit types: exact products, fp32 sums,
+ * Values of the sequences' rows must be finite, and small enough for fp32 sums of them with weights of up to 2^5: their magnitude times a sequence's
+ * keys below 2^122.  fp32: fp32 arithmetic throughout.  16-bit types: exact products, fp32 sums,
  * weights rounded to the type in front of their product with the values.  Pointers 16-byte aligned, rows a multiple of 16
  * bytes apart (k's and v's at most 2^22 elements); out must not overlap the inputs.  Workspace: wq_prefill_workspace_bytes
  * (WQ_ERR_WORKSPACE below it).                                                                                          */
@@ -385,7 +386,7 @@ size_t wq_prefill_workspace_bytes(int64_t total_q, int B, int Hq, int Hkv, int h
  * q [B, Hq, hd], out [B, Hq, hd], both of type q_dtype, which pairs with the caches' dtype16 as in wq_reorder_quantize (bf16 with
  * bf16; fp16 and fp32 with fp16); lse [B, Hq] fp32 or NULL.  Both caches: the same Hkv, hd and dtype16.
  * 16-bit queries: packed keys and values are expanded to fp16 and met by fp16 weights (errors of 2^-11 relative to a value, the
- * result has the query's type); a bf16 query is exact down to 2^-24 of its head's largest entry.  fp32 queries: fp32 arithmetic.
+ * result has the query's type; bf16 rows of large values: as for prompts); a bf16 query is exact down to 2^-24 of its head's largest entry.  fp32 queries: fp32 arithmetic.
  * num_splits: workgroups that share the tokens of a prefix per tile of 256 query rows (fp32: 128; a
  * request has Hq/Hkv of them), 1 .. 64, or 0 = automatic; max_prefix_tokens, max_own_tokens: host bounds on the tokens of one sequence
  * (used for splits and the choice of kernels; any value gives the same result to rounding).  q, out and the caches' buffers 16-byte aligned.  Workspace: wq_shared_workspace_bytes (max_own_tokens 0 where own is NULL).                            */

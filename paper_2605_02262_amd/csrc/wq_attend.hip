@@ -48,9 +48,11 @@ constexpr int COLS = 2;                            // 16-row columns of a wavefr
 // fp32: four wavefronts of 32 rows, 32 keys at a time.  16-bit types: two groups of four wavefronts, 64 keys at a time.
 template <typename CT> constexpr int WAVES = std::is_same_v<CT, F32> ? 4 : 8;
 template <typename CT> constexpr int KEYS = std::is_same_v<CT, F32> ? 32 : 64;
-// The reference of a row's exponents moves only when a logit exceeds it by 2^SLACK; weights are kept 2^SHIFT too large, so that
-// in fp16 one is lost only below 2^-34 of the largest (SHIFT + SLACK < 16).
-constexpr float SLACK = 5.f, SHIFT = 10.f;
+// The reference of a row's exponents moves only when a logit exceeds it by SLACK (weights of up to 2^SLACK); fp16 weights are kept 2^SHIFT too
+// large, so that one is lost only below 2^-34 of the largest (SHIFT + SLACK < 16).  Other types have the range of fp32, which their
+// values use too: their numerators are kept as small as can be.
+constexpr float SLACK = 5.f;
+template <typename CT> constexpr float SHIFT = std::is_same_v<CT, F16> ? 10.f : 0.f;
 
 template <typename CT> constexpr int ESIZE = std::is_same_v<CT, F32> ? 4 : 2;
 template <typename CT, int HD> constexpr int STEPS = HD * ESIZE<CT> / 64;          // products of a key tile: 32 (16) channels each
@@ -230,7 +232,7 @@ __device__ __forceinline__ void form_weights(Rows<HD>& r, Products<CT>& s, Weigh
     }
 #pragma unroll
     for (int n = 0; n < COLS; n++) {
-        const float shift = r.ref[n] == -INFINITY ? 0.f : SHIFT - r.ref[n];
+        const float shift = r.ref[n] == -INFINITY ? 0.f : SHIFT<CT> - r.ref[n];
 #pragma unroll
         for (int g = 0; g < T / 2; g++) {                      // 8 keys of this lane
             float w[8];
@@ -823,7 +825,7 @@ __device__ __forceinline__ void store_rows(const Rows<HD>& r, const Place& p, in
         const int row = p.row0 + (wave * COLS + n) * 16 + (lane & 15);
         if (row >= p.rows) continue;
         const int64_t at = (p.first + row / rep) * Hq + kvh * rep + row % rep;
-        const float ref = r.ref[n] - SHIFT;
+        const float ref = r.ref[n] - SHIFT<CT>;
         if (parts > 0) {
             const int64_t slot = (tile_rows < 0 ? at : tile_rows + row - p.row0) * parts + part;
             float* to = out.part + slot * HD;
@@ -1020,6 +1022,14 @@ __global__ __launch_bounds__(64 * WAVES<QT>, 2) void k_shared(SharedArgs a)
     walk_class(std::integral_constant<int, 4>());
     walk_class(std::integral_constant<int, 8>());
     if constexpr (PIPED) __builtin_amdgcn_s_setreg(FP16_OVFL, 0);
+    if constexpr (std::is_same_v<QT, Bf16>) {                  // from the packed tokens' shift to the rows', exact
+#pragma unroll
+        for (int n = 0; n < COLS; n++) {
+            r.sum[n] *= exp2f(SHIFT<QT> - SHIFT<CT>);
+#pragma unroll
+            for (int ct = 0; ct < HD / 16; ct++) r.o[ct][n] *= exp2f(SHIFT<QT> - SHIFT<CT>);
+        }
+    }
     if (hi > done) {
         const int t0 = lo > done ? lo - done : 0, t1 = hi - done;
 #pragma unroll
@@ -1207,7 +1217,7 @@ __device__ __forceinline__ void walk_few(const char* q_row, float scale, int lim
         float w[8];
 #pragma unroll
         for (int e = 0; e < 8; e++) {
-            w[e] = __builtin_amdgcn_exp2f(s[e >> 2][e & 3] - base + SHIFT);
+            w[e] = __builtin_amdgcn_exp2f(s[e >> 2][e & 3] - base + SHIFT<QT>);
             sum += w[e];
         }
         __builtin_amdgcn_s_waitcnt(0x0F70);                    // vmcnt(0): the values are in LDS
@@ -1239,7 +1249,7 @@ __device__ __forceinline__ void walk_few(const char* q_row, float scale, int lim
         asm volatile("" ::: "memory");
     }
     sum = sum_of_column(sum);
-    ref -= SHIFT;
+    ref -= SHIFT<QT>;
 }
 
 // Wavefronts' numerators [row][hd] in their pieces of LDS, references and sums beside them

@@ -142,3 +142,44 @@ def test_a_cached_row_that_is_not_a_number(dtype, lens, plane):
     for splits in (1, 3):
         out = W.wq_decode_attention_shared(W.Context(W.shared_workspace_bytes(3, 1, *SMALL, 200, 0, splits)), q, prefix, R.i32([0, 3]), None, 0.125, splits, 200)
         assert torch.equal(out.isnan(), hit)
+
+
+# ---- values beyond fp16 --------------------------------------------------------------------------------------------------
+def _large_rows(g, n, Hkv, hd, dtype):
+    return ((torch.rand(n, Hkv, hd, generator=g) + 1) * 2.0 ** 113).to(dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("new,splits", [([100], 1), ([100], 2), ([300], 1), ([1], 1), ([1], 3)])
+def test_large_values_of_a_prompt(dtype, new, splits):
+    """Values below 2^114: 400 weights of up to 2^5 each keep their sums below 2^128."""
+    rows = max(new[0], 390)
+    g = torch.Generator().manual_seed(3)
+    q, k = (torch.randn(n, h, 64, generator=g).mul(0.3).to(dtype).cuda() for n, h in ((new[0], 14), (rows, 2)))
+    v = _large_rows(g, rows, 2, 64, dtype).cuda()
+    ctx = W.Context(W.prefill_workspace_bytes(new[0], 1, *SMALL, rows, splits))
+    out = W.wq_prefill_attention(ctx, q, k, v, R.i32([0, new[0]]), R.i32([0, rows]), 0.125, max_kv_rows=rows, num_splits=splits).double().cpu()
+    want, lse, spread, terms = R.attend(q.double().cpu(), k.double().cpu(), v.double().cpu(), [rows - new[0] + i + 1 for i in range(new[0])], 0.125)
+    w = R.weights_error(rows, 64, terms, float(lse.abs().max()))
+    u = R.HALF_STEP[dtype]
+    assert bool(((out - want).abs() <= ((0.0 if dtype == torch.float32 else u) + 2 * w) * spread + u * want.abs()).all())
+
+
+@pytest.mark.parametrize("lens,own", [((0, 0, 0, 200), 0), ((40, 32, 20, 200), 0), ((40, 0, 0, 0), 150), ((0, 33, 0, 100), 150)])
+@pytest.mark.parametrize("splits", [1, 3])
+def test_large_values_of_shared_caches(lens, own, splits):
+    heads, rng, g = SMALL, np.random.default_rng(2), torch.Generator().manual_seed(4)
+    prefix, (logical,) = R.make_cache(rng, [lens], 2, 64, 32, torch.bfloat16)
+    mine, (own_logical,) = R.make_cache(rng, [(0, 0, 0, own)], 2, 64, 32, torch.bfloat16)
+    values = []
+    for kv, (k, v), n in ((prefix, logical, lens[3]), (mine, own_logical, own)):
+        kv.v16[:n] = _large_rows(g, n, 2, 64, torch.bfloat16).cuda()
+        values.append(torch.cat([v[:v.shape[0] - n], kv.v16[:n].double().cpu()]))
+    q = torch.from_numpy(rng.normal(0, 0.1, (1, 14, 64))).to(torch.bfloat16).cuda()
+    ctx = W.Context(W.shared_workspace_bytes(1, 1, *heads, sum(lens), own, splits))
+    out = W.wq_decode_attention_shared(ctx, q, prefix, R.i32([0, 1]), mine, 0.125, splits, sum(lens), own).double().cpu()
+    k = torch.cat([logical[0], own_logical[0]])
+    want, lse, spread, terms = R.attend(q.double().cpu(), k, torch.cat(values), [k.shape[0]], 0.125)
+    w = R.weights_error(k.shape[0], 64, terms, float(lse.abs().max()))
+    bound = (2 * w + 2.0 ** -8 + math.expm1(2 * 2.0 ** -11 * terms)) * spread + 2.0 ** -8 * want.abs()
+    assert bool(((out - want).abs() <= bound).all()), float(((out - want).abs() / bound).max())
