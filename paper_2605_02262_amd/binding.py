@@ -130,6 +130,7 @@ class Context:
     def __init__(self, workspace_bytes_: int, device: str = "cuda", stream: Optional[torch.cuda.Stream] = None):
         self.device = torch.device(device)
         self.ws = torch.zeros(max(int(workspace_bytes_), 16384), dtype=torch.uint8, device=self.device)
+        self.index = self.ws.get_device()
         self.handle = C.c_void_p()
         st = (stream or torch.cuda.current_stream(self.device)).cuda_stream
         rc = lib().wq_create(C.byref(self.handle), C.c_void_p(st), self.ws.data_ptr(), self.ws.numel())
@@ -342,6 +343,13 @@ def _rows(name: str, t: torch.Tensor, like: Optional[torch.Tensor] = None, shape
     return rows, heads, hd, max(row, heads * hd) if rows <= 1 else row
 
 
+def _here(ctx: Context, *tensors: Optional[torch.Tensor]):
+    """Every tensor on the context's device: a kernel given a host pointer would fault."""
+    for t in tensors:
+        if t is not None and t.get_device() != ctx.index:
+            raise ValueError(f"a tensor of shape {tuple(t.shape)} on {t.device}: the context's device, cuda:{ctx.index}, expected")
+
+
 def _like(t: torch.Tensor) -> torch.Tensor:
     return torch.empty_like(t, memory_format=torch.contiguous_format)
 
@@ -363,6 +371,7 @@ def wq_rope_frequencies(rot_dim: int, base: float, scaling: int = ROPE_PLAIN, fa
 def wq_rope(ctx: Context, q, k, positions, inv_freq, layout: int = ROPE_HALF, mscale: float = 1.0, q_out: Optional[torch.Tensor] = None,
             k_out: Optional[torch.Tensor] = None):
     """Turns q [rows, Hq, hd] and k [rows, Hkv, hd] (or None); 2 * inv_freq.numel() channels of every head."""
+    _here(ctx, q, k, positions, inv_freq, q_out, k_out)
     rows, Hq, hd, qs = _rows("q", q)
     _contiguous("positions", positions, torch.int32, rows)
     half = inv_freq.numel()
@@ -388,6 +397,7 @@ def wq_rope(ctx: Context, q, k, positions, inv_freq, layout: int = ROPE_HALF, ms
 def wq_rope_append_kv(ctx: Context, q, k, v, positions, inv_freq, kv: PackedKV, layout: int = ROPE_HALF, mscale: float = 1.0,
                       q_out: Optional[torch.Tensor] = None):
     """Turns q [B, Hq, hd] (returned) and k [B, Hkv, hd]; k and v become the cache's next rows."""
+    _here(ctx, q, k, v, positions, inv_freq, q_out, kv.off16)
     B, Hq, hd, qs = _rows("q", q)
     shape = (B, kv.Hkv, kv.hd)
     if hd != kv.hd:
@@ -412,6 +422,7 @@ def prefill_workspace_bytes(total_q: int, B: int, Hq: int, Hkv: int, hd: int, ma
 def wq_prefill_attention(ctx: Context, q, k, v, q_off, kv_off, sm_scale: float, prefix_len: Optional[torch.Tensor] = None, max_kv_rows: int = 0,
                          num_splits: int = 0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None):
     """q [total_q, Hq, hd] over k, v [total_kv, Hkv, hd]; q_off, kv_off [B+1], prefix_len [B] int32."""
+    _here(ctx, q, k, v, q_off, kv_off, prefix_len, out, lse)
     total_q, Hq, hd, qs = _rows("q", q)
     total_kv, Hkv, k_hd, ks = _rows("k", k, q)
     if k_hd != hd:
@@ -441,6 +452,7 @@ def wq_decode_attention_shared(ctx: Context, q, prefix: PackedKV, req_off, own: 
                                max_prefix_tokens: int = 0, max_own_tokens: int = 0, out: Optional[torch.Tensor] = None,
                                lse: Optional[torch.Tensor] = None):
     """q [B, Hq, hd]; requests req_off[p] .. req_off[p+1]-1 share sequence p of prefix, request b has sequence b of own (or None)."""
+    _here(ctx, q, req_off, out, lse, prefix.off16, None if own is None else own.off16)
     B, Hq, hd = q.shape
     if hd != prefix.hd:
         raise ValueError("q: the head_dim of the cache expected")

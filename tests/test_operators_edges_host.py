@@ -1,7 +1,9 @@
 """More refusals of the operators around the cache, none of which needs a GPU."""
 import ctypes as C
+from types import SimpleNamespace
 
 import pytest
+import torch
 
 from tests.test_operators_host import BF, P, W, _desc, _prefill, _rope, ctx  # noqa: F401
 
@@ -18,3 +20,19 @@ def test_scales_at_the_ends_of_fp32(W, ctx, sm, code):  # noqa: F811
     """Exponents are powers of two: the scale times log2(e) has to be finite.  (-4: accepted, and then too little workspace.)"""
     assert _prefill(W, ctx, sm=sm, tq=1000000, splits=2) == code
     assert _shared(W, ctx, _desc(W), sm=sm, B=1000, splits=64) == code
+
+
+def test_binding_refuses_tensors_on_another_device(W):  # noqa: F811
+    """A host pointer in a table would fault in the kernel; refused before the library sees it."""
+    ctx = SimpleNamespace(index=0, handle=None)         # noqa: F811  (a context of cuda:0; these tensors are the host's)
+    q, k, i, f = torch.zeros(2, 14, 64), torch.zeros(2, 2, 64), torch.zeros(2, dtype=torch.int32), torch.zeros(32)
+    kv = W.PackedKV(2, 2, 64, 32, torch.float16, [0, 0, 0], [0, 4, 8], device="cpu")
+    there = torch.empty(0, device="meta")               # (no device's either: any one tensor is enough)
+    for call in (lambda: W.wq_rope(ctx, q, k, i, f), lambda: W.wq_rope(ctx, q, None, i, f), lambda: W.wq_rope_append_kv(ctx, q, k, k, i, f, kv),
+                 lambda: W.wq_prefill_attention(ctx, q, k, k, i, i, 0.125), lambda: W.wq_decode_attention_shared(ctx, q, kv, i, None, 0.125)):
+        with pytest.raises(ValueError, match="device"):
+            call()
+    here = SimpleNamespace(get_device=lambda: 0)
+    W._here(ctx, here, None, here)
+    with pytest.raises(ValueError, match="device"):
+        W._here(ctx, here, None, there)
