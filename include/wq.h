@@ -364,7 +364,7 @@ int wq_rope_frequencies(int rot_dim, double base, int scaling, double factor, in
  * Values of the sequences' rows must be finite, and small enough for fp32 sums of them with weights of up to 2^5: their magnitude times a sequence's
  * keys below 2^122.  fp32: fp32 arithmetic throughout.  16-bit types: exact products, fp32 sums,
  * weights rounded to the type in front of their product with the values.  Pointers 16-byte aligned, rows a multiple of 16
- * bytes apart (k's and v's at most 2^22 elements); out must not overlap the inputs.  Workspace: wq_prefill_workspace_bytes
+ * bytes apart (k's and v's at most 2^22 elements); at most 2^18 query heads; out must not overlap the inputs.  Workspace: wq_prefill_workspace_bytes
  * (WQ_ERR_WORKSPACE below it).                                                                                          */
 int wq_prefill_attention(wq_ctx* ctx, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int dtype,
                          int B, int Hq, int Hkv, int hd, const int32_t* q_off, const int32_t* kv_off, const int32_t* prefix_len, int64_t total_q,
@@ -389,7 +389,7 @@ size_t wq_prefill_workspace_bytes(int64_t total_q, int B, int Hq, int Hkv, int h
  * result has the query's type; bf16 rows of large values: as for prompts); a bf16 query is exact down to 2^-24 of its head's largest entry.  fp32 queries: fp32 arithmetic.
  * num_splits: workgroups that share the tokens of a prefix per tile of 256 query rows (fp32: 128; a
  * request has Hq/Hkv of them), 1 .. 64, or 0 = automatic; max_prefix_tokens, max_own_tokens: host bounds on the tokens of one sequence
- * (used for splits and the choice of kernels; any value gives the same result to rounding).  q, out and the caches' buffers 16-byte aligned.  Workspace: wq_shared_workspace_bytes (max_own_tokens 0 where own is NULL).                            */
+ * (used for splits and the choice of kernels; any value gives the same result to rounding).  At most 2^18 query heads; q, out and the caches' buffers 16-byte aligned.  Workspace: wq_shared_workspace_bytes (max_own_tokens 0 where own is NULL).                            */
 int wq_decode_attention_shared(wq_ctx* ctx, const void* q, int q_dtype, int B, int Hq, const wq_packed_kv* prefix, const int32_t* req_off,
                                const wq_packed_kv* own, float sm_scale, int num_splits, int64_t max_prefix_tokens, int64_t max_own_tokens, void* out,
                                float* lse);

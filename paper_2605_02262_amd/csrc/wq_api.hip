@@ -384,6 +384,9 @@ int wq_decode_attention(wq_ctx* ctx, const void* q, int q_dtype, int B, int Hq, 
 // ---- rotary positions, prompt attention, decode over shared caches -----------------------------------------------------
 constexpr int64_t MOST_GROUPS_512 = WQ_MOST_GROUPS_256 / 2, MOST_GROUPS_1024 = WQ_MOST_GROUPS_256 / 4;
 
+// (offsets of a head inside a row, and of a row inside a tile of 64 with as many KV heads, have 32 bits)
+constexpr int MOST_HEADS = 1 << 18;
+
 // what a context's workspace has behind its header
 static size_t room_of(const wq_ctx* ctx) { return ctx->ws && ctx->ws_bytes > WQ_WS_HEADER ? ctx->ws_bytes - WQ_WS_HEADER : 0; }
 
@@ -508,6 +511,7 @@ int wq_prefill_attention(wq_ctx* ctx, const void* q, int64_t q_stride, const voi
     if (hd != 64 && hd != 128) return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "unsupported head dimension %d", hd);
     if (Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || Hq / Hkv > WQ_MAX_REP)
         return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "Hq=%d must be a multiple of Hkv=%d, at most %d query heads per KV head", Hq, Hkv, WQ_MAX_REP);
+    if (Hq > MOST_HEADS) return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "more than 2^18 heads");
     const int rep = Hq / Hkv;
     if (total_q > INT32_MAX / rep || total_kv > INT32_MAX - 256 || B > INT32_MAX / 2)       // (positions and tiles' ends have 32 bits)
         return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "too many rows");
@@ -554,6 +558,7 @@ int wq_decode_attention_shared(wq_ctx* ctx, const void* q, int q_dtype, int B, i
     if (prefix->B > 65535) return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "more than 65535 shared sequences in one call");
     if (Hq % prefix->Hkv != 0 || Hq / prefix->Hkv > WQ_MAX_REP)
         return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "Hq=%d must be a multiple of Hkv=%d, at most %d query heads per KV head", Hq, prefix->Hkv, WQ_MAX_REP);
+    if (Hq > MOST_HEADS) return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "more than 2^18 heads");
     if ((q_dtype == WQ_BF16) != (prefix->dtype16 == WQ_BF16))
         return wq_fail(ctx, WQ_ERR_ARG, "dtype16 must be bf16 for bf16 queries and fp16 for fp16/fp32 queries");
     if (!on_16_bytes(q) || !on_16_bytes(out)) return wq_fail(ctx, WQ_ERR_ARG, "q and out must be 16-byte aligned");

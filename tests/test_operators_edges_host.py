@@ -36,3 +36,14 @@ def test_binding_refuses_tensors_on_another_device(W):  # noqa: F811
     W._here(ctx, here, None, here)
     with pytest.raises(ValueError, match="device"):
         W._here(ctx, here, None, there)
+
+
+def test_more_heads_than_an_offset_of_32_bits_reaches(W, ctx):  # noqa: F811
+    """2^22 fp32 heads of 128: a head lies 2^31 bytes into its row; 2^19 KV heads: a row 2^32 bytes into its tile."""
+    many = 1 << 22
+    assert _prefill(W, ctx, dtype=0, hd=128, Hq=many, Hkv=many // 8, qs=many * 128, tq=1, tk=0, mk=0, B=1) == -2
+    assert b"heads" in W.lib().wq_last_error(ctx)
+    assert _shared(W, ctx, _desc(W, B=1, Hkv=1 << 19, hd=128, group=64), B=1, Hq=1 << 19) == -2
+    assert b"heads" in W.lib().wq_last_error(ctx)
+    # (as many as allowed: what is missing is workspace)
+    assert _shared(W, ctx, _desc(W, B=1, Hkv=1 << 18, hd=128, group=64), B=1, Hq=1 << 18, splits=64) == -4
