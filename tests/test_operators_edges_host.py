@@ -45,5 +45,7 @@ def test_more_heads_than_an_offset_of_32_bits_reaches(W, ctx):  # noqa: F811
     assert b"heads" in W.lib().wq_last_error(ctx)
     assert _shared(W, ctx, _desc(W, B=1, Hkv=1 << 19, hd=128, group=64), B=1, Hq=1 << 19) == -2
     assert b"heads" in W.lib().wq_last_error(ctx)
-    # (as many as allowed: what is missing is workspace)
-    assert _shared(W, ctx, _desc(W, B=1, Hkv=1 << 18, hd=128, group=64), B=1, Hq=1 << 18, splits=64) == -4
+    # (as many as allowed: 64 parts of each are 2^24 workgroups, past a launch's 2^32 threads; with 4 what is missing is workspace)
+    assert _shared(W, ctx, _desc(W, B=1, Hkv=1 << 18, hd=128, group=64), B=1, Hq=1 << 18, splits=64) == -2
+    assert b"workgroups" in W.lib().wq_last_error(ctx)
+    assert _shared(W, ctx, _desc(W, B=1, Hkv=1 << 18, hd=128, group=64), B=1, Hq=1 << 18, splits=4) == -4
