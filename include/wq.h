@@ -343,7 +343,7 @@ int wq_rope_append_kv(wq_ctx* ctx, const void* q, int64_t q_stride, const void* 
  *   WQ_ROPE_PARTS  (1 - g) f_i/factor + g f_i,  g = clamp((r - 1)/(32 - 1), 0, 1),  r = trained_context f_i / 2 pi the turns that a
  *                  pair makes over the context the model was trained with;  mscale = 0.1 ln(factor) + 1   (1 otherwise)
  * Evaluated in double.  A model that was trained with another rule brings its own table.  WQ_ERR_ARG on NULL, a rot_dim that is not
- * a positive multiple of 16, base <= 1, factor < 1, an unknown rule, trained_context <= 0 with WQ_ROPE_PARTS.            */
+ * a positive multiple of 16, base <= 1, factor < 1, a stretched base beyond double's range, an unknown rule, trained_context <= 0 with WQ_ROPE_PARTS.            */
 int wq_rope_frequencies(int rot_dim, double base, int scaling, double factor, int64_t trained_context, float* inv_freq, float* mscale);
 
 /* ---- attention of a prompt's rows ------------------------------------------------------------------------------------

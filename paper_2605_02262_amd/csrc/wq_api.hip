@@ -479,6 +479,7 @@ int wq_rope_frequencies(int rot_dim, double base, int scaling, double factor, in
     if (scaling != WQ_ROPE_PLAIN && !(isfinite(factor) && factor >= 1.0)) return WQ_ERR_ARG;
     if (scaling == WQ_ROPE_PARTS && trained_context <= 0) return WQ_ERR_ARG;
     if (scaling == WQ_ROPE_BASE) base *= pow(factor, (double)rot_dim / (rot_dim - 2));
+    if (!isfinite(base)) return WQ_ERR_ARG;                    // (would turn every pair but the first by nothing)
     for (int i = 0; i < rot_dim / 2; i++) {
         double f = pow(base, -2.0 * i / rot_dim);
         if (scaling == WQ_ROPE_EVEN) f /= factor;

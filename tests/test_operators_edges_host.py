@@ -49,3 +49,11 @@ def test_more_heads_than_an_offset_of_32_bits_reaches(W, ctx):  # noqa: F811
     assert _shared(W, ctx, _desc(W, B=1, Hkv=1 << 18, hd=128, group=64), B=1, Hq=1 << 18, splits=64) == -2
     assert b"workgroups" in W.lib().wq_last_error(ctx)
     assert _shared(W, ctx, _desc(W, B=1, Hkv=1 << 18, hd=128, group=64), B=1, Hq=1 << 18, splits=4) == -4
+
+
+def test_frequencies_of_a_base_out_of_range(W):  # noqa: F811
+    """10^200 stretched by 10^150^(32/30) has no place in a double; just below it has."""
+    with pytest.raises(W.WQError):
+        W.wq_rope_frequencies(32, 1e200, W.ROPE_BASE, 1e150)
+    f = W.wq_rope_frequencies(32, 1e200, W.ROPE_BASE, 1e90)[0]           # 10^(200 + 96)
+    assert all(abs(x - 10.0 ** (-296 * i / 16)) <= 2.0 ** -24 * x + 2.0 ** -149 for i, x in enumerate(f))
