@@ -183,3 +183,73 @@ def test_large_values_of_shared_caches(lens, own, splits):
     w = R.weights_error(k.shape[0], 64, terms, float(lse.abs().max()))
     bound = (2 * w + 2.0 ** -8 + math.expm1(2 * 2.0 ** -11 * terms)) * spread + 2.0 ** -8 * want.abs()
     assert bool(((out - want).abs() <= bound).all()), float(((out - want).abs() / bound).max())
+
+
+# ---- what 16-bit roundings cost -----------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", DTYPES[:2])
+@pytest.mark.parametrize("heads,group", [(SMALL, 32), (LARGE, 64)])
+@pytest.mark.parametrize("spread_q", [1.0, 2.0 ** 4])
+def test_accuracy_of_16_bit_requests(dtype, heads, group, spread_q):
+    """Logits of deviation 3, and of 48 (a peaked softmax whose reference moves).  Roundings are independent, each off by at most half a step (its
+    square a third of that squared on the average): of the result; of a weight (fp16 for packed tokens, the rows' type for theirs); of a packed
+    key's and value's expansion to fp16.  The sum of weights is not rounded, so a weight's rounding acts through its value, a key's through the
+    difference from the result.  No element beyond the worst case of all of them, their common size not beyond the mean of the squares."""
+    Hq, Hkv, hd = heads
+    rng = np.random.default_rng(7)
+    lens, own_lens, B, sm, r = (300, 200, 150, 60), (0, 0, 0, 25), 4, 1.0 / math.sqrt(hd), 2.0 ** -11
+    prefix, (shared,) = R.make_cache(rng, [lens], Hkv, hd, group, dtype)
+    own, mine = R.make_cache(rng, [own_lens] * B, Hkv, hd, group, dtype)
+    q = torch.from_numpy(rng.normal(0, 1.3 * spread_q, (B, Hq, hd))).to(dtype).cuda()
+    longest = sum(lens)
+    ctx = W.Context(W.shared_workspace_bytes(B, 1, *heads, longest, 25))
+    lse = torch.empty(B, Hq, device="cuda")
+    out = W.wq_decode_attention_shared(ctx, q, prefix, R.i32([0, B]), own, sm, 0, longest, 25, lse=lse)
+    again = W.wq_decode_attention_shared(ctx, q, prefix, R.i32([0, B]), own, sm, 0, longest, 25)
+    assert torch.equal(again, out), "two calls differ"
+    u = R.HALF_STEP[dtype]
+    packed = torch.zeros(longest + 25, dtype=torch.float64)
+    packed[:sum(lens[:3])] = 1.0
+    off_weight = torch.where(packed > 0, r, u)
+    got_all = expected_all = 0.0
+    for b in range(B):
+        k, v = torch.cat([shared[0], mine[b][0]]), torch.cat([shared[1], mine[b][1]])
+        qb = q[b].double().cpu()
+        want, want_lse, spread, terms = R.attend(qb[None], k, v, [k.shape[0]], sm)
+        want, spread = want[0], spread[0]
+        err = (out[b].double().cpu() - want).abs()
+        w, tiny = R.weights_error(k.shape[0], hd, terms, float(want_lse.abs().max())), 2.0 ** -25 if dtype == torch.float16 else 0.0
+        bound = (math.expm1(2 * r * terms) + 2 * w + u + r) * spread + u * want.abs() + tiny
+        assert bool((err <= bound).all()), float((err / bound).max())
+        assert bool(((lse[b].double().cpu() - want_lse[0]).abs() <= r * terms + 2 * w + 2.0 ** -22 * want_lse[0].abs()).all())
+        for h in range(Hq):
+            kh, vh = k[:, h // (Hq // Hkv)], v[:, h // (Hq // Hkv)]
+            terms_of = qb[h] * kh * sm
+            p = torch.softmax(terms_of.sum(1), 0)
+            logit = r * r / 3 * packed * terms_of.square().sum(1)
+            var = (u * want[h]).square() / 3 + (p.square()[:, None] * (((off_weight.square() + packed * r * r) / 3)[:, None] * vh.square()
+                                                                          + logit[:, None] * (vh - want[h]).square())).sum(0)
+            expected_all += float(var.sum())
+        got_all += float(err.square().sum())
+    assert got_all <= expected_all, math.sqrt(got_all / expected_all)
+
+
+@pytest.mark.parametrize("dtype", DTYPES[:2])
+@pytest.mark.parametrize("new,rows,splits", [(130, 600, 1), (9, 600, 3), (2, 600, 1)])
+def test_accuracy_of_prompts(dtype, new, rows, splits):
+    """As above, with the two roundings that there are: of a weight and of the result."""
+    Hq, Hkv, hd = LARGE
+    q, k, v = P._case([new], [rows], *LARGE, dtype, 11)
+    q = q[:new]
+    ctx = W.Context(W.prefill_workspace_bytes(new, 1, *LARGE, rows, splits))
+    out = W.wq_prefill_attention(ctx, q, k, v, R.i32([0, new]), R.i32([0, rows]), 1 / math.sqrt(hd), max_kv_rows=rows, num_splits=splits).double().cpu()
+    qd, kd, vd = q.double().cpu(), k[:rows].double().cpu(), v[:rows].double().cpu()
+    limit = [rows - new + i + 1 for i in range(new)]
+    want = R.attend(qd, kd, vd, limit, 1 / math.sqrt(hd))[0]
+    u = R.HALF_STEP[dtype]
+    expected = (u * want).square().sum() / 3
+    hidden = torch.arange(rows)[None] >= torch.tensor(limit)[:, None]
+    for h in range(Hq):
+        s = qd[:, h] @ kd[:, h // (Hq // Hkv)].T / math.sqrt(hd)
+        p = torch.softmax(s.masked_fill(hidden, -math.inf), 1)
+        expected += (p.square() @ vd[:, h // (Hq // Hkv)].square()).sum() * u * u / 3
+    assert float((out - want).square().sum()) <= float(expected), math.sqrt(float((out - want).square().sum() / expected))
