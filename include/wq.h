@@ -358,9 +358,11 @@ int wq_rope_frequencies(int rot_dim, double base, int scaling, double factor, in
  * q [total_q, Hq, hd], k, v [total_kv, Hkv, hd], element type `dtype` for all, rows *_stride elements apart; out [total_q, Hq, hd]
  * of the same type, contiguous; rows of out and lse that belong to no sequence are left as they were.  lse [total_q, Hq]
  * fp32 or NULL.  q_off, kv_off [B+1] ascending, device; total_q, total_kv: host bounds (rows beyond them are not read).
- * max_kv_rows: host bound on one sequence's keys, used for the number of splits only.  num_splits: workgroups that
+ * max_kv_rows: host bound on one sequence's keys, used for the number of splits only (0 reads as few keys, one part: 61 rows behind 12544 take 344 us
+ * instead of 35).  num_splits: workgroups that
  * share a tile of query rows' keys, 1 .. 64, or 0 = automatic (more than one where there are few query rows; with a prefix also for
- * the tiles that would have the last round of compute units to themselves).
+ * the tiles that would have the last round of compute units to themselves).  Kernel, tiles and parts are chosen once, from the batch's averages: long
+ * prompts and many single tokens cost less as two calls (4000 rows and 200 tokens behind 6400 rows, 28/4 heads of 128: 1085 us, apart 146 + 537).
  * Values of the sequences' rows must be finite, and small enough for fp32 sums of them with weights of up to 2^5: their magnitude times a sequence's
  * keys below 2^122.  fp32: fp32 arithmetic throughout.  16-bit types: exact products, fp32 sums,
  * weights rounded to the type in front of their product with the values.  Pointers 16-byte aligned, rows a multiple of 16
@@ -386,10 +388,11 @@ size_t wq_prefill_workspace_bytes(int64_t total_q, int B, int Hq, int Hkv, int h
  * q [B, Hq, hd], out [B, Hq, hd], both of type q_dtype, which pairs with the caches' dtype16 as in wq_reorder_quantize (bf16 with
  * bf16; fp16 and fp32 with fp16); lse [B, Hq] fp32 or NULL.  Both caches: the same Hkv, hd and dtype16.
  * 16-bit queries: packed keys and values are expanded to fp16 and met by fp16 weights (errors of 2^-11 relative to a value, the
- * result has the query's type; bf16 rows of large values: as for prompts); a bf16 query is exact down to 2^-24 of its head's largest entry.  fp32 queries: fp32 arithmetic.
+ * result has the query's type; bf16 rows of large values: as for prompts); a bf16 query's entries are exact from 2^-17 of the power of two above its
+ * head's largest one up, below that off by at most 2^-25 of that power.  fp32 queries: fp32 arithmetic.
  * num_splits: workgroups that share the tokens of a prefix per tile of 256 query rows (fp32: 128; a
  * request has Hq/Hkv of them), 1 .. 64, or 0 = automatic; max_prefix_tokens, max_own_tokens: host bounds on the tokens of one sequence
- * (used for splits and the choice of kernels; any value gives the same result to rounding).  At most 2^18 query heads; q, out and the caches' buffers 16-byte aligned.  Workspace: wq_shared_workspace_bytes (max_own_tokens 0 where own is NULL).                            */
+ * (used for splits and the choice of kernels; any value gives the same result to rounding, max_prefix_tokens 0 in one part).  At most 2^18 query heads; q, out and the caches' buffers 16-byte aligned.  Workspace: wq_shared_workspace_bytes (max_own_tokens 0 where own is NULL).                            */
 int wq_decode_attention_shared(wq_ctx* ctx, const void* q, int q_dtype, int B, int Hq, const wq_packed_kv* prefix, const int32_t* req_off,
                                const wq_packed_kv* own, float sm_scale, int num_splits, int64_t max_prefix_tokens, int64_t max_own_tokens, void* out,
                                float* lse);

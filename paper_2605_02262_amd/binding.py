@@ -421,7 +421,7 @@ def prefill_workspace_bytes(total_q: int, B: int, Hq: int, Hkv: int, hd: int, ma
 
 def wq_prefill_attention(ctx: Context, q, k, v, q_off, kv_off, sm_scale: float, prefix_len: Optional[torch.Tensor] = None, max_kv_rows: int = 0,
                          num_splits: int = 0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None):
-    """q [total_q, Hq, hd] over k, v [total_kv, Hkv, hd]; q_off, kv_off [B+1], prefix_len [B] int32."""
+    """q [total_q, Hq, hd] over k, v [total_kv, Hkv, hd]; q_off, kv_off [B+1], prefix_len [B] int32.  max_kv_rows 0: few rows get one part."""
     _here(ctx, q, k, v, q_off, kv_off, prefix_len, out, lse)
     total_q, Hq, hd, qs = _rows("q", q)
     total_kv, Hkv, k_hd, ks = _rows("k", k, q)
@@ -451,7 +451,8 @@ def shared_workspace_bytes(B: int, P: int, Hq: int, Hkv: int, hd: int, max_prefi
 def wq_decode_attention_shared(ctx: Context, q, prefix: PackedKV, req_off, own: Optional[PackedKV], sm_scale: float, num_splits: int = 0,
                                max_prefix_tokens: int = 0, max_own_tokens: int = 0, out: Optional[torch.Tensor] = None,
                                lse: Optional[torch.Tensor] = None):
-    """q [B, Hq, hd]; requests req_off[p] .. req_off[p+1]-1 share sequence p of prefix, request b has sequence b of own (or None)."""
+    """q [B, Hq, hd]; requests req_off[p] .. req_off[p+1]-1 share sequence p of prefix, request b has sequence b of own (or None).
+    max_prefix_tokens 0: one part."""
     _here(ctx, q, req_off, out, lse, prefix.off16, None if own is None else own.off16)
     B, Hq, hd = q.shape
     if hd != prefix.hd:

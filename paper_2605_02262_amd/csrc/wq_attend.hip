@@ -17,10 +17,12 @@
 // Packed tiles lie in LDS in the operands' own order, [step][lane][16 bytes]: every LDS read of the products is one conflict-free 16-byte
 // load per lane.  Plain rows lie as they came, their 16-byte pieces exchanged by row.
 //
-// What bounds it (28 query heads, 4 KV heads of 128, bf16, one MI355X): the vector unit.  A tile of 64 keys takes a wavefront 64 matrix
+// What bounds it (28 query heads, 4 KV heads of 128, bf16, one MI355X): the phases of vector instructions.  A tile of 64 keys takes a wavefront 64 matrix
 // instructions, 1150 cycles, and 1200 to 1450 cycles of exponents, sums and conversions; the two groups' phases together are 3740
-// cycles.  12800 query rows over as many keys: 1.95 ms = 1.18 PFLOP/s, where a library product of 8192^3 reaches 1.37.  A packed tile also has to be
-// expanded, 16384 codes: 4900 cycles; 50 700 packed tokens under 64 requests (448 rows per KV head): 72 us = 0.65 PFLOP/s.
+// cycles (matrix cores busy 57 % of them, vector unit active 60 %).  12800 query rows over as many keys: 1.95 ms = 1.18 PFLOP/s with a prefix of 98 %,
+// 1.04 ms = 1.13 causal, where a library product of 8192^3 reaches 1.37.  A packed tile also has to be expanded, 16384 codes, 4900 cycles, and the phase in
+// which group 1 forms weights and expands values is the longest: neither unit is full (33 %, 48 %), but that wavefront's instructions follow each
+// other.  50 700 packed tokens under 64 requests (448 rows per KV head): 72 us of a call's 85 in a series = 0.65 PFLOP/s (81 traced by itself).
 // A lone wavefront issues one vector instruction in 6 cycles, two on a SIMD one in 2.7: more of them do not fit the registers.
 // Short walks cost what they cannot overlap: 2 us from the launch to the first load, 2 until its first product, 2 for the result.
 //
@@ -274,7 +276,7 @@ __device__ __forceinline__ void attend_f32(Rows<HD>& r, const Query<F32, HD>& q,
 //   phase 2i + 1  group 0: weights of tile i                                      group 1: products of tile i
 // A tile's keys and values are read in two neighbouring phases, so two tiles of each in LDS are enough.  Expanding packed keys fills the vector
 // slots behind the products (with the weights in the next phase: 88 us instead of 86 for the 50 700 tokens above).  Plain rows need no
-// wavefront's time: group 1 sends for values and the next keys.  The group that multiplies has priority (64 frames 2110 -> 2080 us).
+// wavefront's time: group 1 sends for values and the next keys.  The group that multiplies has priority (64 frames 2110 -> 2050 us).
 // SPLIT: up to 128 rows, all group 0's; group 1 brings it keys and values.
 // A barrier for what is in LDS: loads into registers stay in flight across it (__syncthreads() waits for them)
 __device__ __forceinline__ void meet()
@@ -784,7 +786,8 @@ __device__ __forceinline__ bool not_finite(const Query<F16, HD>& q, int n)
     return (carry & 0x80008000u) != 0;
 }
 
-// ... a bf16 query as fp16, divided by the power of two above the row's largest entry: exact down to 2^-24 of that power
+// ... a bf16 query as fp16, divided by the power of two above the row's largest entry: its 8 bits are exact from 2^-17 of that power up, below
+// that (fp16's smallest step there is 2^-24) off by at most 2^-25 of it
 template <int HD>
 __device__ __forceinline__ float query_as_f16(Query<F16, HD>& q, int n)
 {
@@ -937,7 +940,7 @@ struct SharedArgs {
 };
 
 // QT: the query's type; packed tokens are walked in fp16 (fp32 for fp32 queries), 16-bit rows in the
-// cache's own type.
+// cache's own type.  fp32 with heads of 128 needs 17 registers more than there are (scratch): 16 requests over 5000 tokens 40 us, in fp16 27.
 template <typename QT, int HD>
 __global__ __launch_bounds__(64 * WAVES<QT>, 2) void k_shared(SharedArgs a)
 {
@@ -975,7 +978,7 @@ __global__ __launch_bounds__(64 * WAVES<QT>, 2) void k_shared(SharedArgs a)
         const int row = wrow0 + 16 * n + (lane & 15);
         row_at[n] = row < p.rows ? a.q + ((p.first + row / a.rep) * a.Hq + kvh * a.rep + row % a.rep) * (HD * ESIZE<QT>) : nullptr;
     }
-    const bool any = wrow0 < p.rows && wave * COLS * 16 < R;   // (a wavefront without rows only brings tiles)
+    const bool any = wrow0 < p.rows && wave * COLS * 16 < R;   // (fp32: a wavefront without rows only brings tiles; 16-bit types: it keeps its turns, on zeros)
     int done = 0;                                              // tiles of the classes before
     auto walk_class = [&](auto bits) __attribute__((always_inline)) {
         constexpr int BITS = decltype(bits)::value, c = BITS == 2 ? 0 : (BITS == 4 ? 1 : 2);
@@ -1173,7 +1176,8 @@ __device__ __forceinline__ void walk_few(const char* q_row, float scale, int lim
     constexpr int ST = STEPS<QT, HD>, CT16 = HD / 16, PIECES = HD / 8, PER_LOAD = 64 / PIECES, LOADS = 32 / PER_LOAD;
     using D = Direct<HD>;
     const int lane = threadIdx.x & 63, m = lane & 15, j = lane >> 4;
-    Query<QT, HD> q;                                           // (fp32: read again at each use, from L1; 128 registers would not be left)
+    Query<QT, HD> q;                                           // (fp32: read again at each use, from L1; 128 registers would not be left, and with heads
+                                                               // of 128 ten of the others lie in scratch all the same)
     if constexpr (!std::is_same_v<QT, F32>) load_query<QT, HD>(q, 0, q_row);
     ref = -INFINITY, sum = 0.f;
 #pragma unroll
@@ -1429,7 +1433,8 @@ size_t partials_bytes(int64_t rows, int hd, int parts) { return wq_align256((siz
 int rows_of(int64_t q_rows, int rep, int dtype) { return dtype != WQ_F32 && q_rows * rep > 128 ? 256 : 128; }
 // Prompt attention over so few that k_prefill_few takes them (on the average: any number is right): two tiles of 16, though each reads the
 // keys.  us per call, k_prefill -> k_prefill_few: 4 rows of 7 heads a group, 64 sequences of 6400 keys, heads of 64: 142 -> 79 (5 rows would be three
-// tiles: 143), of 128: 412 -> 315; one sequence of 500 keys: 8.8 -> 7.6 and 9.7 -> 11.9.
+// tiles: 143), of 128: 412 -> 315; one sequence of 500 keys: 8.8 -> 7.6 and 9.7 -> 11.9.  One kernel for the whole call: 200 rows and 64 single tokens over 6400
+// keys each, 28/4 heads of 128, take 331 us, apart 60 + 212.
 bool few_rows(int64_t total_q, int B, int rep, int dtype) { return dtype != WQ_F32 && total_q * rep <= (int64_t)B * 32; }
 
 template <typename CT>
@@ -1471,8 +1476,8 @@ WqPrefillPlan wq_prefill_plan(int64_t total_q, int B, int Hq, int Hkv, int hd, i
         s.splits = s.few ? max_kv_rows <= 512 ? 1 : auto_splits_of((tiles_of(total_q, rep, 0, rows) + used) * Hkv, max_kv_rows, 512, 32 * FEW)
                          : auto_splits_of((tiles_of(total_q, rep, 0, rows) + used) * Hkv, max_kv_rows, 256, dtype == WQ_F32 ? 32 : 64);
         // Tiles of equal length (a prefix) for more than the card's 256 compute units: the last round's, where they are no more than half of
-        // them, are cut along the keys to fill it (1404 tiles, 124 of them cut in two: 1950 us, 2050 uncut).  Where there is no prefix tiles are
-        // launched longest first, and the last ones are short.
+        // them, are cut along the keys to fill it (1404 tiles, 124 of them cut in two: 1950 us, 2050 uncut).  Where there is no prefix a sequence's tiles are
+        // launched longest first, and the last ones are short: 12800 causal rows reach 1.13 PFLOP/s uncut, those above 1.18.
         const int64_t rest = units % 256;
         if (rows == 256 && s.splits == 1 && prefix && units > 256 && rest > 0 && rest <= 128 && max_kv_rows >= TAIL_KEYS) {
             s.tail = (int)rest;
