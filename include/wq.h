@@ -387,7 +387,8 @@ size_t wq_prefill_workspace_bytes(int64_t total_q, int B, int Hq, int Hkv, int h
  * with NaN in its query both become NaN.
  * q [B, Hq, hd], out [B, Hq, hd], both of type q_dtype, which pairs with the caches' dtype16 as in wq_reorder_quantize (bf16 with
  * bf16; fp16 and fp32 with fp16); lse [B, Hq] fp32 or NULL.  Both caches: the same Hkv, hd and dtype16.
- * 16-bit queries: packed keys and values are expanded to fp16 and met by fp16 weights (errors of 2^-11 relative to a value, the
+ * 16-bit queries: packed values are expanded to fp16 and met by fp16 weights, a bf16 query's packed keys too (errors of 2^-11 relative to a value; fp16
+ * queries meet the codes, scales and minima enter in fp32; the
  * result has the query's type; bf16 rows of large values: as for prompts); a bf16 query's entries are exact from 2^-17 of the power of two above its
  * head's largest one up, below that off by at most 2^-25 of that power.  fp32 queries: fp32 arithmetic.
  * num_splits: workgroups that share the tokens of a prefix per tile of 256 query rows (fp32: 128; a

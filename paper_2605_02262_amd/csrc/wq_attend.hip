@@ -12,7 +12,7 @@
 // (its accumulators, queries and scores take 220 to 240 registers a lane).  fp32: 128 rows, 32 keys, four wavefronts.
 //   k_prefill        keys and values plain rows, from memory into LDS without registers between (Direct)
 //   k_prefill_few    the same for so few query rows that the keys are shared out instead
-//   k_shared         packed classes, expanded to fp16 on their way into LDS (PackedKeys, PackedValues), then 16-bit rows
+//   k_shared         packed classes, expanded to fp16 on their way into LDS (PackedKeys, PackedValues; fp16 queries meet keys' codes), then 16-bit rows
 //   k_shared_finish  a request's own 16-bit rows, and the merge of the parts; k_merge, k_merge_tail: the merges of k_prefill's
 // Packed tiles lie in LDS in the operands' own order, [step][lane][16 bytes]: every LDS read of the products is one conflict-free 16-byte
 // load per lane.  Plain rows lie as they came, their 16-byte pieces exchanged by row.
@@ -27,8 +27,8 @@
 // Short walks cost what they cannot overlap: 2 us from the launch to the first load, 2 until its first product, 2 for the result.
 //
 // fp32 queries take the fp32 matrix instruction throughout.  16-bit queries take the 16-bit ones: the weights are rounded to
-// the value's type (the sum of weights is not), packed keys and values to fp16 (2^-11 of a value whose own step is its
-// scale; below the output's own rounding).
+// the value's type (the sum of weights is not), packed values to fp16 (2^-11 of a value whose own step is its
+// scale; below the output's own rounding), and so are packed keys for bf16 queries, whose results are rounded eight times coarser.
 #include <float.h>
 #include <math.h>
 #include <type_traits>
@@ -39,6 +39,7 @@ namespace {
 
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 
@@ -63,6 +64,7 @@ template <typename CT, int HD> constexpr int TILE_BYTES = KEYS<CT> * HD * ESIZE<
 template <typename CT, int HD> using Query = u4[COLS][STEPS<CT, HD>];              // B operands of a wavefront's rows
 typedef __attribute__((address_space(3))) char* Lds;
 typedef __attribute__((address_space(3))) u4* Lds4;
+typedef __attribute__((address_space(3))) uint32_t* Lds1;
 
 template <typename CT>
 __device__ __forceinline__ f4 product(u4 a, u4 b, f4 c)
@@ -167,6 +169,59 @@ __device__ __forceinline__ void multiply_keys(Products<CT>& s, const Query<CT, H
         for (int st = 0; st < ST; st++)
 #pragma unroll
             for (int n = 0; n < COLS; n++) s[t][n] = product<CT>(a[t & 1][st], q[n][st], s[t][n]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// A packed class's codes as they are, for fp16 queries: the group's scale and minimum are applied to the sums in fp32,
+//     q.k^ = sum over the head's groups g of  s_g (q.code)_g + m_g (sum of q)_g
+// A key rounded to fp16 would be off by 3.0e-4 of a result whose own rounding is 2.1e-4, for two vector operations less per logit and group: us per call of
+// 64 requests over 51200 tokens, rounded -> as codes: heads of 128 in one, two and four groups 92 -> 97, 103, 119, heads of 64 in one and two 44 -> 48, 52.
+// metas(t, g): the scales and minima of this lane's four keys, read one group ahead.  A group's sums are finished behind the products of the next (all groups
+// of 16 keys at once, or the minima as one more matrix product, took more registers than there are: 107, 106 for two groups).
+template <int HD, int G, typename Keys, typename Metas>
+__device__ __forceinline__ void multiply_codes(Products<F16>& s, const Query<F16, HD>& q, const float (&q_sum)[COLS][G], const Keys& keys, const Metas& metas)
+{
+    constexpr int T = KEYS<F16> / 16, ST = STEPS<F16, HD>, PER = ST / G;
+    u4 a[2][ST];
+    u4 sm[2];
+    f4 x[2][COLS];
+    sm[0] = metas(0, 0);
+#pragma unroll
+    for (int st = 0; st < ST; st++) a[0][st] = keys(0, st);
+#pragma unroll
+    for (int j = 0; j <= T * G; j++) {
+        const int t = j / G, g = j % G;
+        if (g == 0 && t + 1 < T) {
+#pragma unroll
+            for (int st = 0; st < ST; st++) a[(t + 1) & 1][st] = keys(t + 1, st);
+        }
+        if (j > 0 && j < T * G) sm[j & 1] = metas(t, g);
+        __builtin_amdgcn_sched_barrier(0);
+        if (t < T) {
+#pragma unroll
+            for (int n = 0; n < COLS; n++) x[j & 1][n] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int st = g * PER; st < (g + 1) * PER; st++)
+#pragma unroll
+                for (int n = 0; n < COLS; n++) x[j & 1][n] = product<F16>(a[t & 1][st], q[n][st], x[j & 1][n]);
+        }
+        if (j > 0) {
+            const int bt = (j - 1) / G, bg = (j - 1) % G;
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const uint32_t word = sm[(j - 1) & 1][i];      // (the cast of a vector's element would read its first)
+                const h2 f = __builtin_bit_cast(h2, word);
+#pragma unroll
+                for (int n = 0; n < COLS; n++) {
+                    const float y = bg ? fmaf((float)f[1], q_sum[n][bg], s[bt][n][i]) : (float)f[1] * q_sum[n][bg];
+                    s[bt][n][i] = fmaf((float)f[0], x[(j - 1) & 1][n][i], y);
+                }
+            }
+            // (here, not behind the barrier, where all tiles' sums would wait for it in registers)
+#pragma unroll
+            for (int n = 0; n < COLS; n++) asm volatile("" : "+v"(s[bt][n]));
+        }
         __builtin_amdgcn_sched_barrier(0);
     }
 }
@@ -288,12 +343,12 @@ __device__ __forceinline__ void meet()
 }
 __device__ __forceinline__ int group_of_wave() { return this_wave() >> 2; }
 
-// Tiles t0 .. t1-1.  bring_keys(t), bring_values(t): of the group that does so, into LDS; settle(): a phase's end.  The products of the first tile meet
-// weights of zero with what lies in front of its values: zeros.  (No condition inside the loop but who brings what: the compiler
+// Tiles t0 .. t1-1.  multiply(s, t): a tile's products of keys; bring_keys(t), bring_values(t): of the group that does so, into LDS; settle(): a phase's end.
+// The products of the first tile meet weights of zero with what lies in front of its values: zeros.  (No condition inside the loop but who brings what: the compiler
 // copies the accumulators around every one, and spills them.)
-template <typename CT, int HD, bool SPLIT, typename Order, typename Keys, typename Values, typename BringKeys, typename BringValues, typename Settle>
-__device__ __forceinline__ void take_turns(Rows<HD>& r, const Query<CT, HD>& q, int t0, int t1, int least, const Keys& keys, const Values& values,
-                                           const BringKeys& bring_keys, const BringValues& bring_values, const Settle& settle)
+template <typename CT, int HD, bool SPLIT, typename Order, typename Multiply, typename Values, typename BringKeys, typename BringValues, typename Settle>
+__device__ __forceinline__ void take_turns(Rows<HD>& r, int t0, int t1, int least, const Multiply& multiply, const Values& values, const BringKeys& bring_keys,
+                                           const BringValues& bring_values, const Settle& settle)
 {
     const int group = group_of_wave();
     if (SPLIT && group == 1) {
@@ -319,7 +374,7 @@ __device__ __forceinline__ void take_turns(Rows<HD>& r, const Query<CT, HD>& q, 
 #pragma unroll 1
     for (int t = t0; t < t1; t++) {
         __builtin_amdgcn_s_setprio(3);
-        multiply_keys<CT, HD>(s, q, [&](int kt, int st) { return keys(t, kt, st); });
+        multiply(s, t);
         multiply_values<CT, HD>(r, p, [&](int vs, int ct) { return values(t - 1, vs, ct); });
         __builtin_amdgcn_s_setprio(0);
         if (!SPLIT && group == 0 && t + 1 < t1) bring_keys(t + 1);
@@ -458,12 +513,12 @@ __device__ __forceinline__ void walk_rows(Rows<HD>& r, const Query<CT, HD>& q, c
     else clear_tile<CT, HD>(v_lds + (~lo & 1) * BYTES);
     __syncthreads();
     take_turns<CT, HD, SPLIT, Natural>(
-        r, q, lo, hi, least, [&](int t, int kt, int st) { return rows.keys(k_lds + (t & 1) * BYTES, kt, st); },
+        r, lo, hi, least,
+        [&](Products<CT>& s, int t) { multiply_keys<CT, HD>(s, q, [&](int kt, int st) { return rows.keys(k_lds + (t & 1) * BYTES, kt, st); }); },
         [&](int t, int vs, int ct) { return rows.values(v_lds + (t & 1) * BYTES, vs, ct); }, [](int) {}, bring_values, [] { __syncthreads(); });
 }
 
 // ---- a class of the packed cache -----------------------------------------------------------------------------------------
-typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100); }
 __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302); }
 
@@ -501,12 +556,20 @@ __device__ __forceinline__ uint32_t placed(uint32_t w)
     return (w & (MASK | MASK << 16)) | one;
 }
 template <int BITS, int AT>
-__device__ __forceinline__ uint32_t expanded(uint32_t x, h2 s, h2 m)
+__device__ __forceinline__ h2 code_pair(uint32_t x)
 {
     constexpr _Float16 BIAS = (_Float16)(float)(1 << (10 - AT));
-    const h2 code = __builtin_bit_cast(h2, x) - h2{BIAS, BIAS};
-    return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(code, s, m));       // (one rounding)
+    return __builtin_bit_cast(h2, x) - h2{BIAS, BIAS};
 }
+template <int BITS, int AT>
+__device__ __forceinline__ uint32_t expanded(uint32_t x, h2 s, h2 m)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(code_pair<BITS, AT>(x), s, m));       // (one rounding)
+}
+// ... or the codes alone
+struct Codes {};
+template <int BITS, int AT>
+__device__ __forceinline__ uint32_t expanded(uint32_t x, Codes, Codes) { return __builtin_bit_cast(uint32_t, code_pair<BITS, AT>(x)); }
 
 // A tile in flight between memory and LDS, in registers, brought by 64 * 4 (TOKENS = 64) or 64 * 2 (32) threads each of keys and of values.  A key
 // unit is a quarter of a token's channels (lane of the product), a value unit 8 tokens of every 16th channel of half of the head.
@@ -538,12 +601,22 @@ struct PackedKeys {
         load_words<BYTES>(codes + (int64_t)t * (TOKENS * HD * BITS / 8) + (code_off - (again ? 128 * BYTES : 0)), w);
         meta = (metas + (int64_t)t * (TOKENS * G))[meta_off - (again ? 32 * G : 0)];
     }
-    // pairs of channels as a masked word holds them: see order_query
     __device__ __forceinline__ void stage(Lds4 k_tile) const
     {
-        const int lane = unit & 63;
-        const h2 sm = __builtin_bit_cast(h2, meta), s = {sm[0], sm[0]}, m = {sm[1], sm[1]};
-        Lds4 to = k_tile + (unit >> 6) * STEPS<F16, HD> * 64 + lane;
+        const h2 sm = __builtin_bit_cast(h2, meta);
+        expand(k_tile + (unit >> 6) * STEPS<F16, HD> * 64 + (unit & 63), h2{sm[0], sm[0]}, h2{sm[1], sm[1]}, [](int st) { return st * 64; });
+    }
+    // The codes alone, 32 neighbouring channels per step (a group is whole steps); scales and minima [16-key tile][group][key]
+    __device__ __forceinline__ void stage_codes(Lds4 k_tile, Lds meta_tile) const
+    {
+        const int j = (unit & 63) >> 4, m = unit & 15, piece = j * STEPS<F16, HD>;         // the quarter's first 8 channels
+        expand(k_tile + (unit >> 6) * STEPS<F16, HD> * 64 + (piece >> 2) * 64 + (piece & 3) * 16 + m, Codes(), Codes(), [](int st) { return st * 16; });
+        ((Lds1)meta_tile)[((unit >> 6) * G + (j * G >> 2)) * 16 + m] = meta;        // (a group's quarters write the same)
+    }
+    // pairs of channels as a masked word holds them: see order_query, load_query_codes
+    template <typename SM, typename Place>
+    __device__ __forceinline__ void expand(Lds4 to, SM s, SM m, const Place& place) const
+    {
 #pragma unroll
         for (int st = 0; st < STEPS<F16, HD>; st++) {
             u4 y;
@@ -562,7 +635,7 @@ struct PackedKeys {
                 y[0] = expanded<BITS, 0>(placed<BITS, 0>(x), s, m), y[1] = expanded<BITS, 2>(placed<BITS, 2>(x), s, m);
                 y[2] = expanded<BITS, 4>(placed<BITS, 4>(x), s, m), y[3] = expanded<BITS, 6>(placed<BITS, 6>(x), s, m);
             }
-            to[st * 64] = y;
+            to[place(st)] = y;
         }
     }
     // fp32, codes one by one
@@ -669,10 +742,11 @@ struct PackedValues {
     }
 };
 
-// Tiles t0 .. t1-1 of a class's segment
-template <int HD, int BITS>
-__device__ __forceinline__ void walk_packed(Rows<HD>& r, const Query<F16, HD>& q, const wq_packed_kv& kv, int kvh, int64_t tok0, int len, int t0, int t1,
-                                            Lds k_lds, Lds v_lds)
+// Tiles t0 .. t1-1 of a class's segment.  G: the head's groups, whose codes enter the products as they are; 0: keys expanded to fp16 (q_sum and m_lds
+// are not read)
+template <int HD, int BITS, int G>
+__device__ __forceinline__ void walk_packed(Rows<HD>& r, const Query<F16, HD>& q, const float (&q_sum)[COLS][G ? G : 1], const wq_packed_kv& kv, int kvh, int64_t tok0,
+                                            int len, int t0, int t1, Lds k_lds, Lds v_lds, Lds m_lds)
 {
     using Order = std::conditional_t<BITS == 8, Near, Far>;
     constexpr int BYTES = TILE_BYTES<F16, HD>;
@@ -682,7 +756,8 @@ __device__ __forceinline__ void walk_packed(Rows<HD>& r, const Query<F16, HD>& q
     auto k_of = [&](int t) { return (Lds4)(k_lds + (t & 1) * BYTES); };
     auto v_of = [&](int t) { return (Lds4)(v_lds + (t & 1) * BYTES); };
     auto bring_keys = [&](int t) {
-        keys.stage(k_of(t));
+        if constexpr (G > 0) keys.stage_codes(k_of(t), m_lds + (t & 1) * (64 * 4 * G));
+        else keys.stage(k_of(t));
         if (t + 1 < t1) keys.load(t + 1);
     };
     auto bring_values = [&](int t) {
@@ -699,7 +774,14 @@ __device__ __forceinline__ void walk_packed(Rows<HD>& r, const Query<F16, HD>& q
     }
     __syncthreads();
     take_turns<F16, HD, false, Order>(
-        r, q, t0, t1, len, [&](int t, int kt, int st) { return k_of(t)[(kt * STEPS<F16, HD> + st) * 64 + lane]; },
+        r, t0, t1, len,
+        [&](Products<F16>& s, int t) {
+            auto operand = [&](int kt, int st) { return k_of(t)[(kt * STEPS<F16, HD> + st) * 64 + lane]; };
+            if constexpr (G > 0)
+                multiply_codes<HD, G>(s, q, q_sum, operand, [&](int kt, int g) { return ((Lds4)(m_lds + (t & 1) * (64 * 4 * G)))[(kt * G + g) * 4 + (lane >> 4)]; });
+            else
+                multiply_keys<F16, HD>(s, q, operand);
+        },
         [&](int t, int vs, int ct) { return v_of(t)[(vs * (HD / 16) + ct) * 64 + lane]; }, bring_keys, bring_values, meet);
 }
 
@@ -768,6 +850,40 @@ __device__ __forceinline__ void order_query(Query<F16, HD>& q, int n)
     }
 #pragma unroll
     for (int st = 0; st < STEPS<F16, HD>; st++) q[n][st] = y[st];
+}
+
+// A row's pieces of 8 channels in the rows' order, pairs of channels as stage_codes leaves them; sums over the head's G groups
+template <int BITS, int G, int HD>
+__device__ __forceinline__ void load_query_codes(Query<F16, HD>& q, int n, const char* row, float (&q_sum)[G])
+{
+    constexpr int PER = STEPS<F16, HD> / G;
+    const int j = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int g = 0; g < G; g++) q_sum[g] = 0.f;
+#pragma unroll
+    for (int st = 0; st < STEPS<F16, HD>; st++) {
+        u4 x = {0, 0, 0, 0};
+        if (row) {
+            const int piece = 4 * st + j;
+            if constexpr (BITS == 2) {                         // of two neighbouring pieces
+                const char* at = row + (piece >> 1) * 32 + (piece & 1) * 8;
+                const uint2 a = *reinterpret_cast<const uint2*>(at), b = *reinterpret_cast<const uint2*>(at + 16);
+                x = u4{a.x, b.x, a.y, b.y};
+            } else {                                           // 4 bits: registers 0 with 2, 1 with 3; 8 bits: 0 with 1, 2 with 3
+                x = *reinterpret_cast<const u4*>(row + piece * 16);
+                if constexpr (BITS == 4) x = u4{x[0], x[2], x[1], x[3]};
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const uint32_t word = x[e];
+            const h2 f = __builtin_bit_cast(h2, word);
+            q_sum[st / PER] += (float)f[0] + (float)f[1];
+        }
+        q[n][st] = u4{low_halves(x[0], x[1]), high_halves(x[0], x[1]), low_halves(x[2], x[3]), high_halves(x[2], x[3])};
+    }
+#pragma unroll
+    for (int g = 0; g < G; g++) q_sum[g] = sum_of_column(q_sum[g]);
 }
 
 template <typename QT> constexpr uint32_t EXPONENT16 = std::is_same_v<QT, Bf16> ? 0x7F80 : 0x7C00;
@@ -939,15 +1055,15 @@ struct SharedArgs {
     Out out;
 };
 
-// QT: the query's type; packed tokens are walked in fp16 (fp32 for fp32 queries), 16-bit rows in the
+// QT: the query's type; G as in walk_packed (fp16: the cache's groups per head; else 0); packed tokens are walked in fp16 (fp32 for fp32 queries), 16-bit rows in the
 // cache's own type.  fp32 with heads of 128 needs 17 registers more than there are (scratch): 16 requests over 5000 tokens 40 us, in fp16 27.
-template <typename QT, int HD>
+template <typename QT, int HD, int G>
 __global__ __launch_bounds__(64 * WAVES<QT>, 2) void k_shared(SharedArgs a)
 {
     using CT = std::conditional_t<std::is_same_v<QT, F32>, F32, F16>;
     constexpr bool PIPED = ESIZE<QT> == 2;
     constexpr int BYTES = TILE_BYTES<CT, HD> * (1 + PIPED), R = ROWS<QT>, TK = KEYS<QT>;
-    __shared__ __align__(16) char s_k[BYTES], s_v[BYTES];
+    __shared__ __align__(16) char s_k[BYTES], s_v[BYTES], s_m[G > 0 ? 2 * 64 * 4 * G : 16];
     const int Hkv = a.kv.Hkv, wave = this_wave(), lane = threadIdx.x & 63;
     const wq_packed_kv& kv = a.kv;
     const int unit = (int)blockIdx.x % a.units, split = (int)blockIdx.x / a.units, kvh = unit % Hkv;
@@ -973,6 +1089,7 @@ __global__ __launch_bounds__(64 * WAVES<QT>, 2) void k_shared(SharedArgs a)
     clear(r);
     const int wrow0 = p.row0 + wave * COLS * 16;
     const char* row_at[COLS];
+    [[maybe_unused]] float q_sum[COLS][G > 0 ? G : 1];
 #pragma unroll
     for (int n = 0; n < COLS; n++) {
         const int row = wrow0 + 16 * n + (lane & 15);
@@ -989,17 +1106,18 @@ __global__ __launch_bounds__(64 * WAVES<QT>, 2) void k_shared(SharedArgs a)
         for (int n = 0; n < COLS; n++) {
             r.limit[n] = len[c];
             r.scale[n] = a.scale;
-            load_query_quarter<CT, HD>(q, n, row_at[n]);
+            if constexpr (G > 0) load_query_codes<BITS, G, HD>(q, n, row_at[n], q_sum[n]);
+            else load_query_quarter<CT, HD>(q, n, row_at[n]);
             bool bad = false;
             if constexpr (PIPED) bad = not_finite<QT, HD>(q, n);
             // (kept from 0 and infinity: a masked logit, -infinity, times 0 and a logit of 0 times infinity would be NaN.  A scale that small leaves every
             // logit below 2^-100; with one that large logits that differ at all differ by 2^70 or more)
             if constexpr (std::is_same_v<QT, Bf16>) r.scale[n] = fminf(fmaxf(a.scale * query_as_f16<HD>(q, n), FLT_MIN), FLT_MAX);
             if (bad) r.scale[n] = NAN;
-            if constexpr (PIPED) order_query<BITS, HD>(q, n);
+            if constexpr (PIPED && G == 0) order_query<BITS, HD>(q, n);
         }
         if constexpr (PIPED) {
-            walk_packed<HD, BITS>(r, q, kv, kvh, kv.cls_off[c][p.seq], len[c], t0, t1, (Lds)s_k, (Lds)s_v);
+            walk_packed<HD, BITS, G>(r, q, q_sum, kv, kvh, kv.cls_off[c][p.seq], len[c], t0, t1, (Lds)s_k, (Lds)s_v, (Lds)s_m);
         } else {
             PackedKeys<HD, BITS, 32> keys(kv, kvh, kv.cls_off[c][p.seq], 0);
             PackedValues<HD, BITS, 32> values(kv, kvh, kv.cls_off[c][p.seq], 0);
@@ -1444,8 +1562,13 @@ auto prefill_kernel(int hd, bool split) -> void (*)(PrefillArgs)
         if (split) return hd == 128 ? k_prefill<CT, 128, true> : k_prefill<CT, 64, true>;
     return hd == 128 ? k_prefill<CT, 128, false> : k_prefill<CT, 64, false>;
 }
-template <typename QT>
-auto shared_kernel(int hd) -> void (*)(SharedArgs) { return hd == 128 ? k_shared<QT, 128> : k_shared<QT, 64>; }
+auto shared_kernel(int dtype, int hd, int groups) -> void (*)(SharedArgs)
+{
+    if (dtype == WQ_F32) return hd == 128 ? k_shared<F32, 128, 0> : k_shared<F32, 64, 0>;
+    if (dtype == WQ_BF16) return hd == 128 ? k_shared<Bf16, 128, 0> : k_shared<Bf16, 64, 0>;
+    if (hd == 64) return groups == 1 ? k_shared<F16, 64, 1> : k_shared<F16, 64, 2>;
+    return groups == 1 ? k_shared<F16, 128, 1> : groups == 2 ? k_shared<F16, 128, 2> : k_shared<F16, 128, 4>;
+}
 
 template <typename QT>
 auto finish_kernel(int hd) -> void (*)(FinishArgs) { return hd == 128 ? k_shared_finish<QT, 128> : k_shared_finish<QT, 64>; }
@@ -1587,7 +1710,7 @@ int wq_launch_shared(wq_ctx* ctx, const WqShared& f)
         if (rc != WQ_OK) return rc;
     }
     const dim3 grid((unsigned)f.plan.groups);
-    hipLaunchKernelGGL(f.q_dtype == WQ_F32 ? shared_kernel<F32>(kv->hd) : f.q_dtype == WQ_BF16 ? shared_kernel<Bf16>(kv->hd) : shared_kernel<F16>(kv->hd), grid,
+    hipLaunchKernelGGL(shared_kernel(f.q_dtype, kv->hd, kv->hd / kv->group), grid,
                        dim3(f.q_dtype == WQ_F32 ? 256 : 512), 0, ctx->stream, a);
     FinishArgs m;
     m.q = a.q, m.req_off = f.req_off;

@@ -187,12 +187,12 @@ def test_large_values_of_shared_caches(lens, own, splits):
 
 # ---- what 16-bit roundings cost -----------------------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", DTYPES[:2])
-@pytest.mark.parametrize("heads,group", [(SMALL, 32), (LARGE, 64)])
+@pytest.mark.parametrize("heads,group", [(SMALL, 32), (SMALL, 64), (LARGE, 32), (LARGE, 64), (LARGE, 128)])
 @pytest.mark.parametrize("spread_q", [1.0, 2.0 ** 4])
 def test_accuracy_of_16_bit_requests(dtype, heads, group, spread_q):
     """Logits of deviation 3, and of 48 (a peaked softmax whose reference moves).  Roundings are independent, each off by at most half a step (its
     square a third of that squared on the average): of the result; of a weight (fp16 for packed tokens, the rows' type for theirs); of a packed
-    key's and value's expansion to fp16.  The sum of weights is not rounded, so a weight's rounding acts through its value, a key's through the
+    value's expansion to fp16 and, for bf16 requests, a key's (fp16 ones meet its codes).  The sum of weights is not rounded, so a weight's rounding acts through its value, a key's through the
     difference from the result.  No element beyond the worst case of all of them, their common size not beyond the mean of the squares."""
     Hq, Hkv, hd = heads
     rng = np.random.default_rng(7)
@@ -207,6 +207,9 @@ def test_accuracy_of_16_bit_requests(dtype, heads, group, spread_q):
     again = W.wq_decode_attention_shared(ctx, q, prefix, R.i32([0, B]), own, sm, 0, longest, 25)
     assert torch.equal(again, out), "two calls differ"
     u = R.HALF_STEP[dtype]
+    of_key = r if dtype == torch.bfloat16 else 0.0
+    # (a logit's fp32 sums: of codes times scale and of minima, each up to twice the largest minimum beyond the key itself)
+    minima = max(float(np.nanmax(np.abs((m[0].cpu().numpy().view(np.uint32) >> 16).astype(np.uint16).view(np.float16).astype(np.float64)))) for m in prefix.meta)
     packed = torch.zeros(longest + 25, dtype=torch.float64)
     packed[:sum(lens[:3])] = 1.0
     off_weight = torch.where(packed > 0, r, u)
@@ -217,15 +220,16 @@ def test_accuracy_of_16_bit_requests(dtype, heads, group, spread_q):
         want, want_lse, spread, terms = R.attend(qb[None], k, v, [k.shape[0]], sm)
         want, spread = want[0], spread[0]
         err = (out[b].double().cpu() - want).abs()
-        w, tiny = R.weights_error(k.shape[0], hd, terms, float(want_lse.abs().max())), 2.0 ** -25 if dtype == torch.float16 else 0.0
-        bound = (math.expm1(2 * r * terms) + 2 * w + u + r) * spread + u * want.abs() + tiny
+        sums = terms + (0.0 if of_key else 2 * minima * float(qb.abs().sum(-1).max()) * sm)
+        w, tiny = R.weights_error(k.shape[0], hd, sums, float(want_lse.abs().max())), 2.0 ** -25 if dtype == torch.float16 else 0.0
+        bound = (math.expm1(2 * of_key * terms) + 2 * w + u + r) * spread + u * want.abs() + tiny
         assert bool((err <= bound).all()), float((err / bound).max())
-        assert bool(((lse[b].double().cpu() - want_lse[0]).abs() <= r * terms + 2 * w + 2.0 ** -22 * want_lse[0].abs()).all())
+        assert bool(((lse[b].double().cpu() - want_lse[0]).abs() <= of_key * terms + 2 * w + 2.0 ** -22 * want_lse[0].abs()).all())
         for h in range(Hq):
             kh, vh = k[:, h // (Hq // Hkv)], v[:, h // (Hq // Hkv)]
             terms_of = qb[h] * kh * sm
             p = torch.softmax(terms_of.sum(1), 0)
-            logit = r * r / 3 * packed * terms_of.square().sum(1)
+            logit = of_key * of_key / 3 * packed * terms_of.square().sum(1)
             var = (u * want[h]).square() / 3 + (p.square()[:, None] * (((off_weight.square() + packed * r * r) / 3)[:, None] * vh.square()
                                                                           + logit[:, None] * (vh - want[h]).square())).sum(0)
             expected_all += float(var.sum())
