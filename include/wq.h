@@ -387,10 +387,10 @@ size_t wq_prefill_workspace_bytes(int64_t total_q, int B, int Hq, int Hkv, int h
  * with NaN in its query both become NaN.
  * q [B, Hq, hd], out [B, Hq, hd], both of type q_dtype, which pairs with the caches' dtype16 as in wq_reorder_quantize (bf16 with
  * bf16; fp16 and fp32 with fp16); lse [B, Hq] fp32 or NULL.  Both caches: the same Hkv, hd and dtype16.
- * 16-bit queries: packed values are expanded to fp16 and met by fp16 weights, a bf16 query's packed keys too (errors of 2^-11 relative to a value; fp16
- * queries meet the codes, scales and minima enter in fp32; the
- * result has the query's type; bf16 rows of large values: as for prompts); a bf16 query's entries are exact from 2^-17 of the power of two above its
- * head's largest one up, below that off by at most 2^-25 of that power.  fp32 queries: fp32 arithmetic.
+ * 16-bit queries: the result has the query's type.  Packed values are expanded to fp16 and met by fp16 weights, 16-bit rows by weights of their type
+ * (errors of half a step relative to a value; large bf16 values as for prompts).  An fp16 query meets the codes of packed keys, their scales and minima in
+ * fp32; for a bf16 query they are expanded to fp16, and its own entries are exact from 2^-17 of the power of two above its head's largest one up,
+ * below that off by at most 2^-25 of that power.  fp32 queries: fp32 arithmetic.
  * num_splits: workgroups that share the tokens of a prefix per tile of 256 query rows (fp32: 128; a
  * request has Hq/Hkv of them), 1 .. 64, or 0 = automatic; max_prefix_tokens, max_own_tokens: host bounds on the tokens of one sequence
  * (used for splits and the choice of kernels; any value gives the same result to rounding, max_prefix_tokens 0 in one part).  At most 2^18 query heads; q, out and the caches' buffers 16-byte aligned.  Workspace: wq_shared_workspace_bytes (max_own_tokens 0 where own is NULL).                            */
