@@ -11,8 +11,9 @@
  *   wq_decode_attention  ... and decoding over the mixed cache        (Alg. 2 second half, Sec. 3.3.2)
  *
  * and, around them, what a serving program does with the same rows and caches: wq_rope and wq_rope_append_kv (rotary
- * positions of the rows that are cached), wq_prefill_attention (attention of a prompt's rows before they are packed)
- * and wq_decode_attention_shared (requests that ask about the same packed video).
+ * positions of the rows that are cached), wq_prefill_attention (attention of a prompt's rows before they are packed),
+ * wq_decode_attention_shared (requests that ask about the same packed video), wq_tree_attention, wq_tree_accept and
+ * wq_append_rows (several drafted tokens per step, or a further question's rows) and wq_copy_sequences (forks, compaction).
  *
  * Conventions
  *   - Every pointer named "dev" or documented as device memory is a HIP device pointer on the current
@@ -106,6 +107,10 @@ typedef enum { WQ_DECODE_AUTO = 0, WQ_DECODE_GENERIC = 1, WQ_DECODE_MFMA = 2 } w
                                   * wq_validate_assignment; the windows beyond the bound were left out                  */
 #define WQ_DEV_BAD_ASSIGNMENT 32u /* wq_validate_assignment: perm is not a permutation of a sequence's windows, or its four
                                   * class counts do not add up to the number of its windows                             */
+#define WQ_DEV_TOO_MANY_ROWS 64u /* a sequence has more new rows than the call can take: wq_tree_attention with parents (1024), wq_tree_accept
+                                  * (max_rows), wq_append_rows (max_take); what becomes of it stands there                  */
+#define WQ_DEV_BAD_INDEX 128u    /* wq_append_rows: a row outside its sequence, or a negative number of them; wq_copy_sequences: a sequence
+                                  * outside the source                                                                  */
 #define WQ_DEV_APPEND_TIMEOUT 4u /* wq_decode_append_attention: the workgroup that raises len16[b] gave up waiting (4 s) for
                                   * the sequence's other workgroups to start; len16[b] was raised all the same, the
                                   * workspace header may hold a stale count and must be zeroed before its next use     */
@@ -400,6 +405,65 @@ int wq_decode_attention_shared(wq_ctx* ctx, const void* q, int q_dtype, int B, i
 /* Host-only, pure: workspace of a call with these arguments (P: sequences of the shared cache).  As above: fewer requests can have more parts; with
  * num_splits = 0 a call takes as many as there is room for, at least one (whose room grows with B). */
 size_t wq_shared_workspace_bytes(int B, int P, int Hq, int Hkv, int hd, int64_t max_prefix_tokens, int64_t max_own_tokens, int num_splits);
+
+/* ---- attention of several new rows per sequence over its packed cache -------------------------------------------------
+ * Drafted tokens that the model checks in one step, or the rows of a further question: sequence b of the cache (all four
+ * segments) has the new rows row_off[b] .. row_off[b+1]-1, which are not in the cache.  Its row i (0 the first) sees every token
+ * of the cache, itself, and of the new rows
+ *     parent given   its parent, that row's parent, and so on: parent [total_rows] holds each row's parent, numbered within the
+ *                    sequence; a value outside 0 .. i-1 (-1, say) is none
+ *     parent NULL    the rows 0 .. i-1: a chain
+ *     out[i,h,:] = sum_j softmax_j(sm_scale * q[i,h].k_j) v_j   over what it sees, one softmax (sm_scale as for prompts).  Head h reads KV head h/(Hq/Hkv).
+ * Nothing is written to the cache: wq_append_rows puts the rows that stay there.  A row with NaN in its query becomes NaN, its lse too.
+ * q [total_rows, Hq, hd], k, v [total_rows, Hkv, hd] (Hkv, hd those of the cache), all of type `dtype`, which pairs with dtype16 as in
+ * wq_reorder_quantize; rows *_stride elements apart (pieces of one projection need not be split).  out [total_rows, Hq, hd] of the same
+ * type, contiguous; lse [total_rows, Hq] fp32 or NULL; rows of both that belong to no sequence are left as they were.
+ * row_off [B+1] ascending, device; total_rows: host bound (rows beyond it are not read).  With parents a sequence has at most 1024
+ * rows: those behind become zeros, their lse -infinity, and WQ_DEV_TOO_MANY_ROWS is raised; a chain may be as long as it likes.
+ * max_rows (with parents at most 1024), max_cache_tokens: host bounds on one sequence's new rows and cached tokens, used for the number of parts and the
+ * choice of kernels (any values give the same result to rounding).  num_splits: workgroups that share a tile of query rows' keys,
+ * 1 .. 64, or 0 = automatic.
+ * Arithmetic as in wq_decode_attention_shared; the new rows' keys and values enter as they are (fp32 too, where the cache will hold them in fp16).
+ * Values of the new rows must be finite (those that a row does not see meet a weight of zero), and as small as for prompts.
+ * Pointers 16-byte aligned, rows a multiple of 16 bytes apart (k's and v's at most 2^22 elements); at most 2^18 query heads; out must not overlap the inputs.
+ * Workspace: wq_tree_workspace_bytes (as for prompts: with num_splits = 0 a call takes as many parts as there is room for).  */
+int wq_tree_attention(wq_ctx* ctx, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int dtype, int B, int Hq,
+                      const wq_packed_kv* kv, const int32_t* row_off, const int32_t* parent, int64_t total_rows, int max_rows, float sm_scale, int num_splits,
+                      int64_t max_cache_tokens, void* out, float* lse);
+/* Host-only, pure: workspace of a call with these arguments. */
+size_t wq_tree_workspace_bytes(int64_t total_rows, int B, int Hq, int Hkv, int hd, int64_t max_cache_tokens, int max_rows, int num_splits);
+
+/* ---- which drafted rows stay -------------------------------------------------------------------------------------------
+ * tokens [total_rows]: the token of every row; target [total_rows]: the token that the model chose to follow it.  Sequence b's path begins with
+ * its row 0 (the last token that is certain) and goes on to a row's first child (parent as above; NULL: the next row) whose token is the row's target,
+ * as long as there is one and the path has fewer than max_path rows.
+ * path [B, max_path]: the rows, numbered within the sequence, then -1; n_path [B]: how many they are (0 for a sequence without rows);
+ * next_token [B]: the target of the last one (-1 without rows).  All int32, device.  row_off, total_rows as above.  A sequence with more than
+ * max_rows rows (1 .. 1024) raises WQ_DEV_TOO_MANY_ROWS, and only its first max_rows rows count.  B at most 2^24 - 1.                 */
+int wq_tree_accept(wq_ctx* ctx, const int32_t* tokens, const int32_t* target, const int32_t* parent, int B, const int32_t* row_off, int64_t total_rows, int max_rows,
+                   int max_path, int32_t* path, int32_t* n_path, int32_t* next_token);
+
+/* ---- appending several rows (wq_append_kv for more than one, and for all layers at once) ---------------------------------
+ * k[l], v[l] [total_rows, Hkv, hd], element type `dtype` (pairs with dtype16 as in wq_append_kv), rows *_stride elements apart: layer l's rows;
+ * kv[l]: its cache.  k, v, kv: host arrays of n_layers; the caches agree in B, Hkv, hd and dtype16 and have tables and buffers of their own.
+ * Of sequence b's rows row_off[b] .. row_off[b+1]-1 those that take [B, max_take] names (numbered within the sequence, n_take[b] of them, in this
+ * order: wq_tree_accept's path and n_path), or all of them in order (take and n_take NULL), become rows off16[b] + len16[b] .. of its 16-bit segment, and
+ * len16[b] is raised.  max_take: host bound on a sequence's appended rows.
+ * A sequence is left unchanged in a layer whose segment has no room for all of its rows (WQ_DEV_SEG16_OVERFLOW), and in all layers if it has more than
+ * max_take of them (WQ_DEV_TOO_MANY_ROWS) or names one that it does not have (WQ_DEV_BAD_INDEX).  All pointers 16-byte aligned but the tables',
+ * rows a multiple of 16 bytes apart; inputs must not overlap the caches.                                                            */
+int wq_append_rows(wq_ctx* ctx, int n_layers, const void* const* k, int64_t k_stride, const void* const* v, int64_t v_stride, int dtype, int B, const int32_t* row_off,
+                   int64_t total_rows, const int32_t* take, const int32_t* n_take, int max_take, const wq_packed_kv* kv);
+
+/* ---- sequences copied into another cache ---------------------------------------------------------------------------------
+ * Sequence d of dst becomes a copy of sequence from[d] of src (from [dst->B] int32, device; the same one may be named several times: a
+ * fork; one that is not named is left behind; -1: an empty sequence), for n_layers caches at once (src, dst: host arrays).  dst's classes are laid out
+ * afresh, one sequence behind the other: its cls_off, cls_len, len16 and the first B entries of v_scale_max are written; its off16 (and with it the
+ * room of every 16-bit segment) is the caller's.  A sequence that does not fit a class (WQ_DEV_CLASS_OVERFLOW) or its 16-bit segment
+ * (WQ_DEV_SEG16_OVERFLOW), or whose from[d] is outside -1 .. src->B-1 (WQ_DEV_BAD_INDEX), becomes empty; it keeps its place in the classes as far as
+ * they reach.  All caches: the same Hkv, hd, group and dtype16; all of src the same B, all of dst too; buffers 16-byte aligned; a dst shares no
+ * memory with any src.                                                                                                            */
+int wq_copy_sequences(wq_ctx* ctx, int n_layers, const wq_packed_kv* src, const wq_packed_kv* dst, const int32_t* from);
 
 #ifdef __cplusplus
 }

@@ -24,6 +24,7 @@ ROPE_HALF, ROPE_PAIRS = 0, 1
 ROPE_PLAIN, ROPE_EVEN, ROPE_BASE, ROPE_PARTS = 0, 1, 2, 3
 CLASS_BITS = (2, 4, 8)
 DEV_CLASS_OVERFLOW, DEV_SEG16_OVERFLOW, DEV_APPEND_TIMEOUT, DEV_TOO_MANY_WINDOWS, DEV_BAD_ASSIGNMENT = 1, 2, 4, 16, 32
+DEV_TOO_MANY_ROWS, DEV_BAD_INDEX = 64, 128
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libwq.so")
 _lib = None
@@ -87,6 +88,12 @@ def lib() -> C.CDLL:
         L.wq_decode_attention_shared.argtypes = [vp, vp, i32, i32, i32, C.POINTER(_PackedKV), vp, C.POINTER(_PackedKV), f32, i32, i64, i64, vp, vp]
         L.wq_shared_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i64, i64, i32]
         L.wq_shared_workspace_bytes.restype = C.c_size_t
+        L.wq_tree_attention.argtypes = [vp, vp, i64, vp, i64, vp, i64, i32, i32, i32, C.POINTER(_PackedKV), vp, vp, i64, i32, f32, i32, i64, vp, vp]
+        L.wq_tree_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i64, i32, i32]
+        L.wq_tree_workspace_bytes.restype = C.c_size_t
+        L.wq_tree_accept.argtypes = [vp, vp, vp, vp, i32, vp, i64, i32, i32, vp, vp, vp]
+        L.wq_append_rows.argtypes = [vp, i32, C.POINTER(vp), i64, C.POINTER(vp), i64, i32, i32, vp, i64, vp, vp, i32, C.POINTER(_PackedKV)]
+        L.wq_copy_sequences.argtypes = [vp, i32, C.POINTER(_PackedKV), C.POINTER(_PackedKV), vp]
         L.wq_probe_stream.argtypes = [vp, vp, vp, i64, i32]
         L.wq_probe_mfma.argtypes = [vp, i32, i32, i32, C.POINTER(C.c_double)]
         L.wq_decode_timing.argtypes = [vp, i32]
@@ -469,6 +476,91 @@ def wq_decode_attention_shared(ctx: Context, q, prefix: PackedKV, req_off, own: 
                                                None if own is None else C.byref(own.desc), sm_scale, num_splits, max_prefix_tokens, max_own_tokens,
                                                _ptr(out), _ptr(lse)))
     return out
+
+
+# ------------------------------------------------------------------------------------------------------------
+# several new rows per sequence, copies of sequences
+# ------------------------------------------------------------------------------------------------------------
+def tree_workspace_bytes(total_rows: int, B: int, Hq: int, Hkv: int, hd: int, max_cache_tokens: int, max_rows: int, num_splits: int = 0) -> int:
+    return int(lib().wq_tree_workspace_bytes(total_rows, B, Hq, Hkv, hd, max_cache_tokens, max_rows, num_splits))
+
+
+def wq_tree_attention(ctx: Context, q, k, v, kv: PackedKV, row_off, sm_scale: float, parent: Optional[torch.Tensor] = None, max_rows: int = 0,
+                      max_cache_tokens: int = 0, num_splits: int = 0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None):
+    """New rows q [rows, Hq, hd], k, v [rows, Hkv, hd], row_off[b] .. row_off[b+1]-1 those of sequence b, over its cache and each other: along
+    parent [rows] (a tree; numbered within the sequence, -1: none), or every row the ones before it (None).  max_rows, max_cache_tokens 0: few parts."""
+    _here(ctx, q, k, v, row_off, parent, out, lse, kv.off16)
+    rows, Hq, hd, qs = _rows("q", q)
+    if hd != kv.hd:
+        raise ValueError("q: the head_dim of the cache expected")
+    shape = (rows, kv.Hkv, hd)
+    ks, vs = _rows("k", k, q, shape)[3], _rows("v", v, q, shape)[3]
+    _contiguous("row_off", row_off, torch.int32, kv.B + 1)
+    if parent is not None:
+        _contiguous("parent", parent, torch.int32, rows)
+    if out is None:
+        out = _like(q)
+    else:
+        _contiguous("out", out, q.dtype, q.numel())
+    if lse is not None:
+        _contiguous("lse", lse, torch.float32, rows * Hq)
+    ctx.check(lib().wq_tree_attention(ctx.handle, _ptr(q), qs, _ptr(k), ks, _ptr(v), vs, _dtype_id(q), kv.B, Hq, C.byref(kv.desc), _ptr(row_off), _ptr(parent),
+                                      rows, max_rows, sm_scale, num_splits, max_cache_tokens, _ptr(out), _ptr(lse)))
+    return out
+
+
+def wq_tree_accept(ctx: Context, tokens, target, row_off, parent: Optional[torch.Tensor] = None, max_rows: int = 1024, max_path: int = 64):
+    """(path [B, max_path], n_path [B], next_token [B]): the rows whose tokens the model agrees with, from every sequence's first row on."""
+    _here(ctx, tokens, target, row_off, parent)
+    rows, B = tokens.numel(), row_off.numel() - 1
+    for name, t, n in (("tokens", tokens, rows), ("target", target, rows), ("row_off", row_off, B + 1)) + ((("parent", parent, rows),) if parent is not None else ()):
+        _contiguous(name, t, torch.int32, n)
+    path = torch.empty(B, max(max_path, 0), dtype=torch.int32, device=ctx.device)
+    n_path, next_token = torch.empty(B, dtype=torch.int32, device=ctx.device), torch.empty(B, dtype=torch.int32, device=ctx.device)
+    ctx.check(lib().wq_tree_accept(ctx.handle, _ptr(tokens), _ptr(target), _ptr(parent), B, _ptr(row_off), rows, max_rows, max_path, _ptr(path), _ptr(n_path),
+                                   _ptr(next_token)))
+    return path, n_path, next_token
+
+
+def _descs(kvs: Sequence[PackedKV]):
+    return (_PackedKV * max(len(kvs), 1))(*[kv.desc for kv in kvs])
+
+
+def wq_append_rows(ctx: Context, k: Sequence[torch.Tensor], v: Sequence[torch.Tensor], kv: Sequence[PackedKV], row_off, max_take: int,
+                   take: Optional[torch.Tensor] = None, n_take: Optional[torch.Tensor] = None):
+    """Layer l's rows k[l], v[l] [rows, Hkv, hd] into kv[l]: those that take [B, max_take] and n_take [B] name, or all of a sequence's (None)."""
+    n = len(kv)
+    if n == 0 or len(k) != n or len(v) != n:
+        raise ValueError("k, v, kv: one of each for every layer expected")
+    first, B = k[0], kv[0].B
+    _here(ctx, row_off, take, n_take, *k, *v, *[c.off16 for c in kv])
+    rows, Hkv, hd, ks = _rows("k", first)
+    vs = _rows("v", v[0], first, (rows, Hkv, hd))[3]
+    for name, ts, stride in (("k", k, ks), ("v", v, vs)):
+        for t in ts:
+            if _rows(name, t, first, (rows, Hkv, hd))[3] != stride:
+                raise ValueError(f"{name}: the layers' rows are not equally far apart")
+    for c in kv:
+        if c.Hkv != Hkv or c.hd != hd:
+            raise ValueError("k: the KV heads and head_dim of the caches expected")
+    _contiguous("row_off", row_off, torch.int32, B + 1)
+    if (take is None) != (n_take is None):
+        raise ValueError("take and n_take go together")
+    if take is not None:
+        _contiguous("take", take, torch.int32, B * max_take)
+        _contiguous("n_take", n_take, torch.int32, B)
+    pointers = C.c_void_p * n
+    ctx.check(lib().wq_append_rows(ctx.handle, n, pointers(*[_ptr(t) for t in k]), ks, pointers(*[_ptr(t) for t in v]), vs, _dtype_id(first), B, _ptr(row_off), rows,
+                                   _ptr(take), _ptr(n_take), max_take, _descs(kv)))
+
+
+def wq_copy_sequences(ctx: Context, src: Sequence[PackedKV], dst: Sequence[PackedKV], from_seq):
+    """Sequence d of every layer's dst becomes a copy of sequence from_seq[d] of that layer's src (-1: an empty one); src and dst share no memory."""
+    if len(src) != len(dst) or not src:
+        raise ValueError("src, dst: one of each for every layer expected")
+    _here(ctx, from_seq, *[c.off16 for c in src], *[c.off16 for c in dst])
+    _contiguous("from_seq", from_seq, torch.int32, dst[0].B)
+    ctx.check(lib().wq_copy_sequences(ctx.handle, len(src), _descs(src), _descs(dst), _ptr(from_seq)))
 
 
 def wq_probe_mfma(ctx: Context, random_operands: bool, workgroups: int = 2048, iters: int = 1000) -> float:

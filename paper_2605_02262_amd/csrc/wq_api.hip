@@ -593,6 +593,121 @@ int wq_decode_attention_shared(wq_ctx* ctx, const void* q, int q_dtype, int B, i
     return wq_launch_shared(ctx, {q, q_dtype, B, Hq, prefix, own, req_off, sm_scale, plan, decode_splits, algo, out, lse});
 }
 
+// ---- several new rows per sequence, copies of sequences -------------------------------------------------------------------
+size_t wq_tree_workspace_bytes(int64_t total_rows, int B, int Hq, int Hkv, int hd, int64_t max_cache_tokens, int max_rows, int num_splits)
+{
+    if (total_rows <= 0 || B <= 0 || Hq <= 0 || Hkv <= 0 || hd <= 0 || Hq % Hkv != 0) return WQ_WS_HEADER;
+    const size_t a = wq_tree_plan(total_rows, B, Hq, Hkv, hd, WQ_F32, max_cache_tokens, max_rows, num_splits).bytes;
+    const size_t b = wq_tree_plan(total_rows, B, Hq, Hkv, hd, WQ_BF16, max_cache_tokens, max_rows, num_splits).bytes;
+    return WQ_WS_HEADER + (a > b ? a : b);
+}
+
+int wq_tree_attention(wq_ctx* ctx, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int dtype, int B, int Hq,
+                      const wq_packed_kv* kv, const int32_t* row_off, const int32_t* parent, int64_t total_rows, int max_rows, float sm_scale, int num_splits,
+                      int64_t max_cache_tokens, void* out, float* lse)
+{
+    if (!ctx) return WQ_ERR_ARG;
+    if (B < 0 || total_rows < 0 || max_rows < 0 || max_cache_tokens < 0) return wq_fail(ctx, WQ_ERR_ARG, "negative size");
+    if (!dtype_ok(dtype)) return wq_fail(ctx, WQ_ERR_ARG, "unknown dtype %d", dtype);
+    int rc = check_packed(ctx, kv, B, true);
+    if (rc != WQ_OK) return rc;
+    if (!aligned_cache(kv)) return wq_fail(ctx, WQ_ERR_ARG, "the cache's buffers must be 16-byte aligned");
+    if (Hq <= 0 || Hq % kv->Hkv != 0 || Hq / kv->Hkv > WQ_MAX_REP)
+        return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "Hq=%d must be a multiple of Hkv=%d, at most %d query heads per KV head", Hq, kv->Hkv, WQ_MAX_REP);
+    if (Hq > MOST_HEADS) return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "more than 2^18 heads");
+    if ((dtype == WQ_BF16) != (kv->dtype16 == WQ_BF16))
+        return wq_fail(ctx, WQ_ERR_ARG, "dtype16 must be bf16 for bf16 rows and fp16 for fp16/fp32 rows");
+    if (total_rows > INT32_MAX / WQ_MAX_REP - 256 || B > 65535) return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "too many rows or sequences");
+    if (parent && max_rows > WQ_MAX_TREE) return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "trees of more than %d rows", WQ_MAX_TREE);
+    if (num_splits < 0 || num_splits > WQ_MAX_ATTEND_SPLITS) return wq_fail(ctx, WQ_ERR_ARG, "num_splits out of range");
+    rc = check_scale(ctx, sm_scale);
+    if (rc != WQ_OK) return rc;
+    if (B == 0 || total_rows == 0) return WQ_OK;
+    if (!row_off || !out) return wq_fail(ctx, WQ_ERR_ARG, "NULL table or output");
+    if (!on_16_bytes(out)) return wq_fail(ctx, WQ_ERR_ARG, "out must be 16-byte aligned");
+    rc = check_rows(ctx, "q", q, q_stride, total_rows, Hq, kv->hd, dtype);
+    if (rc == WQ_OK) rc = check_rows(ctx, "k", k, k_stride, total_rows, kv->Hkv, kv->hd, dtype);
+    if (rc == WQ_OK) rc = check_rows(ctx, "v", v, v_stride, total_rows, kv->Hkv, kv->hd, dtype);
+    if (rc != WQ_OK) return rc;
+    if (k_stride > 1 << 22 || v_stride > 1 << 22)             // (offsets inside a tile have 32 bits)
+        return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "rows of k or v are more than 2^22 elements apart");
+    const WqTreePlan plan = wq_tree_plan(total_rows, B, Hq, kv->Hkv, kv->hd, dtype, max_cache_tokens, max_rows, num_splits, room_of(ctx));
+    if (plan.groups > MOST_GROUPS_512 || (plan.splits > 1 && total_rows * Hq > 4 * WQ_MOST_GROUPS_256)) return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "too many rows");
+    if (!ctx->ws || ctx->ws_bytes < WQ_WS_HEADER + plan.bytes)
+        return wq_fail(ctx, WQ_ERR_WORKSPACE, "workspace too small for %d splits of %lld rows", plan.splits, (long long)total_rows);
+    return wq_launch_tree(ctx, {q, k, v, q_stride, k_stride, v_stride, dtype, B, Hq, kv, plan, row_off, parent, total_rows, sm_scale, out, lse});
+}
+
+int wq_tree_accept(wq_ctx* ctx, const int32_t* tokens, const int32_t* target, const int32_t* parent, int B, const int32_t* row_off, int64_t total_rows, int max_rows,
+                   int max_path, int32_t* path, int32_t* n_path, int32_t* next_token)
+{
+    if (!ctx) return WQ_ERR_ARG;
+    if (B < 0 || total_rows < 0 || max_rows <= 0 || max_path <= 0) return wq_fail(ctx, WQ_ERR_ARG, "negative size, or no row");
+    if (max_rows > WQ_MAX_TREE) return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "trees of more than %d rows", WQ_MAX_TREE);
+    if (B > WQ_MOST_GROUPS_256) return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "too many sequences");
+    if (B == 0) return WQ_OK;
+    if (!row_off || !path || !n_path || !next_token || (total_rows > 0 && (!tokens || !target))) return wq_fail(ctx, WQ_ERR_ARG, "NULL table or output");
+    if (!ctx->ws || ctx->ws_bytes < WQ_WS_HEADER) return wq_fail(ctx, WQ_ERR_WORKSPACE, "no workspace");
+    return wq_launch_accept(ctx, {tokens, target, parent, row_off, B, max_rows, max_path, total_rows, path, n_path, next_token});
+}
+
+int wq_append_rows(wq_ctx* ctx, int n_layers, const void* const* k, int64_t k_stride, const void* const* v, int64_t v_stride, int dtype, int B, const int32_t* row_off,
+                   int64_t total_rows, const int32_t* take, const int32_t* n_take, int max_take, const wq_packed_kv* kv)
+{
+    if (!ctx) return WQ_ERR_ARG;
+    if (n_layers < 0 || B < 0 || total_rows < 0 || max_take < 0) return wq_fail(ctx, WQ_ERR_ARG, "negative size");
+    if (!dtype_ok(dtype)) return wq_fail(ctx, WQ_ERR_ARG, "unknown dtype %d", dtype);
+    if (n_layers == 0) return WQ_OK;
+    if (!k || !v || !kv) return wq_fail(ctx, WQ_ERR_ARG, "NULL array of layers");
+    if (!take != !n_take) return wq_fail(ctx, WQ_ERR_ARG, "take and n_take go together");
+    for (int l = 0; l < n_layers; l++) {
+        int rc = check_packed(ctx, kv + l, B, false);
+        if (rc != WQ_OK) return rc;
+        if (kv[l].Hkv != kv[0].Hkv || kv[l].hd != kv[0].hd || kv[l].dtype16 != kv[0].dtype16)
+            return wq_fail(ctx, WQ_ERR_ARG, "the layers' caches differ in Hkv, hd or dtype16");
+        if (kv[l].Hkv > MOST_HEADS) return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "more than 2^18 heads");
+        if (!on_16_bytes(kv[l].k16) || !on_16_bytes(kv[l].v16)) return wq_fail(ctx, WQ_ERR_ARG, "k16 and v16 must be 16-byte aligned");
+        rc = check_rows(ctx, "k", k[l], k_stride, total_rows, kv[l].Hkv, kv[l].hd, dtype);
+        if (rc == WQ_OK) rc = check_rows(ctx, "v", v[l], v_stride, total_rows, kv[l].Hkv, kv[l].hd, dtype);
+        if (rc != WQ_OK) return rc;
+    }
+    if ((dtype == WQ_BF16) != (kv[0].dtype16 == WQ_BF16))
+        return wq_fail(ctx, WQ_ERR_ARG, "dtype16 must be bf16 for bf16 input and fp16 for fp16/fp32 input");
+    if (B == 0 || total_rows == 0 || max_take == 0) return WQ_OK;
+    if (!row_off) return wq_fail(ctx, WQ_ERR_ARG, "NULL table");
+    if (!ctx->ws || ctx->ws_bytes < WQ_WS_HEADER) return wq_fail(ctx, WQ_ERR_WORKSPACE, "no workspace");
+    return wq_launch_append_rows(ctx, {n_layers, k, v, k_stride, v_stride, dtype, B, row_off, total_rows, take, n_take, max_take, kv});
+}
+
+int wq_copy_sequences(wq_ctx* ctx, int n_layers, const wq_packed_kv* src, const wq_packed_kv* dst, const int32_t* from)
+{
+    if (!ctx) return WQ_ERR_ARG;
+    if (n_layers < 0) return wq_fail(ctx, WQ_ERR_ARG, "negative size");
+    if (n_layers == 0) return WQ_OK;
+    if (!src || !dst) return wq_fail(ctx, WQ_ERR_ARG, "NULL array of layers");
+    for (int l = 0; l < n_layers; l++) {
+        for (const wq_packed_kv* kv : {src + l, dst + l}) {
+            const int B = kv == src + l ? src->B : dst->B;
+            if (B < 0 || B > 65535) return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "more than 65535 sequences");
+            const int rc = check_packed(ctx, kv, B, true);
+            if (rc != WQ_OK) return rc;
+            if (!aligned_cache(kv)) return wq_fail(ctx, WQ_ERR_ARG, "the caches' buffers must be 16-byte aligned");
+            if (kv->Hkv != src->Hkv || kv->hd != src->hd || kv->group != src->group || kv->dtype16 != src->dtype16)
+                return wq_fail(ctx, WQ_ERR_ARG, "the caches differ in Hkv, hd, group or dtype16");
+        }
+        const wq_packed_kv &x = src[l], &y = dst[l];
+        bool same = (y.k16 && y.k16 == x.k16) || (y.v16 && y.v16 == x.v16) || y.len16 == x.len16 || y.v_scale_max == x.v_scale_max;
+        for (int c = 0; c < 3; c++)
+            same = same || (y.codes[c] && y.codes[c] == x.codes[c]) || (y.meta[c] && y.meta[c] == x.meta[c]) || y.cls_off[c] == x.cls_off[c] || y.cls_len[c] == x.cls_len[c];
+        if (same) return wq_fail(ctx, WQ_ERR_ARG, "a cache is copied into memory that it is copied from");
+    }
+    if (dst->B == 0) return WQ_OK;
+    if (!from) return wq_fail(ctx, WQ_ERR_ARG, "from is NULL");
+    if (src->Hkv > MOST_HEADS) return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "more than 2^18 heads");
+    if (!ctx->ws || ctx->ws_bytes < WQ_WS_HEADER) return wq_fail(ctx, WQ_ERR_WORKSPACE, "no workspace");
+    return wq_launch_copy_sequences(ctx, n_layers, src, dst, from);
+}
+
 // ---- the entry point that allocates nothing ---------------------------------------------------------------------
 // Its workspace is this array, part of the code object: every GPU that loads the library holds its own copy at its own
 // address.  The name is a host-side stand-in for the symbol; the device address comes from hipGetSymbolAddress, once per

@@ -234,3 +234,46 @@ struct WqShared {
     float* lse;
 };
 int wq_launch_shared(wq_ctx* ctx, const WqShared& f);
+
+constexpr int WQ_MAX_TREE = 1024;      // rows of a tree: what a workgroup keeps of it in LDS
+struct WqTreePlan {
+    int rows, splits;                                             // query rows of a workgroup; parts of every row's keys
+    size_t bytes;                                                 // workspace
+    int64_t groups;                                               // workgroups
+};
+struct WqTree {
+    const void *q, *k, *v;
+    int64_t q_stride, k_stride, v_stride;                         // elements from row to row
+    int dtype, B, Hq;
+    const wq_packed_kv* kv;
+    WqTreePlan plan;
+    const int32_t *row_off, *parent;
+    int64_t total_rows;
+    float sm_scale;
+    void* out;
+    float* lse;
+};
+WqTreePlan wq_tree_plan(int64_t total_rows, int B, int Hq, int Hkv, int hd, int dtype, int64_t max_cache_tokens, int max_rows, int num_splits, size_t room = SIZE_MAX);
+int wq_launch_tree(wq_ctx* ctx, const WqTree& f);
+
+struct WqAccept {
+    const int32_t *tokens, *target, *parent, *row_off;
+    int B, max_rows, max_path;
+    int64_t total_rows;
+    int32_t *path, *n_path, *next_token;
+};
+int wq_launch_accept(wq_ctx* ctx, const WqAccept& f);
+
+struct WqAppendRows {
+    int n_layers;
+    const void *const *k, *const *v;                              // host arrays of a layer's rows each
+    int64_t k_stride, v_stride;                                   // elements from row to row
+    int dtype, B;
+    const int32_t* row_off;
+    int64_t total_rows;
+    const int32_t *take, *n_take;
+    int max_take;
+    const wq_packed_kv* kv;                                       // host array
+};
+int wq_launch_append_rows(wq_ctx* ctx, const WqAppendRows& f);
+int wq_launch_copy_sequences(wq_ctx* ctx, int n_layers, const wq_packed_kv* src, const wq_packed_kv* dst, const int32_t* from);

@@ -1,0 +1,198 @@
+// wq_tree_attention: several new rows of every sequence attend to its packed cache and to each other, along a tree of drafted tokens or as a
+// chain.  A row is a (new row, query head) pair, as in wq_attend.hip; its sequence's keys are the cache's tiles and, behind them, the new rows'.
+#include "wq_attend.h"
+
+namespace {
+
+struct TreeArgs {
+    const char *q, *k, *v;
+    int64_t q_stride, k_stride, v_stride;      // bytes from row to row
+    const int32_t *row_off, *parent;
+    int64_t total;
+    int B, Hq, rep;
+    int units, splits;                         // (tile of rows, KV head) pairs, and the parts that each one's keys are cut into
+    float scale;                               // log2(e) * sm_scale
+    uint32_t* status;
+    wq_packed_kv kv;
+    Out out;
+};
+
+constexpr int WORDS = WQ_MAX_TREE / 64;        // of a row's ancestors
+
+// Which new rows each of the rows node0 .. node0 + n - 1 sees, a bit each: itself, its parent, its parent's parent ..  (a parent lies in front of its
+// child, so every walk ends).  For all threads of a workgroup.
+__device__ __forceinline__ void find_ancestors(const int32_t* parent, int node0, int n, uint64_t* seen, int32_t* s_parent, int threads)
+{
+    const int last = node0 + n < WQ_MAX_TREE ? node0 + n : WQ_MAX_TREE;
+    for (int i = threadIdx.x; i < last; i += threads) s_parent[i] = parent[i];
+    for (int i = threadIdx.x; i < n * WORDS; i += threads) seen[i] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += threads) {
+        int j = node0 + i;
+        if (j >= WQ_MAX_TREE) continue;
+        uint64_t word = 0;
+        int at = j >> 6;
+        while (true) {
+            if (j >> 6 != at) seen[i * WORDS + at] = word, word = 0, at = j >> 6;
+            word |= uint64_t(1) << (j & 63);
+            const int up = s_parent[j];
+            if (up < 0 || up >= j) break;
+            j = up;
+        }
+        seen[i * WORDS + at] = word;
+    }
+    __syncthreads();
+}
+
+// The new rows that a row does not see
+struct Unrelated {
+    const uint64_t* seen;                      // NULL: a chain
+    int node[COLS];                            // the rows' places in it
+    template <typename CT, int HD>
+    __device__ __forceinline__ void hide(const Rows<HD>& r, Products<CT>& s, int key0) const
+    {
+        const int from = 4 * ((threadIdx.x & 63) >> 4) + (key0 & 63);          // this lane's first key in the word
+#pragma unroll
+        for (int n = 0; n < COLS; n++) {
+            uint64_t word;
+            if (seen) {
+                word = seen[node[n] * WORDS + (key0 >> 6)];
+            } else {
+                const int left = r.limit[n] - (key0 & ~63);
+                word = left >= 64 ? ~uint64_t(0) : (left <= 0 ? 0 : (uint64_t(1) << left) - 1);
+            }
+            word >>= from;
+#pragma unroll
+            for (int t = 0; t < KEYS<CT> / 16; t++)
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    if (!(word >> (16 * t + i) & 1)) s[t][n][i] = -INFINITY;
+        }
+    }
+};
+
+// QT, G: see walk_cache
+template <typename QT, int HD, int G>
+__global__ __launch_bounds__(64 * WAVES<QT>, 2) void k_tree(TreeArgs a)
+{
+    using CT = Walked<QT>;
+    constexpr bool PIPED = ESIZE<QT> == 2;
+    constexpr int BYTES = TILE_BYTES<CT, HD> * (1 + PIPED), R = ROWS<QT>, TK = KEYS<QT>;
+    __shared__ __align__(16) char s_k[BYTES], s_v[BYTES], s_m[G > 0 ? 2 * 64 * 4 * G : 16];
+    __shared__ uint64_t s_seen[(R + 1) * WORDS];
+    __shared__ int32_t s_parent[WQ_MAX_TREE];
+    const int Hkv = a.kv.Hkv, wave = this_wave(), lane = threadIdx.x & 63;
+    const wq_packed_kv& kv = a.kv;
+    const int unit = (int)blockIdx.x % a.units, split = (int)blockIdx.x / a.units, kvh = unit % Hkv;
+    Place p;
+    if (!find_place<R>(a.row_off, a.B, a.rep, a.total, unit / Hkv, p)) return;
+    const int n = p.rows / a.rep, node0 = p.row0 / a.rep;      // the sequence's new rows; the first one of this tile
+    if (a.parent && n > WQ_MAX_TREE && p.row0 == 0 && threadIdx.x == 0) atomicOr(a.status, WQ_DEV_TOO_MANY_ROWS);
+    const int last_row = (p.row0 + R < p.rows ? p.row0 + R : p.rows) - 1;
+    int tiles[4], len[4], newest = last_row / a.rep + 1;       // (no row sees one behind itself)
+    if (a.parent && newest > WQ_MAX_TREE) newest = WQ_MAX_TREE;
+    const int cached = tiles_of_cache<TK>(kv, p.seq, len, tiles), all = cached + (newest + TK - 1) / TK;
+    const int lo = (int)((int64_t)split * all / a.splits), hi = (int)((int64_t)(split + 1) * all / a.splits);
+
+    Rows<HD> r;
+    Query<CT, HD> q;
+    clear(r);
+    const int wrow0 = p.row0 + wave * COLS * 16;
+    const char* row_at[COLS];
+#pragma unroll
+    for (int c = 0; c < COLS; c++) {
+        const int row = wrow0 + 16 * c + (lane & 15);
+        row_at[c] = row < p.rows ? a.q + (p.first + row / a.rep) * a.q_stride + (kvh * a.rep + row % a.rep) * (HD * ESIZE<QT>) : nullptr;
+    }
+    const bool any = wrow0 < p.rows && wave * COLS * 16 < R;
+    walk_cache<QT, HD, G, true>(r, q, row_at, a.scale, kv, p.seq, kvh, len, tiles, lo, hi, any, (Lds)s_k, (Lds)s_v, (Lds)s_m);
+    if (hi > cached && lo < hi) {
+        const int t0 = lo > cached ? lo - cached : 0, t1 = hi - cached;
+        Unrelated unrelated;
+        unrelated.seen = a.parent ? s_seen : nullptr;
+        if (a.parent) find_ancestors(a.parent + p.first, node0, last_row / a.rep + 1 - node0, s_seen, s_parent, 64 * WAVES<QT>);
+#pragma unroll
+        for (int c = 0; c < COLS; c++) {
+            const int row = wrow0 + 16 * c + (lane & 15);
+            r.limit[c] = row < p.rows ? row / a.rep + 1 : 0;
+            unrelated.node[c] = row <= last_row ? row / a.rep - node0 : 0;
+            r.scale[c] = a.scale;
+            load_query<CT, HD>(q, c, row_at[c]);
+        }
+        const int least = a.parent || !any ? 0 : wrow0 / a.rep + 1, most = any ? newest : 0;
+        const char* k = a.k + p.first * a.k_stride + kvh * (HD * ESIZE<QT>);
+        const char* v = a.v + p.first * a.v_stride + kvh * (HD * ESIZE<QT>);
+        if constexpr (PIPED) {
+            walk_rows<QT, HD, false>(r, q, k, v, a.k_stride, a.v_stride, newest, t0, t1, least, (Lds)s_k, (Lds)s_v, unrelated);
+        } else {
+            for (int t = t0; t < t1; t++) {
+                const int key0 = t * TK;
+                __syncthreads();
+                stage_rows<F32, HD>(k + key0 * a.k_stride, v + key0 * a.v_stride, a.k_stride, a.v_stride, newest - key0, (Lds4)s_k, (Lds4)s_v);
+                __syncthreads();
+                attend_f32<HD>(r, q, (Lds4)s_k, (Lds4)s_v, key0, least, most, unrelated);
+            }
+        }
+    }
+    if (a.parent) {
+#pragma unroll
+        for (int c = 0; c < COLS; c++)
+            if ((wrow0 + 16 * c + (lane & 15)) / a.rep >= WQ_MAX_TREE) {        // refused: as if it saw nothing
+                r.ref[c] = -INFINITY, r.sum[c] = 0.f;
+#pragma unroll
+                for (int ct = 0; ct < HD / 16; ct++) r.o[ct][c] = f4{0.f, 0.f, 0.f, 0.f};
+            }
+    }
+    if (any) store_rows<QT, HD>(r, p, a.rep, a.Hq, kvh, wave, split, a.splits > 1 ? a.splits : 0, a.out);
+}
+
+auto tree_kernel(int dtype, int hd, int groups) -> void (*)(TreeArgs)
+{
+    if (dtype == WQ_F32) return hd == 128 ? k_tree<F32, 128, 0> : k_tree<F32, 64, 0>;
+    if (dtype == WQ_BF16) return hd == 128 ? k_tree<Bf16, 128, 0> : k_tree<Bf16, 64, 0>;
+    if (hd == 64) return groups == 1 ? k_tree<F16, 64, 1> : k_tree<F16, 64, 2>;
+    return groups == 1 ? k_tree<F16, 128, 1> : groups == 2 ? k_tree<F16, 128, 2> : k_tree<F16, 128, 4>;
+}
+
+}  // namespace
+
+WqTreePlan wq_tree_plan(int64_t total_rows, int B, int Hq, int Hkv, int hd, int dtype, int64_t max_cache_tokens, int max_rows, int num_splits, size_t room)
+{
+    const int rep = Hq / Hkv;
+    const int64_t used = total_rows < B ? total_rows : B;     // sequences that have rows
+    WqTreePlan s = {};
+    s.rows = dtype == WQ_F32 ? 128 : 256;
+    const int64_t units = tiles_of(total_rows, rep, B, s.rows) * Hkv;
+    s.splits = num_splits > 0 ? num_splits
+                              : auto_splits_of((tiles_of(total_rows, rep, 0, s.rows) + used) * Hkv, max_cache_tokens + max_rows, 256, dtype == WQ_F32 ? 32 : 64);
+    auto bytes = [&]() -> size_t { return s.splits > 1 ? partials_bytes(total_rows * Hq, hd, s.splits) : 0; };
+    while (num_splits <= 0 && s.splits > 1 && bytes() > room) s.splits--;
+    s.bytes = bytes();
+    s.groups = units * s.splits;
+    return s;
+}
+
+int wq_launch_tree(wq_ctx* ctx, const WqTree& f)
+{
+    TreeArgs a;
+    const int size = f.dtype == WQ_F32 ? 4 : 2, hd = f.kv->hd;
+    a.q = static_cast<const char*>(f.q), a.k = static_cast<const char*>(f.k), a.v = static_cast<const char*>(f.v);
+    a.q_stride = f.q_stride * size, a.k_stride = f.k_stride * size, a.v_stride = f.v_stride * size;
+    a.row_off = f.row_off, a.parent = f.parent;
+    a.total = f.total_rows;
+    a.B = f.B, a.Hq = f.Hq, a.rep = f.Hq / f.kv->Hkv, a.splits = f.plan.splits;
+    a.units = (int)(f.plan.groups / f.plan.splits);
+    a.scale = f.sm_scale * WQ_LOG2E;
+    a.status = wq_status_ptr(ctx);
+    a.kv = *f.kv;
+    a.out.out = f.out, a.out.lse = f.lse;
+    a.out.part = reinterpret_cast<float*>(ctx->ws + WQ_WS_HEADER);
+    a.out.part_ml = a.out.part + f.total_rows * f.Hq * a.splits * hd;
+    hipLaunchKernelGGL(tree_kernel(f.dtype, hd, hd / f.kv->group), dim3((unsigned)f.plan.groups), dim3(f.dtype == WQ_F32 ? 256 : 512), 0, ctx->stream, a);
+    if (a.splits > 1) {
+        const MergeArgs m = {f.total_rows * f.Hq, f.Hq, a.splits, f.dtype, f.row_off, f.B, a.out};
+        hipLaunchKernelGGL(hd == 128 ? k_merge<128> : k_merge<64>, dim3((unsigned)((m.rows + 3) / 4)), dim3(256), 0, ctx->stream, m);
+    }
+    WQ_HIP_CHECK(ctx, hipGetLastError());
+    return WQ_OK;
+}
