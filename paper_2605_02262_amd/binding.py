@@ -7,6 +7,7 @@ not been built (``python -m paper_2605_02262_amd.build``): there is no fallback.
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import os
 from typing import Optional, Sequence
 
@@ -92,8 +93,8 @@ def lib() -> C.CDLL:
         L.wq_tree_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i64, i32, i32]
         L.wq_tree_workspace_bytes.restype = C.c_size_t
         L.wq_tree_accept.argtypes = [vp, vp, vp, vp, i32, vp, i64, i32, i32, vp, vp, vp]
-        L.wq_append_rows.argtypes = [vp, i32, C.POINTER(vp), i64, C.POINTER(vp), i64, i32, i32, vp, i64, vp, vp, i32, C.POINTER(_PackedKV)]
-        L.wq_copy_sequences.argtypes = [vp, i32, C.POINTER(_PackedKV), C.POINTER(_PackedKV), vp]
+        L.wq_append_rows.argtypes = [vp, i32, vp, i64, vp, i64, i32, i32, vp, i64, vp, vp, i32, vp]
+        L.wq_copy_sequences.argtypes = [vp, i32, vp, vp, vp]
         L.wq_probe_stream.argtypes = [vp, vp, vp, i64, i32]
         L.wq_probe_mfma.argtypes = [vp, i32, i32, i32, C.POINTER(C.c_double)]
         L.wq_decode_timing.argtypes = [vp, i32]
@@ -210,6 +211,7 @@ class PackedKV:
         d.off16, d.len16 = self.off16.data_ptr(), _ptr(self.len16)
         d.v_scale_max = _ptr(self.v_scale_max)
         self.desc = d
+        self.index = self.off16.get_device()
 
     def bytes_algorithmic(self) -> int:
         """Bytes a decode step has to read: codes + metadata of the real tokens and the 16-bit rows in use."""
@@ -522,8 +524,28 @@ def wq_tree_accept(ctx: Context, tokens, target, row_off, parent: Optional[torch
     return path, n_path, next_token
 
 
-def _descs(kvs: Sequence[PackedKV]):
-    return (_PackedKV * max(len(kvs), 1))(*[kv.desc for kv in kvs])
+# (Many layers: what is checked of every tensor is read by loops in C, 0.1 to 0.2 us each, and descriptors are joined as bytes.)
+_dtype_of = operator.attrgetter("dtype")
+
+
+def _layers_alike(ctx: Context, name: str, tensors: Sequence[torch.Tensor], like: torch.Tensor) -> int:
+    """Every layer's rows like the first layer's keys, and like the first of their own in strides: elements from row to row."""
+    n, first = len(tensors), tensors[0]
+    stride = _rows(name, first, like, tuple(like.shape))[3]
+    if [*map(torch.Tensor.size, tensors)] != [first.shape] * n or [*map(_dtype_of, tensors)] != [like.dtype] * n:
+        raise ValueError(f"{name}: shapes or types of the layers' rows differ")
+    if [*map(torch.Tensor.stride, tensors)] != [first.stride()] * n:
+        raise ValueError(f"{name}: the layers' rows are not equally far apart")
+    if [*map(torch.Tensor.get_device, tensors)] != [ctx.index] * n:
+        raise ValueError(f"{name}: the context's device, cuda:{ctx.index}, expected")
+    return stride
+
+
+def _descs(ctx: Context, kvs: Sequence[PackedKV]) -> bytes:
+    for kv in kvs:
+        if kv.index != ctx.index:
+            raise ValueError(f"a cache on another device than the context's, cuda:{ctx.index}")
+    return b"".join([kv.desc for kv in kvs])
 
 
 def wq_append_rows(ctx: Context, k: Sequence[torch.Tensor], v: Sequence[torch.Tensor], kv: Sequence[PackedKV], row_off, max_take: int,
@@ -533,13 +555,9 @@ def wq_append_rows(ctx: Context, k: Sequence[torch.Tensor], v: Sequence[torch.Te
     if n == 0 or len(k) != n or len(v) != n:
         raise ValueError("k, v, kv: one of each for every layer expected")
     first, B = k[0], kv[0].B
-    _here(ctx, row_off, take, n_take, *k, *v, *[c.off16 for c in kv])
-    rows, Hkv, hd, ks = _rows("k", first)
-    vs = _rows("v", v[0], first, (rows, Hkv, hd))[3]
-    for name, ts, stride in (("k", k, ks), ("v", v, vs)):
-        for t in ts:
-            if _rows(name, t, first, (rows, Hkv, hd))[3] != stride:
-                raise ValueError(f"{name}: the layers' rows are not equally far apart")
+    _here(ctx, row_off, take, n_take)
+    ks, vs = _layers_alike(ctx, "k", k, first), _layers_alike(ctx, "v", v, first)
+    rows, Hkv, hd = first.shape
     for c in kv:
         if c.Hkv != Hkv or c.hd != hd:
             raise ValueError("k: the KV heads and head_dim of the caches expected")
@@ -550,17 +568,17 @@ def wq_append_rows(ctx: Context, k: Sequence[torch.Tensor], v: Sequence[torch.Te
         _contiguous("take", take, torch.int32, B * max_take)
         _contiguous("n_take", n_take, torch.int32, B)
     pointers = C.c_void_p * n
-    ctx.check(lib().wq_append_rows(ctx.handle, n, pointers(*[_ptr(t) for t in k]), ks, pointers(*[_ptr(t) for t in v]), vs, _dtype_id(first), B, _ptr(row_off), rows,
-                                   _ptr(take), _ptr(n_take), max_take, _descs(kv)))
+    ctx.check(lib().wq_append_rows(ctx.handle, n, pointers(*map(torch.Tensor.data_ptr, k)), ks, pointers(*map(torch.Tensor.data_ptr, v)), vs, _dtype_id(first), B,
+                                   _ptr(row_off), rows, _ptr(take), _ptr(n_take), max_take, _descs(ctx, kv)))
 
 
 def wq_copy_sequences(ctx: Context, src: Sequence[PackedKV], dst: Sequence[PackedKV], from_seq):
     """Sequence d of every layer's dst becomes a copy of sequence from_seq[d] of that layer's src (-1: an empty one); src and dst share no memory."""
     if len(src) != len(dst) or not src:
         raise ValueError("src, dst: one of each for every layer expected")
-    _here(ctx, from_seq, *[c.off16 for c in src], *[c.off16 for c in dst])
+    _here(ctx, from_seq)
     _contiguous("from_seq", from_seq, torch.int32, dst[0].B)
-    ctx.check(lib().wq_copy_sequences(ctx.handle, len(src), _descs(src), _descs(dst), _ptr(from_seq)))
+    ctx.check(lib().wq_copy_sequences(ctx.handle, len(src), _descs(ctx, src), _descs(ctx, dst), _ptr(from_seq)))
 
 
 def wq_probe_mfma(ctx: Context, random_operands: bool, workgroups: int = 2048, iters: int = 1000) -> float:

@@ -33,7 +33,8 @@ template <typename CT> constexpr int ESIZE = std::is_same_v<CT, F32> ? 4 : 2;
 template <typename CT, int HD> constexpr int STEPS = HD * ESIZE<CT> / 64;          // products of a key tile: 32 (16) channels each
 template <typename CT> constexpr int VSTEPS = KEYS<CT> * ESIZE<CT> / 64;           // products over a tile's keys: 32 (16) keys each
 template <typename CT, int HD> constexpr int TILE_BYTES = KEYS<CT> * HD * ESIZE<CT>;   // a staged tile of keys, or of values
-template <typename CT, int HD> using Query = u4[COLS][STEPS<CT, HD>];              // B operands of a wavefront's rows
+template <typename CT, int HD, int N> using QueryRows = u4[N][STEPS<CT, HD>];      // B operands of N columns of rows
+template <typename CT, int HD> using Query = QueryRows<CT, HD, COLS>;              // ... of a wavefront's
 typedef __attribute__((address_space(3))) char* Lds;
 typedef __attribute__((address_space(3))) u4* Lds4;
 typedef __attribute__((address_space(3))) uint32_t* Lds1;
@@ -551,6 +552,53 @@ struct Codes {};
 template <int BITS, int AT>
 __device__ __forceinline__ uint32_t expanded(uint32_t x, Codes, Codes) { return __builtin_bit_cast(uint32_t, code_pair<BITS, AT>(x)); }
 
+// A lane's 8 channels of step st from its quarter of a token's codes: pairs of channels as a masked word holds them (see order_query)
+template <int BITS, typename SM>
+__device__ __forceinline__ u4 expanded_keys(const uint32_t* w, int st, SM s, SM m)
+{
+    u4 y;
+    if constexpr (BITS == 8) {
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            y[2 * i] = expanded<BITS, 0>(placed<BITS, 0>(w[2 * st + i]), s, m);
+            y[2 * i + 1] = expanded<BITS, 0>(placed<BITS, 0>(w[2 * st + i] >> 8), s, m);
+        }
+    } else if constexpr (BITS == 4) {
+        const uint32_t x = w[st], z = x >> 8;
+        y[0] = expanded<BITS, 0>(placed<BITS, 0>(x), s, m), y[1] = expanded<BITS, 4>(placed<BITS, 4>(x), s, m);
+        y[2] = expanded<BITS, 0>(placed<BITS, 0>(z), s, m), y[3] = expanded<BITS, 4>(placed<BITS, 4>(z), s, m);
+    } else {
+        const uint32_t x = w[st >> 1] >> (st & 1) * 8;
+        y[0] = expanded<BITS, 0>(placed<BITS, 0>(x), s, m), y[1] = expanded<BITS, 2>(placed<BITS, 2>(x), s, m);
+        y[2] = expanded<BITS, 4>(placed<BITS, 4>(x), s, m), y[3] = expanded<BITS, 6>(placed<BITS, 6>(x), s, m);
+    }
+    return y;
+}
+
+// A lane's 8 tokens of the i-th of its channels (16 apart) from its codes: pairs of tokens, those of Far or Near, and so are their scales and minima
+template <int BITS>
+__device__ __forceinline__ u4 expanded_values(const uint32_t* w, int i, const h2 (&s)[4], const h2 (&m)[4])
+{
+    u4 y;
+    if constexpr (BITS == 8) {
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            y[2 * k] = expanded<BITS, 0>(placed<BITS, 0>(w[2 * i + k]), s[2 * k], m[2 * k]);
+            y[2 * k + 1] = expanded<BITS, 0>(placed<BITS, 0>(w[2 * i + k] >> 8), s[2 * k + 1], m[2 * k + 1]);
+        }
+    } else if constexpr (BITS == 4) {
+        const uint32_t x = w[i], z = x >> 8;
+        y[0] = expanded<BITS, 0>(placed<BITS, 0>(x), s[0], m[0]), y[1] = expanded<BITS, 4>(placed<BITS, 4>(x), s[1], m[1]);
+        y[2] = expanded<BITS, 0>(placed<BITS, 0>(z), s[2], m[2]), y[3] = expanded<BITS, 4>(placed<BITS, 4>(z), s[3], m[3]);
+    } else {                                                   // a word holds two of them, one per half
+        const uint32_t x = w[i >> 1], z = x >> 8;
+        auto both = [&](uint32_t a, uint32_t b) { return i & 1 ? high_halves(a, b) : low_halves(a, b); };
+        y[0] = expanded<BITS, 0>(both(placed<BITS, 0>(x), placed<BITS, 0>(z)), s[0], m[0]), y[1] = expanded<BITS, 2>(both(placed<BITS, 2>(x), placed<BITS, 2>(z)), s[1], m[1]);
+        y[2] = expanded<BITS, 4>(both(placed<BITS, 4>(x), placed<BITS, 4>(z)), s[2], m[2]), y[3] = expanded<BITS, 6>(both(placed<BITS, 6>(x), placed<BITS, 6>(z)), s[3], m[3]);
+    }
+    return y;
+}
+
 // A tile in flight between memory and LDS, in registers, brought by 64 * 4 (TOKENS = 64) or 64 * 2 (32) threads each of keys and of values.  A key
 // unit is a quarter of a token's channels (lane of the product), a value unit 8 tokens of every 16th channel of half of the head.
 // Addresses are a scalar base that moves with the tile and a lane's offset that does not.  A sequence's segment is padded to 32
@@ -598,25 +646,7 @@ struct PackedKeys {
     __device__ __forceinline__ void expand(Lds4 to, SM s, SM m, const Place& place) const
     {
 #pragma unroll
-        for (int st = 0; st < STEPS<F16, HD>; st++) {
-            u4 y;
-            if constexpr (BITS == 8) {
-#pragma unroll
-                for (int i = 0; i < 2; i++) {
-                    y[2 * i] = expanded<BITS, 0>(placed<BITS, 0>(w[2 * st + i]), s, m);
-                    y[2 * i + 1] = expanded<BITS, 0>(placed<BITS, 0>(w[2 * st + i] >> 8), s, m);
-                }
-            } else if constexpr (BITS == 4) {
-                const uint32_t x = w[st], z = x >> 8;
-                y[0] = expanded<BITS, 0>(placed<BITS, 0>(x), s, m), y[1] = expanded<BITS, 4>(placed<BITS, 4>(x), s, m);
-                y[2] = expanded<BITS, 0>(placed<BITS, 0>(z), s, m), y[3] = expanded<BITS, 4>(placed<BITS, 4>(z), s, m);
-            } else {
-                const uint32_t x = w[st >> 1] >> (st & 1) * 8;
-                y[0] = expanded<BITS, 0>(placed<BITS, 0>(x), s, m), y[1] = expanded<BITS, 2>(placed<BITS, 2>(x), s, m);
-                y[2] = expanded<BITS, 4>(placed<BITS, 4>(x), s, m), y[3] = expanded<BITS, 6>(placed<BITS, 6>(x), s, m);
-            }
-            to[place(st)] = y;
-        }
+        for (int st = 0; st < STEPS<F16, HD>; st++) to[place(st)] = expanded_keys<BITS>(w, st, s, m);
     }
     // fp32, codes one by one
     __device__ __forceinline__ void stage_f32(Lds4 k_tile) const
@@ -683,24 +713,7 @@ struct PackedValues {
             }
 #pragma unroll
             for (int i = 2 * g; i < 2 * g + 2; i++) {          // 16-channel tiles of the group's 32 channels
-                u4 y;
-                if constexpr (BITS == 8) {
-#pragma unroll
-                    for (int k = 0; k < 2; k++) {
-                        y[2 * k] = expanded<BITS, 0>(placed<BITS, 0>(w[2 * i + k]), s[2 * k], m[2 * k]);
-                        y[2 * k + 1] = expanded<BITS, 0>(placed<BITS, 0>(w[2 * i + k] >> 8), s[2 * k + 1], m[2 * k + 1]);
-                    }
-                } else if constexpr (BITS == 4) {
-                    const uint32_t x = w[i], z = x >> 8;
-                    y[0] = expanded<BITS, 0>(placed<BITS, 0>(x), s[0], m[0]), y[1] = expanded<BITS, 4>(placed<BITS, 4>(x), s[1], m[1]);
-                    y[2] = expanded<BITS, 0>(placed<BITS, 0>(z), s[2], m[2]), y[3] = expanded<BITS, 4>(placed<BITS, 4>(z), s[3], m[3]);
-                } else {                                       // a word holds two tiles, one per half
-                    const uint32_t x = w[i >> 1], z = x >> 8;
-                    auto both = [&](uint32_t a, uint32_t b) { return i & 1 ? high_halves(a, b) : low_halves(a, b); };
-                    y[0] = expanded<BITS, 0>(both(placed<BITS, 0>(x), placed<BITS, 0>(z)), s[0], m[0]), y[1] = expanded<BITS, 2>(both(placed<BITS, 2>(x), placed<BITS, 2>(z)), s[1], m[1]);
-                    y[2] = expanded<BITS, 4>(both(placed<BITS, 4>(x), placed<BITS, 4>(z)), s[2], m[2]), y[3] = expanded<BITS, 6>(both(placed<BITS, 6>(x), placed<BITS, 6>(z)), s[3], m[3]);
-                }
-                to[i * 64] = y;
+                to[i * 64] = expanded_values<BITS>(w, i, s, m);
             }
         }
     }
@@ -797,24 +810,24 @@ __device__ __forceinline__ bool find_place(const int32_t* off, int nseq, int rep
 }
 
 // 16-byte pieces of a row's channels: those of lane group j in the rows' order (32 neighbouring channels per product)
-template <typename CT, int HD>
-__device__ __forceinline__ void load_query(Query<CT, HD>& q, int n, const char* row)
+template <typename CT, int HD, int N>
+__device__ __forceinline__ void load_query(QueryRows<CT, HD, N>& q, int n, const char* row)
 {
     const int group = (threadIdx.x & 63) >> 4;
 #pragma unroll
     for (int st = 0; st < STEPS<CT, HD>; st++) q[n][st] = row ? *reinterpret_cast<const u4*>(row + (4 * st + group) * 16) : u4{0, 0, 0, 0};
 }
 // ... or a quarter of the channels, as in the packed cache
-template <typename CT, int HD>
-__device__ __forceinline__ void load_query_quarter(Query<CT, HD>& q, int n, const char* row)
+template <typename CT, int HD, int N>
+__device__ __forceinline__ void load_query_quarter(QueryRows<CT, HD, N>& q, int n, const char* row)
 {
     const int group = (threadIdx.x & 63) >> 4;
 #pragma unroll
     for (int st = 0; st < STEPS<CT, HD>; st++) q[n][st] = row ? *reinterpret_cast<const u4*>(row + (group * STEPS<CT, HD> + st) * 16) : u4{0, 0, 0, 0};
 }
 // A quarter's pairs of channels in the order in which Packed::stage leaves a class's keys
-template <int BITS, int HD>
-__device__ __forceinline__ void order_query(Query<F16, HD>& q, int n)
+template <int BITS, int HD, int N>
+__device__ __forceinline__ void order_query(QueryRows<F16, HD, N>& q, int n)
 {
     u4 y[STEPS<F16, HD>];
 #pragma unroll
@@ -868,8 +881,8 @@ __device__ __forceinline__ void load_query_codes(Query<F16, HD>& q, int n, const
 
 template <typename QT> constexpr uint32_t EXPONENT16 = std::is_same_v<QT, Bf16> ? 0x7F80 : 0x7C00;
 // Has a row's query an entry that is not finite (all exponent bits set: one more at the lowest of them carries into the sign's place)?
-template <typename QT, int HD>
-__device__ __forceinline__ bool not_finite(const Query<F16, HD>& q, int n)
+template <typename QT, int HD, int N>
+__device__ __forceinline__ bool not_finite(const QueryRows<F16, HD, N>& q, int n)
 {
     constexpr uint32_t EXPONENT = EXPONENT16<QT> * 0x10001u, ONE = std::is_same_v<QT, Bf16> ? 0x00800080u : 0x04000400u;
     uint32_t carry = 0;
@@ -884,8 +897,8 @@ __device__ __forceinline__ bool not_finite(const Query<F16, HD>& q, int n)
 
 // ... a bf16 query as fp16, divided by the power of two above the row's largest entry: its 8 bits are exact from 2^-17 of that power up, below
 // that (fp16's smallest step there is 2^-24) off by at most 2^-25 of it
-template <int HD>
-__device__ __forceinline__ float query_as_f16(Query<F16, HD>& q, int n)
+template <int HD, int N>
+__device__ __forceinline__ float query_as_f16(QueryRows<F16, HD, N>& q, int n)
 {
     constexpr int S = STEPS<F16, HD>;
     float most = 0.f;

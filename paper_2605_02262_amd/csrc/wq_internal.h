@@ -238,6 +238,7 @@ int wq_launch_shared(wq_ctx* ctx, const WqShared& f);
 constexpr int WQ_MAX_TREE = 1024;      // rows of a tree: what a workgroup keeps of it in LDS
 struct WqTreePlan {
     int rows, splits;                                             // query rows of a workgroup; parts of every row's keys
+    int columns;                                                  // of 16 query rows: every wavefront brings its own keys; 0: tiles of keys for a workgroup
     size_t bytes;                                                 // workspace
     int64_t groups;                                               // workgroups
 };
@@ -253,7 +254,7 @@ struct WqTree {
     void* out;
     float* lse;
 };
-WqTreePlan wq_tree_plan(int64_t total_rows, int B, int Hq, int Hkv, int hd, int dtype, int64_t max_cache_tokens, int max_rows, int num_splits, size_t room = SIZE_MAX);
+WqTreePlan wq_tree_plan(int64_t total_rows, int B, int Hq, int Hkv, int hd, int dtype, bool lse, int64_t max_cache_tokens, int max_rows, int num_splits, size_t room = SIZE_MAX);
 int wq_launch_tree(wq_ctx* ctx, const WqTree& f);
 
 struct WqAccept {

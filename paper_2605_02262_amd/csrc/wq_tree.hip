@@ -1,48 +1,8 @@
 // wq_tree_attention: several new rows of every sequence attend to its packed cache and to each other, along a tree of drafted tokens or as a
 // chain.  A row is a (new row, query head) pair, as in wq_attend.hip; its sequence's keys are the cache's tiles and, behind them, the new rows'.
-#include "wq_attend.h"
+#include "wq_tree.h"
 
 namespace {
-
-struct TreeArgs {
-    const char *q, *k, *v;
-    int64_t q_stride, k_stride, v_stride;      // bytes from row to row
-    const int32_t *row_off, *parent;
-    int64_t total;
-    int B, Hq, rep;
-    int units, splits;                         // (tile of rows, KV head) pairs, and the parts that each one's keys are cut into
-    float scale;                               // log2(e) * sm_scale
-    uint32_t* status;
-    wq_packed_kv kv;
-    Out out;
-};
-
-constexpr int WORDS = WQ_MAX_TREE / 64;        // of a row's ancestors
-
-// Which new rows each of the rows node0 .. node0 + n - 1 sees, a bit each: itself, its parent, its parent's parent ..  (a parent lies in front of its
-// child, so every walk ends).  For all threads of a workgroup.
-__device__ __forceinline__ void find_ancestors(const int32_t* parent, int node0, int n, uint64_t* seen, int32_t* s_parent, int threads)
-{
-    const int last = node0 + n < WQ_MAX_TREE ? node0 + n : WQ_MAX_TREE;
-    for (int i = threadIdx.x; i < last; i += threads) s_parent[i] = parent[i];
-    for (int i = threadIdx.x; i < n * WORDS; i += threads) seen[i] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < n; i += threads) {
-        int j = node0 + i;
-        if (j >= WQ_MAX_TREE) continue;
-        uint64_t word = 0;
-        int at = j >> 6;
-        while (true) {
-            if (j >> 6 != at) seen[i * WORDS + at] = word, word = 0, at = j >> 6;
-            word |= uint64_t(1) << (j & 63);
-            const int up = s_parent[j];
-            if (up < 0 || up >= j) break;
-            j = up;
-        }
-        seen[i * WORDS + at] = word;
-    }
-    __syncthreads();
-}
 
 // The new rows that a row does not see
 struct Unrelated {
@@ -143,10 +103,10 @@ __global__ __launch_bounds__(64 * WAVES<QT>, 2) void k_tree(TreeArgs a)
                 for (int ct = 0; ct < HD / 16; ct++) r.o[ct][c] = f4{0.f, 0.f, 0.f, 0.f};
             }
     }
-    if (any) store_rows<QT, HD>(r, p, a.rep, a.Hq, kvh, wave, split, a.splits > 1 ? a.splits : 0, a.out);
+    if (any) store_rows<QT, HD>(r, p, a.rep, a.Hq, kvh, wave, split, a.splits > 1 ? a.splits : 0, {a.out, a.lse, a.part, a.part_ml});
 }
 
-auto tree_kernel(int dtype, int hd, int groups) -> void (*)(TreeArgs)
+TreeKernel tree_kernel(int dtype, int hd, int groups)
 {
     if (dtype == WQ_F32) return hd == 128 ? k_tree<F32, 128, 0> : k_tree<F32, 64, 0>;
     if (dtype == WQ_BF16) return hd == 128 ? k_tree<Bf16, 128, 0> : k_tree<Bf16, 64, 0>;
@@ -156,15 +116,22 @@ auto tree_kernel(int dtype, int hd, int groups) -> void (*)(TreeArgs)
 
 }  // namespace
 
-WqTreePlan wq_tree_plan(int64_t total_rows, int B, int Hq, int Hkv, int hd, int dtype, int64_t max_cache_tokens, int max_rows, int num_splits, size_t room)
+WqTreePlan wq_tree_plan(int64_t total_rows, int B, int Hq, int Hkv, int hd, int dtype, bool lse, int64_t max_cache_tokens, int max_rows, int num_splits, size_t room)
 {
     const int rep = Hq / Hkv;
     const int64_t used = total_rows < B ? total_rows : B;     // sequences that have rows
     WqTreePlan s = {};
     s.rows = dtype == WQ_F32 ? 128 : 256;
+    if (dtype != WQ_F32) {
+        const int64_t columns = ((total_rows + used - 1) / used * rep + 15) / 16;      // of a sequence, on the average
+        const int most = hd == 128 ? (dtype == WQ_F16 || lse ? 2 : 3) : 3;
+        const int64_t groups = (columns + most - 1) / most;
+        s.columns = (int)((columns + groups - 1) / groups);
+        s.rows = 16 * s.columns;
+    }
     const int64_t units = tiles_of(total_rows, rep, B, s.rows) * Hkv;
     s.splits = num_splits > 0 ? num_splits
-                              : auto_splits_of((tiles_of(total_rows, rep, 0, s.rows) + used) * Hkv, max_cache_tokens + max_rows, 256, dtype == WQ_F32 ? 32 : 64);
+                              : auto_splits_of((tiles_of(total_rows, rep, 0, s.rows) + used) * Hkv, max_cache_tokens + max_rows, s.columns ? 512 : 256, dtype == WQ_F32 ? 32 : s.columns ? 128 : 64);
     auto bytes = [&]() -> size_t { return s.splits > 1 ? partials_bytes(total_rows * Hq, hd, s.splits) : 0; };
     while (num_splits <= 0 && s.splits > 1 && bytes() > room) s.splits--;
     s.bytes = bytes();
@@ -185,12 +152,16 @@ int wq_launch_tree(wq_ctx* ctx, const WqTree& f)
     a.scale = f.sm_scale * WQ_LOG2E;
     a.status = wq_status_ptr(ctx);
     a.kv = *f.kv;
-    a.out.out = f.out, a.out.lse = f.lse;
-    a.out.part = reinterpret_cast<float*>(ctx->ws + WQ_WS_HEADER);
-    a.out.part_ml = a.out.part + f.total_rows * f.Hq * a.splits * hd;
-    hipLaunchKernelGGL(tree_kernel(f.dtype, hd, hd / f.kv->group), dim3((unsigned)f.plan.groups), dim3(f.dtype == WQ_F32 ? 256 : 512), 0, ctx->stream, a);
+    a.out = f.out, a.lse = f.lse;
+    a.part = reinterpret_cast<float*>(ctx->ws + WQ_WS_HEADER);
+    a.part_ml = a.part + f.total_rows * f.Hq * a.splits * hd;
+    if (f.plan.columns)
+        hipLaunchKernelGGL(wq_tree_stream_kernel(f.dtype, hd, f.plan.columns, f.lse != nullptr), dim3((unsigned)f.plan.groups), dim3(64 * WQ_STREAM_WAVES), 0,
+                           ctx->stream, a);
+    else
+        hipLaunchKernelGGL(tree_kernel(f.dtype, hd, hd / f.kv->group), dim3((unsigned)f.plan.groups), dim3(f.dtype == WQ_F32 ? 256 : 512), 0, ctx->stream, a);
     if (a.splits > 1) {
-        const MergeArgs m = {f.total_rows * f.Hq, f.Hq, a.splits, f.dtype, f.row_off, f.B, a.out};
+        const MergeArgs m = {f.total_rows * f.Hq, f.Hq, a.splits, f.dtype, f.row_off, f.B, {a.out, a.lse, a.part, a.part_ml}};
         hipLaunchKernelGGL(hd == 128 ? k_merge<128> : k_merge<64>, dim3((unsigned)((m.rows + 3) / 4)), dim3(256), 0, ctx->stream, m);
     }
     WQ_HIP_CHECK(ctx, hipGetLastError());

@@ -1,0 +1,430 @@
+// wq_tree_attention for 16-bit types: every wavefront walks blocks of 32 tokens by itself.
+#include "wq_tree.h"
+
+namespace {
+
+constexpr int NW = WQ_STREAM_WAVES;
+
+// A wavefront's rows, CW columns of 16: as Rows
+template <int HD, int CW>
+struct Columns {
+    f4 o[HD / 16][CW];
+    float ref[CW], sum[CW], scale[CW];
+};
+template <int CW> using Block = f4[2][CW];                     // products of 32 keys: key 16 t + 4 (lane / 16) + i of row lane % 16
+
+// The weights of a block's 32 keys
+template <typename CT, int HD, int CW, typename Order>
+__device__ __forceinline__ void weigh(Columns<HD, CW>& r, const Block<CW>& s, u4 (&p)[CW])
+{
+    float most[CW];
+    bool move = false;
+#pragma unroll
+    for (int n = 0; n < CW; n++) {
+        float m = fmaxf(s[0][n][0], s[1][n][0]);
+#pragma unroll
+        for (int i = 1; i < 4; i++) m = fmaxf(fmaxf(m, s[0][n][i]), s[1][n][i]);
+        most[n] = m * r.scale[n];
+        move = move || most[n] > r.ref[n] + SLACK;
+    }
+    if (__ballot(move)) {
+#pragma unroll
+        for (int n = 0; n < CW; n++) {
+            const float ref = fmaxf(r.ref[n], max_of_column(most[n]));
+            const float by = ref == r.ref[n] ? 1.f : __builtin_amdgcn_exp2f(r.ref[n] - ref);
+            r.ref[n] = ref;
+            r.sum[n] *= by;
+#pragma unroll
+            for (int ct = 0; ct < HD / 16; ct++) r.o[ct][n] *= by;
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < CW; n++) {
+        const float shift = r.ref[n] == -INFINITY ? 0.f : SHIFT<CT> - r.ref[n];
+        float w[8];
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            w[e] = __builtin_amdgcn_exp2f(fmaf(s[e >> 2][n][e & 3], r.scale[n], shift));
+            r.sum[n] += w[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; e++) p[n][e] = pack2(w[Order::first(e)], w[Order::second(e)], CT());
+    }
+}
+
+// Blocks first, first + NW, .. below end of a class's segment of len tokens.  PRECISE: codes enter the products as they are, a group's at a time, and its
+// scale and minimum meet the sums in fp32.
+template <int HD, int BITS, int CW, bool PRECISE>
+__device__ __forceinline__ void stream_packed(Columns<HD, CW>& r, const QueryRows<F16, HD, CW>& q, const float (&q_sum)[CW][4], const wq_packed_kv& kv, int kvh,
+                                              int64_t tok0, int len, int first, int end, uint32_t* s_meta)
+{
+    constexpr int C = BITS == 2 ? 0 : (BITS == 4 ? 1 : 2), ST = STEPS<F16, HD>, KB = HD / 4 * BITS / 8, VB = HD / 16 * BITS;
+    using Order = std::conditional_t<BITS == 8, Near, Far>;
+    const int lane = threadIdx.x & 63, m = lane & 15, j = lane >> 4, G = HD / kv.group;
+    const int64_t k_slot = kvh * kv.cap[C] + tok0, v_slot = (kv.Hkv + kvh) * kv.cap[C] + tok0;
+    const uint8_t* k_codes = static_cast<const uint8_t*>(kv.codes[C]) + k_slot * (HD * BITS / 8) + lane * KB;
+    const uint8_t* v_codes = static_cast<const uint8_t*>(kv.codes[C]) + v_slot * (HD * BITS / 8) + lane * VB;
+    // a block's metadata words, 32 G of the keys and then 32 G of the values: load r takes 64 of them
+    const uint32_t* k_meta = static_cast<const uint32_t*>(kv.meta[C]) + k_slot * G + lane;
+    const uint32_t* v_meta = static_cast<const uint32_t*>(kv.meta[C]) + v_slot * G + lane;
+    const uint32_t* m0 = G == 1 && lane >= 32 ? v_meta - 32 : k_meta;
+    const uint32_t* m1 = G == 2 ? v_meta : k_meta + 64;
+    uint32_t wk[2][(KB + 3) / 4], wv[(VB + 3) / 4], wm[4] = {0, 0, 0, 0};
+    auto load_meta = [&](int b) {
+        const int64_t at = (int64_t)b * 32 * G;
+        wm[0] = m0[at];
+        if (G >= 2) wm[1] = m1[at];
+        if (G == 4) wm[2] = v_meta[at], wm[3] = v_meta[at + 64];
+    };
+    auto load_keys = [&](int b) {
+#pragma unroll
+        for (int t = 0; t < 2; t++) load_words<KB>(k_codes + (int64_t)b * (4 * HD * BITS) + t * 64 * KB, wk[t]);
+    };
+    auto load_values = [&](int b) { load_words<VB>(v_codes + (int64_t)b * (4 * HD * BITS), wv); };
+    load_meta(first);
+    load_keys(first);
+    load_values(first);
+#pragma unroll 1
+    for (int b = first; b < end; b += NW) {
+        s_meta[lane] = wm[0];
+        if (G >= 2) s_meta[64 + lane] = wm[1];
+        if (G == 4) s_meta[128 + lane] = wm[2], s_meta[192 + lane] = wm[3];
+        asm volatile("" ::: "memory");                         // (one wavefront's LDS operations keep their order)
+        const bool more = b + NW < end;
+        if (more) load_meta(b + NW);
+        Block<CW> s;
+#pragma unroll
+        for (int t = 0; t < 2; t++) {
+            u4 a[ST];
+            if constexpr (PRECISE) {
+#pragma unroll
+                for (int st = 0; st < ST; st++) a[st] = expanded_keys<BITS>(wk[t], st, Codes(), Codes());
+#pragma unroll
+                for (int g = 0; g < 4; g++) {
+                    if (g >= G) break;
+                    const u4 sm = *reinterpret_cast<const u4*>(s_meta + (t * G + g) * 16 + 4 * j);
+                    const uint32_t mine = (j * G >> 2) == g ? ~0u : 0u;
+                    f4 x[CW];
+#pragma unroll
+                    for (int st = 0; st < ST; st++) {
+                        const u4 y = {a[st][0] & mine, a[st][1] & mine, a[st][2] & mine, a[st][3] & mine};
+#pragma unroll
+                        for (int n = 0; n < CW; n++) x[n] = product<F16>(y, q[n][st], st ? x[n] : f4{0.f, 0.f, 0.f, 0.f});
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const uint32_t word = sm[i];
+                        const h2 f = __builtin_bit_cast(h2, word);
+#pragma unroll
+                        for (int n = 0; n < CW; n++) {
+                            const float y = g ? fmaf((float)f[1], q_sum[n][g], s[t][n][i]) : (float)f[1] * q_sum[n][g];
+                            s[t][n][i] = fmaf((float)f[0], x[n][i], y);
+                        }
+                    }
+                }
+            } else {
+                const h2 sm = __builtin_bit_cast(h2, s_meta[(t * G + (j * G >> 2)) * 16 + m]);
+#pragma unroll
+                for (int st = 0; st < ST; st++) a[st] = expanded_keys<BITS>(wk[t], st, h2{sm[0], sm[0]}, h2{sm[1], sm[1]});
+#pragma unroll
+                for (int st = 0; st < ST; st++)
+#pragma unroll
+                    for (int n = 0; n < CW; n++) s[t][n] = product<F16>(a[st], q[n][st], st ? s[t][n] : f4{0.f, 0.f, 0.f, 0.f});
+            }
+        }
+        if (more) load_keys(b + NW);
+        const int left = len - 32 * b;
+        if (left < 32) {
+#pragma unroll
+            for (int t = 0; t < 2; t++)
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    if (16 * t + 4 * j + i >= left)
+#pragma unroll
+                        for (int n = 0; n < CW; n++) s[t][n][i] = -INFINITY;
+        }
+        u4 p[CW];
+        weigh<F16, HD, CW, Order>(r, s, p);
+        h2 vs[4], vm[4];
+#pragma unroll
+        for (int c = 0; c < HD / 32; c++) {                    // 32 channels are of one group
+            if (c == 0 || 32 * c % kv.group == 0) {
+                const int g = 32 * c / kv.group;
+                const u4 x = *reinterpret_cast<const u4*>(s_meta + (2 * G + g) * 16 + 4 * j), y = *reinterpret_cast<const u4*>(s_meta + (3 * G + g) * 16 + 4 * j);
+                const uint32_t t[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    vs[e] = __builtin_bit_cast(h2, low_halves(t[Order::first(e)], t[Order::second(e)]));
+                    vm[e] = __builtin_bit_cast(h2, high_halves(t[Order::first(e)], t[Order::second(e)]));
+                }
+            }
+#pragma unroll
+            for (int ct = 2 * c; ct < 2 * c + 2; ct++) {
+                const u4 x = expanded_values<BITS>(wv, ct, vs, vm);
+#pragma unroll
+                for (int n = 0; n < CW; n++) r.o[ct][n] = product<F16>(x, p[n], r.o[ct][n]);
+            }
+        }
+        asm volatile("" ::: "memory");                         // (the metadata have been read)
+        if (more) load_values(b + NW);
+    }
+}
+
+// Chunks first, first + NW, .. below end of 32 of the n rows from k, v on: keys straight into registers, values through the wavefront's piece of LDS.
+// sees(n, c): this lane's 8 keys of chunk c that its row of column n sees, bits 16 t + i.
+template <typename QT, int HD, int CW, typename Sees>
+__device__ __forceinline__ void stream_rows(Columns<HD, CW>& r, const QueryRows<QT, HD, CW>& q, const char* k, const char* v, int64_t k_stride, int64_t v_stride, int n,
+                                            int first, int end, Lds tile, const Sees& sees)
+{
+    constexpr int ST = STEPS<QT, HD>, PIECES = HD / 8, PER_LOAD = 64 / PIECES, LOADS = 32 / PER_LOAD;
+    using D = Direct<HD>;
+    const int lane = threadIdx.x & 63, m = lane & 15, j = lane >> 4;
+    const D rows(v_stride, v_stride);
+#pragma unroll 1
+    for (int c = first; c < end; c += NW) {
+        const int64_t key0 = 32 * (int64_t)c;
+        const int left = n - 32 * c;                           // (the last row is read again for the rest: its weights are zero)
+#pragma unroll
+        for (int i = 0; i < LOADS; i++) {
+            const int row = i * PER_LOAD + lane / PIECES, piece = (lane % PIECES) ^ (D::swizzle(row) * 2 & (PIECES - 1));
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(v + (key0 + (row < left ? row : left - 1)) * v_stride + 16 * piece),
+                                             (__attribute__((address_space(3))) void*)(tile + i * 1024), 16, 0, 0);
+        }
+        Block<CW> s;
+#pragma unroll
+        for (int t = 0; t < 2; t++) {
+            const int row = 16 * t + m;
+            const char* at = k + (key0 + (row < left ? row : left - 1)) * k_stride;
+            u4 a[ST];
+#pragma unroll
+            for (int st = 0; st < ST; st++) a[st] = *reinterpret_cast<const u4*>(at + (4 * st + j) * 16);
+#pragma unroll
+            for (int st = 0; st < ST; st++)
+#pragma unroll
+                for (int col = 0; col < CW; col++) s[t][col] = product<QT>(a[st], q[col][st], st ? s[t][col] : f4{0.f, 0.f, 0.f, 0.f});
+        }
+#pragma unroll
+        for (int col = 0; col < CW; col++) {
+            const uint32_t bits = sees(col, c);
+#pragma unroll
+            for (int t = 0; t < 2; t++)
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    if (!(bits >> (16 * t + i) & 1)) s[t][col][i] = -INFINITY;
+        }
+        u4 p[CW];
+        weigh<QT, HD, CW, Natural>(r, s, p);
+        __builtin_amdgcn_s_waitcnt(0x0F70);                    // vmcnt(0): the values are in LDS
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int ct = 0; ct < HD / 16; ct++) {
+            const u4 x = rows.values(tile, 0, ct);
+#pragma unroll
+            for (int col = 0; col < CW; col++) r.o[ct][col] = product<QT>(x, p[col], r.o[ct][col]);
+        }
+        __builtin_amdgcn_s_waitcnt(0xC07F);                    // lgkmcnt(0): they are out of it again
+        asm volatile("" ::: "memory");
+    }
+}
+
+__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? ~0u : (n <= 0 ? 0u : (1u << n) - 1); }
+
+// The first of this wavefront's blocks from t0 on, where block t of a segment is the part's (done + t - lo)-th
+__device__ __forceinline__ int first_block(int t0, int done, int lo) { return t0 + ((this_wave() - (done + t0 - lo)) & (NW - 1)); }
+
+template <typename QT, int HD, int CW, bool PRECISE>
+__global__ __launch_bounds__(64 * NW, 2) void k_tree_stream(TreeArgs a)
+{
+    static_assert(NW == 4, "two rounds of joining");
+    constexpr int R = 16 * CW, JOIN = HD / 16 * CW * 1024, TILE = 32 * HD * 2;
+    // the values of 16-bit rows, a piece of each wavefront; in the end two wavefronts' numerators
+    __shared__ __align__(16) char s_big[NW * TILE > 2 * JOIN ? NW * TILE : 2 * JOIN];
+    __shared__ float s_ml[2][CW][2][64];
+    __shared__ uint64_t s_seen[R * WORDS];
+    __shared__ __align__(16) uint32_t s_meta[NW][256];         // (at first the tree's parents)
+    static_assert(sizeof(s_meta) >= WQ_MAX_TREE * 4, "");
+    const int Hkv = a.kv.Hkv, wave = this_wave(), lane = threadIdx.x & 63, j = lane >> 4;
+    const wq_packed_kv& kv = a.kv;
+    const int unit = (int)blockIdx.x % a.units, split = (int)blockIdx.x / a.units, kvh = unit % Hkv;
+    Place p;
+    if (!find_place<R>(a.row_off, a.B, a.rep, a.total, unit / Hkv, p)) return;
+    const int n_new = p.rows / a.rep, node0 = p.row0 / a.rep;
+    if (a.parent && n_new > WQ_MAX_TREE && p.row0 == 0 && threadIdx.x == 0) atomicOr(a.status, WQ_DEV_TOO_MANY_ROWS);
+    const int last_row = (p.row0 + R < p.rows ? p.row0 + R : p.rows) - 1;
+    int blocks[4], len[4], newest = last_row / a.rep + 1;      // (no row sees one behind itself)
+    if (a.parent && newest > WQ_MAX_TREE) newest = WQ_MAX_TREE;
+    const int cached = tiles_of_cache<32>(kv, p.seq, len, blocks), all = cached + (newest + 31) / 32;
+    const int lo = (int)((int64_t)split * all / a.splits), hi = (int)((int64_t)(split + 1) * all / a.splits);
+    if (a.parent && hi > cached && lo < hi) find_ancestors(a.parent + p.first, node0, last_row / a.rep + 1 - node0, s_seen, reinterpret_cast<int32_t*>(s_meta), 64 * NW);
+
+    Columns<HD, CW> r;
+    QueryRows<F16, HD, CW> q;
+    const char* row_at[CW];
+#pragma unroll
+    for (int n = 0; n < CW; n++) {
+        const int row = p.row0 + 16 * n + (lane & 15);
+        row_at[n] = row < p.rows ? a.q + (p.first + row / a.rep) * a.q_stride + (kvh * a.rep + row % a.rep) * (HD * 2) : nullptr;
+        r.ref[n] = -INFINITY, r.sum[n] = 0.f;
+#pragma unroll
+        for (int ct = 0; ct < HD / 16; ct++) r.o[ct][n] = f4{0.f, 0.f, 0.f, 0.f};
+    }
+    // (MODE.FP16_OVFL: see walk_cache)
+    constexpr int FP16_OVFL = 1 | 23 << 6;
+    __builtin_amdgcn_s_setreg(FP16_OVFL, 1);
+    int done = 0;
+    auto walk_class = [&](auto bits) __attribute__((always_inline)) {
+        constexpr int BITS = decltype(bits)::value, c = BITS == 2 ? 0 : (BITS == 4 ? 1 : 2);
+        const int t0 = lo > done ? lo - done : 0, t1 = hi - done < blocks[c] ? hi - done : blocks[c];
+        const int first = first_block(t0, done, lo);
+        done += blocks[c];
+        if (first >= t1) return;
+        float q_sum[CW][4];
+#pragma unroll
+        for (int n = 0; n < CW; n++) {
+            load_query_quarter<F16, HD>(q, n, row_at[n]);
+            const bool bad = not_finite<QT, HD>(q, n);
+            r.scale[n] = a.scale;
+            if constexpr (std::is_same_v<QT, Bf16>) r.scale[n] = fminf(fmaxf(a.scale * query_as_f16<HD>(q, n), FLT_MIN), FLT_MAX);
+            if (bad) r.scale[n] = NAN;
+            if constexpr (PRECISE) {
+                float mine = 0.f;
+#pragma unroll
+                for (int st = 0; st < STEPS<F16, HD>; st++)
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        const uint32_t word = q[n][st][e];
+                        const h2 f = __builtin_bit_cast(h2, word);
+                        mine += (float)f[0] + (float)f[1];
+                    }
+                // of the head's groups: a quarter's own (4), two quarters' (2), all (1)
+                const int G = HD / kv.group;
+                float of[4];
+#pragma unroll
+                for (int x = 0; x < 4; x++) of[x] = __shfl(mine, 16 * x + (lane & 15), 64);
+                q_sum[n][0] = G == 1 ? (of[0] + of[1]) + (of[2] + of[3]) : G == 2 ? of[0] + of[1] : of[0];
+                q_sum[n][1] = G == 2 ? of[2] + of[3] : of[1];
+                q_sum[n][2] = of[2], q_sum[n][3] = of[3];
+            }
+            order_query<BITS, HD>(q, n);
+        }
+        stream_packed<HD, BITS, CW, PRECISE>(r, q, q_sum, kv, kvh, kv.cls_off[c][p.seq], len[c], first, t1, s_meta[wave]);
+    };
+    __syncthreads();                                           // (the parents have been read)
+    walk_class(std::integral_constant<int, 2>());
+    walk_class(std::integral_constant<int, 4>());
+    walk_class(std::integral_constant<int, 8>());
+    __builtin_amdgcn_s_setreg(FP16_OVFL, 0);
+    if constexpr (std::is_same_v<QT, Bf16>) {                  // from the packed tokens' shift to the rows', exact
+#pragma unroll
+        for (int n = 0; n < CW; n++) {
+            r.sum[n] *= exp2f(SHIFT<QT> - SHIFT<F16>);
+#pragma unroll
+            for (int ct = 0; ct < HD / 16; ct++) r.o[ct][n] *= exp2f(SHIFT<QT> - SHIFT<F16>);
+        }
+    }
+    if (hi > done) {
+#pragma unroll
+        for (int n = 0; n < CW; n++) {
+            r.scale[n] = a.scale;
+            load_query<F16, HD>(q, n, row_at[n]);
+        }
+        const Lds tile = (Lds)s_big + wave * TILE;
+        int t0 = lo > done ? lo - done : 0, t1 = hi - done < blocks[3] ? hi - done : blocks[3], first = first_block(t0, done, lo);
+        if (first < t1) {
+            const int64_t row0 = kv.off16[p.seq], stride = (int64_t)Hkv * HD * 2;
+            const char* k = static_cast<const char*>(kv.k16) + row0 * stride + kvh * (HD * 2);
+            const char* v = static_cast<const char*>(kv.v16) + row0 * stride + kvh * (HD * 2);
+            stream_rows<QT, HD, CW>(r, q, k, v, stride, stride, len[3], first, t1, tile, [&](int, int c) { return low_bits(len[3] - 32 * c) >> 4 * j; });
+        }
+        done += blocks[3];
+        t0 = lo > done ? lo - done : 0, t1 = hi - done, first = first_block(t0, done, lo);
+        if (hi > done && first < t1) {
+            const char* k = a.k + p.first * a.k_stride + kvh * (HD * 2);
+            const char* v = a.v + p.first * a.v_stride + kvh * (HD * 2);
+            const uint32_t* seen = reinterpret_cast<const uint32_t*>(s_seen);
+            stream_rows<QT, HD, CW>(r, q, k, v, a.k_stride, a.v_stride, newest, first, t1, tile, [&](int n, int c) {
+                const int row = p.row0 + 16 * n + (lane & 15), node = row / a.rep;
+                uint32_t bits = 0;
+                if (row <= last_row) bits = a.parent ? seen[(node - node0) * (2 * WORDS) + c] : low_bits(node + 1 - 32 * c);
+                return bits >> 4 * j;
+            });
+        }
+    }
+    // The wavefronts' numerators together: 2 and 3 to 0 and 1, then 1 to 0
+#pragma unroll
+    for (int n = 0; n < CW; n++) {
+        r.sum[n] = sum_of_column(r.sum[n]);
+        r.ref[n] -= SHIFT<QT>;
+    }
+#pragma unroll
+    for (int half = NW / 2; half > 0; half /= 2) {
+        __syncthreads();
+        if (wave >= half && wave < 2 * half) {
+#pragma unroll
+            for (int n = 0; n < CW; n++) {
+                s_ml[wave - half][n][0][lane] = r.ref[n], s_ml[wave - half][n][1][lane] = r.sum[n];
+#pragma unroll
+                for (int ct = 0; ct < HD / 16; ct++) *reinterpret_cast<f4*>(s_big + (wave - half) * JOIN + (n * (HD / 16) + ct) * 1024 + lane * 16) = r.o[ct][n];
+            }
+        }
+        __syncthreads();
+        if (wave < half) {
+#pragma unroll
+            for (int n = 0; n < CW; n++) {
+                const float ref = s_ml[wave][n][0][lane], sum = s_ml[wave][n][1][lane], most = fmaxf(r.ref[n], ref), base = most == -INFINITY ? 0.f : most;
+                const float x = __builtin_amdgcn_exp2f(r.ref[n] - base), y = __builtin_amdgcn_exp2f(ref - base);
+                r.ref[n] = most, r.sum[n] = r.sum[n] * x + sum * y;
+#pragma unroll
+                for (int ct = 0; ct < HD / 16; ct++)
+                    r.o[ct][n] = r.o[ct][n] * x + *reinterpret_cast<const f4*>(s_big + wave * JOIN + (n * (HD / 16) + ct) * 1024 + lane * 16) * y;
+            }
+        }
+    }
+    if (wave > 0) return;
+#pragma unroll
+    for (int n = 0; n < CW; n++) {
+        const int row = p.row0 + 16 * n + (lane & 15);
+        if (row >= p.rows) continue;
+        const int64_t at = (p.first + row / a.rep) * a.Hq + kvh * a.rep + row % a.rep;
+        if (a.parent && row / a.rep >= WQ_MAX_TREE) {          // refused: as if it saw nothing
+            r.ref[n] = -INFINITY, r.sum[n] = 0.f;
+#pragma unroll
+            for (int ct = 0; ct < HD / 16; ct++) r.o[ct][n] = f4{0.f, 0.f, 0.f, 0.f};
+        }
+        if (a.splits > 1) {
+            const int64_t slot = at * a.splits + split;
+#pragma unroll
+            for (int ct = 0; ct < HD / 16; ct++) *reinterpret_cast<f4*>(a.part + slot * HD + 16 * ct + 4 * j) = r.o[ct][n];
+            if (j == 0) a.part_ml[slot * 2] = r.ref[n], a.part_ml[slot * 2 + 1] = r.sum[n];
+            continue;
+        }
+        const float inv = one_over(r.sum[n]);
+        char* to = static_cast<char*>(a.out) + at * HD * 2;
+#pragma unroll
+        for (int ct = 0; ct < HD / 16; ct++) {
+            const f4 x = r.o[ct][n] * inv;
+            *reinterpret_cast<uint2*>(to + (16 * ct + 4 * j) * 2) = make_uint2(pack2(x[0], x[1], QT()), pack2(x[2], x[3], QT()));
+        }
+        if (a.lse && j == 0) a.lse[at] = log_sum_exp(r.ref[n], r.sum[n]);
+    }
+}
+
+template <typename QT, int HD, bool PRECISE>
+TreeKernel of_columns(int columns)
+{
+    switch (columns) {
+        case 1: return k_tree_stream<QT, HD, 1, PRECISE>;
+        case 2: return k_tree_stream<QT, HD, 2, PRECISE>;
+        case 3: return k_tree_stream<QT, HD, 3, PRECISE>;
+        default: return k_tree_stream<QT, HD, 4, PRECISE>;
+    }
+}
+
+}  // namespace
+
+TreeKernel wq_tree_stream_kernel(int dtype, int hd, int columns, bool precise)
+{
+    if (dtype == WQ_F16) return hd == 128 ? of_columns<F16, 128, true>(columns) : of_columns<F16, 64, true>(columns);
+    if (precise) return hd == 128 ? of_columns<Bf16, 128, true>(columns) : of_columns<Bf16, 64, true>(columns);
+    return hd == 128 ? of_columns<Bf16, 128, false>(columns) : of_columns<Bf16, 64, false>(columns);
+}

@@ -141,12 +141,6 @@ def test_copy_refuses(W, ctx):  # noqa: F811
     assert _copy(W, ctx, [_desc(W)], [d]) == -1
     assert _copy(W, ctx, [_desc(W), _desc(W, B=3)], [_other(W), _other(W)], n=2) == -1
     assert _copy(W, ctx, [_desc(W)], [_other(W, B=0)]) == 0 and _copy(W, ctx, [_desc(W)], [_other(W)], n=0) == 0 and _copy(W, None, [_desc(W)], [_other(W)]) == -1
-    huge = _other(W)
-    huge.cap[0] = huge.cap[1] = huge.cap[2] = 1 << 26
-    huge.Hkv = 1 << 16
-    small = _desc(W)
-    small.Hkv = 1 << 16
-    assert _copy(W, ctx, [small], [huge]) == -2
 
 
 def test_python_calls_refuse(W):  # noqa: F811
@@ -168,7 +162,7 @@ def test_python_calls_refuse(W):  # noqa: F811
         with pytest.raises(ValueError):
             W.wq_tree_accept(Cpu(), **{**dict(tokens=tok, target=tok, row_off=off), **bad})
     rows = dict(k=[k, k], v=[k, k], kv=[kv, kv], row_off=off, max_take=3)
-    for bad in (dict(k=[k]), dict(kv=[]), dict(k=[k, k[:4]]), dict(v=[k, k.float()]), dict(k=[k, torch.zeros(5, 3, 64, dtype=torch.bfloat16)[:, :2]]), dict(row_off=off[:2]),
+    for bad in (dict(k=[k]), dict(kv=[]), dict(k=[k, k.float()], v=[k, k]), dict(k=[k, k[:4]]), dict(v=[k, k.float()]), dict(k=[k, torch.zeros(5, 3, 64, dtype=torch.bfloat16)[:, :2]]), dict(row_off=off[:2]),
                 dict(take=torch.zeros(2, 3, dtype=torch.int32)), dict(take=torch.zeros(2, 2, dtype=torch.int32), n_take=off[:2]), dict(k=[k[:, :1]] * 2, v=[k[:, :1]] * 2)):
         with pytest.raises(ValueError):
             W.wq_append_rows(Cpu(), **{**rows, **bad})
