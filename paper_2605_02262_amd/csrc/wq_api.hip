@@ -600,7 +600,7 @@ size_t wq_tree_workspace_bytes(int64_t total_rows, int B, int Hq, int Hkv, int h
     size_t most = 0;
     for (const int dtype : {WQ_F32, WQ_BF16, WQ_F16})
         for (const bool with_lse : {false, true}) {
-            const size_t bytes = wq_tree_plan(total_rows, B, Hq, Hkv, hd, dtype, with_lse, max_cache_tokens, max_rows, num_splits).bytes;
+            const size_t bytes = wq_tree_plan(total_rows, B, Hq, Hkv, hd, dtype, with_lse, max_cache_tokens, B * max_cache_tokens / 2, max_rows, num_splits).bytes;
             most = bytes > most ? bytes : most;
         }
     return WQ_WS_HEADER + most;
@@ -635,7 +635,8 @@ int wq_tree_attention(wq_ctx* ctx, const void* q, int64_t q_stride, const void* 
     if (rc != WQ_OK) return rc;
     if (k_stride > 1 << 22 || v_stride > 1 << 22)             // (offsets inside a tile have 32 bits)
         return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "rows of k or v are more than 2^22 elements apart");
-    const WqTreePlan plan = wq_tree_plan(total_rows, B, Hq, kv->Hkv, kv->hd, dtype, lse != nullptr, max_cache_tokens, max_rows, num_splits, room_of(ctx));
+    const WqTreePlan plan = wq_tree_plan(total_rows, B, Hq, kv->Hkv, kv->hd, dtype, lse != nullptr, max_cache_tokens,
+                                         kv->cap[0] + kv->cap[1] + kv->cap[2] + kv->cap16, max_rows, num_splits, room_of(ctx));
     if (plan.groups > MOST_GROUPS_512 || (plan.splits > 1 && total_rows * Hq > 4 * WQ_MOST_GROUPS_256)) return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "too many rows");
     if (!ctx->ws || ctx->ws_bytes < WQ_WS_HEADER + plan.bytes)
         return wq_fail(ctx, WQ_ERR_WORKSPACE, "workspace too small for %d splits of %lld rows", plan.splits, (long long)total_rows);

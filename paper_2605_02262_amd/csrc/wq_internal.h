@@ -239,8 +239,9 @@ constexpr int WQ_MAX_TREE = 1024;      // rows of a tree: what a workgroup keeps
 struct WqTreePlan {
     int rows, splits;                                             // query rows of a workgroup; parts of every row's keys
     int columns;                                                  // of 16 query rows: every wavefront brings its own keys; 0: tiles of keys for a workgroup
+    int longest;                                                  // blocks of 32 keys of the longest sequence: shorter ones have fewer parts; 0: all have the same
     size_t bytes;                                                 // workspace
-    int64_t groups;                                               // workgroups
+    int64_t units, groups;                                        // tiles of query rows times KV heads; workgroups
 };
 struct WqTree {
     const void *q, *k, *v;
@@ -254,7 +255,9 @@ struct WqTree {
     void* out;
     float* lse;
 };
-WqTreePlan wq_tree_plan(int64_t total_rows, int B, int Hq, int Hkv, int hd, int dtype, bool lse, int64_t max_cache_tokens, int max_rows, int num_splits, size_t room = SIZE_MAX);
+// slots: tokens that the cache has room for, 0: not known
+WqTreePlan wq_tree_plan(int64_t total_rows, int B, int Hq, int Hkv, int hd, int dtype, bool lse, int64_t max_cache_tokens, int64_t slots, int max_rows, int num_splits,
+                        size_t room = SIZE_MAX);
 int wq_launch_tree(wq_ctx* ctx, const WqTree& f);
 
 struct WqAccept {

@@ -14,12 +14,14 @@ struct TreeArgs {
     wq_packed_kv kv;
     void* out;                                 // as in Out
     float *lse, *part, *part_ml;
+    int longest;                               // wavefronts that bring their own keys: blocks of 32 keys of the longest sequence, or 0
 };
 
 typedef void (*TreeKernel)(TreeArgs);
-// The kernel in which every wavefront brings its own keys, for tiles of 16 * columns query rows
-TreeKernel wq_tree_stream_kernel(int dtype, int hd, int columns, bool precise);
+// The kernel in which every wavefront brings its own keys, for tiles of 16 * columns query rows: see wq_tree_stream.hip
 constexpr int WQ_STREAM_WAVES = 4;
+constexpr int WQ_STREAM_SLOTS = 512;           // workgroups that the card holds at a time
+void wq_launch_tree_stream(wq_ctx* ctx, const TreeArgs& a, int dtype, int columns);
 
 namespace {
 

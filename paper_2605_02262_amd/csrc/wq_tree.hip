@@ -31,14 +31,11 @@ struct Unrelated {
     }
 };
 
-// QT, G: see walk_cache
-template <typename QT, int HD, int G>
-__global__ __launch_bounds__(64 * WAVES<QT>, 2) void k_tree(TreeArgs a)
+template <int HD>
+__global__ __launch_bounds__(64 * WAVES<F32>, 2) void k_tree(TreeArgs a)
 {
-    using CT = Walked<QT>;
-    constexpr bool PIPED = ESIZE<QT> == 2;
-    constexpr int BYTES = TILE_BYTES<CT, HD> * (1 + PIPED), R = ROWS<QT>, TK = KEYS<QT>;
-    __shared__ __align__(16) char s_k[BYTES], s_v[BYTES], s_m[G > 0 ? 2 * 64 * 4 * G : 16];
+    constexpr int BYTES = TILE_BYTES<F32, HD>, R = ROWS<F32>, TK = KEYS<F32>;
+    __shared__ __align__(16) char s_k[BYTES], s_v[BYTES];
     __shared__ uint64_t s_seen[(R + 1) * WORDS];
     __shared__ int32_t s_parent[WQ_MAX_TREE];
     const int Hkv = a.kv.Hkv, wave = this_wave(), lane = threadIdx.x & 63;
@@ -55,43 +52,39 @@ __global__ __launch_bounds__(64 * WAVES<QT>, 2) void k_tree(TreeArgs a)
     const int lo = (int)((int64_t)split * all / a.splits), hi = (int)((int64_t)(split + 1) * all / a.splits);
 
     Rows<HD> r;
-    Query<CT, HD> q;
+    Query<F32, HD> q;
     clear(r);
     const int wrow0 = p.row0 + wave * COLS * 16;
     const char* row_at[COLS];
 #pragma unroll
     for (int c = 0; c < COLS; c++) {
         const int row = wrow0 + 16 * c + (lane & 15);
-        row_at[c] = row < p.rows ? a.q + (p.first + row / a.rep) * a.q_stride + (kvh * a.rep + row % a.rep) * (HD * ESIZE<QT>) : nullptr;
+        row_at[c] = row < p.rows ? a.q + (p.first + row / a.rep) * a.q_stride + (kvh * a.rep + row % a.rep) * (HD * 4) : nullptr;
     }
     const bool any = wrow0 < p.rows && wave * COLS * 16 < R;
-    walk_cache<QT, HD, G, true>(r, q, row_at, a.scale, kv, p.seq, kvh, len, tiles, lo, hi, any, (Lds)s_k, (Lds)s_v, (Lds)s_m);
+    walk_cache<F32, HD, 0, true>(r, q, row_at, a.scale, kv, p.seq, kvh, len, tiles, lo, hi, any, (Lds)s_k, (Lds)s_v, (Lds)s_k);
     if (hi > cached && lo < hi) {
         const int t0 = lo > cached ? lo - cached : 0, t1 = hi - cached;
         Unrelated unrelated;
         unrelated.seen = a.parent ? s_seen : nullptr;
-        if (a.parent) find_ancestors(a.parent + p.first, node0, last_row / a.rep + 1 - node0, s_seen, s_parent, 64 * WAVES<QT>);
+        if (a.parent) find_ancestors(a.parent + p.first, node0, last_row / a.rep + 1 - node0, s_seen, s_parent, 64 * WAVES<F32>);
 #pragma unroll
         for (int c = 0; c < COLS; c++) {
             const int row = wrow0 + 16 * c + (lane & 15);
             r.limit[c] = row < p.rows ? row / a.rep + 1 : 0;
             unrelated.node[c] = row <= last_row ? row / a.rep - node0 : 0;
             r.scale[c] = a.scale;
-            load_query<CT, HD>(q, c, row_at[c]);
+            load_query<F32, HD>(q, c, row_at[c]);
         }
         const int least = a.parent || !any ? 0 : wrow0 / a.rep + 1, most = any ? newest : 0;
-        const char* k = a.k + p.first * a.k_stride + kvh * (HD * ESIZE<QT>);
-        const char* v = a.v + p.first * a.v_stride + kvh * (HD * ESIZE<QT>);
-        if constexpr (PIPED) {
-            walk_rows<QT, HD, false>(r, q, k, v, a.k_stride, a.v_stride, newest, t0, t1, least, (Lds)s_k, (Lds)s_v, unrelated);
-        } else {
-            for (int t = t0; t < t1; t++) {
-                const int key0 = t * TK;
-                __syncthreads();
-                stage_rows<F32, HD>(k + key0 * a.k_stride, v + key0 * a.v_stride, a.k_stride, a.v_stride, newest - key0, (Lds4)s_k, (Lds4)s_v);
-                __syncthreads();
-                attend_f32<HD>(r, q, (Lds4)s_k, (Lds4)s_v, key0, least, most, unrelated);
-            }
+        const char* k = a.k + p.first * a.k_stride + kvh * (HD * 4);
+        const char* v = a.v + p.first * a.v_stride + kvh * (HD * 4);
+        for (int t = t0; t < t1; t++) {
+            const int key0 = t * TK;
+            __syncthreads();
+            stage_rows<F32, HD>(k + key0 * a.k_stride, v + key0 * a.v_stride, a.k_stride, a.v_stride, newest - key0, (Lds4)s_k, (Lds4)s_v);
+            __syncthreads();
+            attend_f32<HD>(r, q, (Lds4)s_k, (Lds4)s_v, key0, least, most, unrelated);
         }
     }
     if (a.parent) {
@@ -103,20 +96,12 @@ __global__ __launch_bounds__(64 * WAVES<QT>, 2) void k_tree(TreeArgs a)
                 for (int ct = 0; ct < HD / 16; ct++) r.o[ct][c] = f4{0.f, 0.f, 0.f, 0.f};
             }
     }
-    if (any) store_rows<QT, HD>(r, p, a.rep, a.Hq, kvh, wave, split, a.splits > 1 ? a.splits : 0, {a.out, a.lse, a.part, a.part_ml});
-}
-
-TreeKernel tree_kernel(int dtype, int hd, int groups)
-{
-    if (dtype == WQ_F32) return hd == 128 ? k_tree<F32, 128, 0> : k_tree<F32, 64, 0>;
-    if (dtype == WQ_BF16) return hd == 128 ? k_tree<Bf16, 128, 0> : k_tree<Bf16, 64, 0>;
-    if (hd == 64) return groups == 1 ? k_tree<F16, 64, 1> : k_tree<F16, 64, 2>;
-    return groups == 1 ? k_tree<F16, 128, 1> : groups == 2 ? k_tree<F16, 128, 2> : k_tree<F16, 128, 4>;
+    if (any) store_rows<F32, HD>(r, p, a.rep, a.Hq, kvh, wave, split, a.splits > 1 ? a.splits : 0, {a.out, a.lse, a.part, a.part_ml});
 }
 
 }  // namespace
 
-WqTreePlan wq_tree_plan(int64_t total_rows, int B, int Hq, int Hkv, int hd, int dtype, bool lse, int64_t max_cache_tokens, int max_rows, int num_splits, size_t room)
+WqTreePlan wq_tree_plan(int64_t total_rows, int B, int Hq, int Hkv, int hd, int dtype, bool lse, int64_t max_cache_tokens, int64_t slots, int max_rows, int num_splits, size_t room)
 {
     const int rep = Hq / Hkv;
     const int64_t used = total_rows < B ? total_rows : B;     // sequences that have rows
@@ -124,42 +109,68 @@ WqTreePlan wq_tree_plan(int64_t total_rows, int B, int Hq, int Hkv, int hd, int 
     s.rows = dtype == WQ_F32 ? 128 : 256;
     if (dtype != WQ_F32) {
         const int64_t columns = ((total_rows + used - 1) / used * rep + 15) / 16;      // of a sequence, on the average
-        const int most = hd == 128 ? (dtype == WQ_F16 || lse ? 2 : 3) : 3;
+        const int most = hd == 128 ? 3 : 4;
         const int64_t groups = (columns + most - 1) / most;
         s.columns = (int)((columns + groups - 1) / groups);
         s.rows = 16 * s.columns;
+        s.units = tiles_of(total_rows, rep, B, s.rows) * Hkv;
+        const int64_t real = (tiles_of(total_rows, rep, 0, s.rows) + used) * Hkv, blocks = (max_cache_tokens + 31) / 32 + (max_rows + 31) / 32;
+        // The cache's capacity says how long the sequences are on the average: those that are shorter than the longest have fewer pieces
+        const double average = slots > 0 && slots < (int64_t)B * max_cache_tokens ? (double)slots / ((double)B * max_cache_tokens) : 1.0;
+        s.longest = num_splits > 0 || blocks > 1 << 23 ? 0 : (int)blocks;
+        if (num_splits > 0) {
+            s.splits = num_splits;
+        } else {
+            // Rounds of workgroups, each of a piece's blocks by four wavefronts and what a start and an end take; pieces have to be joined
+            double best = 0;
+            s.splits = 1;
+            for (int p = 1; p <= WQ_MAX_ATTEND_SPLITS && p <= (blocks < 4 ? 1 : blocks); p++) {
+                const double groups = (double)real * p * average, rounds = groups <= WQ_STREAM_SLOTS ? 1 : ceil(groups / WQ_STREAM_SLOTS);
+                const double time = rounds * (ceil((double)blocks / p / 4) * 1.0 + 4) + (p > 1 ? 4 : 0);
+                if (p == 1 || time < best) best = time, s.splits = p;
+            }
+        }
+        auto size = [&] {
+            s.groups = s.units * s.splits;
+            s.bytes = s.splits > 1 ? wq_align256((size_t)s.groups * s.rows * (hd + 2) * 4) : 0;
+        };
+        size();
+        while (num_splits <= 0 && s.splits > 1 && s.bytes > room) s.splits--, size();
+        return s;
     }
     const int64_t units = tiles_of(total_rows, rep, B, s.rows) * Hkv;
-    s.splits = num_splits > 0 ? num_splits
-                              : auto_splits_of((tiles_of(total_rows, rep, 0, s.rows) + used) * Hkv, max_cache_tokens + max_rows, s.columns ? 512 : 256, dtype == WQ_F32 ? 32 : s.columns ? 128 : 64);
+    s.splits = num_splits > 0 ? num_splits : auto_splits_of((tiles_of(total_rows, rep, 0, s.rows) + used) * Hkv, max_cache_tokens + max_rows, 256, 32);
     auto bytes = [&]() -> size_t { return s.splits > 1 ? partials_bytes(total_rows * Hq, hd, s.splits) : 0; };
     while (num_splits <= 0 && s.splits > 1 && bytes() > room) s.splits--;
     s.bytes = bytes();
+    s.units = units;
     s.groups = units * s.splits;
     return s;
 }
 
 int wq_launch_tree(wq_ctx* ctx, const WqTree& f)
 {
-    TreeArgs a;
+    TreeArgs a = {};
     const int size = f.dtype == WQ_F32 ? 4 : 2, hd = f.kv->hd;
     a.q = static_cast<const char*>(f.q), a.k = static_cast<const char*>(f.k), a.v = static_cast<const char*>(f.v);
     a.q_stride = f.q_stride * size, a.k_stride = f.k_stride * size, a.v_stride = f.v_stride * size;
     a.row_off = f.row_off, a.parent = f.parent;
     a.total = f.total_rows;
     a.B = f.B, a.Hq = f.Hq, a.rep = f.Hq / f.kv->Hkv, a.splits = f.plan.splits;
-    a.units = (int)(f.plan.groups / f.plan.splits);
+    a.units = (int)f.plan.units;
     a.scale = f.sm_scale * WQ_LOG2E;
     a.status = wq_status_ptr(ctx);
     a.kv = *f.kv;
     a.out = f.out, a.lse = f.lse;
     a.part = reinterpret_cast<float*>(ctx->ws + WQ_WS_HEADER);
     a.part_ml = a.part + f.total_rows * f.Hq * a.splits * hd;
-    if (f.plan.columns)
-        hipLaunchKernelGGL(wq_tree_stream_kernel(f.dtype, hd, f.plan.columns, f.lse != nullptr), dim3((unsigned)f.plan.groups), dim3(64 * WQ_STREAM_WAVES), 0,
-                           ctx->stream, a);
-    else
-        hipLaunchKernelGGL(tree_kernel(f.dtype, hd, hd / f.kv->group), dim3((unsigned)f.plan.groups), dim3(f.dtype == WQ_F32 ? 256 : 512), 0, ctx->stream, a);
+    if (f.plan.columns) {
+        a.longest = f.plan.longest;
+        wq_launch_tree_stream(ctx, a, f.dtype, f.plan.columns);
+        WQ_HIP_CHECK(ctx, hipGetLastError());
+        return WQ_OK;
+    }
+    hipLaunchKernelGGL(hd == 128 ? k_tree<128> : k_tree<64>, dim3((unsigned)f.plan.groups), dim3(64 * WAVES<F32>), 0, ctx->stream, a);
     if (a.splits > 1) {
         const MergeArgs m = {f.total_rows * f.Hq, f.Hq, a.splits, f.dtype, f.row_off, f.B, {a.out, a.lse, a.part, a.part_ml}};
         hipLaunchKernelGGL(hd == 128 ? k_merge<128> : k_merge<64>, dim3((unsigned)((m.rows + 3) / 4)), dim3(256), 0, ctx->stream, m);

@@ -55,8 +55,8 @@ __device__ __forceinline__ void weigh(Columns<HD, CW>& r, const Block<CW>& s, u4
 // Blocks first, first + NW, .. below end of a class's segment of len tokens.  PRECISE: codes enter the products as they are, a group's at a time, and its
 // scale and minimum meet the sums in fp32.
 template <int HD, int BITS, int CW, bool PRECISE>
-__device__ __forceinline__ void stream_packed(Columns<HD, CW>& r, const QueryRows<F16, HD, CW>& q, const float (&q_sum)[CW][4], const wq_packed_kv& kv, int kvh,
-                                              int64_t tok0, int len, int first, int end, uint32_t* s_meta)
+__device__ __forceinline__ void stream_packed(Columns<HD, CW>& r, const char* s_query, const float (&q_sum)[CW][4], const wq_packed_kv& kv, int kvh, int64_t tok0, int len,
+                                              int first, int end, uint32_t* s_meta)
 {
     constexpr int C = BITS == 2 ? 0 : (BITS == 4 ? 1 : 2), ST = STEPS<F16, HD>, KB = HD / 4 * BITS / 8, VB = HD / 16 * BITS;
     using Order = std::conditional_t<BITS == 8, Near, Far>;
@@ -84,6 +84,19 @@ __device__ __forceinline__ void stream_packed(Columns<HD, CW>& r, const QueryRow
     load_meta(first);
     load_keys(first);
     load_values(first);
+    // (two columns' queries stay in registers; more are read from LDS at every block, where they would not leave enough of them)
+    constexpr bool HELD = CW * ST <= 8;
+    u4 held[HELD ? CW : 1][HELD ? ST : 1];
+    auto query = [&](int n, int st) -> u4 {
+        if constexpr (HELD) return held[n][st];
+        else return *reinterpret_cast<const u4*>(s_query + (n * ST + st) * 1024 + lane * 16);
+    };
+    if constexpr (HELD) {
+#pragma unroll
+        for (int n = 0; n < CW; n++)
+#pragma unroll
+            for (int st = 0; st < ST; st++) held[n][st] = *reinterpret_cast<const u4*>(s_query + (n * ST + st) * 1024 + lane * 16);
+    }
 #pragma unroll 1
     for (int b = first; b < end; b += NW) {
         s_meta[lane] = wm[0];
@@ -93,10 +106,10 @@ __device__ __forceinline__ void stream_packed(Columns<HD, CW>& r, const QueryRow
         const bool more = b + NW < end;
         if (more) load_meta(b + NW);
         Block<CW> s;
+        if constexpr (PRECISE) {
 #pragma unroll
-        for (int t = 0; t < 2; t++) {
-            u4 a[ST];
-            if constexpr (PRECISE) {
+            for (int t = 0; t < 2; t++) {
+                u4 a[ST];
 #pragma unroll
                 for (int st = 0; st < ST; st++) a[st] = expanded_keys<BITS>(wk[t], st, Codes(), Codes());
 #pragma unroll
@@ -109,7 +122,7 @@ __device__ __forceinline__ void stream_packed(Columns<HD, CW>& r, const QueryRow
                     for (int st = 0; st < ST; st++) {
                         const u4 y = {a[st][0] & mine, a[st][1] & mine, a[st][2] & mine, a[st][3] & mine};
 #pragma unroll
-                        for (int n = 0; n < CW; n++) x[n] = product<F16>(y, q[n][st], st ? x[n] : f4{0.f, 0.f, 0.f, 0.f});
+                        for (int n = 0; n < CW; n++) x[n] = product<F16>(y, query(n, st), st ? x[n] : f4{0.f, 0.f, 0.f, 0.f});
                     }
 #pragma unroll
                     for (int i = 0; i < 4; i++) {
@@ -122,15 +135,23 @@ __device__ __forceinline__ void stream_packed(Columns<HD, CW>& r, const QueryRow
                         }
                     }
                 }
-            } else {
+            }
+        } else {
+            u4 a[2][ST];
+#pragma unroll
+            for (int t = 0; t < 2; t++) {
                 const h2 sm = __builtin_bit_cast(h2, s_meta[(t * G + (j * G >> 2)) * 16 + m]);
 #pragma unroll
-                for (int st = 0; st < ST; st++) a[st] = expanded_keys<BITS>(wk[t], st, h2{sm[0], sm[0]}, h2{sm[1], sm[1]});
-#pragma unroll
-                for (int st = 0; st < ST; st++)
-#pragma unroll
-                    for (int n = 0; n < CW; n++) s[t][n] = product<F16>(a[st], q[n][st], st ? s[t][n] : f4{0.f, 0.f, 0.f, 0.f});
+                for (int st = 0; st < ST; st++) a[t][st] = expanded_keys<BITS>(wk[t], st, h2{sm[0], sm[0]}, h2{sm[1], sm[1]});
             }
+#pragma unroll
+            for (int st = 0; st < ST; st++)
+#pragma unroll
+                for (int n = 0; n < CW; n++) {
+                    const u4 y = query(n, st);
+#pragma unroll
+                    for (int t = 0; t < 2; t++) s[t][n] = product<F16>(a[t][st], y, st ? s[t][n] : f4{0.f, 0.f, 0.f, 0.f});
+                }
         }
         if (more) load_keys(b + NW);
         const int left = len - 32 * b;
@@ -232,39 +253,120 @@ __device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? ~0u : (n 
 // The first of this wavefront's blocks from t0 on, where block t of a segment is the part's (done + t - lo)-th
 __device__ __forceinline__ int first_block(int t0, int done, int lo) { return t0 + ((this_wave() - (done + t0 - lo)) & (NW - 1)); }
 
+// ---- who does what -------------------------------------------------------------------------------------------------------
+// A unit is a tile of R query rows of a sequence under one KV head; its keys are blocks of 32, those of the cache's four segments and then the new
+// rows'.  It is cut into a.splits pieces, a workgroup each; where the caller has told the longest sequence's blocks (a.longest), into as many as its own length is of that: only the
+// device knows it.
+struct Sequence {
+    int len[4], blocks[4], rows, all, pieces;  // rows: (new row, query head) pairs; all: blocks
+};
+__device__ __forceinline__ Sequence sequence_of(const TreeArgs& a, int b, int rows)
+{
+    Sequence s;
+    s.rows = rows;
+    s.all = tiles_of_cache<32>(a.kv, b, s.len, s.blocks) + (rows / a.rep + 31) / 32;
+    int n = a.splits;
+    if (a.longest > 0 && s.all < a.longest) n = (int)(((uint32_t)s.all * (uint32_t)n + a.longest - 1) / a.longest);      // (up to 2^23 blocks, 64 pieces)
+    s.pieces = n < s.all ? n : s.all;
+    return s;
+}
+
+// Where piece i of n begins in a unit of a sequence.  Near a class's border it begins there: a start in another class costs a wavefront two blocks' time, the
+// workgroup 8 blocks.  (Less than half a piece either way: none is empty.)
+__device__ __forceinline__ int begin_of(const Sequence& s, int i)
+{
+    const int n = s.pieces, share = s.all / n, over = s.all - share * n, x = share * i + (i < over ? i : over);
+    if (i <= 0 || i >= n) return x;
+    const int near = (share - 1) / 2 < 8 ? (share - 1) / 2 : 8;
+    int border = 0, y = x;
+#pragma unroll
+    for (int c = 0; c < 4; c++) {
+        border += s.blocks[c];
+        if (abs(x - border) <= near) y = border;
+    }
+    return y > 0 && y < s.all ? y : x;
+}
+
+// A piece's numerators in the workspace: [row][channel], then [row] (reference, sum)
+template <int HD, int R> constexpr int PIECE = R * (HD + 2);
+
 template <typename QT, int HD, int CW, bool PRECISE>
 __global__ __launch_bounds__(64 * NW, 2) void k_tree_stream(TreeArgs a)
 {
     static_assert(NW == 4, "two rounds of joining");
-    constexpr int R = 16 * CW, JOIN = HD / 16 * CW * 1024, TILE = 32 * HD * 2;
-    // the values of 16-bit rows, a piece of each wavefront; in the end two wavefronts' numerators
-    __shared__ __align__(16) char s_big[NW * TILE > 2 * JOIN ? NW * TILE : 2 * JOIN];
-    __shared__ float s_ml[2][CW][2][64];
+    constexpr int R = 16 * CW, ST = STEPS<F16, HD>, JOIN = HD / 16 * CW * 1024, TILE = 32 * HD * 2, QUERY = CW * ST * 1024;
+    constexpr int ENDS = NW / 2 * (JOIN + CW * 512), WALK = 3 * QUERY + NW * TILE, BIG = WALK > ENDS ? WALK : ENDS;
+    // the queries as each class's products take them, and the values of 16-bit rows, a piece of each wavefront; in the end two wavefronts' numerators, references
+    // and sums
+    __shared__ __align__(16) char s_big[BIG];
     __shared__ uint64_t s_seen[R * WORDS];
-    __shared__ __align__(16) uint32_t s_meta[NW][256];         // (at first the tree's parents)
+    __shared__ __align__(16) uint32_t s_meta[NW][256];         // (before the walk a tree's parents)
+    __shared__ float s_scale[R], s_sum[PRECISE ? 4 : 1][R];
     static_assert(sizeof(s_meta) >= WQ_MAX_TREE * 4, "");
     const int Hkv = a.kv.Hkv, wave = this_wave(), lane = threadIdx.x & 63, j = lane >> 4;
     const wq_packed_kv& kv = a.kv;
-    const int unit = (int)blockIdx.x % a.units, split = (int)blockIdx.x / a.units, kvh = unit % Hkv;
+
+    const int unit = (int)blockIdx.x % a.units, piece = (int)blockIdx.x / a.units, kvh = unit % Hkv;
     Place p;
     if (!find_place<R>(a.row_off, a.B, a.rep, a.total, unit / Hkv, p)) return;
-    const int n_new = p.rows / a.rep, node0 = p.row0 / a.rep;
-    if (a.parent && n_new > WQ_MAX_TREE && p.row0 == 0 && threadIdx.x == 0) atomicOr(a.status, WQ_DEV_TOO_MANY_ROWS);
-    const int last_row = (p.row0 + R < p.rows ? p.row0 + R : p.rows) - 1;
-    int blocks[4], len[4], newest = last_row / a.rep + 1;      // (no row sees one behind itself)
+    const int b = p.seq, row0 = p.row0, rows = p.rows;
+    const int64_t first_row = p.first;
+    const Sequence s = sequence_of(a, b, rows);
+    if (piece >= s.pieces) return;
+    const int lo = begin_of(s, piece), hi = begin_of(s, piece + 1);
+    const int node0 = row0 / a.rep, last_row = (row0 + R < rows ? row0 + R : rows) - 1;
+    int newest = last_row / a.rep + 1;                         // (no row sees one behind itself)
     if (a.parent && newest > WQ_MAX_TREE) newest = WQ_MAX_TREE;
-    const int cached = tiles_of_cache<32>(kv, p.seq, len, blocks), all = cached + (newest + 31) / 32;
-    const int lo = (int)((int64_t)split * all / a.splits), hi = (int)((int64_t)(split + 1) * all / a.splits);
-    if (a.parent && hi > cached && lo < hi) find_ancestors(a.parent + p.first, node0, last_row / a.rep + 1 - node0, s_seen, reinterpret_cast<int32_t*>(s_meta), 64 * NW);
+    if (a.parent && rows / a.rep > WQ_MAX_TREE && row0 == 0 && lo == 0 && threadIdx.x == 0) atomicOr(a.status, WQ_DEV_TOO_MANY_ROWS);
+    const int cached = s.all - (rows / a.rep + 31) / 32;
+    if (a.parent && hi > cached) find_ancestors(a.parent + first_row, node0, last_row / a.rep + 1 - node0, s_seen, reinterpret_cast<int32_t*>(s_meta), 64 * NW);
+
+    // Queries: a wavefront prepares a column (CW <= 4), in fp16 and in every class's order
+    auto row_at = [&](int n) -> const char* {
+        const int row = row0 + 16 * n + (lane & 15);
+        return row < rows ? a.q + (first_row + row / a.rep) * a.q_stride + (kvh * a.rep + row % a.rep) * (HD * 2) : nullptr;
+    };
+    if (wave < CW) {
+        QueryRows<F16, HD, 1> q, y;
+        load_query_quarter<F16, HD>(q, 0, row_at(wave));
+        const bool bad = not_finite<QT, HD>(q, 0);
+        float scale = a.scale;
+        if constexpr (std::is_same_v<QT, Bf16>) scale = fminf(fmaxf(a.scale * query_as_f16<HD>(q, 0), FLT_MIN), FLT_MAX);      // (see walk_cache)
+        if (bad) scale = NAN;
+        if (lane < 16) s_scale[16 * wave + lane] = scale;
+        if constexpr (PRECISE) {
+            float mine = 0.f;
+#pragma unroll
+            for (int st = 0; st < ST; st++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const uint32_t word = q[0][st][e];
+                    const h2 f = __builtin_bit_cast(h2, word);
+                    mine += (float)f[0] + (float)f[1];
+                }
+            // of the head's groups: a quarter's own (4), two quarters' (2), all (1)
+            const int G = HD / kv.group;
+            if (G < 4) mine += __shfl_xor(mine, 16, 64);
+            if (G < 2) mine += __shfl_xor(mine, 32, 64);
+            s_sum[j][16 * wave + (lane & 15)] = mine;      // of the quarter's group
+        }
+        auto leave = [&](auto bits, int order) __attribute__((always_inline)) {
+#pragma unroll
+            for (int st = 0; st < ST; st++) y[0][st] = q[0][st];
+            order_query<decltype(bits)::value, HD>(y, 0);
+#pragma unroll
+            for (int st = 0; st < ST; st++) *reinterpret_cast<u4*>(s_big + order * QUERY + (wave * ST + st) * 1024 + lane * 16) = y[0][st];
+        };
+        leave(std::integral_constant<int, 2>(), 0);
+        leave(std::integral_constant<int, 4>(), 1);
+        leave(std::integral_constant<int, 8>(), 2);
+    }
+    __syncthreads();
 
     Columns<HD, CW> r;
-    QueryRows<F16, HD, CW> q;
-    const char* row_at[CW];
 #pragma unroll
     for (int n = 0; n < CW; n++) {
-        const int row = p.row0 + 16 * n + (lane & 15);
-        row_at[n] = row < p.rows ? a.q + (p.first + row / a.rep) * a.q_stride + (kvh * a.rep + row % a.rep) * (HD * 2) : nullptr;
-        r.ref[n] = -INFINITY, r.sum[n] = 0.f;
+        r.ref[n] = -INFINITY, r.sum[n] = 0.f, r.scale[n] = s_scale[16 * n + (lane & 15)];
 #pragma unroll
         for (int ct = 0; ct < HD / 16; ct++) r.o[ct][n] = f4{0.f, 0.f, 0.f, 0.f};
     }
@@ -274,47 +376,25 @@ __global__ __launch_bounds__(64 * NW, 2) void k_tree_stream(TreeArgs a)
     int done = 0;
     auto walk_class = [&](auto bits) __attribute__((always_inline)) {
         constexpr int BITS = decltype(bits)::value, c = BITS == 2 ? 0 : (BITS == 4 ? 1 : 2);
-        const int t0 = lo > done ? lo - done : 0, t1 = hi - done < blocks[c] ? hi - done : blocks[c];
+        const int t0 = lo > done ? lo - done : 0, t1 = hi - done < s.blocks[c] ? hi - done : s.blocks[c];
         const int first = first_block(t0, done, lo);
-        done += blocks[c];
+        done += s.blocks[c];
         if (first >= t1) return;
         float q_sum[CW][4];
+        if constexpr (PRECISE) {
+            const int per = kv.group * 4 / HD;             // quarters of a group
 #pragma unroll
-        for (int n = 0; n < CW; n++) {
-            load_query_quarter<F16, HD>(q, n, row_at[n]);
-            const bool bad = not_finite<QT, HD>(q, n);
-            r.scale[n] = a.scale;
-            if constexpr (std::is_same_v<QT, Bf16>) r.scale[n] = fminf(fmaxf(a.scale * query_as_f16<HD>(q, n), FLT_MIN), FLT_MAX);
-            if (bad) r.scale[n] = NAN;
-            if constexpr (PRECISE) {
-                float mine = 0.f;
+            for (int n = 0; n < CW; n++)
 #pragma unroll
-                for (int st = 0; st < STEPS<F16, HD>; st++)
-#pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        const uint32_t word = q[n][st][e];
-                        const h2 f = __builtin_bit_cast(h2, word);
-                        mine += (float)f[0] + (float)f[1];
-                    }
-                // of the head's groups: a quarter's own (4), two quarters' (2), all (1)
-                const int G = HD / kv.group;
-                float of[4];
-#pragma unroll
-                for (int x = 0; x < 4; x++) of[x] = __shfl(mine, 16 * x + (lane & 15), 64);
-                q_sum[n][0] = G == 1 ? (of[0] + of[1]) + (of[2] + of[3]) : G == 2 ? of[0] + of[1] : of[0];
-                q_sum[n][1] = G == 2 ? of[2] + of[3] : of[1];
-                q_sum[n][2] = of[2], q_sum[n][3] = of[3];
-            }
-            order_query<BITS, HD>(q, n);
+                for (int g = 0; g < 4; g++) q_sum[n][g] = s_sum[g * per & 3][16 * n + (lane & 15)];
         }
-        stream_packed<HD, BITS, CW, PRECISE>(r, q, q_sum, kv, kvh, kv.cls_off[c][p.seq], len[c], first, t1, s_meta[wave]);
+        stream_packed<HD, BITS, CW, PRECISE>(r, s_big + c * QUERY, q_sum, kv, kvh, kv.cls_off[c][b], s.len[c], first, t1, s_meta[wave]);
     };
-    __syncthreads();                                           // (the parents have been read)
     walk_class(std::integral_constant<int, 2>());
     walk_class(std::integral_constant<int, 4>());
     walk_class(std::integral_constant<int, 8>());
     __builtin_amdgcn_s_setreg(FP16_OVFL, 0);
-    if constexpr (std::is_same_v<QT, Bf16>) {                  // from the packed tokens' shift to the rows', exact
+    if constexpr (std::is_same_v<QT, Bf16>) {              // from the packed tokens' shift to the rows', exact
 #pragma unroll
         for (int n = 0; n < CW; n++) {
             r.sum[n] *= exp2f(SHIFT<QT> - SHIFT<F16>);
@@ -323,46 +403,50 @@ __global__ __launch_bounds__(64 * NW, 2) void k_tree_stream(TreeArgs a)
         }
     }
     if (hi > done) {
+        const Lds tile = (Lds)s_big + 3 * QUERY + wave * TILE;
+        int t0 = lo > done ? lo - done : 0, t1 = hi - done < s.blocks[3] ? hi - done : s.blocks[3], first = first_block(t0, done, lo);
+        const int done16 = done + s.blocks[3], n0 = lo > done16 ? lo - done16 : 0, first_new = first_block(n0, done16, lo);
+        const int n1 = hi - done16 < (newest + 31) / 32 ? hi - done16 : (newest + 31) / 32;
+        if (first < t1 || first_new < n1) {
+            QueryRows<F16, HD, CW> q;
 #pragma unroll
-        for (int n = 0; n < CW; n++) {
-            r.scale[n] = a.scale;
-            load_query<F16, HD>(q, n, row_at[n]);
-        }
-        const Lds tile = (Lds)s_big + wave * TILE;
-        int t0 = lo > done ? lo - done : 0, t1 = hi - done < blocks[3] ? hi - done : blocks[3], first = first_block(t0, done, lo);
-        if (first < t1) {
-            const int64_t row0 = kv.off16[p.seq], stride = (int64_t)Hkv * HD * 2;
-            const char* k = static_cast<const char*>(kv.k16) + row0 * stride + kvh * (HD * 2);
-            const char* v = static_cast<const char*>(kv.v16) + row0 * stride + kvh * (HD * 2);
-            stream_rows<QT, HD, CW>(r, q, k, v, stride, stride, len[3], first, t1, tile, [&](int, int c) { return low_bits(len[3] - 32 * c) >> 4 * j; });
-        }
-        done += blocks[3];
-        t0 = lo > done ? lo - done : 0, t1 = hi - done, first = first_block(t0, done, lo);
-        if (hi > done && first < t1) {
-            const char* k = a.k + p.first * a.k_stride + kvh * (HD * 2);
-            const char* v = a.v + p.first * a.v_stride + kvh * (HD * 2);
-            const uint32_t* seen = reinterpret_cast<const uint32_t*>(s_seen);
-            stream_rows<QT, HD, CW>(r, q, k, v, a.k_stride, a.v_stride, newest, first, t1, tile, [&](int n, int c) {
-                const int row = p.row0 + 16 * n + (lane & 15), node = row / a.rep;
-                uint32_t bits = 0;
-                if (row <= last_row) bits = a.parent ? seen[(node - node0) * (2 * WORDS) + c] : low_bits(node + 1 - 32 * c);
-                return bits >> 4 * j;
-            });
+            for (int n = 0; n < CW; n++) {
+                r.scale[n] = a.scale;
+                load_query<F16, HD>(q, n, row_at(n));
+            }
+            if (first < t1) {
+                const int64_t from = kv.off16[b], stride = (int64_t)Hkv * HD * 2;
+                const char* k = static_cast<const char*>(kv.k16) + from * stride + kvh * (HD * 2);
+                const char* v = static_cast<const char*>(kv.v16) + from * stride + kvh * (HD * 2);
+                stream_rows<QT, HD, CW>(r, q, k, v, stride, stride, s.len[3], first, t1, tile, [&](int, int c) { return low_bits(s.len[3] - 32 * c) >> 4 * j; });
+            }
+            if (first_new < n1) {
+                const char* k = a.k + first_row * a.k_stride + kvh * (HD * 2);
+                const char* v = a.v + first_row * a.v_stride + kvh * (HD * 2);
+                const uint32_t* seen = reinterpret_cast<const uint32_t*>(s_seen);
+                stream_rows<QT, HD, CW>(r, q, k, v, a.k_stride, a.v_stride, newest, first_new, n1, tile, [&](int n, int c) {
+                    const int row = row0 + 16 * n + (lane & 15), node = row / a.rep;
+                    uint32_t bits = 0;
+                    if (row <= last_row) bits = a.parent ? seen[(node - node0) * (2 * WORDS) + c] : low_bits(node + 1 - 32 * c);
+                    return bits >> 4 * j;
+                });
+            }
         }
     }
-    // The wavefronts' numerators together: 2 and 3 to 0 and 1, then 1 to 0
+    // The wavefronts' numerators together: the upper half's to the lower half, twice
 #pragma unroll
     for (int n = 0; n < CW; n++) {
         r.sum[n] = sum_of_column(r.sum[n]);
         r.ref[n] -= SHIFT<QT>;
     }
+    float(*s_ml)[64] = reinterpret_cast<float(*)[64]>(s_big + NW / 2 * JOIN);
 #pragma unroll
     for (int half = NW / 2; half > 0; half /= 2) {
         __syncthreads();
         if (wave >= half && wave < 2 * half) {
 #pragma unroll
             for (int n = 0; n < CW; n++) {
-                s_ml[wave - half][n][0][lane] = r.ref[n], s_ml[wave - half][n][1][lane] = r.sum[n];
+                s_ml[((wave - half) * CW + n) * 2][lane] = r.ref[n], s_ml[((wave - half) * CW + n) * 2 + 1][lane] = r.sum[n];
 #pragma unroll
                 for (int ct = 0; ct < HD / 16; ct++) *reinterpret_cast<f4*>(s_big + (wave - half) * JOIN + (n * (HD / 16) + ct) * 1024 + lane * 16) = r.o[ct][n];
             }
@@ -371,7 +455,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_tree_stream(TreeArgs a)
         if (wave < half) {
 #pragma unroll
             for (int n = 0; n < CW; n++) {
-                const float ref = s_ml[wave][n][0][lane], sum = s_ml[wave][n][1][lane], most = fmaxf(r.ref[n], ref), base = most == -INFINITY ? 0.f : most;
+                const float ref = s_ml[(wave * CW + n) * 2][lane], sum = s_ml[(wave * CW + n) * 2 + 1][lane], most = fmaxf(r.ref[n], ref), base = most == -INFINITY ? 0.f : most;
                 const float x = __builtin_amdgcn_exp2f(r.ref[n] - base), y = __builtin_amdgcn_exp2f(ref - base);
                 r.ref[n] = most, r.sum[n] = r.sum[n] * x + sum * y;
 #pragma unroll
@@ -380,33 +464,72 @@ __global__ __launch_bounds__(64 * NW, 2) void k_tree_stream(TreeArgs a)
             }
         }
     }
-    if (wave > 0) return;
+    if (wave == 0) {
+        float* left = a.part + ((int64_t)unit * a.splits + piece) * PIECE<HD, R>;
 #pragma unroll
-    for (int n = 0; n < CW; n++) {
-        const int row = p.row0 + 16 * n + (lane & 15);
-        if (row >= p.rows) continue;
-        const int64_t at = (p.first + row / a.rep) * a.Hq + kvh * a.rep + row % a.rep;
-        if (a.parent && row / a.rep >= WQ_MAX_TREE) {          // refused: as if it saw nothing
-            r.ref[n] = -INFINITY, r.sum[n] = 0.f;
+        for (int n = 0; n < CW; n++) {
+            const int row = row0 + 16 * n + (lane & 15);
+            if (row >= rows) continue;
+            if (a.parent && row / a.rep >= WQ_MAX_TREE) {  // refused: as if it saw nothing
+                r.ref[n] = -INFINITY, r.sum[n] = 0.f;
 #pragma unroll
-            for (int ct = 0; ct < HD / 16; ct++) r.o[ct][n] = f4{0.f, 0.f, 0.f, 0.f};
+                for (int ct = 0; ct < HD / 16; ct++) r.o[ct][n] = f4{0.f, 0.f, 0.f, 0.f};
+            }
+            if (s.pieces > 1) {
+                const int x = 16 * n + (lane & 15);
+#pragma unroll
+                for (int ct = 0; ct < HD / 16; ct++) *reinterpret_cast<f4*>(left + x * HD + 16 * ct + 4 * j) = r.o[ct][n];
+                if (j == 0) left[R * HD + 2 * x] = r.ref[n], left[R * HD + 2 * x + 1] = r.sum[n];
+                continue;
+            }
+            const int64_t to_row = (first_row + row / a.rep) * a.Hq + kvh * a.rep + row % a.rep;
+            const float inv = one_over(r.sum[n]);
+            char* to = static_cast<char*>(a.out) + to_row * HD * 2;
+#pragma unroll
+            for (int ct = 0; ct < HD / 16; ct++) {
+                const f4 x = r.o[ct][n] * inv;
+                *reinterpret_cast<uint2*>(to + (16 * ct + 4 * j) * 2) = make_uint2(pack2(x[0], x[1], QT()), pack2(x[2], x[3], QT()));
+            }
+            if (a.lse && j == 0) a.lse[to_row] = log_sum_exp(r.ref[n], r.sum[n]);
         }
-        if (a.splits > 1) {
-            const int64_t slot = at * a.splits + split;
-#pragma unroll
-            for (int ct = 0; ct < HD / 16; ct++) *reinterpret_cast<f4*>(a.part + slot * HD + 16 * ct + 4 * j) = r.o[ct][n];
-            if (j == 0) a.part_ml[slot * 2] = r.ref[n], a.part_ml[slot * 2 + 1] = r.sum[n];
-            continue;
-        }
-        const float inv = one_over(r.sum[n]);
-        char* to = static_cast<char*>(a.out) + at * HD * 2;
-#pragma unroll
-        for (int ct = 0; ct < HD / 16; ct++) {
-            const f4 x = r.o[ct][n] * inv;
-            *reinterpret_cast<uint2*>(to + (16 * ct + 4 * j) * 2) = make_uint2(pack2(x[0], x[1], QT()), pack2(x[2], x[3], QT()));
-        }
-        if (a.lse && j == 0) a.lse[at] = log_sum_exp(r.ref[n], r.sum[n]);
     }
+}
+
+// The pieces of units that are cut: a wavefront per row
+template <int HD, int R>
+__global__ __launch_bounds__(256) void k_tree_join(TreeArgs a, int dtype)
+{
+    const int lane = threadIdx.x & 63, Hkv = a.kv.Hkv, unit = blockIdx.x / (R / 4), in = blockIdx.x % (R / 4) * 4 + this_wave(), kvh = unit % Hkv;
+    Place p;
+    if (!find_place<R>(a.row_off, a.B, a.rep, a.total, unit / Hkv, p) || p.row0 + in >= p.rows) return;
+    const int pieces = sequence_of(a, p.seq, p.rows).pieces;
+    if (pieces == 1) return;
+    const float* parts = a.part + (int64_t)unit * a.splits * PIECE<HD, R>;
+    auto piece = [&](int i) { return parts + (int64_t)i * PIECE<HD, R>; };
+    constexpr int LANES = HD / 4, GROUPS = 64 / LANES;
+    float m = -INFINITY, l = 0.f;              // lane i: piece i
+    if (lane < pieces) {
+        const float* ml = piece(lane) + R * HD + 2 * in;
+        m = ml[0], l = ml[1];
+    }
+    const float M = wave_max(m), w = __builtin_amdgcn_exp2f(m - (M == -INFINITY ? 0.f : M)), L = wave_sum(l * w);
+    f4 x = {0.f, 0.f, 0.f, 0.f};
+    for (int i0 = 0; i0 < pieces; i0 += 8 * GROUPS) {
+        f4 y[8];
+#pragma unroll
+        for (int k = 0; k < 8; k++) {
+            const int i = i0 + k * GROUPS + lane / LANES;
+            y[k] = i < pieces ? *reinterpret_cast<const f4*>(piece(i) + in * HD + 4 * (lane % LANES)) : f4{0.f, 0.f, 0.f, 0.f};
+        }
+#pragma unroll
+        for (int k = 0; k < 8; k++) {
+            const int i = i0 + k * GROUPS + lane / LANES;
+            const float f = __shfl(w, i & 63, 64);
+            x += y[k] * (i < pieces ? f : 0.f);
+        }
+    }
+    const int row = p.row0 + in;
+    store_merged<HD>({a.out, a.lse, nullptr, nullptr}, dtype, (p.first + row / a.rep) * a.Hq + kvh * a.rep + row % a.rep, sum_of_groups<HD>(x), M, L);
 }
 
 template <typename QT, int HD, bool PRECISE>
@@ -416,15 +539,34 @@ TreeKernel of_columns(int columns)
         case 1: return k_tree_stream<QT, HD, 1, PRECISE>;
         case 2: return k_tree_stream<QT, HD, 2, PRECISE>;
         case 3: return k_tree_stream<QT, HD, 3, PRECISE>;
-        default: return k_tree_stream<QT, HD, 4, PRECISE>;
     }
+    if constexpr (HD == 64) return k_tree_stream<QT, HD, 4, PRECISE>;
+    return nullptr;
 }
 
-}  // namespace
-
-TreeKernel wq_tree_stream_kernel(int dtype, int hd, int columns, bool precise)
+TreeKernel stream_kernel(int dtype, int hd, int columns, bool precise)
 {
     if (dtype == WQ_F16) return hd == 128 ? of_columns<F16, 128, true>(columns) : of_columns<F16, 64, true>(columns);
     if (precise) return hd == 128 ? of_columns<Bf16, 128, true>(columns) : of_columns<Bf16, 64, true>(columns);
     return hd == 128 ? of_columns<Bf16, 128, false>(columns) : of_columns<Bf16, 64, false>(columns);
+}
+
+template <int R>
+void launch(wq_ctx* ctx, const TreeArgs& a, int dtype)
+{
+    void (*const join)(TreeArgs, int) = a.kv.hd == 128 ? k_tree_join<128, R> : k_tree_join<64, R>;
+    hipLaunchKernelGGL(stream_kernel(dtype, a.kv.hd, R / 16, dtype == WQ_F16 || a.lse), dim3((unsigned)(a.units * a.splits)), dim3(64 * NW), 0, ctx->stream, a);
+    if (a.splits > 1) hipLaunchKernelGGL(join, dim3((unsigned)(a.units * (R / 4))), dim3(256), 0, ctx->stream, a, dtype);
+}
+
+}  // namespace
+
+void wq_launch_tree_stream(wq_ctx* ctx, const TreeArgs& a, int dtype, int columns)
+{
+    switch (columns) {
+        case 1: launch<16>(ctx, a, dtype); break;
+        case 2: launch<32>(ctx, a, dtype); break;
+        case 3: launch<48>(ctx, a, dtype); break;
+        default: launch<64>(ctx, a, dtype);
+    }
 }
