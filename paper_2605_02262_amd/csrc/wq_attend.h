@@ -224,6 +224,8 @@ __device__ __forceinline__ void multiply_values(Rows<HD>& r, const Weights<CT>& 
 
 // Which keys of a tile a row does not see: those from its limit on
 struct Limits {
+    __device__ __forceinline__ int key_tile(int t) const { return t; }         // the t-th of the walk
+    __device__ __forceinline__ void ahead(int) const {}        // (its keys are on their way)
     template <typename CT, int HD>
     __device__ __forceinline__ void hide(const Rows<HD>& r, Products<CT>& s, int key0) const
     {
@@ -326,10 +328,9 @@ __device__ __forceinline__ int group_of_wave() { return this_wave() >> 2; }
 // Tiles t0 .. t1-1.  multiply(s, t): a tile's products of keys; bring_keys(t), bring_values(t): of the group that does so, into LDS; settle(): a phase's end.
 // The products of the first tile meet weights of zero with what lies in front of its values: zeros.  (No condition inside the loop but who brings what: the compiler
 // copies the accumulators around every one, and spills them.)
-template <typename CT, int HD, bool SPLIT, typename Order, typename Multiply, typename Values, typename BringKeys, typename BringValues, typename Settle,
-          typename Hidden = Limits>
+template <typename CT, int HD, bool SPLIT, typename Order, typename Multiply, typename Values, typename BringKeys, typename BringValues, typename Settle>
 __device__ __forceinline__ void take_turns(Rows<HD>& r, int t0, int t1, int least, const Multiply& multiply, const Values& values, const BringKeys& bring_keys,
-                                           const BringValues& bring_values, const Settle& settle, const Hidden& hidden = Hidden())
+                                           const BringValues& bring_values, const Settle& settle)
 {
     const int group = group_of_wave();
     if (SPLIT && group == 1) {
@@ -360,12 +361,30 @@ __device__ __forceinline__ void take_turns(Rows<HD>& r, int t0, int t1, int leas
         __builtin_amdgcn_s_setprio(0);
         if (!SPLIT && group == 0 && t + 1 < t1) bring_keys(t + 1);
         settle();
-        form_weights<CT, HD, Order>(r, s, p, t * KEYS<CT>, (t + 1) * KEYS<CT> > least, hidden);
+        form_weights<CT, HD, Order>(r, s, p, t * KEYS<CT>, (t + 1) * KEYS<CT> > least, Limits());
         if (!SPLIT && group == 1 && t + 1 < t1) bring_values(t + 1);
         settle();
     }
     if (SPLIT || group == 0) settle();
     multiply_values<CT, HD>(r, p, [&](int vs, int ct) { return values(t1 - 1, vs, ct); });
+}
+// All wavefronts together: bring(t) sends for, or expands, tile t while tile t - 1 is worked on.  Where two workgroups share a compute unit their phases
+// mix by themselves, and tiles of 128 rows cost little more per row than ones of 256 in turns.
+template <typename CT, int HD, typename Order, typename Multiply, typename Values, typename Bring, typename Settle, typename Hidden = Limits>
+__device__ __forceinline__ void take_all(Rows<HD>& r, int t0, int t1, int least, const Multiply& multiply, const Values& values, const Bring& bring, const Settle& settle,
+                                         const Hidden& hidden = Hidden())
+{
+    Products<CT> s;
+    Weights<CT> p;
+    bring(t0);
+#pragma unroll 1
+    for (int t = t0; t < t1; t++) {
+        settle();
+        multiply(s, t);
+        if (t + 1 < t1) bring(t + 1);
+        form_weights<CT, HD, Order>(r, s, p, t * KEYS<CT>, (t + 1) * KEYS<CT> > least, hidden);
+        multiply_values<CT, HD>(r, p, [&](int vs, int ct) { return values(t, vs, ct); });
+    }
 }
 template <typename CT, int HD>
 __device__ __forceinline__ void clear_tile(Lds tile)
@@ -477,26 +496,36 @@ struct Direct {
     }
 };
 
-// Tiles lo .. hi-1 of the n rows from k, v on, brought by group 1: a tile's values and the next one's keys while group 0 multiplies.
-template <typename CT, int HD, bool SPLIT, typename Hidden = Limits>
+// Tiles lo .. hi-1 of the n rows from k, v on, brought by group 1: a tile's values and the next one's keys while group 0 multiplies.  TOGETHER: by all of four
+// wavefronts, see take_all.
+template <typename CT, int HD, bool SPLIT, bool TOGETHER = false, typename Hidden = Limits>
 __device__ __forceinline__ void walk_rows(Rows<HD>& r, const Query<CT, HD>& q, const char* k, const char* v, int64_t k_stride, int64_t v_stride, int n, int lo,
                                           int hi, int least, Lds k_lds, Lds v_lds, const Hidden& hidden = Hidden())
 {
     constexpr int BYTES = TILE_BYTES<CT, HD>, TK = KEYS<CT>;
     const Direct<HD> rows(k_stride, v_stride);
-    auto load_keys = [&](int t) { rows.load_keys(k + (int64_t)t * TK * k_stride, n - t * TK, k_lds + (t & 1) * BYTES); };
-    auto bring_values = [&](int t) {
-        rows.load_values(v + (int64_t)t * TK * v_stride, n - t * TK, v_lds + (t & 1) * BYTES);
-        if (t + 1 < hi) load_keys(t + 1);
-    };
+    auto load_keys = [&](int t) { rows.load_keys(k + (int64_t)hidden.key_tile(t) * TK * k_stride, n - hidden.key_tile(t) * TK, k_lds + (t & 1) * BYTES); };
+    auto load_values = [&](int t) { rows.load_values(v + (int64_t)hidden.key_tile(t) * TK * v_stride, n - hidden.key_tile(t) * TK, v_lds + (t & 1) * BYTES); };
+    auto multiply = [&](Products<CT>& s, int t) { multiply_keys<CT, HD>(s, q, [&](int kt, int st) { return rows.keys(k_lds + (t & 1) * BYTES, kt, st); }); };
+    auto values = [&](int t, int vs, int ct) { return rows.values(v_lds + (t & 1) * BYTES, vs, ct); };
     __syncthreads();                                           // (whatever was in LDS before has been read)
-    if (group_of_wave() == 1) load_keys(lo);
-    else clear_tile<CT, HD>(v_lds + (~lo & 1) * BYTES);
-    __syncthreads();
-    take_turns<CT, HD, SPLIT, Natural>(
-        r, lo, hi, least,
-        [&](Products<CT>& s, int t) { multiply_keys<CT, HD>(s, q, [&](int kt, int st) { return rows.keys(k_lds + (t & 1) * BYTES, kt, st); }); },
-        [&](int t, int vs, int ct) { return rows.values(v_lds + (t & 1) * BYTES, vs, ct); }, [](int) {}, bring_values, [] { __syncthreads(); }, hidden);
+    if constexpr (TOGETHER) {
+        auto bring = [&](int t) {
+            load_keys(t);
+            load_values(t);
+            hidden.ahead(t);
+        };
+        take_all<CT, HD, Natural>(r, lo, hi, least, multiply, values, bring, [] { __syncthreads(); }, hidden);
+    } else {
+        if (group_of_wave() == 1) load_keys(lo);
+        else clear_tile<CT, HD>(v_lds + (~lo & 1) * BYTES);
+        __syncthreads();
+        auto bring_values = [&](int t) {
+            load_values(t);
+            if (t + 1 < hi) load_keys(t + 1);
+        };
+        take_turns<CT, HD, SPLIT, Natural>(r, lo, hi, least, multiply, values, [](int) {}, bring_values, [] { __syncthreads(); });
+    }
 }
 
 // ---- a class of the packed cache -----------------------------------------------------------------------------------------
@@ -591,10 +620,9 @@ __device__ __forceinline__ u4 expanded_values(const uint32_t* w, int i, const h2
         y[0] = expanded<BITS, 0>(placed<BITS, 0>(x), s[0], m[0]), y[1] = expanded<BITS, 4>(placed<BITS, 4>(x), s[1], m[1]);
         y[2] = expanded<BITS, 0>(placed<BITS, 0>(z), s[2], m[2]), y[3] = expanded<BITS, 4>(placed<BITS, 4>(z), s[3], m[3]);
     } else {                                                   // a word holds two of them, one per half
-        const uint32_t x = w[i >> 1], z = x >> 8;
-        auto both = [&](uint32_t a, uint32_t b) { return i & 1 ? high_halves(a, b) : low_halves(a, b); };
-        y[0] = expanded<BITS, 0>(both(placed<BITS, 0>(x), placed<BITS, 0>(z)), s[0], m[0]), y[1] = expanded<BITS, 2>(both(placed<BITS, 2>(x), placed<BITS, 2>(z)), s[1], m[1]);
-        y[2] = expanded<BITS, 4>(both(placed<BITS, 4>(x), placed<BITS, 4>(z)), s[2], m[2]), y[3] = expanded<BITS, 6>(both(placed<BITS, 6>(x), placed<BITS, 6>(z)), s[3], m[3]);
+        const uint32_t x = w[i >> 1], both = i & 1 ? high_halves(x, x >> 8) : low_halves(x, x >> 8);
+        y[0] = expanded<BITS, 0>(placed<BITS, 0>(both), s[0], m[0]), y[1] = expanded<BITS, 2>(placed<BITS, 2>(both), s[1], m[1]);
+        y[2] = expanded<BITS, 4>(placed<BITS, 4>(both), s[2], m[2]), y[3] = expanded<BITS, 6>(placed<BITS, 6>(both), s[3], m[3]);
     }
     return y;
 }
@@ -737,7 +765,7 @@ struct PackedValues {
 
 // Tiles t0 .. t1-1 of a class's segment.  G: the head's groups, whose codes enter the products as they are; 0: keys expanded to fp16 (q_sum and m_lds
 // are not read)
-template <int HD, int BITS, int G>
+template <int HD, int BITS, int G, bool TOGETHER = false>
 __device__ __forceinline__ void walk_packed(Rows<HD>& r, const Query<F16, HD>& q, const float (&q_sum)[COLS][G ? G : 1], const wq_packed_kv& kv, int kvh, int64_t tok0,
                                             int len, int t0, int t1, Lds k_lds, Lds v_lds, Lds m_lds)
 {
@@ -757,25 +785,34 @@ __device__ __forceinline__ void walk_packed(Rows<HD>& r, const Query<F16, HD>& q
         values.stage(v_of(t));
         if (t + 1 < t1) values.load(t + 1);
     };
+    auto multiply = [&](Products<F16>& s, int t) {
+        auto operand = [&](int kt, int st) { return k_of(t)[(kt * STEPS<F16, HD> + st) * 64 + lane]; };
+        if constexpr (G > 0)
+            multiply_codes<HD, G>(s, q, q_sum, operand, [&](int kt, int g) { return ((Lds4)(m_lds + (t & 1) * (64 * 4 * G)))[(kt * G + g) * 4 + (lane >> 4)]; });
+        else
+            multiply_keys<F16, HD>(s, q, operand);
+    };
+    auto value = [&](int t, int vs, int ct) { return v_of(t)[(vs * (HD / 16) + ct) * 64 + lane]; };
     __syncthreads();                                           // (whatever was in LDS before has been read)
-    if (group_of_wave() == 1) {
-        values.load(t0);
-    } else {
-        clear_tile<F16, HD>(v_lds + (~t0 & 1) * BYTES);
+    if constexpr (TOGETHER) {
         keys.load(t0);
-        bring_keys(t0);
+        values.load(t0);
+        auto bring = [&](int t) {
+            bring_keys(t);
+            bring_values(t);
+        };
+        take_all<F16, HD, Order>(r, t0, t1, len, multiply, value, bring, meet);
+    } else {
+        if (group_of_wave() == 1) {
+            values.load(t0);
+        } else {
+            clear_tile<F16, HD>(v_lds + (~t0 & 1) * BYTES);
+            keys.load(t0);
+            bring_keys(t0);
+        }
+        __syncthreads();
+        take_turns<F16, HD, false, Order>(r, t0, t1, len, multiply, value, bring_keys, bring_values, meet);
     }
-    __syncthreads();
-    take_turns<F16, HD, false, Order>(
-        r, t0, t1, len,
-        [&](Products<F16>& s, int t) {
-            auto operand = [&](int kt, int st) { return k_of(t)[(kt * STEPS<F16, HD> + st) * 64 + lane]; };
-            if constexpr (G > 0)
-                multiply_codes<HD, G>(s, q, q_sum, operand, [&](int kt, int g) { return ((Lds4)(m_lds + (t & 1) * (64 * 4 * G)))[(kt * G + g) * 4 + (lane >> 4)]; });
-            else
-                multiply_keys<F16, HD>(s, q, operand);
-        },
-        [&](int t, int vs, int ct) { return v_of(t)[(vs * (HD / 16) + ct) * 64 + lane]; }, bring_keys, bring_values, meet);
 }
 
 // ---- what both kernels share -------------------------------------------------------------------------------------------
@@ -877,6 +914,26 @@ __device__ __forceinline__ void load_query_codes(Query<F16, HD>& q, int n, const
     }
 #pragma unroll
     for (int g = 0; g < G; g++) q_sum[g] = sum_of_column(q_sum[g]);
+}
+
+// ... the sums alone, of a query that has become fp16 since
+template <int G, int HD>
+__device__ __forceinline__ void sum_query_codes(const Query<F16, HD>& q, int n, float (&q_sum)[G])
+{
+    constexpr int PER = STEPS<F16, HD> / G;
+#pragma unroll
+    for (int g = 0; g < G; g++) {
+        q_sum[g] = 0.f;
+#pragma unroll
+        for (int st = g * PER; st < (g + 1) * PER; st++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const uint32_t word = q[n][st][e];
+                const h2 f = __builtin_bit_cast(h2, word);
+                q_sum[g] += (float)f[0] + (float)f[1];
+            }
+        q_sum[g] = sum_of_column(q_sum[g]);
+    }
 }
 
 template <typename QT> constexpr uint32_t EXPONENT16 = std::is_same_v<QT, Bf16> ? 0x7F80 : 0x7C00;
@@ -982,11 +1039,12 @@ __device__ __forceinline__ int tiles_of_cache(const wq_packed_kv& kv, int seq, i
     return all;
 }
 
-// Tiles lo .. hi-1, the classes one after the other, for the wavefront's rows at row_at (NULL: no row); MORE: hi may lie behind the cache's last.
+// Tiles lo .. hi-1, the classes one after the other, for the wavefront's rows at row_at (NULL: no row).  TREE: hi may lie behind the cache's last
+// tile, and 16-bit types' wavefronts work together.
 // QT: the query's type; G as in walk_packed (fp16: the cache's groups per head; else 0); packed tokens are walked in fp16 (fp32 for fp32 queries), 16-bit rows in the
 // cache's own type.  fp32 with heads of 128 needs 17 registers more than there are (scratch): 16 requests over 5000 tokens 40 us, in fp16 27.
 template <typename QT> using Walked = std::conditional_t<std::is_same_v<QT, F32>, F32, F16>;
-template <typename QT, int HD, int G, bool MORE>
+template <typename QT, int HD, int G, bool TREE>
 __device__ __forceinline__ void walk_cache(Rows<HD>& r, Query<Walked<QT>, HD>& q, const char* const (&row_at)[COLS], float scale, const wq_packed_kv& kv, int seq, int kvh,
                                            const int (&len)[4], const int (&tiles)[4], int lo, int hi, bool any, Lds s_k, Lds s_v, Lds s_m)
 {
@@ -1015,11 +1073,12 @@ __device__ __forceinline__ void walk_cache(Rows<HD>& r, Query<Walked<QT>, HD>& q
             // (kept from 0 and infinity: a masked logit, -infinity, times 0 and a logit of 0 times infinity would be NaN.  A scale that small leaves every
             // logit below 2^-100; with one that large logits that differ at all differ by 2^70 or more)
             if constexpr (std::is_same_v<QT, Bf16>) r.scale[n] = fminf(fmaxf(scale * query_as_f16<HD>(q, n), FLT_MIN), FLT_MAX);
+            if constexpr (std::is_same_v<QT, Bf16> && G > 0) sum_query_codes<G, HD>(q, n, q_sum[n]);
             if (bad) r.scale[n] = NAN;
             if constexpr (PIPED && G == 0) order_query<BITS, HD>(q, n);
         }
         if constexpr (PIPED) {
-            walk_packed<HD, BITS, G>(r, q, q_sum, kv, kvh, kv.cls_off[c][seq], len[c], t0, t1, s_k, s_v, s_m);
+            walk_packed<HD, BITS, G, TREE>(r, q, q_sum, kv, kvh, kv.cls_off[c][seq], len[c], t0, t1, s_k, s_v, s_m);
         } else {
             PackedKeys<HD, BITS, 32> keys(kv, kvh, kv.cls_off[c][seq], 0);
             PackedValues<HD, BITS, 32> values(kv, kvh, kv.cls_off[c][seq], 0);
@@ -1053,8 +1112,8 @@ __device__ __forceinline__ void walk_cache(Rows<HD>& r, Query<Walked<QT>, HD>& q
             for (int ct = 0; ct < HD / 16; ct++) r.o[ct][n] *= exp2f(SHIFT<QT> - SHIFT<CT>);
         }
     }
-    const int t0 = lo > done ? lo - done : 0, t1 = MORE && hi - done > tiles[3] ? tiles[3] : hi - done;
-    if (MORE ? t0 < t1 : hi > done) {              // (of no rows there would be no last one to read again)
+    const int t0 = lo > done ? lo - done : 0, t1 = TREE && hi - done > tiles[3] ? tiles[3] : hi - done;
+    if (TREE ? t0 < t1 : hi > done) {              // (of no rows there would be no last one to read again)
 #pragma unroll
         for (int n = 0; n < COLS; n++) {
             r.limit[n] = len[3];
@@ -1065,7 +1124,7 @@ __device__ __forceinline__ void walk_cache(Rows<HD>& r, Query<Walked<QT>, HD>& q
         const char* k = static_cast<const char*>(kv.k16) + row0 * stride + kvh * (HD * 2);
         const char* v = static_cast<const char*>(kv.v16) + row0 * stride + kvh * (HD * 2);
         if constexpr (PIPED) {
-            walk_rows<QT, HD, false>(r, q, k, v, stride, stride, len[3], t0, t1, len[3], s_k, s_v);
+            walk_rows<QT, HD, false, TREE>(r, q, k, v, stride, stride, len[3], t0, t1, len[3], s_k, s_v);
         } else {
             for (int t = t0; t < t1; t++) {
                 const int key0 = t * TK;

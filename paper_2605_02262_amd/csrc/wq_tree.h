@@ -14,14 +14,16 @@ struct TreeArgs {
     wq_packed_kv kv;
     void* out;                                 // as in Out
     float *lse, *part, *part_ml;
-    int longest;                               // wavefronts that bring their own keys: blocks of 32 keys of the longest sequence, or 0
+    int longest;                               // 16-bit types: blocks of keys of the longest sequence, or 0
 };
 
 typedef void (*TreeKernel)(TreeArgs);
+typedef void (*TreeKernel)(TreeArgs);
 // The kernel in which every wavefront brings its own keys, for tiles of 16 * columns query rows: see wq_tree_stream.hip
-constexpr int WQ_STREAM_WAVES = 4;
-constexpr int WQ_STREAM_SLOTS = 512;           // workgroups that the card holds at a time
-void wq_launch_tree_stream(wq_ctx* ctx, const TreeArgs& a, int dtype, int columns);
+constexpr int WQ_STREAM_WAVES = 4, WQ_STREAM_COLUMNS = 3;
+TreeKernel wq_tree_stream_kernel(int dtype, int hd, int columns, bool lse);
+// ... and in which a workgroup's four bring tiles of 64 for 128 query rows (groups: of a cache's heads, 0 where keys may be rounded): see wq_tree_tiles.hip
+TreeKernel wq_tree_tiles_kernel(int dtype, int hd, int groups);
 
 namespace {
 
@@ -51,5 +53,43 @@ __device__ __forceinline__ void find_ancestors(const int32_t* parent, int node0,
     }
     __syncthreads();
 }
+
+// ---- who does what -------------------------------------------------------------------------------------------------------
+// A unit is a tile of R query rows of a sequence under one KV head; its keys are blocks of TK, those of the cache's four segments and then the new
+// rows'.  It is cut into a.splits pieces, a workgroup each; where the caller has told the longest sequence's blocks (a.longest), into as many as its own length is of that: only the
+// device knows it.
+struct Sequence {
+    int len[4], blocks[4], rows, all, pieces;  // rows: (new row, query head) pairs; all: blocks
+};
+template <int TK>
+__device__ __forceinline__ Sequence sequence_of(const TreeArgs& a, int b, int rows)
+{
+    Sequence s;
+    s.rows = rows;
+    s.all = tiles_of_cache<TK>(a.kv, b, s.len, s.blocks) + (rows / a.rep + TK - 1) / TK;
+    int n = a.splits;
+    if (a.longest > 0 && s.all < a.longest) n = (int)(((uint32_t)s.all * (uint32_t)n + a.longest - 1) / a.longest);      // (up to 2^23 blocks, 64 pieces)
+    s.pieces = n < s.all ? n : s.all;
+    return s;
+}
+
+// Where piece i of n begins in a unit of a sequence.  Near a class's border it begins there: a start in another class costs a workgroup about as much as `near_class`
+// blocks.  (Less than half a piece either way: none is empty.)
+__device__ __forceinline__ int begin_of(const Sequence& s, int i, int near_class)
+{
+    const int n = s.pieces, share = s.all / n, over = s.all - share * n, x = share * i + (i < over ? i : over);
+    if (i <= 0 || i >= n) return x;
+    const int near = (share - 1) / 2 < near_class ? (share - 1) / 2 : near_class;
+    int border = 0, y = x;
+#pragma unroll
+    for (int c = 0; c < 4; c++) {
+        border += s.blocks[c];
+        if (abs(x - border) <= near) y = border;
+    }
+    return y > 0 && y < s.all ? y : x;
+}
+
+// A piece's numerators in the workspace: [row][channel], then [row] (reference, sum)
+template <int HD, int R> constexpr int PIECE = R * (HD + 2);
 
 }  // namespace

@@ -99,6 +99,51 @@ __global__ __launch_bounds__(64 * WAVES<F32>, 2) void k_tree(TreeArgs a)
     if (any) store_rows<F32, HD>(r, p, a.rep, a.Hq, kvh, wave, split, a.splits > 1 ? a.splits : 0, {a.out, a.lse, a.part, a.part_ml});
 }
 
+// The pieces of units that are cut: a wavefront per row
+template <int HD, int R, int TK>
+__global__ __launch_bounds__(256) void k_tree_join(TreeArgs a, int dtype)
+{
+    const int lane = threadIdx.x & 63, Hkv = a.kv.Hkv, unit = blockIdx.x / (R / 4), in = blockIdx.x % (R / 4) * 4 + this_wave(), kvh = unit % Hkv;
+    Place p;
+    if (!find_place<R>(a.row_off, a.B, a.rep, a.total, unit / Hkv, p) || p.row0 + in >= p.rows) return;
+    const int pieces = sequence_of<TK>(a, p.seq, p.rows).pieces;
+    if (pieces == 1) return;
+    const float* parts = a.part + (int64_t)unit * a.splits * PIECE<HD, R>;
+    auto piece = [&](int i) { return parts + (int64_t)i * PIECE<HD, R>; };
+    constexpr int LANES = HD / 4, GROUPS = 64 / LANES;
+    float m = -INFINITY, l = 0.f;              // lane i: piece i
+    if (lane < pieces) {
+        const float* ml = piece(lane) + R * HD + 2 * in;
+        m = ml[0], l = ml[1];
+    }
+    const float M = wave_max(m), w = __builtin_amdgcn_exp2f(m - (M == -INFINITY ? 0.f : M)), L = wave_sum(l * w);
+    f4 x = {0.f, 0.f, 0.f, 0.f};
+    for (int i0 = 0; i0 < pieces; i0 += 8 * GROUPS) {
+        f4 y[8];
+#pragma unroll
+        for (int k = 0; k < 8; k++) {
+            const int i = i0 + k * GROUPS + lane / LANES;
+            y[k] = i < pieces ? *reinterpret_cast<const f4*>(piece(i) + in * HD + 4 * (lane % LANES)) : f4{0.f, 0.f, 0.f, 0.f};
+        }
+#pragma unroll
+        for (int k = 0; k < 8; k++) {
+            const int i = i0 + k * GROUPS + lane / LANES;
+            const float f = __shfl(w, i & 63, 64);
+            x += y[k] * (i < pieces ? f : 0.f);
+        }
+    }
+    const int row = p.row0 + in;
+    store_merged<HD>({a.out, a.lse, nullptr, nullptr}, dtype, (p.first + row / a.rep) * a.Hq + kvh * a.rep + row % a.rep, sum_of_groups<HD>(x), M, L);
+}
+
+template <int R, int TK>
+void launch_pieces(wq_ctx* ctx, const TreeArgs& a, TreeKernel kernel, int dtype)
+{
+    void (*const join)(TreeArgs, int) = a.kv.hd == 128 ? k_tree_join<128, R, TK> : k_tree_join<64, R, TK>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(a.units * a.splits)), dim3(256), 0, ctx->stream, a);
+    if (a.splits > 1) hipLaunchKernelGGL(join, dim3((unsigned)(a.units * (R / 4))), dim3(256), 0, ctx->stream, a, dtype);
+}
+
 }  // namespace
 
 WqTreePlan wq_tree_plan(int64_t total_rows, int B, int Hq, int Hkv, int hd, int dtype, bool lse, int64_t max_cache_tokens, int64_t slots, int max_rows, int num_splits, size_t room)
@@ -108,25 +153,32 @@ WqTreePlan wq_tree_plan(int64_t total_rows, int B, int Hq, int Hkv, int hd, int 
     WqTreePlan s = {};
     s.rows = dtype == WQ_F32 ? 128 : 256;
     if (dtype != WQ_F32) {
-        const int64_t columns = ((total_rows + used - 1) / used * rep + 15) / 16;      // of a sequence, on the average
-        const int most = hd == 128 ? 3 : 4;
-        const int64_t groups = (columns + most - 1) / most;
-        s.columns = (int)((columns + groups - 1) / groups);
+        // Columns of a sequence: of the one with the most rows, where they are few (a second tile reads its keys again), else on the average
+        const int64_t widest = ((int64_t)max_rows * rep + 15) / 16, columns = widest > 0 && widest <= WQ_STREAM_COLUMNS ? widest : ((total_rows + used - 1) / used * rep + 15) / 16;
+        // (three columns of precise logits with heads of 128 need more registers than there are: 147 us for two columns' 100 of 32 ragged sequences, 5 rows of 7 heads)
+        s.columns = (int)(columns <= WQ_STREAM_COLUMNS ? columns : 8);
+        if (s.columns == 3 && hd == 128 && (dtype == WQ_F16 || lse)) s.columns = 2;
         s.rows = 16 * s.columns;
+        const int tile = s.columns <= WQ_STREAM_COLUMNS ? 32 : 64;
         s.units = tiles_of(total_rows, rep, B, s.rows) * Hkv;
-        const int64_t real = (tiles_of(total_rows, rep, 0, s.rows) + used) * Hkv, blocks = (max_cache_tokens + 31) / 32 + (max_rows + 31) / 32;
+        const int64_t each = (total_rows + used - 1) / used, real = used * ((each * rep + s.rows - 1) / s.rows) * Hkv;      // units, if the sequences' rows are alike
+        const int64_t blocks = (max_cache_tokens + tile - 1) / tile + (max_rows + tile - 1) / tile;
         // The cache's capacity says how long the sequences are on the average: those that are shorter than the longest have fewer pieces
         const double average = slots > 0 && slots < (int64_t)B * max_cache_tokens ? (double)slots / ((double)B * max_cache_tokens) : 1.0;
         s.longest = num_splits > 0 || blocks > 1 << 23 ? 0 : (int)blocks;
         if (num_splits > 0) {
             s.splits = num_splits;
         } else {
-            // Rounds of workgroups, each of a piece's blocks by four wavefronts and what a start and an end take; pieces have to be joined
+            // Rounds of the workgroups that the card holds at a time (its registers and LDS hold `slots`; fewer are not spread evenly, and take as long), each of a
+            // piece's steps (a tile, or a block of each wavefront) and what a start and an end take in such steps; pieces have to be joined
+            const bool tiles = s.columns > WQ_STREAM_COLUMNS;
+            const int at_once = hd == 128 ? (s.columns == 1 ? 768 : 512) : (s.columns == 1 ? 1024 : s.columns == WQ_STREAM_COLUMNS ? 512 : 768);
+            const double start = tiles ? 3 : 5, join = tiles ? 2 : 3;
             double best = 0;
             s.splits = 1;
             for (int p = 1; p <= WQ_MAX_ATTEND_SPLITS && p <= (blocks < 4 ? 1 : blocks); p++) {
-                const double groups = (double)real * p * average, rounds = groups <= WQ_STREAM_SLOTS ? 1 : ceil(groups / WQ_STREAM_SLOTS);
-                const double time = rounds * (ceil((double)blocks / p / 4) * 1.0 + 4) + (p > 1 ? 4 : 0);
+                const double groups = (double)real * p * average, rounds = groups <= at_once ? 1 : ceil(groups / at_once);
+                const double time = rounds * (ceil((double)blocks / p / (tiles ? 1 : WQ_STREAM_WAVES)) + start) + (p > 1 ? join : 0);
                 if (p == 1 || time < best) best = time, s.splits = p;
             }
         }
@@ -139,7 +191,7 @@ WqTreePlan wq_tree_plan(int64_t total_rows, int B, int Hq, int Hkv, int hd, int 
         return s;
     }
     const int64_t units = tiles_of(total_rows, rep, B, s.rows) * Hkv;
-    s.splits = num_splits > 0 ? num_splits : auto_splits_of((tiles_of(total_rows, rep, 0, s.rows) + used) * Hkv, max_cache_tokens + max_rows, 256, 32);
+    s.splits = num_splits > 0 ? num_splits : auto_splits_of((tiles_of(total_rows, rep, 0, s.rows) + used) * Hkv, max_cache_tokens + max_rows + 4 * 32, 256, 32);      // (every class ends in a tile of its own)
     auto bytes = [&]() -> size_t { return s.splits > 1 ? partials_bytes(total_rows * Hq, hd, s.splits) : 0; };
     while (num_splits <= 0 && s.splits > 1 && bytes() > room) s.splits--;
     s.bytes = bytes();
@@ -166,7 +218,15 @@ int wq_launch_tree(wq_ctx* ctx, const WqTree& f)
     a.part_ml = a.part + f.total_rows * f.Hq * a.splits * hd;
     if (f.plan.columns) {
         a.longest = f.plan.longest;
-        wq_launch_tree_stream(ctx, a, f.dtype, f.plan.columns);
+        const TreeKernel kernel = f.plan.columns > WQ_STREAM_COLUMNS
+                                      ? wq_tree_tiles_kernel(f.dtype, hd, f.dtype == WQ_F16 || f.lse ? hd / f.kv->group : 0)
+                                      : wq_tree_stream_kernel(f.dtype, hd, f.plan.columns, f.lse != nullptr);
+        switch (f.plan.columns) {
+            case 1: launch_pieces<16, 32>(ctx, a, kernel, f.dtype); break;
+            case 2: launch_pieces<32, 32>(ctx, a, kernel, f.dtype); break;
+            case 3: launch_pieces<48, 32>(ctx, a, kernel, f.dtype); break;
+            default: launch_pieces<128, 64>(ctx, a, kernel, f.dtype);
+        }
         WQ_HIP_CHECK(ctx, hipGetLastError());
         return WQ_OK;
     }

@@ -55,7 +55,7 @@ __device__ __forceinline__ void weigh(Columns<HD, CW>& r, const Block<CW>& s, u4
 // Blocks first, first + NW, .. below end of a class's segment of len tokens.  PRECISE: codes enter the products as they are, a group's at a time, and its
 // scale and minimum meet the sums in fp32.
 template <int HD, int BITS, int CW, bool PRECISE>
-__device__ __forceinline__ void stream_packed(Columns<HD, CW>& r, const char* s_query, const float (&q_sum)[CW][4], const wq_packed_kv& kv, int kvh, int64_t tok0, int len,
+__device__ __forceinline__ void stream_packed(Columns<HD, CW>& r, const char* s_query, const float* s_sum, const wq_packed_kv& kv, int kvh, int64_t tok0, int len,
                                               int first, int end, uint32_t* s_meta)
 {
     constexpr int C = BITS == 2 ? 0 : (BITS == 4 ? 1 : 2), ST = STEPS<F16, HD>, KB = HD / 4 * BITS / 8, VB = HD / 16 * BITS;
@@ -81,6 +81,7 @@ __device__ __forceinline__ void stream_packed(Columns<HD, CW>& r, const char* s_
         for (int t = 0; t < 2; t++) load_words<KB>(k_codes + (int64_t)b * (4 * HD * BITS) + t * 64 * KB, wk[t]);
     };
     auto load_values = [&](int b) { load_words<VB>(v_codes + (int64_t)b * (4 * HD * BITS), wv); };
+    // (one block ahead.  Two cost one column's kernels their third wavefront a SIMD, 31 -> 39 us of 8 x 12800 tokens, and brought two columns' nothing)
     load_meta(first);
     load_keys(first);
     load_values(first);
@@ -117,6 +118,9 @@ __device__ __forceinline__ void stream_packed(Columns<HD, CW>& r, const char* s_
                     if (g >= G) break;
                     const u4 sm = *reinterpret_cast<const u4*>(s_meta + (t * G + g) * 16 + 4 * j);
                     const uint32_t mine = (j * G >> 2) == g ? ~0u : 0u;
+                    float q_sum[CW];
+#pragma unroll
+                    for (int n = 0; n < CW; n++) q_sum[n] = s_sum[(g * 4 / G) * (16 * CW) + 16 * n + m];
                     f4 x[CW];
 #pragma unroll
                     for (int st = 0; st < ST; st++) {
@@ -130,7 +134,7 @@ __device__ __forceinline__ void stream_packed(Columns<HD, CW>& r, const char* s_
                         const h2 f = __builtin_bit_cast(h2, word);
 #pragma unroll
                         for (int n = 0; n < CW; n++) {
-                            const float y = g ? fmaf((float)f[1], q_sum[n][g], s[t][n][i]) : (float)f[1] * q_sum[n][g];
+                            const float y = g ? fmaf((float)f[1], q_sum[n], s[t][n][i]) : (float)f[1] * q_sum[n];
                             s[t][n][i] = fmaf((float)f[0], x[n][i], y);
                         }
                     }
@@ -253,43 +257,6 @@ __device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? ~0u : (n 
 // The first of this wavefront's blocks from t0 on, where block t of a segment is the part's (done + t - lo)-th
 __device__ __forceinline__ int first_block(int t0, int done, int lo) { return t0 + ((this_wave() - (done + t0 - lo)) & (NW - 1)); }
 
-// ---- who does what -------------------------------------------------------------------------------------------------------
-// A unit is a tile of R query rows of a sequence under one KV head; its keys are blocks of 32, those of the cache's four segments and then the new
-// rows'.  It is cut into a.splits pieces, a workgroup each; where the caller has told the longest sequence's blocks (a.longest), into as many as its own length is of that: only the
-// device knows it.
-struct Sequence {
-    int len[4], blocks[4], rows, all, pieces;  // rows: (new row, query head) pairs; all: blocks
-};
-__device__ __forceinline__ Sequence sequence_of(const TreeArgs& a, int b, int rows)
-{
-    Sequence s;
-    s.rows = rows;
-    s.all = tiles_of_cache<32>(a.kv, b, s.len, s.blocks) + (rows / a.rep + 31) / 32;
-    int n = a.splits;
-    if (a.longest > 0 && s.all < a.longest) n = (int)(((uint32_t)s.all * (uint32_t)n + a.longest - 1) / a.longest);      // (up to 2^23 blocks, 64 pieces)
-    s.pieces = n < s.all ? n : s.all;
-    return s;
-}
-
-// Where piece i of n begins in a unit of a sequence.  Near a class's border it begins there: a start in another class costs a wavefront two blocks' time, the
-// workgroup 8 blocks.  (Less than half a piece either way: none is empty.)
-__device__ __forceinline__ int begin_of(const Sequence& s, int i)
-{
-    const int n = s.pieces, share = s.all / n, over = s.all - share * n, x = share * i + (i < over ? i : over);
-    if (i <= 0 || i >= n) return x;
-    const int near = (share - 1) / 2 < 8 ? (share - 1) / 2 : 8;
-    int border = 0, y = x;
-#pragma unroll
-    for (int c = 0; c < 4; c++) {
-        border += s.blocks[c];
-        if (abs(x - border) <= near) y = border;
-    }
-    return y > 0 && y < s.all ? y : x;
-}
-
-// A piece's numerators in the workspace: [row][channel], then [row] (reference, sum)
-template <int HD, int R> constexpr int PIECE = R * (HD + 2);
-
 template <typename QT, int HD, int CW, bool PRECISE>
 __global__ __launch_bounds__(64 * NW, 2) void k_tree_stream(TreeArgs a)
 {
@@ -311,9 +278,9 @@ __global__ __launch_bounds__(64 * NW, 2) void k_tree_stream(TreeArgs a)
     if (!find_place<R>(a.row_off, a.B, a.rep, a.total, unit / Hkv, p)) return;
     const int b = p.seq, row0 = p.row0, rows = p.rows;
     const int64_t first_row = p.first;
-    const Sequence s = sequence_of(a, b, rows);
+    const Sequence s = sequence_of<32>(a, b, rows);
     if (piece >= s.pieces) return;
-    const int lo = begin_of(s, piece), hi = begin_of(s, piece + 1);
+    const int lo = begin_of(s, piece, 8), hi = begin_of(s, piece + 1, 8);
     const int node0 = row0 / a.rep, last_row = (row0 + R < rows ? row0 + R : rows) - 1;
     int newest = last_row / a.rep + 1;                         // (no row sees one behind itself)
     if (a.parent && newest > WQ_MAX_TREE) newest = WQ_MAX_TREE;
@@ -380,15 +347,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_tree_stream(TreeArgs a)
         const int first = first_block(t0, done, lo);
         done += s.blocks[c];
         if (first >= t1) return;
-        float q_sum[CW][4];
-        if constexpr (PRECISE) {
-            const int per = kv.group * 4 / HD;             // quarters of a group
-#pragma unroll
-            for (int n = 0; n < CW; n++)
-#pragma unroll
-                for (int g = 0; g < 4; g++) q_sum[n][g] = s_sum[g * per & 3][16 * n + (lane & 15)];
-        }
-        stream_packed<HD, BITS, CW, PRECISE>(r, s_big + c * QUERY, q_sum, kv, kvh, kv.cls_off[c][b], s.len[c], first, t1, s_meta[wave]);
+        stream_packed<HD, BITS, CW, PRECISE>(r, s_big + c * QUERY, &s_sum[0][0], kv, kvh, kv.cls_off[c][b], s.len[c], first, t1, s_meta[wave]);
     };
     walk_class(std::integral_constant<int, 2>());
     walk_class(std::integral_constant<int, 4>());
@@ -495,52 +454,14 @@ __global__ __launch_bounds__(64 * NW, 2) void k_tree_stream(TreeArgs a)
     }
 }
 
-// The pieces of units that are cut: a wavefront per row
-template <int HD, int R>
-__global__ __launch_bounds__(256) void k_tree_join(TreeArgs a, int dtype)
-{
-    const int lane = threadIdx.x & 63, Hkv = a.kv.Hkv, unit = blockIdx.x / (R / 4), in = blockIdx.x % (R / 4) * 4 + this_wave(), kvh = unit % Hkv;
-    Place p;
-    if (!find_place<R>(a.row_off, a.B, a.rep, a.total, unit / Hkv, p) || p.row0 + in >= p.rows) return;
-    const int pieces = sequence_of(a, p.seq, p.rows).pieces;
-    if (pieces == 1) return;
-    const float* parts = a.part + (int64_t)unit * a.splits * PIECE<HD, R>;
-    auto piece = [&](int i) { return parts + (int64_t)i * PIECE<HD, R>; };
-    constexpr int LANES = HD / 4, GROUPS = 64 / LANES;
-    float m = -INFINITY, l = 0.f;              // lane i: piece i
-    if (lane < pieces) {
-        const float* ml = piece(lane) + R * HD + 2 * in;
-        m = ml[0], l = ml[1];
-    }
-    const float M = wave_max(m), w = __builtin_amdgcn_exp2f(m - (M == -INFINITY ? 0.f : M)), L = wave_sum(l * w);
-    f4 x = {0.f, 0.f, 0.f, 0.f};
-    for (int i0 = 0; i0 < pieces; i0 += 8 * GROUPS) {
-        f4 y[8];
-#pragma unroll
-        for (int k = 0; k < 8; k++) {
-            const int i = i0 + k * GROUPS + lane / LANES;
-            y[k] = i < pieces ? *reinterpret_cast<const f4*>(piece(i) + in * HD + 4 * (lane % LANES)) : f4{0.f, 0.f, 0.f, 0.f};
-        }
-#pragma unroll
-        for (int k = 0; k < 8; k++) {
-            const int i = i0 + k * GROUPS + lane / LANES;
-            const float f = __shfl(w, i & 63, 64);
-            x += y[k] * (i < pieces ? f : 0.f);
-        }
-    }
-    const int row = p.row0 + in;
-    store_merged<HD>({a.out, a.lse, nullptr, nullptr}, dtype, (p.first + row / a.rep) * a.Hq + kvh * a.rep + row % a.rep, sum_of_groups<HD>(x), M, L);
-}
-
 template <typename QT, int HD, bool PRECISE>
 TreeKernel of_columns(int columns)
 {
     switch (columns) {
         case 1: return k_tree_stream<QT, HD, 1, PRECISE>;
         case 2: return k_tree_stream<QT, HD, 2, PRECISE>;
-        case 3: return k_tree_stream<QT, HD, 3, PRECISE>;
     }
-    if constexpr (HD == 64) return k_tree_stream<QT, HD, 4, PRECISE>;
+    if constexpr (!PRECISE || HD == 64) return k_tree_stream<QT, HD, 3, PRECISE>;
     return nullptr;
 }
 
@@ -551,22 +472,6 @@ TreeKernel stream_kernel(int dtype, int hd, int columns, bool precise)
     return hd == 128 ? of_columns<Bf16, 128, false>(columns) : of_columns<Bf16, 64, false>(columns);
 }
 
-template <int R>
-void launch(wq_ctx* ctx, const TreeArgs& a, int dtype)
-{
-    void (*const join)(TreeArgs, int) = a.kv.hd == 128 ? k_tree_join<128, R> : k_tree_join<64, R>;
-    hipLaunchKernelGGL(stream_kernel(dtype, a.kv.hd, R / 16, dtype == WQ_F16 || a.lse), dim3((unsigned)(a.units * a.splits)), dim3(64 * NW), 0, ctx->stream, a);
-    if (a.splits > 1) hipLaunchKernelGGL(join, dim3((unsigned)(a.units * (R / 4))), dim3(256), 0, ctx->stream, a, dtype);
-}
-
 }  // namespace
 
-void wq_launch_tree_stream(wq_ctx* ctx, const TreeArgs& a, int dtype, int columns)
-{
-    switch (columns) {
-        case 1: launch<16>(ctx, a, dtype); break;
-        case 2: launch<32>(ctx, a, dtype); break;
-        case 3: launch<48>(ctx, a, dtype); break;
-        default: launch<64>(ctx, a, dtype);
-    }
-}
+TreeKernel wq_tree_stream_kernel(int dtype, int hd, int columns, bool lse) { return stream_kernel(dtype, hd, columns, dtype == WQ_F16 || lse); }
