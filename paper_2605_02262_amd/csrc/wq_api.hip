@@ -598,11 +598,10 @@ size_t wq_tree_workspace_bytes(int64_t total_rows, int B, int Hq, int Hkv, int h
 {
     if (total_rows <= 0 || B <= 0 || Hq <= 0 || Hkv <= 0 || hd <= 0 || Hq % Hkv != 0) return WQ_WS_HEADER;
     size_t most = 0;
-    for (const int dtype : {WQ_F32, WQ_BF16, WQ_F16})
-        for (const bool with_lse : {false, true}) {
-            const size_t bytes = wq_tree_plan(total_rows, B, Hq, Hkv, hd, dtype, with_lse, max_cache_tokens, B * max_cache_tokens / 2, max_rows, num_splits).bytes;
-            most = bytes > most ? bytes : most;
-        }
+    for (const int dtype : {WQ_F32, WQ_BF16}) {
+        const size_t bytes = wq_tree_plan(total_rows, B, Hq, Hkv, hd, dtype, max_cache_tokens, 0, max_rows, num_splits).bytes;
+        most = bytes > most ? bytes : most;
+    }
     return WQ_WS_HEADER + most;
 }
 
@@ -635,9 +634,10 @@ int wq_tree_attention(wq_ctx* ctx, const void* q, int64_t q_stride, const void* 
     if (rc != WQ_OK) return rc;
     if (k_stride > 1 << 22 || v_stride > 1 << 22)             // (offsets inside a tile have 32 bits)
         return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "rows of k or v are more than 2^22 elements apart");
-    const WqTreePlan plan = wq_tree_plan(total_rows, B, Hq, kv->Hkv, kv->hd, dtype, lse != nullptr, max_cache_tokens,
+    const WqTreePlan plan = wq_tree_plan(total_rows, B, Hq, kv->Hkv, kv->hd, dtype, max_cache_tokens,
                                          kv->cap[0] + kv->cap[1] + kv->cap[2] + kv->cap16, max_rows, num_splits, room_of(ctx));
-    if (plan.groups > MOST_GROUPS_512 || (plan.splits > 1 && total_rows * Hq > 4 * WQ_MOST_GROUPS_256)) return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "too many rows");
+    if (plan.groups > MOST_GROUPS_512 || (plan.splits > 1 && (total_rows * Hq > 4 * WQ_MOST_GROUPS_256 || plan.units * (plan.rows / 4) > WQ_MOST_GROUPS_256)))
+        return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "too many rows");
     if (!ctx->ws || ctx->ws_bytes < WQ_WS_HEADER + plan.bytes)
         return wq_fail(ctx, WQ_ERR_WORKSPACE, "workspace too small for %d splits of %lld rows", plan.splits, (long long)total_rows);
     return wq_launch_tree(ctx, {q, k, v, q_stride, k_stride, v_stride, dtype, B, Hq, kv, plan, row_off, parent, total_rows, sm_scale, out, lse});
@@ -672,13 +672,15 @@ int wq_append_rows(wq_ctx* ctx, int n_layers, const void* const* k, int64_t k_st
             return wq_fail(ctx, WQ_ERR_ARG, "the layers' caches differ in Hkv, hd or dtype16");
         if (kv[l].Hkv > MOST_HEADS) return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "more than 2^18 heads");
         if (!on_16_bytes(kv[l].k16) || !on_16_bytes(kv[l].v16)) return wq_fail(ctx, WQ_ERR_ARG, "k16 and v16 must be 16-byte aligned");
+        for (int m = 0; m < l; m++)
+            if (kv[l].len16 == kv[m].len16 || (kv[l].k16 && kv[l].k16 == kv[m].k16)) return wq_fail(ctx, WQ_ERR_ARG, "two layers share a cache");
         rc = check_rows(ctx, "k", k[l], k_stride, total_rows, kv[l].Hkv, kv[l].hd, dtype);
         if (rc == WQ_OK) rc = check_rows(ctx, "v", v[l], v_stride, total_rows, kv[l].Hkv, kv[l].hd, dtype);
         if (rc != WQ_OK) return rc;
     }
     if ((dtype == WQ_BF16) != (kv[0].dtype16 == WQ_BF16))
         return wq_fail(ctx, WQ_ERR_ARG, "dtype16 must be bf16 for bf16 input and fp16 for fp16/fp32 input");
-    if (B == 0 || total_rows == 0 || max_take == 0) return WQ_OK;
+    if (B == 0 || max_take == 0 || (total_rows == 0 && !take)) return WQ_OK;
     if (!row_off) return wq_fail(ctx, WQ_ERR_ARG, "NULL table");
     if (!ctx->ws || ctx->ws_bytes < WQ_WS_HEADER) return wq_fail(ctx, WQ_ERR_WORKSPACE, "no workspace");
     return wq_launch_append_rows(ctx, {n_layers, k, v, k_stride, v_stride, dtype, B, row_off, total_rows, take, n_take, max_take, kv});
@@ -701,6 +703,8 @@ int wq_copy_sequences(wq_ctx* ctx, int n_layers, const wq_packed_kv* src, const 
                 return wq_fail(ctx, WQ_ERR_ARG, "the caches differ in Hkv, hd, group or dtype16");
         }
         const wq_packed_kv &x = src[l], &y = dst[l];
+        for (int m = 0; m < n_layers; m++)
+            if ((m != l && dst[m].len16 == y.len16) || src[m].len16 == y.len16) return wq_fail(ctx, WQ_ERR_ARG, "a copy shares a table with another cache");
         bool same = (y.k16 && y.k16 == x.k16) || (y.v16 && y.v16 == x.v16) || y.len16 == x.len16 || y.v_scale_max == x.v_scale_max;
         for (int c = 0; c < 3; c++)
             same = same || (y.codes[c] && y.codes[c] == x.codes[c]) || (y.meta[c] && y.meta[c] == x.meta[c]) || y.cls_off[c] == x.cls_off[c] || y.cls_len[c] == x.cls_len[c];

@@ -256,7 +256,7 @@ struct WqTree {
     float* lse;
 };
 // slots: tokens that the cache has room for, 0: not known
-WqTreePlan wq_tree_plan(int64_t total_rows, int B, int Hq, int Hkv, int hd, int dtype, bool lse, int64_t max_cache_tokens, int64_t slots, int max_rows, int num_splits,
+WqTreePlan wq_tree_plan(int64_t total_rows, int B, int Hq, int Hkv, int hd, int dtype, int64_t max_cache_tokens, int64_t slots, int max_rows, int num_splits,
                         size_t room = SIZE_MAX);
 int wq_launch_tree(wq_ctx* ctx, const WqTree& f);
 

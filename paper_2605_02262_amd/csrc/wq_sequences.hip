@@ -203,7 +203,7 @@ __global__ __launch_bounds__(256) void k_copy(CopyArgs a)
             }
         }
         int64_t sum[4];
-        const int mine[4] = {pad32(len[0]) / 32, pad32(len[1]) / 32, pad32(len[2]) / 32, i >= 0 ? (len[3] + rows_per - 1) / rows_per : 0};
+        const int mine[4] = {pad32(len[0]) / 32, pad32(len[1]) / 32, pad32(len[2]) / 32, i >= 0 && fits ? (len[3] + rows_per - 1) / rows_per : 0};
 #pragma unroll
         for (int k = 0; k < 4; k++) {
             sum[k] = mine[k];
@@ -348,7 +348,7 @@ int wq_launch_append_rows(wq_ctx* ctx, const WqAppendRows& f)
     a.k_stride = f.k_stride, a.v_stride = f.v_stride;
     a.row_off = f.row_off, a.take = f.take, a.n_take = f.n_take, a.total_rows = f.total_rows;
     a.B = f.B, a.max_take = f.max_take, a.row_elems = f.kv[0].Hkv * f.kv[0].hd;
-    a.pieces = (f.max_take + PIECE_ROWS - 1) / PIECE_ROWS;
+    a.pieces = (f.max_take - 1) / PIECE_ROWS + 1;
     a.status = wq_status_ptr(ctx);
     void (*const kernel)(AppendArgs) = f.dtype == WQ_F32 ? k_append_rows<float> : k_append_rows<uint16_t>;
     if ((int64_t)(f.n_layers < APPEND_LAYERS ? f.n_layers : APPEND_LAYERS) * f.B > WQ_MOST_GROUPS_256 / a.pieces)

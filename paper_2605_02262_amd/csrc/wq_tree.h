@@ -14,10 +14,10 @@ struct TreeArgs {
     wq_packed_kv kv;
     void* out;                                 // as in Out
     float *lse, *part, *part_ml;
-    int longest;                               // 16-bit types: blocks of keys of the longest sequence, or 0
+    int4* found;                               // 16-bit types: every unit's place and pieces, for the join
+    int longest;                               // ... : blocks of keys of the longest sequence, or 0
 };
 
-typedef void (*TreeKernel)(TreeArgs);
 typedef void (*TreeKernel)(TreeArgs);
 // The kernel in which every wavefront brings its own keys, for tiles of 16 * columns query rows: see wq_tree_stream.hip
 constexpr int WQ_STREAM_WAVES = 4, WQ_STREAM_COLUMNS = 3;
@@ -56,8 +56,8 @@ __device__ __forceinline__ void find_ancestors(const int32_t* parent, int node0,
 
 // ---- who does what -------------------------------------------------------------------------------------------------------
 // A unit is a tile of R query rows of a sequence under one KV head; its keys are blocks of TK, those of the cache's four segments and then the new
-// rows'.  It is cut into a.splits pieces, a workgroup each; where the caller has told the longest sequence's blocks (a.longest), into as many as its own length is of that: only the
-// device knows it.
+// rows'.  It is cut into a.splits pieces, a workgroup each; where the caller has told the longest sequence's blocks (a.longest), into as many as its own
+// length is of that: only the device knows it.
 struct Sequence {
     int len[4], blocks[4], rows, all, pieces;  // rows: (new row, query head) pairs; all: blocks
 };
@@ -87,6 +87,12 @@ __device__ __forceinline__ int begin_of(const Sequence& s, int i, int near_class
         if (abs(x - border) <= near) y = border;
     }
     return y > 0 && y < s.all ? y : x;
+}
+
+// What the join has to know of a unit, from its first piece: x, y first new row and first (row, head) pair, z the sequence's pairs, w pieces (0: no such unit)
+__device__ __forceinline__ void leave_unit(const TreeArgs& a, int unit, int piece, const Place& p, int pieces)
+{
+    if (a.splits > 1 && piece == 0 && threadIdx.x == 0) a.found[unit] = pieces ? make_int4((int)p.first, p.row0, p.rows, pieces) : make_int4(0, 0, 0, 0);
 }
 
 // A piece's numerators in the workspace: [row][channel], then [row] (reference, sum)

@@ -100,14 +100,13 @@ __global__ __launch_bounds__(64 * WAVES<F32>, 2) void k_tree(TreeArgs a)
 }
 
 // The pieces of units that are cut: a wavefront per row
-template <int HD, int R, int TK>
+template <int HD, int R>
 __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a, int dtype)
 {
-    const int lane = threadIdx.x & 63, Hkv = a.kv.Hkv, unit = blockIdx.x / (R / 4), in = blockIdx.x % (R / 4) * 4 + this_wave(), kvh = unit % Hkv;
-    Place p;
-    if (!find_place<R>(a.row_off, a.B, a.rep, a.total, unit / Hkv, p) || p.row0 + in >= p.rows) return;
-    const int pieces = sequence_of<TK>(a, p.seq, p.rows).pieces;
-    if (pieces == 1) return;
+    const int lane = threadIdx.x & 63, unit = blockIdx.x / (R / 4), in = blockIdx.x % (R / 4) * 4 + this_wave(), kvh = unit % a.kv.Hkv;
+    const int4 found = a.found[unit];
+    const int row = found.y + in, pieces = found.w;
+    if (pieces <= 1 || row >= found.z) return;
     const float* parts = a.part + (int64_t)unit * a.splits * PIECE<HD, R>;
     auto piece = [&](int i) { return parts + (int64_t)i * PIECE<HD, R>; };
     constexpr int LANES = HD / 4, GROUPS = 64 / LANES;
@@ -132,37 +131,35 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a, int dtype)
             x += y[k] * (i < pieces ? f : 0.f);
         }
     }
-    const int row = p.row0 + in;
-    store_merged<HD>({a.out, a.lse, nullptr, nullptr}, dtype, (p.first + row / a.rep) * a.Hq + kvh * a.rep + row % a.rep, sum_of_groups<HD>(x), M, L);
+    store_merged<HD>({a.out, a.lse, nullptr, nullptr}, dtype, ((int64_t)found.x + row / a.rep) * a.Hq + kvh * a.rep + row % a.rep, sum_of_groups<HD>(x), M, L);
 }
 
-template <int R, int TK>
+template <int R>
 void launch_pieces(wq_ctx* ctx, const TreeArgs& a, TreeKernel kernel, int dtype)
 {
-    void (*const join)(TreeArgs, int) = a.kv.hd == 128 ? k_tree_join<128, R, TK> : k_tree_join<64, R, TK>;
+    void (*const join)(TreeArgs, int) = a.kv.hd == 128 ? k_tree_join<128, R> : k_tree_join<64, R>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)(a.units * a.splits)), dim3(256), 0, ctx->stream, a);
     if (a.splits > 1) hipLaunchKernelGGL(join, dim3((unsigned)(a.units * (R / 4))), dim3(256), 0, ctx->stream, a, dtype);
 }
 
 }  // namespace
 
-WqTreePlan wq_tree_plan(int64_t total_rows, int B, int Hq, int Hkv, int hd, int dtype, bool lse, int64_t max_cache_tokens, int64_t slots, int max_rows, int num_splits, size_t room)
+WqTreePlan wq_tree_plan(int64_t total_rows, int B, int Hq, int Hkv, int hd, int dtype, int64_t max_cache_tokens, int64_t slots, int max_rows, int num_splits, size_t room)
 {
     const int rep = Hq / Hkv;
     const int64_t used = total_rows < B ? total_rows : B;     // sequences that have rows
     WqTreePlan s = {};
-    s.rows = dtype == WQ_F32 ? 128 : 256;
+    if (max_cache_tokens > int64_t(1) << 40) max_cache_tokens = int64_t(1) << 40;
     if (dtype != WQ_F32) {
-        // Columns of a sequence: of the one with the most rows, where they are few (a second tile reads its keys again), else on the average
-        const int64_t widest = ((int64_t)max_rows * rep + 15) / 16, columns = widest > 0 && widest <= WQ_STREAM_COLUMNS ? widest : ((total_rows + used - 1) / used * rep + 15) / 16;
-        // (three columns of precise logits with heads of 128 need more registers than there are: 147 us for two columns' 100 of 32 ragged sequences, 5 rows of 7 heads)
-        s.columns = (int)(columns <= WQ_STREAM_COLUMNS ? columns : 8);
-        if (s.columns == 3 && hd == 128 && (dtype == WQ_F16 || lse)) s.columns = 2;
+        // Columns of a sequence, on the average.  Up to three: every wavefront brings its own keys; four in two tiles (us of 8 x 56 rows over 12800 tokens, 4 KV heads of
+        // 128: 62, in a tile of 128 rows 73); more (and five: 74, 75) in tiles of 128 rows
+        const int64_t columns = ((total_rows + used - 1) / used * rep + 15) / 16;
+        s.columns = (int)(columns <= WQ_STREAM_COLUMNS ? columns : columns == 4 ? 2 : 8);
         s.rows = 16 * s.columns;
         const int tile = s.columns <= WQ_STREAM_COLUMNS ? 32 : 64;
         s.units = tiles_of(total_rows, rep, B, s.rows) * Hkv;
         const int64_t each = (total_rows + used - 1) / used, real = used * ((each * rep + s.rows - 1) / s.rows) * Hkv;      // units, if the sequences' rows are alike
-        const int64_t blocks = (max_cache_tokens + tile - 1) / tile + (max_rows + tile - 1) / tile;
+        const int64_t blocks = (max_cache_tokens + tile - 1) / tile + ((int64_t)max_rows + tile - 1) / tile;
         // The cache's capacity says how long the sequences are on the average: those that are shorter than the longest have fewer pieces
         const double average = slots > 0 && slots < (int64_t)B * max_cache_tokens ? (double)slots / ((double)B * max_cache_tokens) : 1.0;
         s.longest = num_splits > 0 || blocks > 1 << 23 ? 0 : (int)blocks;
@@ -184,16 +181,18 @@ WqTreePlan wq_tree_plan(int64_t total_rows, int B, int Hq, int Hkv, int hd, int 
         }
         auto size = [&] {
             s.groups = s.units * s.splits;
-            s.bytes = s.splits > 1 ? wq_align256((size_t)s.groups * s.rows * (hd + 2) * 4) : 0;
+            s.bytes = s.splits > 1 ? wq_align256((size_t)s.groups * s.rows * (hd + 2) * 4) + wq_align256((size_t)s.units * sizeof(int4)) : 0;
         };
         size();
-        while (num_splits <= 0 && s.splits > 1 && s.bytes > room) s.splits--, size();
+        // (the join has a workgroup for four rows of every unit)
+        while (num_splits <= 0 && s.splits > 1 && (s.bytes > room || s.groups > WQ_MOST_GROUPS_256 / 2 || s.units * (s.rows / 4) > WQ_MOST_GROUPS_256)) s.splits--, size();
         return s;
     }
+    s.rows = ROWS<F32>;
     const int64_t units = tiles_of(total_rows, rep, B, s.rows) * Hkv;
     s.splits = num_splits > 0 ? num_splits : auto_splits_of((tiles_of(total_rows, rep, 0, s.rows) + used) * Hkv, max_cache_tokens + max_rows + 4 * 32, 256, 32);      // (every class ends in a tile of its own)
     auto bytes = [&]() -> size_t { return s.splits > 1 ? partials_bytes(total_rows * Hq, hd, s.splits) : 0; };
-    while (num_splits <= 0 && s.splits > 1 && bytes() > room) s.splits--;
+    while (num_splits <= 0 && s.splits > 1 && (bytes() > room || units * s.splits > WQ_MOST_GROUPS_256 / 2 || total_rows * Hq > 4 * WQ_MOST_GROUPS_256)) s.splits--;
     s.bytes = bytes();
     s.units = units;
     s.groups = units * s.splits;
@@ -218,14 +217,15 @@ int wq_launch_tree(wq_ctx* ctx, const WqTree& f)
     a.part_ml = a.part + f.total_rows * f.Hq * a.splits * hd;
     if (f.plan.columns) {
         a.longest = f.plan.longest;
+        a.found = reinterpret_cast<int4*>(reinterpret_cast<char*>(a.part) + wq_align256((size_t)f.plan.groups * f.plan.rows * (hd + 2) * 4));
         const TreeKernel kernel = f.plan.columns > WQ_STREAM_COLUMNS
                                       ? wq_tree_tiles_kernel(f.dtype, hd, f.dtype == WQ_F16 || f.lse ? hd / f.kv->group : 0)
                                       : wq_tree_stream_kernel(f.dtype, hd, f.plan.columns, f.lse != nullptr);
         switch (f.plan.columns) {
-            case 1: launch_pieces<16, 32>(ctx, a, kernel, f.dtype); break;
-            case 2: launch_pieces<32, 32>(ctx, a, kernel, f.dtype); break;
-            case 3: launch_pieces<48, 32>(ctx, a, kernel, f.dtype); break;
-            default: launch_pieces<128, 64>(ctx, a, kernel, f.dtype);
+            case 1: launch_pieces<16>(ctx, a, kernel, f.dtype); break;
+            case 2: launch_pieces<32>(ctx, a, kernel, f.dtype); break;
+            case 3: launch_pieces<48>(ctx, a, kernel, f.dtype); break;
+            default: launch_pieces<128>(ctx, a, kernel, f.dtype);
         }
         WQ_HIP_CHECK(ctx, hipGetLastError());
         return WQ_OK;

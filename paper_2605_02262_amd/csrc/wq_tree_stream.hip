@@ -138,6 +138,7 @@ __device__ __forceinline__ void stream_packed(Columns<HD, CW>& r, const char* s_
                             s[t][n][i] = fmaf((float)f[0], x[n][i], y);
                         }
                     }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
         } else {
@@ -260,11 +261,11 @@ __device__ __forceinline__ int first_block(int t0, int done, int lo) { return t0
 template <typename QT, int HD, int CW, bool PRECISE>
 __global__ __launch_bounds__(64 * NW, 2) void k_tree_stream(TreeArgs a)
 {
-    static_assert(NW == 4, "two rounds of joining");
-    constexpr int R = 16 * CW, ST = STEPS<F16, HD>, JOIN = HD / 16 * CW * 1024, TILE = 32 * HD * 2, QUERY = CW * ST * 1024;
-    constexpr int ENDS = NW / 2 * (JOIN + CW * 512), WALK = 3 * QUERY + NW * TILE, BIG = WALK > ENDS ? WALK : ENDS;
-    // the queries as each class's products take them, and the values of 16-bit rows, a piece of each wavefront; in the end two wavefronts' numerators, references
-    // and sums
+    static_assert(NW == 4, "a wavefront for each 16 of 64 channels");
+    constexpr int R = 16 * CW, ST = STEPS<F16, HD>, TILE = 32 * HD * 2, QUERY = CW * ST * 1024;
+    constexpr int ENDS = NW * CW * (4 * 1024 + 128), WALK = 3 * QUERY + NW * TILE, BIG = WALK > ENDS ? WALK : ENDS;
+    // the queries as each class's products take them, and the values of 16-bit rows, a piece of each wavefront; in the end numerators, references and
+    // sums
     __shared__ __align__(16) char s_big[BIG];
     __shared__ uint64_t s_seen[R * WORDS];
     __shared__ __align__(16) uint32_t s_meta[NW][256];         // (before the walk a tree's parents)
@@ -275,11 +276,15 @@ __global__ __launch_bounds__(64 * NW, 2) void k_tree_stream(TreeArgs a)
 
     const int unit = (int)blockIdx.x % a.units, piece = (int)blockIdx.x / a.units, kvh = unit % Hkv;
     Place p;
-    if (!find_place<R>(a.row_off, a.B, a.rep, a.total, unit / Hkv, p)) return;
+    if (!find_place<R>(a.row_off, a.B, a.rep, a.total, unit / Hkv, p)) {
+        leave_unit(a, unit, piece, p, 0);
+        return;
+    }
     const int b = p.seq, row0 = p.row0, rows = p.rows;
     const int64_t first_row = p.first;
     const Sequence s = sequence_of<32>(a, b, rows);
     if (piece >= s.pieces) return;
+    leave_unit(a, unit, piece, p, s.pieces);
     const int lo = begin_of(s, piece, 8), hi = begin_of(s, piece + 1, 8);
     const int node0 = row0 / a.rep, last_row = (row0 + R < rows ? row0 + R : rows) - 1;
     int newest = last_row / a.rep + 1;                         // (no row sees one behind itself)
@@ -392,64 +397,58 @@ __global__ __launch_bounds__(64 * NW, 2) void k_tree_stream(TreeArgs a)
             }
         }
     }
-    // The wavefronts' numerators together: the upper half's to the lower half, twice
+    // The wavefronts' numerators together, 64 channels at a time: each brings its own to the rows' common reference, and each sums up and stores 16 of them
+    float(*s_ml)[CW][2][16] = reinterpret_cast<float(*)[CW][2][16]>(s_big + 4 * NW * CW * 1024);
+    __syncthreads();                                           // (everybody has read the queries and its values)
 #pragma unroll
     for (int n = 0; n < CW; n++) {
         r.sum[n] = sum_of_column(r.sum[n]);
         r.ref[n] -= SHIFT<QT>;
+        if (j == 0) s_ml[wave][n][0][lane] = r.ref[n], s_ml[wave][n][1][lane] = r.sum[n];
     }
-    float(*s_ml)[64] = reinterpret_cast<float(*)[64]>(s_big + NW / 2 * JOIN);
+    __syncthreads();
+    float M[CW], L[CW];
 #pragma unroll
-    for (int half = NW / 2; half > 0; half /= 2) {
-        __syncthreads();
-        if (wave >= half && wave < 2 * half) {
+    for (int n = 0; n < CW; n++) {
+        M[n] = -INFINITY, L[n] = 0.f;
 #pragma unroll
-            for (int n = 0; n < CW; n++) {
-                s_ml[((wave - half) * CW + n) * 2][lane] = r.ref[n], s_ml[((wave - half) * CW + n) * 2 + 1][lane] = r.sum[n];
+        for (int w = 0; w < NW; w++) M[n] = fmaxf(M[n], s_ml[w][n][0][lane & 15]);
+        const float base = M[n] == -INFINITY ? 0.f : M[n], by = __builtin_amdgcn_exp2f(r.ref[n] - base);
 #pragma unroll
-                for (int ct = 0; ct < HD / 16; ct++) *reinterpret_cast<f4*>(s_big + (wave - half) * JOIN + (n * (HD / 16) + ct) * 1024 + lane * 16) = r.o[ct][n];
-            }
-        }
-        __syncthreads();
-        if (wave < half) {
+        for (int w = 0; w < NW; w++) L[n] += s_ml[w][n][1][lane & 15] * __builtin_amdgcn_exp2f(s_ml[w][n][0][lane & 15] - base);
 #pragma unroll
-            for (int n = 0; n < CW; n++) {
-                const float ref = s_ml[(wave * CW + n) * 2][lane], sum = s_ml[(wave * CW + n) * 2 + 1][lane], most = fmaxf(r.ref[n], ref), base = most == -INFINITY ? 0.f : most;
-                const float x = __builtin_amdgcn_exp2f(r.ref[n] - base), y = __builtin_amdgcn_exp2f(ref - base);
-                r.ref[n] = most, r.sum[n] = r.sum[n] * x + sum * y;
-#pragma unroll
-                for (int ct = 0; ct < HD / 16; ct++)
-                    r.o[ct][n] = r.o[ct][n] * x + *reinterpret_cast<const f4*>(s_big + wave * JOIN + (n * (HD / 16) + ct) * 1024 + lane * 16) * y;
-            }
-        }
+        for (int ct = 0; ct < HD / 16; ct++) r.o[ct][n] *= by;
     }
-    if (wave == 0) {
-        float* left = a.part + ((int64_t)unit * a.splits + piece) * PIECE<HD, R>;
+    float* left = a.part + ((int64_t)unit * a.splits + piece) * PIECE<HD, R>;
+#pragma unroll
+    for (int pass = 0; pass < HD / 64; pass++) {
+        if (pass > 0) __syncthreads();
+#pragma unroll
+        for (int n = 0; n < CW; n++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) *reinterpret_cast<f4*>(s_big + ((wave * CW + n) * 4 + i) * 1024 + lane * 16) = r.o[4 * pass + i][n];
+        __syncthreads();
 #pragma unroll
         for (int n = 0; n < CW; n++) {
-            const int row = row0 + 16 * n + (lane & 15);
+            f4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < NW; w++) x += *reinterpret_cast<const f4*>(s_big + ((w * CW + n) * 4 + wave) * 1024 + lane * 16);
+            const int row = row0 + 16 * n + (lane & 15), channel = 64 * pass + 16 * wave + 4 * j;
             if (row >= rows) continue;
-            if (a.parent && row / a.rep >= WQ_MAX_TREE) {  // refused: as if it saw nothing
-                r.ref[n] = -INFINITY, r.sum[n] = 0.f;
-#pragma unroll
-                for (int ct = 0; ct < HD / 16; ct++) r.o[ct][n] = f4{0.f, 0.f, 0.f, 0.f};
-            }
+            const bool refused = a.parent && row / a.rep >= WQ_MAX_TREE;       // as if it saw nothing
+            const float ref = refused ? -INFINITY : M[n], sum = refused ? 0.f : L[n];
+            if (refused) x = f4{0.f, 0.f, 0.f, 0.f};
+            const bool first = pass == 0 && wave == 0 && j == 0;
             if (s.pieces > 1) {
-                const int x = 16 * n + (lane & 15);
-#pragma unroll
-                for (int ct = 0; ct < HD / 16; ct++) *reinterpret_cast<f4*>(left + x * HD + 16 * ct + 4 * j) = r.o[ct][n];
-                if (j == 0) left[R * HD + 2 * x] = r.ref[n], left[R * HD + 2 * x + 1] = r.sum[n];
+                const int at = 16 * n + (lane & 15);
+                *reinterpret_cast<f4*>(left + at * HD + channel) = x;
+                if (first) left[R * HD + 2 * at] = ref, left[R * HD + 2 * at + 1] = sum;
                 continue;
             }
             const int64_t to_row = (first_row + row / a.rep) * a.Hq + kvh * a.rep + row % a.rep;
-            const float inv = one_over(r.sum[n]);
-            char* to = static_cast<char*>(a.out) + to_row * HD * 2;
-#pragma unroll
-            for (int ct = 0; ct < HD / 16; ct++) {
-                const f4 x = r.o[ct][n] * inv;
-                *reinterpret_cast<uint2*>(to + (16 * ct + 4 * j) * 2) = make_uint2(pack2(x[0], x[1], QT()), pack2(x[2], x[3], QT()));
-            }
-            if (a.lse && j == 0) a.lse[to_row] = log_sum_exp(r.ref[n], r.sum[n]);
+            x *= one_over(sum);
+            *reinterpret_cast<uint2*>(static_cast<char*>(a.out) + (to_row * HD + channel) * 2) = make_uint2(pack2(x[0], x[1], QT()), pack2(x[2], x[3], QT()));
+            if (a.lse && first) a.lse[to_row] = log_sum_exp(ref, sum);
         }
     }
 }
@@ -461,8 +460,7 @@ TreeKernel of_columns(int columns)
         case 1: return k_tree_stream<QT, HD, 1, PRECISE>;
         case 2: return k_tree_stream<QT, HD, 2, PRECISE>;
     }
-    if constexpr (!PRECISE || HD == 64) return k_tree_stream<QT, HD, 3, PRECISE>;
-    return nullptr;
+    return k_tree_stream<QT, HD, 3, PRECISE>;
 }
 
 TreeKernel stream_kernel(int dtype, int hd, int columns, bool precise)

@@ -62,9 +62,13 @@ __global__ __launch_bounds__(256, 2) void k_tree_tiles(TreeArgs a)
     const wq_packed_kv& kv = a.kv;
     const int unit = (int)blockIdx.x % a.units, piece = (int)blockIdx.x / a.units, kvh = unit % Hkv;
     Place p;
-    if (!find_place<R>(a.row_off, a.B, a.rep, a.total, unit / Hkv, p)) return;
+    if (!find_place<R>(a.row_off, a.B, a.rep, a.total, unit / Hkv, p)) {
+        leave_unit(a, unit, piece, p, 0);
+        return;
+    }
     const Sequence s = sequence_of<TK>(a, p.seq, p.rows);
     if (piece >= s.pieces) return;
+    leave_unit(a, unit, piece, p, s.pieces);
     const int lo = begin_of(s, piece, 1), hi = begin_of(s, piece + 1, 1), cached = s.all - (p.rows / a.rep + TK - 1) / TK;
     const int node0 = p.row0 / a.rep, last_row = (p.row0 + R < p.rows ? p.row0 + R : p.rows) - 1;
     int newest = last_row / a.rep + 1;                         // (no row sees one behind itself)

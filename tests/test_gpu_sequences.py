@@ -126,6 +126,8 @@ def test_sequences_that_are_refused_stay_as_they_are():
     ctx = W.Context(0)
     W.wq_append_rows(ctx, [x], [x], kvs, R.i32([0, 4]), 4, R.i32([0, 1, 2, 3]), R.i32([-1]))
     assert ctx.device_status() == W.DEV_BAD_INDEX and int(kvs[0].len16) == 2
+    W.wq_append_rows(ctx, [x[:0]], [x[:0]], kvs, R.i32([0, 0]), 4, R.i32([0, 1, 2, 3]), R.i32([1]))      # no row at all
+    assert ctx.device_status() == W.DEV_BAD_INDEX and int(kvs[0].len16) == 2
 
 
 def test_appending_rows_one_by_one_or_at_once():

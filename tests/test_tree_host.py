@@ -50,6 +50,10 @@ def test_tree_attention_without_rows(W, ctx):  # noqa: F811
     assert _tree(W, ctx, rows=0) == 0 and _tree(W, ctx, rows=0, q=None, k=None, v=None, ro=None, out=None) == 0
     assert _tree(W, ctx, _desc(W, B=0), B=0) == 0
     assert W.lib().wq_tree_attention(None, *([None, 0] * 3), 0, 0, 1, None, None, None, 0, 0, 1.0, 0, 0, None, None) == -1
+    # parts that the join's grid cannot hold: refused if asked for, else fewer
+    many = dict(B=65535, Hq=64, rows=65535 * 12, qs=64 * 64, ks=8 * 64, vs=8 * 64, mr=12, par=None)
+    assert _tree(W, ctx, _desc(W, Hkv=8, B=65535), splits=2, **many) == -2
+    assert W.tree_workspace_bytes(65535 * 12, 65535, 64, 8, 64, 1 << 62, (1 << 31) - 1) == 16384
     # a chain has no bound of 1024 rows; a workspace without room for parts is enough for one
     assert _tree(W, ctx, par=None, mr=2000, rows=4000, splits=64) == -4
 
@@ -80,7 +84,7 @@ def test_accept_refuses(W, ctx, bad, code):  # noqa: F811
 def _append(W, ctx, ds=None, k=(P, P), v=(P, P), **more):
     a = dict(n=2, ks=128, vs=128, dtype=BF, B=2, ro=P, rows=10, take=P, nt=P, mt=4)
     a.update(more)
-    ds = ds or [_desc(W), _desc(W)]
+    ds = ds or [_desc(W), _other(W)]
     arr = C.c_void_p * 2
     return W.lib().wq_append_rows(ctx, a["n"], None if k is None else arr(*k), a["ks"], None if v is None else arr(*v), a["vs"], a["dtype"], a["B"], a["ro"], a["rows"],
                                   a["take"], a["nt"], a["mt"], (W._PackedKV * 2)(*ds))
@@ -96,15 +100,20 @@ def test_append_rows_refuses(W, ctx, bad, code):  # noqa: F811
 
 def test_append_rows_refuses_caches(W, ctx):  # noqa: F811
     for more in (dict(Hkv=4), dict(hd=128), dict(dtype16=F16)):
-        assert _append(W, ctx, [_desc(W), _desc(W, **more)]) == -1
+        assert _append(W, ctx, [_desc(W), _other(W, **more)]) == -1
     d = _desc(W)
     d.v16 = P + 8
     assert _append(W, ctx, [_desc(W), d]) == -1
     d = _desc(W)
     d.len16 = None
     assert _append(W, ctx, [d, _desc(W)]) == -1
-    assert _append(W, ctx, [_desc(W, B=1 << 20), _desc(W, B=1 << 20)], B=1 << 20, mt=1 << 20, take=None, nt=None) == -2
-    assert _append(W, ctx, n=0) == 0 and _append(W, ctx, rows=0, k=(None, None), v=(None, None)) == 0 and _append(W, ctx, mt=0) == 0
+    assert _append(W, ctx, [_desc(W, B=1 << 20), _other(W, B=1 << 20)], B=1 << 20, mt=1 << 20, take=None, nt=None) == -2
+    assert _append(W, ctx, mt=(1 << 31) - 1, take=None, nt=None) == -2       # (rounded up in 32 bits it would be negative)
+    assert _append(W, ctx, [_desc(W), _desc(W)]) == -1                       # the same cache twice
+    d = _other(W)
+    d.len16 = P
+    assert _append(W, ctx, [_desc(W), d]) == -1
+    assert _append(W, ctx, n=0) == 0 and _append(W, ctx, rows=0, k=(None, None), v=(None, None), take=None, nt=None) == 0 and _append(W, ctx, mt=0) == 0
     assert _append(W, None) == -1
 
 
