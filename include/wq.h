@@ -420,10 +420,11 @@ size_t wq_shared_workspace_bytes(int B, int P, int Hq, int Hkv, int hd, int64_t 
  * type, contiguous; lse [total_rows, Hq] fp32 or NULL; rows of both that belong to no sequence are left as they were.
  * row_off [B+1] ascending, device; total_rows: host bound (rows beyond it are not read).  With parents a sequence has at most 1024
  * rows: those behind become zeros, their lse -infinity, and WQ_DEV_TOO_MANY_ROWS is raised; a chain may be as long as it likes.
- * max_rows (with parents at most 1024), max_cache_tokens: host bounds on one sequence's new rows and cached tokens, used for the number of parts and the
- * choice of kernels (any values give the same result to rounding).  num_splits: workgroups that share a tile of query rows' keys,
- * 1 .. 64, or 0 = automatic.
- * Arithmetic as in wq_decode_attention_shared; the new rows' keys and values enter as they are (fp32 too, where the cache will hold them in fp16).
+ * max_rows (with parents at most 1024): host bound on one sequence's new rows, 0: not known (the host then counts more workgroups than there is work for, which
+ * takes up to a tenth longer).  Rows of a sequence behind it become zeros as above.  max_cache_tokens: host bound on one sequence's cached tokens, used for the
+ * number of parts (any value gives the same result to rounding).  num_splits: workgroups that share the keys of a tile of query rows, 1 .. 64, or 0 = automatic.
+ * Arithmetic as in wq_decode_attention_shared; for bf16 with lse the codes of packed keys enter the products as they are, as for fp16 (keys rounded to
+ * 16 bits would show in the lse).  The new rows' keys and values enter as they are (fp32 too, where the cache will hold them in fp16).
  * Values of the new rows must be finite (those that a row does not see meet a weight of zero), and as small as for prompts.
  * Pointers 16-byte aligned, rows a multiple of 16 bytes apart (k's and v's at most 2^22 elements); at most 2^18 query heads; out must not overlap the inputs.
  * Workspace: wq_tree_workspace_bytes (as for prompts: with num_splits = 0 a call takes as many parts as there is room for).  */

@@ -640,7 +640,7 @@ int wq_tree_attention(wq_ctx* ctx, const void* q, int64_t q_stride, const void* 
         return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "too many rows");
     if (!ctx->ws || ctx->ws_bytes < WQ_WS_HEADER + plan.bytes)
         return wq_fail(ctx, WQ_ERR_WORKSPACE, "workspace too small for %d splits of %lld rows", plan.splits, (long long)total_rows);
-    return wq_launch_tree(ctx, {q, k, v, q_stride, k_stride, v_stride, dtype, B, Hq, kv, plan, row_off, parent, total_rows, sm_scale, out, lse});
+    return wq_launch_tree(ctx, {q, k, v, q_stride, k_stride, v_stride, dtype, B, Hq, kv, plan, row_off, parent, total_rows, max_rows, sm_scale, out, lse});
 }
 
 int wq_tree_accept(wq_ctx* ctx, const int32_t* tokens, const int32_t* target, const int32_t* parent, int B, const int32_t* row_off, int64_t total_rows, int max_rows,

@@ -239,6 +239,7 @@ constexpr int WQ_MAX_TREE = 1024;      // rows of a tree: what a workgroup keeps
 struct WqTreePlan {
     int rows, splits;                                             // query rows of a workgroup; parts of every row's keys
     int columns;                                                  // of 16 query rows: every wavefront brings its own keys; 0: tiles of keys for a workgroup
+    int tiles;                                                    // of query rows, of every sequence; 0: not known
     int longest;                                                  // blocks of 32 keys of the longest sequence: shorter ones have fewer parts; 0: all have the same
     size_t bytes;                                                 // workspace
     int64_t units, groups;                                        // tiles of query rows times KV heads; workgroups
@@ -251,6 +252,7 @@ struct WqTree {
     WqTreePlan plan;
     const int32_t *row_off, *parent;
     int64_t total_rows;
+    int max_rows;                                                 // 0: not known
     float sm_scale;
     void* out;
     float* lse;

@@ -9,6 +9,8 @@ struct TreeArgs {
     int64_t total;
     int B, Hq, rep;
     int units, splits;                         // (tile of rows, KV head) pairs, and the parts that each one's keys are cut into
+    int most;                                  // new rows of a sequence that count
+    int tiles;                                 // 16-bit types: tiles of rows of every sequence, or 0: numbered as in find_place
     float scale;                               // log2(e) * sm_scale
     uint32_t* status;
     wq_packed_kv kv;
@@ -55,6 +57,30 @@ __device__ __forceinline__ void find_ancestors(const int32_t* parent, int node0,
 }
 
 // ---- who does what -------------------------------------------------------------------------------------------------------
+// The rows of tile `tile`: the B sequences' first tiles, then their second ones ..  Numbers without a tile cost more than their start: the dispatcher deals workgroups
+// out in turn, and those behind wait for a full engine while others have room.  So they are few here, and at the end.
+template <int R>
+__device__ __forceinline__ bool place_of(const TreeArgs& a, int tile, Place& p)
+{
+    if (!a.tiles) return find_place<R>(a.row_off, a.B, a.rep, a.total, tile, p);
+    const int b = tile % a.B;
+    const int64_t first = clipped(a.row_off[b], a.total), end = clipped(a.row_off[b + 1], a.total);
+    p.seq = b, p.first = first, p.rows = end > first ? (int)((end - first) * a.rep) : 0, p.row0 = tile / a.B * R;
+    return p.row0 < p.rows;
+}
+// Rows behind a sequence's last tile, which its caller's bound left out: as if they saw nothing (16-bit types; by the last tile's first piece)
+template <int R, int HD>
+__device__ __forceinline__ void clear_rest(const TreeArgs& a, const Place& p, int kvh, int piece)
+{
+    if (piece > 0 || !a.tiles || p.row0 / R != a.tiles - 1) return;
+    for (int64_t i = threadIdx.x; i < (int64_t)(p.rows - p.row0 - R) * (HD / 8); i += blockDim.x) {
+        const int row = p.row0 + R + (int)(i / (HD / 8));
+        const int64_t at = (p.first + row / a.rep) * a.Hq + kvh * a.rep + row % a.rep;
+        reinterpret_cast<uint4*>(a.out)[at * (HD / 8) + i % (HD / 8)] = make_uint4(0, 0, 0, 0);
+        if (a.lse && i % (HD / 8) == 0) a.lse[at] = -INFINITY;
+    }
+}
+
 // A unit is a tile of R query rows of a sequence under one KV head; its keys are blocks of TK, those of the cache's four segments and then the new
 // rows'.  It is cut into a.splits pieces, a workgroup each; where the caller has told the longest sequence's blocks (a.longest), into as many as its own
 // length is of that: only the device knows it.

@@ -44,10 +44,10 @@ __global__ __launch_bounds__(64 * WAVES<F32>, 2) void k_tree(TreeArgs a)
     Place p;
     if (!find_place<R>(a.row_off, a.B, a.rep, a.total, unit / Hkv, p)) return;
     const int n = p.rows / a.rep, node0 = p.row0 / a.rep;      // the sequence's new rows; the first one of this tile
-    if (a.parent && n > WQ_MAX_TREE && p.row0 == 0 && threadIdx.x == 0) atomicOr(a.status, WQ_DEV_TOO_MANY_ROWS);
+    if (n > a.most && p.row0 == 0 && threadIdx.x == 0) atomicOr(a.status, WQ_DEV_TOO_MANY_ROWS);
     const int last_row = (p.row0 + R < p.rows ? p.row0 + R : p.rows) - 1;
     int tiles[4], len[4], newest = last_row / a.rep + 1;       // (no row sees one behind itself)
-    if (a.parent && newest > WQ_MAX_TREE) newest = WQ_MAX_TREE;
+    if (newest > a.most) newest = a.most;
     const int cached = tiles_of_cache<TK>(kv, p.seq, len, tiles), all = cached + (newest + TK - 1) / TK;
     const int lo = (int)((int64_t)split * all / a.splits), hi = (int)((int64_t)(split + 1) * all / a.splits);
 
@@ -87,15 +87,13 @@ __global__ __launch_bounds__(64 * WAVES<F32>, 2) void k_tree(TreeArgs a)
             attend_f32<HD>(r, q, (Lds4)s_k, (Lds4)s_v, key0, least, most, unrelated);
         }
     }
-    if (a.parent) {
 #pragma unroll
-        for (int c = 0; c < COLS; c++)
-            if ((wrow0 + 16 * c + (lane & 15)) / a.rep >= WQ_MAX_TREE) {        // refused: as if it saw nothing
-                r.ref[c] = -INFINITY, r.sum[c] = 0.f;
+    for (int c = 0; c < COLS; c++)
+        if ((wrow0 + 16 * c + (lane & 15)) / a.rep >= a.most) {        // refused: as if it saw nothing
+            r.ref[c] = -INFINITY, r.sum[c] = 0.f;
 #pragma unroll
-                for (int ct = 0; ct < HD / 16; ct++) r.o[ct][c] = f4{0.f, 0.f, 0.f, 0.f};
-            }
-    }
+            for (int ct = 0; ct < HD / 16; ct++) r.o[ct][c] = f4{0.f, 0.f, 0.f, 0.f};
+        }
     if (any) store_rows<F32, HD>(r, p, a.rep, a.Hq, kvh, wave, split, a.splits > 1 ? a.splits : 0, {a.out, a.lse, a.part, a.part_ml});
 }
 
@@ -158,7 +156,12 @@ WqTreePlan wq_tree_plan(int64_t total_rows, int B, int Hq, int Hkv, int hd, int 
         s.rows = 16 * s.columns;
         const int tile = s.columns <= WQ_STREAM_COLUMNS ? 32 : 64;
         s.units = tiles_of(total_rows, rep, B, s.rows) * Hkv;
-        const int64_t each = (total_rows + used - 1) / used, real = used * ((each * rep + s.rows - 1) / s.rows) * Hkv;      // units, if the sequences' rows are alike
+        if (const int64_t tiles = ((int64_t)max_rows * rep + s.rows - 1) / s.rows; tiles > 0 && tiles * B * Hkv <= s.units) s.tiles = (int)tiles, s.units = tiles * B * Hkv;
+        // Units, if the sequences' rows lie evenly about their average up to max_rows
+        const double mean = (double)total_rows / used, over = max_rows > mean ? max_rows - mean : 0;
+        double real = 0;
+        for (int i = 0; i < 16; i++) real += ceil(fmax(1.0, round(mean + (over > 0 ? over + 0.5 : 0) * (2 * i - 15) / 16)) * rep / s.rows) / 16;
+        real *= (double)used * Hkv;
         const int64_t blocks = (max_cache_tokens + tile - 1) / tile + ((int64_t)max_rows + tile - 1) / tile;
         // The cache's capacity says how long the sequences are on the average: those that are shorter than the longest have fewer pieces
         const double average = slots > 0 && slots < (int64_t)B * max_cache_tokens ? (double)slots / ((double)B * max_cache_tokens) : 1.0;
@@ -166,16 +169,19 @@ WqTreePlan wq_tree_plan(int64_t total_rows, int B, int Hq, int Hkv, int hd, int 
         if (num_splits > 0) {
             s.splits = num_splits;
         } else {
-            // Rounds of the workgroups that the card holds at a time (its registers and LDS hold `slots`; fewer are not spread evenly, and take as long), each of a
-            // piece's steps (a tile, or a block of each wavefront) and what a start and an end take in such steps; pieces have to be joined
+            // Rounds of the workgroups that the card holds at a time: `most` a compute unit, as its registers and LDS have it.  In steps of a workgroup that has a
+            // unit for itself (1.2 us: a tile of 64 keys, or a block of 32 of every wavefront): a piece's steps, which take longer where workgroups share a unit, its
+            // start and end; the join's launch and what the pieces leave in memory for it.  (us of 8 x 12800 tokens, 4 rows of 7 heads for each of 4 KV heads: 34 in 8
+            // pieces, a workgroup a unit; 35 in 12; 32 in 16, two a unit; 38 in 20)
             const bool tiles = s.columns > WQ_STREAM_COLUMNS;
-            const int at_once = hd == 128 ? (s.columns == 1 ? 768 : 512) : (s.columns == 1 ? 1024 : s.columns == WQ_STREAM_COLUMNS ? 512 : 768);
-            const double start = tiles ? 3 : 5, join = tiles ? 2 : 3;
+            const int most = hd == 128 ? (s.columns == 1 ? 3 : 2) : (s.columns == 1 ? 4 : s.columns == WQ_STREAM_COLUMNS ? 2 : 3);
+            constexpr double SLOWER[5] = {1, 1, 1.5, 2.1, 3};
             double best = 0;
             s.splits = 1;
             for (int p = 1; p <= WQ_MAX_ATTEND_SPLITS && p <= (blocks < 4 ? 1 : blocks); p++) {
-                const double groups = (double)real * p * average, rounds = groups <= at_once ? 1 : ceil(groups / at_once);
-                const double time = rounds * (ceil((double)blocks / p / (tiles ? 1 : WQ_STREAM_WAVES)) + start) + (p > 1 ? join : 0);
+                const double groups = real * (average < 0.95 ? fmin(p, p * average + 0.5) : p), rounds = ceil(groups / (256 * most));
+                const double steps = ceil((double)blocks / p / (tiles ? 1 : WQ_STREAM_WAVES)) * SLOWER[(int)fmin(most, ceil(groups / 256))];
+                const double time = rounds * (steps + (tiles ? 5 : 6)) + (p > 1 ? 4 + groups * s.rows * hd * 4 / 6.6e6 : 0);
                 if (p == 1 || time < best) best = time, s.splits = p;
             }
         }
@@ -207,6 +213,8 @@ int wq_launch_tree(wq_ctx* ctx, const WqTree& f)
     a.q_stride = f.q_stride * size, a.k_stride = f.k_stride * size, a.v_stride = f.v_stride * size;
     a.row_off = f.row_off, a.parent = f.parent;
     a.total = f.total_rows;
+    a.most = f.max_rows > 0 ? f.max_rows : INT32_MAX;
+    if (f.parent && a.most > WQ_MAX_TREE) a.most = WQ_MAX_TREE;
     a.B = f.B, a.Hq = f.Hq, a.rep = f.Hq / f.kv->Hkv, a.splits = f.plan.splits;
     a.units = (int)f.plan.units;
     a.scale = f.sm_scale * WQ_LOG2E;
@@ -217,6 +225,7 @@ int wq_launch_tree(wq_ctx* ctx, const WqTree& f)
     a.part_ml = a.part + f.total_rows * f.Hq * a.splits * hd;
     if (f.plan.columns) {
         a.longest = f.plan.longest;
+        a.tiles = f.plan.tiles;
         a.found = reinterpret_cast<int4*>(reinterpret_cast<char*>(a.part) + wq_align256((size_t)f.plan.groups * f.plan.rows * (hd + 2) * 4));
         const TreeKernel kernel = f.plan.columns > WQ_STREAM_COLUMNS
                                       ? wq_tree_tiles_kernel(f.dtype, hd, f.dtype == WQ_F16 || f.lse ? hd / f.kv->group : 0)

@@ -276,10 +276,11 @@ __global__ __launch_bounds__(64 * NW, 2) void k_tree_stream(TreeArgs a)
 
     const int unit = (int)blockIdx.x % a.units, piece = (int)blockIdx.x / a.units, kvh = unit % Hkv;
     Place p;
-    if (!find_place<R>(a.row_off, a.B, a.rep, a.total, unit / Hkv, p)) {
+    if (!place_of<R>(a, unit / Hkv, p)) {
         leave_unit(a, unit, piece, p, 0);
         return;
     }
+    clear_rest<R, HD>(a, p, kvh, piece);
     const int b = p.seq, row0 = p.row0, rows = p.rows;
     const int64_t first_row = p.first;
     const Sequence s = sequence_of<32>(a, b, rows);
@@ -288,8 +289,8 @@ __global__ __launch_bounds__(64 * NW, 2) void k_tree_stream(TreeArgs a)
     const int lo = begin_of(s, piece, 8), hi = begin_of(s, piece + 1, 8);
     const int node0 = row0 / a.rep, last_row = (row0 + R < rows ? row0 + R : rows) - 1;
     int newest = last_row / a.rep + 1;                         // (no row sees one behind itself)
-    if (a.parent && newest > WQ_MAX_TREE) newest = WQ_MAX_TREE;
-    if (a.parent && rows / a.rep > WQ_MAX_TREE && row0 == 0 && lo == 0 && threadIdx.x == 0) atomicOr(a.status, WQ_DEV_TOO_MANY_ROWS);
+    if (newest > a.most) newest = a.most;
+    if (rows / a.rep > a.most && row0 == 0 && lo == 0 && threadIdx.x == 0) atomicOr(a.status, WQ_DEV_TOO_MANY_ROWS);
     const int cached = s.all - (rows / a.rep + 31) / 32;
     if (a.parent && hi > cached) find_ancestors(a.parent + first_row, node0, last_row / a.rep + 1 - node0, s_seen, reinterpret_cast<int32_t*>(s_meta), 64 * NW);
 
@@ -435,7 +436,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_tree_stream(TreeArgs a)
             for (int w = 0; w < NW; w++) x += *reinterpret_cast<const f4*>(s_big + ((w * CW + n) * 4 + wave) * 1024 + lane * 16);
             const int row = row0 + 16 * n + (lane & 15), channel = 64 * pass + 16 * wave + 4 * j;
             if (row >= rows) continue;
-            const bool refused = a.parent && row / a.rep >= WQ_MAX_TREE;       // as if it saw nothing
+            const bool refused = row / a.rep >= a.most;       // as if it saw nothing
             const float ref = refused ? -INFINITY : M[n], sum = refused ? 0.f : L[n];
             if (refused) x = f4{0.f, 0.f, 0.f, 0.f};
             const bool first = pass == 0 && wave == 0 && j == 0;

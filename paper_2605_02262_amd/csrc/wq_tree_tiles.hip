@@ -62,18 +62,19 @@ __global__ __launch_bounds__(256, 2) void k_tree_tiles(TreeArgs a)
     const wq_packed_kv& kv = a.kv;
     const int unit = (int)blockIdx.x % a.units, piece = (int)blockIdx.x / a.units, kvh = unit % Hkv;
     Place p;
-    if (!find_place<R>(a.row_off, a.B, a.rep, a.total, unit / Hkv, p)) {
+    if (!place_of<R>(a, unit / Hkv, p)) {
         leave_unit(a, unit, piece, p, 0);
         return;
     }
+    clear_rest<R, HD>(a, p, kvh, piece);
     const Sequence s = sequence_of<TK>(a, p.seq, p.rows);
     if (piece >= s.pieces) return;
     leave_unit(a, unit, piece, p, s.pieces);
     const int lo = begin_of(s, piece, 1), hi = begin_of(s, piece + 1, 1), cached = s.all - (p.rows / a.rep + TK - 1) / TK;
     const int node0 = p.row0 / a.rep, last_row = (p.row0 + R < p.rows ? p.row0 + R : p.rows) - 1;
     int newest = last_row / a.rep + 1;                         // (no row sees one behind itself)
-    if (a.parent && newest > WQ_MAX_TREE) newest = WQ_MAX_TREE;
-    if (a.parent && p.rows / a.rep > WQ_MAX_TREE && p.row0 == 0 && lo == 0 && threadIdx.x == 0) atomicOr(a.status, WQ_DEV_TOO_MANY_ROWS);
+    if (newest > a.most) newest = a.most;
+    if (p.rows / a.rep > a.most && p.row0 == 0 && lo == 0 && threadIdx.x == 0) atomicOr(a.status, WQ_DEV_TOO_MANY_ROWS);
 
     Rows<HD> r;
     Query<F16, HD> q;
@@ -115,7 +116,7 @@ __global__ __launch_bounds__(256, 2) void k_tree_tiles(TreeArgs a)
         float sum = sum_of_column(r.sum[n]);
         if (row >= p.rows) continue;
         float ref = r.ref[n] - SHIFT<QT>;
-        if (a.parent && row / a.rep >= WQ_MAX_TREE) {          // refused: as if it saw nothing
+        if (row / a.rep >= a.most) {          // refused: as if it saw nothing
             ref = -INFINITY, sum = 0.f;
 #pragma unroll
             for (int ct = 0; ct < HD / 16; ct++) r.o[ct][n] = f4{0.f, 0.f, 0.f, 0.f};

@@ -155,6 +155,34 @@ def test_a_tree_with_too_many_rows():
             _compare(out[s], lse[s], q[s], kk, vv, sees, 0.125, torch.bfloat16)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,most,chain", [([40, 3, 9], 5, True), ([300, 0, 70], 20, True), ([60, 4, 0], 8, False), ([5, 6, 5], 5, False), ([700, 650, 3], 640, True)])
+def test_sequences_with_more_rows_than_the_caller_said(dtype, rows, most, chain):
+    Hq, Hkv, hd = 14, 2, 64
+    rng = np.random.default_rng(9)
+    kv, cached = R.make_cache(rng, [(0, 40, 0, 3), (0, 0, 9, 0), (64, 0, 1, 33)], Hkv, hd, 32, torch.bfloat16 if dtype == torch.bfloat16 else torch.float16)
+    off = np.cumsum([0] + rows)
+    total = int(off[-1])
+    q, k, v = _inputs(rng, total + 2, (Hq, Hkv, hd), dtype)          # (the last two rows belong to nobody)
+    parents = [T.random_tree(rng, n) for n in rows]
+    for splits in (0, 1, 3):
+        ctx = W.Context(max(1 << 22, W.tree_workspace_bytes(total + 2, 3, Hq, Hkv, hd, 98, most, splits)))
+        out, lse = torch.full((total + 2, Hq, hd), 77.0, device="cuda", dtype=dtype), torch.full((total + 2, Hq), 77.0, device="cuda")
+        parent = None if chain else R.i32(sum(parents, []) + [0, 0])
+        W.wq_tree_attention(ctx, q, k, v, kv, R.i32(off), 0.125, parent, most, 98, splits, out, lse)
+        assert ctx.device_status() == W.DEV_TOO_MANY_ROWS
+        assert bool((out[total:] == 77).all()) and bool((lse[total:] == 77).all())
+        for b, n in enumerate(rows):
+            a, m = int(off[b]), min(n, most)
+            assert bool((out[a + m:a + n] == 0).all()) and bool((lse[a + m:a + n] == -math.inf).all())
+            if not m:
+                continue
+            s = slice(a, a + m)
+            kk, vv = (torch.cat([c, x[s].double().cpu()]) for c, x in zip(cached[b], (k, v)))
+            new = torch.tril(torch.ones(m, m, dtype=torch.bool)) if chain else T.seen(parents[b][:m], m)
+            _compare(out[s], lse[s], q[s], kk, vv, torch.cat([torch.ones(m, cached[b][0].shape[0], dtype=torch.bool), new], 1), 0.125, dtype)
+
+
 def test_long_caches():
     _check([(2500, 2000, 1100, 150)], [40], (14, 2, 128), 64, torch.bfloat16)
     _check([(2500, 2000, 1100, 150), (9, 0, 0, 4000)], [4, 2], LARGE, 64, torch.bfloat16)

@@ -22,7 +22,7 @@ def _tree(W, ctx, d=None, **more):
     (dict(Hq=15), -2), (dict(Hq=18, qs=18 * 64), -2), (dict(Hq=0), -2), (dict(rows=1 << 31), -2), (dict(mr=1025), -2), (dict(splits=-1), -1), (dict(splits=65), -1),
     (dict(sm=0.0), -1), (dict(sm=-1.0), -1), (dict(sm=math.nan), -1), (dict(sm=math.inf), -1), (dict(sm=3e38), -1), (dict(q=None), -1), (dict(k=None), -1), (dict(v=None), -1),
     (dict(ro=None), -1), (dict(out=None), -1), (dict(out=P + 8), -1), (dict(q=P + 8), -1), (dict(k=P + 2), -1), (dict(qs=100), -1), (dict(ks=132), -1), (dict(vs=64), -1),
-    (dict(ks=(1 << 22) + 8), -2), (dict(vs=1 << 23), -2), (dict(splits=64), -4), (dict(rows=100000, splits=2), -4)])
+    (dict(ks=(1 << 22) + 8), -2), (dict(vs=1 << 23), -2), (dict(splits=64), -4), (dict(rows=100000, splits=2, mr=0), -4)])
 def test_tree_attention_refuses(W, ctx, bad, code):  # noqa: F811
     assert _tree(W, ctx, **bad) == code
     assert W.lib().wq_last_error(ctx)
@@ -51,7 +51,7 @@ def test_tree_attention_without_rows(W, ctx):  # noqa: F811
     assert _tree(W, ctx, _desc(W, B=0), B=0) == 0
     assert W.lib().wq_tree_attention(None, *([None, 0] * 3), 0, 0, 1, None, None, None, 0, 0, 1.0, 0, 0, None, None) == -1
     # parts that the join's grid cannot hold: refused if asked for, else fewer
-    many = dict(B=65535, Hq=64, rows=65535 * 12, qs=64 * 64, ks=8 * 64, vs=8 * 64, mr=12, par=None)
+    many = dict(B=65535, Hq=64, rows=65535 * 12, qs=64 * 64, ks=8 * 64, vs=8 * 64, mr=17, par=None)
     assert _tree(W, ctx, _desc(W, Hkv=8, B=65535), splits=2, **many) == -2
     assert W.tree_workspace_bytes(65535 * 12, 65535, 64, 8, 64, 1 << 62, (1 << 31) - 1) == 16384
     # a chain has no bound of 1024 rows; a workspace without room for parts is enough for one
