@@ -766,14 +766,12 @@ struct PackedValues {
 // Tiles t0 .. t1-1 of a class's segment.  G: the head's groups, whose codes enter the products as they are; 0: keys expanded to fp16 (q_sum and m_lds
 // are not read)
 template <int HD, int BITS, int G, bool TOGETHER = false>
-__device__ __forceinline__ void walk_packed(Rows<HD>& r, const Query<F16, HD>& q, const float (&q_sum)[COLS][G ? G : 1], const wq_packed_kv& kv, int kvh, int64_t tok0,
-                                            int len, int t0, int t1, Lds k_lds, Lds v_lds, Lds m_lds)
+__device__ __forceinline__ void walk_packed(Rows<HD>& r, const Query<F16, HD>& q, const float (&q_sum)[COLS][G ? G : 1], PackedKeys<HD, BITS, 64>& keys,
+                                            PackedValues<HD, BITS, 64>& values, int len, int t0, int t1, Lds k_lds, Lds v_lds, Lds m_lds)
 {
     using Order = std::conditional_t<BITS == 8, Near, Far>;
     constexpr int BYTES = TILE_BYTES<F16, HD>;
-    const int slots = (len + 31) / 32 * 32, lane = threadIdx.x & 63;
-    PackedKeys<HD, BITS, 64> keys(kv, kvh, tok0, slots);
-    PackedValues<HD, BITS, 64> values(kv, kvh, tok0, slots);
+    const int lane = threadIdx.x & 63;
     auto k_of = [&](int t) { return (Lds4)(k_lds + (t & 1) * BYTES); };
     auto v_of = [&](int t) { return (Lds4)(v_lds + (t & 1) * BYTES); };
     auto bring_keys = [&](int t) {
@@ -794,9 +792,7 @@ __device__ __forceinline__ void walk_packed(Rows<HD>& r, const Query<F16, HD>& q
     };
     auto value = [&](int t, int vs, int ct) { return v_of(t)[(vs * (HD / 16) + ct) * 64 + lane]; };
     __syncthreads();                                           // (whatever was in LDS before has been read)
-    if constexpr (TOGETHER) {
-        keys.load(t0);
-        values.load(t0);
+    if constexpr (TOGETHER) {                                  // (its caller has loaded tile t0)
         auto bring = [&](int t) {
             bring_keys(t);
             bring_values(t);
@@ -1062,23 +1058,34 @@ __device__ __forceinline__ void walk_cache(Rows<HD>& r, Query<Walked<QT>, HD>& q
         const int t0 = lo > done ? lo - done : 0, t1 = hi - done < tiles[c] ? hi - done : tiles[c];
         done += tiles[c];
         if (t0 >= t1) return;
+        auto prepare = [&]() __attribute__((always_inline)) {
 #pragma unroll
-        for (int n = 0; n < COLS; n++) {
-            r.limit[n] = len[c];
-            r.scale[n] = scale;
-            if constexpr (G > 0) load_query_codes<BITS, G, HD>(q, n, row_at[n], q_sum[n]);
-            else load_query_quarter<CT, HD>(q, n, row_at[n]);
-            bool bad = false;
-            if constexpr (PIPED) bad = not_finite<QT, HD>(q, n);
-            // (kept from 0 and infinity: a masked logit, -infinity, times 0 and a logit of 0 times infinity would be NaN.  A scale that small leaves every
-            // logit below 2^-100; with one that large logits that differ at all differ by 2^70 or more)
-            if constexpr (std::is_same_v<QT, Bf16>) r.scale[n] = fminf(fmaxf(scale * query_as_f16<HD>(q, n), FLT_MIN), FLT_MAX);
-            if constexpr (std::is_same_v<QT, Bf16> && G > 0) sum_query_codes<G, HD>(q, n, q_sum[n]);
-            if (bad) r.scale[n] = NAN;
-            if constexpr (PIPED && G == 0) order_query<BITS, HD>(q, n);
-        }
+            for (int n = 0; n < COLS; n++) {
+                r.limit[n] = len[c];
+                r.scale[n] = scale;
+                if constexpr (G > 0) load_query_codes<BITS, G, HD>(q, n, row_at[n], q_sum[n]);
+                else load_query_quarter<CT, HD>(q, n, row_at[n]);
+                bool bad = false;
+                if constexpr (PIPED) bad = not_finite<QT, HD>(q, n);
+                // (kept from 0 and infinity: a masked logit, -infinity, times 0 and a logit of 0 times infinity would be NaN.  A scale that small leaves every
+                // logit below 2^-100; with one that large logits that differ at all differ by 2^70 or more)
+                if constexpr (std::is_same_v<QT, Bf16>) r.scale[n] = fminf(fmaxf(scale * query_as_f16<HD>(q, n), FLT_MIN), FLT_MAX);
+                if constexpr (std::is_same_v<QT, Bf16> && G > 0) sum_query_codes<G, HD>(q, n, q_sum[n]);
+                if (bad) r.scale[n] = NAN;
+                if constexpr (PIPED && G == 0) order_query<BITS, HD>(q, n);
+            }
+        };
+        if constexpr (!PIPED || !TREE) prepare();
         if constexpr (PIPED) {
-            walk_packed<HD, BITS, G, TREE>(r, q, q_sum, kv, kvh, kv.cls_off[c][seq], len[c], t0, t1, s_k, s_v, s_m);
+            const int slots = (len[c] + 31) / 32 * 32;
+            PackedKeys<HD, BITS, 64> keys(kv, kvh, kv.cls_off[c][seq], slots);
+            PackedValues<HD, BITS, 64> values(kv, kvh, kv.cls_off[c][seq], slots);
+            if constexpr (TREE) {                              // the first tile is on its way while the queries are prepared
+                keys.load(t0);
+                values.load(t0);
+                prepare();
+            }
+            walk_packed<HD, BITS, G, TREE>(r, q, q_sum, keys, values, len[c], t0, t1, s_k, s_v, s_m);
         } else {
             PackedKeys<HD, BITS, 32> keys(kv, kvh, kv.cls_off[c][seq], 0);
             PackedValues<HD, BITS, 32> values(kv, kvh, kv.cls_off[c][seq], 0);

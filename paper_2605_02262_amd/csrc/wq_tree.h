@@ -63,7 +63,7 @@ template <int R>
 __device__ __forceinline__ bool place_of(const TreeArgs& a, int tile, Place& p)
 {
     if (!a.tiles) return find_place<R>(a.row_off, a.B, a.rep, a.total, tile, p);
-    const int b = tile % a.B;
+    const int b = tile % a.B;                              // (known before the rows are: the cache's tables are read beside them)
     const int64_t first = clipped(a.row_off[b], a.total), end = clipped(a.row_off[b + 1], a.total);
     p.seq = b, p.first = first, p.rows = end > first ? (int)((end - first) * a.rep) : 0, p.row0 = tile / a.B * R;
     return p.row0 < p.rows;

@@ -275,15 +275,23 @@ __global__ __launch_bounds__(64 * NW, 2) void k_tree_stream(TreeArgs a)
     const wq_packed_kv& kv = a.kv;
 
     const int unit = (int)blockIdx.x % a.units, piece = (int)blockIdx.x / a.units, kvh = unit % Hkv;
-    Place p;
-    if (!place_of<R>(a, unit / Hkv, p)) {
+    Place p = {};
+    const bool there = place_of<R>(a, unit / Hkv, p);
+    const int b = p.seq, row0 = p.row0, rows = there ? p.rows : 0;
+    const int64_t first_row = p.first;
+    // A wavefront prepares a column's queries (CW <= 4); they are on their way while the cache's tables are
+    auto row_at = [&](int n) -> const char* {
+        const int row = row0 + 16 * n + (lane & 15);
+        return row < rows ? a.q + (first_row + row / a.rep) * a.q_stride + (kvh * a.rep + row % a.rep) * (HD * 2) : nullptr;
+    };
+    QueryRows<F16, HD, 1> query;
+    if (wave < CW) load_query_quarter<F16, HD>(query, 0, row_at(wave));
+    const Sequence s = sequence_of<32>(a, b, rows);
+    if (!there) {
         leave_unit(a, unit, piece, p, 0);
         return;
     }
     clear_rest<R, HD>(a, p, kvh, piece);
-    const int b = p.seq, row0 = p.row0, rows = p.rows;
-    const int64_t first_row = p.first;
-    const Sequence s = sequence_of<32>(a, b, rows);
     if (piece >= s.pieces) return;
     leave_unit(a, unit, piece, p, s.pieces);
     const int lo = begin_of(s, piece, 8), hi = begin_of(s, piece + 1, 8);
@@ -294,14 +302,9 @@ __global__ __launch_bounds__(64 * NW, 2) void k_tree_stream(TreeArgs a)
     const int cached = s.all - (rows / a.rep + 31) / 32;
     if (a.parent && hi > cached) find_ancestors(a.parent + first_row, node0, last_row / a.rep + 1 - node0, s_seen, reinterpret_cast<int32_t*>(s_meta), 64 * NW);
 
-    // Queries: a wavefront prepares a column (CW <= 4), in fp16 and in every class's order
-    auto row_at = [&](int n) -> const char* {
-        const int row = row0 + 16 * n + (lane & 15);
-        return row < rows ? a.q + (first_row + row / a.rep) * a.q_stride + (kvh * a.rep + row % a.rep) * (HD * 2) : nullptr;
-    };
+    // Queries in fp16 and in every class's order
     if (wave < CW) {
-        QueryRows<F16, HD, 1> q, y;
-        load_query_quarter<F16, HD>(q, 0, row_at(wave));
+        QueryRows<F16, HD, 1>&q = query, y;
         const bool bad = not_finite<QT, HD>(q, 0);
         float scale = a.scale;
         if constexpr (std::is_same_v<QT, Bf16>) scale = fminf(fmaxf(a.scale * query_as_f16<HD>(q, 0), FLT_MIN), FLT_MAX);      // (see walk_cache)

@@ -61,13 +61,14 @@ __global__ __launch_bounds__(256, 2) void k_tree_tiles(TreeArgs a)
     const int Hkv = a.kv.Hkv, wave = this_wave(), lane = threadIdx.x & 63;
     const wq_packed_kv& kv = a.kv;
     const int unit = (int)blockIdx.x % a.units, piece = (int)blockIdx.x / a.units, kvh = unit % Hkv;
-    Place p;
-    if (!place_of<R>(a, unit / Hkv, p)) {
+    Place p = {};
+    const bool there = place_of<R>(a, unit / Hkv, p);
+    const Sequence s = sequence_of<TK>(a, p.seq, there ? p.rows : 0);
+    if (!there) {
         leave_unit(a, unit, piece, p, 0);
         return;
     }
     clear_rest<R, HD>(a, p, kvh, piece);
-    const Sequence s = sequence_of<TK>(a, p.seq, p.rows);
     if (piece >= s.pieces) return;
     leave_unit(a, unit, piece, p, s.pieces);
     const int lo = begin_of(s, piece, 1), hi = begin_of(s, piece + 1, 1), cached = s.all - (p.rows / a.rep + TK - 1) / TK;
