@@ -1,5 +1,10 @@
 // wq_tree_attention: several new rows of every sequence attend to its packed cache and to each other, along a tree of drafted tokens or as a
 // chain.  A row is a (new row, query head) pair, as in wq_attend.hip; its sequence's keys are the cache's tiles and, behind them, the new rows'.
+//     out = sum_j w_j v_j / sum_j w_j,   w_j = 2^(scale q.k_j - ref),   ref a running reference of the row, lse = ln 2 (ref + log2 sum_j w_j)
+// in one pass over the keys; what several workgroups have of a row's sums is brought to a common ref and added (k_tree_join).
+// 16-bit types: by the rows that a sequence has under a KV head.  Up to 48 (and 49 to 64 as two tiles): wq_tree_stream.hip, near the cache's bytes for few;
+// more: wq_tree_tiles.hip, bound by the vector instructions that expand codes and form weights.  Here: who gets what, the join, and fp32, whose products have a
+// ninth of the 16-bit rate (3 trees of 7 rows over 144 tokens 13.4 us, of that two launches 9).
 #include "wq_tree.h"
 
 namespace {
@@ -97,7 +102,8 @@ __global__ __launch_bounds__(64 * WAVES<F32>, 2) void k_tree(TreeArgs a)
     if (any) store_rows<F32, HD>(r, p, a.rep, a.Hq, kvh, wave, split, a.splits > 1 ? a.splits : 0, {a.out, a.lse, a.part, a.part_ml});
 }
 
-// The pieces of units that are cut: a wavefront per row
+// The pieces of units that are cut: a wavefront per row; a row's pieces are read by halves of it in turn.  A launch of its own: with the last workgroup of a unit
+// joining, 32 pieces of 128 rows (2 MB) would go through one compute unit.  (us: 4.5 of 1000 rows in 4 pieces, 7 of 4096 in 16)
 template <int HD, int R>
 __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a, int dtype)
 {
@@ -108,6 +114,15 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a, int dtype)
     const float* parts = a.part + (int64_t)unit * a.splits * PIECE<HD, R>;
     auto piece = [&](int i) { return parts + (int64_t)i * PIECE<HD, R>; };
     constexpr int LANES = HD / 4, GROUPS = 64 / LANES;
+    f4 y[8];
+    auto load = [&](int i0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = 0; k < 8; k++) {
+            const int i = i0 + k * GROUPS + lane / LANES;
+            y[k] = i < pieces ? *reinterpret_cast<const f4*>(piece(i) + in * HD + 4 * (lane % LANES)) : f4{0.f, 0.f, 0.f, 0.f};
+        }
+    };
+    load(0);                                   // (on their way while the weights are found)
     float m = -INFINITY, l = 0.f;              // lane i: piece i
     if (lane < pieces) {
         const float* ml = piece(lane) + R * HD + 2 * in;
@@ -116,12 +131,7 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a, int dtype)
     const float M = wave_max(m), w = __builtin_amdgcn_exp2f(m - (M == -INFINITY ? 0.f : M)), L = wave_sum(l * w);
     f4 x = {0.f, 0.f, 0.f, 0.f};
     for (int i0 = 0; i0 < pieces; i0 += 8 * GROUPS) {
-        f4 y[8];
-#pragma unroll
-        for (int k = 0; k < 8; k++) {
-            const int i = i0 + k * GROUPS + lane / LANES;
-            y[k] = i < pieces ? *reinterpret_cast<const f4*>(piece(i) + in * HD + 4 * (lane % LANES)) : f4{0.f, 0.f, 0.f, 0.f};
-        }
+        if (i0 > 0) load(i0);
 #pragma unroll
         for (int k = 0; k < 8; k++) {
             const int i = i0 + k * GROUPS + lane / LANES;
@@ -148,6 +158,13 @@ WqTreePlan wq_tree_plan(int64_t total_rows, int B, int Hq, int Hkv, int hd, int 
     const int64_t used = total_rows < B ? total_rows : B;     // sequences that have rows
     WqTreePlan s = {};
     if (max_cache_tokens > int64_t(1) << 40) max_cache_tokens = int64_t(1) << 40;
+    // Units, if the sequences' rows lie evenly about their average up to max_rows
+    const double mean = (double)total_rows / used, over = max_rows > mean ? max_rows - mean : 0;
+    auto units_of = [&](int rows) {
+        double n = 0;
+        for (int i = 0; i < 16; i++) n += ceil(fmax(1.0, round(mean + (over > 0 ? over + 0.5 : 0) * (2 * i - 15) / 16)) * rep / rows) / 16;
+        return n * used * Hkv;
+    };
     if (dtype != WQ_F32) {
         // Columns of a sequence, on the average.  Up to three: every wavefront brings its own keys; four in two tiles (us of 8 x 56 rows over 12800 tokens, 4 KV heads of
         // 128: 62, in a tile of 128 rows 73); more (and five: 74, 75) in tiles of 128 rows
@@ -157,11 +174,7 @@ WqTreePlan wq_tree_plan(int64_t total_rows, int B, int Hq, int Hkv, int hd, int 
         const int tile = s.columns <= WQ_STREAM_COLUMNS ? 32 : 64;
         s.units = tiles_of(total_rows, rep, B, s.rows) * Hkv;
         if (const int64_t tiles = ((int64_t)max_rows * rep + s.rows - 1) / s.rows; tiles > 0 && tiles * B * Hkv <= s.units) s.tiles = (int)tiles, s.units = tiles * B * Hkv;
-        // Units, if the sequences' rows lie evenly about their average up to max_rows
-        const double mean = (double)total_rows / used, over = max_rows > mean ? max_rows - mean : 0;
-        double real = 0;
-        for (int i = 0; i < 16; i++) real += ceil(fmax(1.0, round(mean + (over > 0 ? over + 0.5 : 0) * (2 * i - 15) / 16)) * rep / s.rows) / 16;
-        real *= (double)used * Hkv;
+        const double real = units_of(s.rows);
         const int64_t blocks = (max_cache_tokens + tile - 1) / tile + ((int64_t)max_rows + tile - 1) / tile;
         // The cache's capacity says how long the sequences are on the average: those that are shorter than the longest have fewer pieces
         const double average = slots > 0 && slots < (int64_t)B * max_cache_tokens ? (double)slots / ((double)B * max_cache_tokens) : 1.0;
@@ -196,7 +209,20 @@ WqTreePlan wq_tree_plan(int64_t total_rows, int B, int Hq, int Hkv, int hd, int 
     }
     s.rows = ROWS<F32>;
     const int64_t units = tiles_of(total_rows, rep, B, s.rows) * Hkv;
-    s.splits = num_splits > 0 ? num_splits : auto_splits_of((tiles_of(total_rows, rep, 0, s.rows) + used) * Hkv, max_cache_tokens + max_rows + 4 * 32, 256, 32);      // (every class ends in a tile of its own)
+    s.splits = num_splits > 0 ? num_splits : 1;
+    if (num_splits <= 0) {
+        // Rounds as above, in steps of 32 keys.  A workgroup whose sequences have few rows multiplies with some of its wavefronts only, and shares its unit at little
+        // cost (us of 30 x 18700 tokens, 4 rows of 7 heads for each of 4 KV heads of 128: 1288 in 2 parts, 240 workgroups; 681 in 4; 700 in 8; 629 in 24)
+        const int64_t blocks = (max_cache_tokens + 31) / 32 + ((int64_t)max_rows + 31) / 32;
+        const int most = hd == 128 ? 2 : 3;
+        const double real = units_of(s.rows), active = fmin(4.0, ceil(mean * rep / 32)) / 4, slower = 1 + 0.7 * active;
+        double best = 0;
+        for (int p = 1; p <= WQ_MAX_ATTEND_SPLITS && p <= (blocks < 4 ? 1 : blocks); p++) {
+            const double groups = real * p, rounds = ceil(groups / (256 * most)), share = fmin(most, ceil(groups / 256));
+            const double time = rounds * (ceil((double)blocks / p) * pow(slower, share - 1) + 3) + (p > 1 ? 2 + p * 0.1 : 0);
+            if (p == 1 || time < best) best = time, s.splits = p;
+        }
+    }
     auto bytes = [&]() -> size_t { return s.splits > 1 ? partials_bytes(total_rows * Hq, hd, s.splits) : 0; };
     while (num_splits <= 0 && s.splits > 1 && (bytes() > room || units * s.splits > WQ_MOST_GROUPS_256 / 2 || total_rows * Hq > 4 * WQ_MOST_GROUPS_256)) s.splits--;
     s.bytes = bytes();
