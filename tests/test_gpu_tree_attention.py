@@ -342,3 +342,34 @@ def test_on_a_stream_in_a_graph():
             q.mul_(-1)
             torch.cuda.synchronize()
         assert ctx.device_status() == 0
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_many_sequences(dtype):
+    rng = np.random.default_rng(11)
+    lens = [(int(rng.integers(0, 40)), int(rng.integers(0, 70)), 0, int(rng.integers(0, 9))) for _ in range(150)]
+    _check(lens, [int(x) for x in rng.integers(0, 4, 150)], (7, 1, 64), 32, dtype)
+    _check(lens, [int(x) for x in rng.integers(0, 30, 150)], (7, 1, 64), 32, dtype, None, hints=False)
+
+
+def test_calls_on_two_streams_at_once():
+    """A context and a workspace each; what both give is what one after the other gives."""
+    rng = np.random.default_rng(12)
+    kv, _ = R.make_cache(rng, [(900, 700, 300, 60), (64, 0, 33, 5)], 4, 128, 64, torch.bfloat16)
+    sets = []
+    for n in (6, 40):
+        q, k, v = _inputs(rng, 2 * n, (28, 4, 128), torch.bfloat16)
+        ctx = W.Context(W.tree_workspace_bytes(2 * n, 2, 28, 4, 128, 2000, n))
+        sets.append((ctx, q, k, v, R.i32([0, n, 2 * n]), R.i32(T.random_tree(rng, n) + T.random_tree(rng, n)), n, torch.cuda.Stream()))
+    call = lambda s, out=None: W.wq_tree_attention(s[0], s[1], s[2], s[3], kv, s[4], 0.0884, s[5], s[6], 2000, out=out)      # noqa: E731
+    want = [call(s) for s in sets]
+    torch.cuda.synchronize()
+    outs = [torch.empty_like(w) for w in want]
+    for s in sets:
+        s[0].set_stream(s[-1])
+    for _ in range(10):
+        for s, out in zip(sets, outs):
+            call(s, out)
+    torch.cuda.synchronize()
+    for out, w, s in zip(outs, want, sets):
+        assert torch.equal(out, w) and s[0].device_status() == 0
