@@ -57,7 +57,7 @@ struct Unseen {
 
 // QT, G: see walk_cache; G > 0 also for bf16, where log-sum-exps are asked for
 template <typename QT, int HD, int G>
-__global__ __launch_bounds__(256, 2) void k_tree_tiles(TreeArgs a)
+__global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_tree_tiles(TreeArgs a)
 {
     constexpr int BYTES = TILE_BYTES<F16, HD>, R = 128, TK = 64;
     __shared__ __align__(16) char s_k[2 * BYTES], s_v[2 * BYTES], s_m[G > 0 ? 2 * 64 * 4 * G : 16];

@@ -60,8 +60,10 @@ def _check(lens, rows, heads, group, dtype, parents="random", splits=0, front=0,
     out = torch.full((total, Hq, hd), 77.0, dtype=dtype, device="cuda")
     lse = torch.full((total, Hq), 77.0, device="cuda")
     assert W.wq_tree_attention(ctx, q, k, v, kv, R.i32(off), sm, parent, most, longest, splits, out, lse) is out
+    alone = torch.full_like(out, 77.0)                       # without lse: other kernels for bf16
+    W.wq_tree_attention(ctx, q, k, v, kv, R.i32(off), sm, parent, most, longest, splits, alone)
     assert ctx.device_status() == 0
-    for x in (out, lse):
+    for x in (out, lse, alone):
         assert bool((x[:front] == 77).all()) and bool((x[off[-1]:] == 77).all())
     num = den = 0.0
     for b, n in enumerate(rows):
@@ -70,8 +72,9 @@ def _check(lens, rows, heads, group, dtype, parents="random", splits=0, front=0,
         s = slice(off[b], off[b + 1])
         kk, vv = (torch.cat([c, x[s].double().cpu()]) for c, x in zip(cached[b], (k, v)))
         sees = torch.cat([torch.ones(n, cached[b][0].shape[0], dtype=torch.bool), T.seen(None if parents is None else parents[b], n)], 1)
-        e, d = _compare(out[s], lse[s], q[s], kk, vv, sees, sm, dtype)
-        num, den = num + e, den + d
+        for got in (out, alone):
+            e, d = _compare(got[s], lse[s], q[s], kk, vv, sees, sm, dtype)
+            num, den = num + e, den + d
     # roundings are independent: their common size is well below the worst case.  Output and weights at u (rms u / sqrt 3 each), values at 2^-11, a
     # logit of deviation 2 by 2^-11 of its terms
     if dtype != torch.float32 and spread_q == 1.0:
