@@ -422,7 +422,8 @@ size_t wq_shared_workspace_bytes(int B, int P, int Hq, int Hkv, int hd, int64_t 
  * rows: those behind become zeros, their lse -infinity, and WQ_DEV_TOO_MANY_ROWS is raised; a chain may be as long as it likes.
  * max_rows (with parents at most 1024): host bound on one sequence's new rows, 0: not known (the host then counts more workgroups than there is work for, which
  * takes up to a tenth longer).  Rows of a sequence behind it become zeros as above.  max_cache_tokens: host bound on one sequence's cached tokens, used for the
- * number of parts (any value gives the same result to rounding).  num_splits: workgroups that share the keys of a tile of query rows, 1 .. 64, or 0 = automatic.
+ * number of parts (any value gives the same result to rounding).  num_splits: workgroups that share the keys of a tile of query rows, 1 .. 64 (fp32
+ * with up to 640 query rows of a sequence under a KV head: more than 32 are as 32), or 0 = automatic.
  * Arithmetic as in wq_decode_attention_shared; for bf16 with lse the codes of packed keys enter the products as they are, as for fp16 (keys rounded to
  * 16 bits would show in the lse).  The new rows' keys and values enter as they are (fp32 too, where the cache will hold them in fp16).
  * Values of the new rows must be finite (those that a row does not see meet a weight of zero), and as small as for prompts.

@@ -239,6 +239,7 @@ constexpr int WQ_MAX_TREE = 1024;      // rows of a tree: what a workgroup keeps
 struct WqTreePlan {
     int rows, splits;                                             // query rows of a workgroup; parts of every row's keys
     int columns;                                                  // of 16 query rows: every wavefront brings its own keys; 0: tiles of keys for a workgroup
+    bool few;                                                     // fp32: tiles of 32 rows, whose keys are halved once more (two parts of every split)
     int tiles;                                                    // of query rows, of every sequence; 0: not known
     int longest;                                                  // blocks of 32 keys of the longest sequence: shorter ones have fewer parts; 0: all have the same
     size_t bytes;                                                 // workspace

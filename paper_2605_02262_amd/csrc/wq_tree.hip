@@ -4,7 +4,7 @@
 // in one pass over the keys; what several workgroups have of a row's sums is brought to a common ref and added (k_tree_join).
 // 16-bit types: by the rows that a sequence has under a KV head.  Up to 48 (and 49 to 64 as two tiles): wq_tree_stream.hip, near the cache's bytes for few;
 // more: wq_tree_tiles.hip, bound by the vector instructions that expand codes and form weights.  Here: who gets what, the join, and fp32, whose products have a
-// ninth of the 16-bit rate (3 trees of 7 rows over 144 tokens 13.4 us, of that two launches 9).
+// ninth of the 16-bit rate (3 trees of 7 rows over 144 tokens 11.7 us, of that two launches 9).
 #include "wq_tree.h"
 
 namespace {
@@ -100,6 +100,128 @@ __global__ __launch_bounds__(64 * WAVES<F32>, 2) void k_tree(TreeArgs a)
             for (int ct = 0; ct < HD / 16; ct++) r.o[ct][c] = f4{0.f, 0.f, 0.f, 0.f};
         }
     if (any) store_rows<F32, HD>(r, p, a.rep, a.Hq, kvh, wave, split, a.splits > 1 ? a.splits : 0, {a.out, a.lse, a.part, a.part_ml});
+}
+
+// fp32, in tiles of 32 rows: the four wavefronts take 16 rows and 16 of a tile's 32 keys each, and leave a part for the merge for each half of the keys.  Bound by the
+// matrix cores: 28 rows are all one wavefront's in k_tree, and with heads of 128 that one keeps 97 of its registers in scratch, this one none (154).
+template <int HD>
+__global__ __launch_bounds__(256, 2) void k_tree_few(TreeArgs a)
+{
+    constexpr int BYTES = TILE_BYTES<F32, HD>, R = 32, TK = KEYS<F32>, ST = STEPS<F32, HD>;
+    __shared__ __align__(16) char s_k[BYTES], s_v[BYTES];
+    __shared__ uint64_t s_seen[(R + 1) * WORDS];
+    __shared__ int32_t s_parent[WQ_MAX_TREE];
+    const int Hkv = a.kv.Hkv, wave = this_wave(), lane = threadIdx.x & 63, j = lane >> 4, half = wave >> 1;
+    const wq_packed_kv& kv = a.kv;
+    const int unit = (int)blockIdx.x % a.units, split = (int)blockIdx.x / a.units, kvh = unit % Hkv;
+    Place p;
+    if (!find_place<R>(a.row_off, a.B, a.rep, a.total, unit / Hkv, p)) return;
+    const int node0 = p.row0 / a.rep;
+    if (p.rows / a.rep > a.most && p.row0 == 0 && threadIdx.x == 0) atomicOr(a.status, WQ_DEV_TOO_MANY_ROWS);
+    const int last_row = (p.row0 + R < p.rows ? p.row0 + R : p.rows) - 1;
+    int tiles[4], len[4], newest = last_row / a.rep + 1;       // (no row sees one behind itself)
+    if (newest > a.most) newest = a.most;
+    const int cached = tiles_of_cache<TK>(kv, p.seq, len, tiles), all = cached + (newest + TK - 1) / TK;
+    const int lo = (int)((int64_t)split * all / a.splits), hi = (int)((int64_t)(split + 1) * all / a.splits);
+    const int row = p.row0 + 16 * (wave & 1) + (lane & 15);
+    const char* row_at = row < p.rows ? a.q + (p.first + row / a.rep) * a.q_stride + (kvh * a.rep + row % a.rep) * (HD * 4) : nullptr;
+    const bool any = p.row0 + 16 * (wave & 1) < p.rows;
+
+    f4 o[HD / 16];
+    float ref = -INFINITY, sum = 0.f;
+    QueryRows<F32, HD, 1> q;
+#pragma unroll
+    for (int ct = 0; ct < HD / 16; ct++) o[ct] = f4{0.f, 0.f, 0.f, 0.f};
+    // The staged tile's keys from key0 on, of which the row sees those that sees() says
+    auto attend = [&](int key0, auto sees) __attribute__((always_inline)) {
+        if (!any) return;
+        f4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int st = 0; st < ST; st++) s = product<F32>(((Lds4)s_k)[(half * ST + st) * 64 + lane], q[0][st], s);
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+            if (!sees(key0 + 16 * half + 4 * j + i)) s[i] = -INFINITY;
+        const float most = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])) * a.scale;
+        if (__ballot(most > ref + SLACK)) {
+            const float to = fmaxf(ref, max_of_column(most)), by = to == ref ? 1.f : __builtin_amdgcn_exp2f(ref - to);
+            ref = to;
+            sum *= by;
+#pragma unroll
+            for (int ct = 0; ct < HD / 16; ct++) o[ct] *= by;
+        }
+        const float shift = ref == -INFINITY ? 0.f : -ref;
+        u4 w;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const float x = __builtin_amdgcn_exp2f(fmaf(s[i], a.scale, shift));
+            sum += x;
+            w[i] = __float_as_uint(x);
+        }
+#pragma unroll
+        for (int ct = 0; ct < HD / 16; ct++) o[ct] = product<F32>(((Lds4)s_v)[(half * (HD / 16) + ct) * 64 + lane], w, o[ct]);
+    };
+    int done = 0;
+    auto walk_class = [&](auto bits) __attribute__((always_inline)) {
+        constexpr int BITS = decltype(bits)::value, c = BITS == 2 ? 0 : (BITS == 4 ? 1 : 2);
+        const int t0 = lo > done ? lo - done : 0, t1 = hi - done < tiles[c] ? hi - done : tiles[c];
+        done += tiles[c];
+        if (t0 >= t1) return;
+        PackedKeys<HD, BITS, 32> keys(kv, kvh, kv.cls_off[c][p.seq], 0);
+        PackedValues<HD, BITS, 32> values(kv, kvh, kv.cls_off[c][p.seq], 0);
+        const bool brings_keys = wave < 2;
+        auto load = [&](int t) {
+            if (brings_keys) keys.load(t);
+            else values.load(t);
+        };
+        load(t0);
+        load_query_quarter<F32, HD>(q, 0, row_at);
+        for (int t = t0; t < t1; t++) {
+            __syncthreads();                                   // (the tile before has been read)
+            if (brings_keys) keys.stage_f32((Lds4)s_k);
+            else values.stage_f32((Lds4)s_v);
+            __syncthreads();
+            if (t + 1 < t1) load(t + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            attend(t * TK, [&](int key) { return key < len[c]; });
+        }
+    };
+    walk_class(std::integral_constant<int, 2>());
+    walk_class(std::integral_constant<int, 4>());
+    walk_class(std::integral_constant<int, 8>());
+    if (hi > done && lo < hi) {
+        load_query<F32, HD>(q, 0, row_at);
+        const int64_t row0 = kv.off16[p.seq], stride = (int64_t)Hkv * HD * 2;
+        const char* k16 = static_cast<const char*>(kv.k16) + row0 * stride + kvh * (HD * 2);
+        const char* v16 = static_cast<const char*>(kv.v16) + row0 * stride + kvh * (HD * 2);
+        for (int t = lo > done ? lo - done : 0; t < tiles[3] && t < hi - done; t++) {
+            const int key0 = t * TK;
+            __syncthreads();
+            stage_rows<F16, HD>(k16 + key0 * stride, v16 + key0 * stride, stride, stride, len[3] - key0, (Lds4)s_k, (Lds4)s_v);
+            __syncthreads();
+            attend(key0, [&](int key) { return key < len[3]; });
+        }
+    }
+    if (hi > cached && lo < hi) {
+        if (a.parent) find_ancestors(a.parent + p.first, node0, last_row / a.rep + 1 - node0, s_seen, s_parent, 256);
+        const int limit = row < p.rows ? row / a.rep + 1 : 0;
+        const uint64_t* seen = s_seen + (row <= last_row ? row / a.rep - node0 : 0) * WORDS;
+        const char* k = a.k + p.first * a.k_stride + kvh * (HD * 4);
+        const char* v = a.v + p.first * a.v_stride + kvh * (HD * 4);
+        for (int t = lo > cached ? lo - cached : 0; t < hi - cached; t++) {
+            const int key0 = t * TK;
+            __syncthreads();
+            stage_rows<F32, HD>(k + key0 * a.k_stride, v + key0 * a.v_stride, a.k_stride, a.v_stride, newest - key0, (Lds4)s_k, (Lds4)s_v);
+            __syncthreads();
+            attend(key0, [&](int key) { return a.parent ? (seen[key >> 6] >> (key & 63) & 1) != 0 : key < limit; });
+        }
+    }
+    sum = sum_of_column(sum);
+    if (row >= p.rows) return;
+    const bool refused = row / a.rep >= a.most;                // as if it saw nothing
+    const int64_t slot = ((p.first + row / a.rep) * a.Hq + kvh * a.rep + row % a.rep) * (2 * a.splits) + 2 * split + half;
+#pragma unroll
+    for (int ct = 0; ct < HD / 16; ct++) *reinterpret_cast<f4*>(a.part + slot * HD + 16 * ct + 4 * j) = refused ? f4{0.f, 0.f, 0.f, 0.f} : o[ct];
+    if (j == 0) a.part_ml[2 * slot] = refused ? -INFINITY : ref, a.part_ml[2 * slot + 1] = refused ? 0.f : sum;
 }
 
 // The pieces of units that are cut: a wavefront per row; a row's pieces are read by halves of it in turn.  A launch of its own: with the last workgroup of a unit
@@ -207,28 +329,37 @@ WqTreePlan wq_tree_plan(int64_t total_rows, int B, int Hq, int Hkv, int hd, int 
         while (num_splits <= 0 && s.splits > 1 && (s.bytes > room || s.groups > WQ_MOST_GROUPS_256 / 2 || s.units * (s.rows / 4) > WQ_MOST_GROUPS_256)) s.splits--, size();
         return s;
     }
-    s.rows = ROWS<F32>;
-    const int64_t units = tiles_of(total_rows, rep, B, s.rows) * Hkv;
-    s.splits = num_splits > 0 ? num_splits : 1;
-    if (num_splits <= 0) {
-        // Rounds as above, in steps of 32 keys.  A workgroup whose sequences have few rows multiplies with some of its wavefronts only, and shares its unit at little
-        // cost (us of 30 x 18700 tokens, 4 rows of 7 heads for each of 4 KV heads of 128: 1288 in 2 parts, 240 workgroups; 681 in 4; 700 in 8; 629 in 24)
-        const int64_t blocks = (max_cache_tokens + 31) / 32 + ((int64_t)max_rows + 31) / 32;
-        const int most = hd == 128 ? 2 : 3;
-        const double real = units_of(s.rows), active = fmin(4.0, ceil(mean * rep / 32)) / 4, slower = 1 + 0.7 * active;
-        double best = 0;
-        for (int p = 1; p <= WQ_MAX_ATTEND_SPLITS && p <= (blocks < 4 ? 1 : blocks); p++) {
-            const double groups = real * p, rounds = ceil(groups / (256 * most)), share = fmin(most, ceil(groups / 256));
-            const double time = rounds * (ceil((double)blocks / p) * pow(slower, share - 1) + 3) + (p > 1 ? 2 + p * 0.1 : 0);
-            if (p == 1 || time < best) best = time, s.splits = p;
+    // fp32: rounds as above, in steps of 32 keys of k_tree with a unit for itself; a workgroup of it whose sequences have few rows multiplies with some of its wavefronts
+    // only, and shares the unit at little cost.  k_tree_few where a sequence has up to 640 rows under a KV head, on the average, and its keys are cut anyway (us, beside
+    // k_tree, 4 KV heads of 128: 28 rows over 30 x 18700 tokens 371, 686; 8 x 6500 tokens, 91 rows 185, 215, 280 rows 360, 418, 1400 rows as long; 2 heads of 64,
+    // 8 x 6800 tokens: 140 rows 92, 96, 2100 rows 670, 578)
+    auto fit = [&](bool few) {
+        WqTreePlan x = {};
+        x.few = few, x.rows = few ? 32 : ROWS<F32>;
+        x.units = tiles_of(total_rows, rep, B, x.rows) * Hkv;
+        const int top = few ? WQ_MAX_ATTEND_SPLITS / 2 : WQ_MAX_ATTEND_SPLITS;      // (a lane of the merge for every part)
+        x.splits = num_splits > 0 ? (num_splits < top ? num_splits : top) : 1;
+        if (num_splits <= 0) {
+            const int64_t blocks = (max_cache_tokens + 31) / 32 + ((int64_t)max_rows + 31) / 32;
+            const int most = few ? (hd == 128 ? 3 : 5) : (hd == 128 ? 2 : 3);
+            const double real = units_of(x.rows), active = fmin(4.0, ceil(mean * rep / 32)) / 4, slower = 1 + 0.7 * active;
+            constexpr double SHARED[6] = {0.6, 0.6, 0.8, 0.9, 1.05, 1.25};
+            double best = 0;
+            for (int p = 1; p <= top && p <= (blocks < 4 ? 1 : blocks); p++) {
+                const double groups = real * p, rounds = ceil(groups / (256 * most)), share = fmin(most, ceil(groups / 256));
+                const double time = rounds * (ceil((double)blocks / p) * (few ? SHARED[(int)share] : pow(slower, share - 1)) + 3) + (p > 1 ? 2 + p * 0.1 : 0);
+                if (p == 1 || time < best) best = time, x.splits = p;
+            }
         }
-    }
-    auto bytes = [&]() -> size_t { return s.splits > 1 ? partials_bytes(total_rows * Hq, hd, s.splits) : 0; };
-    while (num_splits <= 0 && s.splits > 1 && (bytes() > room || units * s.splits > WQ_MOST_GROUPS_256 / 2 || total_rows * Hq > 4 * WQ_MOST_GROUPS_256)) s.splits--;
-    s.bytes = bytes();
-    s.units = units;
-    s.groups = units * s.splits;
-    return s;
+        auto bytes = [&]() -> size_t { return x.splits > 1 ? partials_bytes(total_rows * Hq, hd, x.splits * (few ? 2 : 1)) : 0; };
+        while (num_splits <= 0 && x.splits > 1 && (bytes() > room || x.units * x.splits > WQ_MOST_GROUPS_256 / 2 || total_rows * Hq > 4 * WQ_MOST_GROUPS_256)) x.splits--;
+        x.bytes = bytes();
+        x.groups = x.units * x.splits;
+        return x;
+    };
+    if (mean * rep <= 640)
+        if (const WqTreePlan x = fit(true); x.splits > 1) return x;
+    return fit(false);
 }
 
 int wq_launch_tree(wq_ctx* ctx, const WqTree& f)
@@ -248,7 +379,8 @@ int wq_launch_tree(wq_ctx* ctx, const WqTree& f)
     a.kv = *f.kv;
     a.out = f.out, a.lse = f.lse;
     a.part = reinterpret_cast<float*>(ctx->ws + WQ_WS_HEADER);
-    a.part_ml = a.part + f.total_rows * f.Hq * a.splits * hd;
+    const int parts = a.splits * (f.plan.few ? 2 : 1);
+    a.part_ml = a.part + f.total_rows * f.Hq * parts * hd;
     if (f.plan.columns) {
         a.longest = f.plan.longest;
         a.tiles = f.plan.tiles;
@@ -265,9 +397,9 @@ int wq_launch_tree(wq_ctx* ctx, const WqTree& f)
         WQ_HIP_CHECK(ctx, hipGetLastError());
         return WQ_OK;
     }
-    hipLaunchKernelGGL(hd == 128 ? k_tree<128> : k_tree<64>, dim3((unsigned)f.plan.groups), dim3(64 * WAVES<F32>), 0, ctx->stream, a);
+    hipLaunchKernelGGL(f.plan.few ? (hd == 128 ? k_tree_few<128> : k_tree_few<64>) : (hd == 128 ? k_tree<128> : k_tree<64>), dim3((unsigned)f.plan.groups), dim3(64 * WAVES<F32>), 0, ctx->stream, a);
     if (a.splits > 1) {
-        const MergeArgs m = {f.total_rows * f.Hq, f.Hq, a.splits, f.dtype, f.row_off, f.B, {a.out, a.lse, a.part, a.part_ml}};
+        const MergeArgs m = {f.total_rows * f.Hq, f.Hq, parts, f.dtype, f.row_off, f.B, {a.out, a.lse, a.part, a.part_ml}};
         hipLaunchKernelGGL(hd == 128 ? k_merge<128> : k_merge<64>, dim3((unsigned)((m.rows + 3) / 4)), dim3(256), 0, ctx->stream, m);
     }
     WQ_HIP_CHECK(ctx, hipGetLastError());
