@@ -598,10 +598,12 @@ size_t wq_tree_workspace_bytes(int64_t total_rows, int B, int Hq, int Hkv, int h
 {
     if (total_rows <= 0 || B <= 0 || Hq <= 0 || Hkv <= 0 || hd <= 0 || Hq % Hkv != 0) return WQ_WS_HEADER;
     size_t most = 0;
-    for (const int dtype : {WQ_F32, WQ_BF16}) {
-        const size_t bytes = wq_tree_plan(total_rows, B, Hq, Hkv, hd, dtype, max_cache_tokens, 0, max_rows, num_splits).bytes;
-        most = bytes > most ? bytes : most;
-    }
+    max_cache_tokens = max_cache_tokens < int64_t(1) << 40 ? max_cache_tokens : int64_t(1) << 40;
+    for (const int dtype : {WQ_F32, WQ_BF16})
+        for (int quarters = 1; quarters <= 4; quarters++) {    // (of the longest sequence's length, on the average: a ragged batch has more parts)
+            const size_t bytes = wq_tree_plan(total_rows, B, Hq, Hkv, hd, dtype, max_cache_tokens, B * max_cache_tokens / 4 * quarters, max_rows, num_splits).bytes;
+            most = bytes > most ? bytes : most;
+        }
     return WQ_WS_HEADER + most;
 }
 

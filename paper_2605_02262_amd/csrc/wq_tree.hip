@@ -307,14 +307,15 @@ WqTreePlan wq_tree_plan(int64_t total_rows, int B, int Hq, int Hkv, int hd, int 
             // Rounds of the workgroups that the card holds at a time: `most` a compute unit, as its registers and LDS have it.  In steps of a workgroup that has a
             // unit for itself (1.2 us: a tile of 64 keys, or a block of 32 of every wavefront): a piece's steps, which take longer where workgroups share a unit, its
             // start and end; the join's launch and what the pieces leave in memory for it.  (us of 8 x 12800 tokens, 4 rows of 7 heads for each of 4 KV heads: 34 in 8
-            // pieces, a workgroup a unit; 35 in 12; 32 in 16, two a unit; 38 in 20)
+            // pieces, a workgroup a unit; 35 in 12; 32 in 16, two a unit; 38 in 20.  Where lengths differ, blocks of wavefronts fill in for each other, half a round lost
+            // at the end: 32 chains 107 in 3, 110 in 4, 103 in 6, 95 in 8)
             const bool tiles = s.columns > WQ_STREAM_COLUMNS;
             const int most = hd == 128 ? (s.columns == 1 ? 3 : 2) : (s.columns == 1 ? 4 : s.columns == WQ_STREAM_COLUMNS ? 2 : 3);
             constexpr double SLOWER[5] = {1, 1, 1.5, 2.1, 3};
             double best = 0;
             s.splits = 1;
             for (int p = 1; p <= WQ_MAX_ATTEND_SPLITS && p <= (blocks < 4 ? 1 : blocks); p++) {
-                const double groups = real * (average < 0.95 ? fmin(p, p * average + 0.5) : p), rounds = ceil(groups / (256 * most));
+                const double groups = real * (average < 0.95 ? fmin(p, p * average + 0.5) : p), rounds = average < 0.95 && !tiles ? fmax(1.0, groups / (256 * most) + 0.5) : ceil(groups / (256 * most));
                 const double steps = ceil((double)blocks / p / (tiles ? 1 : WQ_STREAM_WAVES)) * SLOWER[(int)fmin(most, ceil(groups / 256))];
                 const double time = rounds * (steps + (tiles ? 5 : 6)) + (p > 1 ? 4 + groups * s.rows * hd * 4 / 6.6e6 : 0);
                 if (p == 1 || time < best) best = time, s.splits = p;
