@@ -3,7 +3,7 @@
 // by a workgroup cost barriers and a way through LDS.  Here a wavefront's codes go from memory to registers, are expanded there into the products' operands and never
 // leave; the four of a workgroup take blocks in turn and put their sums together at the end.  A block of 32 tokens is 450 instructions for one column, 580 for two,
 // 720 for three (bf16, heads of 128; products of codes as they are 600 for two), so one column is near memory; two and three are bound by
-// those instructions, one behind the other in the two wavefronts that a SIMD has registers for (2.1 us for a block each, vector unit 41 % active).
+// those instructions, one behind the other in the two wavefronts that a SIMD has registers for (2.1 us for a block each, vector unit 48 % active).
 // us of 8 sequences of 12800 tokens, 28 + 4 heads of 128 (91 MB, 17.5 at a copy's rate): one row 25.4, 4 rows 31.0, 6 rows 36.7; a workgroup of the last: starts
 // within 7 us, tables and queries 5, walk 15 to 20 (5 TB/s while it lasts), sums together 3; join 5.  Tiles shared by the workgroup: 28 (one row), 41 (6 rows).
 #include "wq_tree.h"
