@@ -601,7 +601,7 @@ size_t wq_tree_workspace_bytes(int64_t total_rows, int B, int Hq, int Hkv, int h
     max_cache_tokens = max_cache_tokens < int64_t(1) << 40 ? max_cache_tokens : int64_t(1) << 40;
     for (const int dtype : {WQ_F32, WQ_BF16})
         for (int quarters = 1; quarters <= 4; quarters++) {    // (of the longest sequence's length, on the average: a ragged batch has more parts)
-            const size_t bytes = wq_tree_plan(total_rows, B, Hq, Hkv, hd, dtype, max_cache_tokens, B * max_cache_tokens / 4 * quarters, max_rows, num_splits).bytes;
+            const size_t bytes = wq_tree_plan(total_rows, B, Hq, Hkv, hd, dtype, max_cache_tokens, (B < 65536 ? B : 65535) * max_cache_tokens / 4 * quarters, max_rows, num_splits).bytes;
             most = bytes > most ? bytes : most;
         }
     return WQ_WS_HEADER + most;

@@ -61,7 +61,7 @@ def test_tree_attention_without_rows(W, ctx):  # noqa: F811
 def test_tree_workspace_bytes(W):  # noqa: F811
     f = W.tree_workspace_bytes
     assert f(0, 1, 14, 2, 64, 1000, 10) == f(10, 0, 14, 2, 64, 1000, 10) == f(10, 1, 15, 2, 64, 1000, 10) == 16384
-    assert f(10, 1, 14, 2, 64, 1000, 10, 1) == 16384
+    assert f(10, 1, 14, 2, 64, 1000, 10, 1) == 16384 and f(10, (1 << 31) - 1, 14, 2, 64, (1 << 63) - 1, 10, 1) == 16384
     assert f(10, 1, 14, 2, 64, 1000, 10, 4) >= 16384 + 10 * 14 * 4 * 66 * 4
     assert f(10, 1, 14, 2, 64, 10 ** 6, 10) > f(10, 1, 14, 2, 64, 1000, 10, 1)
 
