@@ -1019,127 +1019,112 @@ __device__ __forceinline__ void store_rows(const Rows<HD>& r, const Place& p, in
 template <typename CT, bool SPLIT = false> constexpr int ROWS = std::is_same_v<CT, F32> || SPLIT ? 128 : 256;       // of a workgroup
 
 // ---- a sequence's packed cache, a workgroup's part of it ------------------------------------------------------------------
-// The tokens of the four segments, and the tiles of TK tokens that they make
-template <int TK>
-__device__ __forceinline__ int tiles_of_cache(const wq_packed_kv& kv, int seq, int (&len)[4], int (&tiles)[4])
-{
-    int all = 0;
-#pragma unroll
-    for (int c = 0; c < 4; c++) {
-        const int64_t room = c < 3 ? kv.cap[c] - kv.cls_off[c][seq] : kv.cap16 - kv.off16[seq];
-        len[c] = c < 3 ? kv.cls_len[c][seq] : kv.len16[seq];
-        if (len[c] > room) len[c] = (int)room;
-        tiles[c] = len[c] > 0 ? (len[c] + TK - 1) / TK : 0;
-        all += tiles[c];
-    }
-    return all;
-}
-
-// Tiles lo .. hi-1, the classes one after the other, for the wavefront's rows at row_at (NULL: no row).  TREE: hi may lie behind the cache's last
-// tile, and 16-bit types' wavefronts work together.
+// Tiles t0 .. t1-1 of the class of BITS bits, for the wavefront's rows at row_at (NULL: no row).
 // QT: the query's type; G as in walk_packed (fp16: the cache's groups per head; else 0); packed tokens are walked in fp16 (fp32 for fp32 queries), 16-bit rows in the
-// cache's own type.  fp32 with heads of 128 needs 17 registers more than there are (scratch): 16 requests over 5000 tokens 40 us, in fp16 27.
+// cache's own type.  TREE: 16-bit types' wavefronts work together.  fp32 with heads of 128 needs 17 registers more than there are (scratch): 16 requests over 5000 tokens
+// 40 us, in fp16 27.
 template <typename QT> using Walked = std::conditional_t<std::is_same_v<QT, F32>, F32, F16>;
-template <typename QT, int HD, int G, bool TREE>
-__device__ __forceinline__ void walk_cache(Rows<HD>& r, Query<Walked<QT>, HD>& q, const char* const (&row_at)[COLS], float scale, const wq_packed_kv& kv, int seq, int kvh,
-                                           const int (&len)[4], const int (&tiles)[4], int lo, int hi, bool any, Lds s_k, Lds s_v, Lds s_m)
+template <typename QT, int HD, int G, bool TREE, int BITS>
+__device__ __forceinline__ void walk_class(Rows<HD>& r, Query<Walked<QT>, HD>& q, const char* const (&row_at)[COLS], const float& scale, const wq_packed_kv& kv, int seq,
+                                           int kvh, int len, int t0, int t1, bool any, Lds s_k, Lds s_v, Lds s_m)
 {
     using CT = Walked<QT>;
     constexpr bool PIPED = ESIZE<QT> == 2;
-    constexpr int TK = KEYS<QT>;
-    // MODE.FP16_OVFL: an expanded value past fp16's range becomes its largest one.  Matrix products read NaN and infinity as numbers then, too: a
-    // query that is not finite makes its row's scale NaN (below), and rows are walked without
-    constexpr int FP16_OVFL = 1 | 23 << 6;
-    if constexpr (PIPED) __builtin_amdgcn_s_setreg(FP16_OVFL, 1);
+    constexpr int TK = KEYS<QT>, c = BITS == 2 ? 0 : (BITS == 4 ? 1 : 2);
     [[maybe_unused]] float q_sum[COLS][G > 0 ? G : 1];
-    int done = 0;                                              // tiles of the classes before
-    auto walk_class = [&](auto bits) __attribute__((always_inline)) {
-        constexpr int BITS = decltype(bits)::value, c = BITS == 2 ? 0 : (BITS == 4 ? 1 : 2);
-        const int t0 = lo > done ? lo - done : 0, t1 = hi - done < tiles[c] ? hi - done : tiles[c];
-        done += tiles[c];
-        if (t0 >= t1) return;
-        auto prepare = [&]() __attribute__((always_inline)) {
+    auto prepare = [&]() __attribute__((always_inline)) {
 #pragma unroll
-            for (int n = 0; n < COLS; n++) {
-                r.limit[n] = len[c];
-                r.scale[n] = scale;
-                if constexpr (G > 0) load_query_codes<BITS, G, HD>(q, n, row_at[n], q_sum[n]);
-                else load_query_quarter<CT, HD>(q, n, row_at[n]);
-                bool bad = false;
-                if constexpr (PIPED) bad = not_finite<QT, HD>(q, n);
-                // (kept from 0 and infinity: a masked logit, -infinity, times 0 and a logit of 0 times infinity would be NaN.  A scale that small leaves every
-                // logit below 2^-100; with one that large logits that differ at all differ by 2^70 or more)
-                if constexpr (std::is_same_v<QT, Bf16>) r.scale[n] = fminf(fmaxf(scale * query_as_f16<HD>(q, n), FLT_MIN), FLT_MAX);
-                if constexpr (std::is_same_v<QT, Bf16> && G > 0) sum_query_codes<G, HD>(q, n, q_sum[n]);
-                if (bad) r.scale[n] = NAN;
-                if constexpr (PIPED && G == 0) order_query<BITS, HD>(q, n);
-            }
-        };
-        if constexpr (!PIPED || !TREE) prepare();
-        if constexpr (PIPED) {
-            const int slots = (len[c] + 31) / 32 * 32;
-            PackedKeys<HD, BITS, 64> keys(kv, kvh, kv.cls_off[c][seq], slots);
-            PackedValues<HD, BITS, 64> values(kv, kvh, kv.cls_off[c][seq], slots);
-            if constexpr (TREE) {                              // the first tile is on its way while the queries are prepared
-                keys.load(t0);
-                values.load(t0);
-                prepare();
-            }
-            walk_packed<HD, BITS, G, TREE>(r, q, q_sum, keys, values, len[c], t0, t1, s_k, s_v, s_m);
-        } else {
-            PackedKeys<HD, BITS, 32> keys(kv, kvh, kv.cls_off[c][seq], 0);
-            PackedValues<HD, BITS, 32> values(kv, kvh, kv.cls_off[c][seq], 0);
-            const bool brings_keys = this_wave() < 2;
-            auto load = [&](int t) {
-                if (brings_keys) keys.load(t);
-                else values.load(t);
-            };
-            __syncthreads();                                   // (whatever was in LDS before has been read)
-            load(t0);
-            for (int t = t0; t < t1; t++) {
-                if (brings_keys) keys.stage_f32((Lds4)s_k);
-                else values.stage_f32((Lds4)s_v);
-                __syncthreads();
-                if (t + 1 < t1) load(t + 1);
-                __builtin_amdgcn_sched_barrier(0);
-                attend_f32<HD>(r, q, (Lds4)s_k, (Lds4)s_v, t * TK, len[c], any ? len[c] : 0);
-                __syncthreads();
-            }
+        for (int n = 0; n < COLS; n++) {
+            r.limit[n] = len;
+            r.scale[n] = scale;
+            if constexpr (G > 0) load_query_codes<BITS, G, HD>(q, n, row_at[n], q_sum[n]);
+            else load_query_quarter<CT, HD>(q, n, row_at[n]);
+            bool bad = false;
+            if constexpr (PIPED) bad = not_finite<QT, HD>(q, n);
+            // (kept from 0 and infinity: a masked logit, -infinity, times 0 and a logit of 0 times infinity would be NaN.  A scale that small leaves every
+            // logit below 2^-100; with one that large logits that differ at all differ by 2^70 or more)
+            if constexpr (std::is_same_v<QT, Bf16>) r.scale[n] = fminf(fmaxf(scale * query_as_f16<HD>(q, n), FLT_MIN), FLT_MAX);
+            if constexpr (std::is_same_v<QT, Bf16> && G > 0) sum_query_codes<G, HD>(q, n, q_sum[n]);
+            if (bad) r.scale[n] = NAN;
+            if constexpr (PIPED && G == 0) order_query<BITS, HD>(q, n);
         }
     };
-    walk_class(std::integral_constant<int, 2>());
-    walk_class(std::integral_constant<int, 4>());
-    walk_class(std::integral_constant<int, 8>());
-    if constexpr (PIPED) __builtin_amdgcn_s_setreg(FP16_OVFL, 0);
-    if constexpr (std::is_same_v<QT, Bf16>) {                  // from the packed tokens' shift to the rows', exact
-#pragma unroll
-        for (int n = 0; n < COLS; n++) {
-            r.sum[n] *= exp2f(SHIFT<QT> - SHIFT<CT>);
-#pragma unroll
-            for (int ct = 0; ct < HD / 16; ct++) r.o[ct][n] *= exp2f(SHIFT<QT> - SHIFT<CT>);
+    if constexpr (!PIPED || !TREE) prepare();
+    if constexpr (PIPED) {
+        const int slots = (len + 31) / 32 * 32;
+        PackedKeys<HD, BITS, 64> keys(kv, kvh, kv.cls_off[c][seq], slots);
+        PackedValues<HD, BITS, 64> values(kv, kvh, kv.cls_off[c][seq], slots);
+        if constexpr (TREE) {                                  // the first tile is on its way while the queries are prepared
+            keys.load(t0);
+            values.load(t0);
+            prepare();
+        }
+        walk_packed<HD, BITS, G, TREE>(r, q, q_sum, keys, values, len, t0, t1, s_k, s_v, s_m);
+    } else {
+        PackedKeys<HD, BITS, 32> keys(kv, kvh, kv.cls_off[c][seq], 0);
+        PackedValues<HD, BITS, 32> values(kv, kvh, kv.cls_off[c][seq], 0);
+        const bool brings_keys = this_wave() < 2;
+        auto load = [&](int t) {
+            if (brings_keys) keys.load(t);
+            else values.load(t);
+        };
+        __syncthreads();                                       // (whatever was in LDS before has been read)
+        load(t0);
+        for (int t = t0; t < t1; t++) {
+            if (brings_keys) keys.stage_f32((Lds4)s_k);
+            else values.stage_f32((Lds4)s_v);
+            __syncthreads();
+            if (t + 1 < t1) load(t + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            attend_f32<HD>(r, q, (Lds4)s_k, (Lds4)s_v, t * TK, len, any ? len : 0);
+            __syncthreads();
         }
     }
-    const int t0 = lo > done ? lo - done : 0, t1 = TREE && hi - done > tiles[3] ? tiles[3] : hi - done;
-    if (TREE ? t0 < t1 : hi > done) {              // (of no rows there would be no last one to read again)
+}
+// ... of the 16-bit rows
+template <typename QT, int HD, bool TREE>
+__device__ __forceinline__ void walk_rows16(Rows<HD>& r, Query<Walked<QT>, HD>& q, const char* const (&row_at)[COLS], const float& scale, const wq_packed_kv& kv, int seq,
+                                            int kvh, int len, int t0, int t1, bool any, Lds s_k, Lds s_v)
+{
+    constexpr int TK = KEYS<QT>;
+#pragma unroll
+    for (int n = 0; n < COLS; n++) {
+        r.limit[n] = len;
+        r.scale[n] = scale;
+        load_query<Walked<QT>, HD>(q, n, row_at[n]);
+    }
+    const int64_t row0 = kv.off16[seq], stride = (int64_t)kv.Hkv * HD * 2;
+    const char* k = static_cast<const char*>(kv.k16) + row0 * stride + kvh * (HD * 2);
+    const char* v = static_cast<const char*>(kv.v16) + row0 * stride + kvh * (HD * 2);
+    if constexpr (ESIZE<QT> == 2) {
+        walk_rows<QT, HD, false, TREE>(r, q, k, v, stride, stride, len, t0, t1, len, s_k, s_v);
+    } else {
+        for (int t = t0; t < t1; t++) {
+            const int key0 = t * TK;
+            __syncthreads();
+            stage_rows<F16, HD>(k + key0 * stride, v + key0 * stride, stride, stride, len - key0, (Lds4)s_k, (Lds4)s_v);
+            __syncthreads();
+            attend_f32<HD>(r, q, (Lds4)s_k, (Lds4)s_v, key0, len, any ? len : 0);
+        }
+    }
+}
+// MODE.FP16_OVFL: an expanded value past fp16's range becomes its largest one.  Matrix products read NaN and infinity as numbers then, too: a query that is not finite
+// makes its row's scale NaN (above), and rows are walked without
+template <typename QT>
+__device__ __forceinline__ void largest_instead_of_infinity(bool on)
+{
+    if constexpr (ESIZE<QT> == 2) on ? __builtin_amdgcn_s_setreg(1 | 23 << 6, 1) : __builtin_amdgcn_s_setreg(1 | 23 << 6, 0);
+}
+// From the packed tokens' shift of the weights to the rows', exact
+template <typename QT, int HD>
+__device__ __forceinline__ void shift_rows(Rows<HD>& r)
+{
+    if constexpr (std::is_same_v<QT, Bf16>) {
 #pragma unroll
         for (int n = 0; n < COLS; n++) {
-            r.limit[n] = len[3];
-            r.scale[n] = scale;
-            load_query<CT, HD>(q, n, row_at[n]);
-        }
-        const int64_t row0 = kv.off16[seq], stride = (int64_t)kv.Hkv * HD * 2;
-        const char* k = static_cast<const char*>(kv.k16) + row0 * stride + kvh * (HD * 2);
-        const char* v = static_cast<const char*>(kv.v16) + row0 * stride + kvh * (HD * 2);
-        if constexpr (PIPED) {
-            walk_rows<QT, HD, false, TREE>(r, q, k, v, stride, stride, len[3], t0, t1, len[3], s_k, s_v);
-        } else {
-            for (int t = t0; t < t1; t++) {
-                const int key0 = t * TK;
-                __syncthreads();
-                stage_rows<F16, HD>(k + key0 * stride, v + key0 * stride, stride, stride, len[3] - key0, (Lds4)s_k, (Lds4)s_v);
-                __syncthreads();
-                attend_f32<HD>(r, q, (Lds4)s_k, (Lds4)s_v, key0, len[3], any ? len[3] : 0);
-            }
+            r.sum[n] *= exp2f(SHIFT<QT> - SHIFT<Walked<QT>>);
+#pragma unroll
+            for (int ct = 0; ct < HD / 16; ct++) r.o[ct][n] *= exp2f(SHIFT<QT> - SHIFT<Walked<QT>>);
         }
     }
 }

@@ -129,8 +129,17 @@ __global__ __launch_bounds__(64 * WAVES<QT>, 2) void k_shared(SharedArgs a)
     const int unit = (int)blockIdx.x % a.units, split = (int)blockIdx.x / a.units, kvh = unit % Hkv;
     Place p;
     if (!find_place<R>(a.req_off, a.P, a.rep, a.B, unit / Hkv, p)) return;
-    int tiles[4], len[4];
-    const int all = tiles_of_cache<TK>(kv, p.seq, len, tiles);
+    // (Both loops over the classes stand here, not in functions like the trees' (wq_tree.h): the compiler keeps 36 more scalars in vector registers then, and with fp32 and heads
+    // of 128 five more registers in scratch.  us, here and there: 64 requests over 51200 tokens 84.5, 85.2; the configuration's tiers 31.8, 32.3; fp32, 64 over 12800: 152, 155)
+    int tiles[4], all = 0, len[4];
+#pragma unroll
+    for (int c = 0; c < 4; c++) {
+        const int64_t room = c < 3 ? kv.cap[c] - kv.cls_off[c][p.seq] : kv.cap16 - kv.off16[p.seq];
+        len[c] = c < 3 ? kv.cls_len[c][p.seq] : kv.len16[p.seq];
+        if (len[c] > room) len[c] = (int)room;
+        tiles[c] = len[c] > 0 ? (len[c] + TK - 1) / TK : 0;
+        all += tiles[c];
+    }
     const int lo = (int)((int64_t)split * all / a.splits), hi = (int)((int64_t)(split + 1) * all / a.splits);
 
     Rows<HD> r;
@@ -143,8 +152,21 @@ __global__ __launch_bounds__(64 * WAVES<QT>, 2) void k_shared(SharedArgs a)
         const int row = wrow0 + 16 * n + (lane & 15);
         row_at[n] = row < p.rows ? a.q + ((p.first + row / a.rep) * a.Hq + kvh * a.rep + row % a.rep) * (HD * ESIZE<QT>) : nullptr;
     }
-    const bool any = wrow0 < p.rows && wave * COLS * 16 < R;   // (fp32: a wavefront without rows only brings tiles; 16-bit types: it keeps its turns, on zeros)
-    walk_cache<QT, HD, G, false>(r, q, row_at, a.scale, kv, p.seq, kvh, len, tiles, lo, hi, any, (Lds)s_k, (Lds)s_v, (Lds)s_m);
+    const bool any = wrow0 < p.rows;   // (fp32: a wavefront without rows only brings tiles; 16-bit types: it keeps its turns, on zeros)
+    int done = 0;                                              // tiles of the classes before
+    auto walk = [&](auto bits) __attribute__((always_inline)) {
+        constexpr int BITS = decltype(bits)::value, c = BITS == 2 ? 0 : (BITS == 4 ? 1 : 2);
+        const int t0 = lo > done ? lo - done : 0, t1 = hi - done < tiles[c] ? hi - done : tiles[c];
+        done += tiles[c];
+        if (t0 < t1) walk_class<QT, HD, G, false, BITS>(r, q, row_at, a.scale, kv, p.seq, kvh, len[c], t0, t1, any, (Lds)s_k, (Lds)s_v, (Lds)s_m);
+    };
+    largest_instead_of_infinity<QT>(true);
+    walk(std::integral_constant<int, 2>());
+    walk(std::integral_constant<int, 4>());
+    walk(std::integral_constant<int, 8>());
+    largest_instead_of_infinity<QT>(false);
+    shift_rows<QT>(r);
+    if (hi > done) walk_rows16<QT, HD, false>(r, q, row_at, a.scale, kv, p.seq, kvh, len[3], lo > done ? lo - done : 0, hi - done, any, (Lds)s_k, (Lds)s_v);
     if (any) store_rows<QT, HD>(r, p, a.rep, a.Hq, kvh, wave, split, a.splits, a.out);
 }
 

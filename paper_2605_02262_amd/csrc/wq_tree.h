@@ -31,6 +31,44 @@ namespace {
 
 constexpr int WORDS = WQ_MAX_TREE / 64;        // of a row's ancestors
 
+// The tokens of the four segments, and the tiles of TK tokens that they make
+template <int TK>
+__device__ __forceinline__ int tiles_of_cache(const wq_packed_kv& kv, int seq, int (&len)[4], int (&tiles)[4])
+{
+    int all = 0;
+#pragma unroll
+    for (int c = 0; c < 4; c++) {
+        const int64_t room = c < 3 ? kv.cap[c] - kv.cls_off[c][seq] : kv.cap16 - kv.off16[seq];
+        len[c] = c < 3 ? kv.cls_len[c][seq] : kv.len16[seq];
+        if (len[c] > room) len[c] = (int)room;
+        tiles[c] = len[c] > 0 ? (len[c] + TK - 1) / TK : 0;
+        all += tiles[c];
+    }
+    return all;
+}
+
+// Tiles lo .. hi-1 of a cache, the classes one after the other; hi may lie behind its last tile
+template <typename QT, int HD, int G>
+__device__ __forceinline__ void walk_cache(Rows<HD>& r, Query<Walked<QT>, HD>& q, const char* const (&row_at)[COLS], float scale, const wq_packed_kv& kv, int seq, int kvh,
+                                           const int (&len)[4], const int (&tiles)[4], int lo, int hi, bool any, Lds s_k, Lds s_v, Lds s_m)
+{
+    int done = 0;                                              // tiles of the classes before
+    auto walk = [&](auto bits) __attribute__((always_inline)) {
+        constexpr int BITS = decltype(bits)::value, c = BITS == 2 ? 0 : (BITS == 4 ? 1 : 2);
+        const int t0 = lo > done ? lo - done : 0, t1 = hi - done < tiles[c] ? hi - done : tiles[c];
+        done += tiles[c];
+        if (t0 < t1) walk_class<QT, HD, G, true, BITS>(r, q, row_at, scale, kv, seq, kvh, len[c], t0, t1, any, s_k, s_v, s_m);
+    };
+    largest_instead_of_infinity<QT>(true);
+    walk(std::integral_constant<int, 2>());
+    walk(std::integral_constant<int, 4>());
+    walk(std::integral_constant<int, 8>());
+    largest_instead_of_infinity<QT>(false);
+    shift_rows<QT>(r);
+    const int t0 = lo > done ? lo - done : 0, t1 = hi - done > tiles[3] ? tiles[3] : hi - done;
+    if (t0 < t1) walk_rows16<QT, HD, true>(r, q, row_at, scale, kv, seq, kvh, len[3], t0, t1, any, s_k, s_v);      // (of no rows there would be no last one to read again)
+}
+
 // Which new rows each of the rows node0 .. node0 + n - 1 sees, a bit each: itself, its parent, its parent's parent ..  (a parent lies in front of its
 // child, so every walk ends).  For all threads of a workgroup.
 __device__ __forceinline__ void find_ancestors(const int32_t* parent, int node0, int n, uint64_t* seen, int32_t* s_parent, int threads)

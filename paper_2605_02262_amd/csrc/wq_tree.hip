@@ -67,7 +67,7 @@ __global__ __launch_bounds__(64 * WAVES<F32>, 2) void k_tree(TreeArgs a)
         row_at[c] = row < p.rows ? a.q + (p.first + row / a.rep) * a.q_stride + (kvh * a.rep + row % a.rep) * (HD * 4) : nullptr;
     }
     const bool any = wrow0 < p.rows && wave * COLS * 16 < R;
-    walk_cache<F32, HD, 0, true>(r, q, row_at, a.scale, kv, p.seq, kvh, len, tiles, lo, hi, any, (Lds)s_k, (Lds)s_v, (Lds)s_k);
+    walk_cache<F32, HD, 0>(r, q, row_at, a.scale, kv, p.seq, kvh, len, tiles, lo, hi, any, (Lds)s_k, (Lds)s_v, (Lds)s_k);
     if (hi > cached && lo < hi) {
         const int t0 = lo > cached ? lo - cached : 0, t1 = hi - cached;
         Unrelated unrelated;
@@ -103,7 +103,7 @@ __global__ __launch_bounds__(64 * WAVES<F32>, 2) void k_tree(TreeArgs a)
 }
 
 // fp32, in tiles of 32 rows: the four wavefronts take 16 rows and 16 of a tile's 32 keys each, and leave a part for the merge for each half of the keys.  Bound by the
-// matrix cores: 28 rows are all one wavefront's in k_tree, and with heads of 128 that one keeps 97 of its registers in scratch, this one none (154).
+// matrix cores: 28 rows are all one wavefront's in k_tree, and with heads of 128 that one keeps 46 of its registers in scratch, this one none (154).
 template <int HD>
 __global__ __launch_bounds__(256, 2) void k_tree_few(TreeArgs a)
 {

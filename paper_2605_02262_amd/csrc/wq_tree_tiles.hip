@@ -92,7 +92,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_tree_tiles(TreeArgs a
         const int row = wrow0 + 16 * n + (lane & 15);
         row_at[n] = row < p.rows ? a.q + (p.first + row / a.rep) * a.q_stride + (kvh * a.rep + row % a.rep) * (HD * 2) : nullptr;
     }
-    walk_cache<QT, HD, G, true>(r, q, row_at, a.scale, kv, p.seq, kvh, s.len, s.blocks, lo, hi, true, (Lds)s_k, (Lds)s_v, (Lds)s_m);
+    walk_cache<QT, HD, G>(r, q, row_at, a.scale, kv, p.seq, kvh, s.len, s.blocks, lo, hi, true, (Lds)s_k, (Lds)s_v, (Lds)s_m);
     const int t0 = lo > cached ? lo - cached : 0, t1 = hi - cached < (newest + TK - 1) / TK ? hi - cached : (newest + TK - 1) / TK;
     if (t0 < t1) {
         int up = node0 + threadIdx.x < WQ_MAX_TREE ? node0 + (int)threadIdx.x : -1;
