@@ -450,7 +450,7 @@ int wq_tree_accept(wq_ctx* ctx, const int32_t* tokens, const int32_t* target, co
  * kv[l]: its cache.  k, v, kv: host arrays of n_layers; the caches agree in B, Hkv, hd and dtype16 and have tables and buffers of their own.
  * Of sequence b's rows row_off[b] .. row_off[b+1]-1 those that take [B, max_take] names (numbered within the sequence, n_take[b] of them, in this
  * order: wq_tree_accept's path and n_path), or all of them in order (take and n_take NULL), become rows off16[b] + len16[b] .. of its 16-bit segment, and
- * len16[b] is raised.  max_take: host bound on a sequence's appended rows.
+ * len16[b] is raised.  max_take: host bound on a sequence's appended rows; with 0 nothing is launched: no row is appended, no table read, no status raised.
  * A sequence is left unchanged in a layer whose segment has no room for all of its rows (WQ_DEV_SEG16_OVERFLOW), and in all layers if it has more than
  * max_take of them (WQ_DEV_TOO_MANY_ROWS) or names one that it does not have (WQ_DEV_BAD_INDEX).  All pointers 16-byte aligned but the tables',
  * rows a multiple of 16 bytes apart; inputs must not overlap the caches.                                                            */

@@ -666,7 +666,7 @@ int wq_append_rows(wq_ctx* ctx, int n_layers, const void* const* k, int64_t k_st
     if (!dtype_ok(dtype)) return wq_fail(ctx, WQ_ERR_ARG, "unknown dtype %d", dtype);
     if (n_layers == 0) return WQ_OK;
     if (!k || !v || !kv) return wq_fail(ctx, WQ_ERR_ARG, "NULL array of layers");
-    if (!take != !n_take) return wq_fail(ctx, WQ_ERR_ARG, "take and n_take go together");
+    if (max_take > 0 && !take != !n_take) return wq_fail(ctx, WQ_ERR_ARG, "take and n_take go together");      // (a table of no columns has no address)
     for (int l = 0; l < n_layers; l++) {
         int rc = check_packed(ctx, kv + l, B, false);
         if (rc != WQ_OK) return rc;
