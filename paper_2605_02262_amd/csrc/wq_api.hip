@@ -674,8 +674,12 @@ int wq_append_rows(wq_ctx* ctx, int n_layers, const void* const* k, int64_t k_st
             return wq_fail(ctx, WQ_ERR_ARG, "the layers' caches differ in Hkv, hd or dtype16");
         if (kv[l].Hkv > MOST_HEADS) return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "more than 2^18 heads");
         if (!on_16_bytes(kv[l].k16) || !on_16_bytes(kv[l].v16)) return wq_fail(ctx, WQ_ERR_ARG, "k16 and v16 must be 16-byte aligned");
-        for (int m = 0; m < l; m++)
-            if (kv[l].len16 == kv[m].len16 || (kv[l].k16 && kv[l].k16 == kv[m].k16)) return wq_fail(ctx, WQ_ERR_ARG, "two layers share a cache");
+        for (int m = 0; m < l; m++) {
+            bool same = kv[l].len16 == kv[m].len16;
+            if (kv[l].cap16 > 0 && kv[m].cap16 > 0)
+                same = same || kv[l].k16 == kv[m].k16 || kv[l].k16 == kv[m].v16 || kv[l].v16 == kv[m].k16 || kv[l].v16 == kv[m].v16;
+            if (same) return wq_fail(ctx, WQ_ERR_ARG, "layers %d and %d share a cache's rows or lengths", m, l);
+        }
         rc = check_rows(ctx, "k", k[l], k_stride, total_rows, kv[l].Hkv, kv[l].hd, dtype);
         if (rc == WQ_OK) rc = check_rows(ctx, "v", v[l], v_stride, total_rows, kv[l].Hkv, kv[l].hd, dtype);
         if (rc != WQ_OK) return rc;
