@@ -534,8 +534,10 @@ def _layers_alike(ctx: Context, name: str, tensors: Sequence[torch.Tensor], like
     stride = _rows(name, first, like, tuple(like.shape))[3]
     if [*map(torch.Tensor.size, tensors)] != [first.shape] * n or [*map(_dtype_of, tensors)] != [like.dtype] * n:
         raise ValueError(f"{name}: shapes or types of the layers' rows differ")
-    if [*map(torch.Tensor.stride, tensors)] != [first.stride()] * n:
-        raise ValueError(f"{name}: the layers' rows are not equally far apart")
+    if [*map(torch.Tensor.stride, tensors)] != [first.stride()] * n:        # (of a dimension of one they say nothing)
+        for t in tensors:
+            if _rows(name, t)[3] != stride and t.shape[0] > 1:
+                raise ValueError(f"{name}: the layers' rows are not equally far apart")
     if [*map(torch.Tensor.get_device, tensors)] != [ctx.index] * n:
         raise ValueError(f"{name}: the context's device, cuda:{ctx.index}, expected")
     return stride

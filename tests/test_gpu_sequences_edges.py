@@ -20,3 +20,15 @@ def test_appending_no_row(selected):
     assert ctx.device_status() == 0
     for kv in kvs:
         assert kv.len16.tolist() == [2, 0] and bool((kv.k16 == 7).all()) and bool((kv.v16 == 9).all())
+
+
+def test_layers_of_one_row_with_strides_of_their_own():
+    x = torch.randn(3, 8, 2, 64, generator=torch.Generator().manual_seed(0)).to(torch.bfloat16).cuda()
+    layers = [x[0, :1], x[1].flatten()[64:].as_strided((1, 2, 64), (1536, 64, 1)), x[2, 4:5]]
+    kvs = _caches(3, 1, 2, 64, torch.bfloat16, [4], [1])
+    ctx = W.Context(0)
+    W.wq_append_rows(ctx, layers, layers[::-1], kvs, R.i32([0, 1]), 1)
+    assert ctx.device_status() == 0
+    for kv, k, v in zip(kvs, layers, layers[::-1]):
+        assert kv.len16.tolist() == [2] and torch.equal(kv.k16[1], k[0]) and torch.equal(kv.v16[1], v[0])
+        assert bool((kv.k16[2:] == 7).all()) and bool((kv.v16[2:] == 9).all())

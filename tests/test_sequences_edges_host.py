@@ -1,5 +1,6 @@
 """Calls for appended rows and copied sequences that the caller may make and that refusals could hit, or miss (no GPU is needed)."""
 import pytest
+import torch
 
 from tests.test_operators_host import W, _desc, ctx  # noqa: F401  (fixtures)
 from tests.test_tree_host import _append, _copy, _other
@@ -90,3 +91,41 @@ def test_copies_may_share_what_they_only_read(W, ctx):  # noqa: F811
     assert W.lib().wq_copy_sequences(ctx, 700, arr(*many), arr(*to), None) == -1 and W.lib().wq_last_error(ctx) == b"from is NULL"
     to[699].meta[2] = to[3].k16
     assert W.lib().wq_copy_sequences(ctx, 700, arr(*many), arr(*to), None) == -1 and b"memory" in W.lib().wq_last_error(ctx)
+
+
+class _Cpu:
+    """A context whose device is the host: a call that the binding lets through ends here."""
+    index, device, handle = -1, torch.device("cpu"), None
+
+    def check(self, rc):
+        raise KeyError("reached the library")
+
+
+def _rows(rows, heads, *strides):
+    """The same rows in layers with these strides."""
+    return [torch.zeros(4096, dtype=torch.bfloat16).as_strided((rows, heads, 64), s) for s in strides]
+
+
+def _append_layers(W, k, v):  # noqa: F811
+    heads = k[0].shape[1]
+    kvs = [W.PackedKV(2, heads, 64, 32, torch.bfloat16, [0, 0, 0], [0, 8, 16], device="cpu") for _ in k]
+    W.wq_append_rows(_Cpu(), k, v, kvs, torch.zeros(3, dtype=torch.int32), 3)
+
+
+def test_strides_that_say_nothing(W):  # noqa: F811
+    """One row, or one head: how far the next would be away differs from layer to layer, and no next one is read."""
+    for k in (_rows(1, 2, (128, 64, 1), (1536, 64, 1), (64, 64, 1)), _rows(5, 1, (128, 64, 1), (128, 128, 1), (128, 7, 1)), _rows(1, 1, (64, 64, 1), (1, 3, 1), (72, 64, 1)),
+              _rows(0, 2, (128, 64, 1), (256, 64, 1), (0, 0, 1))):
+        for a, b in ((k, k), (k, [k[0]] * 3), ([k[1]] * 3, k)):
+            with pytest.raises(KeyError):
+                _append_layers(W, a, b)
+
+
+def test_strides_that_differ(W):  # noqa: F811
+    plain = _rows(2, 2, (128, 64, 1)) * 2
+    for k in (_rows(2, 2, (128, 64, 1), (192, 64, 1)), _rows(2, 1, (128, 64, 1), (192, 64, 1)), _rows(1, 2, (128, 64, 1), (128, 128, 1)), _rows(2, 2, (128, 64, 1), (64, 128, 1)),
+              _rows(2, 2, (128, 64, 1), (256, 64, 2))):
+        same = plain if k[0].shape == plain[0].shape else [k[0], k[0]]
+        for a, b in ((k, same), (same, k)):
+            with pytest.raises(ValueError):
+                _append_layers(W, a, b)
