@@ -107,8 +107,8 @@ typedef enum { WQ_DECODE_AUTO = 0, WQ_DECODE_GENERIC = 1, WQ_DECODE_MFMA = 2 } w
                                   * wq_validate_assignment; the windows beyond the bound were left out                  */
 #define WQ_DEV_BAD_ASSIGNMENT 32u /* wq_validate_assignment: perm is not a permutation of a sequence's windows, or its four
                                   * class counts do not add up to the number of its windows                             */
-#define WQ_DEV_TOO_MANY_ROWS 64u /* a sequence has more new rows than the call can take: wq_tree_attention with parents (1024), wq_tree_accept
-                                  * (max_rows), wq_append_rows (max_take); what becomes of it stands there                  */
+#define WQ_DEV_TOO_MANY_ROWS 64u /* a sequence has more new rows than the call can take: wq_tree_attention (max_rows; with parents 1024 at most),
+                                  * wq_tree_accept (max_rows), wq_append_rows (max_take); what becomes of it stands there      */
 #define WQ_DEV_BAD_INDEX 128u    /* wq_append_rows: a row outside its sequence, or a negative number of them; wq_copy_sequences: a sequence
                                   * outside the source                                                                  */
 #define WQ_DEV_APPEND_TIMEOUT 4u /* wq_decode_append_attention: the workgroup that raises len16[b] gave up waiting (4 s) for
@@ -451,7 +451,8 @@ int wq_tree_accept(wq_ctx* ctx, const int32_t* tokens, const int32_t* target, co
  * Of sequence b's rows row_off[b] .. row_off[b+1]-1 those that take [B, max_take] names (numbered within the sequence, n_take[b] of them, in this
  * order: wq_tree_accept's path and n_path), or all of them in order (take and n_take NULL), become rows off16[b] + len16[b] .. of its 16-bit segment, and
  * len16[b] is raised.  max_take: host bound on a sequence's appended rows; with 0 nothing is launched: no row is appended, no table read, no status raised.
- * A sequence is left unchanged in a layer whose segment has no room for all of its rows (WQ_DEV_SEG16_OVERFLOW), and in all layers if it has more than
+ * A sequence is left unchanged in a layer whose segment has no room for all of its rows (WQ_DEV_SEG16_OVERFLOW; other layers have them then, and the lengths
+ * differ: equal segments in all layers keep them together), and in all layers if it has more than
  * max_take of them (WQ_DEV_TOO_MANY_ROWS) or names one that it does not have (WQ_DEV_BAD_INDEX).  All pointers 16-byte aligned but the tables',
  * rows a multiple of 16 bytes apart; inputs must not overlap the caches.                                                            */
 int wq_append_rows(wq_ctx* ctx, int n_layers, const void* const* k, int64_t k_stride, const void* const* v, int64_t v_stride, int dtype, int B, const int32_t* row_off,

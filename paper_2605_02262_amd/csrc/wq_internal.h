@@ -238,10 +238,10 @@ int wq_launch_shared(wq_ctx* ctx, const WqShared& f);
 constexpr int WQ_MAX_TREE = 1024;      // rows of a tree: what a workgroup keeps of it in LDS
 struct WqTreePlan {
     int rows, splits;                                             // query rows of a workgroup; parts of every row's keys
-    int columns;                                                  // of 16 query rows: every wavefront brings its own keys; 0: tiles of keys for a workgroup
+    int columns;                                                  // of 16 query rows; up to WQ_STREAM_COLUMNS every wavefront brings its own keys, more (8): a workgroup's tiles; 0: fp32
     bool few;                                                     // fp32: tiles of 32 rows, whose keys are halved once more (two parts of every split)
     int tiles;                                                    // of query rows, of every sequence; 0: not known
-    int longest;                                                  // blocks of 32 keys of the longest sequence: shorter ones have fewer parts; 0: all have the same
+    int longest;                                                  // blocks of keys (32; 64 for 8 columns) of the longest sequence: shorter ones have fewer parts; 0: all have the same
     size_t bytes;                                                 // workspace
     int64_t units, groups;                                        // tiles of query rows times KV heads; workgroups
 };

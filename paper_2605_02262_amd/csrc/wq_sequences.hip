@@ -9,7 +9,7 @@ namespace {
 __device__ __forceinline__ int64_t clipped(int64_t x, int64_t most) { return x < 0 ? 0 : (x > most ? most : x); }
 
 // ---- wq_tree_accept ----------------------------------------------------------------------------------------------------
-// Bound by its start and three memory round trips (2.9 us of 8 sequences, 3.7 of 512).  A workgroup per sequence.  Every row looks whether its parent's choice is its token, the first such row of a parent is its child, and one
+// Bound by its start and three memory round trips (3.1 us of 8 sequences, 3.5 of 512).  A workgroup per sequence.  Every row looks whether its parent's choice is its token, the first such row of a parent is its child, and one
 // lane follows the children from row 0.
 __global__ __launch_bounds__(256) void k_accept(WqAccept a, uint32_t* status)
 {

@@ -1,4 +1,4 @@
-// What the two kernels of wq_tree_attention share: their arguments, and who sees whom in a tree.
+// What the kernels of wq_tree_attention share: their arguments, a packed cache's walk, who sees whom in a tree, who does what.
 #pragma once
 #include "wq_attend.h"
 

@@ -3,8 +3,11 @@
 //     out = sum_j w_j v_j / sum_j w_j,   w_j = 2^(scale q.k_j - ref),   ref a running reference of the row, lse = ln 2 (ref + log2 sum_j w_j)
 // in one pass over the keys; what several workgroups have of a row's sums is brought to a common ref and added (k_tree_join).
 // 16-bit types: by the rows that a sequence has under a KV head.  Up to 48 (and 49 to 64 as two tiles): wq_tree_stream.hip, near the cache's bytes for few;
-// more: wq_tree_tiles.hip, bound by the vector instructions that expand codes and form weights.  Here: who gets what, the join, and fp32, whose products have a
-// ninth of the 16-bit rate (3 trees of 7 rows over 144 tokens 11.7 us, of that two launches 9).
+// more: wq_tree_tiles.hip, bound by products and the vector instructions that expand codes and form weights, one after the other.  Here: who gets what, the join, and
+// fp32, whose products have a ninth of the 16-bit rate (3 trees of 7 rows over 144 tokens 11.7 us, of that two launches 9).
+// Roundings of 16-bit queries: weights to the values' type and packed values to fp16, which the products take, and without lse packed keys for bf16; references, sums of
+// weights, numerators, parts and their join stay fp32.  A result is off by 1.7e-3 in bf16 (its own rounding alone: as much) and 2.6e-4 in fp16 (2.1e-4).  Weights in
+// two parts of 16 bits would be half as many products again, a fifth of a tile's time.
 #include "wq_tree.h"
 
 namespace {
@@ -288,8 +291,10 @@ WqTreePlan wq_tree_plan(int64_t total_rows, int B, int Hq, int Hkv, int hd, int 
         return n * used * Hkv;
     };
     if (dtype != WQ_F32) {
-        // Columns of a sequence, on the average.  Up to three: every wavefront brings its own keys; four in two tiles (us of 8 x 56 rows over 12800 tokens, 4 KV heads of
-        // 128: 62, in a tile of 128 rows 73); more (and five: 74, 75) in tiles of 128 rows
+        // Columns of a sequence, on the average.  Up to three: every wavefront brings its own keys; four in two tiles; more in tiles of 128 rows.  us of four columns in
+        // tiles of 32 rows, of 128: 28 + 4 heads of 128, 8 sequences of 12800 tokens 40, 46, 32 of 4200 50, 60, 4 of 50400 62, 73 (fp16 75, 83), one of 12800 23.8, 23.2;
+        // 32 + 8 of 128 64, 75, 79, 104, 115, 127; 14 + 2 of 64 21, 25, 24, 30, 29, 34.  Of five, 8 x 12800: 53, 48 (32 + 8 heads: 94, 76); one sequence 22.8, 24.8, and heads of 64
+        // 25.0, 27.8 would be better off in tiles of 32
         const int64_t columns = ((total_rows + used - 1) / used * rep + 15) / 16;
         s.columns = (int)(columns <= WQ_STREAM_COLUMNS ? columns : columns == 4 ? 2 : 8);
         s.rows = 16 * s.columns;
@@ -305,8 +310,8 @@ WqTreePlan wq_tree_plan(int64_t total_rows, int B, int Hq, int Hkv, int hd, int 
             s.splits = num_splits;
         } else {
             // Rounds of the workgroups that the card holds at a time: `most` a compute unit, as its registers and LDS have it.  In steps of a workgroup that has a
-            // unit for itself (1.2 us: a tile of 64 keys, or a block of 32 of every wavefront): a piece's steps, which take longer where workgroups share a unit, its
-            // start and end; the join's launch and what the pieces leave in memory for it.  (us of 8 x 12800 tokens, 4 rows of 7 heads for each of 4 KV heads: 34 in 8
+            // unit for itself (1.2 us: a tile of 64 keys, or a block of 32 of every wavefront): a piece's steps, which take longer where workgroups share a unit (SLOWER), its
+            // start and end; the join's launch and what the pieces leave in memory for it (6.6e6 bytes a step: 5.5 TB/s).  (us of 8 x 12800 tokens, 4 rows of 7 heads for each of 4 KV heads: 34 in 8
             // pieces, a workgroup a unit; 35 in 12; 32 in 16, two a unit; 38 in 20.  Where lengths differ, blocks of wavefronts fill in for each other, half a round lost
             // at the end: 32 chains 107 in 3, 110 in 4, 103 in 6, 95 in 8)
             const bool tiles = s.columns > WQ_STREAM_COLUMNS;
@@ -332,8 +337,9 @@ WqTreePlan wq_tree_plan(int64_t total_rows, int B, int Hq, int Hkv, int hd, int 
     }
     // fp32: rounds as above, in steps of 32 keys of k_tree with a unit for itself; a workgroup of it whose sequences have few rows multiplies with some of its wavefronts
     // only, and shares the unit at little cost.  k_tree_few where a sequence has up to 640 rows under a KV head, on the average, and its keys are cut anyway (us, beside
-    // k_tree, 4 KV heads of 128: 28 rows over 30 x 18700 tokens 371, 686; 8 x 6500 tokens, 91 rows 185, 215, 280 rows 360, 418, 1400 rows as long; 2 heads of 64,
-    // 8 x 6800 tokens: 140 rows 92, 96, 2100 rows 670, 578)
+    // k_tree, 4 KV heads of 128: 28 rows over 30 x 18700 tokens 450, 802; 8 x 6500 tokens, 91 rows 186, 208, 280 rows 356, 401, 420 rows 524, 492, 595 rows 731, 641, 637 rows
+    // 758, 952, 1400 rows as long; 2 heads of 64, 8 x 6800 tokens: 140 rows 89, 90, 630 rows 259, 271, 2100 rows 668, 581; 8 heads of 64 with a query head each, 300 rows
+    // 460, 486; 8 of 128 with four, 600 rows 1375, 1257.  Between 400 and 640 either may be the faster one)
     auto fit = [&](bool few) {
         WqTreePlan x = {};
         x.few = few, x.rows = few ? 32 : ROWS<F32>;

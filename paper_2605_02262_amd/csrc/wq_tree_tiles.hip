@@ -1,8 +1,9 @@
 // wq_tree_attention for 16-bit types and many rows: a workgroup's four wavefronts, 32 rows each, expand every tile of 64 keys together.
-// A tile's codes are expanded once for 128 rows and read by all four from LDS (two buffers: the next tile is expanded behind this one's products).  Bound by vector
-// instructions: 382 of a wavefront and tile beside 63 matrix instructions (vector unit 57 % active, matrix cores busy 35 %, no bank conflicts, 2.08 GHz), so two
-// workgroups share a compute unit and their phases mix: 64 rows of 4 sequences of 50688 tokens, 28 + 4 heads of 128, 247 us (floor 136); one workgroup of 256 rows
-// in two groups that take turns, as in wq_attend.hip, 315.  16 rows of 8 sequences of 12800 tokens 55 us: 32 us of tiles, 5 of start, 10 until the last
+// A tile's codes are expanded once for 128 rows and read by all four from LDS (two buffers: the next tile is expanded between this one's products of keys and its
+// weights).  Bound by matrix and vector phases one after the other: a wavefront and tile are 64 matrix instructions of 16 cycles and 318 vector instructions of 4, and
+// two wavefronts share a SIMD, whose phases overlap only by chance.  Of the cycles (no bank conflicts, 2.08 GHz) the matrix cores are busy in 38 %, the vector unit in 61 %,
+// its issue of the matrix instructions among them (9 %).  64 rows of 4 sequences of 50688 tokens, 28 + 4 heads of 128: 247 us (floor 136); one workgroup of 256
+// rows in two groups that take turns, as in wq_attend.hip, 315.  16 rows of 8 sequences of 12800 tokens 55 us: 32 us of tiles, 5 of start, 10 until the last
 // workgroup starts, join 7.
 #include "wq_tree.h"
 
