@@ -465,7 +465,7 @@ int wq_append_rows(wq_ctx* ctx, int n_layers, const void* const* k, int64_t k_st
  * room of every 16-bit segment) is the caller's.  A sequence that does not fit a class (WQ_DEV_CLASS_OVERFLOW) or its 16-bit segment
  * (WQ_DEV_SEG16_OVERFLOW), or whose from[d] is outside -1 .. src->B-1 (WQ_DEV_BAD_INDEX), becomes empty; it keeps its place in the classes as far as
  * they reach.  All caches: the same Hkv, hd, group and dtype16; all of src the same B, all of dst too; buffers 16-byte aligned; a dst shares no
- * memory with any src or other dst (off16, which is only read, apart).                                                              */
+ * memory with any src or other dst, but off16, which is only read, and cls_off and cls_len with other dsts whose sequences have the same lengths.      */
 int wq_copy_sequences(wq_ctx* ctx, int n_layers, const wq_packed_kv* src, const wq_packed_kv* dst, const int32_t* from);
 
 #ifdef __cplusplus

@@ -1,4 +1,5 @@
 """Appended rows and copied sequences at the ends of what a call may ask for."""
+import numpy as np
 import pytest
 import torch
 
@@ -32,3 +33,24 @@ def test_layers_of_one_row_with_strides_of_their_own():
     for kv, k, v in zip(kvs, layers, layers[::-1]):
         assert kv.len16.tolist() == [2] and torch.equal(kv.k16[1], k[0]) and torch.equal(kv.v16[1], v[0])
         assert bool((kv.k16[2:] == 7).all()) and bool((kv.v16[2:] == 9).all())
+
+
+def test_copied_layers_that_share_the_classes_tables():
+    """Layers whose sequences have the same lengths, as one choice of bits for all of them gives."""
+    lens, src = [(100, 64, 33, 20), (0, 40, 0, 3), (7, 0, 90, 0)], [2, 0, 0, 1]
+    from_kv = [R.make_cache(np.random.default_rng(i), lens, 2, 64, 32, torch.bfloat16)[0] for i in range(3)]
+    caps, room = [sum(-(-lens[s][c] // 32) * 32 for s in src) for c in range(3)], R.offsets([lens[s][3] for s in src])
+    alone, shared = ([W.PackedKV(4, 2, 64, 32, torch.bfloat16, caps, room, fill=0) for _ in range(3)] for _ in range(2))
+    for kv in shared[1:]:
+        kv.cls_off, kv.cls_len = shared[0].cls_off, shared[0].cls_len
+        for c in range(3):
+            kv.desc.cls_off[c], kv.desc.cls_len[c] = kv.cls_off[c].data_ptr(), kv.cls_len[c].data_ptr()
+    ctx = W.Context(0)
+    for to in (alone, shared):
+        W.wq_copy_sequences(ctx, from_kv, to, R.i32(src))
+    assert ctx.device_status() == 0
+    for a, b in zip(alone, shared):
+        for c in range(3):
+            for x, y in ((a.codes, b.codes), (a.meta, b.meta), (a.cls_off, b.cls_off), (a.cls_len, b.cls_len)):
+                assert torch.equal(x[c], y[c])
+        assert torch.equal(a.k16, b.k16) and torch.equal(a.v16, b.v16) and torch.equal(a.len16, b.len16) and torch.equal(a.v_scale_max[:4], b.v_scale_max[:4])

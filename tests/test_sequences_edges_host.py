@@ -44,6 +44,7 @@ def _apart(W, at, layer):  # noqa: F811
 
 
 BUFFERS = ["codes", "meta", "cls_off", "cls_len", "k16", "v16", "len16", "v_scale_max"]
+TABLES = BUFFERS[2:4]
 
 
 def _get(d, name):
@@ -72,15 +73,20 @@ def test_copies_that_share_memory(W, ctx, mine, other):  # noqa: F811
         kept = _get(b, other)
         _set(b, other, _get(a, mine))
         code, why = call()
-        assert code == -1 and b"memory" in why, (mine, other)
+        if a in dst and mine in TABLES and other in TABLES:              # (tables that are written alike)
+            assert why == b"from is NULL"
+        else:
+            assert code == -1 and b"memory" in why, (mine, other)
         _set(b, other, kept)
     assert call() == (-1, b"from is NULL")
 
 
-def test_copies_may_share_what_they_only_read(W, ctx):  # noqa: F811
+def test_copies_may_share_what_they_read_or_write_alike(W, ctx):  # noqa: F811
     src, dst = ([_apart(W, at, i) for i in range(3)] for at in (0x10000000, 0x20000000))
     dst[0].off16 = dst[1].off16 = src[0].off16 = src[2].off16            # where the 16-bit segments lie
     src[1] = src[0]                                                      # one source for two layers
+    for c in range(3):                                                   # layers of the same lengths
+        dst[1].cls_off[c], dst[1].cls_len[c] = dst[0].cls_off[c], dst[0].cls_len[c]
     for d in dst:                                                        # buffers of no tokens
         d.cap[0] = d.cap16 = 0
         d.codes[0], d.meta[0], d.k16, d.v16 = src[0].codes[0], src[0].meta[0], src[0].k16, src[0].v16
